@@ -83,6 +83,8 @@ extern "C" {
                                 /* gradient described in Sec. 3.1)                                */
 #define AERO_BF16 0
 #define AERO_FP32 1
+#define AERO_NO_TOKEN (-1)      /* token id that stands for no token (embedding calls, teacher lists);       */
+                                /* any other id outside [0,V) raises AERO_ST_BAD_TARGET and is taken for it  */
 
 #define AERO_CAT_ZERO    0      /* categories of Appendix C, threshold tau = 0.5, decided on      */
 #define AERO_CAT_PARTIAL 1      /* integers: Partial iff 0 < c and 2c < n                         */
@@ -498,6 +500,68 @@ size_t aero_allocate_workspace_bytes(int32_t P);
 int aero_allocate_sim(aero_ctx* ctx, const aero_cfg* cfg, const aero_alloc_cfg* ac, int32_t P, const uint32_t* thr,
                       int32_t* n_gen, int32_t* c, int32_t* n_train, int64_t* counters,
                       void* workspace, size_t workspace_bytes);
+
+/* ------------------------------------------------------------------------------
+ * Around stage (b): the operators next to the lm_head in a training step.  (No passage of the
+ * paper: they are the ends of the policy model that stage (b) is called from, and the lm_head
+ * product a frozen policy is scored with.)  They take plain [T,d] rows -- no group structure --
+ * of the type cfg->dtype names; only that field of cfg is read.
+ *
+ * Final RMS norm, per row t:
+ *   s = x + residual   (residual NULL: s = x)
+ *   rstd = 1 / sqrt(mean_k s_k^2 + eps),   h_k = s_k rstd gamma_k
+ *   8-bit form: q_scale = max_k |h_k| / 127,  q_k = round(h_k / q_scale)   (a row of zeros: scale 0)
+ * s, the statistics and h are fp32 until each output is rounded once.  A row that holds a NaN or an
+ * infinity gets a NaN (or infinite) q_scale, so that its values are not taken for numbers.
+ *   aero_rmsnorm_fwd: x, residual [T,d], gamma [d] (cfg->dtype) -> any of sum [T,d] (s), h [T,d]
+ *     (cfg->dtype), rstd [T] f32, q [T,d] i8 with q_scale [T] f32; an output that is NULL is not
+ *     written (q and q_scale only together).  eps > 0.
+ *   aero_rmsnorm_bwd: with shat = s rstd,
+ *       dx = rstd (gamma dh - shat mean_k(gamma dh shat)) + dsum        (the gradient of x and of residual)
+ *       dgamma (+)= sum_t dh shat                                       (fixed order: same bits each call)
+ *     dh, dsum (gradient that reaches s by the residual stream; NULL: none), s [T,d], gamma [d],
+ *     rstd [T] -> dx [T,d], dgamma [d] f32, overwritten or, when accumulate_dgamma != 0, added to.
+ *     workspace: at least aero_rmsnorm_workspace_bytes(T, d) bytes, 256-byte aligned.
+ *   aero_quantize_rows: the 8-bit form of rows x [T,d] as they are (e.g. of W, once per weight).
+ * An output may be the same array as an input of its shape and type; other overlaps are not allowed.
+ * d up to 16384, any d and any element-aligned base (16-byte aligned rows are faster).
+ */
+int aero_rmsnorm_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, const void* x, const void* residual,
+                     const void* gamma, float eps, void* sum, void* h, float* rstd, int8_t* q, float* q_scale);
+
+size_t aero_rmsnorm_workspace_bytes(int64_t T, int32_t d);
+
+int aero_rmsnorm_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, const void* dh, const void* dsum,
+                     const void* s, const void* gamma, const float* rstd, void* dx, float* dgamma, int accumulate_dgamma,
+                     void* workspace, size_t workspace_bytes);
+
+int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, const void* x, int8_t* q, float* q_scale);
+
+/* The embedding with W [V,d] (cfg->dtype), the lm_head weight when the two are tied:
+ *   aero_embed_fwd:  X[t,:] = scale W[y_t,:]          (rounded once; y_t = AERO_NO_TOKEN: zeros)
+ *   aero_embed_bwd:  dW[v,:] (+)= scale sum_{t: y_t = v} dX[t,:]
+ * dW [V,d] f32 is overwritten or, when accumulate_dW != 0, added to -- with tied weights the dW of
+ * stage (b).  The rows of one token are added in an order that depends on y alone, without atomics:
+ * repeated calls give the same bits.  y [T] i32.  d up to 65536, any element-aligned base.
+ * workspace: at least aero_embed_workspace_bytes(T, d) bytes, 256-byte aligned.
+ */
+int aero_embed_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, const int32_t* y, const void* W,
+                   float scale, void* X);
+
+size_t aero_embed_workspace_bytes(int64_t T, int32_t d);
+
+int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, const int32_t* y, const void* dX,
+                   float scale, float* dW, int accumulate_dW, void* workspace, size_t workspace_bytes);
+
+/* The lm_head product in 8-bit integers, with a scale per token and per vocabulary row (the form
+ * aero_rmsnorm_fwd and aero_quantize_rows produce):
+ *   out[t,v] = h_scale[t] w_scale[v] sum_k h8[t,k] w8[v,k]
+ * The sum is exact (32-bit integers); it is multiplied by the two scales in fp32 and rounded once to
+ * out_dtype (AERO_BF16 | AERO_FP32).  h8 [T,d], w8 [V,d] i8 (-128 .. 127), 16-byte aligned bases,
+ * d % 16 == 0, d <= 65536, V <= 2^30; h_scale [T], w_scale [V] f32; out [T,V].
+ */
+int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t* h8, const float* h_scale,
+                   const int8_t* w8, const float* w_scale, int32_t out_dtype, void* out);
 
 /* Optional timing of the dominant kernel.  With timing on, aero_grpo_loss_fwd_bwd records a pair of
  * CUDA events on the context's stream around each launch of its lm_head kernel (up to 256 launches

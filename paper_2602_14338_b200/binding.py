@@ -20,6 +20,7 @@ AERO_STATS_KEPT, AERO_STATS_ALL = 0, 1
 AERO_TOKEN_MEAN, AERO_SEQ_MEAN = 0, 1
 AERO_DENOM_SURVIVING, AERO_DENOM_ALL = 0, 1
 AERO_BF16, AERO_FP32 = 0, 1
+AERO_NO_TOKEN = -1
 AERO_ST_BAD_TARGET, AERO_ST_BAD_OFFSETS, AERO_ST_BAD_REWARD, AERO_ST_EMPTY_ROLLOUT, AERO_ST_TIMEOUT = 1, 2, 4, 8, 16
 AERO_ST_RANGE = 32
 
@@ -33,6 +34,8 @@ EXPORTS = [
     "aero_fwd_bwd_workspace_bytes", "aero_grpo_loss_fwd_bwd", "aero_grpo_loss_kl_fwd_bwd", "aero_grpo_loss_reg_fwd_bwd",
     "aero_enable_kernel_timing", "aero_kernel_timing_ms",
     "aero_set_tuning", "aero_finalize_weights", "aero_selftest_bounded_wait",
+    "aero_rmsnorm_fwd", "aero_rmsnorm_bwd", "aero_rmsnorm_workspace_bytes", "aero_quantize_rows",
+    "aero_embed_fwd", "aero_embed_bwd", "aero_embed_workspace_bytes", "aero_lmhead_q8",
 ]
 
 
@@ -115,6 +118,17 @@ def load_library():
     lib.aero_step_workspace_bytes.argtypes = [i32, i32, i64, i32, i32, i64, i32]
     lib.aero_grpo_step_host.argtypes = ([vp, C.POINTER(AeroCfg), i32, i32, i64, i32, i32] + [vp] * 12 + [C.c_int] +
                                         [vp, vp, vp, vp, sz])
+    cp = C.POINTER(AeroCfg)
+    lib.aero_rmsnorm_fwd.argtypes = [vp, cp, i64, i32, vp, vp, vp, f32] + [vp] * 5
+    lib.aero_rmsnorm_workspace_bytes.restype = sz
+    lib.aero_rmsnorm_workspace_bytes.argtypes = [i64, i32]
+    lib.aero_rmsnorm_bwd.argtypes = [vp, cp, i64, i32] + [vp] * 7 + [C.c_int, vp, sz]
+    lib.aero_quantize_rows.argtypes = [vp, cp, i64, i32] + [vp] * 3
+    lib.aero_embed_fwd.argtypes = [vp, cp, i64, i32, i32, vp, vp, f32, vp]
+    lib.aero_embed_workspace_bytes.restype = sz
+    lib.aero_embed_workspace_bytes.argtypes = [i64, i32]
+    lib.aero_embed_bwd.argtypes = [vp, cp, i64, i32, i32, vp, vp, f32, vp, C.c_int, vp, sz]
+    lib.aero_lmhead_q8.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, i32, vp]
     lib.aero_launch_count.restype = C.c_int64
     lib.aero_launch_count.argtypes = [vp]
     _lib = lib
@@ -456,6 +470,130 @@ class Context:
             workspace.data_ptr(), workspace.numel())
         _check(rc, "aero_grpo_loss_bwd")
         return dH, dW
+
+    # ---- around stage (b): final norm, tied embedding, 8-bit lm_head ------------------------
+    def _arg(self, t, dtype, shape, name):
+        """Data pointer of a tensor that must be on this context's device, contiguous, of this type and shape."""
+        if t is None:
+            return None
+        if tuple(t.shape) != tuple(shape):
+            raise AeroError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        if t.dtype != dtype:
+            raise AeroError(f"{name} must have dtype {dtype}, got {t.dtype}")
+        if t.device != self.device:
+            raise AeroError(f"{name} must be on {self.device}, got {t.device}")
+        if not t.is_contiguous():
+            raise AeroError(f"{name} must be contiguous")
+        return t.data_ptr()
+
+    def _new(self, shape, dtype):
+        """An output tensor allocated for the context's stream, where the kernels that write it run."""
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _scratch(self, nbytes):
+        """A workspace of its own for one call, allocated for the context's stream: the allocator hands the
+        memory on in that stream's order only, and under graph capture it comes from the graph's pool, so
+        two graphs, or a graph and later calls, never share one."""
+        return self._new(max(int(nbytes), 256), torch.uint8)
+
+    def rmsnorm_fwd(self, cfg, x, gamma, residual=None, eps=1e-6, h=True, quant=False, out=None):
+        """aero_rmsnorm_fwd: returns a dict with rstd, sum (when a residual is given), h (unless h=False) and,
+        with quant=True, q (int8) and q_scale.  `out` may hold any of these tensors already; out["sum"] or
+        out["h"] may be x or residual itself."""
+        T, d = x.shape
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        o = dict(out) if out is not None else {}
+        want = [("rstd", (T,), torch.float32)]
+        if residual is not None or "sum" in o:
+            want.append(("sum", (T, d), dt))
+        if h:
+            want.append(("h", (T, d), dt))
+        if quant:
+            want += [("q", (T, d), torch.int8), ("q_scale", (T,), torch.float32)]
+        ptr = {}
+        for name, shape, t in want:
+            if name not in o:
+                o[name] = self._new(shape, t)
+            ptr[name] = self._arg(o[name], t, shape, name)
+        rc = self.lib.aero_rmsnorm_fwd(
+            self.h, C.byref(cfg), T, d, self._arg(x, dt, (T, d), "x"), self._arg(residual, dt, (T, d), "residual"),
+            self._arg(gamma, dt, (d,), "gamma"), eps, ptr.get("sum"), ptr.get("h"), ptr["rstd"], ptr.get("q"),
+            ptr.get("q_scale"))
+        _check(rc, "aero_rmsnorm_fwd")
+        return o
+
+    def rmsnorm_bwd(self, cfg, dh, s, gamma, rstd, dsum=None, dx=None, dgamma=None, accumulate_dgamma=False):
+        """aero_rmsnorm_bwd: returns (dx, dgamma); s and rstd are the forward's sum (x where there was no
+        residual) and rstd."""
+        T, d = s.shape
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        if accumulate_dgamma and dgamma is None:
+            raise AeroError("accumulate_dgamma needs the dgamma to add to")
+        dx = dx if dx is not None else self._new((T, d), dt)
+        dgamma = dgamma if dgamma is not None else self._new((d,), torch.float32)
+        ws = self._scratch(self.lib.aero_rmsnorm_workspace_bytes(T, d))
+        rc = self.lib.aero_rmsnorm_bwd(
+            self.h, C.byref(cfg), T, d, self._arg(dh, dt, (T, d), "dh"), self._arg(dsum, dt, (T, d), "dsum"),
+            self._arg(s, dt, (T, d), "s"), self._arg(gamma, dt, (d,), "gamma"), self._arg(rstd, torch.float32, (T,), "rstd"),
+            self._arg(dx, dt, (T, d), "dx"), self._arg(dgamma, torch.float32, (d,), "dgamma"),
+            1 if accumulate_dgamma else 0, ws.data_ptr(), ws.numel())
+        _check(rc, "aero_rmsnorm_bwd")
+        return dx, dgamma
+
+    def quantize_rows(self, cfg, x, out=None):
+        """aero_quantize_rows: (q int8, q_scale) of the rows of x."""
+        T, d = x.shape
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        q, scale = out if out is not None else (self._new((T, d), torch.int8), self._new((T,), torch.float32))
+        rc = self.lib.aero_quantize_rows(self.h, C.byref(cfg), T, d, self._arg(x, dt, (T, d), "x"),
+                                         self._arg(q, torch.int8, (T, d), "q"),
+                                         self._arg(scale, torch.float32, (T,), "q_scale"))
+        _check(rc, "aero_quantize_rows")
+        return q, scale
+
+    def embed_fwd(self, cfg, W, y, scale=1.0, out=None):
+        """aero_embed_fwd: scale * W[y] (zeros where y is AERO_NO_TOKEN)."""
+        V, d = W.shape
+        T = y.numel()
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        X = out if out is not None else self._new((T, d), dt)
+        rc = self.lib.aero_embed_fwd(self.h, C.byref(cfg), T, d, V, self._arg(y, torch.int32, (T,), "y"),
+                                     self._arg(W, dt, (V, d), "W"), scale, self._arg(X, dt, (T, d), "out"))
+        _check(rc, "aero_embed_fwd")
+        return X
+
+    def embed_bwd(self, cfg, dX, y, V, scale=1.0, dW=None, accumulate_dW=False):
+        """aero_embed_bwd: dW [V,d] f32, the scaled sum of the rows of dX by token (added to a given dW with
+        accumulate_dW=True)."""
+        T, d = dX.shape
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        if accumulate_dW and dW is None:
+            raise AeroError("accumulate_dW needs the dW to add to")
+        dW = dW if dW is not None else self._new((V, d), torch.float32)
+        ws = self._scratch(self.lib.aero_embed_workspace_bytes(T, d))
+        rc = self.lib.aero_embed_bwd(self.h, C.byref(cfg), T, d, V, self._arg(y, torch.int32, (T,), "y"),
+                                     self._arg(dX, dt, (T, d), "dX"), scale,
+                                     self._arg(dW, torch.float32, (V, d), "dW"), 1 if accumulate_dW else 0,
+                                     ws.data_ptr(), ws.numel())
+        _check(rc, "aero_embed_bwd")
+        return dW
+
+    def lmhead_q8(self, h8, h_scale, w8, w_scale, out_dtype=torch.bfloat16, out=None):
+        """aero_lmhead_q8: logits [T,V] of 8-bit rows h8 [T,d] and weights w8 [V,d] with their scales."""
+        T, d = h8.shape
+        V = w8.shape[0]
+        if out_dtype not in (torch.bfloat16, torch.float32):
+            raise AeroError(f"out_dtype must be torch.bfloat16 or torch.float32, got {out_dtype}")
+        o = out if out is not None else self._new((T, V), out_dtype)
+        rc = self.lib.aero_lmhead_q8(self.h, T, d, V, self._arg(h8, torch.int8, (T, d), "h8"),
+                                     self._arg(h_scale, torch.float32, (T,), "h_scale"),
+                                     self._arg(w8, torch.int8, (V, d), "w8"),
+                                     self._arg(w_scale, torch.float32, (V,), "w_scale"),
+                                     AERO_FP32 if out_dtype == torch.float32 else AERO_BF16,
+                                     self._arg(o, out_dtype, (T, V), "out"))
+        _check(rc, "aero_lmhead_q8")
+        return o
 
     # ---- allocation controller, simulated ----------------------------------------------------
     def allocate_sim(self, cfg, acfg, thr, out=None):

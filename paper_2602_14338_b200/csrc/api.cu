@@ -1,30 +1,9 @@
 // C ABI entry points: argument validation, context management and dispatch to the
 // stage launchers.  Nothing here touches array data on the host.
-#include "common.cuh"
+#include "entry.cuh"
 
 #include <new>
 #include <string>
-
-#include <nvtx3/nvToolsExt.h>
-
-namespace {
-
-// NVTX range over one ABI call (visible in Nsight timelines; a no-op without a profiler attached)
-struct Range {
-  explicit Range(const char* name) { nvtxRangePushA(name); }
-  ~Range() { nvtxRangePop(); }
-};
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-bool aligned256(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 255u) == 0; }
-
-int check_ctx(aero_ctx* ctx) {
-  if (!ctx) return AERO_ERR_INVALID;
-  if (cudaSetDevice(ctx->device) != cudaSuccess) return AERO_ERR_CUDA;
-  return AERO_OK;
-}
-
-}  // namespace
 
 extern "C" {
 
@@ -123,7 +102,7 @@ int aero_enable_kernel_timing(aero_ctx* ctx, int on) {
 
 int aero_kernel_timing_ms(aero_ctx* ctx, float* total_ms, int* launches) {
   if (!ctx || !total_ms || !launches) return AERO_ERR_INVALID;
-  int rc = check_ctx(ctx);
+  int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   AERO_CUDA_TRY(cudaStreamSynchronize(ctx->stream));
   float sum = 0.f;
@@ -172,7 +151,7 @@ int aero_set_tuning(aero_ctx* ctx, const char* name, int value) {
 
 int aero_last_status(aero_ctx* ctx, uint32_t* bits) {
   if (!ctx || !bits) return AERO_ERR_INVALID;
-  int rc = check_ctx(ctx);
+  int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   // read and clear in stream order, so that neither can overtake (or be overtaken by) kernels of
   // this context on a stream that does not synchronise with the default stream
@@ -192,16 +171,16 @@ int aero_group_stats(aero_ctx* ctx, const aero_cfg* cfg, int32_t P, int32_t R,
                      float* u_tilde, float* alpha_out, float* beta_out,
                      int32_t* kept_ids, int64_t* kept_tok_off, int64_t* counters,
                      float* metrics, void* workspace, size_t workspace_bytes) {
-  Range nv("aero_group_stats");
+  AeroRange nv("aero_group_stats");
   if (!ctx || !cfg || P < 0 || R < 0) return AERO_ERR_INVALID;
   if (!go || !cs || !kept_tok_off || !counters) return AERO_ERR_INVALID;
   if (R > 0 && (!reward || !adv || !w || !keep || !kept_ids)) return AERO_ERR_INVALID;
   if (P > 0 && (!gmask || !cat || !u_tilde || !alpha_out || !beta_out)) return AERO_ERR_INVALID;
   if ((alpha_in == nullptr) != (beta_in == nullptr)) return AERO_ERR_INVALID;
   if (cfg->k_ratio < 1 || cfg->n_explore < 1 || cfg->rescue_S < 0) return AERO_ERR_INVALID;
-  if (!workspace || !aligned256(workspace)) return AERO_ERR_INVALID;
+  if (!workspace || !aero_aligned256(workspace)) return AERO_ERR_INVALID;
   if (workspace_bytes < aero_group_ws_bytes_impl(P, R)) return AERO_ERR_WORKSPACE;
-  const int rc = check_ctx(ctx);
+  const int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   return aero_group_stats_launch(ctx, cfg, P, R, go, reward, cs, key, keep_in, alpha_in, beta_in,
                                  adv, w, keep, gmask, cat, u_tilde, alpha_out, beta_out,
@@ -210,10 +189,10 @@ int aero_group_stats(aero_ctx* ctx, const aero_cfg* cfg, int32_t P, int32_t R,
 
 int aero_finalize_weights(aero_ctx* ctx, const aero_cfg* cfg, int32_t R, int32_t P_local, int64_t P_global,
                           float* w, const int64_t* counters_local, const int64_t* counters_global) {
-  Range nv("aero_finalize_weights");
+  AeroRange nv("aero_finalize_weights");
   if (!ctx || !cfg || R < 0 || P_local < 0 || P_global < P_local) return AERO_ERR_INVALID;
   if (!counters_local || !counters_global || (R > 0 && !w)) return AERO_ERR_INVALID;
-  const int rc = check_ctx(ctx);
+  const int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   return aero_finalize_weights_launch(ctx, cfg, R, P_local, P_global, w, counters_local, counters_global);
 }
@@ -237,12 +216,12 @@ static int fwd_dispatch(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d
     if (T > 0 && (!old_logp || !g)) return AERO_ERR_INVALID;
     if (R > 0 && (!adv || !w || !keep)) return AERO_ERR_INVALID;
   }
-  if (!workspace || !aligned256(workspace)) return AERO_ERR_INVALID;
+  if (!workspace || !aero_aligned256(workspace)) return AERO_ERR_INVALID;
   if (cfg->dtype != AERO_FP32 && cfg->dtype != AERO_BF16) return AERO_ERR_UNSUPPORTED;
   if (cfg->dtype == AERO_BF16 && d % 64 != 0) return AERO_ERR_UNSUPPORTED;
-  if (cfg->dtype == AERO_BF16 && (!aligned16(H) || !aligned16(W))) return AERO_ERR_INVALID;
+  if (cfg->dtype == AERO_BF16 && (!aero_aligned16(H) || !aero_aligned16(W))) return AERO_ERR_INVALID;
   if (workspace_bytes < aero_fwd_workspace_bytes(T, d, V, R)) return AERO_ERR_WORKSPACE;
-  const int rc = check_ctx(ctx);
+  const int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   if (cfg->dtype == AERO_FP32) {
     return aero_fwd_fp32(ctx, cfg, T, d, V, R, static_cast<const float*>(H), static_cast<const float*>(W),
@@ -257,7 +236,7 @@ int aero_grpo_loss_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
                        const int64_t* cs, const float* adv, const float* w, const uint8_t* keep,
                        float* logp, float* lse, float* g, float* loss, float* metrics,
                        int accumulate, void* workspace, size_t workspace_bytes) {
-  Range nv("aero_grpo_loss_fwd");
+  AeroRange nv("aero_grpo_loss_fwd");
   const aero_fwd_extra ex = {nullptr, 0.f, 0.f, nullptr, 0};
   return fwd_dispatch(ctx, cfg, T, d, V, R, H, W, y, old_logp, cs, adv, w, keep, logp, lse, g, loss, metrics,
                       accumulate, workspace, workspace_bytes, ex);
@@ -269,7 +248,7 @@ int aero_grpo_loss_reg_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_
                            const int64_t* cs, const float* adv, const float* w, const uint8_t* keep,
                            float* logp, float* lse, float* g, float* entropy, float* loss, float* metrics,
                            int accumulate, void* workspace, size_t workspace_bytes) {
-  Range nv("aero_grpo_loss_reg_fwd");
+  AeroRange nv("aero_grpo_loss_reg_fwd");
   if (!cfg) return AERO_ERR_INVALID;
   const aero_fwd_extra ex = {ref_logp, ref_logp ? cfg->kl_beta : 0.f, entropy ? cfg->ent_coef : 0.f, entropy, 0};
   return fwd_dispatch(ctx, cfg, T, d, V, R, H, W, y, old_logp, cs, adv, w, keep, logp, lse, g, loss, metrics,
@@ -280,7 +259,7 @@ int aero_logprob_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, i
                      const void* H, const void* W, const int32_t* y,
                      float* logp, float* lse, float* entropy,
                      void* workspace, size_t workspace_bytes) {
-  Range nv("aero_logprob_fwd");
+  AeroRange nv("aero_logprob_fwd");
   const aero_fwd_extra ex = {nullptr, 0.f, 0.f, entropy, 1};
   return fwd_dispatch(ctx, cfg, T, d, V, 0, H, W, y, nullptr, nullptr, nullptr, nullptr, nullptr, logp, lse, nullptr,
                       nullptr, nullptr, 0, workspace, workspace_bytes, ex);
@@ -298,12 +277,12 @@ int aero_grpo_loss_reg_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, in
                                float* logp, float* lse, float* g, float* entropy, float* loss, float* metrics,
                                float grad_scale, void* dH, float* dW, int accumulate_dW,
                                void* workspace, size_t workspace_bytes) {
-  Range nv("aero_grpo_loss_fwd_bwd");
+  AeroRange nv("aero_grpo_loss_fwd_bwd");
   if (!ctx || !cfg || T < 0 || d <= 0 || V <= 0 || R < 0 || T >= (int64_t)1 << 31) return AERO_ERR_INVALID;
   if (!W || !cs || !loss || !dW) return AERO_ERR_INVALID;
   if (T > 0 && (!H || !y || !old_logp || !logp || !lse || !g || !dH)) return AERO_ERR_INVALID;
   if (R > 0 && (!adv || !w || !keep)) return AERO_ERR_INVALID;
-  if (!workspace || !aligned256(workspace)) return AERO_ERR_INVALID;
+  if (!workspace || !aero_aligned256(workspace)) return AERO_ERR_INVALID;
   if (cfg->dtype == AERO_FP32) {
     int rc = aero_grpo_loss_reg_fwd(ctx, cfg, T, d, V, R, H, W, y, old_logp, ref_logp, cs, adv, w, keep, logp, lse, g,
                                     entropy, loss, metrics, 0, workspace, workspace_bytes);
@@ -316,9 +295,9 @@ int aero_grpo_loss_reg_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, in
   }
   if (cfg->dtype != AERO_BF16) return AERO_ERR_UNSUPPORTED;
   if (d % 64 != 0) return AERO_ERR_UNSUPPORTED;
-  if (!aligned16(H) || !aligned16(W) || !aligned16(dH) || !aligned16(dW)) return AERO_ERR_INVALID;
+  if (!aero_aligned16(H) || !aero_aligned16(W) || !aero_aligned16(dH) || !aero_aligned16(dW)) return AERO_ERR_INVALID;
   if (workspace_bytes < aero_fwd_bwd_ws_bytes_tc(T, d, V, R, 128)) return AERO_ERR_WORKSPACE;
-  const int rc = check_ctx(ctx);
+  const int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   return aero_fwd_bwd_tc(ctx, cfg, T, d, V, R, H, W, y, old_logp, ref_logp, cfg->kl_beta, entropy, cfg->ent_coef, cs, adv, w,
                          keep, logp, lse, g, loss, metrics, grad_scale, dH, dW, accumulate_dW, workspace, workspace_bytes);
@@ -360,17 +339,17 @@ static int bwd_dispatch(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d
   if (T > 0 && (!H || !y || !lse || !g || !dH)) return AERO_ERR_INVALID;
   if (R > 0 && !keep) return AERO_ERR_INVALID;
   if (cfg->dtype == AERO_FP32) {
-    const int rc = check_ctx(ctx);
+    const int rc = aero_check_ctx(ctx);
     if (rc) return rc;
     return aero_bwd_fp32(ctx, cfg, T, d, V, R, static_cast<const float*>(H), static_cast<const float*>(W),
                          y, cs, keep, lse, g, grad_scale, static_cast<float*>(dH), dW, accumulate_dW, ex);
   }
   if (cfg->dtype != AERO_BF16) return AERO_ERR_UNSUPPORTED;
   if (d % 64 != 0) return AERO_ERR_UNSUPPORTED;
-  if (!aligned16(H) || !aligned16(W) || !aligned16(dH) || !aligned16(dW)) return AERO_ERR_INVALID;
-  if (!workspace || !aligned256(workspace)) return AERO_ERR_INVALID;
+  if (!aero_aligned16(H) || !aero_aligned16(W) || !aero_aligned16(dH) || !aero_aligned16(dW)) return AERO_ERR_INVALID;
+  if (!workspace || !aero_aligned256(workspace)) return AERO_ERR_INVALID;
   if (workspace_bytes < aero_bwd_ws_bytes_tc(T, d, V, R, 128)) return AERO_ERR_WORKSPACE;
-  const int rc = check_ctx(ctx);
+  const int rc = aero_check_ctx(ctx);
   if (rc) return rc;
   return aero_bwd_tc(ctx, cfg, T, d, V, R, H, W, y, cs, keep, lse, g, grad_scale, dH, dW, accumulate_dW,
                      workspace, workspace_bytes, ex);
@@ -382,7 +361,7 @@ int aero_grpo_loss_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
                        const float* lse, const float* g, const float* logp, float grad_scale,
                        void* dH, float* dW, int accumulate_dW,
                        void* workspace, size_t workspace_bytes) {
-  Range nv("aero_grpo_loss_bwd");
+  AeroRange nv("aero_grpo_loss_bwd");
   const aero_bwd_extra ex = {nullptr, nullptr, 0.f, logp};
   return bwd_dispatch(ctx, cfg, T, d, V, R, H, W, y, cs, keep, lse, g, grad_scale, dH, dW, accumulate_dW, workspace,
                       workspace_bytes, ex);
@@ -394,7 +373,7 @@ int aero_grpo_loss_reg_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_
                            const float* lse, const float* g, const float* logp, const float* entropy, const float* w,
                            float grad_scale, void* dH, float* dW, int accumulate_dW,
                            void* workspace, size_t workspace_bytes) {
-  Range nv("aero_grpo_loss_reg_bwd");
+  AeroRange nv("aero_grpo_loss_reg_bwd");
   if (!cfg) return AERO_ERR_INVALID;
   if ((entropy == nullptr) != (w == nullptr)) return AERO_ERR_INVALID;
   const aero_bwd_extra ex = {entropy, w, entropy ? cfg->ent_coef : 0.f, logp};
