@@ -127,8 +127,10 @@ static inline int aero_vsplit_cap(int32_t d) {
   const int a = aero_vsplit_auto(d);
   return a > kAeroMaxForcedVsplit ? a : kAeroMaxForcedVsplit;
 }
-static inline int aero_vsplit(const aero_ctx* ctx, int32_t d) {
-  return ctx->tune_vsplit > 0 ? ctx->tune_vsplit : aero_vsplit_auto(d);
+// (never more splits than vocabulary tiles of 256: a split without a tile has no running state to merge)
+static inline int aero_vsplit(const aero_ctx* ctx, int32_t d, int32_t V) {
+  const int s = ctx->tune_vsplit > 0 ? ctx->tune_vsplit : aero_vsplit_auto(d), nvt = (V + 255) / 256;
+  return s < nvt ? s : nvt;
 }
 // Meeting points per unit of the lm_head kernel's producers (0 switches the pacing off).
 static inline int aero_nsync(const aero_ctx* ctx) { return ctx->tune_nsync >= 0 ? ctx->tune_nsync : 32; }

@@ -52,7 +52,10 @@ constexpr int THREADS = 192;
 // bit 0: dz mode, bit 1: entropy term, bit 2: the forward also stores exp(z - c_t) of the chunk (see MODE_FWD_P)
 constexpr int MODE_FWD = 0, MODE_DZ = 1, MODE_FWD_ENT = 2, MODE_DZ_ENT = 3, MODE_FWD_P = 4, MODE_FWD_P_ENT = 6;
 constexpr float kShiftMargin = 40.f;   // c_t = (largest logit of the row's first 32 columns) + this margin
-constexpr float kMasked = -1e30f;   // stands for -inf in columns past V (finite, so that 0 * z stays 0)
+// Stands for -inf in columns past V and in the target's own (finite, so that 0 * z stays 0; a power of two, so that
+// its product with log2(e) is exact and columns that are all masked give exponents of 0, not of rounding noise).
+constexpr float kMasked = -0x1p100f;
+constexpr float kMaskedMax2 = -0x1p99f;   // a running maximum below this (log2 domain) has seen masked columns only
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Ctl {
@@ -152,7 +155,8 @@ __device__ __forceinline__ void finish_rows(const Params& p, bool ent_mode, bool
   double part[kPartialStride] = {0.0, 0.0, 0.0, 0.0, 0.0};
   if (live) {
     float ls, lp, ent = 0.f;
-    if (l > 0.f) {
+    const bool others = l > 0.f && m2 > kMaskedMax2;       // (a vocabulary of one: no other column)
+    if (others) {
       const float a = fmaf(zy, kLog2e, -m2);               // the target's exponent relative to m2
       const float big = fmaxf(a, 0.f);                     // everything below is scaled by 2^-big: no overflow
       const float ey = exp2f(a - big), lr = l * exp2f(-big);
@@ -166,7 +170,7 @@ __device__ __forceinline__ void finish_rows(const Params& p, bool ent_mode, bool
     p.logp[row] = lp;
     p.lse_out[row] = ls;
     if (ent_mode) p.ent_out[row] = ent;
-    if (p.zmax_out != nullptr) p.zmax_out[row] = l > 0.f ? m2 * kLn2 : -INFINITY;
+    if (p.zmax_out != nullptr) p.zmax_out[row] = others ? m2 * kLn2 : -INFINITY;
     if (p.old_logp != nullptr) {
       const int i = aero_owner(p.cs, p.R, row);
       const float old = p.old_logp[row];

@@ -440,7 +440,7 @@ int aero_fwd_bwd_tc(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, in
       AERO_CUDA_TRY(cudaFuncSetAttribute(k_dw2, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)gemmbwd::PSMEM_BYTES));
     }
 
-    const int vs = aero_vsplit(ctx, d);
+    const int vs = aero_vsplit(ctx, d, V);
     const int nvt = (V + lmhead::BN - 1) / lmhead::BN;
     const int n_nt = (d + gemmbwd::BN - 1) / gemmbwd::BN;
     const long long dw_units = (long long)((V + gemmbwd::BM - 1) / gemmbwd::BM) * n_nt;

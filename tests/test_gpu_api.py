@@ -211,3 +211,36 @@ def test_two_prompt_shards_on_one_gpu_equal_the_unsharded_batch(ctx, mode):
     assert TL.rel_l2(dH.float().cpu().numpy()[~edge], rdH[~edge]) < 1e-2
     if not edge.any():
         assert TL.rel_l2(dW.cpu().numpy(), rdW) < 1e-2
+
+
+@pytest.mark.parametrize("d,V", [(64, 1), (64, 2), (64, 33), (2112, 200), (2112, 257)])
+def test_smallest_vocabularies(ctx, d, V):
+    """A vocabulary of one (p = 1, nothing but the target's own column), one of fewer tiles than the kernel has
+    vocabulary splits (d > 2048), and one whose second split holds a single column, also as the target.  Exact:
+    logits of these sizes are off by at most (d/8 + 8) 2^-23 of sum |h w|, far below the path's 1e-2."""
+    rng = np.random.default_rng(d + V)
+    T = 40
+    H = torch.from_numpy(rng.standard_normal((T, d))).to(torch.bfloat16)
+    W = torch.from_numpy(rng.standard_normal((V, d)) * 0.05).to(torch.bfloat16)
+    y = rng.integers(0, V, T).astype(np.int32)
+    y[::3] = V - 1
+    cs, keep = np.array([0, 15, T], np.int64), np.ones(2, np.uint8)
+    adv, w = np.array([1.0, -0.5], np.float32), np.full(2, 1.0 / T, np.float32)
+    Hd, Wd = H.double().numpy(), W.double().numpy()
+    z = O.logits(Hd, Wd)
+    lp, lse = O.log_softmax_pick(z, y)
+    old = (lp - 0.01).astype(np.float32)
+    ref = O.grpo_loss_fwd(O.Cfg(), Hd, Wd, y, old, cs, adv.astype(float), w.astype(float), keep)
+    rdH, rdW = O.grpo_loss_bwd(Hd, Wd, y, cs, keep, ref["lse"], ref["g"])
+    cfg = B.cfg_default()
+    a = (H.cuda(), W.cuda(), TL.dev(y))
+    f = ctx.grpo_loss_fwd(cfg, *a, TL.dev(old), TL.dev(cs), TL.dev(adv), TL.dev(w), TL.dev(keep))
+    dH, dW = ctx.grpo_loss_bwd(cfg, *a, TL.dev(cs), TL.dev(keep), f["lse"], f["g"], logp=f["logp"])
+    f2, dH2, dW2 = ctx.grpo_loss_fwd_bwd(cfg, *a, TL.dev(old), TL.dev(cs), TL.dev(adv), TL.dev(w), TL.dev(keep))
+    for o in (f, f2):
+        assert np.abs(o["logp"].cpu().numpy() - lp).max() <= 1e-2 and np.abs(o["lse"].cpu().numpy() - lse).max() <= 1e-2
+    size = np.linalg.norm(ref["g"]) * np.linalg.norm(Wd)
+    for h, v in ((dH, dW), (dH2, dW2)):
+        assert np.linalg.norm(h.double().cpu().numpy() - rdH) <= 1e-2 * np.linalg.norm(rdH) + 1e-6 * size
+        assert np.linalg.norm(v.double().cpu().numpy() - rdW) <= 1e-2 * np.linalg.norm(rdW) + 1e-6 * np.linalg.norm(ref["g"]) * np.linalg.norm(Hd)
+    assert ctx.last_status() == 0
