@@ -505,7 +505,8 @@ int aero_allocate_sim(aero_ctx* ctx, const aero_cfg* cfg, const aero_alloc_cfg* 
  * Around stage (b): the operators next to the lm_head in a training step.  (No passage of the
  * paper: they are the ends of the policy model that stage (b) is called from, and the lm_head
  * product a frozen policy is scored with.)  They take plain [T,d] rows -- no group structure --
- * of the type cfg->dtype names; only that field of cfg is read.
+ * of the type cfg->dtype names (distillation also the rollouts of stage (b)); only that field of cfg is
+ * read.
  *
  * Final RMS norm, per row t:
  *   s = x + residual   (residual NULL: s = x)
@@ -536,6 +537,57 @@ int aero_rmsnorm_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, c
                      void* workspace, size_t workspace_bytes);
 
 int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, const void* x, int8_t* q, float* q_scale);
+
+/* Distillation from a teacher's top logits through the lm_head: the loss and gradients of stage (b) with a
+ * list of K tokens and teacher logits per row in place of the sampled token.  H, W, cs, w, keep as in
+ * aero_grpo_loss_fwd (w and keep from aero_group_stats, or any token weights).  For every row t of a
+ * kept rollout i:
+ *   q_tk  = exp(logits[t,k] - n_t),   n_t = teacher_lse[t], or log sum_k exp(logits[t,k]) when teacher_lse
+ *           is NULL (the list normalised by itself);   Q_t = sum_k q_tk
+ *   kl_t  = sum_k q_tk (log q_tk - log p_t,ids[t,k]),   p_t = softmax(W h_t)
+ *   loss  = sum_t w_i kl_t
+ *   dz_tv = grad_scale w_i (Q_t p_tv - sum_{k: ids[t,k] = v} q_tk);   dH = dz W,   dW (+)= dz^T H
+ * A list place with id AERO_NO_TOKEN is empty (its logit is not read), any other id outside [0,V) raises
+ * AERO_ST_BAD_TARGET and counts as empty, a logit of -infinity or NaN has q = 0; a row whose list holds no weight
+ * contributes nothing.  A token listed twice counts with the sum of its q.  Rows of dropped rollouts get
+ * lse = kl = 0 and dH = 0.  1 <= K <= 256.
+ * Inputs   ids [T,K] i32, logits [T,K] f32, teacher_lse [T] f32 or NULL.
+ * Outputs  lse, kl [T] f32; loss [1] f32 (overwritten; fixed order of the sums); metrics [4] f32 or NULL: fraction
+ *          of kept tokens whose list holds no weight, mean kl, mean sum_k p_t,ids[t,k], kept tokens; dH [T,d]
+ *          (cfg->dtype); dW [V,d] of type dw_dtype: AERO_FP32 (overwritten, or added to when
+ *          accumulate_dW != 0) or, for bf16 rows, AERO_BF16 (overwritten, rounded once).
+ * Precision as in stage (b): dz is rounded to bf16 before the two products (fp32 accumulation), its listed
+ * entries from fp32 log-probs; the rows of H enter dW as they are.  lse and kl take the first listed token's logit
+ * as an fp32 dot product.  aero_distill_bwd takes lse from the forward and recomputes the logits
+ * (8 d V FLOP per token over the two calls), aero_distill_fwd_bwd does not (6 d V; a row with a logit too far
+ * above its first ones is redone as in aero_grpo_loss_fwd_bwd, AERO_ST_RANGE beyond 1024 per chunk).
+ * workspace: at least the matching *_workspace_bytes, 256-byte aligned; chunk_tokens as in
+ *          aero_bwd_workspace_bytes, and a bf16 dW of rows that do not fit one chunk takes V d floats more.
+ */
+size_t aero_distill_fwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t K);
+
+int aero_distill_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K,
+                     const void* H, const void* W, const int32_t* ids, const float* logits, const float* teacher_lse,
+                     const int64_t* cs, const float* w, const uint8_t* keep,
+                     float* lse, float* kl, float* loss, float* metrics, void* workspace, size_t workspace_bytes);
+
+size_t aero_distill_bwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int64_t chunk_tokens,
+                                        int32_t dw_dtype);
+
+int aero_distill_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K,
+                     const void* H, const void* W, const int32_t* ids, const float* logits, const float* teacher_lse,
+                     const int64_t* cs, const float* w, const uint8_t* keep, const float* lse, float grad_scale,
+                     void* dH, void* dW, int32_t dw_dtype, int accumulate_dW, void* workspace, size_t workspace_bytes);
+
+size_t aero_distill_fwd_bwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int64_t chunk_tokens,
+                                            int32_t dw_dtype);
+
+int aero_distill_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K,
+                         const void* H, const void* W, const int32_t* ids, const float* logits, const float* teacher_lse,
+                         const int64_t* cs, const float* w, const uint8_t* keep,
+                         float* lse, float* kl, float* loss, float* metrics, float grad_scale,
+                         void* dH, void* dW, int32_t dw_dtype, int accumulate_dW, void* workspace,
+                         size_t workspace_bytes);
 
 /* The embedding with W [V,d] (cfg->dtype), the lm_head weight when the two are tied:
  *   aero_embed_fwd:  X[t,:] = scale W[y_t,:]          (rounded once; y_t = AERO_NO_TOKEN: zeros)

@@ -59,3 +59,46 @@ def embed_bwd(dX, y, V, scale=1.0):
 def lmhead_q8(h8, h_scale, w8, w_scale):
     acc = np.asarray(h8, np.float64) @ np.asarray(w8, np.float64).T       # integers below 2^53: exact
     return acc * np.asarray(h_scale, np.float64)[:, None] * np.asarray(w_scale, np.float64)[None, :]
+
+
+# ---- distillation from a teacher's top logits ---------------------------------------------------
+def teacher_probs(ids, logits, teacher_lse, V):
+    """Row by row: log q of each list place (-inf for an empty one, or one whose logit is -inf or NaN)."""
+    ids, logits = np.asarray(ids), np.asarray(logits, np.float64)
+    there = (ids >= 0) & (ids < V)
+    a = np.where(there & ~np.isnan(logits), logits, -np.inf)
+    lq = np.full(a.shape, -np.inf)
+    for t in range(len(a)):
+        if not (a[t] > -np.inf).any():
+            continue
+        m = a[t].max()
+        n = teacher_lse[t] if teacher_lse is not None else m + np.log(np.exp(a[t] - m).sum())
+        lq[t] = a[t] - n
+    return there, lq
+
+
+def distill(H, W, ids, logits, cs, w, keep, teacher_lse=None, grad_scale=1.0):
+    """loss = sum_t w_i sum_k q_tk (log q_tk - log p_t,id) over the rows of kept rollouts, and its gradients:
+    dict of lse, kl, Q, mass (student's probability of the listed tokens, by list place), loss, dz, dH, dW."""
+    H, W = np.asarray(H, np.float64), np.asarray(W, np.float64)
+    T, V = H.shape[0], W.shape[0]
+    cs = np.asarray(cs)
+    owner = np.searchsorted(cs, np.arange(T), side="right") - 1
+    kept = np.asarray(keep)[owner] != 0
+    wt = np.asarray(w, np.float64)[owner] * kept
+    z = H @ W.T
+    m = z.max(axis=1, keepdims=True)
+    lse = (m + np.log(np.exp(z - m).sum(axis=1, keepdims=True)))[:, 0]
+    there, lq = teacher_probs(ids, logits, teacher_lse, V)
+    at = np.where(there, ids, 0).astype(np.int64)
+    q = np.exp(lq)
+    lp = np.take_along_axis(z, at, axis=1) - lse[:, None]
+    with np.errstate(invalid="ignore"):
+        kl = np.where(q > 0, q * (lq - lp), 0.0).sum(axis=1) * kept
+    Q = q.sum(axis=1)
+    dz = Q[:, None] * np.exp(z - lse[:, None])
+    for t in range(T):
+        np.add.at(dz[t], at[t], -q[t])
+    dz *= (grad_scale * wt)[:, None]
+    return dict(lse=lse * kept, kl=kl, Q=Q, q=q, lq=lq, lp=lp, there=there, kept=kept, wt=wt, z=z, loss=float((wt * kl).sum()),
+                dz=dz, dH=dz @ W, dW=dz.T @ H, mass=np.where(there, np.exp(lp), 0.0).sum(axis=1))

@@ -36,6 +36,8 @@ EXPORTS = [
     "aero_set_tuning", "aero_finalize_weights", "aero_selftest_bounded_wait",
     "aero_rmsnorm_fwd", "aero_rmsnorm_bwd", "aero_rmsnorm_workspace_bytes", "aero_quantize_rows",
     "aero_embed_fwd", "aero_embed_bwd", "aero_embed_workspace_bytes", "aero_lmhead_q8",
+    "aero_distill_fwd", "aero_distill_bwd", "aero_distill_fwd_bwd", "aero_distill_fwd_workspace_bytes",
+    "aero_distill_bwd_workspace_bytes", "aero_distill_fwd_bwd_workspace_bytes",
 ]
 
 
@@ -129,6 +131,15 @@ def load_library():
     lib.aero_embed_workspace_bytes.argtypes = [i64, i32]
     lib.aero_embed_bwd.argtypes = [vp, cp, i64, i32, i32, vp, vp, f32, vp, C.c_int, vp, sz]
     lib.aero_lmhead_q8.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, i32, vp]
+    shape = [vp, cp, i64, i32, i32, i32, i32]
+    lib.aero_distill_fwd_workspace_bytes.restype = sz
+    lib.aero_distill_fwd_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    for f in (lib.aero_distill_bwd_workspace_bytes, lib.aero_distill_fwd_bwd_workspace_bytes):
+        f.restype = sz
+        f.argtypes = [i64, i32, i32, i32, i32, i64, i32]
+    lib.aero_distill_fwd.argtypes = shape + [vp] * 12 + [vp, sz]
+    lib.aero_distill_bwd.argtypes = shape + [vp] * 9 + [f32, vp, vp, i32, C.c_int, vp, sz]
+    lib.aero_distill_fwd_bwd.argtypes = shape + [vp] * 12 + [f32, vp, vp, i32, C.c_int, vp, sz]
     lib.aero_launch_count.restype = C.c_int64
     lib.aero_launch_count.argtypes = [vp]
     _lib = lib
@@ -594,6 +605,76 @@ class Context:
                                      self._arg(o, out_dtype, (T, V), "out"))
         _check(rc, "aero_lmhead_q8")
         return o
+
+    # ---- distillation from a teacher's top logits --------------------------------------------
+    def _distill_inputs(self, cfg, H, W, ids, logits, teacher_lse, cs, w, keep):
+        T, d = H.shape
+        V, R, K = W.shape[0], cs.numel() - 1, ids.shape[-1]
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        ptrs = (self._arg(H, dt, (T, d), "H"), self._arg(W, dt, (V, d), "W"), self._arg(ids, torch.int32, (T, K), "ids"),
+                self._arg(logits, torch.float32, (T, K), "logits"),
+                self._arg(teacher_lse, torch.float32, (T,), "teacher_lse"), self._arg(cs, torch.int64, (R + 1,), "cs"),
+                self._arg(w, torch.float32, (R,), "w"), self._arg(keep, torch.uint8, (R,), "keep"))
+        return (T, d, V, R, K), dt, ptrs
+
+    def _distill_outputs(self, T, out):
+        o = dict(out) if out is not None else {}
+        for name, shape in (("lse", (T,)), ("kl", (T,)), ("loss", (1,)), ("metrics", (4,))):
+            if name not in o:
+                o[name] = self._new(shape, torch.float32)
+        return o, tuple(self._arg(o[n], torch.float32, s, n)
+                        for n, s in (("lse", (T,)), ("kl", (T,)), ("loss", (1,)), ("metrics", (4,))))
+
+    def _distill_grads(self, shape, dt, dH, dW, dw_dtype, accumulate_dW):
+        T, d, V, R, K = shape
+        if dw_dtype not in (torch.float32, torch.bfloat16):
+            raise AeroError(f"dw_dtype must be torch.float32 or torch.bfloat16, got {dw_dtype}")
+        if accumulate_dW and dW is None:
+            raise AeroError("accumulate_dW needs the dW to add to")
+        dH = dH if dH is not None else self._new((T, d), dt)
+        dW = dW if dW is not None else self._new((V, d), dw_dtype)
+        return dH, dW, self._arg(dH, dt, (T, d), "dH"), self._arg(dW, dw_dtype, (V, d), "dW")
+
+    @staticmethod
+    def _distill_chunk(T, R, chunk_tokens):
+        # by default all of a batch that fits two waves of token tiles (each kept run may end in a tile of its own)
+        return chunk_tokens if chunk_tokens is not None else min(T + 128 * (R + 2), 2 * 148 * 128)
+
+    def distill_fwd(self, cfg, H, W, ids, logits, cs, w, keep, teacher_lse=None, out=None):
+        """aero_distill_fwd: a dict of lse, kl [T], loss [1] and metrics [4]."""
+        shape, dt, ptrs = self._distill_inputs(cfg, H, W, ids, logits, teacher_lse, cs, w, keep)
+        o, outs = self._distill_outputs(shape[0], out)
+        ws = self._scratch(self.lib.aero_distill_fwd_workspace_bytes(*shape))
+        _check(self.lib.aero_distill_fwd(self.h, C.byref(cfg), *shape, *ptrs, *outs, ws.data_ptr(), ws.numel()),
+               "aero_distill_fwd")
+        return o
+
+    def distill_bwd(self, cfg, H, W, ids, logits, cs, w, keep, lse, teacher_lse=None, grad_scale=1.0, dH=None, dW=None,
+                    dw_dtype=torch.float32, accumulate_dW=False, chunk_tokens=None):
+        """aero_distill_bwd: (dH, dW) from the forward's lse."""
+        shape, dt, ptrs = self._distill_inputs(cfg, H, W, ids, logits, teacher_lse, cs, w, keep)
+        dH, dW, pH, pW = self._distill_grads(shape, dt, dH, dW, dw_dtype, accumulate_dW)
+        dwt = AERO_FP32 if dw_dtype == torch.float32 else AERO_BF16
+        ws = self._scratch(self.lib.aero_distill_bwd_workspace_bytes(
+            *shape, self._distill_chunk(shape[0], shape[3], chunk_tokens), dwt))
+        _check(self.lib.aero_distill_bwd(self.h, C.byref(cfg), *shape, *ptrs,
+                                         self._arg(lse, torch.float32, (shape[0],), "lse"), grad_scale, pH, pW, dwt,
+                                         1 if accumulate_dW else 0, ws.data_ptr(), ws.numel()), "aero_distill_bwd")
+        return dH, dW
+
+    def distill_fwd_bwd(self, cfg, H, W, ids, logits, cs, w, keep, teacher_lse=None, out=None, grad_scale=1.0, dH=None,
+                        dW=None, dw_dtype=torch.float32, accumulate_dW=False, chunk_tokens=None):
+        """aero_distill_fwd_bwd: (forward outputs dict, dH, dW) in one call, without recomputing the logits."""
+        shape, dt, ptrs = self._distill_inputs(cfg, H, W, ids, logits, teacher_lse, cs, w, keep)
+        o, outs = self._distill_outputs(shape[0], out)
+        dH, dW, pH, pW = self._distill_grads(shape, dt, dH, dW, dw_dtype, accumulate_dW)
+        dwt = AERO_FP32 if dw_dtype == torch.float32 else AERO_BF16
+        ws = self._scratch(self.lib.aero_distill_fwd_bwd_workspace_bytes(
+            *shape, self._distill_chunk(shape[0], shape[3], chunk_tokens), dwt))
+        _check(self.lib.aero_distill_fwd_bwd(self.h, C.byref(cfg), *shape, *ptrs, *outs, grad_scale, pH, pW, dwt,
+                                             1 if accumulate_dW else 0, ws.data_ptr(), ws.numel()),
+               "aero_distill_fwd_bwd")
+        return o, dH, dW
 
     # ---- allocation controller, simulated ----------------------------------------------------
     def allocate_sim(self, cfg, acfg, thr, out=None):

@@ -46,6 +46,14 @@ struct Params {
   float* dW;
   uint32_t* status;
   const float* row_scale;       // dH: factor of each token row, applied to the finished tile (NULL: none)
+  // dW: the chunk's product replaces what is there instead of being added to it -- in fp32 (overwrite), or
+  // rounded to bf16 (dW16 not NULL)
+  int overwrite;
+  __nv_bfloat16* dW16;
+  // dH: split of the vocabulary (the reduction) into *ksplit ranges, each leaving fp32 sums of its tiles in
+  // part [range][tile of the chunk * 128 + row][d]; NULL, or 1 in memory: no split, the tiles go to dH
+  const int* ksplit;
+  float* part;
   int h_local;                  // dW: operand B holds the chunk's rows tile after tile, not all T rows
   // Pacing: CTAs that run at the same time share operand tiles through L2 (the units of one row tile read the
   // same dz tiles, the units of one column tile the same W or H slab), which works only while they walk the
@@ -59,6 +67,50 @@ struct Params {
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<uint32_t*>(&v);
+}
+
+// 32 columns of one row of dW from the accumulator.
+__device__ __forceinline__ void store_dw(const Params& p, long long row, int col0, const uint32_t (&r)[32]) {
+  if (p.dW16) {
+    uint4* dst = reinterpret_cast<uint4*>(p.dW16 + row * p.d + col0);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      dst[q] = make_uint4(pack_bf16(__uint_as_float(r[8 * q]), __uint_as_float(r[8 * q + 1])),
+                          pack_bf16(__uint_as_float(r[8 * q + 2]), __uint_as_float(r[8 * q + 3])),
+                          pack_bf16(__uint_as_float(r[8 * q + 4]), __uint_as_float(r[8 * q + 5])),
+                          pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
+    return;
+  }
+  float4* dst = reinterpret_cast<float4*>(p.dW + row * p.d + col0);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) {
+    float4 v = p.overwrite ? make_float4(0.f, 0.f, 0.f, 0.f) : dst[q];
+    v.x += __uint_as_float(r[4 * q]);
+    v.y += __uint_as_float(r[4 * q + 1]);
+    v.z += __uint_as_float(r[4 * q + 2]);
+    v.w += __uint_as_float(r[4 * q + 3]);
+    dst[q] = v;
+  }
+}
+
+// Numbering of the units.  Without a split row tile by row tile: CTAs running together share the dz tiles of a
+// few row tiles and one slab of W or H per column tile.  With a split there are few row tiles, so they come
+// first: CTAs running together share the W slabs of one range, and W passes through L2 once.
+struct Units {
+  int n_m, n_nt, nkb, ks;
+  __device__ int m(int u) const { return ks == 1 ? u / n_nt : u % n_m; }
+  __device__ int n(int u) const { return ks == 1 ? u % n_nt : u / n_m % n_nt; }
+  __device__ int range(int u) const { return ks == 1 ? 0 : u / n_m / n_nt; }
+  __device__ int k0(int u) const { return (int)((long long)range(u) * nkb / ks); }
+  __device__ int k1(int u) const { return (int)((long long)(range(u) + 1) * nkb / ks); }
+};
+
+// 32 columns of one row of a range's fp32 sums of dH.
+__device__ __forceinline__ void store_part(const Params& p, int range, long long row, int chunk_tiles, int col0,
+                                           const uint32_t (&r)[32]) {
+  uint4* dst = reinterpret_cast<uint4*>(p.part + ((long long)range * chunk_tiles * BM + row) * p.d + col0);
+#pragma unroll
+  for (int q = 0; q < 8; ++q) dst[q] = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
 }
 
 template <int KIND>
@@ -88,7 +140,9 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   const int n_nt = (p.d + BN - 1) / BN;
   const int n_mt = KIND == KIND_DH ? chunk_tiles : (p.V + BM - 1) / BM;
   const int nkb = KIND == KIND_DH ? (int)(p.ldz / BK) : chunk_tiles * (BM / BK);
-  const int n_units = nkb > 0 ? n_mt * n_nt : 0;
+  const int ks = KIND == KIND_DH && p.ksplit ? *p.ksplit : 1;
+  const int n_units = nkb > 0 ? n_mt * n_nt * ks : 0;
+  const Units un = {n_mt, n_nt, nkb, ks};
 
   if (warp == 4) {
     // ---------------- TMA producer ----------------
@@ -99,10 +153,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
       unsigned int meetings = 0;
       const int max_units = (n_units + (int)gridDim.x - 1) / (int)gridDim.x;     // of the longest schedule
       for (int u = blockIdx.x; ok && u < n_units; u += gridDim.x) {
-        const int mt = u / n_nt, nt = u % n_nt;
+        const int mt = un.m(u), nt = un.n(u);
         int next_meet = 0;
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
-          if (p.nsync > 0 && next_meet < p.nsync && kb >= (int)((long long)next_meet * nkb / p.nsync)) {
+        const int k0 = un.k0(u), k1 = un.k1(u);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
+          if (p.nsync > 0 && next_meet < p.nsync && kb - k0 >= (int)((long long)next_meet * (k1 - k0) / p.nsync)) {
             ++next_meet;
             ++meetings;
             atomicAdd(p.sync_ctr, 1u);
@@ -159,7 +214,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         if (!tc::mbar_wait(&ctl->tempty[buf], aph ^ 1u, abort_flag)) { ok = false; break; }
         tc::tc_fence_after();
         const uint32_t tmem_d = tmem_base + buf * BN;
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const int k0 = un.k0(u), k1 = un.k1(u);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
           const int s = it % STAGES;
           const uint32_t ph = (it / STAGES) & 1u;
           if (!tc::mbar_wait(&ctl->full[s], ph, abort_flag)) { ok = false; break; }
@@ -174,7 +230,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           constexpr uint32_t b_step = 2048u >> 4;
 #pragma unroll
           for (int kk = 0; kk < BK / UMMA_K; ++kk)
-            tc::umma_bf16(tmem_d, adesc + a_step * kk, bdesc + b_step * kk, idesc, (kb | kk) != 0 ? 1u : 0u);
+            tc::umma_bf16(tmem_d, adesc + a_step * kk, bdesc + b_step * kk, idesc, kb > k0 || kk > 0 ? 1u : 0u);
           tc::umma_commit(&ctl->empty[s]);
         }
         if (ok) tc::umma_commit(&ctl->tfull[buf]);
@@ -186,7 +242,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     bool ok = true;
     const int r_in_tile = warp * 32 + lane;
     for (int u = blockIdx.x; ok && u < n_units; u += gridDim.x, ++at) {
-      const int mt = u / n_nt, nt = u % n_nt;
+      const int mt = un.m(u), nt = un.n(u);
       const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], aph, abort_flag))) { ok = false; break; }
       tc::tc_fence_after();
@@ -210,6 +266,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         const int col0 = nt * BN + c * 32;
         if (!row_ok) {
           // rows outside the tile's run, past T or past V: nothing to write
+        } else if (KIND == KIND_DH && ks > 1) {
+          store_part(p, un.range(u), (long long)mt * BM + r_in_tile, chunk_tiles, col0, r);
         } else if (KIND == KIND_DH) {
           uint4* dst = reinterpret_cast<uint4*>(p.dH + out_row * p.d + col0);
           if (p.row_scale) {
@@ -225,16 +283,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
                                 pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
           }
         } else {
-          float4* dst = reinterpret_cast<float4*>(p.dW + out_row * p.d + col0);
-#pragma unroll
-          for (int q = 0; q < 8; ++q) {
-            float4 v = dst[q];
-            v.x += __uint_as_float(r[4 * q]);
-            v.y += __uint_as_float(r[4 * q + 1]);
-            v.z += __uint_as_float(r[4 * q + 2]);
-            v.w += __uint_as_float(r[4 * q + 3]);
-            dst[q] = v;
-          }
+          store_dw(p, out_row, col0, r);
         }
       }
       tc::tc_fence_before();
@@ -307,7 +356,9 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   const int n_mt = KIND == KIND_DH ? chunk_tiles : (p.V + BM - 1) / BM;      // row tiles of 128
   const int n_mp = (n_mt + 1) / 2;                                           // ... in pairs
   const int nkb = KIND == KIND_DH ? (int)(p.ldz / BK) : chunk_tiles * (BM / BK);
-  const int n_units = nkb > 0 ? n_mp * n_nt : 0;
+  const int ks = KIND == KIND_DH && p.ksplit ? *p.ksplit : 1;
+  const int n_units = nkb > 0 ? n_mp * n_nt * ks : 0;
+  const Units un = {n_mp, n_nt, nkb, ks};
 
   if (warp == 4) {
     // ---------------- TMA producer (one per CTA) ----------------
@@ -318,13 +369,14 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
       unsigned int meetings = 0;
       const int max_units = (n_units + npairs - 1) / npairs;     // of the longest schedule
       for (int u = pair; ok && u < n_units; u += npairs) {
-        const int mp = u / n_nt, nt = u % n_nt;
+        const int mp = un.m(u), nt = un.n(u);
         // the pair's second row tile may not exist: its CTA then stages the first one again (dH) or rows
         // past V, which the copy fills with zeros (dW), and discards the result
         const int mt = (KIND == KIND_DH && 2 * mp + (int)rank >= n_mt) ? 2 * mp : 2 * mp + (int)rank;
         int next_meet = 0;
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
-          if (p.nsync > 0 && next_meet < p.nsync && kb >= (int)((long long)next_meet * nkb / p.nsync)) {
+        const int k0 = un.k0(u), k1 = un.k1(u);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
+          if (p.nsync > 0 && next_meet < p.nsync && kb - k0 >= (int)((long long)next_meet * (k1 - k0) / p.nsync)) {
             ++next_meet;
             ++meetings;
             atomicAdd(p.sync_ctr, 1u);
@@ -375,7 +427,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         if (!tc::mbar_wait(&ctl->tempty[buf], aph ^ 1u, abort_flag)) { ok = false; break; }
         tc::tc_fence_after();
         const uint32_t tmem_d = tmem_base + buf * BN;
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const int k0 = un.k0(u), k1 = un.k1(u);
+        for (int kb = k0; kb < k1; ++kb, ++it) {
           const int s = it % PSTAGES;
           const uint32_t ph = (it / PSTAGES) & 1u;
           if (!tc::mbar_wait(&ctl->full[s], ph, abort_flag)) { ok = false; break; }
@@ -388,7 +441,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
           constexpr uint32_t b_step = 2048u >> 4;
 #pragma unroll
           for (int kk = 0; kk < BK / UMMA_K; ++kk)
-            tc::umma_bf16_pair(tmem_d, adesc + a_step * kk, bdesc + b_step * kk, idesc, (kb | kk) != 0 ? 1u : 0u);
+            tc::umma_bf16_pair(tmem_d, adesc + a_step * kk, bdesc + b_step * kk, idesc, kb > k0 || kk > 0 ? 1u : 0u);
           tc::umma_commit_pair(&ctl->empty[s], 3);     // frees the stage in both CTAs when these MMAs retire
         }
         if (ok) tc::umma_commit_pair(&ctl->tfull[buf], 3);
@@ -400,7 +453,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     bool ok = true;
     const int r_in_tile = warp * 32 + lane;
     for (int u = pair; ok && u < n_units; u += npairs, ++at) {
-      const int mp = u / n_nt, nt = u % n_nt;
+      const int mp = un.m(u), nt = un.n(u);
       const int mt = 2 * mp + (int)rank;
       const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], aph, abort_flag))) { ok = false; break; }
@@ -428,6 +481,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
           const int col0 = nt * BN + c * 32;
           if (!row_ok) {
             // rows outside the tile's run, past T or past V: nothing to write
+          } else if (KIND == KIND_DH && ks > 1) {
+            store_part(p, un.range(u), (long long)mt * BM + r_in_tile, chunk_tiles, col0, r);
           } else if (KIND == KIND_DH) {
             uint4* dst = reinterpret_cast<uint4*>(p.dH + out_row * p.d + col0);
             if (p.row_scale) {
@@ -443,16 +498,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                   pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
             }
           } else {
-            float4* dst = reinterpret_cast<float4*>(p.dW + out_row * p.d + col0);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              float4 v = dst[q];
-              v.x += __uint_as_float(r[4 * q]);
-              v.y += __uint_as_float(r[4 * q + 1]);
-              v.z += __uint_as_float(r[4 * q + 2]);
-              v.w += __uint_as_float(r[4 * q + 3]);
-              dst[q] = v;
-            }
+            store_dw(p, out_row, col0, r);
           }
         }
       }

@@ -81,6 +81,8 @@ struct Params {
   // 136 MB at d = 3584) shrink to what L2 holds.  Forward modes then leave the per-row running
   // state in xstate [vsplit][T] for merge_kernel instead of finishing the row.
   int vsplit;
+  const int* plan;              // NULL, or the split count of this launch in device memory (vsplit unused); forward modes then
+                                // leave the running state in xstate for any count, 1 included
   float4* xstate;
   // Pacing: all CTAs re-read the same W tiles from L2, which only works while they walk the
   // vocabulary in step; small rate differences between SMs add up over a long launch.  The
@@ -266,7 +268,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
   // The pair's k-th unit is token tiles first, first + 1 (the second may not exist: its CTA
   // then stages the first tile's rows again and discards the result) and one of the vsplit
   // ranges of vocabulary tiles; the pairs that share tiles are neighbours.
-  const int vsplit = p.vsplit;
+  const int vsplit = p.plan ? *p.plan : p.vsplit;
   auto unit_first = [&](int k) { return p.tile_begin + 2 * ((pair + k * npairs) / vsplit); };
   auto unit_j0 = [&](int k) { return (int)((long long)((pair + k * npairs) % vsplit) * nvt / vsplit); };
   auto unit_j1 = [&](int k) { return (int)((long long)((pair + k * npairs) % vsplit + 1) * nvt / vsplit); };
@@ -591,7 +593,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         else aero_raise(p.status, AERO_ST_RANGE);
       }
       if (!IS_DZ && ok && have_tile) {
-        if (vsplit > 1) {
+        if (vsplit > 1 || p.plan) {
           if (live) p.xstate[(size_t)((pair + k * npairs) % vsplit) * p.T + row] = make_float4(m2, l, zy, sz);
         } else {
           finish_rows(p, ENT, live, row, tile, warp, lane, m2, l, zy, sz);

@@ -1,0 +1,367 @@
+"""GPU tests of distillation from a teacher's top logits (aero_distill_fwd / _bwd / _fwd_bwd) against the
+fp64 statement.
+
+Tolerances, for one row with S = max_v sum_k |h_k w_vk|:
+  a logit        (d/8 + 8) 2^-23 S: fp32 accumulation in steps of 16 products, twice for the order of the adds
+  log-sum-exp    the logits' error, (V/32 + 64) 2^-24 for the running sum, 2^-20 |lse| for the logarithms
+  kl             Q (lse + logit), 2^-18 sum q (|log q| + |log p|) for exp and log of the list
+  dz             2^-8 |dz| (rounded to bf16; fp32 path: none) and, one-call step, 2^-8 Q p w (its p~ was too),
+                 (Q p + q) w (lse + logit + 2^-17)
+                 and Q w 2^-67: p~ = exp(z - c) with c at most 40 above the largest of the row's first logits
+                 leaves bf16's range (2^-126 = e^-87) for z 47 below them, that is p below e^-47 < 2^-67
+                 (fp32 path: below 2^-126)
+  dH, dW         the dz errors through |W|, |H|; 2^-14 of the magnitudes for accumulation; the rounding of the
+                 output."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import model_ends as M
+from paper_2602_14338_b200 import binding as B
+from tests import aero_testlib as TL
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.Context(0)
+    yield c
+    assert c.last_status() == 0
+    c.close()
+
+
+class Case:
+    def __init__(self, T, d, V, K, dtype="bf16", R=None, seed=0, lean=True, teacher_lse=False, drop=True, spread=2.5):
+        rng = np.random.default_rng(1000 * seed + T + d + V + K)
+        dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.dtype, self.T, self.d, self.V, self.K = dtype, T, d, V, K
+        W = torch.from_numpy(rng.standard_normal((V, d)) * 0.05).to(dt)
+        ids = rng.integers(0, V, (T, K))
+        H = torch.from_numpy(rng.standard_normal((T, d)))
+        if lean and T:
+            s = rng.choice([0.0, 4.0, 8.0, 14.0], T)       # from a flat row to one the student is sure of
+            lead = W[torch.from_numpy(ids[:, 0])].double()
+            H = 0.5 * H + torch.from_numpy(s)[:, None] * lead / lead.square().sum(1, keepdim=True)
+        self.Ht, self.Wt = H.to(dt), W
+        logits = rng.standard_normal((T, K)) * spread + 11.0
+        if T >= 6:
+            ids[1, K // 2:] = M.NO_TOKEN                   # a shorter list
+            ids[2] = M.NO_TOKEN                            # an empty one
+            logits[2] = np.nan                             # (its logits are not read)
+            logits[3, :] = -np.inf                         # present, without weight
+            ids[4] = ids[4, 0]                             # one token in every place
+            logits[5, K // 2:] = -np.inf
+        self.ids, self.logits = ids.astype(np.int32), logits.astype(np.float32)
+        self.tlse = (np.log(np.exp(np.where(np.isfinite(logits), logits, -80)).sum(1)) + 0.3).astype(np.float32) if teacher_lse else None
+        R = R if R is not None else max(1, min(T // 5, 9))
+        cut = np.sort(rng.choice(np.arange(1, T), R - 1, replace=False)) if R > 1 else np.array([], int)
+        self.cs = np.concatenate([[0], cut, [T]]).astype(np.int64)
+        self.keep = np.ones(R, np.uint8)
+        if drop and R > 2:
+            self.keep[1::3] = 0
+        self.w = (rng.random(R) * self.keep / max(T, 1)).astype(np.float32)
+
+    def device(self):
+        t = lambda a: None if a is None else torch.from_numpy(a).cuda()
+        return dict(H=self.Ht.cuda(), W=self.Wt.cuda(), ids=t(self.ids), logits=t(self.logits), cs=t(self.cs), w=t(self.w),
+                    keep=t(self.keep)), t(self.tlse)
+
+    @property
+    def cfg(self):
+        return B.cfg_default(dtype=B.AERO_BF16 if self.dtype == "bf16" else B.AERO_FP32)
+
+    def reference(self, grad_scale=1.0):
+        H, W = self.Ht.double().numpy(), self.Wt.double().numpy()
+        r = M.distill(H, W, self.ids, self.logits, self.cs, self.w, self.keep, self.tlse, grad_scale)
+        S = (np.abs(H) @ np.abs(W).T).max(axis=1) if self.T else np.zeros(0)
+        tz = (self.d / 8 + 8) * 2.0 ** -23 * S
+        r["t_lse"] = tz + (self.V / 32 + 64) * 2.0 ** -24 + 2.0 ** -20 * np.abs(r["lse"])
+        with np.errstate(invalid="ignore"):
+            sizes = np.where(r["q"] > 0, r["q"] * (np.abs(r["lq"]) + np.abs(r["lp"])), 0).sum(axis=1)
+        r["t_kl"] = r["Q"] * (r["t_lse"] + tz) + 2.0 ** -18 * sizes + 1e-12
+        both = r["Q"][:, None] * np.exp(r["z"] - (r["z"].max(1) if self.T else np.zeros(0))[:, None]
+                                        - np.log(np.exp(r["z"] - r["z"].max(1)[:, None]).sum(1))[:, None])
+        soft = both * (abs(grad_scale) * r["wt"])[:, None]
+        for t in range(self.T):
+            np.add.at(both[t], np.where(r["there"][t], self.ids[t], 0), r["q"][t])
+        both *= (abs(grad_scale) * r["wt"])[:, None]
+        half = 2.0 ** -8 if self.dtype == "bf16" else 0.0
+        edz = half * (np.abs(r["dz"]) + soft) + both * (r["t_lse"] + tz + 2.0 ** -17)[:, None]
+        edz += (abs(grad_scale) * r["wt"] * r["Q"])[:, None] * (2.0 ** -67 if self.dtype == "bf16" else 2.0 ** -126)
+        r["t_dH"] = edz @ np.abs(W) + 2.0 ** -14 * (np.abs(r["dz"]) @ np.abs(W)) + half * np.abs(r["dH"])
+        r["t_dW"] = edz.T @ np.abs(H) + 2.0 ** -14 * (np.abs(r["dz"]).T @ np.abs(H))
+        return r
+
+
+def close(got, want, tol, what):
+    got = got.double().cpu().numpy() if torch.is_tensor(got) else got
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), f"{what}: {bad.sum()} values, worst {np.nanmax(np.abs(got - want) / np.maximum(tol, 1e-300)):.3g} of the bound"
+
+
+def check_forward(case, out, r):
+    close(out["lse"], r["lse"], r["t_lse"], "lse")
+    close(out["kl"], r["kl"], r["t_kl"], "kl")
+    loss = float(out["loss"])
+    assert abs(loss - r["loss"]) <= (r["wt"] * r["t_kl"]).sum() + 2.0 ** -22 * (r["wt"] * np.abs(r["kl"])).sum() + 1e-12
+    kept = max(int(r["kept"].sum()), 1)
+    met = out["metrics"].cpu().numpy()
+    assert met[3] == r["kept"].sum()
+    assert met[0] == pytest.approx((r["kept"] & (r["Q"] == 0)).sum() / kept, abs=1e-6)
+    assert met[1] == pytest.approx(r["kl"].sum() / kept, rel=1e-3, abs=1e-5)
+    assert met[2] == pytest.approx((r["mass"] * r["kept"]).sum() / kept, rel=1e-3, abs=1e-5)
+
+
+def check_grads(case, dH, dW, r, dw_half=0.0, base=0.0):
+    close(dH, r["dH"], r["t_dH"], "dH")
+    close(dW, r["dW"] + base, r["t_dW"] + dw_half * np.abs(r["dW"]) + 2.0 ** -22 * np.abs(base), "dW")
+    dropped = torch.from_numpy(~r["kept"]).cuda()
+    assert not dH[dropped].any()
+
+
+BF16 = [dict(T=1, d=64, V=1, K=1), dict(T=1, d=64, V=100, K=3), dict(T=7, d=64, V=65, K=1), dict(T=130, d=128, V=300, K=8),
+        dict(T=300, d=192, V=1000, K=33, teacher_lse=True), dict(T=700, d=256, V=2049, K=64), dict(T=257, d=1536, V=700, K=256),
+        dict(T=64, d=3584, V=1500, K=5, teacher_lse=True), dict(T=1000, d=64, V=4096, K=20, R=60)]
+FP32 = [dict(T=1, d=1, V=1, K=1), dict(T=3, d=57, V=100, K=3), dict(T=60, d=64, V=300, K=8, teacher_lse=True),
+        dict(T=200, d=96, V=700, K=40)]
+
+
+@pytest.mark.parametrize("kw", [dict(k, dtype="bf16") for k in BF16] + [dict(k, dtype="fp32") for k in FP32])
+def test_forward_backward_and_one_call(ctx, kw):
+    case = Case(**kw)
+    dv, tl = case.device()
+    r = case.reference(grad_scale=1.5)
+    out = ctx.distill_fwd(case.cfg, **dv, teacher_lse=tl)
+    check_forward(case, out, r)
+    dH, dW = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"], teacher_lse=tl, grad_scale=1.5)
+    check_grads(case, dH, dW, r)
+    out2, dH2, dW2 = ctx.distill_fwd_bwd(case.cfg, **dv, teacher_lse=tl, grad_scale=1.5)
+    check_forward(case, out2, r)
+    check_grads(case, dH2, dW2, r)
+    # the same bits again
+    out3, dH3, dW3 = ctx.distill_fwd_bwd(case.cfg, **dv, teacher_lse=tl, grad_scale=1.5)
+    for a, b in ((out2["lse"], out3["lse"]), (out2["kl"], out3["kl"]), (out2["loss"], out3["loss"]), (dH2, dH3), (dW2, dW3)):
+        assert torch.equal(a, b)
+    # added to what is there
+    base = torch.randn(case.V, case.d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) * 1e-2
+    b64 = base.double().cpu().numpy()
+    _, _, acc = ctx.distill_fwd_bwd(case.cfg, **dv, teacher_lse=tl, grad_scale=1.5, dW=base.clone(), accumulate_dW=True)
+    check_grads(case, dH2, acc, r, base=b64)
+    _, acc = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"], teacher_lse=tl, grad_scale=1.5, dW=base.clone(), accumulate_dW=True)
+    check_grads(case, dH2, acc, r, base=b64)
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("tuning", [dict(vsplit=2), dict(vsplit=4), dict(rowscale=0), dict(gemm_pairs=1), dict(gemm_pairs=0, vsplit=2, rowscale=0)])
+def test_every_schedule_of_stage_b(ctx, tuning):
+    case = Case(T=500, d=256, V=3000, K=17, R=11)
+    dv, tl = case.device()
+    r = case.reference()
+    ctx.set_tuning(**tuning)
+    try:
+        out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv)
+        fwd = ctx.distill_fwd(case.cfg, **dv)
+        dH2, dW2 = ctx.distill_bwd(case.cfg, **dv, lse=fwd["lse"])
+    finally:
+        ctx.set_tuning()
+    check_forward(case, out, r)
+    check_forward(case, fwd, r)
+    check_grads(case, dH, dW, r)
+    check_grads(case, dH2, dW2, r)
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("chunk_tokens", [128, 256, None])
+def test_chunks_and_dw_types(ctx, chunk_tokens):
+    case = Case(T=900, d=128, V=1111, K=9, R=13)
+    dv, _ = case.device()
+    r = case.reference()
+    lse = ctx.distill_fwd(case.cfg, **dv)["lse"]
+    for dt, half in ((torch.float32, 0.0), (torch.bfloat16, 2.0 ** -8)):
+        _, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dw_dtype=dt, chunk_tokens=chunk_tokens)
+        assert dW.dtype == dt
+        check_grads(case, dH, dW, r, half)
+        dH, dW = ctx.distill_bwd(case.cfg, **dv, lse=lse, dw_dtype=dt, chunk_tokens=chunk_tokens)
+        check_grads(case, dH, dW, r, half)
+    assert ctx.last_status() == 0
+
+
+def test_bf16_dw_of_a_few_rows_needs_no_room_for_sums(ctx):
+    """One chunk whose block is smaller than an fp32 dW would be."""
+    case = Case(T=100, d=256, V=3000, K=9, R=1)
+    dv, _ = case.device()
+    r = case.reference()
+    _, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dw_dtype=torch.bfloat16)
+    check_grads(case, dH, dW, r, 2.0 ** -8)
+    lse = ctx.distill_fwd(case.cfg, **dv)["lse"]
+    dH, dW = ctx.distill_bwd(case.cfg, **dv, lse=lse, dw_dtype=torch.bfloat16)
+    check_grads(case, dH, dW, r, 2.0 ** -8)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_nothing_kept_and_no_rows(ctx, dtype):
+    case = Case(T=200, d=64, V=300, K=4, R=3, dtype=dtype)
+    case.keep[:] = 0
+    dv, _ = case.device()
+    full = lambda *s, dt=torch.float32: torch.full(s, 7.0, dtype=dt, device="cuda")
+    types = (torch.float32, torch.bfloat16) if dtype == "bf16" else (torch.float32,)
+    for dt in types:
+        out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dW=full(300, 64, dt=dt), dw_dtype=dt,
+                                          dH=full(200, 64, dt=case.Ht.dtype))
+        assert not dH.any() and not dW.any() and float(out["loss"]) == 0 and not out["kl"].any() and not out["lse"].any()
+        dH, dW = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"], dW=full(300, 64, dt=dt), dw_dtype=dt, dH=full(200, 64, dt=case.Ht.dtype))
+        assert not dH.any() and not dW.any()
+    # no rows at all
+    dv.update(H=dv["H"][:0], ids=dv["ids"][:0], logits=dv["logits"][:0], cs=torch.zeros(1, dtype=torch.int64, device="cuda"),
+              w=dv["w"][:0], keep=dv["keep"][:0])
+    out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dW=full(300, 64))
+    assert dH.shape == (0, 64) and not dW.any() and float(out["loss"]) == 0
+    # rows, but no rollout owns them
+    dv.update(H=torch.zeros(5, 64, dtype=case.Ht.dtype, device="cuda"), ids=torch.zeros(5, 4, dtype=torch.int32, device="cuda"),
+              logits=torch.zeros(5, 4, device="cuda"))
+    out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dW=full(300, 64), dH=full(5, 64, dt=case.Ht.dtype))
+    assert not dH.any() and not dW.any() and float(out["loss"]) == 0 and not out["kl"].any() and not out["lse"].any()
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_bad_ids_raise_the_status_bit_and_count_as_empty(ctx, dtype):
+    case = Case(T=150, d=64, V=200, K=5, dtype=dtype, R=4)
+    dv, _ = case.device()
+    good = dv["ids"].clone()
+    kept = int(case.cs[2])                          # first row of the third rollout (kept)
+    good[kept, 1] = M.NO_TOKEN
+    good[0, 0] = M.NO_TOKEN
+    want, wH, wW = ctx.distill_fwd_bwd(case.cfg, **dict(dv, ids=good))
+    assert ctx.last_status() == 0
+    bad = good.clone()
+    bad[kept, 1] = 200
+    bad[0, 0] = -7
+    got, gH, gW = ctx.distill_fwd_bwd(case.cfg, **dict(dv, ids=bad))
+    assert ctx.last_status() == B.AERO_ST_BAD_TARGET
+    assert torch.equal(got["kl"], want["kl"]) and torch.equal(gH, wH) and torch.equal(gW, wW)
+
+
+@pytest.mark.parametrize("rowscale", [1, 0])
+@pytest.mark.parametrize("kind", ["one far logit", "many high logits"])
+def test_rows_beyond_the_range_of_the_stored_exponentials(ctx, kind, rowscale):
+    """One logit 130 above the row's first 32 ones (more than bf16 holds of exp(z - c)), and thousands of logits 118
+    above them (each in range, their sum not): such rows are redone."""
+    case = Case(T=300, d=64, V=6000, K=6, R=3, drop=False, lean=False)
+    W = torch.randn(6000, 64, generator=torch.Generator().manual_seed(3)) * 0.02
+    H = torch.randn(300, 64, generator=torch.Generator().manual_seed(4))
+    H[:, 0] = 0.0
+    rows = torch.arange(5, 300, 7)
+    H[rows, 0] = 10.0
+    if kind == "one far logit":
+        W[4000, 0] = 13.0
+        case.ids[::2, 1] = 4000
+    else:
+        W[1000:5500, 0] = 11.8
+    case.Ht, case.Wt = H.to(torch.bfloat16), W.to(torch.bfloat16)
+    dv, _ = case.device()
+    r = case.reference()
+    ctx.set_tuning(rowscale=rowscale)
+    try:
+        out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv)
+    finally:
+        ctx.set_tuning()
+    assert ctx.last_status() == 0
+    check_forward(case, out, r)
+    check_grads(case, dH, dW, r)
+
+
+def test_gradient_rows_of_a_sure_student(ctx):
+    """Rows whose listed token has probability near one on both sides: p - q keeps the accuracy of the log-probs."""
+    case = Case(T=256, d=256, V=4096, K=4, R=2, drop=False, lean=False, spread=0.0)
+    lead = case.Wt[torch.from_numpy(case.ids[:, 0]).long()].double()
+    strength = torch.tensor([15.0, 18.0, 21.0, 24.0], dtype=torch.float64).repeat(64)[:, None]
+    case.Ht = (0.05 * torch.randn(256, 256, generator=torch.Generator().manual_seed(1), dtype=torch.float64)
+               + strength * lead / lead.square().sum(1, keepdim=True)).to(torch.bfloat16)
+    case.logits[:, 0] = 25.0
+    dv, _ = case.device()
+    r = case.reference()
+    assert np.median(np.exp(r["lp"][6:, 0])) > 0.99
+    out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv)
+    check_forward(case, out, r)
+    check_grads(case, dH, dW, r)
+
+
+def test_captured_and_replayed(ctx):
+    side = torch.cuda.Stream()
+    c = B.Context(0, stream=side)
+    case = Case(T=200, d=128, V=900, K=7, R=4)
+    dv, _ = case.device()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        c.distill_fwd_bwd(case.cfg, **dv)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        out, dH, dW = c.distill_fwd_bwd(case.cfg, **dv)
+    for seed in (5, 6):
+        other = Case(T=200, d=128, V=900, K=7, R=4, seed=seed)
+        ov, _ = other.device()
+        for k in ("H", "W", "ids", "logits", "w"):
+            dv[k].copy_(ov[k])
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want, wH, wW = ctx.distill_fwd_bwd(case.cfg, **dv)
+        assert torch.equal(out["kl"], want["kl"]) and torch.equal(out["loss"], want["loss"])
+        assert torch.equal(dH, wH) and torch.equal(dW, wW)
+    assert c.last_status() == 0
+    del g
+    c.close()
+
+
+def test_a_step_of_the_ends_together(ctx):
+    """As a training step uses them: the frozen teacher's final norm with its 8-bit output and the 8-bit product give
+    logits, whose largest are the teacher's list; the student's norm gives H; the group stage gives keep and weights; the
+    distillation gives dH and the tied weight's dW; the norm's backward gives the gradient of the last hidden state, the
+    embedding's backward adds its share to the tied dW."""
+    T, d, V, K, P = 600, 256, 3000, 12, 6
+    g = torch.Generator().manual_seed(11)
+    bf = lambda *s, std=1.0: (torch.randn(*s, generator=g) * std).to(torch.bfloat16).cuda()
+    x, res, gamma, W = bf(T, d), bf(T, d), bf(d, std=0.1) + 1, bf(V, d, std=0.1)
+    tx, tgamma, tW = bf(T, d), bf(d, std=0.1) + 1, bf(V, d, std=0.1)
+    cfg = B.cfg_default()
+    # teacher
+    t8 = ctx.rmsnorm_fwd(cfg, tx, tgamma, h=False, quant=True)
+    w8, ws = ctx.quantize_rows(cfg, tW)
+    z = ctx.lmhead_q8(t8["q"], t8["q_scale"], w8, ws, out_dtype=torch.float32)
+    top = torch.topk(z, K, dim=1)
+    ids, logits = top.indices.int().contiguous(), top.values.contiguous()
+    tlse = torch.logsumexp(z, dim=1)
+    exact = M.rmsnorm_fwd(tx.double().cpu().numpy(), tgamma.double().cpu().numpy())[2] @ tW.double().cpu().numpy().T
+    # each operand is off by at most half a step of its row: 1/254 of the row's largest value
+    h = np.abs(M.rmsnorm_fwd(tx.double().cpu().numpy(), tgamma.double().cpu().numpy())[2])
+    wv = np.abs(tW.double().cpu().numpy())
+    bound = (h.max(1)[:, None] * wv.sum(1)[None, :] + h.sum(1)[:, None] * wv.max(1)[None, :]) / 254 + d * h.max(1)[:, None] * wv.max(1)[None, :] / 254 ** 2
+    assert (np.abs(z.double().cpu().numpy() - exact) <= 1.01 * bound).all()
+    # student
+    cs = torch.arange(0, T + 1, T // (P * 4), dtype=torch.int64, device="cuda")
+    go = torch.arange(0, P * 4 + 1, 4, dtype=torch.int32, device="cuda")
+    reward = torch.tensor(([1.0, 0, 0, 1] + [1.0] * 4 + [0.0, 1, 0, 0]) * 2, device="cuda")
+    grp = ctx.group_stats(cfg, go, reward, cs)
+    n = ctx.rmsnorm_fwd(cfg, x, gamma, residual=res)
+    out, dH, dW = ctx.distill_fwd_bwd(cfg, n["h"], W, ids, logits, cs, grp["w"], grp["keep"], teacher_lse=tlse)
+    dx, dgamma = ctx.rmsnorm_bwd(cfg, dH, n["sum"], gamma, n["rstd"])
+    y = torch.randint(0, V, (T,), generator=g).int().cuda()
+    emb = ctx.embed_fwd(cfg, W, y, scale=16.0)
+    tied = ctx.embed_bwd(cfg, dx, y, V, scale=16.0, dW=dW.clone(), accumulate_dW=True)
+    assert ctx.last_status() == 0
+    # the same chain in fp64 from what each operator was given
+    f = lambda t: t.double().cpu().numpy()
+    s64, r64, h64 = M.rmsnorm_fwd(f(x), f(gamma), f(res))
+    ref = M.distill(f(n["h"]), f(W), ids.cpu().numpy(), f(logits), cs.cpu().numpy(), f(grp["w"]), grp["keep"].cpu().numpy(), f(tlse))
+    assert grp["keep"].sum().item() == 16 and float(out["metrics"][3]) == 400
+    assert abs(float(out["loss"]) - ref["loss"]) <= 1e-4 * abs(ref["loss"])
+    rdx, rdg = M.rmsnorm_bwd(ref["dH"], s64, f(gamma), r64)
+    rtied = ref["dW"] + M.embed_bwd(rdx, y.cpu().numpy(), V, 16.0)[0]
+    # bf16 roundings along the way (h, dz, scaled rows, dH, dx: 2^-8 each at most)
+    assert TL.rel_l2(f(n["h"]), h64) <= 2.0 ** -8
+    assert TL.rel_l2(f(dx), rdx) <= 5 * 2.0 ** -8 and TL.rel_l2(f(dgamma), rdg) <= 5 * 2.0 ** -8
+    assert TL.rel_l2(f(tied), rtied) <= 5 * 2.0 ** -8
+    assert TL.rel_l2(f(emb), M.embed_fwd(f(W), y.cpu().numpy(), 16.0)) <= 2.0 ** -8

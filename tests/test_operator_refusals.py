@@ -89,6 +89,51 @@ def test_lmhead_q8_refusals(lib, fake):
     assert call(h=P + 8) == INVALID and call(w=P + 8) == INVALID and call(out=P + 1) == INVALID
 
 
+def test_distill_refusals(lib, fake):
+    T, d, V, R, K = 300, 64, 200, 3, 5
+    need = (lib.aero_distill_fwd_workspace_bytes(T, d, V, R, K), lib.aero_distill_bwd_workspace_bytes(T, d, V, R, K, 128, 1),
+            lib.aero_distill_fwd_bwd_workspace_bytes(T, d, V, R, K, 128, 1))
+
+    def args(kw):
+        a = dict(ctx=fake, c=cfg(), T=T, d=d, V=V, R=R, K=K, H=P, W=P, ids=P, logits=P, tlse=None, cs=P, w=P, keep=P,
+                 lse=P, kl=P, loss=P, met=None, gs=1.0, dH=P, dW=P, dt=1, acc=0, ws=P, wsb=None)
+        a.update(kw)
+        return a
+
+    def fwd(**kw):
+        a = args(kw)
+        return lib.aero_distill_fwd(*[a[k] for k in "ctx c T d V R K H W ids logits tlse cs w keep lse kl loss met ws".split()],
+                                    need[0] if a["wsb"] is None else a["wsb"])
+
+    def bwd(**kw):
+        a = args(kw)
+        return lib.aero_distill_bwd(*[a[k] for k in "ctx c T d V R K H W ids logits tlse cs w keep lse gs dH dW dt acc ws".split()],
+                                    need[1] if a["wsb"] is None else a["wsb"])
+
+    def both(**kw):
+        a = args(kw)
+        return lib.aero_distill_fwd_bwd(
+            *[a[k] for k in "ctx c T d V R K H W ids logits tlse cs w keep lse kl loss met gs dH dW dt acc ws".split()],
+            need[2] if a["wsb"] is None else a["wsb"])
+
+    for call, own in ((fwd, "lse kl loss"), (bwd, "lse dH dW"), (both, "lse kl loss dH dW")):
+        for name in ("ctx H W ids logits cs w keep ws " + own).split():
+            assert call(**{name: None}) == INVALID, name
+        assert call(K=0) == INVALID and call(T=-1) == INVALID and call(T=1 << 31) == INVALID and call(R=-1) == INVALID
+        assert call(K=257) == UNSUPPORTED and call(d=96) == UNSUPPORTED and call(c=cfg(9)) == UNSUPPORTED
+        assert call(H=P + 8) == INVALID and call(W=P + 8) == INVALID and call(ws=P + 16) == INVALID
+        assert call(wsb=64) == WORKSPACE
+    for call in (bwd, both):
+        assert call(dH=P + 8) == INVALID and call(dW=P + 4) == INVALID
+        assert call(dt=7) == UNSUPPORTED and call(dt=B.AERO_BF16, acc=1) == INVALID
+        assert call(dt=B.AERO_BF16, c=cfg(B.AERO_FP32)) == UNSUPPORTED
+    # a bf16 dW of several chunks needs room for its fp32 sums; of one chunk it does not
+    assert both(dt=B.AERO_BF16) == WORKSPACE and bwd(dt=B.AERO_BF16) == WORKSPACE
+    size = lambda chunk, dt: lib.aero_distill_fwd_bwd_workspace_bytes(T, d, V, R, K, chunk, dt)
+    assert size(128, B.AERO_BF16) - size(128, B.AERO_FP32) >= 4 * V * d
+    assert size(T + 128 * (R + 2), B.AERO_BF16) == size(T + 128 * (R + 2), B.AERO_FP32)
+
+
 def test_binding_checks_type_shape_device_and_layout():
     ctx = B.Context.__new__(B.Context)
     ctx.device = torch.device("cpu")

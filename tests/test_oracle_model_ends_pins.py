@@ -69,3 +69,64 @@ def test_8bit_product_by_scalar_loops():
     for t in range(3):
         for v in range(5):
             assert z[t, v] == pytest.approx(sum(int(a) * int(b) for a, b in zip(h8[t], w8[v])) * sh[t] * sw[v], rel=1e-14)
+
+
+def _distill_case(seed=0, T=9, d=5, V=12, K=4):
+    rng = np.random.default_rng(seed)
+    H, W = rng.standard_normal((T, d)), rng.standard_normal((V, d))
+    ids = np.stack([rng.choice(V, K, replace=False) for _ in range(T)])
+    logits = rng.standard_normal((T, K)) * 2
+    ids[1, 2:] = M.NO_TOKEN
+    ids[2] = M.NO_TOKEN
+    ids[3, 1] = ids[3, 0]                       # a token listed twice
+    logits[4, 0] = -np.inf
+    cs, keep, w = np.array([0, 3, 5, T]), np.array([1, 0, 1]), np.array([0.3, 0.0, 0.2])
+    return H, W, ids, logits, cs, w, keep
+
+
+@pytest.mark.parametrize("given_lse", [False, True])
+def test_distillation_against_autograd_of_its_definition(given_lse):
+    H, W, ids, logits, cs, w, keep = _distill_case(1)
+    tl = np.full(len(H), 3.0) if given_lse else None
+    got = M.distill(H, W, ids, logits, cs, w, keep, tl, grad_scale=1.3)
+    Ht, Wt = torch.tensor(H, requires_grad=True), torch.tensor(W, requires_grad=True)
+    logp = torch.log_softmax(Ht @ Wt.T, dim=1)
+    loss = 0.0
+    for i in range(3):
+        for t in range(cs[i], cs[i + 1] if keep[i] else cs[i]):
+            place = [k for k in range(ids.shape[1]) if ids[t, k] >= 0 and logits[t, k] > -np.inf]
+            a = torch.tensor([logits[t, k] for k in place], dtype=torch.float64)
+            lq = a - (tl[t] if given_lse else torch.logsumexp(a, 0)) if place else a
+            for j, k in enumerate(place):
+                loss = loss + w[i] * torch.exp(lq[j]) * (lq[j] - logp[t, ids[t, k]])
+    (1.3 * loss).backward()
+    assert got["loss"] == pytest.approx(loss.item(), rel=1e-12)
+    assert np.allclose(got["dH"], Ht.grad.numpy(), rtol=1e-10, atol=1e-13)
+    assert np.allclose(got["dW"], Wt.grad.numpy(), rtol=1e-10, atol=1e-13)
+    assert got["kl"][2] == 0 and not got["dH"][2].any() and not got["dH"][3:5].any() and not got["lse"][3:5].any()
+
+
+def test_distillation_gradient_against_differences():
+    H, W, ids, logits, cs, w, keep = _distill_case(2)
+    got = M.distill(H, W, ids, logits, cs, w, keep)
+    step = 1e-6
+    for t, k in ((0, 0), (1, 3), (5, 2), (8, 4)):
+        e = np.zeros_like(H)
+        e[t, k] = step
+        f = lambda s: M.distill(H + s * e, W, ids, logits, cs, w, keep)["loss"]
+        assert got["dH"][t, k] == pytest.approx((f(1) - f(-1)) / (2 * step), rel=1e-5, abs=1e-9)
+    for v, k in ((0, 1), (7, 4), (11, 0)):
+        e = np.zeros_like(W)
+        e[v, k] = step
+        f = lambda s: M.distill(H, W + s * e, ids, logits, cs, w, keep)["loss"]
+        assert got["dW"][v, k] == pytest.approx((f(1) - f(-1)) / (2 * step), rel=1e-5, abs=1e-9)
+
+
+def test_distillation_from_the_policy_itself_is_at_its_minimum():
+    """The whole vocabulary listed with the student's own logits: kl = 0 and no gradient; columns of dW sum to 0."""
+    H, W, _, _, cs, w, keep = _distill_case(3)
+    z = H @ W.T
+    got = M.distill(H, W, np.tile(np.arange(len(W)), (len(H), 1)), z, cs, w, keep)
+    assert np.abs(got["kl"]).max() < 1e-12 and np.abs(got["dH"]).max() < 1e-12
+    ids, logits = _distill_case(3)[2:4]
+    assert np.abs(M.distill(H, W, ids, logits, cs, w, keep)["dW"].sum(axis=0)).max() < 1e-12
