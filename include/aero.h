@@ -595,12 +595,12 @@ int aero_distill_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t 
  * dW [V,d] f32 is overwritten or, when accumulate_dW != 0, added to -- with tied weights the dW of
  * stage (b).  The rows of one token are added in an order that depends on y alone, without atomics:
  * repeated calls give the same bits.  y [T] i32.  d up to 65536, any element-aligned base.
- * workspace: at least aero_embed_workspace_bytes(T, d) bytes, 256-byte aligned.
+ * workspace: at least aero_embed_workspace_bytes(T, d, V) bytes, 256-byte aligned.
  */
 int aero_embed_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, const int32_t* y, const void* W,
                    float scale, void* X);
 
-size_t aero_embed_workspace_bytes(int64_t T, int32_t d);
+size_t aero_embed_workspace_bytes(int64_t T, int32_t d, int32_t V);
 
 int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, const int32_t* y, const void* dX,
                    float scale, float* dW, int accumulate_dW, void* workspace, size_t workspace_bytes);

@@ -128,7 +128,7 @@ def load_library():
     lib.aero_quantize_rows.argtypes = [vp, cp, i64, i32] + [vp] * 3
     lib.aero_embed_fwd.argtypes = [vp, cp, i64, i32, i32, vp, vp, f32, vp]
     lib.aero_embed_workspace_bytes.restype = sz
-    lib.aero_embed_workspace_bytes.argtypes = [i64, i32]
+    lib.aero_embed_workspace_bytes.argtypes = [i64, i32, i32]
     lib.aero_embed_bwd.argtypes = [vp, cp, i64, i32, i32, vp, vp, f32, vp, C.c_int, vp, sz]
     lib.aero_lmhead_q8.argtypes = [vp, i64, i32, i32, vp, vp, vp, vp, i32, vp]
     shape = [vp, cp, i64, i32, i32, i32, i32]
@@ -499,6 +499,8 @@ class Context:
 
     def _new(self, shape, dtype):
         """An output tensor allocated for the context's stream, where the kernels that write it run."""
+        if torch._C._cuda_getCurrentRawStream(self.device.index) == self.stream.cuda_stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
@@ -582,7 +584,7 @@ class Context:
         if accumulate_dW and dW is None:
             raise AeroError("accumulate_dW needs the dW to add to")
         dW = dW if dW is not None else self._new((V, d), torch.float32)
-        ws = self._scratch(self.lib.aero_embed_workspace_bytes(T, d))
+        ws = self._scratch(self.lib.aero_embed_workspace_bytes(T, d, V))
         rc = self.lib.aero_embed_bwd(self.h, C.byref(cfg), T, d, V, self._arg(y, torch.int32, (T,), "y"),
                                      self._arg(dX, dt, (T, d), "dX"), scale,
                                      self._arg(dW, torch.float32, (V, d), "dW"), 1 if accumulate_dW else 0,

@@ -8,6 +8,10 @@
 // that makes up a tenth of the batch costs no more than any other: a warp adds the rows of its tile,
 // writes the sums of tokens that lie inside the tile, and leaves those that reach over its ends as
 // partial rows, which one more kernel joins.
+//
+// Bound by memory: dX is read once and every row of dW written once.  A dW that is overwritten is not
+// cleared beforehand: the rows of tokens that do not occur are cleared by blocks of their own, which run
+// beside the sort, whose few blocks leave the memory idle.
 #include "entry.cuh"
 #include "vec.cuh"
 
@@ -15,10 +19,9 @@
 
 namespace {
 
-constexpr int kSmallT = 2048;
-constexpr int kSortTile = 4096, kSortThreads = 256, kSortWarps = kSortThreads / 32;
+constexpr int kSmallT = 4096;
+constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 constexpr int kMaxRadix = 512;
-constexpr int kTile = 32;             // sorted positions per warp of the summing kernel
 
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) embed_fwd_kernel(long long T_, int d, int V, const int32_t* __restrict__ y,
@@ -71,55 +74,103 @@ __device__ __forceinline__ void put(float* dst, const float (&s)[VEC], float sca
   }
 }
 
-// Block (t, slab): the first occurrence of a token adds the rows of all its occurrences, in order.
+// Blocks from `first` on clear the rows v0 .. v1 - 1 of dW whose token does not occur.
+struct Clear {
+  float* dW;               // NULL: nothing to clear
+  const uint8_t* occurs;   // [V]
+  int d, v0, v1;
+  unsigned first;
+};
+
+__device__ __forceinline__ bool clear_rows(const Clear& z) {
+  if (blockIdx.x < z.first) return false;
+  const int lane = threadIdx.x & 31, per_block = blockDim.x >> 5;
+  const bool vec = z.d % 4 == 0 && (reinterpret_cast<uintptr_t>(z.dW) & 15u) == 0;
+  constexpr int G = 8;                                   // rows a warp looks at together
+  const long long step = (long long)(gridDim.x - z.first) * per_block * G;
+  for (long long v = z.v0 + ((long long)(blockIdx.x - z.first) * per_block + (threadIdx.x >> 5)) * G; v < z.v1; v += step) {
+    unsigned absent = __ballot_sync(0xffffffffu, lane < G && v + lane < z.v1 && !z.occurs[v + lane]);
+    for (; absent != 0; absent &= absent - 1) {
+      float* row = z.dW + (v + __ffs(absent) - 1) * z.d;
+      if (vec) {
+        for (int k = lane; k < z.d / 4; k += 32) reinterpret_cast<float4*>(row)[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      } else {
+        for (int k = lane; k < z.d; k += 32) row[k] = 0.f;
+      }
+    }
+  }
+  return true;
+}
+
+// Block (t, y): the first occurrence of a token adds the rows of all its occurrences, slabs of 32 * VEC columns y,
+// y + gridDim.y, ...  Each warp looks through a quarter of the ids and adds the rows it finds, in order; the four
+// sums are added in order.  A block whose token occurs earlier leaves.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int V, const int32_t* __restrict__ y,
                                                               const T* __restrict__ dX, float scale, float* __restrict__ dW,
                                                               int accumulate, uint32_t* status) {
-  __shared__ int list[128];
-  __shared__ int n_in_warp[4];
-  const int t = blockIdx.x, c = (blockIdx.y * 128 + threadIdx.x) * VEC;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  using Raw = typename rowvec::Raw<T, VEC>::type;
+  __shared__ uint16_t list[4][kSmallT / 4];
+  __shared__ int found[4];
+  __shared__ float sums[3][32 * VEC];
+  const int t = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int id = y[t];
   if (id < 0 || id >= V) {
     if (id != AERO_NO_TOKEN && blockIdx.y == 0 && threadIdx.x == 0) aero_raise(status, AERO_ST_BAD_TARGET);
     return;
   }
-  bool seen = false;
-  for (int j = threadIdx.x; j < t; j += 128) seen |= y[j] == id;
-  if (__syncthreads_or(seen)) return;                  // an earlier block has this token
-  float acc[VEC];
+  const int p0 = (int)((long long)T_ * warp / 4), p1 = (int)((long long)T_ * (warp + 1) / 4);
+  int n = 0, first = 0x7fffffff;
+#pragma unroll 4
+  for (int base = p0; base < p1; base += 32) {
+    const int p = base + lane;
+    const unsigned hits = __ballot_sync(0xffffffffu, p < p1 && y[p] == id);
+    if (hits >> lane & 1u) list[warp][n + __popc(hits & ((1u << lane) - 1u))] = (uint16_t)p;
+    if (hits && n == 0) first = base + __ffs(hits) - 1;
+    n += __popc(hits);
+  }
+  if (lane == 0) found[warp] = n;
+  if (__syncthreads_or(first < t)) return;             // an earlier block has this token
+  const int all = found[0] + found[1] + found[2] + found[3];
+  bool alone = false;
+  for (int w = 0; w < 4; ++w) alone |= found[w] == all;          // (the same answer in all four warps)
+  for (int c = (blockIdx.y * 32 + lane) * VEC; c - lane * VEC < d; c += gridDim.y * 32 * VEC) {
+    float acc[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-  for (int base = t; base < T_; base += 128) {
-    const int j = base + threadIdx.x;
-    const bool hit = j < T_ && y[j] == id;
-    const unsigned mask = __ballot_sync(0xffffffffu, hit);
-    if (lane == 0) n_in_warp[warp] = __popc(mask);
-    __syncthreads();
-    int off = 0, n = 0;
-    for (int w = 0; w < 4; ++w) {
-      if (w < warp) off += n_in_warp[w];
-      n += n_in_warp[w];
-    }
-    if (hit) list[off + __popc(mask & ((1u << lane) - 1u))] = j;
-    __syncthreads();
-    if (c < d) {
-      for (int k = 0; k < n; k += 4) {
-        float f[4][VEC];
+    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+    constexpr int U = 4;
+    for (int k = 0; k < n && c < d; k += U) {
+      Raw raw[U];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (k + q < n) rowvec::load<T, VEC>(dX + (long long)list[k + q] * d + c, f[q]);
+      for (int q = 0; q < U; ++q)
+        if (k + q < n) raw[q] = *reinterpret_cast<const Raw*>(dX + (long long)list[warp][k + q] * d + c);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-          if (k + q < n)
+      for (int q = 0; q < U; ++q) {
+        if (k + q < n) {
+          float f[VEC];
+          rowvec::open<T, VEC>(raw[q], f);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] += f[q][e];
+          for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+        }
       }
+    }
+    if (alone) {                                         // all occurrences in one warp's quarter (often only one): no join
+      if (n > 0 && c < d) put<VEC>(dW + (long long)id * d + c, acc, scale, accumulate != 0);
+      continue;
+    }
+    if (warp < 3) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sums[warp][e * 32 + lane] = acc[e];
+    }
+    __syncthreads();
+    if (warp == 3 && c < d) {
+      float s[VEC];
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s[e] = (sums[0][e * 32 + lane] + sums[1][e * 32 + lane]) + (sums[2][e * 32 + lane] + acc[e]);
+      put<VEC>(dW + (long long)id * d + c, s, scale, accumulate != 0);
     }
     __syncthreads();
   }
-  if (c < d) put<VEC>(dW + (long long)id * d + c, acc, scale, accumulate != 0);
 }
 
 // ---- stable radix sort of the positions by token -------------------------------------------------
@@ -134,66 +185,74 @@ __device__ __forceinline__ uint32_t key_of(const int32_t* y, const uint32_t* key
 
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(int n, int V, const int32_t* __restrict__ y,
                                                                   const uint32_t* __restrict__ keys, int shift, int radix,
-                                                                  uint32_t* __restrict__ counts, uint32_t* status) {
+                                                                  int blocks, uint32_t* __restrict__ counts,
+                                                                  uint8_t* __restrict__ occurs, Clear z, uint32_t* status) {
   __shared__ uint32_t h[kMaxRadix];
+  if (clear_rows(z)) return;
   for (int i = threadIdx.x; i < radix; i += kSortThreads) h[i] = 0;
   __syncthreads();
   const int base = blockIdx.x * kSortTile;
   bool bad = false;
-  for (int k = threadIdx.x; k < kSortTile && base + k < n; k += kSortThreads) {
+#pragma unroll
+  for (int k = threadIdx.x; k < kSortTile; k += kSortThreads) {
+    if (base + k >= n) continue;
     const uint32_t key = key_of(y, keys, base + k, V);
     if (!keys && key == (uint32_t)V) bad |= y[base + k] != AERO_NO_TOKEN;
+    if (occurs && key != (uint32_t)V) occurs[key] = 1;
     atomicAdd(&h[(key >> shift) & (radix - 1)], 1u);
   }
   if (bad) aero_raise(status, AERO_ST_BAD_TARGET);
   __syncthreads();
-  for (int i = threadIdx.x; i < radix; i += kSortThreads) counts[(size_t)i * gridDim.x + blockIdx.x] = h[i];
+  for (int i = threadIdx.x; i < radix; i += kSortThreads) counts[(size_t)i * blocks + blockIdx.x] = h[i];
 }
 
-// exclusive prefix of n counts in place, one block
-__global__ void __launch_bounds__(1024) sort_prefix_kernel(uint32_t* __restrict__ counts, int n) {
-  __shared__ uint32_t warp_sum[32];
+// exclusive prefix of n counts (a multiple of 4) in place, one block
+__global__ void __launch_bounds__(1024) sort_prefix_kernel(uint4* __restrict__ counts, int n, Clear z) {
+  __shared__ uint32_t warp_sum[2][32];
+  if (clear_rows(z)) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   uint32_t carry = 0;
-  for (int base = 0; base < n; base += 4096) {
-    const int i = base + threadIdx.x * 4;
-    uint32_t v[4], sum = 0;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      v[q] = i + q < n ? counts[i + q] : 0u;
-      sum += v[q];
-    }
+  int turn = 0;
+  uint4 next = (int)threadIdx.x < n / 4 ? counts[threadIdx.x] : make_uint4(0, 0, 0, 0);
+  for (int base = 0; base < n / 4; base += 1024, turn ^= 1) {
+    const int i = base + threadIdx.x;
+    const uint4 v = next;
+    next = i + 1024 < n / 4 ? counts[i + 1024] : make_uint4(0, 0, 0, 0);
+    const uint32_t sum = v.x + v.y + v.z + v.w;
     uint32_t incl = sum;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += u;
     }
-    if (lane == 31) warp_sum[warp] = incl;
+    if (lane == 31) warp_sum[turn][warp] = incl;
     __syncthreads();
-    uint32_t before = 0, total = 0;
-    for (int w = 0; w < 32; ++w) {
-      if (w < warp) before += warp_sum[w];
-      total += warp_sum[w];
-    }
-    uint32_t run = carry + before + incl - sum;
+    // every warp scans the 32 warps' sums for itself
+    uint32_t w = warp_sum[turn][lane];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if (i + q < n) counts[i + q] = run;
-      run += v[q];
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t u = __shfl_up_sync(0xffffffffu, w, o);
+      if (lane >= o) w += u;
     }
+    const uint32_t before = warp > 0 ? __shfl_sync(0xffffffffu, w, warp - 1) : 0u, total = __shfl_sync(0xffffffffu, w, 31);
+    uint4 r;
+    r.x = carry + before + incl - sum;
+    r.y = r.x + v.x;
+    r.z = r.y + v.y;
+    r.w = r.z + v.z;
+    if (i < n / 4) counts[i] = r;
     carry += total;
-    __syncthreads();
   }
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int n, int V, const int32_t* __restrict__ y,
                                                                     const uint32_t* __restrict__ keys,
                                                                     const uint32_t* __restrict__ pos, int shift, int radix,
-                                                                    const uint32_t* __restrict__ starts,
+                                                                    int blocks, const uint32_t* __restrict__ starts,
                                                                     uint32_t* __restrict__ keys_out,
-                                                                    uint32_t* __restrict__ pos_out) {
+                                                                    uint32_t* __restrict__ pos_out, Clear z) {
   __shared__ uint32_t h[kSortWarps][kMaxRadix];
+  if (clear_rows(z)) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kSortWarps * radix; i += kSortThreads) h[i / radix][i % radix] = 0;
   __syncthreads();
@@ -217,7 +276,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int n, int V
   }
   __syncthreads();
   for (int g = threadIdx.x; g < radix; g += kSortThreads) {
-    uint32_t run = starts[(size_t)g * gridDim.x + blockIdx.x];
+    uint32_t run = starts[(size_t)g * blocks + blockIdx.x];
     for (int w = 0; w < kSortWarps; ++w) {
       const uint32_t c = h[w][g];
       h[w][g] = run;
@@ -237,105 +296,164 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int n, int V
 }
 
 // ---- sums over the sorted positions ----------------------------------------------------------------
-// Warp (tile, slab): tile = kTile sorted positions, slab = 32 * VEC columns.  A run of equal keys that
-// lies inside the tile goes to dW; one that continues from the tile before goes to part[tile][0], one
-// that starts here and continues in the tile after to part[tile][1].
+// Warp (tile, slab): tile = kTile sorted positions, slab = 32 * VEC columns.  A run of equal keys that lies inside the
+// tile goes to dW; one that continues from the tile before goes to part[tile][0], one that starts here and continues
+// in the tile after to part[tile][1].  Rows are held packed and two are in flight beyond the two being added: more per
+// warp costs registers, and it is warps that keep the memory busy (204780 x 1536: 379 us with eight unpacked rows a
+// turn, 202 with four packed ones, 173 with two; 277 with tiles of 128 positions).
+constexpr int kTile = 32, kInFlight = 2;
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) embed_bwd_sum_kernel(int n, int d, int V, const uint32_t* __restrict__ keys,
                                                             const uint32_t* __restrict__ pos, const T* __restrict__ dX,
                                                             float scale, float* __restrict__ dW, int accumulate,
                                                             float* __restrict__ part) {
+  using Raw = typename rowvec::Raw<T, VEC>::type;
+  constexpr int U = kInFlight;
   const int lane = threadIdx.x & 31;
   const int slabs = (d + 32 * VEC - 1) / (32 * VEC);
   const long long u = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   const long long tile = u / slabs;
-  const int p0 = (int)(tile * kTile);
   if (tile * kTile >= n) return;
+  const int p0 = (int)(tile * kTile), count = min(kTile, n - p0);
   const int c = ((int)(u - tile * slabs) * 32 + lane) * VEC;
-  const int count = min(kTile, n - p0);
-  const uint32_t my_key = lane < count ? keys[p0 + lane] : (uint32_t)V;
+  const uint32_t none = (uint32_t)V;
+  const uint32_t my_key = lane < count ? keys[p0 + lane] : none;
   const uint32_t my_pos = lane < count ? pos[p0 + lane] : 0u;
-  const uint32_t before = p0 > 0 ? keys[p0 - 1] : (uint32_t)V;
-  const uint32_t after = p0 + count < n ? keys[p0 + count] : (uint32_t)V;
+  const uint32_t before = p0 > 0 ? keys[p0 - 1] : none;
+  const uint32_t after = p0 + count < n ? keys[p0 + count] : none;
+  // positions without a token are sorted last: the first `live` positions have one
+  const int live = __popc(__ballot_sync(0xffffffffu, my_key != none));
   float acc[VEC];
 #pragma unroll
   for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
   int run0 = 0;                                          // first position of the current run
-  constexpr int U = 8;
-  for (int k = 0; k < count; k += U) {
-    if (__shfl_sync(0xffffffffu, my_key, k) == (uint32_t)V) break;       // only positions without a token follow
-    float f[U][VEC];
+  Raw next[U];
+  auto fetch = [&](int k) {
 #pragma unroll
     for (int q = 0; q < U; ++q) {
-      const uint32_t row = __shfl_sync(0xffffffffu, my_pos, k + q), key = __shfl_sync(0xffffffffu, my_key, k + q);
-      if (key != (uint32_t)V && c < d) rowvec::load<T, VEC>(dX + (long long)row * d + c, f[q]);
+      const uint32_t row = __shfl_sync(0xffffffffu, my_pos, (k + q) & 31);
+      if (k + q < live && c < d) next[q] = *reinterpret_cast<const Raw*>(dX + (long long)row * d + c);
     }
+  };
+  fetch(0);
+  for (int k = 0; k < live; k += U) {
+    Raw cur[U];
+#pragma unroll
+    for (int q = 0; q < U; ++q) cur[q] = next[q];
+    fetch(k + U);
 #pragma unroll
     for (int q = 0; q < U; ++q) {
-      const uint32_t key = __shfl_sync(0xffffffffu, my_key, k + q);
-      if (key == (uint32_t)V) break;
+      if (k + q < live) {
+        const uint32_t key = __shfl_sync(0xffffffffu, my_key, k + q);
+        float f[VEC];
+        rowvec::open<T, VEC>(cur[q], f);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] += f[q][e];
-      const bool last = k + q + 1 >= count;
-      const uint32_t next = last ? after : __shfl_sync(0xffffffffu, my_key, (k + q + 1) & 31);
-      if (next != key || last) {
-        const bool head = run0 == 0 && before == key, tail = last && next == key;
-        if (c < d) {
-          if (head || tail) put<VEC>(part + ((size_t)tile * 2 + (head ? 0 : 1)) * d + c, acc, 1.f, false);
-          else put<VEC>(dW + (long long)key * d + c, acc, scale, accumulate != 0);
+        for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+        const bool last = k + q + 1 >= count;
+        const uint32_t following = last ? after : __shfl_sync(0xffffffffu, my_key, (k + q + 1) & 31);
+        if (following != key || last) {
+          const bool head = run0 == 0 && before == key, tail = last && following == key;
+          if (c < d) {
+            if (head || tail) put<VEC>(part + ((size_t)tile * 2 + (head ? 0 : 1)) * d + c, acc, 1.f, false);
+            else put<VEC>(dW + (long long)key * d + c, acc, scale, accumulate != 0);
+          }
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+          run0 = k + q + 1;
         }
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-        run0 = k + q + 1;
       }
     }
   }
 }
 
-// A run that starts in tile b and reaches into the tiles after it: block (b, 128 columns), eight warps
-// take a contiguous eighth of the tiles each, added up in order.
+// Runs that start in a tile and reach into the tiles after it.  A block looks at kJoin tiles and 128 columns: a run of
+// a few tiles is added up by one warp, a longer one by all eight, a contiguous eighth of its tiles each, in order.
+constexpr int kJoin = 32, kShortRun = 8;
 __global__ void __launch_bounds__(256) embed_bwd_join_kernel(int n, int d, int V, const uint32_t* __restrict__ keys,
                                                              const float* __restrict__ part, float scale,
                                                              float* __restrict__ dW, int accumulate) {
   __shared__ float sh[8][128];
-  const long long b = blockIdx.x;
-  const long long end = (b + 1) * kTile;                 // first position of the next tile
-  if (end >= n) return;
-  const uint32_t key = keys[end - 1];
-  if (key == (uint32_t)V || keys[end] != key) return;
-  const bool starts_here = keys[b * kTile] != key || b == 0 || keys[b * kTile - 1] != key;
-  if (!starts_here) return;
-  // last position of the run by bisection: keys are sorted
-  long long lo = end, hi = n;                            // keys[lo] == key, keys[hi] != key
-  while (hi - lo > 1) {
-    const long long mid = (lo + hi) >> 1;
-    if (keys[mid] == key) lo = mid; else hi = mid;
+  __shared__ int long_last[kJoin];
+  __shared__ unsigned starts;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.y * 128;
+  const int tiles = (n + kTile - 1) / kTile;
+  if (warp == 0) {
+    // a lane per tile: does a run start in it and go on in the next one?
+    const long long b = (long long)blockIdx.x * kJoin + lane, end = (b + 1) * kTile;
+    bool yes = false;
+    if (b + 1 < tiles) {
+      const uint32_t key = keys[end - 1];
+      yes = key != (uint32_t)V && keys[end] == key && (keys[end - kTile] != key || b == 0 || keys[end - kTile - 1] != key);
+    }
+    const unsigned m = __ballot_sync(0xffffffffu, yes);
+    long_last[lane] = -1;
+    if (lane == 0) starts = m;
   }
-  const long long last = lo / kTile;                     // the run's last tile; tiles b + 1 .. last hold it in slot 0
-  const long long count = last - b;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int c0 = blockIdx.y * 128;
-  float acc[4] = {0.f, 0.f, 0.f, 0.f};
-  const long long k0 = b + 1 + count * warp / 8, k1 = b + 1 + count * (warp + 1) / 8;
-#pragma unroll 4
-  for (long long k = k0; k < k1; ++k) {
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (c0 + q * 32 + lane < d) acc[q] += part[(size_t)k * 2 * d + c0 + q * 32 + lane];
-  }
-#pragma unroll
-  for (int q = 0; q < 4; ++q) sh[warp][q * 32 + lane] = acc[q];
   __syncthreads();
-  if (threadIdx.x < 128 && c0 + (int)threadIdx.x < d) {
-    const int c = c0 + threadIdx.x;
-    float sum = part[((size_t)b * 2 + 1) * d + c];
-    for (int w = 0; w < 8; ++w) sum += sh[w][threadIdx.x];
+  if (starts == 0) return;
+  int col[4];                                                    // (columns past d read the last one and are dropped)
+#pragma unroll
+  for (int q = 0; q < 4; ++q) col[q] = min(c0 + q * 32 + lane, d - 1);
+  auto add = [&](int k0, int k1, float (&acc)[4]) {              // slot 0 of tiles k0 .. k1 - 1, 32 loads in flight
+    for (int k = k0; k < k1; k += 8) {
+      float v[8][4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[i][q] = part[(size_t)min(k + i, k1 - 1) * 2 * d + col[q]];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) acc[q] += k + i < k1 ? v[i][q] : 0.f;
+    }
+  };
+  auto finish = [&](int b, uint32_t key, int c, float sum) {     // + the run's share of its first tile (slot 1)
+    sum += part[((size_t)b * 2 + 1) * d + c];
     float* dst = dW + (long long)key * d + c;
     *dst = accumulate ? fmaf(sum, scale, *dst) : sum * scale;
+  };
+  for (int i = warp; i < kJoin; i += 8) {
+    if (!(starts >> i & 1u)) continue;
+    const int b = blockIdx.x * kJoin + i;
+    const uint32_t key = keys[((long long)b + 1) * kTile - 1];
+    // the run's last tile: tiles b + 1 .. last start with its key, those after do not; a search 32 tiles wide
+    int lo = b + 1, hi = tiles;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 31) / 32, k = lo + (lane + 1) * step;
+      const int ahead = __popc(__ballot_sync(0xffffffffu, k < hi && keys[(long long)k * kTile] == key));
+      hi = min(hi, lo + (ahead + 1) * step);
+      lo += ahead * step;
+    }
+    if (lo - b > kShortRun) {
+      if (lane == 0) long_last[i] = lo;
+      continue;
+    }
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    add(b + 1, lo + 1, acc);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (c0 + q * 32 + lane < d) finish(b, key, c0 + q * 32 + lane, acc[q]);
+  }
+  __syncthreads();
+  for (int i = 0; i < kJoin; ++i) {
+    if (long_last[i] < 0) continue;
+    const int b = blockIdx.x * kJoin + i, count = long_last[i] - b;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    add(b + 1 + (int)((long long)count * warp / 8), b + 1 + (int)((long long)count * (warp + 1) / 8), acc);
+    __syncthreads();                                             // the previous run's sums have been read
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sh[warp][q * 32 + lane] = acc[q];
+    __syncthreads();
+    if (threadIdx.x < 128 && c0 + (int)threadIdx.x < d) {
+      float sum = 0.f;
+      for (int w = 0; w < 8; ++w) sum += sh[w][threadIdx.x];
+      finish(b, keys[((long long)b + 1) * kTile - 1], c0 + threadIdx.x, sum);
+    }
   }
 }
 
 struct Ws {
+  uint8_t* occurs;
   uint32_t* keys[2];
   uint32_t* pos[2];
   uint32_t* counts;
@@ -343,35 +461,56 @@ struct Ws {
   size_t bytes;
 };
 
-Ws carve(void* base, int64_t T, int32_t d) {
-  Ws w;
+Ws carve(void* base, int64_t T, int32_t d, int32_t V) {
+  Ws w = {};
   char* p = static_cast<char*>(base);
   size_t off = 0;
-  const size_t arr = aero_align_up((size_t)T * sizeof(uint32_t), 256);
-  for (int i = 0; i < 2; ++i) {
-    w.keys[i] = reinterpret_cast<uint32_t*>(p + off); off += arr;
-    w.pos[i] = reinterpret_cast<uint32_t*>(p + off); off += arr;
+  auto take = [&](size_t bytes) { char* r = p + off; off += aero_align_up(bytes, 256); return r; };
+  if (T > kSmallT) {
+    w.occurs = reinterpret_cast<uint8_t*>(take((size_t)V));
+    for (int i = 0; i < 2; ++i) {
+      w.keys[i] = reinterpret_cast<uint32_t*>(take((size_t)T * sizeof(uint32_t)));
+      w.pos[i] = reinterpret_cast<uint32_t*>(take((size_t)T * sizeof(uint32_t)));
+    }
+    const size_t blocks = ((size_t)T + kSortTile - 1) / kSortTile, tiles = ((size_t)T + kTile - 1) / kTile;
+    w.counts = reinterpret_cast<uint32_t*>(take(blocks * kMaxRadix * sizeof(uint32_t)));
+    w.part = reinterpret_cast<float*>(take(tiles * 2 * (size_t)d * sizeof(float)));
   }
-  const size_t blocks = ((size_t)T + kSortTile - 1) / kSortTile;
-  w.counts = reinterpret_cast<uint32_t*>(p + off); off += aero_align_up(blocks * kMaxRadix * sizeof(uint32_t), 256);
-  const size_t tiles = ((size_t)T + kTile - 1) / kTile;
-  w.part = reinterpret_cast<float*>(p + off); off += aero_align_up(tiles * 2 * (size_t)d * sizeof(float), 256);
-  w.bytes = off;
+  w.bytes = off > 0 ? off : 256;
   return w;
 }
 
-int sort_positions(aero_ctx* ctx, const Ws& w, int n, int V, const int32_t* y, const uint32_t** keys, const uint32_t** pos) {
+// The sort's launches clear an equal share of the rows of dW each (all but the first, which finds the tokens).
+int sort_positions(aero_ctx* ctx, const Ws& w, int n, int d, int V, const int32_t* y, float* clear, const uint32_t** keys,
+                   const uint32_t** pos) {
   int bits = 1;
   while (bits < 32 && ((uint32_t)V >> bits) != 0) ++bits;          // the keys are 0 .. V
-  const int passes = (bits + 8) / 9, per = (bits + passes - 1) / passes;
-  const int blocks = (n + kSortTile - 1) / kSortTile;
+  const int passes = (bits + 8) / 9;
+  int per = (bits + passes - 1) / passes;
+  if (per < 2) per = 2;                                            // (counts in fours)
+  const unsigned blocks = (unsigned)((n + kSortTile - 1) / kSortTile);
+  const unsigned helpers = clear ? 4u * (unsigned)ctx->sm_count : 0u;
+  const int shares = 3 * passes - 1;
+  int share = 0;
+  auto next_share = [&](unsigned first) {
+    Clear z = {clear, w.occurs, d, (int)((long long)V * share / shares), (int)((long long)V * (share + 1) / shares), first};
+    ++share;
+    return z;
+  };
+  const Clear none = {nullptr, nullptr, 0, 0, 0, 0xffffffffu};
+  if (clear) AERO_CUDA_TRY(cudaMemsetAsync(w.occurs, 0, (size_t)V, ctx->stream));
   const uint32_t *kin = nullptr, *pin = nullptr;
   for (int p = 0; p < passes; ++p) {
     const int radix = 1 << per, shift = p * per;
-    sort_count_kernel<<<blocks, kSortThreads, 0, ctx->stream>>>(n, V, y, kin, shift, radix, w.counts, ctx->d_status);
-    sort_prefix_kernel<<<1, 1024, 0, ctx->stream>>>(w.counts, radix * blocks);
-    sort_scatter_kernel<<<blocks, kSortThreads, 0, ctx->stream>>>(n, V, y, kin, pin, shift, radix, w.counts, w.keys[p & 1],
-                                                                  w.pos[p & 1]);
+    const bool find = p == 0;
+    sort_count_kernel<<<blocks + (find ? 0u : helpers), kSortThreads, 0, ctx->stream>>>(
+        n, V, y, kin, shift, radix, (int)blocks, w.counts, find && clear ? w.occurs : nullptr,
+        find || !clear ? none : next_share(blocks), ctx->d_status);
+    sort_prefix_kernel<<<1 + helpers / 4, 1024, 0, ctx->stream>>>(reinterpret_cast<uint4*>(w.counts), radix * (int)blocks,
+                                                                  clear ? next_share(1) : none);
+    sort_scatter_kernel<<<blocks + helpers, kSortThreads, 0, ctx->stream>>>(n, V, y, kin, pin, shift, radix, (int)blocks,
+                                                                            w.counts, w.keys[p & 1], w.pos[p & 1],
+                                                                            clear ? next_share(blocks) : none);
     ctx->launches += 3;
     kin = w.keys[p & 1];
     pin = w.pos[p & 1];
@@ -385,22 +524,25 @@ int sort_positions(aero_ctx* ctx, const Ws& w, int n, int V, const int32_t* y, c
 template <typename T, int VEC>
 int bwd_launch(aero_ctx* ctx, int64_t T_, int32_t d, int32_t V, const int32_t* y, const T* dX, float scale, float* dW,
                int accumulate, void* ws) {
+  const Ws w = carve(ws, T_, d, V);
+  const int n = (int)T_;
   if (T_ <= kSmallT) {
-    const dim3 grid((unsigned)T_, (unsigned)((d + 128 * VEC - 1) / (128 * VEC)));
-    embed_bwd_small_kernel<T, VEC><<<grid, 128, 0, ctx->stream>>>((int)T_, d, V, y, dX, scale, dW, accumulate, ctx->d_status);
+    // (the rows of few tokens are written twice at most: clearing all of dW beforehand costs no more)
+    if (!accumulate) AERO_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)V * d * sizeof(float), ctx->stream));
+    const int slabs = (d + 32 * VEC - 1) / (32 * VEC);
+    embed_bwd_small_kernel<T, VEC><<<dim3((unsigned)T_, (unsigned)((slabs + 2) / 3)), 128, 0, ctx->stream>>>(
+        n, d, V, y, dX, scale, dW, accumulate, ctx->d_status);
     ctx->launches += 1;
     AERO_CUDA_TRY(cudaGetLastError());
     return AERO_OK;
   }
-  const Ws w = carve(ws, T_, d);
-  const int n = (int)T_;
   const uint32_t *keys, *pos;
-  const int rc = sort_positions(ctx, w, n, V, y, &keys, &pos);
+  const int rc = sort_positions(ctx, w, n, d, V, y, accumulate ? nullptr : dW, &keys, &pos);
   if (rc) return rc;
   const long long tiles = (n + kTile - 1) / kTile, slabs = (d + 32 * VEC - 1) / (32 * VEC);
   embed_bwd_sum_kernel<T, VEC><<<(unsigned)((tiles * slabs + 7) / 8), 256, 0, ctx->stream>>>(n, d, V, keys, pos, dX, scale, dW,
                                                                                              accumulate, w.part);
-  const dim3 jgrid((unsigned)tiles, (unsigned)((d + 127) / 128));
+  const dim3 jgrid((unsigned)((tiles + kJoin - 1) / kJoin), (unsigned)((d + 127) / 128));
   embed_bwd_join_kernel<<<jgrid, 256, 0, ctx->stream>>>(n, d, V, keys, w.part, scale, dW, accumulate);
   ctx->launches += 2;
   AERO_CUDA_TRY(cudaGetLastError());
@@ -447,9 +589,8 @@ int aero_embed_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int
                                    static_cast<__nv_bfloat16*>(X));
 }
 
-size_t aero_embed_workspace_bytes(int64_t T, int32_t d) {
-  if (T < 0 || d <= 0) return 0;
-  return T <= kSmallT ? 256 : carve(nullptr, T, d).bytes;
+size_t aero_embed_workspace_bytes(int64_t T, int32_t d, int32_t V) {
+  return T < 0 || d <= 0 || V <= 0 ? 0 : carve(nullptr, T, d, V).bytes;
 }
 
 int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, const int32_t* y, const void* dX,
@@ -459,10 +600,12 @@ int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int
   if (rc) return rc;
   if (!ctx || !dW || (T > 0 && (!y || !dX)) || !workspace || !aero_aligned256(workspace)) return AERO_ERR_INVALID;
   if (reinterpret_cast<uintptr_t>(dX) % (cfg->dtype == AERO_FP32 ? 4 : 2)) return AERO_ERR_INVALID;
-  if (workspace_bytes < aero_embed_workspace_bytes(T, d)) return AERO_ERR_WORKSPACE;
+  if (workspace_bytes < aero_embed_workspace_bytes(T, d, V)) return AERO_ERR_WORKSPACE;
   if ((rc = aero_check_ctx(ctx))) return rc;
-  if (!accumulate_dW) AERO_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)V * d * sizeof(float), ctx->stream));
-  if (T == 0) return AERO_OK;
+  if (T == 0) {
+    if (!accumulate_dW) AERO_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)V * d * sizeof(float), ctx->stream));
+    return AERO_OK;
+  }
   const bool al = aero_aligned16(dX) && aero_aligned16(dW);
   if (cfg->dtype == AERO_FP32) {
     const float* x = static_cast<const float*>(dX);

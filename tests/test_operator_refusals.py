@@ -67,8 +67,8 @@ def test_embed_refusals(lib, fake):
     assert fwd(V=0) == INVALID and fwd(T=-1) == INVALID and fwd(d=-8) == INVALID and fwd(W=P + 1) == INVALID
     assert fwd(d=65537) == UNSUPPORTED and fwd(c=cfg(3)) == UNSUPPORTED
 
-    need = lib.aero_embed_workspace_bytes(5000, 64)
-    assert need > 4 * 4 * 5000 and lib.aero_embed_workspace_bytes(4, 64) <= 256
+    need = lib.aero_embed_workspace_bytes(5000, 64, 10)
+    assert need > 4 * 4 * 5000 and lib.aero_embed_workspace_bytes(4, 64, 10) <= 256
 
     def bwd(ctx=fake, T=5000, d=64, V=10, y=P, dX=P, dW=P, ws=P, wsb=need):
         return lib.aero_embed_bwd(ctx, cfg(), T, d, V, y, dX, 1.0, dW, 1, ws, wsb)
