@@ -55,4 +55,13 @@ __device__ __forceinline__ void store(T* p, const float (&f)[VEC]) {
   else *reinterpret_cast<uint4*>(p) = pack(f);
 }
 
+// The same VEC elements as they lie in memory, for loads issued ahead of their use.
+template <typename T, int VEC> struct Raw { using type = uint4; };
+template <typename T> struct Raw<T, 1> { using type = T; };
+template <typename T, int VEC>
+__device__ __forceinline__ void open(const typename Raw<T, VEC>::type& r, float (&f)[VEC]) {
+  if constexpr (VEC == 1) f[0] = Elem<T>::load(&r);
+  else unpack(r, f);
+}
+
 }  // namespace rowvec
