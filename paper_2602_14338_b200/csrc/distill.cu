@@ -5,14 +5,14 @@
 //   dz_tv = grad_scale w_i (Q_t p_tv - sum_{k: id_tk = v} q_tk)
 // The softmax part w_i Q_t p_tv is what stage (b) computes for a row with g_t = -w_i Q_t, so the lm_head
 // kernel, the chunk block and the two backward products are stage (b)'s own.  What is new is the list:
-// its logits are K dot products per row (distill_rows_kernel, one warp per row, 2 K d FLOP and K rows
-// of W out of L2 against the 2 V d of the row's logits), and after the chunk block holds the softmax
+// its logits are K dot products per row (distill_dots_kernel: 2 K d FLOP and K rows of W out of L2
+// against the 2 V d of the row's logits), and after the chunk block holds the softmax
 // part its K entries are written from those fp32 values (distill_scatter_kernel), never subtracted
 // from a rounded probability.
 //
 // A chunk of token tiles in the one-call step: plan_kernel chooses the splits from the number of tiles
 // the device has found; lmhead_kernel<MODE_FWD_P> leaves p~ = exp(z - c_t) in the block and the rows'
-// running states; distill_rows_kernel finishes the rows; distill_scale_kernel turns p~ into the softmax
+// running states; distill_dots_kernel and distill_rows_kernel finish the rows; distill_scale_kernel turns p~ into the softmax
 // part; range_fix_kernel redoes rows whose p~ left bf16's range; distill_scatter_kernel; the products
 // dH and dW.  (The row-factor form of aero_grpo_loss_fwd_bwd, which saves the pass over the block, would
 // multiply the rows of H by exp(c_t - lse_t) and round them to bf16 once more before dW; here the list's
@@ -39,6 +39,7 @@ struct List {
   const float* logits;     // [T,K]
   const float* tlse;       // [T] or NULL: the list itself is normalised
   float* kl;               // [T] out, or NULL
+  float* z;                // [T,K] student logits at the listed tokens
   float* entry;            // [T,K] dz at the listed tokens, or NULL (forward only)
   double* partials;        // one record per block of the row kernel, or NULL
 };
@@ -112,9 +113,58 @@ __device__ __forceinline__ float2 join_states(const float4* xs, long long T, lon
   return make_float2(lse, lp);
 }
 
+// Student logits at the listed tokens: kDots list places of one row per warp, so that even a few hundred rows put
+// thousands of warps on the machine (one warp for the whole list took 100 us for 300 rows of 64 places).  Bound by
+// the gather of K rows of W per token out of L2.
+constexpr int kDots = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
+__global__ void __launch_bounds__(256) distill_dots_kernel(RowsArgs a) {
   constexpr int VEC = rowvec::Elem<T>::kVec;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long t = row_of(a, warp);
+  const int K = a.ls.K, d = a.d, k0 = blockIdx.y * kDots;
+  if (t < 0) return;
+  int v[kDots];
+  const T* w[kDots];
+  int last = -1;
+#pragma unroll
+  for (int q = 0; q < kDots; ++q) {
+    v[q] = k0 + q < K ? a.ls.ids[t * K + k0 + q] : -1;
+    if (v[q] >= a.V) v[q] = -1;
+    if (v[q] >= 0) last = v[q];
+  }
+  if (last < 0) return;
+#pragma unroll
+  for (int q = 0; q < kDots; ++q) w[q] = static_cast<const T*>(a.W) + (long long)(v[q] >= 0 ? v[q] : last) * d;
+  const T* h = static_cast<const T*>(a.H) + t * d;
+  float acc[kDots] = {0.f, 0.f, 0.f, 0.f};
+  if (d % VEC == 0) {
+#pragma unroll 2
+    for (int e = lane * VEC; e < d; e += 32 * VEC) {
+      float x[VEC], y[kDots][VEC];
+      rowvec::load<T, VEC>(h + e, x);
+#pragma unroll
+      for (int q = 0; q < kDots; ++q) rowvec::load<T, VEC>(w[q] + e, y[q]);
+#pragma unroll
+      for (int q = 0; q < kDots; ++q)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[q] = fmaf(x[i], y[q][i], acc[q]);
+    }
+  } else {
+    for (int e = lane; e < d; e += 32) {
+      const float x = rowvec::Elem<T>::load(h + e);
+#pragma unroll
+      for (int q = 0; q < kDots; ++q) acc[q] = fmaf(x, rowvec::Elem<T>::load(w[q] + e), acc[q]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < kDots; ++q) {
+    acc[q] = warp_sum(acc[q]);
+    if (lane == 0 && v[q] >= 0) a.ls.z[t * K + k0 + q] = acc[q];
+  }
+}
+
+__global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
   __shared__ double rec[8][kPartialStride];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const long long t = row_of(a, warp);
@@ -168,53 +218,16 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
         if (id[s] >= 0 && lg[s] > -INFINITY) sum += expf(lg[s] - hi);
       norm = hi + logf(warp_sum(sum));            // (an empty list: -inf, no place below uses it)
     }
-    // student logits at the listed tokens, four dot products at a time
-    const T* h = static_cast<const T*>(a.H) + t * d;
+    // student logits at the listed tokens, from distill_dots_kernel
     float zy = 0.f;
     bool any_listed = false;
-    for (int k0 = 0; k0 < K; k0 += 4) {
-      int v[4];
-      const T* w[4];
-      bool any = false;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        int mine = -1;
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s)
-          if (s == (k0 + q) / 32) mine = id[s];
-        v[q] = k0 + q < K ? __shfl_sync(0xffffffffu, mine, (k0 + q) & 31) : -1;
-        any |= v[q] >= 0;
-        w[q] = static_cast<const T*>(a.W) + (long long)(v[q] >= 0 ? v[q] : yt) * d;
-      }
-      if (!any) continue;
-      any_listed = true;
-      float acc[4] = {0.f, 0.f, 0.f, 0.f};
-      if (d % VEC == 0) {
-        for (int e = lane * VEC; e < d; e += 32 * VEC) {
-          float x[VEC];
-          rowvec::load<T, VEC>(h + e, x);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float y[VEC];
-            rowvec::load<T, VEC>(w[q] + e, y);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[q] = fmaf(x[i], y[i], acc[q]);
-          }
-        }
-      } else {
-        for (int e = lane; e < d; e += 32) {
-          const float x = rowvec::Elem<T>::load(h + e);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) acc[q] = fmaf(x, rowvec::Elem<T>::load(w[q] + e), acc[q]);
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        acc[q] = warp_sum(acc[q]);
-        if (v[q] == yt) zy = acc[q];
-#pragma unroll
-        for (int s = 0; s < kSlots; ++s)
-          if (s == (k0 + q) / 32 && lane == ((k0 + q) & 31)) z[s] = acc[q];
+    for (int s = 0; s < kSlots; ++s) {
+      if (s * 32 < K) {
+        if (id[s] >= 0) z[s] = a.ls.z[t * K + s * 32 + lane];
+        const unsigned is_y = __ballot_sync(0xffffffffu, id[s] == yt && id[s] >= 0);
+        if (is_y) zy = __shfl_sync(0xffffffffu, z[s], __ffs(is_y) - 1);
+        any_listed |= is_y != 0;
       }
     }
     if (a.xstate) {
@@ -346,7 +359,7 @@ __global__ void __launch_bounds__(256) distill_scatter_kernel(BlockArgs b) {
   }
 }
 
-// dH of the chunk's rows from the fp32 sums of the ranges, added in order; one warp per row.
+// dH of the chunk's rows from the fp32 sums of the ranges, added in order; a warp takes 256 columns of a row.
 __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const int* __restrict__ ksplit,
                                                               const float* __restrict__ part, __nv_bfloat16* __restrict__ dH) {
   const int ks = *ksplit;
@@ -355,7 +368,8 @@ __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const 
   const long long t = row_of(a, warp);
   if (t < 0) return;
   const long long rows = (long long)(min(*a.n_tiles, a.tile_end) - a.tile_begin) * 128, row = (long long)blockIdx.x * 8 + warp;
-  for (int c = lane * 8; c < a.d; c += 256) {
+  const int c = blockIdx.y * 256 + lane * 8;
+  if (c < a.d) {
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int k = 0; k < ks; ++k) {
@@ -581,6 +595,7 @@ struct Ws {
   int* range_rows;
   int32_t* y;
   float* g;
+  float* z;
   float* entry;
   double* partials;
   size_t n_partials;
@@ -611,6 +626,7 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   w.range_rows = reinterpret_cast<int*>(take(kRangeCap * sizeof(int)));
   w.y = reinterpret_cast<int32_t*>(take(Tn * 4));
   w.g = reinterpret_cast<float*>(take(Tn * 4));
+  w.z = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   if (mode != kFwd) w.entry = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   const size_t mt = (size_t)max_tiles_of(T, R);
   w.n_partials = mt * kBlocksPerTile;
@@ -721,7 +737,7 @@ unsigned row_grid(int64_t T) {
 
 RowsArgs rows_of(const Call& c, const Ws& s, float* lse, float* kl, bool partials, float grad_scale) {
   RowsArgs a = {};
-  a.ls = {c.K, c.ids, c.logits, c.tlse, kl, s.entry, partials ? s.partials : nullptr};
+  a.ls = {c.K, c.ids, c.logits, c.tlse, kl, s.z, s.entry, partials ? s.partials : nullptr};
   a.T = c.T; a.d = c.d; a.V = c.V; a.R = c.R; a.H = c.H; a.W = c.W; a.cs = c.cs; a.w = c.w; a.keep = c.keep;
   a.lse = lse; a.y = s.y; a.g = s.g; a.grad_scale = grad_scale; a.plan = s.plan;
   return a;
@@ -742,8 +758,9 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
 
 // ---- fp32 path -------------------------------------------------------------------------------------------
 int rows_fp32(const RowsArgs& a, aero_ctx* ctx) {
-  distill_rows_kernel<float><<<(unsigned)((a.T + 7) / 8), 256, 0, ctx->stream>>>(a);
-  ctx->launches += 1;
+  distill_dots_kernel<float><<<dim3((unsigned)((a.T + 7) / 8), (unsigned)((a.ls.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+  distill_rows_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, ctx->stream>>>(a);
+  ctx->launches += 2;
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
 }
@@ -854,8 +871,10 @@ int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float
     a.xstate = s.xstate;
     a.tile_row = s.tiles.tile_row; a.tile_valid = s.tiles.tile_valid; a.n_tiles = s.tiles.n_tiles;
     a.tile_begin = 0; a.tile_end = s.tiles.max_tiles;
-    distill_rows_kernel<__nv_bfloat16><<<(unsigned)s.tiles.max_tiles * kBlocksPerTile, 256, 0, ctx->stream>>>(a);
-    ctx->launches += 1;
+    const unsigned blocks = (unsigned)s.tiles.max_tiles * kBlocksPerTile;
+    distill_dots_kernel<__nv_bfloat16><<<dim3(blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+    distill_rows_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
+    ctx->launches += 2;
     AERO_CUDA_TRY(cudaGetLastError());
   }
   return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
@@ -889,9 +908,13 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
   if ((rc = aero_make_tmap_blocked(ctx, &tmH_mn, Hl, tpc * lmhead::BM, d, d, 64, bn))) return rc;
   auto k_dh = pairs ? gemmbwd::gemm_pair_kernel<gemmbwd::KIND_DH> : gemmbwd::gemm_kernel<gemmbwd::KIND_DH>;
   auto k_dw = pairs ? gemmbwd::gemm_pair_kernel<gemmbwd::KIND_DW> : gemmbwd::gemm_kernel<gemmbwd::KIND_DW>;
-  const int gemm_smem = (int)(pairs ? gemmbwd::PSMEM_BYTES : gemmbwd::SMEM_BYTES);
-  AERO_CUDA_TRY(cudaFuncSetAttribute(k_dh, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem));
-  AERO_CUDA_TRY(cudaFuncSetAttribute(k_dw, cudaFuncAttributeMaxDynamicSharedMemorySize, gemm_smem));
+  const int dh_smem = (int)(pairs ? gemmbwd::PSMEM_BYTES : gemmbwd::SMEM_BYTES), dw_smem = dh_smem + (int)gemmbwd::OUT_EXTRA;
+  AERO_CUDA_TRY(cudaFuncSetAttribute(k_dh, cudaFuncAttributeMaxDynamicSharedMemorySize, dh_smem));
+  AERO_CUDA_TRY(cudaFuncSetAttribute(k_dw, cudaFuncAttributeMaxDynamicSharedMemorySize, dw_smem));
+  CUtensorMap tmO = tmDZ_k;
+  if (gr.dW16) rc = aero_make_tmap_2d(ctx, &tmO, BF, 2, gr.dW16, V, d, d, 32, 64);
+  else if (!gr.accumulate) rc = aero_make_tmap_2d(ctx, &tmO, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, gr.dW, V, d, d, 32, 32);
+  if (rc) return rc;
   const int gemm_grid = pairs ? 2 * (ctx->sm_count / 2 > 0 ? ctx->sm_count / 2 : 1) : ctx->sm_count;
   const bool many = c.T > (int64_t)ctx->sm_count * lmhead::BM;
 
@@ -907,13 +930,15 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     lmhead::Params p = {};
     p.tile_begin = (int)begin; p.tile_end = (int)end;
     p.dz = gr.block; p.ldz = ldz;
+    distill_dots_kernel<__nv_bfloat16><<<dim3(row_blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+    ctx->launches += 1;
     BlockArgs b = {a, gr.block, (int)nblk, (V + lmhead::BN - 1) / lmhead::BN, s.shift};
     if (mode == kBoth) {
       p.xstate = s.xstate; p.shift_out = s.shift;
       p.range_rows = s.range_rows; p.range_count = s.range_count; p.range_cap = kRangeCap;
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBoth))) return rc;
       a.xstate = s.xstate;
-      distill_rows_kernel<__nv_bfloat16><<<row_blocks, 256, 0, ctx->stream>>>(a);
+      distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);
       distill_scale_kernel<<<dim3((unsigned)b.nvt, (unsigned)(end - begin)), 256, 0, ctx->stream>>>(b);
       RangeArgs f = {};
       f.rows = s.range_rows; f.count = s.range_count; f.cap = kRangeCap; f.dz = gr.block; f.nblk = (int)nblk;
@@ -923,7 +948,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
       range_fix_kernel<<<2 * ctx->sm_count, 256, 0, ctx->stream>>>(f);
       ctx->launches += 3;
     } else {
-      distill_rows_kernel<__nv_bfloat16><<<row_blocks, 256, 0, ctx->stream>>>(a);
+      distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);
       ctx->launches += 1;
       p.lse_in = lse; p.g_in = s.g; p.grad_scale = gr.grad_scale;
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBwd))) return rc;
@@ -933,19 +958,19 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     gp.T = c.T; gp.d = d; gp.V = V; gp.ldz = ldz;
     gp.tile_row = s.tiles.tile_row; gp.tile_valid = s.tiles.tile_valid; gp.n_tiles = s.tiles.n_tiles;
     gp.tile_begin = (int)begin; gp.tpc = (int)tpc;
-    gp.dH = gr.dH; gp.dW = gr.dW; gp.dW16 = gr.dW16; gp.status = ctx->d_status;
-    gp.overwrite = begin == 0 && !gr.accumulate ? 1 : 0;
+    gp.dH = gr.dH; gp.dW = gr.dW; gp.status = ctx->d_status;
+    gp.out = gr.dW16 ? gemmbwd::kOutBf16 : (begin == 0 && !gr.accumulate ? gemmbwd::kOutFp32 : 0);
     gp.h_local = 1;
     gp.ksplit = s.k_hi > 1 ? s.plan + 1 : nullptr; gp.part = s.part;
     gp.nsync = many ? aero_gemm_sync(ctx) : 0;
     gp.sync_ctr = reinterpret_cast<unsigned int*>(s.zero) + 4;
-    k_dh<<<gemm_grid, gemmbwd::THREADS, gemm_smem, ctx->stream>>>(tmDZ_k, tmW_mn, gp);
+    k_dh<<<gemm_grid, gemmbwd::THREADS, dh_smem, ctx->stream>>>(tmDZ_k, tmW_mn, tmDZ_k, gp);
     if (s.k_hi > 1) {
-      distill_join_dh_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a, s.plan + 1, s.part, gr.dH);
+      distill_join_dh_kernel<<<dim3(row_blocks, (unsigned)((d + 255) / 256)), 256, 0, ctx->stream>>>(a, s.plan + 1, s.part, gr.dH);
       ctx->launches += 1;
     }
     gp.sync_ctr = reinterpret_cast<unsigned int*>(s.zero) + 8;
-    k_dw<<<gemm_grid, gemmbwd::THREADS, gemm_smem, ctx->stream>>>(tmDZ_mn, tmH_mn, gp);
+    k_dw<<<gemm_grid, gemmbwd::THREADS, dw_smem, ctx->stream>>>(tmDZ_mn, tmH_mn, tmO, gp);
     ctx->launches += 3;
     AERO_CUDA_TRY(cudaGetLastError());
   }

@@ -32,7 +32,7 @@ struct Ctl {
   uint32_t tmem_base;
   int abort;
 };
-constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + sizeof(Ctl);
+constexpr size_t SMEM_BYTES = 1024 + (size_t)STAGES * STAGE_BYTES + sizeof(Ctl);   // + OUT_EXTRA where dW is overwritten
 
 struct Params {
   long long T;
@@ -46,10 +46,9 @@ struct Params {
   float* dW;
   uint32_t* status;
   const float* row_scale;       // dH: factor of each token row, applied to the finished tile (NULL: none)
-  // dW: the chunk's product replaces what is there instead of being added to it -- in fp32 (overwrite), or
-  // rounded to bf16 (dW16 not NULL)
-  int overwrite;
-  __nv_bfloat16* dW16;
+  // dW: the chunk's product replaces what is there instead of being added to it, as fp32 (kOutFp32) or rounded to
+  // bf16 (kOutBf16), through the map of the output (box of 32 rows x 128 bytes); 0: added to the fp32 dW
+  int out;
   // dH: split of the vocabulary (the reduction) into *ksplit ranges, each leaving fp32 sums of its tiles in
   // part [range][tile of the chunk * 128 + row][d]; NULL, or 1 in memory: no split, the tiles go to dH
   const int* ksplit;
@@ -69,27 +68,55 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&v);
 }
 
-// 32 columns of one row of dW from the accumulator.
-__device__ __forceinline__ void store_dw(const Params& p, long long row, int col0, const uint32_t (&r)[32]) {
-  if (p.dW16) {
-    uint4* dst = reinterpret_cast<uint4*>(p.dW16 + row * p.d + col0);
+constexpr int kOutFp32 = 1, kOutBf16 = 2;
+// staging of the overwriting dW epilogue, after the control block: per epilogue warp two buffers of 32 rows x 128 bytes
+constexpr uint32_t OUT_BUF_BYTES = 32 * 128, OUT_EXTRA = 1024 + 4 * 2 * OUT_BUF_BYTES;
+__device__ __forceinline__ uint8_t* out_staging(void* ctl_end) {
+  return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(ctl_end) + 1023) & ~(uintptr_t)1023);
+}
+
+// Writes an accumulator tile of dW (this warp's 32 rows from row0, columns col0 .. col0 + ncol) by TMA from a swizzled
+// staging buffer: whole 128-byte pieces, asynchronous, instead of 32 rows a store instruction (a tile of 300 tokens'
+// dW spends its time here: 251 -> 141 us at d = 1536).
+__device__ __forceinline__ void store_dw_tile(const Params& p, const CUtensorMap* tmO, uint32_t taddr, uint8_t* stg, int lane,
+                                              long long row0, int col0, int ncol, uint32_t& nstore) {
+  for (int c = 0; c * 32 < ncol; ++c) {
+    uint32_t r[32];
+    __syncwarp();                       // the TMEM load is warp-collective
+    tc::tmem_ld_32x32(taddr + c * 32, r);
+    tc::tmem_ld_wait();
+    if (p.out == kOutBf16) {
+      const int half = c & 1;
+      if (half == 0) {
+        if (lane == 0) tc::tma_store_wait_read<1>();      // the buffer's previous copy has been read
+        __syncwarp();
+      }
+      uint8_t* buf = stg + (nstore & 1u) * OUT_BUF_BYTES + lane * 128;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      dst[q] = make_uint4(pack_bf16(__uint_as_float(r[8 * q]), __uint_as_float(r[8 * q + 1])),
-                          pack_bf16(__uint_as_float(r[8 * q + 2]), __uint_as_float(r[8 * q + 3])),
-                          pack_bf16(__uint_as_float(r[8 * q + 4]), __uint_as_float(r[8 * q + 5])),
-                          pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
-    return;
-  }
-  float4* dst = reinterpret_cast<float4*>(p.dW + row * p.d + col0);
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<uint4*>(buf + (((half * 4 + q) ^ (lane & 7)) * 16)) =
+            make_uint4(pack_bf16(__uint_as_float(r[8 * q]), __uint_as_float(r[8 * q + 1])),
+                       pack_bf16(__uint_as_float(r[8 * q + 2]), __uint_as_float(r[8 * q + 3])),
+                       pack_bf16(__uint_as_float(r[8 * q + 4]), __uint_as_float(r[8 * q + 5])),
+                       pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
+      if (half == 0) continue;
+    } else {
+      if (lane == 0) tc::tma_store_wait_read<1>();
+      __syncwarp();
+      uint8_t* buf = stg + (nstore & 1u) * OUT_BUF_BYTES + lane * 128;
 #pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    float4 v = p.overwrite ? make_float4(0.f, 0.f, 0.f, 0.f) : dst[q];
-    v.x += __uint_as_float(r[4 * q]);
-    v.y += __uint_as_float(r[4 * q + 1]);
-    v.z += __uint_as_float(r[4 * q + 2]);
-    v.w += __uint_as_float(r[4 * q + 3]);
-    dst[q] = v;
+      for (int q = 0; q < 8; ++q)
+        *reinterpret_cast<uint4*>(buf + ((q ^ (lane & 7)) * 16)) = make_uint4(r[4 * q], r[4 * q + 1], r[4 * q + 2], r[4 * q + 3]);
+    }
+    tc::fence_proxy_async();
+    __syncwarp();
+    if (lane == 0) {
+      // (rows past V are clipped by the map; a copy that would start past it is left out)
+      if (row0 < p.V)
+        tc::tma_store_2d(tmO, stg + (nstore & 1u) * OUT_BUF_BYTES, col0 + c * 32 - (p.out == kOutBf16 ? 32 : 0), (int)row0);
+      tc::tma_store_commit();
+    }
+    ++nstore;
   }
 }
 
@@ -115,7 +142,8 @@ __device__ __forceinline__ void store_part(const Params& p, int range, long long
 
 template <int KIND>
 __global__ void __launch_bounds__(THREADS, 1)
-gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
+gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+            const __grid_constant__ CUtensorMap tmO, const Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   Ctl* ctl = reinterpret_cast<Ctl*>(smem + (size_t)STAGES * STAGE_BYTES);
@@ -238,9 +266,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     }
   } else {
     // ---------------- epilogue warps 0..3 ----------------
-    uint32_t at = 0;
+    uint32_t at = 0, nstore = 0;
     bool ok = true;
     const int r_in_tile = warp * 32 + lane;
+    uint8_t* stg = out_staging(ctl + 1) + warp * 2 * OUT_BUF_BYTES;
     for (int u = blockIdx.x; ok && u < n_units; u += gridDim.x, ++at) {
       const int mt = un.m(u), nt = un.n(u);
       const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
@@ -258,7 +287,10 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
         row_ok = out_row < p.V;
       }
       const int ncol = min(BN, p.d - nt * BN);
-      for (int c = 0; c * 32 < ncol; ++c) {
+      if (KIND == KIND_DW && p.out) {
+        store_dw_tile(p, &tmO, taddr, stg, lane, (long long)mt * BM + warp * 32, nt * BN, ncol, nstore);
+      }
+      for (int c = 0; !(KIND == KIND_DW && p.out) && c * 32 < ncol; ++c) {
         uint32_t r[32];
         __syncwarp();                       // the TMEM load is warp-collective
         tc::tmem_ld_32x32(taddr + c * 32, r);
@@ -283,7 +315,16 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
                                 pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
           }
         } else {
-          store_dw(p, out_row, col0, r);
+          float4* dst = reinterpret_cast<float4*>(p.dW + out_row * p.d + col0);
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            float4 v = dst[q];
+            v.x += __uint_as_float(r[4 * q]);
+            v.y += __uint_as_float(r[4 * q + 1]);
+            v.z += __uint_as_float(r[4 * q + 2]);
+            v.w += __uint_as_float(r[4 * q + 3]);
+            dst[q] = v;
+          }
         }
       }
       tc::tc_fence_before();
@@ -293,6 +334,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   }
 
   // ---------------- teardown ----------------
+  if (KIND == KIND_DW && p.out && warp < 4 && lane == 0) tc::tma_store_wait_all<0>();   // own stores have landed
   __syncwarp();
   if (*abort_flag) {
     const unsigned long long t0 = tc::globaltimer_ns();
@@ -327,7 +369,8 @@ constexpr size_t PSMEM_BYTES = 1024 + (size_t)PSTAGES * PSTAGE_BYTES + sizeof(PC
 
 template <int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
-gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const Params p) {
+gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                 const __grid_constant__ CUtensorMap tmO, const Params p) {
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   PCtl* ctl = reinterpret_cast<PCtl*>(smem + (size_t)PSTAGES * PSTAGE_BYTES);
@@ -449,9 +492,10 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     }
   } else {
     // ---------------- epilogue warps 0..3 (each CTA its own row tile) ----------------
-    uint32_t at = 0;
+    uint32_t at = 0, nstore = 0;
     bool ok = true;
     const int r_in_tile = warp * 32 + lane;
+    uint8_t* stg = out_staging(ctl + 1) + warp * 2 * OUT_BUF_BYTES;
     for (int u = pair; ok && u < n_units; u += npairs, ++at) {
       const int mp = un.m(u), nt = un.n(u);
       const int mt = 2 * mp + (int)rank;
@@ -472,7 +516,9 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
         }
       }
       const int ncol = min(BN, p.d - nt * BN);
-      if (mt < n_mt) {
+      if (KIND == KIND_DW && p.out) {
+        if (mt < n_mt) store_dw_tile(p, &tmO, taddr, stg, lane, (long long)mt * BM + warp * 32, nt * BN, ncol, nstore);
+      } else if (mt < n_mt) {
         for (int c = 0; c * 32 < ncol; ++c) {
           uint32_t r[32];
           __syncwarp();                       // the TMEM load is warp-collective
@@ -498,7 +544,16 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
                                   pack_bf16(__uint_as_float(r[8 * q + 6]), __uint_as_float(r[8 * q + 7])));
             }
           } else {
-            store_dw(p, out_row, col0, r);
+            float4* dst = reinterpret_cast<float4*>(p.dW + out_row * p.d + col0);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              float4 v = dst[q];
+              v.x += __uint_as_float(r[4 * q]);
+              v.y += __uint_as_float(r[4 * q + 1]);
+              v.z += __uint_as_float(r[4 * q + 2]);
+              v.w += __uint_as_float(r[4 * q + 3]);
+              dst[q] = v;
+            }
           }
         }
       }
@@ -509,6 +564,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   }
 
   // ---------------- teardown ----------------
+  if (KIND == KIND_DW && p.out && warp < 4 && lane == 0) tc::tma_store_wait_all<0>();   // own stores have landed
   __syncwarp();
   if (*abort_flag) {
     const unsigned long long t0 = tc::globaltimer_ns();

@@ -127,16 +127,16 @@ int aero_bwd_tc(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_
     if (pairs) {
       const long long dh_pu = (tpc + 1) / 2 * n_nt, dw_pu = ((long long)((V + gemmbwd::BM - 1) / gemmbwd::BM) + 1) / 2 * n_nt;
       k_dh2<<<2 * (int)(dh_pu < max_pairs ? dh_pu : max_pairs), gemmbwd::THREADS, gemmbwd::PSMEM_BYTES, ctx->stream>>>(
-          tmDZ_k, tmW_mn2, gp);
+          tmDZ_k, tmW_mn2, tmDZ_k, gp);
       gp.sync_ctr = sync_ctr + 8;
       k_dw2<<<2 * (int)(dw_pu < max_pairs ? dw_pu : max_pairs), gemmbwd::THREADS, gemmbwd::PSMEM_BYTES, ctx->stream>>>(
-          tmDZ_mn, tmH_mn2, gp);
+          tmDZ_mn, tmH_mn2, tmDZ_k, gp);
     } else {
       k_dh<<<(int)(dh_units < ctx->sm_count ? dh_units : ctx->sm_count), gemmbwd::THREADS, gemmbwd::SMEM_BYTES,
-             ctx->stream>>>(tmDZ_k, tmW_mn, gp);
+             ctx->stream>>>(tmDZ_k, tmW_mn, tmDZ_k, gp);
       gp.sync_ctr = sync_ctr + 8;
       k_dw<<<(int)(dw_units < ctx->sm_count ? dw_units : ctx->sm_count), gemmbwd::THREADS, gemmbwd::SMEM_BYTES,
-             ctx->stream>>>(tmDZ_mn, tmH_mn, gp);
+             ctx->stream>>>(tmDZ_mn, tmH_mn, tmDZ_k, gp);
     }
     ctx->launches += 3;
     AERO_CUDA_TRY(cudaGetLastError());

@@ -187,9 +187,11 @@ def test_chunks_and_dw_types(ctx, chunk_tokens):
     assert ctx.last_status() == 0
 
 
-def test_bf16_dw_of_a_few_rows_needs_no_room_for_sums(ctx):
-    """One chunk whose block is smaller than an fp32 dW would be."""
-    case = Case(T=100, d=256, V=3000, K=9, R=1)
+@pytest.mark.parametrize("T,d,V", [(100, 256, 3000), (300, 2112, 700), (129, 3584, 290)])
+def test_bf16_dw_of_a_few_rows_needs_no_room_for_sums(ctx, T, d, V):
+    """One chunk whose block is smaller than an fp32 dW would be; single CTAs and CTA pairs, vocabularies that end inside
+    a 128-row tile and inside one of its 32-row pieces."""
+    case = Case(T=T, d=d, V=V, K=9, R=1)
     dv, _ = case.device()
     r = case.reference()
     _, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dw_dtype=torch.bfloat16)
