@@ -548,9 +548,10 @@ int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
  *   loss  = sum_t w_i kl_t
  *   dz_tv = grad_scale w_i (Q_t p_tv - sum_{k: ids[t,k] = v} q_tk);   dH = dz W,   dW (+)= dz^T H
  * A list place with id AERO_NO_TOKEN is empty (its logit is not read), any other id outside [0,V) raises
- * AERO_ST_BAD_TARGET and counts as empty, a logit of -infinity or NaN has q = 0; a row whose list holds no weight
- * contributes nothing.  A token listed twice counts with the sum of its q.  Rows of dropped rollouts get
- * lse = kl = 0 and dH = 0.  1 <= K <= 256.
+ * AERO_ST_BAD_TARGET and counts as empty, a logit of -infinity or NaN has q = 0; a row whose list holds no
+ * weight contributes nothing.  A token listed twice counts with the sum of its q.  Rows of dropped rollouts
+ * get lse = kl = 0 and dH = 0, whatever they hold.  1 <= K <= 256; bf16: d % 64 == 0; fp32 (plain path for
+ * small shapes): d <= 1024.
  * Inputs   ids [T,K] i32, logits [T,K] f32, teacher_lse [T] f32 or NULL.
  * Outputs  lse, kl [T] f32; loss [1] f32 (overwritten; fixed order of the sums); metrics [4] f32 or NULL: fraction
  *          of kept tokens whose list holds no weight, mean kl, mean sum_k p_t,ids[t,k], kept tokens; dH [T,d]

@@ -480,109 +480,128 @@ __global__ void __launch_bounds__(256) plan_kernel(PlanArgs a) {
 }
 
 // ---- fp32 path, for small shapes -----------------------------------------------------------------
-// log-sum-exp of the kept rows' logits, one warp per row
-__global__ void __launch_bounds__(256) lse_fp32_kernel(long long T, int d, int V, int R, const float* __restrict__ H,
-                                                       const float* __restrict__ W, const int64_t* __restrict__ cs,
-                                                       const uint8_t* __restrict__ keep, float* __restrict__ lse) {
-  const int lane = threadIdx.x & 31;
-  const long long nwarps = (long long)gridDim.x * 8;
-  for (long long t = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); t < T; t += nwarps) {
-    if (!keep[aero_owner(cs, R, t)]) continue;
-    float m = -INFINITY, l = 0.f;
-    for (int v = lane; v < V; v += 32) {
-      float z = 0.f;
-      for (int k = 0; k < d; ++k) z = fmaf(H[t * d + k], W[(long long)v * d + k], z);
-      const float mn = fmaxf(m, z);
-      l = l * expf(m - mn) + expf(z - mn);
-      m = mn;
-    }
-    const float M = warp_max(m);
-    l = warp_sum(m > -INFINITY ? l * expf(m - M) : 0.f);
-    if (lane == 0) lse[t] = M + logf(l);
-  }
-}
+// Blocks of eight warps; 32 rows of the other operand at a time stand in shared memory, a row apart by an odd number
+// of words, and a lane has one of them: a logit is d products in a lane, without a reduction.
+constexpr int kMaxD32 = 1024;
 
-struct Fp32Bwd {
+struct Fp32Args {
   RowsArgs r;
-  void* dH;
+  float* dH;               // gradients; NULL: the log-sum-exp alone
   float* dW;
   int accumulate;
 };
 
-// dH[t, :] = sum_v dz_tv W[v, :], one warp per row: the softmax part over all v, then the list's
-// entries beyond it.
-__global__ void __launch_bounds__(256) dh_fp32_kernel(Fp32Bwd b) {
-  const int lane = threadIdx.x & 31, d = b.r.d, V = b.r.V, K = b.r.ls.K;
-  const float* W = static_cast<const float*>(b.r.W);
-  const long long nwarps = (long long)gridDim.x * 8;
-  for (long long t = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); t < b.r.T; t += nwarps) {
-    float* out = static_cast<float*>(b.dH) + t * d;
-    const float* h = static_cast<const float*>(b.r.H) + t * d;
-    const bool kept = b.r.keep[aero_owner(b.r.cs, b.r.R, t)] != 0;
-    const float c = kept ? -b.r.grad_scale * b.r.g[t] : 0.f;
-    for (int c0 = 0; c0 < d; c0 += 32) {
-      float acc = 0.f;
-      if (c != 0.f) {
-        const int col = c0 + lane;
-        for (int v = 0; v < V; ++v) {
-          float z = 0.f;
-          for (int k = lane; k < d; k += 32) z = fmaf(h[k], W[(long long)v * d + k], z);
-          const float p = c * expf(warp_sum(z) - b.r.lse[t]);
-          if (col < d) acc = fmaf(p, W[(long long)v * d + col], acc);
-        }
-        // at a listed token the entry takes the place of the softmax part
-        for (int k = 0; k < K; ++k) {
-          const int v = b.r.ls.ids[t * K + k];
-          if (v < 0 || v >= V) continue;
-          bool first = true;
-          for (int j = lane; j < k; j += 32) first &= b.r.ls.ids[t * K + j] != v;
-          if (!__all_sync(0xffffffffu, first)) continue;
-          float z = 0.f;
-          for (int e = lane; e < d; e += 32) z = fmaf(h[e], W[(long long)v * d + e], z);
-          const float p = c * expf(warp_sum(z) - b.r.lse[t]);
-          if (col < d) acc = fmaf(b.r.ls.entry[t * K + k] - p, W[(long long)v * d + col], acc);
-        }
+// 32 rows of `src` from row r0 into the staging area (zeros past `n`, and where `g` says that the row has no weight, so
+// that what stands in rows of dropped rollouts is not looked at)
+__device__ __forceinline__ void stage_rows(float* dst, int pitch, const float* src, long long r0, long long n, int d,
+                                           const float* g) {
+  for (int i = threadIdx.x >> 5; i < 32; i += 8) {
+    const bool there = r0 + i < n && (g == nullptr || g[r0 + i] != 0.f);
+    for (int k = threadIdx.x & 31; k < d; k += 32) dst[i * pitch + k] = there ? src[(r0 + i) * d + k] : 0.f;
+  }
+}
+__device__ __forceinline__ float dot(const float* a, const float* b, int d) {
+  float z = 0.f;
+#pragma unroll 4
+  for (int k = 0; k < d; ++k) z = fmaf(a[k], b[k], z);
+  return z;
+}
+
+// A warp per token row: its log-sum-exp, or its row of dH.  NC * 32 >= d.
+template <int NC, bool GRADS>
+__global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
+  extern __shared__ float sm[];
+  const RowsArgs& a = f.r;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.d, pitch = d | 1, K = a.ls.K;
+  float* tile = sm;
+  float* h = sm + 32 * pitch + warp * d;
+  const long long t = (long long)blockIdx.x * 8 + warp;
+  const bool kept = t < a.T && a.keep[aero_owner(a.cs, a.R, t)] != 0;
+  const float lse = GRADS && kept ? a.lse[t] : 0.f, c = GRADS && kept ? -a.grad_scale * a.g[t] : 0.f;
+  for (int k = lane; k < d; k += 32) h[k] = kept ? static_cast<const float*>(a.H)[t * d + k] : 0.f;
+  float m = -INFINITY, l = 0.f, acc[NC];
+#pragma unroll
+  for (int q = 0; q < NC; ++q) acc[q] = 0.f;
+  for (int v0 = 0; v0 < a.V; v0 += 32) {
+    __syncthreads();
+    stage_rows(tile, pitch, static_cast<const float*>(a.W), v0, a.V, d, nullptr);
+    __syncthreads();
+    const float z = dot(h, tile + lane * pitch, d);
+    const bool in = v0 + lane < a.V;
+    if (!GRADS) {
+      if (in) {
+        const float mn = fmaxf(m, z);
+        l = l * expf(m - mn) + expf(z - mn);
+        m = mn;
       }
-      if (c0 + lane < d) out[c0 + lane] = acc;
+      continue;
     }
+    if (c == 0.f) continue;                              // (the same for the whole warp)
+    float dz = in ? c * expf(z - lse) : 0.f;
+    for (int k0 = 0; k0 < K; k0 += 32) {                 // at a listed token the entry takes the place of the softmax part
+      const int id = k0 + lane < K ? a.ls.ids[t * K + k0 + lane] : -1;
+      for (unsigned hits = __ballot_sync(0xffffffffu, id >= v0 && id < v0 + 32 && id < a.V); hits != 0; hits &= hits - 1) {
+        const int src = __ffs(hits) - 1, v = __shfl_sync(0xffffffffu, id, src);
+        if (v == v0 + lane) dz = a.ls.entry[t * K + k0 + src];
+      }
+    }
+    for (int v = 0; v < 32; ++v) {
+      const float x = __shfl_sync(0xffffffffu, dz, v);
+#pragma unroll
+      for (int q = 0; q < NC; ++q)
+        if (q * 32 + lane < d) acc[q] = fmaf(x, tile[v * pitch + q * 32 + lane], acc[q]);
+    }
+  }
+  if (GRADS) {
+    if (t < a.T)
+#pragma unroll
+      for (int q = 0; q < NC; ++q)
+        if (q * 32 + lane < d) f.dH[t * d + q * 32 + lane] = acc[q];
+  } else {
+    const float M = warp_max(m);
+    l = warp_sum(m > -INFINITY ? l * expf(m - M) : 0.f);
+    if (lane == 0 && kept) a.lse[t] = M + logf(l);
   }
 }
 
-// dW[v, :] (+)= sum_t dz_tv H[t, :], one warp per vocabulary row, tokens in order.
-__global__ void __launch_bounds__(256) dw_fp32_kernel(Fp32Bwd b) {
-  const int lane = threadIdx.x & 31, d = b.r.d, K = b.r.ls.K;
-  const float* H = static_cast<const float*>(b.r.H);
-  for (int v = blockIdx.x * 8 + (threadIdx.x >> 5); v < b.r.V; v += gridDim.x * 8) {
-    const float* w = static_cast<const float*>(b.r.W) + (long long)v * d;
-    for (int c0 = 0; c0 < d; c0 += 32) {
-      const int col = c0 + lane;
-      float acc = 0.f;
-      for (long long t = 0; t < b.r.T; ++t) {
-        if (!b.r.keep[aero_owner(b.r.cs, b.r.R, t)]) continue;
-        const float c = -b.r.grad_scale * b.r.g[t];
-        if (c == 0.f) continue;
-        float dz = 0.f;
-        bool listed = false;
-        for (int k0 = 0; k0 < K && !listed; k0 += 32) {
-          const unsigned hit = __ballot_sync(0xffffffffu, k0 + lane < K && b.r.ls.ids[t * K + k0 + lane] == v);
-          if (hit) {
-            dz = b.r.ls.entry[t * K + k0 + __ffs(hit) - 1];
-            listed = true;
-          }
-        }
-        if (!listed) {
-          float z = 0.f;
-          for (int k = lane; k < d; k += 32) z = fmaf(H[t * d + k], w[k], z);
-          dz = c * expf(warp_sum(z) - b.r.lse[t]);
-        }
-        if (col < d) acc = fmaf(dz, H[t * d + col], acc);
-      }
-      if (col < d) {
-        float* o = b.dW + (long long)v * d + col;
-        *o = b.accumulate ? *o + acc : acc;
-      }
+// A warp per vocabulary row: dW[v, :] (+)= sum_t dz_tv H[t, :], tokens in order.
+template <int NC>
+__global__ void __launch_bounds__(256) fp32_vocabulary_kernel(Fp32Args f) {
+  extern __shared__ float sm[];
+  const RowsArgs& a = f.r;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.d, pitch = d | 1, K = a.ls.K;
+  float* tile = sm;
+  float* w = sm + 32 * pitch + warp * d;
+  const int v = blockIdx.x * 8 + warp;
+  for (int k = lane; k < d; k += 32) w[k] = v < a.V ? static_cast<const float*>(a.W)[(long long)v * d + k] : 0.f;
+  float acc[NC];
+#pragma unroll
+  for (int q = 0; q < NC; ++q) acc[q] = 0.f;
+  for (long long t0 = 0; t0 < a.T; t0 += 32) {
+    __syncthreads();
+    stage_rows(tile, pitch, static_cast<const float*>(a.H), t0, a.T, d, a.g);
+    __syncthreads();
+    const long long t = t0 + lane;
+    const float c = t < a.T ? -a.grad_scale * a.g[t] : 0.f;      // (0 for the rows of dropped rollouts)
+    const float z = dot(w, tile + lane * pitch, d);
+    float dz = c != 0.f ? c * expf(z - a.lse[t]) : 0.f;
+    if (c != 0.f)
+      for (int k = 0; k < K; ++k)
+        if (a.ls.ids[t * K + k] == v) dz = a.ls.entry[t * K + k];
+    for (int i = 0; i < 32; ++i) {
+      const float x = __shfl_sync(0xffffffffu, dz, i);
+#pragma unroll
+      for (int q = 0; q < NC; ++q)
+        if (q * 32 + lane < d) acc[q] = fmaf(x, tile[i * pitch + q * 32 + lane], acc[q]);
     }
   }
+  if (v < a.V)
+#pragma unroll
+    for (int q = 0; q < NC; ++q)
+      if (q * 32 + lane < d) {
+        float* o = f.dW + (long long)v * d + q * 32 + lane;
+        *o = f.accumulate ? *o + acc[q] : acc[q];
+      }
 }
 
 // ---- workspace -----------------------------------------------------------------------------------------
@@ -716,7 +735,7 @@ int check_call(const aero_cfg* cfg, const Call& c, const void* ws) {
   if (c.R > 0 && (!c.w || !c.keep)) return AERO_ERR_INVALID;
   if (cfg->dtype != AERO_BF16 && cfg->dtype != AERO_FP32) return AERO_ERR_UNSUPPORTED;
   if (c.K > kMaxK) return AERO_ERR_UNSUPPORTED;
-  if (cfg->dtype == AERO_BF16 && c.d % 64 != 0) return AERO_ERR_UNSUPPORTED;
+  if (cfg->dtype == AERO_BF16 ? c.d % 64 != 0 : c.d > kMaxD32) return AERO_ERR_UNSUPPORTED;
   if (!aero_aligned16(c.H) || !aero_aligned16(c.W)) return AERO_ERR_INVALID;
   return AERO_OK;
 }
@@ -757,10 +776,22 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
 }
 
 // ---- fp32 path -------------------------------------------------------------------------------------------
+// list logits and rows: all T at once, 8 per block
 int rows_fp32(const RowsArgs& a, aero_ctx* ctx) {
-  distill_dots_kernel<float><<<dim3((unsigned)((a.T + 7) / 8), (unsigned)((a.ls.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
-  distill_rows_kernel<<<(unsigned)((a.T + 7) / 8), 256, 0, ctx->stream>>>(a);
+  const unsigned blocks = (unsigned)((a.T + 7) / 8);
+  distill_dots_kernel<float><<<dim3(blocks, (unsigned)((a.ls.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+  distill_rows_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
   ctx->launches += 2;
+  AERO_CUDA_TRY(cudaGetLastError());
+  return AERO_OK;
+}
+
+template <typename K>
+int launch_fp32(aero_ctx* ctx, K kernel, const Fp32Args& f, long long warps) {
+  const size_t smem = (size_t)(32 * (f.r.d | 1) + 8 * f.r.d) * sizeof(float);
+  AERO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+  kernel<<<(unsigned)((warps + 7) / 8), 256, smem, ctx->stream>>>(f);
+  ctx->launches += 1;
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
 }
@@ -772,9 +803,7 @@ int fwd_fp32(const Call& c, const Ws& s, float* lse, float* kl, float* loss, flo
   if (c.T > 0 && c.R > 0) {
     RowsArgs a = rows_of(c, s, lse, kl, true, 1.f);
     a.ls.entry = nullptr;
-    lse_fp32_kernel<<<row_grid(c.T), 256, 0, ctx->stream>>>(c.T, c.d, c.V, c.R, static_cast<const float*>(c.H),
-                                                            static_cast<const float*>(c.W), c.cs, c.keep, lse);
-    ctx->launches += 1;
+    if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T))) return rc;
     if ((rc = rows_fp32(a, ctx))) return rc;
   }
   return aero_loss_finalize(ctx, s.partials, (int)((c.T + 7) / 8), kPartialStride, loss, metrics, 0);
@@ -789,13 +818,13 @@ int bwd_fp32(const Call& c, const Ws& s, const float* lse, float grad_scale, flo
     if (c.T > 0) AERO_CUDA_TRY(cudaMemsetAsync(dH, 0, (size_t)c.T * c.d * sizeof(float), ctx->stream));
     return AERO_OK;
   }
-  const Fp32Bwd b = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
-  if ((rc = rows_fp32(b.r, ctx))) return rc;
-  dh_fp32_kernel<<<row_grid(c.T), 256, 0, ctx->stream>>>(b);
-  dw_fp32_kernel<<<row_grid(c.V), 256, 0, ctx->stream>>>(b);
-  ctx->launches += 2;
-  AERO_CUDA_TRY(cudaGetLastError());
-  return AERO_OK;
+  AERO_CUDA_TRY(cudaMemsetAsync(s.g, 0, (size_t)c.T * sizeof(float), ctx->stream));      // rows of dropped rollouts
+  const Fp32Args f = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
+  if ((rc = rows_fp32(f.r, ctx))) return rc;
+  const bool narrow = c.d <= 128;                        // sums of a row: 4 or 32 registers a lane
+  rc = launch_fp32(ctx, narrow ? fp32_rows_kernel<4, true> : fp32_rows_kernel<kMaxD32 / 32, true>, f, c.T);
+  if (rc) return rc;
+  return launch_fp32(ctx, narrow ? fp32_vocabulary_kernel<4> : fp32_vocabulary_kernel<kMaxD32 / 32>, f, c.V);
 }
 
 // ---- bf16 path on the tensor cores -------------------------------------------------------------------------

@@ -124,7 +124,7 @@ BF16 = [dict(T=1, d=64, V=1, K=1), dict(T=1, d=64, V=100, K=3), dict(T=7, d=64, 
         dict(T=300, d=192, V=1000, K=33, teacher_lse=True), dict(T=700, d=256, V=2049, K=64), dict(T=257, d=1536, V=700, K=256),
         dict(T=64, d=3584, V=1500, K=5, teacher_lse=True), dict(T=1000, d=64, V=4096, K=20, R=60)]
 FP32 = [dict(T=1, d=1, V=1, K=1), dict(T=3, d=57, V=100, K=3), dict(T=60, d=64, V=300, K=8, teacher_lse=True),
-        dict(T=200, d=96, V=700, K=40)]
+        dict(T=200, d=96, V=700, K=40), dict(T=41, d=129, V=77, K=70), dict(T=33, d=1024, V=100, K=6)]
 
 
 @pytest.mark.parametrize("kw", [dict(k, dtype="bf16") for k in BF16] + [dict(k, dtype="fp32") for k in FP32])
@@ -224,6 +224,30 @@ def test_nothing_kept_and_no_rows(ctx, dtype):
               logits=torch.zeros(5, 4, device="cuda"))
     out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dW=full(300, 64), dH=full(5, 64, dt=case.Ht.dtype))
     assert not dH.any() and not dW.any() and float(out["loss"]) == 0 and not out["kl"].any() and not out["lse"].any()
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_of_dropped_rollouts_are_not_looked_at(ctx, dtype):
+    """NaN and infinities in the hidden states, lists and logits of dropped rollouts change nothing."""
+    case = Case(T=330, d=64, V=500, K=5, dtype=dtype, R=7)
+    assert not case.keep.all()
+    dv, _ = case.device()
+    want = ctx.distill_fwd_bwd(case.cfg, **dv)
+    fwd = ctx.distill_fwd(case.cfg, **dv)
+    wb = ctx.distill_bwd(case.cfg, **dv, lse=fwd["lse"])
+    owner = np.searchsorted(case.cs, np.arange(case.T), side="right") - 1
+    gone = torch.from_numpy(case.keep[owner] == 0).cuda()
+    dv["H"][gone] = float("nan")
+    dv["H"][gone, 3] = float("inf")
+    dv["logits"][gone] = float("nan")
+    dv["ids"][gone, 0] = 10 ** 6
+    got = ctx.distill_fwd_bwd(case.cfg, **dv)
+    gb = ctx.distill_bwd(case.cfg, **dv, lse=fwd["lse"])
+    assert torch.equal(got[0]["kl"], want[0]["kl"]) and torch.equal(got[0]["loss"], want[0]["loss"])
+    for a, b in ((got[1], want[1]), (got[2], want[2]), (gb[0], wb[0]), (gb[1], wb[1])):
+        assert torch.equal(a, b)
+    assert torch.equal(ctx.distill_fwd(case.cfg, **dv)["kl"], fwd["kl"])
     assert ctx.last_status() == 0
 
 

@@ -121,6 +121,7 @@ def test_distill_refusals(lib, fake):
             assert call(**{name: None}) == INVALID, name
         assert call(K=0) == INVALID and call(T=-1) == INVALID and call(T=1 << 31) == INVALID and call(R=-1) == INVALID
         assert call(K=257) == UNSUPPORTED and call(d=96) == UNSUPPORTED and call(c=cfg(9)) == UNSUPPORTED
+        assert call(c=cfg(B.AERO_FP32), d=1025) == UNSUPPORTED
         assert call(H=P + 8) == INVALID and call(W=P + 8) == INVALID and call(ws=P + 16) == INVALID
         assert call(wsb=64) == WORKSPACE
     for call in (bwd, both):
