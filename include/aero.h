@@ -550,7 +550,7 @@ int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
  * A list place with id AERO_NO_TOKEN is empty (its logit is not read), any other id outside [0,V) raises
  * AERO_ST_BAD_TARGET and counts as empty, a logit of -infinity or NaN has q = 0; a row whose list holds no
  * weight contributes nothing.  A token listed twice counts with the sum of its q.  Rows of dropped rollouts
- * get lse = kl = 0 and dH = 0, whatever they hold.  1 <= K <= 256; bf16: d % 64 == 0; fp32 (plain path for
+ * and rows that no rollout owns get lse = kl = 0 and dH = 0, whatever they hold.  1 <= K <= 256; bf16: d % 64 == 0; fp32 (plain path for
  * small shapes): d <= 1024.
  * Inputs   ids [T,K] i32, logits [T,K] f32, teacher_lse [T] f32 or NULL.
  * Outputs  lse, kl [T] f32; loss [1] f32 (overwritten; fixed order of the sums); metrics [4] f32 or NULL: fraction
@@ -611,7 +611,7 @@ int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int
  *   out[t,v] = h_scale[t] w_scale[v] sum_k h8[t,k] w8[v,k]
  * The sum is exact (32-bit integers); it is multiplied by the two scales in fp32 and rounded once to
  * out_dtype (AERO_BF16 | AERO_FP32).  h8 [T,d], w8 [V,d] i8 (-128 .. 127), 16-byte aligned bases,
- * d % 16 == 0, d <= 65536, V <= 2^30; h_scale [T], w_scale [V] f32; out [T,V].
+ * d % 16 == 0, d <= 65536, T and V <= 2^30; h_scale [T], w_scale [V] f32; out [T,V].
  */
 int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t* h8, const float* h_scale,
                    const int8_t* w8, const float* w_scale, int32_t out_dtype, void* out);

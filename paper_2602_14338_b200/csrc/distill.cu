@@ -51,8 +51,8 @@ struct RowsArgs {
   const void* H;
   const void* W;
   const int64_t* cs;
-  const float* w;
   const uint8_t* keep;
+  const float* wrow;       // weight of each row
   float* lse;              // in: the rows' log-sum-exp, unless xstate gives it (then out)
   const int32_t* y;        // the first listed token
   float* g;                // out: -w_i Q_t, or NULL
@@ -77,12 +77,21 @@ __device__ __forceinline__ float warp_max(float v) {
   return v;
 }
 
+// The kept rollout that owns token row t, or -1: the row belongs to a dropped rollout, to none (behind the last one), or to
+// one whose offsets leave [0, T).
+__device__ __forceinline__ int kept_owner(const int64_t* __restrict__ cs, const uint8_t* __restrict__ keep, int R, long long T,
+                                          long long t) {
+  if (R <= 0 || t >= T) return -1;
+  const int i = aero_owner(cs, R, t);
+  const long long a = cs[i], b = cs[i + 1];
+  return keep[i] != 0 && a >= 0 && a <= t && t < b && b <= T ? i : -1;
+}
+
 // The token row of this block's warp; -1: none (past the list, or of a dropped rollout)
 __device__ __forceinline__ long long row_of(const RowsArgs& a, int warp) {
   if (a.tile_row == nullptr) {
     const long long t = (long long)blockIdx.x * 8 + warp;
-    if (t >= a.T) return -1;
-    return a.keep[aero_owner(a.cs, a.R, t)] ? t : -1;
+    return kept_owner(a.cs, a.keep, a.R, a.T, t) >= 0 ? t : -1;
   }
   const int tile = a.tile_begin + blockIdx.x / kBlocksPerTile, r = (blockIdx.x % kBlocksPerTile) * 8 + warp;
   if (tile >= min(*a.n_tiles, a.tile_end) || r >= a.tile_valid[tile]) return -1;
@@ -176,7 +185,7 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
     for (int k = lane; k < d / 8; k += 32) dst[k] = src ? src[k] : make_uint4(0, 0, 0, 0);
   }
   if (t >= 0) {
-    const float wi = a.w[aero_owner(a.cs, a.R, t)];
+    const float wi = a.wrow[t];
     const int yt = a.y[t];
     float lse, lp_y = 0.f;
     if (a.xstate) {
@@ -382,15 +391,17 @@ __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const 
   }
 }
 
-// Before anything else, one warp per row: y_t = the first listed token (0 where the list is empty), the outputs of
-// rows of dropped rollouts, and zeros for the arrays the later kernels count in.
+// Before anything else, one warp per row: y_t = the first listed token (0 where the list is empty) and the row's
+// weight, or the outputs of a row that belongs to no kept rollout.
 struct FirstArgs {
   long long T;
   int d, V, R, K;
   const int32_t* ids;
   const int64_t* cs;
+  const float* w;
   const uint8_t* keep;
   int32_t* y;
+  float* wrow;
   float* lse;              // out, or NULL
   float* kl;               // out, or NULL
   __nv_bfloat16* dH;       // out (bf16 path with gradients), or NULL
@@ -401,8 +412,8 @@ __global__ void __launch_bounds__(256) distill_first_kernel(FirstArgs a) {
   const int lane = threadIdx.x & 31;
   const long long nwarps = (long long)gridDim.x * 8;
   for (long long t = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); t < a.T; t += nwarps) {
-    const bool kept = a.R > 0 && a.keep[aero_owner(a.cs, a.R, t)] != 0;
-    if (!kept) {
+    const int owner = kept_owner(a.cs, a.keep, a.R, a.T, t);
+    if (owner < 0) {
       if (lane == 0) {
         if (a.lse) a.lse[t] = 0.f;
         if (a.kl) a.kl[t] = 0.f;
@@ -421,7 +432,10 @@ __global__ void __launch_bounds__(256) distill_first_kernel(FirstArgs a) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
     if (__any_sync(0xffffffffu, bad) && lane == 0) aero_raise(a.status, AERO_ST_BAD_TARGET);
-    if (lane == 0) a.y[t] = first < a.K ? a.ids[t * a.K + first] : 0;
+    if (lane == 0) {
+      a.y[t] = first < a.K ? a.ids[t * a.K + first] : 0;
+      a.wrow[t] = a.w[owner];
+    }
   }
 }
 
@@ -516,7 +530,7 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
   float* tile = sm;
   float* h = sm + 32 * pitch + warp * d;
   const long long t = (long long)blockIdx.x * 8 + warp;
-  const bool kept = t < a.T && a.keep[aero_owner(a.cs, a.R, t)] != 0;
+  const bool kept = kept_owner(a.cs, a.keep, a.R, a.T, t) >= 0;
   const float lse = GRADS && kept ? a.lse[t] : 0.f, c = GRADS && kept ? -a.grad_scale * a.g[t] : 0.f;
   for (int k = lane; k < d; k += 32) h[k] = kept ? static_cast<const float*>(a.H)[t * d + k] : 0.f;
   float m = -INFINITY, l = 0.f, acc[NC];
@@ -613,6 +627,7 @@ struct Ws {
   int* range_count;
   int* range_rows;
   int32_t* y;
+  float* wrow;
   float* g;
   float* z;
   float* entry;
@@ -644,6 +659,7 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   w.range_count = w.zero + 192;
   w.range_rows = reinterpret_cast<int*>(take(kRangeCap * sizeof(int)));
   w.y = reinterpret_cast<int32_t*>(take(Tn * 4));
+  w.wrow = reinterpret_cast<float*>(take(Tn * 4));
   w.g = reinterpret_cast<float*>(take(Tn * 4));
   w.z = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   if (mode != kFwd) w.entry = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
@@ -757,7 +773,7 @@ unsigned row_grid(int64_t T) {
 RowsArgs rows_of(const Call& c, const Ws& s, float* lse, float* kl, bool partials, float grad_scale) {
   RowsArgs a = {};
   a.ls = {c.K, c.ids, c.logits, c.tlse, kl, s.z, s.entry, partials ? s.partials : nullptr};
-  a.T = c.T; a.d = c.d; a.V = c.V; a.R = c.R; a.H = c.H; a.W = c.W; a.cs = c.cs; a.w = c.w; a.keep = c.keep;
+  a.T = c.T; a.d = c.d; a.V = c.V; a.R = c.R; a.H = c.H; a.W = c.W; a.cs = c.cs; a.keep = c.keep; a.wrow = s.wrow;
   a.lse = lse; a.y = s.y; a.g = s.g; a.grad_scale = grad_scale; a.plan = s.plan;
   return a;
 }
@@ -767,7 +783,7 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
   AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, 1024, ctx->stream));
   if (partials) AERO_CUDA_TRY(cudaMemsetAsync(s.partials, 0, s.n_partials * kPartialStride * sizeof(double), ctx->stream));
   if (c.T == 0) return AERO_OK;
-  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.cs, c.keep, s.y, lse, kl, static_cast<__nv_bfloat16*>(dH16),
+  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.cs, c.w, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
                        ctx->d_status};
   distill_first_kernel<<<row_grid(c.T), 256, 0, ctx->stream>>>(f);
   ctx->launches += 1;

@@ -319,7 +319,7 @@ q8_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ 
 extern "C" int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t* h8, const float* h_scale,
                               const int8_t* w8, const float* w_scale, int32_t out_dtype, void* out) {
   AeroRange nv("aero_lmhead_q8");
-  if (!ctx || T < 0 || T >= (int64_t)1 << 31 || d <= 0 || V <= 0 || !w8 || !w_scale) return AERO_ERR_INVALID;
+  if (!ctx || T < 0 || T > (int64_t)1 << 30 || d <= 0 || V <= 0 || !w8 || !w_scale) return AERO_ERR_INVALID;
   if (T > 0 && (!h8 || !h_scale || !out)) return AERO_ERR_INVALID;
   if (out_dtype != AERO_BF16 && out_dtype != AERO_FP32) return AERO_ERR_UNSUPPORTED;
   if (d % 16 != 0 || d > kMaxD || V > (1 << 30)) return AERO_ERR_UNSUPPORTED;

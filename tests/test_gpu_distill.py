@@ -252,6 +252,26 @@ def test_rows_of_dropped_rollouts_are_not_looked_at(ctx, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_rows_that_no_rollout_owns(ctx, dtype):
+    """Rows before the first offset and behind the last one come out as zeros."""
+    case = Case(T=290, d=64, V=400, K=5, dtype=dtype, R=4, drop=False)
+    dv, _ = case.device()
+    pad = lambda a, fill: torch.cat([torch.full_like(a[:7], fill), a, torch.full_like(a[:50], fill)])
+    padded = dict(dv, H=pad(dv["H"], 1.0), ids=pad(dv["ids"], 3), logits=pad(dv["logits"], 1.0), cs=dv["cs"] + 7)
+    full = torch.full((347, 64), 9.0, dtype=case.Ht.dtype, device="cuda")
+    out = {k: torch.full((347,), 9.0, device="cuda") for k in ("lse", "kl")}
+    want, wH, wW = ctx.distill_fwd_bwd(case.cfg, **dv)
+    got, gH, gW = ctx.distill_fwd_bwd(case.cfg, **padded, dH=full, out=out)
+    r = case.reference()
+    check_grads(case, gH[7:297], gW, r)
+    close(got["kl"][7:297], r["kl"], r["t_kl"], "kl")
+    assert torch.equal(got["loss"], want["loss"]) or abs(float(got["loss"] - want["loss"])) <= 1e-5 * abs(float(want["loss"]))
+    for a in (got["lse"], got["kl"], gH):
+        assert not a[:7].any() and not a[297:].any()
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_bad_ids_raise_the_status_bit_and_count_as_empty(ctx, dtype):
     case = Case(T=150, d=64, V=200, K=5, dtype=dtype, R=4)
     dv, _ = case.device()

@@ -85,6 +85,7 @@ def test_lmhead_q8_refusals(lib, fake):
     for name in ("ctx", "h", "hs", "w", "ws", "out"):
         assert call(**{name: None}) == INVALID, name
     assert call(T=-1) == INVALID and call(V=0) == INVALID and call(d=0) == INVALID
+    assert call(T=(1 << 30) + 1) == INVALID
     assert call(d=72) == UNSUPPORTED and call(d=65552) == UNSUPPORTED and call(dt=5) == UNSUPPORTED
     assert call(h=P + 8) == INVALID and call(w=P + 8) == INVALID and call(out=P + 1) == INVALID
 
