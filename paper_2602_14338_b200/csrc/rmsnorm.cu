@@ -333,19 +333,21 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(), bwd_blocks<VEC, NV>())
   }
 }
 
-// dgamma (+)= the blocks' shares: 32 columns per block, 32 rows of shares at a time
+// dgamma (+)= the blocks' shares: 16 columns per block, 64 rows of shares at a time
 __global__ void __launch_bounds__(1024) dgamma_kernel(const float* __restrict__ part, int n, int d, float* dgamma,
                                                       int accumulate) {
-  __shared__ float sh[32][33];
-  const int col = blockIdx.x * 32 + (threadIdx.x & 31), r0 = threadIdx.x >> 5;
+  __shared__ float sh[64][17];
+  const int c = threadIdx.x & 15, col = blockIdx.x * 16 + c, r0 = threadIdx.x >> 4;
   float v = 0.f;
-  if (col < d)
-    for (int r = r0; r < n; r += 32) v += part[(size_t)r * d + col];
-  sh[r0][threadIdx.x & 31] = v;
+  if (col < d) {
+#pragma unroll 8
+    for (int r = r0; r < n; r += 64) v += part[(size_t)r * d + col];
+  }
+  sh[r0][c] = v;
   __syncthreads();
   if (r0 == 0 && col < d) {
     float sum = 0.f;
-    for (int r = 0; r < 32; ++r) sum += sh[r][threadIdx.x];
+    for (int r = 0; r < 64; ++r) sum += sh[r][c];
     dgamma[col] = accumulate ? dgamma[col] + sum : sum;
   }
 }
@@ -413,7 +415,7 @@ int launch_bwd(aero_ctx* ctx, const BwdArgs& a, float* dgamma, int accumulate) {
                            &grid);
   });
   if (rc) return rc;
-  dgamma_kernel<<<(a.d + 31) / 32, 1024, 0, ctx->stream>>>(a.part, grid, a.d, dgamma, accumulate);
+  dgamma_kernel<<<(a.d + 15) / 16, 1024, 0, ctx->stream>>>(a.part, grid, a.d, dgamma, accumulate);
   ctx->launches += 1;
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
