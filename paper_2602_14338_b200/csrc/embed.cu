@@ -301,12 +301,38 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int n, int V
 // in the tile after to part[tile][1].  Rows are held packed and two are in flight beyond the two being added: more per
 // warp costs registers, and it is warps that keep the memory busy (204780 x 1536: 379 us with eight unpacked rows a
 // turn, 202 with four packed ones, 173 with two; 277 with tiles of 128 positions).
-constexpr int kTile = 32, kInFlight = 2;
+constexpr int kTile = 32, kInFlight = 2, kShortRun = 8;
+
+// Runs that reach over the end of the tile they start in, for the joining kernel: first and last tile; those of few
+// tiles from the front, longer ones from the back.
+struct Runs {
+  int2* list;              // [tiles]
+  int* count;              // [2]: short, long
+  int tiles;
+};
+
+// The warp that adds up the first slab of such a run's first tile b puts it on the list: tiles b + 1 .. last start with
+// its key, those after do not; a search 32 tiles wide, first over the nearest ones.
+__device__ __forceinline__ void list_run(const Runs& runs, const uint32_t* __restrict__ keys, uint32_t key, int b, int lane) {
+  int lo = b + 1, hi = runs.tiles, step = 1;
+  while (hi - lo > 1) {
+    const int k = lo + (lane + 1) * step;
+    const int ahead = __popc(__ballot_sync(0xffffffffu, k < hi && keys[(long long)k * kTile] == key));
+    if (ahead < 32) hi = min(hi, lo + (ahead + 1) * step);
+    lo += ahead * step;
+    step = ahead == 32 ? max(1, (hi - lo + 31) / 32) : (hi - lo + 31) / 32;
+  }
+  if (lane == 0) {
+    if (lo - b <= kShortRun) runs.list[atomicAdd(&runs.count[0], 1)] = make_int2(b, lo);
+    else runs.list[runs.tiles - 1 - atomicAdd(&runs.count[1], 1)] = make_int2(b, lo);
+  }
+}
+
 template <typename T, int VEC>
 __global__ void __launch_bounds__(256) embed_bwd_sum_kernel(int n, int d, int V, const uint32_t* __restrict__ keys,
                                                             const uint32_t* __restrict__ pos, const T* __restrict__ dX,
                                                             float scale, float* __restrict__ dW, int accumulate,
-                                                            float* __restrict__ part) {
+                                                            float* __restrict__ part, Runs runs) {
   using Raw = typename rowvec::Raw<T, VEC>::type;
   constexpr int U = kInFlight;
   const int lane = threadIdx.x & 31;
@@ -357,6 +383,7 @@ __global__ void __launch_bounds__(256) embed_bwd_sum_kernel(int n, int d, int V,
             if (head || tail) put<VEC>(part + ((size_t)tile * 2 + (head ? 0 : 1)) * d + c, acc, 1.f, false);
             else put<VEC>(dW + (long long)key * d + c, acc, scale, accumulate != 0);
           }
+          if (tail && !head && c < 32 * VEC) list_run(runs, keys, key, (int)tile, lane);
 #pragma unroll
           for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
           run0 = k + q + 1;
@@ -366,34 +393,21 @@ __global__ void __launch_bounds__(256) embed_bwd_sum_kernel(int n, int d, int V,
   }
 }
 
-// Runs that start in a tile and reach into the tiles after it.  A block looks at kJoin tiles and 128 columns: a run of
-// a few tiles is added up by one warp, a longer one by all eight, a contiguous eighth of its tiles each, in order.
-constexpr int kJoin = 32, kShortRun = 8;
-__global__ void __launch_bounds__(256) embed_bwd_join_kernel(int n, int d, int V, const uint32_t* __restrict__ keys,
+// Adds up the partial sums of the listed runs, 128 columns at a time: a run of a few tiles by one warp, a longer one by
+// the eight warps of a block, a contiguous eighth of its tiles each, in order.  (The order of the list does not matter:
+// every run has its own row of dW.)  The list is what makes this short: blocks that each looked through 32 tiles for
+// runs took 57 us at 204780 x 1536, most of it waiting for the few that had found some; from the list it is 28 us.
+__global__ void __launch_bounds__(256) embed_bwd_join_kernel(int d, const uint32_t* __restrict__ keys,
                                                              const float* __restrict__ part, float scale,
-                                                             float* __restrict__ dW, int accumulate) {
+                                                             float* __restrict__ dW, int accumulate, Runs runs) {
   __shared__ float sh[8][128];
-  __shared__ int long_last[kJoin];
-  __shared__ unsigned starts;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, c0 = blockIdx.y * 128;
-  const int tiles = (n + kTile - 1) / kTile;
-  if (warp == 0) {
-    // a lane per tile: does a run start in it and go on in the next one?
-    const long long b = (long long)blockIdx.x * kJoin + lane, end = (b + 1) * kTile;
-    bool yes = false;
-    if (b + 1 < tiles) {
-      const uint32_t key = keys[end - 1];
-      yes = key != (uint32_t)V && keys[end] == key && (keys[end - kTile] != key || b == 0 || keys[end - kTile - 1] != key);
-    }
-    const unsigned m = __ballot_sync(0xffffffffu, yes);
-    long_last[lane] = -1;
-    if (lane == 0) starts = m;
-  }
-  __syncthreads();
-  if (starts == 0) return;
-  int col[4];                                                    // (columns past d read the last one and are dropped)
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, slabs = (d + 127) / 128;
+  int c0 = 0, col[4];                                            // (columns past d read the last one and are dropped)
+  auto at_slab = [&](int slab) {
+    c0 = slab * 128;
 #pragma unroll
-  for (int q = 0; q < 4; ++q) col[q] = min(c0 + q * 32 + lane, d - 1);
+    for (int q = 0; q < 4; ++q) col[q] = min(c0 + q * 32 + lane, d - 1);
+  };
   auto add = [&](int k0, int k1, float (&acc)[4]) {              // slot 0 of tiles k0 .. k1 - 1, 32 loads in flight
     for (int k = k0; k < k1; k += 8) {
       float v[8][4];
@@ -407,39 +421,18 @@ __global__ void __launch_bounds__(256) embed_bwd_join_kernel(int n, int d, int V
         for (int q = 0; q < 4; ++q) acc[q] += k + i < k1 ? v[i][q] : 0.f;
     }
   };
-  auto finish = [&](int b, uint32_t key, int c, float sum) {     // + the run's share of its first tile (slot 1)
+  auto finish = [&](int b, int c, float sum) {                   // + the run's share of its first tile (slot 1)
     sum += part[((size_t)b * 2 + 1) * d + c];
-    float* dst = dW + (long long)key * d + c;
+    float* dst = dW + (long long)keys[((long long)b + 1) * kTile - 1] * d + c;
     *dst = accumulate ? fmaf(sum, scale, *dst) : sum * scale;
   };
-  for (int i = warp; i < kJoin; i += 8) {
-    if (!(starts >> i & 1u)) continue;
-    const int b = blockIdx.x * kJoin + i;
-    const uint32_t key = keys[((long long)b + 1) * kTile - 1];
-    // the run's last tile: tiles b + 1 .. last start with its key, those after do not; a search 32 tiles wide
-    int lo = b + 1, hi = tiles;
-    while (hi - lo > 1) {
-      const int step = (hi - lo + 31) / 32, k = lo + (lane + 1) * step;
-      const int ahead = __popc(__ballot_sync(0xffffffffu, k < hi && keys[(long long)k * kTile] == key));
-      hi = min(hi, lo + (ahead + 1) * step);
-      lo += ahead * step;
-    }
-    if (lo - b > kShortRun) {
-      if (lane == 0) long_last[i] = lo;
-      continue;
-    }
+  const long long n_short = (long long)runs.count[0] * slabs, n_long = (long long)runs.count[1] * slabs;
+  for (long long i = blockIdx.x; i < n_long; i += gridDim.x) {   // (long ones first: they take longest)
+    const int2 run = runs.list[runs.tiles - 1 - i / slabs];
+    at_slab((int)(i % slabs));
+    const int count = run.y - run.x;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    add(b + 1, lo + 1, acc);
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (c0 + q * 32 + lane < d) finish(b, key, c0 + q * 32 + lane, acc[q]);
-  }
-  __syncthreads();
-  for (int i = 0; i < kJoin; ++i) {
-    if (long_last[i] < 0) continue;
-    const int b = blockIdx.x * kJoin + i, count = long_last[i] - b;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    add(b + 1 + (int)((long long)count * warp / 8), b + 1 + (int)((long long)count * (warp + 1) / 8), acc);
+    add(run.x + 1 + (int)((long long)count * warp / 8), run.x + 1 + (int)((long long)count * (warp + 1) / 8), acc);
     __syncthreads();                                             // the previous run's sums have been read
 #pragma unroll
     for (int q = 0; q < 4; ++q) sh[warp][q * 32 + lane] = acc[q];
@@ -447,8 +440,17 @@ __global__ void __launch_bounds__(256) embed_bwd_join_kernel(int n, int d, int V
     if (threadIdx.x < 128 && c0 + (int)threadIdx.x < d) {
       float sum = 0.f;
       for (int w = 0; w < 8; ++w) sum += sh[w][threadIdx.x];
-      finish(b, keys[((long long)b + 1) * kTile - 1], c0 + threadIdx.x, sum);
+      finish(run.x, c0 + threadIdx.x, sum);
     }
+  }
+  for (long long i = (long long)blockIdx.x * 8 + warp; i < n_short; i += (long long)gridDim.x * 8) {
+    const int2 run = runs.list[i / slabs];
+    at_slab((int)(i % slabs));
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    add(run.x + 1, run.y + 1, acc);
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      if (c0 + q * 32 + lane < d) finish(run.x, c0 + q * 32 + lane, acc[q]);
   }
 }
 
@@ -458,6 +460,7 @@ struct Ws {
   uint32_t* pos[2];
   uint32_t* counts;
   float* part;
+  Runs runs;
   size_t bytes;
 };
 
@@ -475,6 +478,9 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V) {
     const size_t blocks = ((size_t)T + kSortTile - 1) / kSortTile, tiles = ((size_t)T + kTile - 1) / kTile;
     w.counts = reinterpret_cast<uint32_t*>(take(blocks * kMaxRadix * sizeof(uint32_t)));
     w.part = reinterpret_cast<float*>(take(tiles * 2 * (size_t)d * sizeof(float)));
+    w.runs.list = reinterpret_cast<int2*>(take(tiles * sizeof(int2)));
+    w.runs.count = reinterpret_cast<int*>(take(2 * sizeof(int)));
+    w.runs.tiles = (int)tiles;
   }
   w.bytes = off > 0 ? off : 256;
   return w;
@@ -540,10 +546,10 @@ int bwd_launch(aero_ctx* ctx, int64_t T_, int32_t d, int32_t V, const int32_t* y
   const int rc = sort_positions(ctx, w, n, d, V, y, accumulate ? nullptr : dW, &keys, &pos);
   if (rc) return rc;
   const long long tiles = (n + kTile - 1) / kTile, slabs = (d + 32 * VEC - 1) / (32 * VEC);
-  embed_bwd_sum_kernel<T, VEC><<<(unsigned)((tiles * slabs + 7) / 8), 256, 0, ctx->stream>>>(n, d, V, keys, pos, dX, scale, dW,
-                                                                                             accumulate, w.part);
-  const dim3 jgrid((unsigned)((tiles + kJoin - 1) / kJoin), (unsigned)((d + 127) / 128));
-  embed_bwd_join_kernel<<<jgrid, 256, 0, ctx->stream>>>(n, d, V, keys, w.part, scale, dW, accumulate);
+  AERO_CUDA_TRY(cudaMemsetAsync(w.runs.count, 0, 2 * sizeof(int), ctx->stream));
+  embed_bwd_sum_kernel<T, VEC><<<(unsigned)((tiles * slabs + 7) / 8), 256, 0, ctx->stream>>>(
+      n, d, V, keys, pos, dX, scale, dW, accumulate, w.part, w.runs);
+  embed_bwd_join_kernel<<<8 * ctx->sm_count, 256, 0, ctx->stream>>>(d, keys, w.part, scale, dW, accumulate, w.runs);
   ctx->launches += 2;
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
