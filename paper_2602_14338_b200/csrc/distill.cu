@@ -494,8 +494,9 @@ __global__ void __launch_bounds__(256) plan_kernel(PlanArgs a) {
 }
 
 // ---- fp32 path, for small shapes -----------------------------------------------------------------
-// Blocks of eight warps; 32 rows of the other operand at a time stand in shared memory, a row apart by an odd number
-// of words, and a lane has one of them: a logit is d products in a lane, without a reduction.
+// A block per row, its warps sharing the other operand's rows between them: 32 at a time stand in a warp's part of
+// shared memory, a row apart by an odd number of words, and a lane has one of them, so that a logit is d products
+// in a lane, without a reduction.  The warps' results are added in order.
 constexpr int kMaxD32 = 1024;
 
 struct Fp32Args {
@@ -505,14 +506,18 @@ struct Fp32Args {
   int accumulate;
 };
 
-// 32 rows of `src` from row r0 into the staging area (zeros past `n`, and where `g` says that the row has no weight, so
-// that what stands in rows of dropped rollouts is not looked at)
+// 32 rows of `src` from row r0 into the warp's staging area (zeros past `n`, and where `g` says that the row has no
+// weight, so that what stands in rows of dropped rollouts is not looked at)
 __device__ __forceinline__ void stage_rows(float* dst, int pitch, const float* src, long long r0, long long n, int d,
                                            const float* g) {
-  for (int i = threadIdx.x >> 5; i < 32; i += 8) {
+  const int lane = threadIdx.x & 31;
+  __syncwarp();
+#pragma unroll 4
+  for (int i = 0; i < 32; ++i) {
     const bool there = r0 + i < n && (g == nullptr || g[r0 + i] != 0.f);
-    for (int k = threadIdx.x & 31; k < d; k += 32) dst[i * pitch + k] = there ? src[(r0 + i) * d + k] : 0.f;
+    for (int k = lane; k < d; k += 32) dst[i * pitch + k] = there ? src[(r0 + i) * d + k] : 0.f;
   }
+  __syncwarp();
 }
 __device__ __forceinline__ float dot(const float* a, const float* b, int d) {
   float z = 0.f;
@@ -520,26 +525,53 @@ __device__ __forceinline__ float dot(const float* a, const float* b, int d) {
   for (int k = 0; k < d; ++k) z = fmaf(a[k], b[k], z);
   return z;
 }
+// acc += sum_i x_i tile[i, :], lane i holding x_i
+template <int NC>
+__device__ __forceinline__ void add_rows(float (&acc)[NC], float x_mine, const float* tile, int pitch, int d) {
+  const int lane = threadIdx.x & 31;
+  for (int i = 0; i < 32; ++i) {
+    const float x = __shfl_sync(0xffffffffu, x_mine, i);
+#pragma unroll
+    for (int q = 0; q < NC; ++q)
+      if (q * 32 + lane < d) acc[q] = fmaf(x, tile[i * pitch + q * 32 + lane], acc[q]);
+  }
+}
+// the warps' rows of sums, added in order, to out[d]
+template <int NC>
+__device__ __forceinline__ void join_rows(const float (&acc)[NC], float* sm, int d, float* out, bool accumulate) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = blockDim.x >> 5;
+  __syncthreads();                                       // the staged rows have been read
+#pragma unroll
+  for (int q = 0; q < NC; ++q)
+    if (q * 32 + lane < d) sm[warp * d + q * 32 + lane] = acc[q];
+  __syncthreads();
+  for (int k = threadIdx.x; k < d; k += blockDim.x) {
+    float s = 0.f;
+    for (int w = 0; w < nw; ++w) s += sm[w * d + k];
+    out[k] = accumulate ? out[k] + s : s;
+  }
+}
 
-// A warp per token row: its log-sum-exp, or its row of dH.  NC * 32 >= d.
+// Block t: the row's log-sum-exp, or its row of dH.  NC * 32 >= d.
 template <int NC, bool GRADS>
 __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
   extern __shared__ float sm[];
+  __shared__ float2 state[8];
   const RowsArgs& a = f.r;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.d, pitch = d | 1, K = a.ls.K;
-  float* tile = sm;
-  float* h = sm + 32 * pitch + warp * d;
-  const long long t = (long long)blockIdx.x * 8 + warp;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = blockDim.x >> 5, d = a.d, pitch = d | 1, K = a.ls.K;
+  float* h = sm;
+  float* tile = sm + d + warp * 32 * pitch;
+  const long long t = blockIdx.x;
   const bool kept = kept_owner(a.cs, a.keep, a.R, a.T, t) >= 0;
   const float lse = GRADS && kept ? a.lse[t] : 0.f, c = GRADS && kept ? -a.grad_scale * a.g[t] : 0.f;
-  for (int k = lane; k < d; k += 32) h[k] = kept ? static_cast<const float*>(a.H)[t * d + k] : 0.f;
+  for (int k = threadIdx.x; k < d; k += blockDim.x) h[k] = kept ? static_cast<const float*>(a.H)[t * d + k] : 0.f;
+  __syncthreads();
   float m = -INFINITY, l = 0.f, acc[NC];
 #pragma unroll
   for (int q = 0; q < NC; ++q) acc[q] = 0.f;
-  for (int v0 = 0; v0 < a.V; v0 += 32) {
-    __syncthreads();
+  const bool work = GRADS ? c != 0.f : kept;
+  for (int v0 = warp * 32; work && v0 < a.V; v0 += nw * 32) {
     stage_rows(tile, pitch, static_cast<const float*>(a.W), v0, a.V, d, nullptr);
-    __syncthreads();
     const float z = dot(h, tile + lane * pitch, d);
     const bool in = v0 + lane < a.V;
     if (!GRADS) {
@@ -550,7 +582,6 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
       }
       continue;
     }
-    if (c == 0.f) continue;                              // (the same for the whole warp)
     float dz = in ? c * expf(z - lse) : 0.f;
     for (int k0 = 0; k0 < K; k0 += 32) {                 // at a listed token the entry takes the place of the softmax part
       const int id = k0 + lane < K ? a.ls.ids[t * K + k0 + lane] : -1;
@@ -559,63 +590,55 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
         if (v == v0 + lane) dz = a.ls.entry[t * K + k0 + src];
       }
     }
-    for (int v = 0; v < 32; ++v) {
-      const float x = __shfl_sync(0xffffffffu, dz, v);
-#pragma unroll
-      for (int q = 0; q < NC; ++q)
-        if (q * 32 + lane < d) acc[q] = fmaf(x, tile[v * pitch + q * 32 + lane], acc[q]);
-    }
+    add_rows<NC>(acc, dz, tile, pitch, d);
   }
   if (GRADS) {
-    if (t < a.T)
-#pragma unroll
-      for (int q = 0; q < NC; ++q)
-        if (q * 32 + lane < d) f.dH[t * d + q * 32 + lane] = acc[q];
+    join_rows<NC>(acc, sm, d, f.dH + t * d, false);
   } else {
     const float M = warp_max(m);
     l = warp_sum(m > -INFINITY ? l * expf(m - M) : 0.f);
-    if (lane == 0 && kept) a.lse[t] = M + logf(l);
+    if (lane == 0) state[warp] = make_float2(M, l);
+    __syncthreads();
+    if (threadIdx.x == 0 && kept) {
+      float top = -INFINITY, sum = 0.f;
+      for (int w = 0; w < nw; ++w) top = fmaxf(top, state[w].x);
+      for (int w = 0; w < nw; ++w)
+        if (state[w].x > -INFINITY) sum += state[w].y * expf(state[w].x - top);
+      a.lse[t] = top + logf(sum);
+    }
   }
 }
 
-// A warp per vocabulary row: dW[v, :] (+)= sum_t dz_tv H[t, :], tokens in order.
+// Block v: dW[v, :] (+)= sum_t dz_tv H[t, :].
 template <int NC>
 __global__ void __launch_bounds__(256) fp32_vocabulary_kernel(Fp32Args f) {
   extern __shared__ float sm[];
   const RowsArgs& a = f.r;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, d = a.d, pitch = d | 1, K = a.ls.K;
-  float* tile = sm;
-  float* w = sm + 32 * pitch + warp * d;
-  const int v = blockIdx.x * 8 + warp;
-  for (int k = lane; k < d; k += 32) w[k] = v < a.V ? static_cast<const float*>(a.W)[(long long)v * d + k] : 0.f;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = blockDim.x >> 5, d = a.d, pitch = d | 1, K = a.ls.K;
+  float* w = sm;
+  float* tile = sm + d + warp * 32 * pitch;
+  const int v = blockIdx.x;
+  for (int k = threadIdx.x; k < d; k += blockDim.x) w[k] = static_cast<const float*>(a.W)[(long long)v * d + k];
+  __syncthreads();
   float acc[NC];
 #pragma unroll
   for (int q = 0; q < NC; ++q) acc[q] = 0.f;
-  for (long long t0 = 0; t0 < a.T; t0 += 32) {
-    __syncthreads();
-    stage_rows(tile, pitch, static_cast<const float*>(a.H), t0, a.T, d, a.g);
-    __syncthreads();
+  for (long long t0 = warp * 32; t0 < a.T; t0 += nw * 32) {
     const long long t = t0 + lane;
     const float c = t < a.T ? -a.grad_scale * a.g[t] : 0.f;      // (0 for the rows of dropped rollouts)
+    if (!__any_sync(0xffffffffu, c != 0.f)) continue;
+    stage_rows(tile, pitch, static_cast<const float*>(a.H), t0, a.T, d, a.g);
     const float z = dot(w, tile + lane * pitch, d);
-    float dz = c != 0.f ? c * expf(z - a.lse[t]) : 0.f;
-    if (c != 0.f)
+    float dz = 0.f;
+    if (c != 0.f) {
+      dz = c * expf(z - a.lse[t]);
+#pragma unroll 4
       for (int k = 0; k < K; ++k)
         if (a.ls.ids[t * K + k] == v) dz = a.ls.entry[t * K + k];
-    for (int i = 0; i < 32; ++i) {
-      const float x = __shfl_sync(0xffffffffu, dz, i);
-#pragma unroll
-      for (int q = 0; q < NC; ++q)
-        if (q * 32 + lane < d) acc[q] = fmaf(x, tile[i * pitch + q * 32 + lane], acc[q]);
     }
+    add_rows<NC>(acc, dz, tile, pitch, d);
   }
-  if (v < a.V)
-#pragma unroll
-    for (int q = 0; q < NC; ++q)
-      if (q * 32 + lane < d) {
-        float* o = f.dW + (long long)v * d + q * 32 + lane;
-        *o = f.accumulate ? *o + acc[q] : acc[q];
-      }
+  join_rows<NC>(acc, sm, d, f.dW + (long long)v * d, f.accumulate != 0);
 }
 
 // ---- workspace -----------------------------------------------------------------------------------------
@@ -802,11 +825,17 @@ int rows_fp32(const RowsArgs& a, aero_ctx* ctx) {
   return AERO_OK;
 }
 
+// a block per row of `rows`, of as many warps (up to eight) as have work and room for their staged rows
 template <typename K>
-int launch_fp32(aero_ctx* ctx, K kernel, const Fp32Args& f, long long warps) {
-  const size_t smem = (size_t)(32 * (f.r.d | 1) + 8 * f.r.d) * sizeof(float);
+int launch_fp32(aero_ctx* ctx, K kernel, const Fp32Args& f, long long rows, long long others) {
+  const int d = f.r.d;
+  const size_t per_warp = (size_t)32 * (d | 1) * sizeof(float);
+  int warps = (int)((200 * 1024) / per_warp);
+  if (warps > 8) warps = 8;
+  if (warps > (others + 31) / 32) warps = (int)((others + 31) / 32);
+  const size_t smem = d * sizeof(float) + warps * per_warp;
   AERO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-  kernel<<<(unsigned)((warps + 7) / 8), 256, smem, ctx->stream>>>(f);
+  kernel<<<(unsigned)rows, warps * 32, smem, ctx->stream>>>(f);
   ctx->launches += 1;
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
@@ -819,7 +848,7 @@ int fwd_fp32(const Call& c, const Ws& s, float* lse, float* kl, float* loss, flo
   if (c.T > 0 && c.R > 0) {
     RowsArgs a = rows_of(c, s, lse, kl, true, 1.f);
     a.ls.entry = nullptr;
-    if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T))) return rc;
+    if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T, c.V))) return rc;
     if ((rc = rows_fp32(a, ctx))) return rc;
   }
   return aero_loss_finalize(ctx, s.partials, (int)((c.T + 7) / 8), kPartialStride, loss, metrics, 0);
@@ -838,9 +867,9 @@ int bwd_fp32(const Call& c, const Ws& s, const float* lse, float grad_scale, flo
   const Fp32Args f = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
   if ((rc = rows_fp32(f.r, ctx))) return rc;
   const bool narrow = c.d <= 128;                        // sums of a row: 4 or 32 registers a lane
-  rc = launch_fp32(ctx, narrow ? fp32_rows_kernel<4, true> : fp32_rows_kernel<kMaxD32 / 32, true>, f, c.T);
+  rc = launch_fp32(ctx, narrow ? fp32_rows_kernel<4, true> : fp32_rows_kernel<kMaxD32 / 32, true>, f, c.T, c.V);
   if (rc) return rc;
-  return launch_fp32(ctx, narrow ? fp32_vocabulary_kernel<4> : fp32_vocabulary_kernel<kMaxD32 / 32>, f, c.V);
+  return launch_fp32(ctx, narrow ? fp32_vocabulary_kernel<4> : fp32_vocabulary_kernel<kMaxD32 / 32>, f, c.V, c.T);
 }
 
 // ---- bf16 path on the tensor cores -------------------------------------------------------------------------
