@@ -36,7 +36,7 @@ def _stale() -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, out: str | None = None, defines=()) -> str:
-    """Build the library.  `out` and `defines` (e.g. ["AERO_TC_STAGES=3"]) make a tuning variant
+    """Build the library.  `out` and `defines` (e.g. ["AERO_LMHEAD_STAGES=3"]) make a tuning variant
     somewhere else; binding.py loads it when AERO_B200_LIB names it."""
     if out is None and not force and not _stale():
         return OUT

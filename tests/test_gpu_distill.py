@@ -362,6 +362,37 @@ def test_captured_and_replayed(ctx):
     c.close()
 
 
+def test_with_stage_b_in_one_process(ctx):
+    """Stage (b) and the distillation share kernels, whichever of them a process runs first: the log-prob pass and the
+    three calls of the loss, the distillation's, and the first again, each with the same bits as before."""
+    case = Case(T=300, d=192, V=1000, K=8)
+    dv, _ = case.device()
+    T, R = case.T, len(case.keep)
+    g = torch.Generator().manual_seed(3)
+    y = torch.randint(0, case.V, (T,), generator=g).int().cuda()
+    old = (-torch.rand(T, generator=g) * 5).cuda()
+    adv = torch.randn(R, generator=g).cuda()
+
+    def stage_b():
+        f = ctx.grpo_loss_fwd(case.cfg, dv["H"], dv["W"], y, old, dv["cs"], adv, dv["w"], dv["keep"])
+        dH, dW = ctx.grpo_loss_bwd(case.cfg, dv["H"], dv["W"], y, dv["cs"], dv["keep"], f["lse"], f["g"], logp=f["logp"])
+        f2, dH2, dW2 = ctx.grpo_loss_fwd_bwd(case.cfg, dv["H"], dv["W"], y, old, dv["cs"], adv, dv["w"], dv["keep"])
+        kept = dv["keep"].bool()[torch.searchsorted(dv["cs"], torch.arange(T, device="cuda"), right=True) - 1]
+        return [f["lse"][kept].clone(), dW.clone(), f2["lse"][kept].clone(), dW2.clone()]
+
+    def distill():
+        f = ctx.distill_fwd(case.cfg, **dv)
+        dH, dW = ctx.distill_bwd(case.cfg, **dv, lse=f["lse"])
+        f2, dH2, dW2 = ctx.distill_fwd_bwd(case.cfg, **dv)
+        return [f["lse"].clone(), dH.clone(), dW.clone(), f2["lse"].clone(), dH2.clone(), dW2.clone()]
+
+    b, e = stage_b(), distill()
+    for was, now in zip(b + e, stage_b() + distill()):
+        assert torch.equal(was, now)
+    check_forward(case, ctx.distill_fwd(case.cfg, **dv), case.reference())
+    assert ctx.last_status() == 0
+
+
 def test_a_step_of_the_ends_together(ctx):
     """As a training step uses them: the frozen teacher's final norm with its 8-bit output and the 8-bit product give
     logits, whose largest are the teacher's list; the student's norm gives H; the group stage gives keep and weights; the
