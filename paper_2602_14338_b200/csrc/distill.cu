@@ -442,8 +442,10 @@ __global__ void __launch_bounds__(256) distill_first_kernel(FirstArgs a) {
 // Splits of this chunk's launches, from the number of token tiles the device found: plan[0] vocabulary splits of
 // the lm_head kernel, plan[1] ranges of the reduction of dH.  Each candidate's cost is the rounds of its units over
 // the CTA (pair)s times the length of a unit, in vocabulary tiles or 64-deep slabs, plus what a unit and a split
-// cost besides (measured: about 0.4 tiles, and 8 slabs and the traffic of the fp32 sums).  Without the splits a
-// call of a few hundred tokens leaves most SMs idle (300 tokens at d = 1536: 6.7 ms instead of 0.9 ms).
+// cost besides: 0.4 tiles (with 1 or 2 instead the loss of 2000 tokens takes 643 or 647 us, not 624, of 5000 tokens
+// 1496 or 1517, not 1471), and an estimate of 8 slabs and the traffic of the fp32 sums.  With stage (b)'s at most
+// four splits of the vocabulary and none of dH a small call leaves most SMs idle (d = 1536: loss of 1000 tokens 1290
+// us instead of 370, step of 300 tokens 2410 instead of 490).
 // Block 0 plans; with dW given all blocks clear it if there is no tile at all (the products then write nothing).
 struct PlanArgs {
   const int32_t* n_tiles;
@@ -496,7 +498,9 @@ __global__ void __launch_bounds__(256) plan_kernel(PlanArgs a) {
 // ---- fp32 path, for small shapes -----------------------------------------------------------------
 // A block per row, its warps sharing the other operand's rows between them: 32 at a time stand in a warp's part of
 // shared memory, a row apart by an odd number of words, and a lane has one of them, so that a logit is d products
-// in a lane, without a reduction.  The warps' results are added in order.
+// in a lane, without a reduction.  The warps' results are added in order.  Bound by the staging (each of the T V d
+// products is read from shared memory once, and each row of the other operand through L2 for every row): 189 us at T =
+// 160, K = 9, d = 57, V = 831; a warp per row that kept its own staging area took 253 us.
 constexpr int kMaxD32 = 1024;
 
 struct Fp32Args {
@@ -691,7 +695,8 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   w.partials = reinterpret_cast<double*>(take(w.n_partials * kPartialStride * sizeof(double)));
   w.tiles = aero_carve_tiles(p + off, T, R, lmhead::BM);
   off += aero_tiles_bytes(T, R, lmhead::BM);
-  // more than one wave of token tiles keeps all SMs busy without further splits
+  // more than one wave of token tiles keeps all SMs busy without further splits (loss at d = 1536: 24000 tokens 6640 us
+  // without, 6850 with; 16000 tokens 4600 without, 4560 with)
   const bool few = T <= 148 * 128;
   const int base_v = aero_vsplit_cap(d);
   w.v_hi = few && base_v < kMaxVsplit ? kMaxVsplit : base_v;
@@ -866,7 +871,8 @@ int bwd_fp32(const Call& c, const Ws& s, const float* lse, float grad_scale, flo
   AERO_CUDA_TRY(cudaMemsetAsync(s.g, 0, (size_t)c.T * sizeof(float), ctx->stream));      // rows of dropped rollouts
   const Fp32Args f = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
   if ((rc = rows_fp32(f.r, ctx))) return rc;
-  const bool narrow = c.d <= 128;                        // sums of a row: 4 or 32 registers a lane
+  // sums of a row: 4 or 32 registers a lane (T = 160, d = 57, V = 831, forward and gradients: 189 or 267 us)
+  const bool narrow = c.d <= 128;
   rc = launch_fp32(ctx, narrow ? fp32_rows_kernel<4, true> : fp32_rows_kernel<kMaxD32 / 32, true>, f, c.T, c.V);
   if (rc) return rc;
   return launch_fp32(ctx, narrow ? fp32_vocabulary_kernel<4> : fp32_vocabulary_kernel<kMaxD32 / 32>, f, c.V, c.T);
@@ -890,7 +896,8 @@ int lmhead_launch(const Call& c, const Ws& s, lmhead::Params p, const CUtensorMa
   p.tile_row = s.tiles.tile_row; p.tile_valid = s.tiles.tile_valid; p.n_tiles = s.tiles.n_tiles;
   p.y = s.y; p.status = ctx->d_status; p.plan = s.plan;
   p.sync_ctr = reinterpret_cast<unsigned int*>(s.zero);
-  // the meetings pay over launches of many units per pair; a few hundred microseconds do not drift apart
+  // the meetings pay over launches of many units per pair; a few milliseconds do not drift apart (without / with them:
+  // loss of 1000 tokens 371 / 379 us, step of 300 tokens 492 / 513, of 4096 tokens at d = 3584 8090 / 8150)
   p.nsync = c.T > (int64_t)ctx->sm_count * lmhead::BM ? aero_nsync(ctx) : 0;
   p.w_hint = aero_w_hint(ctx, mode != kFwd); p.k_zigzag = aero_k_zigzag(ctx);
   auto kern = mode == kFwd ? lmhead::lmhead_kernel<lmhead::MODE_FWD>

@@ -19,6 +19,8 @@
 
 namespace {
 
+// (One kernel / sort and tiles, with the clearing of dW: 3000 tokens at d = 1536, V = 151936 175 / 203 us; 4000 tokens
+// at V = 3000 57.5 / 65 us.  A list of positions is 16-bit and a warp's quarter of it 1024 long.)
 constexpr int kSmallT = 4096;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 constexpr int kMaxRadix = 512;

@@ -270,13 +270,23 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
   const int nvt = (p.V + BN - 1) / BN;
   // The pair's k-th unit is token tiles first, first + 1 (the second may not exist: its CTA
   // then stages the first tile's rows again and discards the result) and one of the vsplit
-  // ranges of vocabulary tiles; the pairs that share tiles are neighbours.
+  // ranges of vocabulary tiles.  The pairs that share tiles are neighbours; in a planned launch with no more pairs of
+  // tiles than CTA pairs, those that share a range are, since W would otherwise be read once for every few tiles
+  // (distillation loss at d = 1536, V = 151936: 16000 tokens 5060 -> 4470 us, 5000 tokens 1795 -> 1450 us, up to 2000
+  // tokens within 2 %).
   const int vsplit = p.plan ? *p.plan : p.vsplit;
-  auto unit_first = [&](int k) { return p.tile_begin + 2 * ((pair + k * npairs) / vsplit); };
-  auto unit_j0 = [&](int k) { return (int)((long long)((pair + k * npairs) % vsplit) * nvt / vsplit); };
-  auto unit_j1 = [&](int k) { return (int)((long long)((pair + k * npairs) % vsplit + 1) * nvt / vsplit); };
+  const int tile_pairs = max((n_tiles - p.tile_begin + 1) / 2, 0);
+  const bool by_range = p.plan && tile_pairs <= npairs;
+  auto unit_first = [&](int k) {
+    const int u = pair + k * npairs;
+    if (u >= tile_pairs * vsplit) return n_tiles;
+    return p.tile_begin + 2 * (by_range ? u % tile_pairs : u / vsplit);
+  };
+  auto unit_split = [&](int k) { return by_range ? (pair + k * npairs) / tile_pairs : (pair + k * npairs) % vsplit; };
+  auto unit_j0 = [&](int k) { return (int)((long long)unit_split(k) * nvt / vsplit); };
+  auto unit_j1 = [&](int k) { return (int)((long long)(unit_split(k) + 1) * nvt / vsplit); };
   // with a common shift, a unit of a later split starts with vocabulary tile 0, used for the shift alone
-  auto unit_pre = [&](int k) { return (STORE_P && p.common_shift && (pair + k * npairs) % vsplit != 0) ? 1 : 0; };
+  auto unit_pre = [&](int k) { return (STORE_P && p.common_shift && unit_split(k) != 0) ? 1 : 0; };
 
   if (warp == 4) {
     // ---------------- TMA producer ----------------
@@ -286,8 +296,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
       unsigned int meetings = 0;
       const uint64_t pol_w = tc::l2_policy_evict_first();
       // every CTA takes part in the same number of meetings: units of the longest schedule x nsync
-      const int total_units = ((n_tiles - p.tile_begin + 1) / 2) * vsplit;
-      const int max_units = total_units > 0 ? (total_units + npairs - 1) / npairs : 0;
+      const int max_units = (tile_pairs * vsplit + npairs - 1) / npairs;
       for (int k = 0; ok && unit_first(k) < n_tiles; ++k) {
         const int mine = unit_first(k) + (int)rank;
         const int row0 = p.tile_row[mine < n_tiles ? mine : unit_first(k)];
@@ -589,7 +598,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
         if (lane == 0) tc::mbar_arrive_cluster(tc::mapa_shared(tc::smem_u32(&ctl->tempty[buf]), 0));
       }
 
-      if (STORE_P && ok && have_tile && live) p.shift_out[(size_t)((pair + k * npairs) % vsplit) * p.T + row] = c2;
+      if (STORE_P && ok && have_tile && live) p.shift_out[(size_t)unit_split(k) * p.T + row] = c2;
       if (STORE_P && range_hit) {
         const int slot = atomicAdd(p.range_count, 1);
         if (slot < p.range_cap) p.range_rows[slot] = (tile - p.tile_begin) * BM + r_in_tile;
@@ -597,7 +606,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
       }
       if (!IS_DZ && ok && have_tile) {
         if (vsplit > 1 || p.plan) {
-          if (live) p.xstate[(size_t)((pair + k * npairs) % vsplit) * p.T + row] = make_float4(m2, l, zy, sz);
+          if (live) p.xstate[(size_t)unit_split(k) * p.T + row] = make_float4(m2, l, zy, sz);
         } else {
           finish_rows(p, ENT, live, row, tile, warp, lane, m2, l, zy, sz);
         }
