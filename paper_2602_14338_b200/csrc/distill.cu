@@ -28,7 +28,11 @@
 namespace {
 
 constexpr int kMaxK = 256, kSlots = kMaxK / 32;
-constexpr int kBlocksPerTile = 16;      // blocks of 8 rows that cover a token tile in the row kernels
+constexpr int kUnitsPerTile = 16;       // units of 8 rows that cover a token tile in the row kernels
+// Blocks of the row kernels at most: they walk the units that there are.  Only the device knows these, and the bound
+// that the host has, a tile of its own for every second rollout, may be far above (20000 tokens in 20000 rollouts, all
+// kept, d = 1536: loss 12.0 -> 9.0 ms, step 35.6 -> 27.3 ms).
+constexpr int kRowBlocks = 2368;
 constexpr int kMaxVsplit = 148;         // vocabulary splits the plan may choose
 constexpr int kMaxKsplit = 16;          // ranges of the reduction of dH it may choose
 
@@ -87,14 +91,18 @@ __device__ __forceinline__ int kept_owner(const int64_t* __restrict__ cs, const 
   return keep[i] != 0 && a >= 0 && a <= t && t < b && b <= T ? i : -1;
 }
 
-// The token row of this block's warp; -1: none (past the list, or of a dropped rollout)
-__device__ __forceinline__ long long row_of(const RowsArgs& a, int warp) {
+// Units of 8 rows of this launch, and the token row of a warp in one of them; -1: none (past the tile's rows, or of a
+// dropped rollout)
+__device__ __forceinline__ long long units_of(const RowsArgs& a) {
+  return a.tile_row == nullptr ? (a.T + 7) / 8 : (long long)(min(*a.n_tiles, a.tile_end) - a.tile_begin) * kUnitsPerTile;
+}
+__device__ __forceinline__ long long row_of(const RowsArgs& a, long long unit, int warp) {
   if (a.tile_row == nullptr) {
-    const long long t = (long long)blockIdx.x * 8 + warp;
+    const long long t = unit * 8 + warp;
     return kept_owner(a.cs, a.keep, a.R, a.T, t) >= 0 ? t : -1;
   }
-  const int tile = a.tile_begin + blockIdx.x / kBlocksPerTile, r = (blockIdx.x % kBlocksPerTile) * 8 + warp;
-  if (tile >= min(*a.n_tiles, a.tile_end) || r >= a.tile_valid[tile]) return -1;
+  const int tile = a.tile_begin + (int)(unit / kUnitsPerTile), r = (int)(unit % kUnitsPerTile) * 8 + warp;
+  if (r >= a.tile_valid[tile]) return -1;
   const long long t = (long long)a.tile_row[tile] + r;
   return t < a.T ? t : -1;
 }
@@ -127,12 +135,9 @@ __device__ __forceinline__ float2 join_states(const float4* xs, long long T, lon
 // the gather of K rows of W per token out of L2.
 constexpr int kDots = 4;
 template <typename T>
-__global__ void __launch_bounds__(256) distill_dots_kernel(RowsArgs a) {
+__device__ __forceinline__ void list_dots(const RowsArgs& a, long long t, int k0, int lane) {
   constexpr int VEC = rowvec::Elem<T>::kVec;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long t = row_of(a, warp);
-  const int K = a.ls.K, d = a.d, k0 = blockIdx.y * kDots;
-  if (t < 0) return;
+  const int K = a.ls.K, d = a.d;
   int v[kDots];
   const T* w[kDots];
   int last = -1;
@@ -172,135 +177,146 @@ __global__ void __launch_bounds__(256) distill_dots_kernel(RowsArgs a) {
     if (lane == 0 && v[q] >= 0) a.ls.z[t * K + k0 + q] = acc[q];
   }
 }
+template <typename T>
+__global__ void __launch_bounds__(256) distill_dots_kernel(RowsArgs a) {
+  const long long n = units_of(a);
+  for (long long u = blockIdx.x; u < n; u += gridDim.x) {
+    const long long t = row_of(a, u, threadIdx.x >> 5);
+    if (t >= 0) list_dots<T>(a, t, blockIdx.y * kDots, threadIdx.x & 31);
+  }
+}
 
 __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
   __shared__ double rec[8][kPartialStride];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long t = row_of(a, warp);
   const int K = a.ls.K, d = a.d;
   double part[kPartialStride] = {0.0, 0.0, 0.0, 0.0, 0.0};
-  if (a.Hl && a.tile_begin + (int)(blockIdx.x / kBlocksPerTile) < min(*a.n_tiles, a.tile_end)) {
-    uint4* dst = reinterpret_cast<uint4*>(a.Hl + ((size_t)blockIdx.x * 8 + warp) * d);
-    const uint4* src = t >= 0 ? reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.H) + t * d) : nullptr;
-    for (int k = lane; k < d / 8; k += 32) dst[k] = src ? src[k] : make_uint4(0, 0, 0, 0);
-  }
-  if (t >= 0) {
-    const float wi = a.wrow[t];
-    const int yt = a.y[t];
-    float lse, lp_y = 0.f;
-    if (a.xstate) {
-      const float2 s = join_states(a.xstate, a.T, t, *a.plan, lane);
-      lse = s.x;
-      lp_y = s.y;
-    } else {
-      lse = a.lse[t];
+  const long long n = units_of(a);
+  for (long long u = blockIdx.x; u < n; u += gridDim.x) {
+    const long long t = row_of(a, u, warp);
+    if (a.Hl) {
+      uint4* dst = reinterpret_cast<uint4*>(a.Hl + ((size_t)u * 8 + warp) * d);
+      const uint4* src = t >= 0 ? reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.H) + t * d) : nullptr;
+      for (int k = lane; k < d / 8; k += 32) dst[k] = src ? src[k] : make_uint4(0, 0, 0, 0);
     }
-    // slot s of a lane holds list place 32 s + lane
-    int id[kSlots];
-    float lg[kSlots], z[kSlots];
-    float hi = -INFINITY;
+    if (t >= 0) {
+      const float wi = a.wrow[t];
+      const int yt = a.y[t];
+      float lse, lp_y = 0.f;
+      if (a.xstate) {
+        const float2 s = join_states(a.xstate, a.T, t, *a.plan, lane);
+        lse = s.x;
+        lp_y = s.y;
+      } else {
+        lse = a.lse[t];
+      }
+      // slot s of a lane holds list place 32 s + lane
+      int id[kSlots];
+      float lg[kSlots], z[kSlots];
+      float hi = -INFINITY;
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      id[s] = -1;
-      lg[s] = -INFINITY;
-      z[s] = 0.f;
-      if (s * 32 < K) {
-        const int k = s * 32 + lane;
-        if (k < K) {
-          const int v = a.ls.ids[t * K + k];
-          if (v >= 0 && v < a.V) {
-            id[s] = v;
-            lg[s] = a.ls.logits[t * K + k];
-            hi = fmaxf(hi, lg[s]);
+      for (int s = 0; s < kSlots; ++s) {
+        id[s] = -1;
+        lg[s] = -INFINITY;
+        z[s] = 0.f;
+        if (s * 32 < K) {
+          const int k = s * 32 + lane;
+          if (k < K) {
+            const int v = a.ls.ids[t * K + k];
+            if (v >= 0 && v < a.V) {
+              id[s] = v;
+              lg[s] = a.ls.logits[t * K + k];
+              hi = fmaxf(hi, lg[s]);
+            }
           }
         }
       }
-    }
-    float norm;
-    if (a.ls.tlse) {
-      norm = a.ls.tlse[t];
-    } else {
-      hi = warp_max(hi);
-      float sum = 0.f;
+      float norm;
+      if (a.ls.tlse) {
+        norm = a.ls.tlse[t];
+      } else {
+        hi = warp_max(hi);
+        float sum = 0.f;
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s)
-        if (id[s] >= 0 && lg[s] > -INFINITY) sum += expf(lg[s] - hi);
-      norm = hi + logf(warp_sum(sum));            // (an empty list: -inf, no place below uses it)
-    }
-    // student logits at the listed tokens, from distill_dots_kernel
-    float zy = 0.f;
-    bool any_listed = false;
-#pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      if (s * 32 < K) {
-        if (id[s] >= 0) z[s] = a.ls.z[t * K + s * 32 + lane];
-        const unsigned is_y = __ballot_sync(0xffffffffu, id[s] == yt && id[s] >= 0);
-        if (is_y) zy = __shfl_sync(0xffffffffu, z[s], __ffs(is_y) - 1);
-        any_listed |= is_y != 0;
+        for (int s = 0; s < kSlots; ++s)
+          if (id[s] >= 0 && lg[s] > -INFINITY) sum += expf(lg[s] - hi);
+        norm = hi + logf(warp_sum(sum));            // (an empty list: -inf, no place below uses it)
       }
-    }
-    if (a.xstate) {
-      // y's logit again, now as the dot product: the accumulation of the tensor cores is off by up to 2^-23 of the
-      // partial sums a step, which for a logit that makes up most of the sum would be most of lse's error.  With
-      // L = (1 - p_y) / p_y the correction keeps the accuracy of a log-prob close to 0.
-      const float dlt = any_listed ? zy - (lse + lp_y) : 0.f;
-      lp_y = lp_y > -30.f ? -log1pf(expm1f(-lp_y) * expf(-dlt)) : lp_y + dlt;
-      if (any_listed) lse = zy - lp_y;
-      if (lane == 0) a.lse[t] = lse;
-    } else {
-      lp_y = zy - lse;
-    }
-    float kl = 0.f, Q = 0.f, mass = 0.f, q[kSlots], pr[kSlots];
+      // student logits at the listed tokens, from distill_dots_kernel
+      float zy = 0.f;
+      bool any_listed = false;
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s) {
-      q[s] = 0.f;
-      pr[s] = 0.f;
-      if (id[s] >= 0) {
-        const float lp = id[s] == yt ? lp_y : z[s] - lse;
-        pr[s] = expf(lp);
-        mass += pr[s];
-        if (lg[s] > -INFINITY) {                    // a logit of -inf or NaN carries no weight
-          const float lq = lg[s] - norm;
-          q[s] = expf(lq);
-          if (q[s] != 0.f) kl = fmaf(q[s], lq - lp, kl);
-          Q += q[s];
+      for (int s = 0; s < kSlots; ++s) {
+        if (s * 32 < K) {
+          if (id[s] >= 0) z[s] = a.ls.z[t * K + s * 32 + lane];
+          const unsigned is_y = __ballot_sync(0xffffffffu, id[s] == yt && id[s] >= 0);
+          if (is_y) zy = __shfl_sync(0xffffffffu, z[s], __ffs(is_y) - 1);
+          any_listed |= is_y != 0;
         }
       }
-    }
-    kl = warp_sum(kl);
-    Q = warp_sum(Q);
-    mass = warp_sum(mass);
-    if (a.ls.entry) {
-      // a token listed twice has one entry, with the sum of its q
-      const float c = a.grad_scale * wi;
-      float qsum[kSlots];
+      if (a.xstate) {
+        // y's logit again, now as the dot product: the accumulation of the tensor cores is off by up to 2^-23 of the
+        // partial sums a step, which for a logit that makes up most of the sum would be most of lse's error.  With
+        // L = (1 - p_y) / p_y the correction keeps the accuracy of a log-prob close to 0.
+        const float dlt = any_listed ? zy - (lse + lp_y) : 0.f;
+        lp_y = lp_y > -30.f ? -log1pf(expm1f(-lp_y) * expf(-dlt)) : lp_y + dlt;
+        if (any_listed) lse = zy - lp_y;
+        if (lane == 0) a.lse[t] = lse;
+      } else {
+        lp_y = zy - lse;
+      }
+      float kl = 0.f, Q = 0.f, mass = 0.f, q[kSlots], pr[kSlots];
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s) qsum[s] = 0.f;
-#pragma unroll
-      for (int s2 = 0; s2 < kSlots; ++s2) {
-        if (s2 * 32 < K) {
-          for (int l = 0; l < 32 && s2 * 32 + l < K; ++l) {
-            const int v = __shfl_sync(0xffffffffu, id[s2], l);
-            const float qv = __shfl_sync(0xffffffffu, q[s2], l);
-#pragma unroll
-            for (int s = 0; s < kSlots; ++s)
-              if (id[s] == v) qsum[s] += qv;
+      for (int s = 0; s < kSlots; ++s) {
+        q[s] = 0.f;
+        pr[s] = 0.f;
+        if (id[s] >= 0) {
+          const float lp = id[s] == yt ? lp_y : z[s] - lse;
+          pr[s] = expf(lp);
+          mass += pr[s];
+          if (lg[s] > -INFINITY) {                    // a logit of -inf or NaN carries no weight
+            const float lq = lg[s] - norm;
+            q[s] = expf(lq);
+            if (q[s] != 0.f) kl = fmaf(q[s], lq - lp, kl);
+            Q += q[s];
           }
         }
       }
+      kl = warp_sum(kl);
+      Q = warp_sum(Q);
+      mass = warp_sum(mass);
+      if (a.ls.entry) {
+        // a token listed twice has one entry, with the sum of its q
+        const float c = a.grad_scale * wi;
+        float qsum[kSlots];
 #pragma unroll
-      for (int s = 0; s < kSlots; ++s)
-        if (s * 32 + lane < K) a.ls.entry[t * K + s * 32 + lane] = c * (Q * pr[s] - qsum[s]);
+        for (int s = 0; s < kSlots; ++s) qsum[s] = 0.f;
+#pragma unroll
+        for (int s2 = 0; s2 < kSlots; ++s2) {
+          if (s2 * 32 < K) {
+            for (int l = 0; l < 32 && s2 * 32 + l < K; ++l) {
+              const int v = __shfl_sync(0xffffffffu, id[s2], l);
+              const float qv = __shfl_sync(0xffffffffu, q[s2], l);
+#pragma unroll
+              for (int s = 0; s < kSlots; ++s)
+                if (id[s] == v) qsum[s] += qv;
+            }
+          }
+        }
+#pragma unroll
+        for (int s = 0; s < kSlots; ++s)
+          if (s * 32 + lane < K) a.ls.entry[t * K + s * 32 + lane] = c * (Q * pr[s] - qsum[s]);
+      }
+      if (lane == 0) {
+        if (a.g) a.g[t] = -wi * Q;
+        if (a.ls.kl) a.ls.kl[t] = kl;
+      }
+      part[0] -= (double)wi * (double)kl;             // (the finalising kernel returns minus this sum)
+      part[1] += Q > 0.f ? 0.0 : 1.0;
+      part[2] += kl;
+      part[3] += mass;
+      part[4] += 1.0;
     }
-    if (lane == 0) {
-      if (a.g) a.g[t] = -wi * Q;
-      if (a.ls.kl) a.ls.kl[t] = kl;
-    }
-    part[0] = -(double)wi * (double)kl;             // (the finalising kernel returns minus this sum)
-    part[1] = Q > 0.f ? 0.0 : 1.0;
-    part[2] = kl;
-    part[3] = mass;
-    part[4] = 1.0;
   }
   if (a.ls.partials) {
     if (lane == 0)
@@ -309,7 +325,7 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
     if (threadIdx.x < kPartialStride) {
       double s = 0.0;
       for (int w = 0; w < 8; ++w) s += rec[w][threadIdx.x];
-      a.ls.partials[((size_t)a.tile_begin * kBlocksPerTile + blockIdx.x) * kPartialStride + threadIdx.x] = s;
+      a.ls.partials[(size_t)blockIdx.x * kPartialStride + threadIdx.x] += s;      // (one chunk after another)
     }
   }
 }
@@ -327,44 +343,50 @@ struct BlockArgs {
 __global__ void __launch_bounds__(256) distill_scale_kernel(BlockArgs b) {
   __shared__ float2 f[128];
   const RowsArgs& a = b.a;
-  const int tile = a.tile_begin + blockIdx.y, j = blockIdx.x;
-  if (tile >= min(*a.n_tiles, a.tile_end)) return;
-  if (threadIdx.x < 128) {
-    const int r = threadIdx.x;
-    const long long t = (long long)a.tile_row[tile] + r;
-    float2 v = make_float2(0.f, 0.f);
-    if (r < a.tile_valid[tile] && t < a.T) {
-      // the split whose range of vocabulary tiles holds tile j
-      const int s = (int)(((long long)(j + 1) * *a.plan - 1) / b.nvt);
-      const float h = exp2f(0.5f * (b.shift[(size_t)s * a.T + t] - a.lse[t] * lmhead::kLog2e));
-      v = make_float2(h, -a.g[t] * a.grad_scale * h);
+  const int j = blockIdx.x, tile_end = min(*a.n_tiles, a.tile_end);
+  const int n = min(4, b.nblk - 4 * j) * 128 * 8;              // 16-byte vectors of a piece
+  for (int tile = a.tile_begin + blockIdx.y; tile < tile_end; tile += gridDim.y) {
+    __syncthreads();                                           // the previous tile's factors have been used
+    if (threadIdx.x < 128) {
+      const int r = threadIdx.x;
+      const long long t = (long long)a.tile_row[tile] + r;
+      float2 v = make_float2(0.f, 0.f);
+      if (r < a.tile_valid[tile] && t < a.T) {
+        // the split whose range of vocabulary tiles holds tile j
+        const int s = (int)(((long long)(j + 1) * *a.plan - 1) / b.nvt);
+        const float h = exp2f(0.5f * (b.shift[(size_t)s * a.T + t] - a.lse[t] * lmhead::kLog2e));
+        v = make_float2(h, -a.g[t] * a.grad_scale * h);
+      }
+      f[r] = v;
     }
-    f[r] = v;
-  }
-  __syncthreads();
-  const int n = min(4, b.nblk - 4 * j) * 128 * 8;              // 16-byte vectors of this piece
-  uint4* p = reinterpret_cast<uint4*>(b.dz + ((size_t)blockIdx.y * b.nblk + 4 * j) * 128 * 64);
+    __syncthreads();
+    uint4* p = reinterpret_cast<uint4*>(b.dz + ((size_t)(tile - a.tile_begin) * b.nblk + 4 * j) * 128 * 64);
 #pragma unroll 4
-  for (int i = threadIdx.x; i < n; i += 256) {
-    const float2 c = f[(i >> 3) & 127];
-    float x[8];
-    rowvec::unpack(p[i], x);
+    for (int i = threadIdx.x; i < n; i += 256) {
+      const float2 c = f[(i >> 3) & 127];
+      float x[8];
+      rowvec::unpack(p[i], x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = c.y != 0.f ? x[e] * c.x * c.y : 0.f;      // (a row without weight: zeros)
-    p[i] = rowvec::pack(x);
+      for (int e = 0; e < 8; ++e) x[e] = c.y != 0.f ? x[e] * c.x * c.y : 0.f;      // (a row without weight: zeros)
+      p[i] = rowvec::pack(x);
+    }
   }
 }
 
 // The entries of dz at the listed tokens, over the softmax part.
 __global__ void __launch_bounds__(256) distill_scatter_kernel(BlockArgs b) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long t = row_of(b.a, warp);
-  if (t < 0) return;
-  const int lt = blockIdx.x / kBlocksPerTile, r = (blockIdx.x % kBlocksPerTile) * 8 + warp, K = b.a.ls.K;
-  for (int k = lane; k < K; k += 32) {
-    const int v = b.a.ls.ids[t * K + k];
-    if (v < 0 || v >= b.a.V) continue;
-    b.dz[(((size_t)lt * b.nblk + v / 64) * 128 + r) * 64 + v % 64] = __float2bfloat16_rn(b.a.ls.entry[t * K + k]);
+  const int K = b.a.ls.K;
+  const long long n = units_of(b.a);
+  for (long long u = blockIdx.x; u < n; u += gridDim.x) {
+    const long long t = row_of(b.a, u, warp);
+    if (t < 0) continue;
+    const int lt = (int)(u / kUnitsPerTile), r = (int)(u % kUnitsPerTile) * 8 + warp;
+    for (int k = lane; k < K; k += 32) {
+      const int v = b.a.ls.ids[t * K + k];
+      if (v < 0 || v >= b.a.V) continue;
+      b.dz[(((size_t)lt * b.nblk + v / 64) * 128 + r) * 64 + v % 64] = __float2bfloat16_rn(b.a.ls.entry[t * K + k]);
+    }
   }
 }
 
@@ -374,18 +396,20 @@ __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const 
   const int ks = *ksplit;
   if (ks <= 1) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long t = row_of(a, warp);
-  if (t < 0) return;
-  const long long rows = (long long)(min(*a.n_tiles, a.tile_end) - a.tile_begin) * 128, row = (long long)blockIdx.x * 8 + warp;
+  const int n = (int)units_of(a);
+  const long long rows = (long long)n * 8;
   const int c = blockIdx.y * 256 + lane * 8;
-  if (c < a.d) {
+  if (c >= a.d) return;
+  for (int u = blockIdx.x; u < n; u += gridDim.x) {
+    const long long t = row_of(a, u, warp);
+    if (t < 0) continue;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int k = 0; k < ks; ++k) {
-      const float4* p = reinterpret_cast<const float4*>(part + (k * rows + row) * a.d + c);
-      const float4 u = p[0], v = p[1];
-      s[0] += u.x; s[1] += u.y; s[2] += u.z; s[3] += u.w;
-      s[4] += v.x; s[5] += v.y; s[6] += v.z; s[7] += v.w;
+      const float4* p = reinterpret_cast<const float4*>(part + (k * rows + u * 8 + warp) * a.d + c);
+      const float4 x = p[0], y = p[1];
+      s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+      s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
     }
     rowvec::store<__nv_bfloat16, 8>(dH + t * a.d + c, s);
   }
@@ -671,8 +695,10 @@ struct Ws {
 
 inline long long ldz_of(int32_t V) { return ((long long)V + 63) / 64 * 64; }
 inline size_t chunk_tile_bytes(int32_t d, int32_t V) { return (size_t)128 * ((size_t)ldz_of(V) * 2 + (size_t)d * 2); }
-// token tiles a call may have: one per 128 rows, and each run of kept rollouts may end in one of its own
-inline int64_t max_tiles_of(int64_t T, int32_t R) { return T / 128 + R + 2; }
+// token tiles a call may have: one per 128 rows, and each run of kept rollouts (a rollout that is not kept, or empty, lies
+// between any two) may end in one of its own
+inline int64_t max_tiles_of(int64_t T, int32_t R) { return T / 128 + ((int64_t)R + 1) / 2 + 1; }
+inline unsigned row_blocks_of(int64_t units) { return (unsigned)(units < kRowBlocks ? (units > 0 ? units : 1) : kRowBlocks); }
 
 Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode mode) {
   Ws w = {};
@@ -691,9 +717,10 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   w.z = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   if (mode != kFwd) w.entry = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   const size_t mt = (size_t)max_tiles_of(T, R);
-  w.n_partials = mt * kBlocksPerTile;
+  w.n_partials = kRowBlocks;
   w.partials = reinterpret_cast<double*>(take(w.n_partials * kPartialStride * sizeof(double)));
   w.tiles = aero_carve_tiles(p + off, T, R, lmhead::BM);
+  w.tiles.max_tiles = (int32_t)mt;
   off += aero_tiles_bytes(T, R, lmhead::BM);
   // more than one wave of token tiles keeps all SMs busy without further splits (loss at d = 1536: 24000 tokens 6640 us
   // without, 6850 with; 16000 tokens 4600 without, 4560 with)
@@ -737,7 +764,7 @@ struct Room {
   Room(size_t bytes, int64_t T, int32_t d, int32_t V, int32_t R, bool bf16, int sm_count) {
     const long long mt = max_tiles_of(T, R);
     tpc = (long long)(bytes / chunk_tile_bytes(d, V));
-    if (tpc > 32768) tpc = 32768;                                           // grid.y of the scaling kernel
+    if (tpc > 32768) tpc = 32768;                                           // unit numbers stay within 32 bits
     if (tpc >= mt) { tpc = mt; return; }
     if (bf16) {
       sums = true;
@@ -822,7 +849,7 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
 // ---- fp32 path -------------------------------------------------------------------------------------------
 // list logits and rows: all T at once, 8 per block
 int rows_fp32(const RowsArgs& a, aero_ctx* ctx) {
-  const unsigned blocks = (unsigned)((a.T + 7) / 8);
+  const unsigned blocks = row_blocks_of((a.T + 7) / 8);
   distill_dots_kernel<float><<<dim3(blocks, (unsigned)((a.ls.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
   distill_rows_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
   ctx->launches += 2;
@@ -856,7 +883,7 @@ int fwd_fp32(const Call& c, const Ws& s, float* lse, float* kl, float* loss, flo
     if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T, c.V))) return rc;
     if ((rc = rows_fp32(a, ctx))) return rc;
   }
-  return aero_loss_finalize(ctx, s.partials, (int)((c.T + 7) / 8), kPartialStride, loss, metrics, 0);
+  return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
 }
 
 int bwd_fp32(const Call& c, const Ws& s, const float* lse, float grad_scale, float* dH, float* dW, int accumulate) {
@@ -952,7 +979,7 @@ int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float
     a.xstate = s.xstate;
     a.tile_row = s.tiles.tile_row; a.tile_valid = s.tiles.tile_valid; a.n_tiles = s.tiles.n_tiles;
     a.tile_begin = 0; a.tile_end = s.tiles.max_tiles;
-    const unsigned blocks = (unsigned)s.tiles.max_tiles * kBlocksPerTile;
+    const unsigned blocks = row_blocks_of((int64_t)s.tiles.max_tiles * kUnitsPerTile);
     distill_dots_kernel<__nv_bfloat16><<<dim3(blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
     distill_rows_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
     ctx->launches += 2;
@@ -1001,7 +1028,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
 
   for (long long begin = 0; begin < s.tiles.max_tiles; begin += tpc) {
     const long long end = begin + tpc < s.tiles.max_tiles ? begin + tpc : s.tiles.max_tiles;
-    const unsigned row_blocks = (unsigned)(end - begin) * kBlocksPerTile;
+    const unsigned row_blocks = row_blocks_of((end - begin) * kUnitsPerTile);
     void* clear = begin > 0 || gr.accumulate ? nullptr : (gr.dW16 ? static_cast<void*>(gr.dW16) : static_cast<void*>(gr.dW));
     if (begin > 0) AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, 1024, ctx->stream));
     if ((rc = plan_launch(c, s, begin, tpc, pairs, clear, (size_t)V * d * (gr.dW16 ? 2 : 4)))) return rc;
@@ -1020,7 +1047,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBoth))) return rc;
       a.xstate = s.xstate;
       distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);
-      distill_scale_kernel<<<dim3((unsigned)b.nvt, (unsigned)(end - begin)), 256, 0, ctx->stream>>>(b);
+      distill_scale_kernel<<<dim3((unsigned)b.nvt, (unsigned)(end - begin < 64 ? end - begin : 64)), 256, 0, ctx->stream>>>(b);
       RangeArgs f = {};
       f.rows = s.range_rows; f.count = s.range_count; f.cap = kRangeCap; f.dz = gr.block; f.nblk = (int)nblk;
       f.tile_row = s.tiles.tile_row; f.tile_begin = (int)begin; f.T = c.T; f.d = d; f.V = V; f.y = s.y;
