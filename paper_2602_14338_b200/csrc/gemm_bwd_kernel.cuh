@@ -132,6 +132,26 @@ struct Units {
   __device__ int k1(int u) const { return (int)((long long)(range(u) + 1) * nkb / ks); }
 };
 
+// The units of one worker (CTA or CTA pair).  Normally every so many of all units.  dW of a chunk of so few token tiles
+// that all its slabs fit the ring at once is walked column tile by column tile instead: a worker keeps one column tile
+// and goes down the vocabulary, each slab of H always meets the same stage, and after the first turn only dz is loaded
+// (16 KB a slab instead of 48 or 32).  What is left is the writing of dW (bf16, d = 1536, V = 151936, 256 rows: 126 ->
+// 115 us, half of the memory's rate; eight epilogue warps instead of four changed nothing).
+struct Walk {
+  int first, step, end, ring, nt;                        // nt >= 0: the column tile kept, units are row tiles
+  bool keep;
+  __device__ Walk(const Units& un, int n_units, int worker, int workers, int stages, bool dw) {
+    keep = dw && un.nkb > 0 && un.nkb <= stages && un.n_nt <= workers;
+    nt = keep ? worker % un.n_nt : -1;
+    first = keep ? worker / un.n_nt : worker;
+    step = keep ? (workers - nt + un.n_nt - 1) / un.n_nt : workers;
+    end = keep ? un.n_m : n_units;
+    ring = keep ? stages / un.nkb * un.nkb : stages;     // stages in use
+  }
+  __device__ int m(const Units& un, int u) const { return keep ? u : un.m(u); }
+  __device__ int n(const Units& un, int u) const { return keep ? nt : un.n(u); }
+};
+
 // 32 columns of one row of a range's fp32 sums of dH.
 __device__ __forceinline__ void store_part(const Params& p, int range, long long row, int chunk_tiles, int col0,
                                            const uint32_t (&r)[32]) {
@@ -171,21 +191,24 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
   const int ks = KIND == KIND_DH && p.ksplit ? *p.ksplit : 1;
   const int n_units = nkb > 0 ? n_mt * n_nt * ks : 0;
   const Units un = {n_mt, n_nt, nkb, ks};
+  const Walk walk(un, n_units, blockIdx.x, gridDim.x, STAGES, KIND == KIND_DW);
+  const int nsync = walk.keep ? 0 : p.nsync;
 
   if (warp == 4) {
     // ---------------- TMA producer ----------------
     if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true, first_turn = true;
       int row_cur = 0, row_next = 0;
       unsigned int meetings = 0;
       const int max_units = (n_units + (int)gridDim.x - 1) / (int)gridDim.x;     // of the longest schedule
-      for (int u = blockIdx.x; ok && u < n_units; u += gridDim.x) {
-        const int mt = un.m(u), nt = un.n(u);
+      for (int u = walk.first; ok && u < walk.end; u += walk.step) {
+        const int mt = walk.m(un, u), nt = walk.n(un, u);
         int next_meet = 0;
         const int k0 = un.k0(u), k1 = un.k1(u);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          if (p.nsync > 0 && next_meet < p.nsync && kb - k0 >= (int)((long long)next_meet * (k1 - k0) / p.nsync)) {
+        for (int kb = k0; kb < k1; ++kb) {
+          if (nsync > 0 && next_meet < nsync && kb - k0 >= (int)((long long)next_meet * (k1 - k0) / nsync)) {
             ++next_meet;
             ++meetings;
             atomicAdd(p.sync_ctr, 1u);
@@ -196,12 +219,11 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
               __nanosleep(100);
             }
           }
-          const int s = it % STAGES;
-          const uint32_t ph = (it / STAGES) & 1u;
           if (!tc::mbar_wait(&ctl->empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
           uint8_t* a_s = smem + (size_t)s * STAGE_BYTES;
           uint8_t* b_s = a_s + A_BYTES;
-          tc::mbar_arrive_expect_tx(&ctl->full[s], STAGE_BYTES);
+          const bool with_b = first_turn || !walk.keep;
+          tc::mbar_arrive_expect_tx(&ctl->full[s], with_b ? STAGE_BYTES : A_BYTES);
           if (KIND == KIND_DH) {
             // A: dz rows of the tile (K-major, K = vocabulary); B: W rows kb*64.. as four
             // 64-column blocks (MN-major, blocked view)
@@ -218,34 +240,34 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
             }
             const int hrow = p.h_local ? kb * BK : row_cur + (kb % (BM / BK)) * BK;
             tc::tma_load_4d(a_s, &tmA, 0, (kb % (BM / BK)) * BK, mt * (BM / 64), kb / (BM / BK), &ctl->full[s]);
-            tc::tma_load_3d(b_s, &tmB, 0, hrow, nt * (BN / 64), &ctl->full[s]);
+            if (with_b) tc::tma_load_3d(b_s, &tmB, 0, hrow, nt * (BN / 64), &ctl->full[s]);
           }
+          if (++s == walk.ring) { s = 0; ph ^= 1u; first_turn = false; }
         }
         // a unit with fewer slabs than meeting points still counts them all
-        if (p.nsync > 0 && next_meet < p.nsync) {
-          atomicAdd(p.sync_ctr, (unsigned)(p.nsync - next_meet));
-          meetings += (unsigned)(p.nsync - next_meet);
+        if (nsync > 0 && next_meet < nsync) {
+          atomicAdd(p.sync_ctr, (unsigned)(nsync - next_meet));
+          meetings += (unsigned)(nsync - next_meet);
         }
       }
       // out of units: stand in for the meetings the longest schedule still has
-      if (p.nsync > 0 && meetings < (unsigned)(max_units * p.nsync))
-        atomicAdd(p.sync_ctr, (unsigned)(max_units * p.nsync) - meetings);
+      if (nsync > 0 && meetings < (unsigned)(max_units * nsync))
+        atomicAdd(p.sync_ctr, (unsigned)(max_units * nsync) - meetings);
     }
   } else if (warp == 5) {
     // ---------------- MMA issuer ----------------
     if (lane == 0) {
       constexpr uint32_t idesc = tc::make_idesc_bf16(BM, BN, KIND == KIND_DW ? 1 : 0, 1);
-      uint32_t it = 0, at = 0;
+      int s = 0;
+      uint32_t ph = 0, at = 0;
       bool ok = true;
-      for (int u = blockIdx.x; ok && u < n_units; u += gridDim.x, ++at) {
+      for (int u = walk.first; ok && u < walk.end; u += walk.step, ++at) {
         const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
         if (!tc::mbar_wait(&ctl->tempty[buf], aph ^ 1u, abort_flag)) { ok = false; break; }
         tc::tc_fence_after();
         const uint32_t tmem_d = tmem_base + buf * BN;
         const int k0 = un.k0(u), k1 = un.k1(u);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          const int s = it % STAGES;
-          const uint32_t ph = (it / STAGES) & 1u;
+        for (int kb = k0; kb < k1; ++kb) {
           if (!tc::mbar_wait(&ctl->full[s], ph, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
           const uint32_t a_addr = tc::smem_u32(smem + (size_t)s * STAGE_BYTES);
@@ -260,6 +282,7 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
           for (int kk = 0; kk < BK / UMMA_K; ++kk)
             tc::umma_bf16(tmem_d, adesc + a_step * kk, bdesc + b_step * kk, idesc, kb > k0 || kk > 0 ? 1u : 0u);
           tc::umma_commit(&ctl->empty[s]);
+          if (++s == walk.ring) { s = 0; ph ^= 1u; }
         }
         if (ok) tc::umma_commit(&ctl->tfull[buf]);
       }
@@ -270,8 +293,8 @@ gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUt
     bool ok = true;
     const int r_in_tile = warp * 32 + lane;
     uint8_t* stg = out_staging(ctl + 1) + warp * 2 * OUT_BUF_BYTES;
-    for (int u = blockIdx.x; ok && u < n_units; u += gridDim.x, ++at) {
-      const int mt = un.m(u), nt = un.n(u);
+    for (int u = walk.first; ok && u < walk.end; u += walk.step, ++at) {
+      const int mt = walk.m(un, u), nt = walk.n(un, u);
       const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], aph, abort_flag))) { ok = false; break; }
       tc::tc_fence_after();
@@ -402,24 +425,27 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
   const int ks = KIND == KIND_DH && p.ksplit ? *p.ksplit : 1;
   const int n_units = nkb > 0 ? n_mp * n_nt * ks : 0;
   const Units un = {n_mp, n_nt, nkb, ks};
+  const Walk walk(un, n_units, pair, npairs, PSTAGES, KIND == KIND_DW);
+  const int nsync = walk.keep ? 0 : p.nsync;
 
   if (warp == 4) {
     // ---------------- TMA producer (one per CTA) ----------------
     if (lane == 0) {
-      uint32_t it = 0;
-      bool ok = true;
+      int s = 0;
+      uint32_t ph = 0;
+      bool ok = true, first_turn = true;
       int row_cur = 0, row_next = 0;
       unsigned int meetings = 0;
       const int max_units = (n_units + npairs - 1) / npairs;     // of the longest schedule
-      for (int u = pair; ok && u < n_units; u += npairs) {
-        const int mp = un.m(u), nt = un.n(u);
+      for (int u = walk.first; ok && u < walk.end; u += walk.step) {
+        const int mp = walk.m(un, u), nt = walk.n(un, u);
         // the pair's second row tile may not exist: its CTA then stages the first one again (dH) or rows
         // past V, which the copy fills with zeros (dW), and discards the result
         const int mt = (KIND == KIND_DH && 2 * mp + (int)rank >= n_mt) ? 2 * mp : 2 * mp + (int)rank;
         int next_meet = 0;
         const int k0 = un.k0(u), k1 = un.k1(u);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          if (p.nsync > 0 && next_meet < p.nsync && kb - k0 >= (int)((long long)next_meet * (k1 - k0) / p.nsync)) {
+        for (int kb = k0; kb < k1; ++kb) {
+          if (nsync > 0 && next_meet < nsync && kb - k0 >= (int)((long long)next_meet * (k1 - k0) / nsync)) {
             ++next_meet;
             ++meetings;
             atomicAdd(p.sync_ctr, 1u);
@@ -430,13 +456,12 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
               __nanosleep(100);
             }
           }
-          const int s = it % PSTAGES;
-          const uint32_t ph = (it / PSTAGES) & 1u;
           if (!tc::mbar_wait(&ctl->empty[s], ph ^ 1u, abort_flag)) { ok = false; break; }
           uint8_t* a_s = smem + (size_t)s * PSTAGE_BYTES;
           uint8_t* b_s = a_s + A_BYTES;
           const uint32_t full0 = tc::mapa_shared(tc::smem_u32(&ctl->full[s]), 0);
-          if (rank == 0) tc::mbar_arrive_expect_tx(&ctl->full[s], 2 * PSTAGE_BYTES);
+          const bool with_b = first_turn || !walk.keep;
+          if (rank == 0) tc::mbar_arrive_expect_tx(&ctl->full[s], 2 * (with_b ? PSTAGE_BYTES : A_BYTES));
           if (KIND == KIND_DH) {
             tc::tma_load_4d_pair(a_s, &tmA, 0, 0, kb, mt, full0);
             tc::tma_load_3d_pair(b_s, &tmB, 0, kb * BK, nt * (BN / 64) + (int)rank * (PBNH / 64), full0);
@@ -448,32 +473,32 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
             }
             const int hrow = p.h_local ? kb * BK : row_cur + (kb % (BM / BK)) * BK;
             tc::tma_load_4d_pair(a_s, &tmA, 0, (kb % (BM / BK)) * BK, mt * (BM / 64), kb / (BM / BK), full0);
-            tc::tma_load_3d_pair(b_s, &tmB, 0, hrow, nt * (BN / 64) + (int)rank * (PBNH / 64), full0);
+            if (with_b) tc::tma_load_3d_pair(b_s, &tmB, 0, hrow, nt * (BN / 64) + (int)rank * (PBNH / 64), full0);
           }
+          if (++s == walk.ring) { s = 0; ph ^= 1u; first_turn = false; }
         }
-        if (p.nsync > 0 && next_meet < p.nsync) {
-          atomicAdd(p.sync_ctr, (unsigned)(p.nsync - next_meet));
-          meetings += (unsigned)(p.nsync - next_meet);
+        if (nsync > 0 && next_meet < nsync) {
+          atomicAdd(p.sync_ctr, (unsigned)(nsync - next_meet));
+          meetings += (unsigned)(nsync - next_meet);
         }
       }
-      if (p.nsync > 0 && meetings < (unsigned)(max_units * p.nsync))
-        atomicAdd(p.sync_ctr, (unsigned)(max_units * p.nsync) - meetings);
+      if (nsync > 0 && meetings < (unsigned)(max_units * nsync))
+        atomicAdd(p.sync_ctr, (unsigned)(max_units * nsync) - meetings);
     }
   } else if (warp == 5) {
     // ---------------- MMA issuer (rank 0, for the pair) ----------------
     if (lane == 0 && rank == 0) {
       constexpr uint32_t idesc = tc::make_idesc_bf16(2 * BM, BN, KIND == KIND_DW ? 1 : 0, 1);
-      uint32_t it = 0, at = 0;
+      int s = 0;
+      uint32_t ph = 0, at = 0;
       bool ok = true;
-      for (int u = pair; ok && u < n_units; u += npairs, ++at) {
+      for (int u = walk.first; ok && u < walk.end; u += walk.step, ++at) {
         const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
         if (!tc::mbar_wait(&ctl->tempty[buf], aph ^ 1u, abort_flag)) { ok = false; break; }
         tc::tc_fence_after();
         const uint32_t tmem_d = tmem_base + buf * BN;
         const int k0 = un.k0(u), k1 = un.k1(u);
-        for (int kb = k0; kb < k1; ++kb, ++it) {
-          const int s = it % PSTAGES;
-          const uint32_t ph = (it / PSTAGES) & 1u;
+        for (int kb = k0; kb < k1; ++kb) {
           if (!tc::mbar_wait(&ctl->full[s], ph, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
           const uint32_t a_addr = tc::smem_u32(smem + (size_t)s * PSTAGE_BYTES);
@@ -486,6 +511,7 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
           for (int kk = 0; kk < BK / UMMA_K; ++kk)
             tc::umma_bf16_pair(tmem_d, adesc + a_step * kk, bdesc + b_step * kk, idesc, kb > k0 || kk > 0 ? 1u : 0u);
           tc::umma_commit_pair(&ctl->empty[s], 3);     // frees the stage in both CTAs when these MMAs retire
+          if (++s == walk.ring) { s = 0; ph ^= 1u; }
         }
         if (ok) tc::umma_commit_pair(&ctl->tfull[buf], 3);
       }
@@ -496,8 +522,8 @@ gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant_
     bool ok = true;
     const int r_in_tile = warp * 32 + lane;
     uint8_t* stg = out_staging(ctl + 1) + warp * 2 * OUT_BUF_BYTES;
-    for (int u = pair; ok && u < n_units; u += npairs, ++at) {
-      const int mp = un.m(u), nt = un.n(u);
+    for (int u = walk.first; ok && u < walk.end; u += walk.step, ++at) {
+      const int mp = walk.m(un, u), nt = walk.n(un, u);
       const int mt = 2 * mp + (int)rank;
       const uint32_t buf = at & 1u, aph = (at >> 1) & 1u;
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], aph, abort_flag))) { ok = false; break; }

@@ -123,7 +123,10 @@ def check_grads(case, dH, dW, r, dw_half=0.0, base=0.0):
 BF16 = [dict(T=1, d=64, V=1, K=1), dict(T=1, d=64, V=100, K=3), dict(T=7, d=64, V=65, K=1), dict(T=130, d=128, V=300, K=8),
         dict(T=300, d=192, V=1000, K=33, teacher_lse=True), dict(T=700, d=256, V=2049, K=64), dict(T=257, d=1536, V=700, K=256),
         dict(T=64, d=3584, V=1500, K=5, teacher_lse=True), dict(T=1000, d=64, V=4096, K=20, R=60),
-        dict(T=700, d=64, V=300, K=3, R=700), dict(T=20000, d=64, V=100, K=2, R=5000)]
+        dict(T=700, d=64, V=300, K=3, R=700), dict(T=20000, d=64, V=100, K=2, R=5000),
+        # chunks of one to three token tiles, several units per worker of the dW product, on CTAs and on pairs of them
+        dict(T=100, d=64, V=60000, K=4, R=1), dict(T=250, d=320, V=24000, K=4, R=1), dict(T=100, d=2112, V=8000, K=4, R=1),
+        dict(T=250, d=2112, V=8000, K=4, R=1), dict(T=380, d=2112, V=8000, K=4, R=1)]
 FP32 = [dict(T=1, d=1, V=1, K=1), dict(T=3, d=57, V=100, K=3), dict(T=60, d=64, V=300, K=8, teacher_lse=True),
         dict(T=200, d=96, V=700, K=40), dict(T=41, d=129, V=77, K=70), dict(T=33, d=1024, V=100, K=6)]
 
