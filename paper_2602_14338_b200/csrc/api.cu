@@ -7,7 +7,7 @@
 
 extern "C" {
 
-int aero_version(void) { return 102; }
+int aero_version(void) { return 103; }
 
 const char* aero_error_string(int code) {
   switch (code) {
