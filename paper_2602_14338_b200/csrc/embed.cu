@@ -86,19 +86,16 @@ struct Clear {
 
 __device__ __forceinline__ bool clear_rows(const Clear& z) {
   if (blockIdx.x < z.first) return false;
-  const int lane = threadIdx.x & 31, per_block = blockDim.x >> 5;
+  const int lane = threadIdx.x & 31;
   const bool vec = z.d % 4 == 0 && (reinterpret_cast<uintptr_t>(z.dW) & 15u) == 0;
-  constexpr int G = 8;                                   // rows a warp looks at together
-  const long long step = (long long)(gridDim.x - z.first) * per_block * G;
-  for (long long v = z.v0 + ((long long)(blockIdx.x - z.first) * per_block + (threadIdx.x >> 5)) * G; v < z.v1; v += step) {
-    unsigned absent = __ballot_sync(0xffffffffu, lane < G && v + lane < z.v1 && !z.occurs[v + lane]);
-    for (; absent != 0; absent &= absent - 1) {
-      float* row = z.dW + (v + __ffs(absent) - 1) * z.d;
-      if (vec) {
-        for (int k = lane; k < z.d / 4; k += 32) reinterpret_cast<float4*>(row)[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      } else {
-        for (int k = lane; k < z.d; k += 32) row[k] = 0.f;
-      }
+  const long long step = (long long)(gridDim.x - z.first) * (blockDim.x >> 5);
+  for (long long v = z.v0 + (long long)(blockIdx.x - z.first) * (blockDim.x >> 5) + (threadIdx.x >> 5); v < z.v1; v += step) {
+    if (z.occurs[v]) continue;
+    float* row = z.dW + v * z.d;
+    if (vec) {
+      for (int k = lane; k < z.d / 4; k += 32) reinterpret_cast<float4*>(row)[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+      for (int k = lane; k < z.d; k += 32) row[k] = 0.f;
     }
   }
   return true;
@@ -208,52 +205,54 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(int n, int V, 
   for (int i = threadIdx.x; i < radix; i += kSortThreads) counts[(size_t)i * blocks + blockIdx.x] = h[i];
 }
 
-// exclusive prefix of n counts (a multiple of 4) in place, one block
-__global__ void __launch_bounds__(1024) sort_prefix_kernel(uint4* __restrict__ counts, int n, Clear z) {
-  __shared__ uint32_t warp_sum[2][32];
-  if (clear_rows(z)) return;
+// exclusive sum over the block's threads, and the sum of all; `sh` may be used again after a barrier
+__device__ __forceinline__ uint32_t block_before(uint32_t v, uint32_t* sh, uint32_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t incl = v;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += u;
+  }
+  if (lane == 31) sh[warp] = incl;
+  __syncthreads();
+  uint32_t before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWarps; ++w) {
+    if (w < warp) before += sh[w];
+    total += sh[w];
+  }
+  return before + incl - v;
+}
+
+// Exclusive prefix of each digit's counts over the blocks, in place, and the digit's total: a block per digit.  (The
+// prefix over the totals is left to the blocks of the scatter; 3 us for 204780 keys.)
+__global__ void __launch_bounds__(kSortThreads) sort_prefix_kernel(uint32_t* __restrict__ counts, int blocks,
+                                                                   uint32_t* __restrict__ totals, Clear z) {
+  __shared__ uint32_t sh[2][kSortWarps];
+  if (clear_rows(z)) return;
+  uint32_t* row = counts + (size_t)blockIdx.x * blocks;
   uint32_t carry = 0;
-  int turn = 0;
-  uint4 next = (int)threadIdx.x < n / 4 ? counts[threadIdx.x] : make_uint4(0, 0, 0, 0);
-  for (int base = 0; base < n / 4; base += 1024, turn ^= 1) {
+  for (int base = 0, turn = 0; base < blocks; base += kSortThreads, turn ^= 1) {
     const int i = base + threadIdx.x;
-    const uint4 v = next;
-    next = i + 1024 < n / 4 ? counts[i + 1024] : make_uint4(0, 0, 0, 0);
-    const uint32_t sum = v.x + v.y + v.z + v.w;
-    uint32_t incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t u = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += u;
-    }
-    if (lane == 31) warp_sum[turn][warp] = incl;
-    __syncthreads();
-    // every warp scans the 32 warps' sums for itself
-    uint32_t w = warp_sum[turn][lane];
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t u = __shfl_up_sync(0xffffffffu, w, o);
-      if (lane >= o) w += u;
-    }
-    const uint32_t before = warp > 0 ? __shfl_sync(0xffffffffu, w, warp - 1) : 0u, total = __shfl_sync(0xffffffffu, w, 31);
-    uint4 r;
-    r.x = carry + before + incl - sum;
-    r.y = r.x + v.x;
-    r.z = r.y + v.y;
-    r.w = r.z + v.z;
-    if (i < n / 4) counts[i] = r;
+    const uint32_t v = i < blocks ? row[i] : 0u;
+    uint32_t total;
+    const uint32_t before = block_before(v, sh[turn], total);
+    if (i < blocks) row[i] = carry + before;
     carry += total;
   }
+  if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int n, int V, const int32_t* __restrict__ y,
                                                                     const uint32_t* __restrict__ keys,
                                                                     const uint32_t* __restrict__ pos, int shift, int radix,
                                                                     int blocks, const uint32_t* __restrict__ starts,
+                                                                    const uint32_t* __restrict__ totals,
                                                                     uint32_t* __restrict__ keys_out,
                                                                     uint32_t* __restrict__ pos_out, Clear z) {
-  __shared__ uint32_t h[kSortWarps][kMaxRadix];
+  __shared__ uint32_t h[kSortWarps][kMaxRadix], first[kMaxRadix], sh[kSortWarps];
   if (clear_rows(z)) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   for (int i = threadIdx.x; i < kSortWarps * radix; i += kSortThreads) h[i / radix][i % radix] = 0;
@@ -276,9 +275,16 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(int n, int V
     __syncwarp();
     rank[s] = before + __popc(same & ((1u << lane) - 1u));
   }
+  // where each digit's keys start: thread i has digits 2 i and 2 i + 1
+  static_assert(kMaxRadix == 2 * kSortThreads, "two digits per thread");
+  const int d0 = 2 * threadIdx.x;
+  const uint32_t n0 = d0 < radix ? totals[d0] : 0u, n1 = d0 + 1 < radix ? totals[d0 + 1] : 0u;
+  uint32_t all;
+  first[d0] = block_before(n0 + n1, sh, all);
+  first[d0 + 1] = first[d0] + n0;
   __syncthreads();
   for (int g = threadIdx.x; g < radix; g += kSortThreads) {
-    uint32_t run = starts[(size_t)g * blocks + blockIdx.x];
+    uint32_t run = first[g] + starts[(size_t)g * blocks + blockIdx.x];
     for (int w = 0; w < kSortWarps; ++w) {
       const uint32_t c = h[w][g];
       h[w][g] = run;
@@ -461,6 +467,7 @@ struct Ws {
   uint32_t* keys[2];
   uint32_t* pos[2];
   uint32_t* counts;
+  uint32_t* totals;
   float* part;
   Runs runs;
   size_t bytes;
@@ -479,6 +486,7 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V) {
     }
     const size_t blocks = ((size_t)T + kSortTile - 1) / kSortTile, tiles = ((size_t)T + kTile - 1) / kTile;
     w.counts = reinterpret_cast<uint32_t*>(take(blocks * kMaxRadix * sizeof(uint32_t)));
+    w.totals = reinterpret_cast<uint32_t*>(take(kMaxRadix * sizeof(uint32_t)));
     w.part = reinterpret_cast<float*>(take(tiles * 2 * (size_t)d * sizeof(float)));
     w.runs.list = reinterpret_cast<int2*>(take(tiles * sizeof(int2)));
     w.runs.count = reinterpret_cast<int*>(take(2 * sizeof(int)));
@@ -488,16 +496,17 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V) {
   return w;
 }
 
-// The sort's launches clear an equal share of the rows of dW each (all but the first, which finds the tokens).
+// The sort's launches clear an equal share of the rows of dW each (all but the first, which finds the tokens): a warp per
+// row and 32 blocks per SM, so that the stores of all rows are under way at once (204780 x 1536 / 30000 x 3584: 16 blocks
+// 357 / 414 us, 32 354 / 405, 128 371 / 412; four blocks whose warps took eight rows each 375 / 469).
 int sort_positions(aero_ctx* ctx, const Ws& w, int n, int d, int V, const int32_t* y, float* clear, const uint32_t** keys,
                    const uint32_t** pos) {
   int bits = 1;
   while (bits < 32 && ((uint32_t)V >> bits) != 0) ++bits;          // the keys are 0 .. V
   const int passes = (bits + 8) / 9;
-  int per = (bits + passes - 1) / passes;
-  if (per < 2) per = 2;                                            // (counts in fours)
+  const int per = (bits + passes - 1) / passes;
   const unsigned blocks = (unsigned)((n + kSortTile - 1) / kSortTile);
-  const unsigned helpers = clear ? 4u * (unsigned)ctx->sm_count : 0u;
+  const unsigned helpers = clear ? 32u * (unsigned)ctx->sm_count : 0u;
   const int shares = 3 * passes - 1;
   int share = 0;
   auto next_share = [&](unsigned first) {
@@ -514,10 +523,10 @@ int sort_positions(aero_ctx* ctx, const Ws& w, int n, int d, int V, const int32_
     sort_count_kernel<<<blocks + (find ? 0u : helpers), kSortThreads, 0, ctx->stream>>>(
         n, V, y, kin, shift, radix, (int)blocks, w.counts, find && clear ? w.occurs : nullptr,
         find || !clear ? none : next_share(blocks), ctx->d_status);
-    sort_prefix_kernel<<<1 + helpers / 4, 1024, 0, ctx->stream>>>(reinterpret_cast<uint4*>(w.counts), radix * (int)blocks,
-                                                                  clear ? next_share(1) : none);
+    sort_prefix_kernel<<<radix + helpers, kSortThreads, 0, ctx->stream>>>(w.counts, (int)blocks, w.totals,
+                                                                          clear ? next_share(radix) : none);
     sort_scatter_kernel<<<blocks + helpers, kSortThreads, 0, ctx->stream>>>(n, V, y, kin, pin, shift, radix, (int)blocks,
-                                                                            w.counts, w.keys[p & 1], w.pos[p & 1],
+                                                                            w.counts, w.totals, w.keys[p & 1], w.pos[p & 1],
                                                                             clear ? next_share(blocks) : none);
     ctx->launches += 3;
     kin = w.keys[p & 1];
