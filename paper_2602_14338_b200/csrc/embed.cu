@@ -19,9 +19,10 @@
 
 namespace {
 
-// (One kernel / sort and tiles, with the clearing of dW: 3000 tokens at d = 1536, V = 151936 175 / 203 us; 4000 tokens
-// at V = 3000 57.5 / 65 us.  A list of positions is 16-bit and a warp's quarter of it 1024 long.)
-constexpr int kSmallT = 4096;
+// One kernel / sort and tiles, with the clearing of dW: d = 1536, V = 151936 2500 tokens 168 / 189 us, 3500 186 / 190, 4090
+// 196 / 189; d = 3584, V = 152064 2500 tokens 352 / 360 us, 4090 398 / 362; d = 1536, V = 3000 2500 tokens 38 / 65 us, 4090
+// 59 / 66.  (Positions are listed in 16 bits.)
+constexpr int kSmallT = 2816;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
 constexpr int kMaxRadix = 512;
 

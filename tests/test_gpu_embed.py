@@ -65,7 +65,9 @@ def test_lookup(ctx, dtype, T, V, d, shift):
 CASES = [(0, 9, 8, "text"), (1, 1, 1, "same"), (1, 1000, 1536, "text"), (5, 3, 33, "two"), (777, 500, 1536, "text"),
          (2048, 40, 264, "text"), (2049, 40, 264, "text"), (2100, 1, 24, "same"), (4096, 5000, 100, "text"),
          (4097, 3, 72, "two"), (9000, 150000, 40, "text"), (20000, 700, 136, "text"), (20000, 1000, 72, "same"),
-         (2500, 33, 64, "none"), (70001, 511, 16, "text"), (6000, 512, 3, "text"), (33000, 262143, 8, "text")]
+         (2500, 33, 64, "none"), (70001, 511, 16, "text"), (6000, 512, 3, "text"), (33000, 262143, 8, "text"),
+         (2816, 5000, 100, "text"), (2817, 5000, 100, "text"), (3500, 1, 8, "same"), (3500, 2, 8, "two"), (5000, 33, 64, "none"),
+         (600000, 1000, 4, "text")]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
