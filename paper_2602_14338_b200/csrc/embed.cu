@@ -19,8 +19,8 @@
 
 namespace {
 
-// One kernel / sort and tiles, with the clearing of dW: d = 1536, V = 151936 2500 tokens 168 / 189 us, 3500 186 / 190, 4090
-// 196 / 189; d = 3584, V = 152064 2500 tokens 352 / 360 us, 4090 398 / 362; d = 1536, V = 3000 2500 tokens 38 / 65 us, 4090
+// One kernel / sort and tiles, with the clearing of dW: d = 1536, V = 151936 2500 tokens 164 / 189 us, 3500 186 / 190, 4090
+// 196 / 189; d = 3584, V = 152064 2500 tokens 353 / 360 us, 4090 398 / 362; d = 1536, V = 3000 2500 tokens 38 / 65 us, 4090
 // 59 / 66.  (Positions are listed in 16 bits.)
 constexpr int kSmallT = 2816;
 constexpr int kSortTile = 2048, kSortThreads = 256, kSortWarps = kSortThreads / 32;
@@ -102,17 +102,24 @@ __device__ __forceinline__ bool clear_rows(const Clear& z) {
   return true;
 }
 
-// Block (t, y): the first occurrence of a token adds the rows of all its occurrences, slabs of 32 * VEC columns y,
+template <int VEC>
+__host__ __device__ constexpr int small_nj() { return VEC == 1 ? 4 : 1; }
+
+// Block (t, y): the first occurrence of a token adds the rows of all its occurrences, slabs of NJ * 32 * VEC columns y,
 // y + gridDim.y, ...  Each warp looks through a quarter of the ids and adds the rows it finds, in order; the four
-// sums are added in order.  A block whose token occurs earlier leaves.
+// sums are added in order.  A block whose token occurs earlier leaves.  A frequent token is one chain of loads: single
+// elements (VEC = 1) are taken four columns of a lane at a time, so that as many rows need no more turns and no more
+// blocks look through the ids (2500 fp32 rows, d = 2001, V = 5000: 157 -> 102 us with four columns; whole vectors with
+// eight rows in flight instead of four: 2500 bf16 rows, d = 1536, V = 151936 168 -> 164 us).
 template <typename T, int VEC>
 __global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int V, const int32_t* __restrict__ y,
                                                               const T* __restrict__ dX, float scale, float* __restrict__ dW,
                                                               int accumulate, uint32_t* status) {
   using Raw = typename rowvec::Raw<T, VEC>::type;
+  constexpr int NJ = small_nj<VEC>(), S = 32 * VEC;      // a slab: NJ pieces of S columns
   __shared__ uint16_t list[4][kSmallT / 4];
   __shared__ int found[4];
-  __shared__ float sums[3][32 * VEC];
+  __shared__ float sums[3][NJ * S];
   const int t = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int id = y[t];
   if (id < 0 || id >= V) {
@@ -134,40 +141,59 @@ __global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int
   const int all = found[0] + found[1] + found[2] + found[3];
   bool alone = false;
   for (int w = 0; w < 4; ++w) alone |= found[w] == all;          // (the same answer in all four warps)
-  for (int c = (blockIdx.y * 32 + lane) * VEC; c - lane * VEC < d; c += gridDim.y * 32 * VEC) {
-    float acc[VEC];
+  for (int s0 = blockIdx.y * NJ * S; s0 < d; s0 += gridDim.y * NJ * S) {
+    const int c = s0 + lane * VEC;                       // and c + S, ... c + (NJ - 1) S
+    float acc[NJ][VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
-    constexpr int U = 4;
-    for (int k = 0; k < n && c < d; k += U) {
-      Raw raw[U];
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) acc[j][e] = 0.f;
+    constexpr int U = VEC == 1 ? 4 : 8;                  // rows in flight
+    for (int k = 0; k < n; k += U) {
+      Raw raw[U][NJ];
 #pragma unroll
       for (int q = 0; q < U; ++q)
-        if (k + q < n) raw[q] = *reinterpret_cast<const Raw*>(dX + (long long)list[warp][k + q] * d + c);
 #pragma unroll
-      for (int q = 0; q < U; ++q) {
-        if (k + q < n) {
-          float f[VEC];
-          rowvec::open<T, VEC>(raw[q], f);
+        for (int j = 0; j < NJ; ++j)
+          if (k + q < n && c + j * S < d) raw[q][j] = *reinterpret_cast<const Raw*>(dX + (long long)list[warp][k + q] * d + c + j * S);
 #pragma unroll
-          for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+      for (int q = 0; q < U; ++q)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          if (k + q < n && c + j * S < d) {
+            float f[VEC];
+            rowvec::open<T, VEC>(raw[q][j], f);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[j][e] += f[e];
+          }
         }
-      }
     }
+    float* dst = dW + (long long)id * d + c;
     if (alone) {                                         // all occurrences in one warp's quarter (often only one): no join
-      if (n > 0 && c < d) put<VEC>(dW + (long long)id * d + c, acc, scale, accumulate != 0);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+        if (n > 0 && c + j * S < d) put<VEC>(dst + j * S, acc[j], scale, accumulate != 0);
       continue;
     }
     if (warp < 3) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sums[warp][e * 32 + lane] = acc[e];
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sums[warp][(j * VEC + e) * 32 + lane] = acc[j][e];
     }
     __syncthreads();
-    if (warp == 3 && c < d) {
-      float s[VEC];
+    if (warp == 3) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s[e] = (sums[0][e * 32 + lane] + sums[1][e * 32 + lane]) + (sums[2][e * 32 + lane] + acc[e]);
-      put<VEC>(dW + (long long)id * d + c, s, scale, accumulate != 0);
+      for (int j = 0; j < NJ; ++j) {
+        if (c + j * S >= d) continue;
+        float s[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const int i = (j * VEC + e) * 32 + lane;
+          s[e] = (sums[0][i] + sums[1][i]) + (sums[2][i] + acc[j][e]);
+        }
+        put<VEC>(dst + j * S, s, scale, accumulate != 0);
+      }
     }
     __syncthreads();
   }
@@ -547,7 +573,7 @@ int bwd_launch(aero_ctx* ctx, int64_t T_, int32_t d, int32_t V, const int32_t* y
   if (T_ <= kSmallT) {
     // (the rows of few tokens are written twice at most: clearing all of dW beforehand costs no more)
     if (!accumulate) AERO_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)V * d * sizeof(float), ctx->stream));
-    const int slabs = (d + 32 * VEC - 1) / (32 * VEC);
+    const int slabs = (d + small_nj<VEC>() * 32 * VEC - 1) / (small_nj<VEC>() * 32 * VEC);
     embed_bwd_small_kernel<T, VEC><<<dim3((unsigned)T_, (unsigned)((slabs + 2) / 3)), 128, 0, ctx->stream>>>(
         n, d, V, y, dX, scale, dW, accumulate, ctx->d_status);
     ctx->launches += 1;
