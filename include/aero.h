@@ -506,7 +506,7 @@ int aero_allocate_sim(aero_ctx* ctx, const aero_cfg* cfg, const aero_alloc_cfg* 
  * paper: they are the ends of the policy model that stage (b) is called from, and the lm_head
  * product a frozen policy is scored with.)  They take plain [T,d] rows -- no group structure --
  * of the type cfg->dtype names (distillation also the rollouts of stage (b)); only that field of cfg is
- * read.
+ * read.  All run on the context's stream, and inputs made on another one are the caller's to order.
  *
  * Final RMS norm, per row t:
  *   s = x + residual   (residual NULL: s = x)
@@ -550,16 +550,17 @@ int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
  * A list place with id AERO_NO_TOKEN is empty (its logit is not read), any other id outside [0,V) raises
  * AERO_ST_BAD_TARGET and counts as empty, a logit of -infinity or NaN has q = 0; a row whose list holds no
  * weight contributes nothing.  A token listed twice counts with the sum of its q.  Rows of dropped rollouts
- * and rows that no rollout owns get lse = kl = 0 and dH = 0, whatever they hold.  1 <= K <= 256; bf16: d % 64 == 0; fp32 (plain path for
- * small shapes): d <= 1024.
+ * and rows that no rollout owns get lse = kl = 0 and dH = 0, whatever they hold.  1 <= K <= 256; bf16: d % 64 == 0;
+ * fp32 (plain path for small shapes): d <= 1024.
  * Inputs   ids [T,K] i32, logits [T,K] f32, teacher_lse [T] f32 or NULL.
  * Outputs  lse, kl [T] f32; loss [1] f32 (overwritten; fixed order of the sums); metrics [4] f32 or NULL: fraction
  *          of kept tokens whose list holds no weight, mean kl, mean sum_k p_t,ids[t,k], kept tokens; dH [T,d]
  *          (cfg->dtype); dW [V,d] of type dw_dtype: AERO_FP32 (overwritten, or added to when
  *          accumulate_dW != 0) or, for bf16 rows, AERO_BF16 (overwritten, rounded once).
  * Precision as in stage (b): dz is rounded to bf16 before the two products (fp32 accumulation), its listed
- * entries from fp32 log-probs; the rows of H enter dW as they are.  lse and kl take the first listed token's logit
- * as an fp32 dot product.  aero_distill_bwd takes lse from the forward and recomputes the logits
+ * entries once, from fp32 log-probs; its softmax part once by aero_distill_bwd and twice by aero_distill_fwd_bwd, which
+ * scales the stored bf16 exponentials; the rows of H enter dW as they are.  lse and kl take the first listed token's
+ * logit as an fp32 dot product.  aero_distill_bwd takes lse from the forward and recomputes the logits
  * (8 d V FLOP per token over the two calls), aero_distill_fwd_bwd does not (6 d V; a row with a logit too far
  * above its first ones is redone as in aero_grpo_loss_fwd_bwd, AERO_ST_RANGE beyond 1024 per chunk).
  * workspace: at least the matching *_workspace_bytes, 256-byte aligned; chunk_tokens as in
