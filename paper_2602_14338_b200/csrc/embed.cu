@@ -102,31 +102,35 @@ __device__ __forceinline__ bool clear_rows(const Clear& z) {
   return true;
 }
 
+// pieces of 32 vectors per slab, and warps of a block, for whole vectors and for single elements
 template <int VEC>
 __host__ __device__ constexpr int small_nj() { return VEC == 1 ? 4 : 1; }
+template <int VEC>
+__host__ __device__ constexpr int small_warps() { return VEC == 1 ? 8 : 4; }
 
 // Block (t, y): the first occurrence of a token adds the rows of all its occurrences, slabs of NJ * 32 * VEC columns y,
-// y + gridDim.y, ...  Each warp looks through a quarter of the ids and adds the rows it finds, in order; the four
-// sums are added in order.  A block whose token occurs earlier leaves.  A frequent token is one chain of loads: single
+// y + gridDim.y, ...  Each warp looks through an equal stretch of the ids and adds the rows it finds, in order; the
+// warps' sums are added in order.  A block whose token occurs earlier leaves.  A frequent token is one chain of loads: single
 // elements (VEC = 1) are taken four columns of a lane at a time, so that as many rows need no more turns and no more
 // blocks look through the ids (2500 fp32 rows, d = 2001, V = 5000: 157 -> 102 us with four columns; whole vectors with
-// eight rows in flight instead of four: 2500 bf16 rows, d = 1536, V = 151936 168 -> 164 us).
+// eight rows in flight instead of four: 2500 bf16 rows, d = 1536, V = 151936 168 -> 164 us).  Four warps or eight: whole
+// vectors at d = 3584, V = 152064 352 / 384 us, single elements (1953 bf16 rows, d = 726, V = 1511) 46 / 38 us.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int V, const int32_t* __restrict__ y,
+__global__ void __launch_bounds__(small_warps<VEC>() * 32) embed_bwd_small_kernel(int T_, int d, int V, const int32_t* __restrict__ y,
                                                               const T* __restrict__ dX, float scale, float* __restrict__ dW,
                                                               int accumulate, uint32_t* status) {
   using Raw = typename rowvec::Raw<T, VEC>::type;
-  constexpr int NJ = small_nj<VEC>(), S = 32 * VEC;      // a slab: NJ pieces of S columns
-  __shared__ uint16_t list[4][kSmallT / 4];
-  __shared__ int found[4];
-  __shared__ float sums[3][NJ * S];
+  constexpr int NW = small_warps<VEC>(), NJ = small_nj<VEC>(), S = 32 * VEC;      // a slab: NJ pieces of S columns
+  __shared__ uint16_t list[NW][kSmallT / NW];
+  __shared__ int found[NW];
+  __shared__ float sums[NW - 1][NJ * S];
   const int t = blockIdx.x, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int id = y[t];
   if (id < 0 || id >= V) {
     if (id != AERO_NO_TOKEN && blockIdx.y == 0 && threadIdx.x == 0) aero_raise(status, AERO_ST_BAD_TARGET);
     return;
   }
-  const int p0 = (int)((long long)T_ * warp / 4), p1 = (int)((long long)T_ * (warp + 1) / 4);
+  const int p0 = T_ * warp / NW, p1 = T_ * (warp + 1) / NW;
   int n = 0, first = 0x7fffffff;
 #pragma unroll 4
   for (int base = p0; base < p1; base += 32) {
@@ -138,9 +142,10 @@ __global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int
   }
   if (lane == 0) found[warp] = n;
   if (__syncthreads_or(first < t)) return;             // an earlier block has this token
-  const int all = found[0] + found[1] + found[2] + found[3];
+  int all = 0;
   bool alone = false;
-  for (int w = 0; w < 4; ++w) alone |= found[w] == all;          // (the same answer in all four warps)
+  for (int w = 0; w < NW; ++w) all += found[w];
+  for (int w = 0; w < NW; ++w) alone |= found[w] == all;          // (the same answer in all warps)
   for (int s0 = blockIdx.y * NJ * S; s0 < d; s0 += gridDim.y * NJ * S) {
     const int c = s0 + lane * VEC;                       // and c + S, ... c + (NJ - 1) S
     float acc[NJ][VEC];
@@ -169,20 +174,20 @@ __global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int
         }
     }
     float* dst = dW + (long long)id * d + c;
-    if (alone) {                                         // all occurrences in one warp's quarter (often only one): no join
+    if (alone) {                                         // all occurrences in one warp's stretch (often only one): no join
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
         if (n > 0 && c + j * S < d) put<VEC>(dst + j * S, acc[j], scale, accumulate != 0);
       continue;
     }
-    if (warp < 3) {
+    if (warp < NW - 1) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) sums[warp][(j * VEC + e) * 32 + lane] = acc[j][e];
     }
     __syncthreads();
-    if (warp == 3) {
+    if (warp == NW - 1) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         if (c + j * S >= d) continue;
@@ -190,7 +195,10 @@ __global__ void __launch_bounds__(128) embed_bwd_small_kernel(int T_, int d, int
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           const int i = (j * VEC + e) * 32 + lane;
-          s[e] = (sums[0][i] + sums[1][i]) + (sums[2][i] + acc[j][e]);
+          s[e] = sums[0][i];
+#pragma unroll
+          for (int w = 1; w < NW - 1; ++w) s[e] += sums[w][i];
+          s[e] += acc[j][e];
         }
         put<VEC>(dst + j * S, s, scale, accumulate != 0);
       }
@@ -574,7 +582,7 @@ int bwd_launch(aero_ctx* ctx, int64_t T_, int32_t d, int32_t V, const int32_t* y
     // (the rows of few tokens are written twice at most: clearing all of dW beforehand costs no more)
     if (!accumulate) AERO_CUDA_TRY(cudaMemsetAsync(dW, 0, (size_t)V * d * sizeof(float), ctx->stream));
     const int slabs = (d + small_nj<VEC>() * 32 * VEC - 1) / (small_nj<VEC>() * 32 * VEC);
-    embed_bwd_small_kernel<T, VEC><<<dim3((unsigned)T_, (unsigned)((slabs + 2) / 3)), 128, 0, ctx->stream>>>(
+    embed_bwd_small_kernel<T, VEC><<<dim3((unsigned)T_, (unsigned)((slabs + 2) / 3)), small_warps<VEC>() * 32, 0, ctx->stream>>>(
         n, d, V, y, dX, scale, dW, accumulate, ctx->d_status);
     ctx->launches += 1;
     AERO_CUDA_TRY(cudaGetLastError());
