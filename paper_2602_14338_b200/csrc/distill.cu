@@ -718,7 +718,8 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   w.z = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   if (mode != kFwd) w.entry = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   const size_t mt = (size_t)max_tiles_of(T, R);
-  w.n_partials = kRowBlocks;
+  const long long tile_units = (long long)mt * kUnitsPerTile, row_units = ((long long)T + 7) / 8;      // of the two paths
+  w.n_partials = row_blocks_of(tile_units > row_units ? tile_units : row_units);
   w.partials = reinterpret_cast<double*>(take(w.n_partials * kPartialStride * sizeof(double)));
   w.tiles = aero_carve_tiles(p + off, T, R, lmhead::BM);
   w.tiles.max_tiles = (int32_t)mt;
