@@ -506,7 +506,8 @@ int aero_allocate_sim(aero_ctx* ctx, const aero_cfg* cfg, const aero_alloc_cfg* 
  * paper: they are the ends of the policy model that stage (b) is called from, and the lm_head
  * product a frozen policy is scored with.)  They take plain [T,d] rows -- no group structure --
  * of the type cfg->dtype names (distillation also the rollouts of stage (b)); only that field of cfg is
- * read.  All run on the context's stream, and inputs made on another one are the caller's to order.
+ * read.  All run on the context's stream, and inputs made on another one are the caller's to order.  Outputs do not
+ * overlap inputs, except where the norm below says that they may.
  *
  * Final RMS norm, per row t:
  *   s = x + residual   (residual NULL: s = x)

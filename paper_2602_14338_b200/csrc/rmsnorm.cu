@@ -333,7 +333,8 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(), bwd_blocks<VEC, NV>())
   }
 }
 
-// dgamma (+)= the blocks' shares: 16 columns per block, 64 rows of shares at a time
+// dgamma (+)= the blocks' shares: 16 columns per block, 64 rows of shares at a time (592 shares of 1536: 6.4 us; 32 columns
+// and 32 rows took 8.4)
 __global__ void __launch_bounds__(1024) dgamma_kernel(const float* __restrict__ part, int n, int d, float* dgamma,
                                                       int accumulate) {
   __shared__ float sh[64][17];
