@@ -10,17 +10,20 @@ import torch
 own = False
 
 SMALL, LARGE = (1536, 151936), (3584, 152064)
-_CTX = None
+_CTX = {}
 
 
 def _context():
-    """The handle a program keeps: one library context on the current stream."""
-    global _CTX
-    if _CTX is None:
+    """The handle a program keeps for the current device, on the current stream."""
+    device, stream = torch.cuda.current_device(), torch.cuda.current_stream()
+    if device not in _CTX:
         from paper_2602_14338_b200 import binding
 
-        _CTX = binding.Context(torch.cuda.current_device())
-    return _CTX
+        _CTX[device] = binding.Context(device, stream=stream)
+    ctx = _CTX[device]
+    if ctx.stream != stream:
+        ctx.set_stream(stream)
+    return ctx
 
 
 def _cfg(dtype):
