@@ -674,9 +674,10 @@ __global__ void __launch_bounds__(256) fp32_vocabulary_kernel(Fp32Args f) {
 enum Mode { kFwd, kBwd, kBoth };
 
 struct Ws {
-  int* zero;                 // 1 KB that starts at zero: pacing counters, plan, count of the range list
+  int* zero;                 // starts at zero: 1 KB of pacing counters, plan, count of the range list, then its rows' bits
   int* plan;
   int* range_count;
+  unsigned int* range_seen;
   int* range_rows;
   int32_t* y;
   float* wrow;
@@ -699,6 +700,8 @@ inline size_t chunk_tile_bytes(int32_t d, int32_t V) { return (size_t)128 * ((si
 // token tiles a call may have: one per 128 rows, and each run of kept rollouts (a rollout that is not kept, or empty, lies
 // between any two) may end in one of its own
 inline int64_t max_tiles_of(int64_t T, int32_t R) { return T / 128 + ((int64_t)R + 1) / 2 + 1; }
+// of Ws::zero, with the bits of so many token tiles' rows
+inline size_t zero_bytes(size_t tiles) { return 1024 + tiles * lmhead::BM / 8; }
 inline unsigned row_blocks_of(int64_t units) { return (unsigned)(units < kRowBlocks ? (units > 0 ? units : 1) : kRowBlocks); }
 
 Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode mode) {
@@ -708,16 +711,17 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   char* p = static_cast<char*>(base);
   size_t off = 0;
   auto take = [&](size_t bytes) { char* r = p + off; off += aero_align_up(bytes, 256); return r; };
-  w.zero = reinterpret_cast<int*>(take(1024));
+  const size_t mt = (size_t)max_tiles_of(T, R);
+  w.zero = reinterpret_cast<int*>(take(zero_bytes(mode == kBoth ? mt : 0)));
   w.plan = w.zero + 128;
   w.range_count = w.zero + 192;
+  w.range_seen = reinterpret_cast<unsigned int*>(w.zero + 256);
   w.range_rows = reinterpret_cast<int*>(take(kRangeCap * sizeof(int)));
   w.y = reinterpret_cast<int32_t*>(take(Tn * 4));
   w.wrow = reinterpret_cast<float*>(take(Tn * 4));
   w.g = reinterpret_cast<float*>(take(Tn * 4));
   w.z = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
   if (mode != kFwd) w.entry = reinterpret_cast<float*>(take(Tn * (size_t)K * 4));
-  const size_t mt = (size_t)max_tiles_of(T, R);
   const long long tile_units = (long long)mt * kUnitsPerTile, row_units = ((long long)T + 7) / 8;      // of the two paths
   w.n_partials = row_blocks_of(tile_units > row_units ? tile_units : row_units);
   w.partials = reinterpret_cast<double*>(take(w.n_partials * kPartialStride * sizeof(double)));
@@ -835,9 +839,9 @@ RowsArgs rows_of(const Call& c, const Ws& s, float* lse, float* kl, bool partial
   return a;
 }
 
-int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool partials) {
+int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool partials, long long chunk_tiles = 0) {
   aero_ctx* ctx = c.ctx;
-  AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, 1024, ctx->stream));
+  AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, zero_bytes((size_t)chunk_tiles), ctx->stream));
   if (partials) AERO_CUDA_TRY(cudaMemsetAsync(s.partials, 0, s.n_partials * kPartialStride * sizeof(double), ctx->stream));
   if (c.T == 0) return AERO_OK;
   const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.cs, c.w, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
@@ -994,7 +998,8 @@ int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float
 int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const Grads& gr) {
   aero_ctx* ctx = c.ctx;
   const int d = c.d, V = c.V;
-  int rc = start(c, s, mode == kBoth ? lse : nullptr, kl, gr.dH, mode == kBoth);
+  const long long tpc = gr.tpc, listed_tiles = mode == kBoth ? tpc : 0;
+  int rc = start(c, s, mode == kBoth ? lse : nullptr, kl, gr.dH, mode == kBoth, listed_tiles);
   if (rc) return rc;
   if (c.T == 0 || c.R == 0) {
     if (gr.dW16) AERO_CUDA_TRY(cudaMemsetAsync(gr.dW16, 0, (size_t)V * d * 2, ctx->stream));
@@ -1002,7 +1007,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     return AERO_OK;
   }
   if ((rc = aero_build_tiles(ctx, c.T, c.R, c.cs, c.keep, lmhead::BM, s.tiles))) return rc;
-  const long long ldz = ldz_of(V), tpc = gr.tpc;
+  const long long ldz = ldz_of(V);
   const uint64_t nblk = (uint64_t)(ldz / 64);
   __nv_bfloat16* Hl = gr.block + (size_t)tpc * lmhead::BM * (size_t)ldz;
   const bool pairs = aero_gemm_pairs(ctx, d);
@@ -1032,7 +1037,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     const long long end = begin + tpc < s.tiles.max_tiles ? begin + tpc : s.tiles.max_tiles;
     const unsigned row_blocks = row_blocks_of((end - begin) * kUnitsPerTile);
     void* clear = begin > 0 || gr.accumulate ? nullptr : (gr.dW16 ? static_cast<void*>(gr.dW16) : static_cast<void*>(gr.dW));
-    if (begin > 0) AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, 1024, ctx->stream));
+    if (begin > 0) AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, zero_bytes((size_t)listed_tiles), ctx->stream));
     if ((rc = plan_launch(c, s, begin, tpc, pairs, clear, (size_t)V * d * (gr.dW16 ? 2 : 4)))) return rc;
     RowsArgs a = rows_of(c, s, lse, kl, mode == kBoth, gr.grad_scale);
     a.tile_row = s.tiles.tile_row; a.tile_valid = s.tiles.tile_valid; a.n_tiles = s.tiles.n_tiles;
@@ -1045,7 +1050,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     BlockArgs b = {a, gr.block, (int)nblk, (V + lmhead::BN - 1) / lmhead::BN, s.shift};
     if (mode == kBoth) {
       p.xstate = s.xstate; p.shift_out = s.shift;
-      p.range_rows = s.range_rows; p.range_count = s.range_count; p.range_cap = kRangeCap;
+      p.range_rows = s.range_rows; p.range_count = s.range_count; p.range_seen = s.range_seen; p.range_cap = kRangeCap;
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBoth))) return rc;
       a.xstate = s.xstate;
       distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);

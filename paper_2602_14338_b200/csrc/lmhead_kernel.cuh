@@ -124,6 +124,7 @@ struct Params {
   // inside the chunk) so that the step can redo them; AERO_ST_RANGE is raised only if the list overflows
   int* range_rows;
   int* range_count;
+  unsigned int* range_seen;     // bit per chunk-local row: already listed (cleared with the count)
   int range_cap;
   double* partials;             // [tile][4 epilogue warps][kPartialStride]
   // dz modes
@@ -599,10 +600,23 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
       }
 
       if (STORE_P && ok && have_tile && live) p.shift_out[(size_t)unit_split(k) * p.T + row] = c2;
-      if (STORE_P && range_hit) {
-        const int slot = atomicAdd(p.range_count, 1);
-        if (slot < p.range_cap) p.range_rows[slot] = (tile - p.tile_begin) * BM + r_in_tile;
-        else aero_raise(p.status, AERO_ST_RANGE);
+      if (STORE_P) {
+        // each row once, however many splits it is out of range in: a word per 32 rows says which are listed
+        const unsigned hits = __ballot_sync(0xffffffffu, range_hit);
+        if (hits != 0) {
+          unsigned fresh = 0;
+          int slot = 0;
+          if (lane == 0) {
+            fresh = hits & ~atomicOr(p.range_seen + (tile - p.tile_begin) * (BM / 32) + warp, hits);
+            slot = atomicAdd(p.range_count, __popc(fresh));
+          }
+          fresh = __shfl_sync(0xffffffffu, fresh, 0);
+          slot = __shfl_sync(0xffffffffu, slot, 0) + __popc(fresh & ((1u << lane) - 1u));
+          if (fresh >> lane & 1u) {
+            if (slot < p.range_cap) p.range_rows[slot] = (tile - p.tile_begin) * BM + r_in_tile;
+            else aero_raise(p.status, AERO_ST_RANGE);
+          }
+        }
       }
       if (!IS_DZ && ok && have_tile) {
         if (vsplit > 1 || p.plan) {

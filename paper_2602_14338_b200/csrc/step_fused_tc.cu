@@ -240,6 +240,7 @@ struct FusedWs {
   float* row_scale;
   float* zmax;
   int* range_count;
+  unsigned int* range_seen;      // bit per row of a chunk, behind the count: cleared together
   int* range_rows;
   __nv_bfloat16* dz;
   size_t head_bytes;
@@ -261,6 +262,7 @@ FusedWs carve(void* ws, int64_t T, int32_t d, int32_t R) {
   f.n_partials = (size_t)f.tiles.max_tiles * 4;
   f.sync_ctr = reinterpret_cast<unsigned int*>(p + off);       off += 256;
   f.range_count = reinterpret_cast<int*>(p + off);             off += 256;
+  f.range_seen = reinterpret_cast<unsigned int*>(p + off);     off += aero_align_up((size_t)f.tiles.max_tiles * lmhead::BM / 8, 256);
   f.range_rows = reinterpret_cast<int*>(p + off);              off += aero_align_up(kRangeCap * sizeof(int), 256);
   f.xstate = reinterpret_cast<float4*>(p + off);               off += aero_align_up(vs * Tn * sizeof(float4), 256);
   f.shift = reinterpret_cast<float*>(p + off);                 off += aero_align_up(vs * Tn * sizeof(float), 256);
@@ -393,8 +395,9 @@ int aero_fwd_bwd_tc(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, in
       p.logp = logp; p.lse_out = lse; p.g_out = g; p.partials = f.partials;
       p.shift_out = f.shift; p.dz = f.dz; p.ldz = ldz;
       p.common_shift = rowscale && vs > 1 ? 1 : 0;
-      p.range_rows = f.range_rows; p.range_count = f.range_count; p.range_cap = kRangeCap;
-      AERO_CUDA_TRY(cudaMemsetAsync(f.sync_ctr, 0, 512, ctx->stream));      // pacing counter and the range list's count
+      p.range_rows = f.range_rows; p.range_count = f.range_count; p.range_seen = f.range_seen; p.range_cap = kRangeCap;
+      // pacing counter, the range list's count and its rows' bits
+      AERO_CUDA_TRY(cudaMemsetAsync(f.sync_ctr, 0, 512 + (size_t)tpc * lmhead::BM / 8, ctx->stream));
       const long long pairs = (tpc + 1) / 2 * vs;
       const int grid = 2 * (int)(pairs < max_pairs ? pairs : max_pairs);
       const bool timed = ctx->timing && ctx->n_timed < 256;

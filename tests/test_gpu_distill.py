@@ -322,6 +322,25 @@ def test_rows_beyond_the_range_of_the_stored_exponentials(ctx, kind, rowscale):
     check_grads(case, dH, dW, r)
 
 
+def test_rows_out_of_range_in_many_splits_are_listed_once(ctx):
+    """64 rows with a logit 130 above the first ones in every vocabulary tile of 235, over which a small call spreads
+    dozens of splits: 64 rows to redo, not that many for every split (the list holds 1024)."""
+    case = Case(T=64, d=64, V=60000, K=6, R=2, drop=False, lean=False)
+    W = torch.randn(60000, 64, generator=torch.Generator().manual_seed(3)) * 0.02
+    H = torch.randn(64, 64, generator=torch.Generator().manual_seed(4))
+    H[:, 0] = 10.0
+    W[:, 0] = 0.0
+    W[100::256, 0] = 13.0
+    case.ids[::2, 1] = 100 + 256 * 7
+    case.Ht, case.Wt = H.to(torch.bfloat16), W.to(torch.bfloat16)
+    dv, _ = case.device()
+    r = case.reference()
+    out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv)
+    assert ctx.last_status() == 0
+    check_forward(case, out, r)
+    check_grads(case, dH, dW, r)
+
+
 def test_gradient_rows_of_a_sure_student(ctx):
     """Rows whose listed token has probability near one on both sides: p - q keeps the accuracy of the log-probs."""
     case = Case(T=256, d=256, V=4096, K=4, R=2, drop=False, lean=False, spread=0.0)

@@ -536,6 +536,57 @@ def test_one_call_step_redoes_rows_with_a_logit_out_of_range(ctx):
     assert TL.rel_l2(dHe.float().cpu().numpy(), dH2.float().cpu().numpy()) > 5 * GRAD_L2      # the term carries weight
 
 
+@pytest.mark.parametrize("rowscale", [-1, 0])
+def test_rows_out_of_range_in_every_split_are_listed_once(ctx, rowscale):
+    """400 rows whose logits reach 130 above the first ones in each of four vocabulary splits: the list of 1024 rows
+    to redo holds them all.
+
+    The gradients are compared with fp64 ones of the call's own g, entry by entry.  Half of the targets are among the 16 high
+    columns, whose shares of dH[:, 0] (13 g / 16 each) add up to zero there, so that an entry's bound has to follow the
+    sizes of what is added, not its sum.  With a logit's error e = (d/8 + 8) 2^-23 S (fp32 accumulation, S = sum_k |h_k w_vk|)
+    and log-sum-exp's e + (V/32 + 64) 2^-24 + 2^-20 |lse|:
+      dz      2^-8 |dz| (rounded to bf16), 2^-8 |g| p (its exponential was, too), |g| (p + 1[y]) (both errors + 2^-17),
+              2^-125 (columns 130 below the high ones: |g| < 1, and an exponential or a product below 2^-126, the least
+              normal number of both types, may become zero)
+      dH, dW  the errors of dz through |W|, |H|; for dW 2^-8 |dz| again (rows of H scaled and rounded); 2^-14 of the sizes for
+              accumulation; 2^-8 |dH| for its rounding."""
+    T, d, V, R = 400, 64, 4000, 4
+    g = torch.Generator().manual_seed(7)
+    H, W = torch.randn(T, d, generator=g), torch.randn(V, d, generator=g) * 0.02
+    H[:, 0], W[:, 0] = 10.0, 0.0
+    W[100::256, 0] = 13.0
+    y = torch.randint(0, V, (T,), generator=g).int()
+    y[::2] = 100 + 256 * 5
+    H, W, y = H.to(torch.bfloat16).cuda(), W.to(torch.bfloat16).cuda(), y.cuda()
+    cs = torch.arange(0, T + 1, T // R, dtype=torch.int64, device="cuda")
+    adv = torch.tensor([1.0, -0.5, 0.7, -1.0], device="cuda")
+    w, keep = torch.full((R,), 1.0 / T, device="cuda"), torch.ones(R, dtype=torch.uint8, device="cuda")
+    cfg = TL.lib_cfg(O.Cfg(), "bf16")
+    old = ctx.grpo_loss_fwd(cfg, H, W, y, torch.zeros(T, device="cuda"), cs, adv, w, keep)["logp"].clone() + 0.01
+    ctx.set_tuning(vsplit=4, rowscale=rowscale)
+    try:
+        f, dH, dW = ctx.grpo_loss_fwd_bwd(cfg, H, W, y, old, cs, adv, w, keep)
+    finally:
+        ctx.set_tuning()
+    assert ctx.last_status() == 0
+    h, wt = H.double().cpu().numpy(), W.double().cpu().numpy()
+    z = h @ wt.T
+    lse = np.logaddexp.reduce(z, axis=1)
+    p = np.exp(z - lse[:, None])
+    hot = np.zeros_like(p)
+    hot[np.arange(T), y.cpu().numpy()] = 1.0
+    gt = f["g"].double().cpu().numpy()[:T, None]
+    assert (gt != 0).all()
+    dz = gt * (hot - p)
+    e = (d / 8 + 8) * 2.0 ** -23 * (np.abs(h) @ np.abs(wt).T).max(axis=1)
+    e_lse = e + (V / 32 + 64) * 2.0 ** -24 + 2.0 ** -20 * np.abs(lse)
+    edz = 2.0 ** -8 * (np.abs(dz) + np.abs(gt) * p) + np.abs(gt) * (p + hot) * (e + e_lse + 2.0 ** -17)[:, None] + 2.0 ** -125
+    tol_h = edz @ np.abs(wt) + 2.0 ** -14 * (np.abs(dz) @ np.abs(wt)) + 2.0 ** -8 * np.abs(dz @ wt)
+    tol_w = (edz + (2.0 ** -8 + 2.0 ** -14) * np.abs(dz)).T @ np.abs(h)
+    assert (np.abs(dH.double().cpu().numpy() - dz @ wt) <= tol_h).all()
+    assert (np.abs(dW.double().cpu().numpy() - dz.T @ h) <= tol_w).all()
+
+
 def _row_err(a, b, rows):
     """Relative L2 error of each listed row of a against b."""
     a, b = np.asarray(a, np.float64)[rows], np.asarray(b, np.float64)[rows]
