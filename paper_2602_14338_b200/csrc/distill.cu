@@ -266,15 +266,15 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
       } else {
         lp_y = zy - lse;
       }
-      float kl = 0.f, Q = 0.f, mass = 0.f, q[kSlots], pr[kSlots];
+      float kl = 0.f, Q = 0.f, mass = 0.f, q[kSlots], lps[kSlots];
 #pragma unroll
       for (int s = 0; s < kSlots; ++s) {
         q[s] = 0.f;
-        pr[s] = 0.f;
+        lps[s] = -INFINITY;
         if (id[s] >= 0) {
           const float lp = id[s] == yt ? lp_y : z[s] - lse;
-          pr[s] = expf(lp);
-          mass += pr[s];
+          lps[s] = lp;
+          mass += expf(lp);
           if (lg[s] > -INFINITY) {                    // a logit of -inf or NaN carries no weight
             const float lq = lg[s] - norm;
             q[s] = expf(lq);
@@ -287,11 +287,13 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
       Q = warp_sum(Q);
       mass = warp_sum(mass);
       if (a.ls.entry) {
-        // a token listed twice has one entry, with the sum of its q
+        // Q p - q of a token, with q the sum over its places and q_o that over the other tokens', as q_o p + q (p - 1): both
+        // terms keep their relative accuracy where p and q are close to 1, which a difference of rounded numbers next to
+        // 1 does not
         const float c = a.grad_scale * wi;
-        float qsum[kSlots];
+        float same[kSlots], other[kSlots];
 #pragma unroll
-        for (int s = 0; s < kSlots; ++s) qsum[s] = 0.f;
+        for (int s = 0; s < kSlots; ++s) same[s] = other[s] = 0.f;
 #pragma unroll
         for (int s2 = 0; s2 < kSlots; ++s2) {
           if (s2 * 32 < K) {
@@ -299,14 +301,16 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
               const int v = __shfl_sync(0xffffffffu, id[s2], l);
               const float qv = __shfl_sync(0xffffffffu, q[s2], l);
 #pragma unroll
-              for (int s = 0; s < kSlots; ++s)
-                if (id[s] == v) qsum[s] += qv;
+              for (int s = 0; s < kSlots; ++s) {
+                if (id[s] == v) same[s] += qv;
+                else other[s] += qv;
+              }
             }
           }
         }
 #pragma unroll
         for (int s = 0; s < kSlots; ++s)
-          if (s * 32 + lane < K) a.ls.entry[t * K + s * 32 + lane] = c * (Q * pr[s] - qsum[s]);
+          if (s * 32 + lane < K) a.ls.entry[t * K + s * 32 + lane] = c * (other[s] * expf(lps[s]) + same[s] * expm1f(lps[s]));
       }
       if (lane == 0) {
         if (a.g) a.g[t] = -wi * Q;

@@ -357,6 +357,53 @@ def test_gradient_rows_of_a_sure_student(ctx):
     check_grads(case, dH, dW, r)
 
 
+class SureCase(Case):
+    """Rows that leave between 1e-5 and 1e-8 of the probability to all other tokens, on the student's side and on the
+    teacher's.  Every row lists token Y, alone or with two others; Y alone has a weight in column 2 of W, which H does not use, so
+    dH[t, 2] is Y's entry of row t and nothing else.
+
+    The entry is w (q_o p - q (1 - p)), q_o the weight of the other listed tokens.  Its two terms may be off by 2^-17 (exp,
+    log) plus the errors of the logits and of the log-sum-exp without Y, as listed at the head of this file; the entry and dH
+    are rounded once each."""
+    Y = 1234
+
+    def __init__(self, K, dtype):
+        super().__init__(T=96, d=64, V=4096, K=K, dtype=dtype, R=1, drop=False, lean=False)
+        g = torch.Generator().manual_seed(5)
+        dt = self.Ht.dtype
+        W = torch.randn(4096, 64, generator=g) * 0.02
+        H = torch.randn(96, 64, generator=g)
+        W[:, 1:3], H[:, 1:3] = 0.0, 0.0
+        W[self.Y] = 0.0
+        W[self.Y, 1:3] = 1.0
+        H[:, 1] = torch.linspace(19.0, 27.0, 96)
+        self.Ht, self.Wt = H.to(dt), W.to(dt)
+        self.ids[:] = np.array([self.Y, 17, 3000])[:K]
+        self.logits[:] = np.array([25.0, 6.0, 3.0])[:K]
+        self.w[:] = 1.0 / 96
+
+    def check(self, dH):
+        r = self.reference()
+        q, q_o = r["q"][:, 0], r["q"][:, 1:].sum(axis=1)
+        p = np.exp(r["lp"][:, 0])
+        left = np.exp(np.logaddexp.reduce(np.delete(r["z"], self.Y, axis=1), axis=1) - r["lse"])      # 1 - p
+        assert 5e-9 < left.min() < 2e-8 and 5e-6 < left.max() < 5e-5
+        S = (np.abs(self.Ht.double().numpy()) @ np.abs(self.Wt.double().numpy()).T).max(axis=1)
+        rel = 2 * (self.d / 8 + 8) * 2.0 ** -23 * S + (self.V / 32 + 64) * 2.0 ** -24 + 2.0 ** -17
+        half = 2 * 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -22
+        want = r["wt"] * (q_o * p - q * left)
+        close(dH[:, 2], want, half * np.abs(want) + rel * r["wt"] * (q_o * p + q * left), "entry of the sure token")
+
+
+@pytest.mark.parametrize("K", [1, 3])
+def test_entry_of_a_token_that_both_are_sure_of(ctx, K):
+    case = SureCase(K, "bf16")
+    dv, _ = case.device()
+    _, dH, _ = ctx.distill_fwd_bwd(case.cfg, **dv)
+    case.check(dH)
+    assert ctx.last_status() == 0
+
+
 def test_captured_and_replayed(ctx):
     side = torch.cuda.Stream()
     c = B.Context(0, stream=side)
