@@ -66,10 +66,10 @@ extern "C" {
 #define AERO_ST_BAD_REWARD     4u   /* reward not exactly 0 or 1                       */
 #define AERO_ST_EMPTY_ROLLOUT  8u   /* cs[i+1] == cs[i] for a present rollout          */
 #define AERO_ST_TIMEOUT       16u   /* a bounded wait inside a kernel ran out          */
-#define AERO_ST_RANGE         32u   /* aero_grpo_loss_fwd_bwd: more than 1024 rows of one chunk have a   */
+#define AERO_ST_RANGE         32u   /* one-call steps (aero_*_fwd_bwd): more than 1024 rows of one chunk have a */
                                     /* logit over 125 octaves above the shift taken from the row's first  */
                                     /* logits; the rows beyond the 1024 the call redoes have a saturated   */
-                                    /* gradient (use aero_grpo_loss_fwd + aero_grpo_loss_bwd instead)      */
+                                    /* gradient (use the separate forward and backward calls instead)      */
 
 /* ---- enumerations ------------------------------------------------------------- */
 #define AERO_UNIFORM_MASK   0   /* all-correct / all-incorrect groups are dropped (Sec. 3.2)      */
@@ -561,9 +561,10 @@ int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
  * Precision as in stage (b): dz is rounded to bf16 before the two products (fp32 accumulation), its listed
  * entries once, from fp32 log-probs; its softmax part once by aero_distill_bwd and twice by aero_distill_fwd_bwd, which
  * scales the stored bf16 exponentials; the rows of H enter dW as they are.  lse and kl take the first listed token's
- * logit as an fp32 dot product.  aero_distill_bwd takes lse from the forward and recomputes the logits
- * (8 d V FLOP per token over the two calls), aero_distill_fwd_bwd does not (6 d V; a row with a logit too far
- * above its first ones is redone as in aero_grpo_loss_fwd_bwd, AERO_ST_RANGE beyond 1024 per chunk).
+ * logit as an fp32 dot product, and the entry of that token keeps the relative accuracy of 1 - p however close p is to
+ * 1.  aero_distill_bwd takes lse from the forward and recomputes the logits (8 d V FLOP per token over the two calls); where
+ * 1 - p of the first listed token comes near the rounding of lse it is made of the other columns' part of dz.
+ * aero_distill_fwd_bwd does not recompute them (6 d V; a row with a logit too far above its first ones is redone as in aero_grpo_loss_fwd_bwd, AERO_ST_RANGE beyond 1024 per chunk).
  * workspace: at least the matching *_workspace_bytes, 256-byte aligned; chunk_tokens as in
  *          aero_bwd_workspace_bytes, and a bf16 dW of rows that do not fit one chunk takes V d floats more.
  */

@@ -61,6 +61,7 @@ struct RowsArgs {
   float* lse;              // in: the rows' log-sum-exp, unless xstate gives it (then out)
   const int32_t* y;        // the first listed token
   float* g;                // out: -w_i Q_t, or NULL
+  float4* ysum;            // out: weight of the other listed tokens and of y in the list, y's logit; or NULL
   float grad_scale;
   const float4* xstate;    // running states of the lm_head kernel, [split][T], or NULL
   const int* plan;         // split count
@@ -129,6 +130,17 @@ __device__ __forceinline__ float2 join_states(const float4* xs, long long T, lon
   const float lse = (M + big + log2f(lr + ey)) * lmhead::kLn2;
   const float lp = a > -40.f ? -log1pf(l * exp2f(-a)) : (a - log2f(l + exp2f(a))) * lmhead::kLn2;
   return make_float2(lse, lp);
+}
+
+// The backward alone has only the rounded lse, and zy - lse is no log-prob of y where 1 - p_y comes near lse's rounding.  From
+// 2^12 of these roundings down a row takes (1 - p_y) / p_y from the sum of the other columns' exponentials and y's own
+// instead, in which lse cancels.
+__device__ __forceinline__ bool sure_of_y(float zy, float lse) { return zy - lse > -0x1p-12f * fmaxf(fabsf(lse), 1.f); }
+// dz of such a row at y; outside = sum_{v != y} exp(z_v - lse)
+__device__ __forceinline__ float sure_entry(const RowsArgs& a, long long t, float outside) {
+  const float4 q = a.ysum[t];
+  const float lp = -log1pf(outside * expf(a.lse[t] - q.z));
+  return a.grad_scale * a.wrow[t] * (q.x * expf(lp) + q.y * expm1f(lp));
 }
 
 // Student logits at the listed tokens: kDots list places of one row per warp, so that even a few hundred rows put
@@ -310,9 +322,13 @@ __global__ void __launch_bounds__(256) distill_rows_kernel(RowsArgs a) {
         }
 #pragma unroll
         for (int s = 0; s < kSlots; ++s)
-          if (s * 32 + lane < K) a.ls.entry[t * K + s * 32 + lane] = c * (other[s] * expf(lps[s]) + same[s] * expm1f(lps[s]));
+          if (s * 32 + lane < K) {
+            a.ls.entry[t * K + s * 32 + lane] = c * (other[s] * expf(lps[s]) + same[s] * expm1f(lps[s]));
+            if (a.ysum && id[s] == yt) a.ysum[t] = make_float4(other[s], same[s], zy, 0.f);
+          }
       }
       if (lane == 0) {
+        if (a.ysum && !any_listed) a.ysum[t] = make_float4(0.f, 0.f, -INFINITY, 0.f);
         if (a.g) a.g[t] = -wi * Q;
         if (a.ls.kl) a.ls.kl[t] = kl;
       }
@@ -340,6 +356,7 @@ struct BlockArgs {
   __nv_bfloat16* dz;            // the chunk's block, tiled: [tile - tile_begin][nblk][128][64]
   int nblk, nvt;
   const float* shift;           // [split][T], log2 domain
+  float* outside;               // backward alone: probability outside y's column of the rows that are sure of y; else NULL
 };
 
 // p~ -> the softmax part of dz, -g_t grad_scale exp(c_t - lse_t) p~, in place: block (vocabulary tile of 256
@@ -378,6 +395,40 @@ __global__ void __launch_bounds__(256) distill_scale_kernel(BlockArgs b) {
   }
 }
 
+// Of the rows that are sure of y (sure_of_y), the probability outside y's column, from the softmax part that the block
+// holds: its values are rounded to bf16, and the entry that is made of their sum will be too.  (Summing in the lm_head kernel's
+// epilogue instead made all rows pay: 340 -> 393 us for the kernel at 1000 rows, d = 1536, V = 151936.)  A block per row.
+__global__ void __launch_bounds__(256) distill_outside_kernel(BlockArgs b) {
+  __shared__ float sh[8];
+  const RowsArgs& a = b.a;
+  const long long rows = units_of(a) * 8;
+  for (long long i = blockIdx.x; i < rows; i += gridDim.x) {
+    const long long t = row_of(a, i / 8, (int)(i % 8));
+    if (t < 0) continue;
+    const float c0 = -a.g[t] * a.grad_scale;
+    if (c0 == 0.f || !sure_of_y(a.ysum[t].z, a.lse[t])) continue;
+    const int y = a.y[t], n = b.nblk * 8;                         // 16-byte vectors of the row, 8 in a row of a 64-column tile
+    const uint4* p = reinterpret_cast<const uint4*>(b.dz + ((size_t)(i / 128) * b.nblk * 128 + i % 128) * 64);
+    float sum = 0.f;
+#pragma unroll 8
+    for (int k = threadIdx.x; k < n; k += 256) {
+      float x[8];
+      rowvec::unpack(p[(size_t)(k >> 3) * (128 * 8) + (k & 7)], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += k * 8 + e != y ? x[e] : 0.f;
+    }
+    sum = warp_sum(sum);
+    __syncthreads();                                              // the previous row's sums have been read
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      sum = 0.f;
+      for (int w = 0; w < 8; ++w) sum += sh[w];
+      b.outside[t] = sum / c0;
+    }
+  }
+}
+
 // The entries of dz at the listed tokens, over the softmax part.
 __global__ void __launch_bounds__(256) distill_scatter_kernel(BlockArgs b) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -387,10 +438,17 @@ __global__ void __launch_bounds__(256) distill_scatter_kernel(BlockArgs b) {
     const long long t = row_of(b.a, u, warp);
     if (t < 0) continue;
     const int lt = (int)(u / kUnitsPerTile), r = (int)(u % kUnitsPerTile) * 8 + warp;
+    int y = -1;
+    float at_y = 0.f;
+    if (b.outside && b.a.g[t] * b.a.grad_scale != 0.f && sure_of_y(b.a.ysum[t].z, b.a.lse[t])) {
+      y = b.a.y[t];
+      at_y = sure_entry(b.a, t, b.outside[t]);
+    }
     for (int k = lane; k < K; k += 32) {
       const int v = b.a.ls.ids[t * K + k];
       if (v < 0 || v >= b.a.V) continue;
-      b.dz[(((size_t)lt * b.nblk + v / 64) * 128 + r) * 64 + v % 64] = __float2bfloat16_rn(b.a.ls.entry[t * K + k]);
+      b.dz[(((size_t)lt * b.nblk + v / 64) * 128 + r) * 64 + v % 64] =
+          __float2bfloat16_rn(v == y ? at_y : b.a.ls.entry[t * K + k]);
     }
   }
 }
@@ -569,9 +627,10 @@ __device__ __forceinline__ void add_rows(float (&acc)[NC], float x_mine, const f
       if (q * 32 + lane < d) acc[q] = fmaf(x, tile[i * pitch + q * 32 + lane], acc[q]);
   }
 }
-// the warps' rows of sums, added in order, to out[d]
+// the warps' rows of sums, added in order, to out[d]; then x times the row `last`
 template <int NC>
-__device__ __forceinline__ void join_rows(const float (&acc)[NC], float* sm, int d, float* out, bool accumulate) {
+__device__ __forceinline__ void join_rows(const float (&acc)[NC], float* sm, int d, float* out, bool accumulate, float x = 0.f,
+                                          const float* last = nullptr) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nw = blockDim.x >> 5;
   __syncthreads();                                       // the staged rows have been read
 #pragma unroll
@@ -581,11 +640,13 @@ __device__ __forceinline__ void join_rows(const float (&acc)[NC], float* sm, int
   for (int k = threadIdx.x; k < d; k += blockDim.x) {
     float s = 0.f;
     for (int w = 0; w < nw; ++w) s += sm[w * d + k];
+    if (last) s = fmaf(x, last[k], s);
     out[k] = accumulate ? out[k] + s : s;
   }
 }
 
-// Block t: the row's log-sum-exp, or its row of dH.  NC * 32 >= d.
+// Block t: the row's log-sum-exp, or its row of dH.  NC * 32 >= d.  A row of dH that is sure of y (sure_of_y) sums
+// the probability of the other columns on its way, makes y's entry of it and adds that entry's share last.
 template <int NC, bool GRADS>
 __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
   extern __shared__ float sm[];
@@ -603,6 +664,8 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
 #pragma unroll
   for (int q = 0; q < NC; ++q) acc[q] = 0.f;
   const bool work = GRADS ? c != 0.f : kept;
+  const int yt = GRADS && work && sure_of_y(a.ysum[t].z, lse) ? a.y[t] : -1;
+  float rest = 0.f;
   for (int v0 = warp * 32; work && v0 < a.V; v0 += nw * 32) {
     stage_rows(tile, pitch, static_cast<const float*>(a.W), v0, a.V, d, nullptr);
     const float z = dot(h, tile + lane * pitch, d);
@@ -615,7 +678,9 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
       }
       continue;
     }
-    float dz = in ? c * expf(z - lse) : 0.f;
+    const float p = in ? expf(z - lse) : 0.f;
+    float dz = c * p;
+    if (v0 + lane != yt) rest += p;
     for (int k0 = 0; k0 < K; k0 += 32) {                 // at a listed token the entry takes the place of the softmax part
       const int id = k0 + lane < K ? a.ls.ids[t * K + k0 + lane] : -1;
       for (unsigned hits = __ballot_sync(0xffffffffu, id >= v0 && id < v0 + 32 && id < a.V); hits != 0; hits &= hits - 1) {
@@ -623,10 +688,22 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
         if (v == v0 + lane) dz = a.ls.entry[t * K + k0 + src];
       }
     }
+    if (v0 + lane == yt) dz = 0.f;
     add_rows<NC>(acc, dz, tile, pitch, d);
   }
   if (GRADS) {
-    join_rows<NC>(acc, sm, d, f.dH + t * d, false);
+    float entry = 0.f;
+    if (yt >= 0) {
+      rest = warp_sum(rest);
+      if (lane == 0) state[warp].x = rest;
+      __syncthreads();
+      float outside = 0.f;
+      for (int w = 0; w < nw; ++w) outside += state[w].x;
+      entry = sure_entry(a, t, outside);
+      for (int k = threadIdx.x; k < K; k += blockDim.x)                            // (for the rows of dW)
+        if (a.ls.ids[t * K + k] == yt) a.ls.entry[t * K + k] = entry;
+    }
+    join_rows<NC>(acc, sm, d, f.dH + t * d, false, entry, yt >= 0 ? static_cast<const float*>(a.W) + (long long)yt * d : nullptr);
   } else {
     const float M = warp_max(m);
     l = warp_sum(m > -INFINITY ? l * expf(m - M) : 0.f);
@@ -688,6 +765,8 @@ struct Ws {
   float* g;
   float* z;
   float* entry;
+  float4* ysum;
+  float* outside;
   double* partials;
   size_t n_partials;
   aero_tiles tiles;
@@ -739,6 +818,8 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, Mode
   w.v_hi = few && base_v < kMaxVsplit ? kMaxVsplit : base_v;
   if (w.v_hi > nvt) w.v_hi = nvt;
   if (mode != kBwd) w.xstate = reinterpret_cast<float4*>(take((size_t)w.v_hi * Tn * sizeof(float4)));
+  if (mode == kBwd) w.outside = reinterpret_cast<float*>(take(Tn * 4));
+  if (mode != kFwd) w.ysum = reinterpret_cast<float4*>(take(Tn * sizeof(float4)));
   if (mode == kBoth) w.shift = reinterpret_cast<float*>(take((size_t)w.v_hi * Tn * sizeof(float)));
   w.k_hi = 1;
   if (mode != kFwd && few) {
@@ -906,7 +987,8 @@ int bwd_fp32(const Call& c, const Ws& s, const float* lse, float grad_scale, flo
     return AERO_OK;
   }
   AERO_CUDA_TRY(cudaMemsetAsync(s.g, 0, (size_t)c.T * sizeof(float), ctx->stream));      // rows of dropped rollouts
-  const Fp32Args f = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
+  Fp32Args f = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
+  f.r.ysum = s.ysum;
   if ((rc = rows_fp32(f.r, ctx))) return rc;
   // sums of a row: 4 or 32 registers a lane (T = 160, d = 57, V = 831, forward and gradients: 189 or 267 us)
   const bool narrow = c.d <= 128;
@@ -1051,7 +1133,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     p.dz = gr.block; p.ldz = ldz;
     distill_dots_kernel<__nv_bfloat16><<<dim3(row_blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
     ctx->launches += 1;
-    BlockArgs b = {a, gr.block, (int)nblk, (V + lmhead::BN - 1) / lmhead::BN, s.shift};
+    BlockArgs b = {a, gr.block, (int)nblk, (V + lmhead::BN - 1) / lmhead::BN, s.shift, s.outside};
     if (mode == kBoth) {
       p.xstate = s.xstate; p.shift_out = s.shift;
       p.range_rows = s.range_rows; p.range_count = s.range_count; p.range_seen = s.range_seen; p.range_cap = kRangeCap;
@@ -1067,10 +1149,14 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
       range_fix_kernel<<<2 * ctx->sm_count, 256, 0, ctx->stream>>>(f);
       ctx->launches += 3;
     } else {
+      a.ysum = s.ysum;
+      b.a.ysum = s.ysum;
       distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);
       ctx->launches += 1;
       p.lse_in = lse; p.g_in = s.g; p.grad_scale = gr.grad_scale;
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBwd))) return rc;
+      distill_outside_kernel<<<row_blocks_of((end - begin) * lmhead::BM), 256, 0, ctx->stream>>>(b);
+      ctx->launches += 1;
     }
     distill_scatter_kernel<<<row_blocks, 256, 0, ctx->stream>>>(b);
     gemmbwd::Params gp = {};

@@ -382,7 +382,7 @@ class SureCase(Case):
         self.logits[:] = np.array([25.0, 6.0, 3.0])[:K]
         self.w[:] = 1.0 / 96
 
-    def check(self, dH):
+    def check(self, dH, more=0.0):
         r = self.reference()
         q, q_o = r["q"][:, 0], r["q"][:, 1:].sum(axis=1)
         p = np.exp(r["lp"][:, 0])
@@ -392,7 +392,7 @@ class SureCase(Case):
         rel = 2 * (self.d / 8 + 8) * 2.0 ** -23 * S + (self.V / 32 + 64) * 2.0 ** -24 + 2.0 ** -17
         half = 2 * 2.0 ** -8 if self.dtype == "bf16" else 2.0 ** -22
         want = r["wt"] * (q_o * p - q * left)
-        close(dH[:, 2], want, half * np.abs(want) + rel * r["wt"] * (q_o * p + q * left), "entry of the sure token")
+        close(dH[:, 2], want, half * np.abs(want) + (rel + more) * r["wt"] * (q_o * p + q * left), "entry of the sure token")
 
 
 @pytest.mark.parametrize("K", [1, 3])
@@ -401,6 +401,22 @@ def test_entry_of_a_token_that_both_are_sure_of(ctx, K):
     dv, _ = case.device()
     _, dH, _ = ctx.distill_fwd_bwd(case.cfg, **dv)
     case.check(dH)
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("K,dtype", [(1, "bf16"), (3, "bf16"), (1, "fp32"), (3, "fp32")])
+def test_entry_of_a_sure_token_from_the_rounded_lse(ctx, K, dtype):
+    """The backward alone gets lse rounded to 2^-20, far above 1 - p; and both forms in fp32.  For bf16 rows it makes 1 - p of the
+    other columns' dz, which are rounded to bf16."""
+    case, more = SureCase(K, dtype), 2.0 ** -8 if dtype == "bf16" else 0.0
+    dv, _ = case.device()
+    out, dH, _ = ctx.distill_fwd_bwd(case.cfg, **dv)
+    case.check(dH)
+    dH, _ = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"])
+    case.check(dH, more)
+    # an lse that is as far off as rounding can make it stands in all terms alike and changes 1 - p by as much, relative
+    dH, _ = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"] * (1 + 2.0 ** -23))
+    case.check(dH, more)
     assert ctx.last_status() == 0
 
 
