@@ -560,11 +560,12 @@ int aero_quantize_rows(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
  *          accumulate_dW != 0) or, for bf16 rows, AERO_BF16 (overwritten, rounded once).
  * Precision as in stage (b): dz is rounded to bf16 before the two products (fp32 accumulation), its listed
  * entries once, from fp32 log-probs; its softmax part once by aero_distill_bwd and twice by aero_distill_fwd_bwd, which
- * scales the stored bf16 exponentials; the rows of H enter dW as they are.  lse and kl take the first listed token's
- * logit as an fp32 dot product, and the entry of that token keeps the relative accuracy of 1 - p however close p is to
- * 1.  aero_distill_bwd takes lse from the forward and recomputes the logits (8 d V FLOP per token over the two calls); where
- * 1 - p of the first listed token comes near the rounding of lse it is made of the other columns' part of dz.
- * aero_distill_fwd_bwd does not recompute them (6 d V; a row with a logit too far above its first ones is redone as in aero_grpo_loss_fwd_bwd, AERO_ST_RANGE beyond 1024 per chunk).
+ * scales the stored bf16 exponentials; the rows of H enter dW as they are.  lse and kl take the logit of the listed token
+ * with the largest teacher logit as an fp32 dot product, and that token's entry keeps the relative accuracy of 1 - p
+ * however close p is to 1.  aero_distill_bwd takes lse from the forward and recomputes the logits (8 d V FLOP per
+ * token over the two calls); where that 1 - p comes near the rounding of lse it is made of the other columns' part of
+ * dz.  aero_distill_fwd_bwd does not recompute them (6 d V; a row with a logit too far above its first ones is redone
+ * as in aero_grpo_loss_fwd_bwd, AERO_ST_RANGE beyond 1024 per chunk).
  * workspace: at least the matching *_workspace_bytes, 256-byte aligned; chunk_tokens as in
  *          aero_bwd_workspace_bytes, and a bf16 dW of rows that do not fit one chunk takes V d floats more.
  */

@@ -59,7 +59,7 @@ struct RowsArgs {
   const uint8_t* keep;
   const float* wrow;       // weight of each row
   float* lse;              // in: the rows' log-sum-exp, unless xstate gives it (then out)
-  const int32_t* y;        // the first listed token
+  const int32_t* y;        // the listed token with the largest teacher logit
   float* g;                // out: -w_i Q_t, or NULL
   float4* ysum;            // out: weight of the other listed tokens and of y in the list, y's logit; or NULL
   float grad_scale;
@@ -478,12 +478,15 @@ __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const 
   }
 }
 
-// Before anything else, one warp per row: y_t = the first listed token (0 where the list is empty) and the row's
-// weight, or the outputs of a row that belongs to no kept rollout.
+// Before anything else, one warp per row: y_t = the listed token with the largest teacher logit (the first of equals; 0 where the
+// list is empty) and the row's weight, or the outputs of a row that belongs to no kept rollout.  y's entry of dz keeps the
+// relative accuracy of 1 - p_y.  No other token needs that: its q (in one place) is at most y's, and its entry q_o p - q (1 - p) then has
+// in q_o p, q_o >= q_y >= q, a term that the rounding of its log-prob is small against.
 struct FirstArgs {
   long long T;
   int d, V, R, K;
   const int32_t* ids;
+  const float* logits;
   const int64_t* cs;
   const float* w;
   const uint8_t* keep;
@@ -510,14 +513,24 @@ __global__ void __launch_bounds__(256) distill_first_kernel(FirstArgs a) {
       continue;
     }
     int first = 0x7fffffff;
+    float top = -INFINITY;
     bool bad = false;
     for (int k = lane; k < a.K; k += 32) {
       const int v = a.ids[t * a.K + k];
-      if (v >= 0 && v < a.V) first = min(first, k);
-      else bad |= v != AERO_NO_TOKEN;
+      const float x = a.logits[t * a.K + k];
+      if (v >= 0 && v < a.V) {
+        if (x > top || first == 0x7fffffff) first = k;        // (a NaN is larger than nothing)
+        top = fmaxf(top, x);
+      } else {
+        bad |= v != AERO_NO_TOKEN;
+      }
     }
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) first = min(first, __shfl_xor_sync(0xffffffffu, first, o));
+    for (int o = 16; o > 0; o >>= 1) {
+      const int f = __shfl_xor_sync(0xffffffffu, first, o);
+      const float x = __shfl_xor_sync(0xffffffffu, top, o);
+      if (x > top || (x == top && f < first)) { first = f; top = x; }
+    }
     if (__any_sync(0xffffffffu, bad) && lane == 0) aero_raise(a.status, AERO_ST_BAD_TARGET);
     if (lane == 0) {
       a.y[t] = first < a.K ? a.ids[t * a.K + first] : 0;
@@ -929,7 +942,7 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
   AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, zero_bytes((size_t)chunk_tiles), ctx->stream));
   if (partials) AERO_CUDA_TRY(cudaMemsetAsync(s.partials, 0, s.n_partials * kPartialStride * sizeof(double), ctx->stream));
   if (c.T == 0) return AERO_OK;
-  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.cs, c.w, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
+  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.logits, c.cs, c.w, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
                        ctx->d_status};
   distill_first_kernel<<<row_grid(c.T), 256, 0, ctx->stream>>>(f);
   ctx->launches += 1;

@@ -367,7 +367,7 @@ class SureCase(Case):
     are rounded once each."""
     Y = 1234
 
-    def __init__(self, K, dtype):
+    def __init__(self, K, dtype, last=False):
         super().__init__(T=96, d=64, V=4096, K=K, dtype=dtype, R=1, drop=False, lean=False)
         g = torch.Generator().manual_seed(5)
         dt = self.Ht.dtype
@@ -380,12 +380,15 @@ class SureCase(Case):
         self.Ht, self.Wt = H.to(dt), W.to(dt)
         self.ids[:] = np.array([self.Y, 17, 3000])[:K]
         self.logits[:] = np.array([25.0, 6.0, 3.0])[:K]
+        if last:                                           # Y in the last place
+            self.ids, self.logits = self.ids[:, ::-1].copy(), self.logits[:, ::-1].copy()
+        self.at = K - 1 if last else 0
         self.w[:] = 1.0 / 96
 
     def check(self, dH, more=0.0):
         r = self.reference()
-        q, q_o = r["q"][:, 0], r["q"][:, 1:].sum(axis=1)
-        p = np.exp(r["lp"][:, 0])
+        q, q_o = r["q"][:, self.at], np.delete(r["q"], self.at, axis=1).sum(axis=1)
+        p = np.exp(r["lp"][:, self.at])
         left = np.exp(np.logaddexp.reduce(np.delete(r["z"], self.Y, axis=1), axis=1) - r["lse"])      # 1 - p
         assert 5e-9 < left.min() < 2e-8 and 5e-6 < left.max() < 5e-5
         S = (np.abs(self.Ht.double().numpy()) @ np.abs(self.Wt.double().numpy()).T).max(axis=1)
@@ -416,6 +419,18 @@ def test_entry_of_a_sure_token_from_the_rounded_lse(ctx, K, dtype):
     case.check(dH, more)
     # an lse that is as far off as rounding can make it stands in all terms alike and changes 1 - p by as much, relative
     dH, _ = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"] * (1 + 2.0 ** -23))
+    case.check(dH, more)
+    assert ctx.last_status() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_entry_of_a_sure_token_that_is_not_listed_first(ctx, dtype):
+    """The teacher's list need not be sorted."""
+    case, more = SureCase(3, dtype, last=True), 2.0 ** -8 if dtype == "bf16" else 0.0
+    dv, _ = case.device()
+    out, dH, _ = ctx.distill_fwd_bwd(case.cfg, **dv)
+    case.check(dH)
+    dH, _ = ctx.distill_bwd(case.cfg, **dv, lse=out["lse"])
     case.check(dH, more)
     assert ctx.last_status() == 0
 
