@@ -514,7 +514,7 @@ int aero_allocate_sim(aero_ctx* ctx, const aero_cfg* cfg, const aero_alloc_cfg* 
  *   rstd = 1 / sqrt(mean_k s_k^2 + eps),   h_k = s_k rstd gamma_k
  *   8-bit form: q_scale = max_k |h_k| / 127,  q_k = round(h_k / q_scale)   (a row of zeros: scale 0)
  * s, the statistics and h are fp32 until each output is rounded once.  A row that holds a NaN or an
- * infinity gets a NaN (or infinite) q_scale, so that its values are not taken for numbers.
+ * infinity, or meets one in gamma, gets a NaN (or infinite) q_scale, so that its values are not taken for numbers.
  *   aero_rmsnorm_fwd: x, residual [T,d], gamma [d] (cfg->dtype) -> any of sum [T,d] (s), h [T,d]
  *     (cfg->dtype), rstd [T] f32, q [T,d] i8 with q_scale [T] f32; an output that is NULL is not
  *     written (q and q_scale only together).  eps > 0.

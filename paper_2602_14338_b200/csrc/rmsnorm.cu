@@ -64,12 +64,19 @@ template <int VEC, int NV>
 constexpr int bwd_blocks() { return VEC == 8 ? (NV == 1 ? 4 : (NV == 2 ? 2 : 1)) : 1; }
 constexpr int kWarps = 4;             // rows at a time per block of the warp kernel
 
+// the larger of two, or NaN if either is (fmaxf would drop it)
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // sum and maximum over a warp, the same value in every lane (fixed order)
 __device__ __forceinline__ float2 warp_sum_max(float sum, float mx) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    mx = max_or_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   }
   return make_float2(sum, mx);
 }
@@ -83,7 +90,7 @@ __device__ __forceinline__ float2 block_sum_max(float sum, float mx, float2* sh)
   float2 r = sh[0];
   for (int w = 1; w < nw; ++w) {
     r.x += sh[w].x;
-    r.y = fmaxf(r.y, sh[w].y);
+    r.y = max_or_nan(r.y, sh[w].y);
   }
   return r;
 }
@@ -93,8 +100,7 @@ struct RowScale {
   float rstd, amax, up, inv;
   __device__ RowScale(const FwdArgs& a, float2 red) {
     rstd = a.gamma ? 1.f / sqrtf(red.x / (float)a.d + a.eps) : 1.f;
-    // a NaN drops out of the maximum but not out of the sum of squares: the scale takes it from there
-    amax = red.x == red.x ? red.y * rstd : red.x;
+    amax = red.y * rstd;                                      // (NaN if the row or gamma holds one)
     up = amax < 0x1p-100f ? 0x1p100f : 1.f;                  // keeps 127 / amax finite for the smallest rows
     inv = amax > 0.f ? 127.f / (amax * up) : 0.f;
   }
@@ -161,7 +167,7 @@ __global__ void __launch_bounds__(kWarps * 32) rmsnorm_fwd_warp_kernel(FwdArgs a
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           ss = fmaf(s[e], s[e], ss);
-          if (a.q) mx = fmaxf(mx, fabsf(gm ? s[e] * g[e] : s[e]));
+          if (a.q) mx = max_or_nan(mx, fabsf(gm ? s[e] * g[e] : s[e]));
         }
       }
     }
@@ -232,7 +238,7 @@ __global__ void __launch_bounds__(max_threads<VEC, NV>(), fwd_blocks<VEC, NV>())
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           ss = fmaf(s[j][e], s[j][e], ss);
-          mx = fmaxf(mx, fabsf(gm ? s[j][e] * g[e] : s[j][e]));
+          mx = max_or_nan(mx, fabsf(gm ? s[j][e] * g[e] : s[j][e]));
         }
       }
     }

@@ -104,6 +104,21 @@ def test_rows_of_zeros_nan_and_infinities(ctx):
     assert torch.allclose(out["h"][4], torch.ones(96, device="cuda"), atol=1e-5)
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,d", [("fp32", 96), ("bf16", 1536), ("bf16", 3584), ("fp32", 3584), ("bf16", 97), ("fp32", 5001)])
+def test_a_gamma_that_is_no_number_shows_in_the_scale(ctx, dtype, d, bad):
+    """A row per warp, per block in whole vectors and in single elements: h is no number in that column, and the 8-bit row's scale
+    says so too."""
+    x = torch.ones(3, d, dtype=DT[dtype], device="cuda")
+    x[1] = 0.5
+    gamma = torch.ones(d, dtype=DT[dtype], device="cuda")
+    gamma[d - 7] = bad
+    out = ctx.rmsnorm_fwd(cfg_of(dtype), x, gamma, quant=True)
+    assert not torch.isfinite(out["h"][:, d - 7]).any() and torch.isfinite(out["h"][:, :d - 7]).all()
+    assert not torch.isfinite(out["q_scale"]).any()
+    assert torch.isfinite(out["rstd"]).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("T,d", SHAPES + [(1300, 96)])
 @pytest.mark.parametrize("dsum,shift", [(True, 0), (False, 0), (True, 1)])
