@@ -540,7 +540,7 @@ int sort_positions(aero_ctx* ctx, const Ws& w, int n, int d, int V, const int32_
   while (bits < 32 && ((uint32_t)V >> bits) != 0) ++bits;          // the keys are 0 .. V
   const int passes = (bits + 8) / 9;
   const int per = (bits + passes - 1) / passes;
-  const unsigned blocks = (unsigned)((n + kSortTile - 1) / kSortTile);
+  const unsigned blocks = (unsigned)(((long long)n + kSortTile - 1) / kSortTile);
   const unsigned helpers = clear ? 32u * (unsigned)ctx->sm_count : 0u;
   const int shares = 3 * passes - 1;
   int share = 0;
@@ -591,7 +591,7 @@ int bwd_launch(aero_ctx* ctx, int64_t T_, int32_t d, int32_t V, const int32_t* y
   const uint32_t *keys, *pos;
   const int rc = sort_positions(ctx, w, n, d, V, y, accumulate ? nullptr : dW, &keys, &pos);
   if (rc) return rc;
-  const long long tiles = (n + kTile - 1) / kTile, slabs = (d + 32 * VEC - 1) / (32 * VEC);
+  const long long tiles = ((long long)n + kTile - 1) / kTile, slabs = (d + 32 * VEC - 1) / (32 * VEC);
   AERO_CUDA_TRY(cudaMemsetAsync(w.runs.count, 0, 2 * sizeof(int), ctx->stream));
   embed_bwd_sum_kernel<T, VEC><<<(unsigned)((tiles * slabs + 7) / 8), 256, 0, ctx->stream>>>(
       n, d, V, keys, pos, dX, scale, dW, accumulate, w.part, w.runs);

@@ -149,3 +149,31 @@ def test_two_graphs_replayed_at_once_have_workspaces_of_their_own(ctx):
     for side, c, g, dX, y, dW in runs:
         assert torch.equal(dW, ctx.embed_bwd(cfg, dX, y, V))
         assert c.last_status() == 0
+
+
+def test_gradient_of_the_most_tokens(ctx):
+    """2^31 - 1 rows, the most a call takes: the rounded-up numbers of sort blocks and of tiles pass 32 bits on the way.  Rows of
+    one element, 0 or 1, over 300 tokens, so that every sum is a whole number below 2^24 and exact in any order."""
+    T, V, piece = 2 ** 31 - 1, 300, 1 << 27
+    g = torch.Generator(device="cuda").manual_seed(9)
+    y = torch.empty(T, dtype=torch.int32, device="cuda")
+    dX = torch.empty(T, 1, dtype=torch.bfloat16, device="cuda")
+    want = torch.zeros(V, dtype=torch.int64, device="cuda")
+    for a in range(0, T, piece):
+        n = min(piece, T - a)
+        ids = torch.randint(0, V, (n,), generator=g, device="cuda", dtype=torch.int32)
+        one = torch.randint(0, 2, (n,), generator=g, device="cuda", dtype=torch.int8)
+        y[a:a + n], dX[a:a + n, 0] = ids, one
+        want += torch.bincount(ids[one.bool()], minlength=V)
+    y[-1], dX[-1] = V - 1, 1.0
+    want[V - 1] += 1 - int(one[-1]) if int(ids[-1]) == V - 1 else 1
+    if int(ids[-1]) != V - 1:
+        want[int(ids[-1])] -= int(one[-1])
+    del ids, one
+    dW = ctx.embed_bwd(cfg_of("bf16"), dX, y, V)
+    assert int(want.max()) < 2 ** 24 and torch.equal(dW[:, 0].long(), want) and torch.equal(dW[:, 0], want.float())
+    dW = ctx.embed_bwd(cfg_of("bf16"), dX, y, V, dW=dW, accumulate_dW=True)
+    assert torch.equal(dW[:, 0], 2 * want.float())
+    assert ctx.last_status() == 0
+    del y, dX, dW
+    torch.cuda.empty_cache()                       # some 60 GB
