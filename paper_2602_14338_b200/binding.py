@@ -513,7 +513,7 @@ class Context:
     def rmsnorm_fwd(self, cfg, x, gamma, residual=None, eps=1e-6, h=True, quant=False, out=None):
         """aero_rmsnorm_fwd: returns a dict with rstd, sum (when a residual is given), h (unless h=False) and,
         with quant=True, q (int8) and q_scale.  `out` may hold any of these tensors already; out["sum"] or
-        out["h"] may be x or residual itself."""
+        out["h"] may be x or residual itself.  What the call does not write is not returned, even if `out` holds it."""
         T, d = x.shape
         dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
         o = dict(out) if out is not None else {}
@@ -534,7 +534,7 @@ class Context:
             self._arg(gamma, dt, (d,), "gamma"), eps, ptr.get("sum"), ptr.get("h"), ptr["rstd"], ptr.get("q"),
             ptr.get("q_scale"))
         _check(rc, "aero_rmsnorm_fwd")
-        return o
+        return {name: o[name] for name in ptr}
 
     def rmsnorm_bwd(self, cfg, dh, s, gamma, rstd, dsum=None, dx=None, dgamma=None, accumulate_dgamma=False):
         """aero_rmsnorm_bwd: returns (dx, dgamma); s and rstd are the forward's sum (x where there was no

@@ -84,6 +84,17 @@ def test_forward_outputs_are_optional_and_may_be_the_inputs(ctx):
     assert out["sum"] is r2 and torch.equal(r2, ref["sum"]) and torch.equal(x2, ref["h"])
 
 
+def test_outputs_of_an_earlier_call_are_not_returned_as_this_ones(ctx):
+    cfg = cfg_of("bf16")
+    gamma = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    first = ctx.rmsnorm_fwd(cfg, rows(9, 64, torch.bfloat16, 5), gamma, quant=True)
+    assert set(first) == {"rstd", "h", "q", "q_scale"}
+    again = ctx.rmsnorm_fwd(cfg, rows(9, 64, torch.bfloat16, 6), gamma, out=first)
+    assert set(again) == {"rstd", "h"} and again["h"] is first["h"]
+    again = ctx.rmsnorm_fwd(cfg, rows(9, 64, torch.bfloat16, 6), gamma, h=False, quant=True, out=first)
+    assert set(again) == {"rstd", "q", "q_scale"} and again["q"] is first["q"]
+
+
 def test_rows_of_zeros_nan_and_infinities(ctx):
     cfg = cfg_of("fp32")
     x = torch.ones(5, 96, device="cuda")
