@@ -191,6 +191,24 @@ def test_chunks_and_dw_types(ctx, chunk_tokens):
     assert ctx.last_status() == 0
 
 
+def test_more_rows_than_one_wave_over_many_vocabulary_tiles(ctx):
+    """More than 148 tiles of rows: no planned splits beyond stage (b)'s (8 at most, over nine vocabulary tiles), no split of dH; in
+    one chunk and in two, whose bf16 dW has its sums in the workspace."""
+    case = Case(T=19500, d=64, V=2300, K=3, R=40)
+    dv, _ = case.device()
+    r = case.reference()
+    fwd = ctx.distill_fwd(case.cfg, **dv)
+    check_forward(case, fwd, r)
+    for chunk_tokens in (None, 148 * 64):
+        for dt, half in ((torch.float32, 0.0), (torch.bfloat16, 2.0 ** -8)):
+            out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv, dw_dtype=dt, chunk_tokens=chunk_tokens)
+            check_forward(case, out, r)
+            check_grads(case, dH, dW, r, half)
+            dH, dW = ctx.distill_bwd(case.cfg, **dv, lse=fwd["lse"], dw_dtype=dt, chunk_tokens=chunk_tokens)
+            check_grads(case, dH, dW, r, half)
+    assert ctx.last_status() == 0
+
+
 @pytest.mark.parametrize("T,d,V", [(100, 256, 3000), (300, 2112, 700), (129, 3584, 290)])
 def test_bf16_dw_of_a_few_rows_needs_no_room_for_sums(ctx, T, d, V):
     """One chunk whose block is smaller than an fp32 dW would be; single CTAs and CTA pairs, vocabularies that end inside

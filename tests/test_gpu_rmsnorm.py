@@ -161,6 +161,23 @@ def test_backward(ctx, dtype, T, d, dsum, shift):
     assert torch.equal(over, dx) or shift
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("T,d", [(9, 1536), (700, 96), (5, 3584), (300, 97), (3, 5001)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_dx_over_each_of_its_inputs(ctx, dtype, T, d, shift):
+    """dx may be the array of dh, of s or of dsum, in whole vectors and in single elements: the same bits as into one of its own."""
+    dt = DT[dtype]
+    s, dh, ds = rows(T, d, dt, 41, shift), rows(T, d, dt, 42, shift), rows(T, d, dt, 43, shift)
+    gamma = (1 + 0.3 * torch.randn(d, generator=torch.Generator().manual_seed(3))).to(dt).cuda()
+    rstd = torch.rsqrt(s.double().square().mean(1) + 1e-5).float()
+    own = torch.empty(T * d + shift, dtype=dt, device="cuda")[shift:].view(T, d)
+    _, want_dg = ctx.rmsnorm_bwd(cfg_of(dtype), dh, s, gamma, rstd, dsum=ds, dx=own)
+    for i in range(3):
+        a = [t.clone() if shift == 0 else rows(T, d, dt, 41 + k, shift) for k, t in enumerate((s, dh, ds))]
+        dx, dg = ctx.rmsnorm_bwd(cfg_of(dtype), a[1], a[0], gamma, rstd, dsum=a[2], dx=a[i])
+        assert dx is a[i] and torch.equal(dx, own) and torch.equal(dg, want_dg)
+
+
 def test_no_rows(ctx):
     cfg = cfg_of("bf16")
     e = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
