@@ -31,7 +31,7 @@ struct Ctl {
   uint32_t tmem_base;
   int abort;
 };
-constexpr int kMaxStages = 12, kPairSlabs = 2, PSTAGES = 3;
+constexpr int kMaxStages = 4, kPairSlabs = 2, PSTAGES = 3;
 constexpr uint32_t P_STAGE = kPairSlabs * (A_BYTES + kPairN / 2 * BK);
 constexpr size_t kRing = 204 * 1024;              // q8_rows_kernel: as many stages as fit
 constexpr size_t R_SMEM = 1024 + kRing + sizeof(Ctl<kMaxStages>);
@@ -345,8 +345,8 @@ extern "C" int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, co
     // token 105 / 94.5 / 93.7 / 92.2 us; 128 tokens 114 / 109 / 116 us, the last with two stages).
     const size_t slab = A_BYTES + (size_t)p.n * BK;
     p.slabs = (int)(kRing / (3 * slab));
-    p.stages = (int)(kRing / (p.slabs * slab));
-    if (p.stages > kMaxStages) p.stages = kMaxStages;
+    p.stages = (int)(kRing / (p.slabs * slab));            // 3 or 4: at least two slabs fit three times, whatever n
+    static_assert(kRing / (3 * (A_BYTES + kRowsN * BK)) >= 2 && kMaxStages == 4, "depth of the ring");
     auto kernel = out_dtype == AERO_FP32 ? q8_rows_kernel<float> : q8_rows_kernel<__nv_bfloat16>;
     AERO_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)R_SMEM));
     const int blocks = (V + kRowBlock - 1) / kRowBlock;

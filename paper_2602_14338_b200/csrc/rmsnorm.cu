@@ -375,8 +375,9 @@ int launch_resident(aero_ctx* ctx, K kernel, const A& a, int threads, long long 
   return AERO_OK;
 }
 
-// Calls launch(vectors per thread, threads) for a block per row of `nvec` vectors.
-template <int VEC, typename F>
+// Calls launch(vectors per thread, threads) for a block per row of `nvec` vectors, of which there are more than fit 256 threads
+// once where LONG.
+template <int VEC, bool LONG, typename F>
 int with_block_shape(int nvec, F launch) {
   auto threads = [&](int nv) { return ((nvec + nv - 1) / nv + 31) / 32 * 32; };
   if constexpr (VEC == 1) {
@@ -384,7 +385,8 @@ int with_block_shape(int nvec, F launch) {
     return launch(std::integral_constant<int, 16>(), threads(16));
   } else {
     constexpr int kMost = 32 / VEC;                     // 32 elements per thread, 512 threads: kMaxD
-    if (threads(1) <= 256) return launch(std::integral_constant<int, 1>(), threads(1));
+    if constexpr (!LONG)
+      if (threads(1) <= 256) return launch(std::integral_constant<int, 1>(), threads(1));
     if (threads(2) <= 256) return launch(std::integral_constant<int, 2>(), threads(2));
     if (kMost > 4 && threads(4) <= 256) return launch(std::integral_constant<int, 4>(), threads(4));
     return launch(std::integral_constant<int, kMost>(), threads(kMost));
@@ -409,7 +411,8 @@ int launch_fwd(aero_ctx* ctx, const FwdArgs& a) {
                                nullptr);
       });
   }
-  return with_block_shape<VEC>(nvec, [&](auto nv, int threads) {
+  static_assert(kFwdLane * 32 == 256, "rows that are left have more than 256 vectors");
+  return with_block_shape<VEC, (VEC > 1)>(nvec, [&](auto nv, int threads) {
     return launch_resident(ctx, rmsnorm_fwd_kernel<T, VEC, decltype(nv)::value>, a, threads, a.T, nullptr);
   });
 }
@@ -417,7 +420,7 @@ int launch_fwd(aero_ctx* ctx, const FwdArgs& a) {
 template <typename T, int VEC>
 int launch_bwd(aero_ctx* ctx, const BwdArgs& a, float* dgamma, int accumulate) {
   int grid = 1;
-  const int rc = with_block_shape<VEC>(a.d / VEC, [&](auto nv, int threads) {
+  const int rc = with_block_shape<VEC, false>(a.d / VEC, [&](auto nv, int threads) {
     return launch_resident(ctx, rmsnorm_bwd_kernel<T, VEC, decltype(nv)::value>, a, threads, a.T < kBwdBlocks ? a.T : kBwdBlocks,
                            &grid);
   });
