@@ -15,14 +15,14 @@ _CTX = {}
 
 def _context():
     """The handle a program keeps for the current device, on the current stream."""
-    device, stream = torch.cuda.current_device(), torch.cuda.current_stream()
-    if device not in _CTX:
+    device = torch.cuda.current_device()
+    ctx = _CTX.get(device)
+    if ctx is None:
         from paper_2602_14338_b200 import binding
 
-        _CTX[device] = binding.Context(device, stream=stream)
-    ctx = _CTX[device]
-    if ctx.stream != stream:
-        ctx.set_stream(stream)
+        ctx = _CTX[device] = binding.Context(device)
+    if ctx.stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device):
+        ctx.set_stream(torch.cuda.current_stream())
     return ctx
 
 
