@@ -525,7 +525,7 @@ int aero_allocate_sim(aero_ctx* ctx, const aero_cfg* cfg, const aero_alloc_cfg* 
  *     rstd [T] -> dx [T,d], dgamma [d] f32, overwritten or, when accumulate_dgamma != 0, added to.
  *     workspace: at least aero_rmsnorm_workspace_bytes(T, d) bytes, 256-byte aligned.
  *   aero_quantize_rows: the 8-bit form of rows x [T,d] as they are (e.g. of W, once per weight).
- * An output may be the same array as an input of its shape and type; other overlaps are not allowed.
+ * An output of [T,d] rows may be the same array as an input of [T,d] rows of its type; other overlaps are not allowed.
  * d up to 16384, any d and any element-aligned base (16-byte aligned rows are faster).
  */
 int aero_rmsnorm_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, const void* x, const void* residual,

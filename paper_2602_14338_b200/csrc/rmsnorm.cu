@@ -466,6 +466,8 @@ int aero_rmsnorm_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, c
   if (rc) return rc;
   if (!ctx || !gamma || !(eps > 0.f) || (q == nullptr) != (q_scale == nullptr)) return AERO_ERR_INVALID;
   if (T > 0 && !sum && !h && !rstd && !q) return AERO_ERR_INVALID;
+  // (other rows still read gamma when a row's statistics are written; fp32 gives the three one type, and T = d one shape)
+  if (cfg->dtype == AERO_FP32 && (gamma == rstd || gamma == q_scale)) return AERO_ERR_INVALID;
   if (T > 0 && !x) return AERO_ERR_INVALID;
   const size_t esz = cfg->dtype == AERO_FP32 ? 4 : 2;
   for (const void* p : {x, residual, gamma, (const void*)sum, (const void*)h})

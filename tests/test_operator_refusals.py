@@ -59,6 +59,14 @@ def test_rmsnorm_refusals(lib, fake):
     assert quant(d=16385) == UNSUPPORTED and quant(x=P + 1) == INVALID
 
 
+def test_statistics_of_the_norm_over_gamma_are_refused(lib, fake):
+    """gamma is read by other rows while a row's rstd and q_scale are written (same type, and same shape where T = d)."""
+    def fwd(gamma, rstd, q, qs):
+        return lib.aero_rmsnorm_fwd(fake, cfg(B.AERO_FP32), 64, 64, 2 * P, None, gamma, 1e-6, None, None, rstd, q, qs)
+
+    assert fwd(P, P, None, None) == INVALID and fwd(P, None, 3 * P, P) == INVALID
+
+
 def test_embed_refusals(lib, fake):
     def fwd(ctx=fake, T=4, d=64, V=10, y=P, W=P, X=P, c=None):
         return lib.aero_embed_fwd(ctx, c or cfg(), T, d, V, y, W, 1.0, X)
