@@ -122,9 +122,10 @@ __device__ __forceinline__ float2 join_states(const float4* xs, long long T, lon
     m = mm;
   }
   const float M = warp_max(m);
-  l = warp_sum(m > -INFINITY ? l * exp2f(m - M) : 0.f);
+  // (a logit that is no number shows in l alone, in m only if it is the largest: l has to come through as it is)
+  l = warp_sum(m > -INFINITY ? l * exp2f(m - M) : l);
   zy = warp_sum(zy);                                   // one split has y's column, the others hold 0
-  if (!(l > 0.f) || M <= lmhead::kMaskedMax2) return make_float2(zy, 0.f);      // a vocabulary of one
+  if (l <= 0.f || (l == l && M <= lmhead::kMaskedMax2)) return make_float2(zy, 0.f);      // a vocabulary of one
   const float a = fmaf(zy, lmhead::kLog2e, -M), big = fmaxf(a, 0.f);
   const float ey = exp2f(a - big), lr = l * exp2f(-big);
   const float lse = (M + big + log2f(lr + ey)) * lmhead::kLn2;
@@ -719,14 +720,14 @@ __global__ void __launch_bounds__(256) fp32_rows_kernel(Fp32Args f) {
     join_rows<NC>(acc, sm, d, f.dH + t * d, false, entry, yt >= 0 ? static_cast<const float*>(a.W) + (long long)yt * d : nullptr);
   } else {
     const float M = warp_max(m);
-    l = warp_sum(m > -INFINITY ? l * expf(m - M) : 0.f);
+    l = warp_sum(m > -INFINITY ? l * expf(m - M) : l);   // (l alone shows a logit that is no number)
     if (lane == 0) state[warp] = make_float2(M, l);
     __syncthreads();
     if (threadIdx.x == 0 && kept) {
       float top = -INFINITY, sum = 0.f;
       for (int w = 0; w < nw; ++w) top = fmaxf(top, state[w].x);
       for (int w = 0; w < nw; ++w)
-        if (state[w].x > -INFINITY) sum += state[w].y * expf(state[w].x - top);
+        sum += state[w].x > -INFINITY ? state[w].y * expf(state[w].x - top) : state[w].y;
       a.lse[t] = top + logf(sum);
     }
   }

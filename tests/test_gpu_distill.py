@@ -273,6 +273,31 @@ def test_rows_of_dropped_rollouts_are_not_looked_at(ctx, dtype):
     assert ctx.last_status() == 0
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("where", ["one column", "a split of columns", "all but the listed ones"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_logit_that_is_no_number_shows_in_every_output(ctx, dtype, where, bad):
+    """Rows of W that nobody lists hold NaN or infinities: the log-sum-exp of every kept row, the loss and the gradients are then
+    no numbers either, wherever in the vocabulary these rows are."""
+    V = 3000 if dtype == "bf16" else 300
+    case = Case(T=150, d=64, V=V, K=5, dtype=dtype, R=4)
+    hit = {"one column": slice(V - 60, V - 59), "a split of columns": slice(V // 3, V // 3 + V // 4), "all but the listed ones": slice(20, V)}[where]
+    case.ids = np.where(case.ids >= 0, case.ids % 20, case.ids).astype(np.int32)
+    dv, _ = case.device()
+    dv["W"][hit] = bad
+    kept = torch.from_numpy(case.keep[np.searchsorted(case.cs, np.arange(case.T), side="right") - 1] != 0).cuda()
+    fwd = ctx.distill_fwd(case.cfg, **dv)
+    out, dH, dW = ctx.distill_fwd_bwd(case.cfg, **dv)
+    dH2, dW2 = ctx.distill_bwd(case.cfg, **dv, lse=fwd["lse"])
+    for o in (fwd, out):
+        assert not torch.isfinite(o["lse"][kept]).any() and not o["lse"][~kept].any()
+        assert not torch.isfinite(o["loss"]).any()
+    for h, w in ((dH, dW), (dH2, dW2)):
+        assert not torch.isfinite(h[0]).any() and not h[~kept].any()      # (row 0 has a full list)
+        assert not torch.isfinite(w[hit]).all(dim=1).any()
+    assert ctx.last_status() & ~B.AERO_ST_RANGE == 0
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_rows_that_no_rollout_owns(ctx, dtype):
     """Rows before the first offset and behind the last one come out as zeros."""
