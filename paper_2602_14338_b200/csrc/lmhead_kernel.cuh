@@ -161,7 +161,8 @@ __device__ __forceinline__ void finish_rows(const Params& p, bool ent_mode, bool
   double part[kPartialStride] = {0.0, 0.0, 0.0, 0.0, 0.0};
   if (live) {
     float ls, lp, ent = 0.f;
-    const bool others = l > 0.f && m2 > kMaskedMax2;       // (a vocabulary of one: no other column)
+    // (a vocabulary of one: no other column; a sum that is no number stays one, whatever the maximum has seen)
+    const bool others = !(l <= 0.f || (l == l && m2 <= kMaskedMax2));
     if (others) {
       const float a = fmaf(zy, kLog2e, -m2);               // the target's exponent relative to m2
       const float big = fmaxf(a, 0.f);                     // everything below is scaled by 2^-big: no overflow

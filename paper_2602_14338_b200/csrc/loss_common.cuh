@@ -32,5 +32,6 @@ __device__ __forceinline__ SurrogateOut aero_surrogate(float logp, float old_log
   const bool unclipped = a <= b;
   o.g = unclipped ? -w * A * o.rho : 0.f;
   o.clipped = (!unclipped && A != 0.f) ? 1.f : 0.f;
+  if (o.rho != o.rho) { o.s = o.g = o.rho; o.clipped = 0.f; }      // no number: min, max and <= would make one of it
   return o;
 }

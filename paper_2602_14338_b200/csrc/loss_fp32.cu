@@ -72,7 +72,7 @@ fwd_fp32_kernel(aero_cfg cfg, long long T, int d, int V, int R,
     if (lane == 0) {
       const float zy = dot_row(h, W + (size_t)yt * d, d);
       float ls = zy, lp = 0.f, ent = 0.f;         // (a vocabulary of one: p_y = 1)
-      if (l > 0.f) {
+      if (!(l <= 0.f)) {                          // (a sum that is no number stays one)
         const float a = zy - M, big = fmaxf(a, 0.f);
         const float ey = expf(a - big), lr = l * expf(-big);
         ls = M + big + logf(lr + ey);

@@ -587,6 +587,37 @@ def test_rows_out_of_range_in_every_split_are_listed_once(ctx, rowscale):
     assert (np.abs(dW.double().cpu().numpy() - dz.T @ h) <= tol_w).all()
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,vsplit", [("bf16", 0), ("bf16", 4), ("fp32", 0)])
+def test_a_logit_that_is_no_number_shows_in_the_outputs(ctx, dtype, vsplit, bad):
+    """A row of W that is no target holds NaN or infinities: log-prob, log-sum-exp, loss and gradients are no numbers either."""
+    T, d, V, R = 200, 64, 3000 if dtype == "bf16" else 300, 4
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator().manual_seed(8)
+    H, W = torch.randn(T, d, generator=g).to(dt).cuda(), (torch.randn(V, d, generator=g) * 0.05).to(dt).cuda()
+    W[V - 60] = bad
+    y = torch.randint(0, V - 100, (T,), generator=g).int().cuda()
+    cs = torch.arange(0, T + 1, T // R, dtype=torch.int64, device="cuda")
+    adv = torch.tensor([1.0, -0.5, 0.7, -1.0], device="cuda")
+    w, keep = torch.full((R,), 1.0 / T, device="cuda"), torch.ones(R, dtype=torch.uint8, device="cuda")
+    old = torch.full((T,), -8.0, device="cuda")
+    cfg = TL.lib_cfg(O.Cfg(), dtype)
+    none = lambda t: not torch.isfinite(t.float()).any()
+    ctx.set_tuning(vsplit=vsplit)
+    try:
+        lp = ctx.logprob_fwd(cfg, H, W, y)
+        f = ctx.grpo_loss_fwd(cfg, H, W, y, old, cs, adv, w, keep)
+        dH, dW = ctx.grpo_loss_bwd(cfg, H, W, y, cs, keep, f["lse"], f["g"], logp=f["logp"])
+        f1, dH1, dW1 = ctx.grpo_loss_fwd_bwd(cfg, H, W, y, old, cs, adv, w, keep)
+    finally:
+        ctx.set_tuning()
+    assert none(lp["logp"][:T]) and none(lp["lse"][:T])
+    for o in (f, f1):
+        assert none(o["logp"][:T]) and none(o["lse"][:T]) and none(o["g"][:T]) and none(o["loss"])
+    assert none(dH) and none(dH1) and none(dW[V - 60]) and none(dW1[V - 60])
+    assert ctx.last_status() & ~B.AERO_ST_RANGE == 0
+
+
 def _row_err(a, b, rows):
     """Relative L2 error of each listed row of a against b."""
     a, b = np.asarray(a, np.float64)[rows], np.asarray(b, np.float64)[rows]
