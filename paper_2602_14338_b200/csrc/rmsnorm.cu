@@ -50,14 +50,15 @@ struct BwdArgs {
 };
 
 // Block shapes: at most 256 threads while few vectors per thread suffice, so that several rows are in flight on
-// an SM; the largest vector count of a kind goes up to kMaxD.
+// an SM; the largest vector count of a kind goes up to kMaxD.  In the backward that form holds two rows, their next ones and
+// dgamma's share and spills 0.7 to 1.5 KB a thread (8192 x 8192 bf16: 202 us, its bytes alone 82).
 template <int VEC, int NV>
 constexpr int max_threads() {
   return VEC == 1 ? 1024 : (NV * VEC == 32 ? 512 : 256);
 }
 // Blocks per SM the compiler is to make room for.  Measured (us; 1 / 2 / 3 / 4 / 5 blocks asked for): forward, 16384 x 3584 bf16
 // with a residual 89 / 89 / 79 / 110 / 177; backward, 20011 x 1536 bf16 59 / 59 / 57 / 54 / 67, 16384 x 3584 118 / 94 / 143 / 141
-// / 223: the registers are worth more than the blocks once rows have to be spilled.  fp32 rows are best left alone.
+// / 223: the registers are worth more than the blocks once rows have to be spilled.  fp32 rows: one block, others not measured.
 template <int VEC, int NV>
 constexpr int fwd_blocks() { return VEC == 8 && NV == 2 ? 3 : 1; }
 template <int VEC, int NV>
