@@ -506,6 +506,58 @@ def test_captured_and_replayed(ctx):
     c.close()
 
 
+def test_separate_calls_captured_and_replayed(ctx):
+    """The forward and the backward of its lse in one graph, with rows the student is sure of, replayed on other contents."""
+    side = torch.cuda.Stream()
+    c = B.Context(0, stream=side)
+    case = SureCase(3, "bf16")
+    dv, _ = case.device()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        lse = c.distill_fwd(case.cfg, **dv)["lse"]
+        c.distill_bwd(case.cfg, **dv, lse=lse)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        out = c.distill_fwd(case.cfg, **dv)
+        dH, dW = c.distill_bwd(case.cfg, **dv, lse=out["lse"])
+    for turn in (1, 2):
+        dv["H"].copy_(dv["H"].roll(7 * turn, 0))
+        dv["logits"].mul_(0.9)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want = ctx.distill_fwd(case.cfg, **dv)
+        wH, wW = ctx.distill_bwd(case.cfg, **dv, lse=want["lse"])
+        assert torch.equal(out["lse"], want["lse"]) and torch.equal(out["loss"], want["loss"])
+        assert torch.equal(dH, wH) and torch.equal(dW, wW)
+    assert c.last_status() == 0
+    del g
+    c.close()
+
+
+def test_two_calls_at_once(ctx):
+    """Two contexts on two streams, their calls under way at the same time: the same bits as one after the other."""
+    cases = [Case(T=300, d=192, V=5000, K=9, R=4), Case(T=700, d=256, V=3000, K=20, R=6)]
+    inputs = [c.device()[0] for c in cases]
+    want = [ctx.distill_fwd_bwd(c.cfg, **dv) for c, dv in zip(cases, inputs)]
+    side = [torch.cuda.Stream(), torch.cuda.Stream()]
+    own = [B.Context(0, stream=s) for s in side]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(4):
+        for i in (0, 1):
+            with torch.cuda.stream(side[i]):
+                got[i].append(own[i].distill_fwd_bwd(cases[i].cfg, **inputs[i]))
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for o, dH, dW in got[i]:
+            assert torch.equal(o["kl"], want[i][0]["kl"]) and torch.equal(o["loss"], want[i][0]["loss"])
+            assert torch.equal(dH, want[i][1]) and torch.equal(dW, want[i][2])
+        assert own[i].last_status() == 0
+        own[i].close()
+
+
 def test_with_stage_b_in_one_process(ctx):
     """Stage (b) and the distillation share kernels, whichever of them a process runs first: the log-prob pass and the
     three calls of the loss, the distillation's, and the first again, each with the same bits as before."""
