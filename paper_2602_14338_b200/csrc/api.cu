@@ -7,7 +7,7 @@
 
 extern "C" {
 
-int aero_version(void) { return 103; }
+int aero_version(void) { return 104; }
 
 const char* aero_error_string(int code) {
   switch (code) {
