@@ -78,7 +78,7 @@ def draw(rng):
             return dict(op=op, grads=rng.random() < 0.7, T=T, R=rng.randint(2, min(T, 10)), kind=kind, mean=mean, dtype="fp32",
                         d=rng.randint(8, 96), V=rng.randint(100, 900))
         d, V = rng.choice([SMALL, LARGE, (64 * rng.randint(1, 64), _log_int(rng, 600, LARGE[1]))])
-        T = _log_int(rng, 16, 4096 * LARGE[0] // max(d, LARGE[0]))
+        T = _log_int(rng, 16, 3000 * LARGE[0] // max(d, LARGE[0]))
         return dict(op=op, grads=rng.random() < 0.7, T=T, R=rng.randint(2, min(T, 24)), kind=kind, mean=mean, dtype="bf16", d=d, V=V)
     if op == "adamw":
         if rng.random() < 0.5:          # many small tensors
