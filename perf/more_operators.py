@@ -85,7 +85,7 @@ def draw(rng):
             count = rng.randint(2, 200)
             numel = small = _log_int(rng, 1, 100000)
         else:                           # one large tensor and a few small ones
-            count, numel, small = rng.randint(1, 4), _log_int(rng, 100000, SMALL[0] * SMALL[1]), rng.randint(1, 9000)
+            count, numel, small = rng.randint(1, 4), _log_int(rng, 100000, 160 * 10 ** 6), rng.randint(1, 9000)
         return dict(op=op, bits=rng.choice([8, 32]), numel=numel, count=count, small=small, param=rng.choice(["bf16", "fp32"]),
                     grad=rng.choice(["bf16", "fp32"]))
     block = rng.choice([16, 32])
