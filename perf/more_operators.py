@@ -45,17 +45,17 @@ def listed():
         # an ordinary micro-batch of the large policy, loss and gradients, log-probs averaged over a rollout's tokens
         dict(name="preference step 4096", op="pref", grads=True, T=4096, R=16, kind="square", mean=True, dtype="bf16", **big),
         # the norms and biases of the small policy, updated in full precision
-        dict(name="adamw 32 bits, 60 tensors", op="adamw", bits=32, numel=1536, count=60, small=1536, param="fp32", grad="fp32"),
+        dict(name="adamw 32 bits 60 tensors", op="adamw", bits=32, numel=1536, count=60, small=1536, param="fp32", grad="fp32"),
         # an adapter of the large policy: bf16 weights with their fp32 master
-        dict(name="adamw 32 bits, adapters", op="adamw", bits=32, numel=3584 * 64, count=40, small=64 * 1537, param="bf16",
+        dict(name="adamw 32 bits adapters", op="adamw", bits=32, numel=3584 * 64, count=40, small=64 * 1537, param="bf16",
              grad="bf16"),
         # the tied weight of the small policy and its final norm, states in 8 bits
-        dict(name="adamw 8 bits, tied weight", op="adamw", bits=8, numel=SMALL[0] * SMALL[1], count=2, small=1536, param="bf16",
+        dict(name="adamw 8 bits tied weight", op="adamw", bits=8, numel=SMALL[0] * SMALL[1], count=2, small=1536, param="bf16",
              grad="bf16"),
         # final hidden states of a batch of sequences being decoded, to 4 bits and back
-        dict(name="4 bits there and back, 61 rows", op="fp4_rows", T=61, d=SMALL[0], block=16, dtype="bf16"),
+        dict(name="4 bits and back 61 rows", op="fp4_rows", T=61, d=SMALL[0], block=16, dtype="bf16"),
         # the lm_head weight of the large policy, once per weight, and read back
-        dict(name="4 bits there and back, lm_head", op="fp4_rows", T=LARGE[1], d=LARGE[0], block=16, dtype="bf16"),
+        dict(name="4 bits and back lm_head", op="fp4_rows", T=LARGE[1], d=LARGE[0], block=16, dtype="bf16"),
         # next-token logits of one sequence
         dict(name="product 4 bits 1", op="fp4", T=1, out="fp32", block=16, **big),
         # next-token logits of a batch of sequences being decoded, in the format with a power of two per 32
