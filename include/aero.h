@@ -620,6 +620,62 @@ int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int
 int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t* h8, const float* h_scale,
                    const int8_t* w8, const float* w_scale, int32_t out_dtype, void* out);
 
+/* One AdamW step over many tensors (the weights, norms and biases that dW and dgamma above are the gradients of).
+ * With g' = grad_scale clip g, clip = min(1, max_norm / (norm + 1e-6)), norm the 2-norm of grad_scale g over all tensors
+ * (max_norm <= 0: no clipping), and t the number of this step, per element:
+ *   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+ *   p = (1 - lr_i weight_decay_i) p - lr_i (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),   lr_i = lr lr_scale_i
+ * Tensors are described by an array in HOST memory, which is read before the call returns; no tensor may occur twice.
+ *   param [n] bf16 or fp32, updated in place; with master [n] f32 (bf16 parameters only) the master is updated and param
+ *   is its rounding, without it a bf16 param is rounded after each step.  grad [n] bf16 or fp32, read only.
+ *   state_bits 32: m, v [n] f32.
+ *   state_bits 8: m [n] e4m3, v [n] the root of v as an unsigned float of 4 exponent (bias 7) and 4 mantissa bits
+ *     (code c: (16 + c % 16) 2^(c / 16 - 11), below code 16 c 2^-10), each times a scale per 256 elements:
+ *     m_scale, v_scale [ceil(n / 256)] f32, the block's largest value over 448 and 496 (at least 2^-100 over these).
+ *     Rounded to even; a root that is not zero keeps at least code 1.  All-zero states (codes and scales) are those before
+ *     the first step.  A NaN or an infinity in a block makes all of the block's states NaN.
+ *   Any n and any element-aligned base (16-byte aligned tensors are faster).  A tensor with n = 0 is left out.
+ * step [1] i64 (device): the number of steps taken; the call adds one and uses the sum as t, so a captured call counts
+ *   on when it is replayed.  lr [1] f32 (device) in place of cfg's lr, or NULL.
+ * skip_nonfinite != 0: if the norm is infinite or NaN, tensors and step are left as they are.
+ * stats [4] f32 (device) or NULL: norm (0 if neither clipping nor skip_nonfinite asks for it), clip, 1 if skipped, t.
+ * Arithmetic in fp32, the norm's sum in 64 bits and in a fixed order: repeated calls give the same bits.
+ * workspace: at least aero_adamw_workspace_bytes(n_tensors) bytes, 256-byte aligned.
+ * aero_adamw_states: the states as numbers, in out_dtype (AERO_BF16 | AERO_FP32): m_out[i], v_out[i] (arrays of device
+ *   pointers in host memory; either may be NULL) of n elements of tensor i.  Only n, m, v, their scales and state_bits are read.
+ */
+typedef struct aero_adamw_cfg {
+  double beta1, beta2;     /* default 0.9, 0.999; in [0, 1).  (In fp32 1 - 0.999 would be 1e-5 off.) */
+  float lr;                /* default 1e-3  */
+  float eps;               /* default 1e-8  */
+  float max_norm;          /* default 0: no clipping */
+  float grad_scale;        /* default 1: gradients are multiplied by it first (1 / a loss scale, 1 / micro-batches) */
+  int32_t skip_nonfinite;  /* default 0 */
+} aero_adamw_cfg;
+
+typedef struct aero_adamw_tensor {
+  int64_t n;
+  void* param;
+  const void* grad;
+  float* master;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  int32_t param_dtype;     /* AERO_BF16 | AERO_FP32 */
+  int32_t grad_dtype;
+  int32_t state_bits;      /* 8 | 32 */
+  float weight_decay;
+  float lr_scale;
+} aero_adamw_tensor;
+
+void aero_adamw_cfg_default(aero_adamw_cfg* ac);
+size_t aero_adamw_workspace_bytes(int32_t n_tensors);
+int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, const aero_adamw_tensor* tensors,
+                    int64_t* step, const float* lr, float* stats, void* workspace, size_t workspace_bytes);
+int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor* tensors, int32_t out_dtype, void* const* m_out,
+                      void* const* v_out);
+
 /* Optional timing of the dominant kernel.  With timing on, aero_grpo_loss_fwd_bwd records a pair of
  * CUDA events on the context's stream around each launch of its lm_head kernel (up to 256 launches
  * between read-outs; the events are created on first use).  aero_kernel_timing_ms synchronises the

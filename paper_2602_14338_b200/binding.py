@@ -38,6 +38,7 @@ EXPORTS = [
     "aero_embed_fwd", "aero_embed_bwd", "aero_embed_workspace_bytes", "aero_lmhead_q8",
     "aero_distill_fwd", "aero_distill_bwd", "aero_distill_fwd_bwd", "aero_distill_fwd_workspace_bytes",
     "aero_distill_bwd_workspace_bytes", "aero_distill_fwd_bwd_workspace_bytes",
+    "aero_adamw_cfg_default", "aero_adamw_workspace_bytes", "aero_adamw_step", "aero_adamw_states",
 ]
 
 
@@ -55,6 +56,17 @@ class AeroCfg(C.Structure):
 
 class AeroAllocCfg(C.Structure):
     _fields_ = [("n_extra", C.c_int32), ("k_max", C.c_int32), ("n_max", C.c_int32), ("n_budget", C.c_int32)]
+
+
+class AeroAdamWCfg(C.Structure):
+    _fields_ = [("beta1", C.c_double), ("beta2", C.c_double), ("lr", C.c_float), ("eps", C.c_float), ("max_norm", C.c_float),
+                ("grad_scale", C.c_float), ("skip_nonfinite", C.c_int32)]
+
+
+class AeroAdamWTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("param", C.c_void_p), ("grad", C.c_void_p), ("master", C.c_void_p), ("m", C.c_void_p),
+                ("v", C.c_void_p), ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("param_dtype", C.c_int32),
+                ("grad_dtype", C.c_int32), ("state_bits", C.c_int32), ("weight_decay", C.c_float), ("lr_scale", C.c_float)]
 
 
 class AeroError(RuntimeError):
@@ -140,6 +152,13 @@ def load_library():
     lib.aero_distill_fwd.argtypes = shape + [vp] * 12 + [vp, sz]
     lib.aero_distill_bwd.argtypes = shape + [vp] * 9 + [f32, vp, vp, i32, C.c_int, vp, sz]
     lib.aero_distill_fwd_bwd.argtypes = shape + [vp] * 12 + [f32, vp, vp, i32, C.c_int, vp, sz]
+    ap, tp = C.POINTER(AeroAdamWCfg), C.POINTER(AeroAdamWTensor)
+    lib.aero_adamw_cfg_default.restype = None
+    lib.aero_adamw_cfg_default.argtypes = [ap]
+    lib.aero_adamw_workspace_bytes.restype = sz
+    lib.aero_adamw_workspace_bytes.argtypes = [i32]
+    lib.aero_adamw_step.argtypes = [vp, ap, i32, tp, vp, vp, vp, vp, sz]
+    lib.aero_adamw_states.argtypes = [vp, i32, tp, i32, C.POINTER(vp), C.POINTER(vp)]
     lib.aero_launch_count.restype = C.c_int64
     lib.aero_launch_count.argtypes = [vp]
     _lib = lib
@@ -170,6 +189,74 @@ def alloc_cfg_default(**over) -> AeroAllocCfg:
             raise AttributeError(k)
         setattr(ac, k, v)
     return ac
+
+
+def adamw_cfg_default(**over) -> AeroAdamWCfg:
+    ac = AeroAdamWCfg()
+    load_library().aero_adamw_cfg_default(C.byref(ac))
+    for k, v in over.items():
+        if not hasattr(ac, k):
+            raise AttributeError(k)
+        setattr(ac, k, v)
+    return ac
+
+
+class AdamWPlan:
+    """The tensors of Context.adamw_step, checked and described once: a list of dicts with param, grad, m and v and, where they
+    apply, master (fp32 master of a bf16 param), m_scale and v_scale (8-bit states), weight_decay (0) and lr_scale (1).  States
+    are fp32, or m in torch.float8_e4m3fn and v in torch.uint8 with a scale per 256 elements.  The plan keeps the tensors; a
+    program whose gradients move makes another one."""
+
+    _DTYPES = {torch.bfloat16: AERO_BF16, torch.float32: AERO_FP32}
+
+    def __init__(self, tensors):
+        self.tensors = [dict(t) for t in tensors]
+        self.device = None
+        self.array = (AeroAdamWTensor * max(1, len(self.tensors)))()
+        written = set()
+        for i, t in enumerate(self.tensors):
+            unknown = set(t) - {"param", "grad", "master", "m", "v", "m_scale", "v_scale", "weight_decay", "lr_scale"}
+            if unknown:
+                raise AeroError(f"tensor {i}: unknown {sorted(unknown)}")
+            n = t["param"].numel()
+            bits = 32 if t["m"].dtype == torch.float32 else 8
+            want = dict(param=(n, tuple(self._DTYPES)), grad=(n, tuple(self._DTYPES)), master=(n, (torch.float32,)))
+            if bits == 32:
+                want.update(m=(n, (torch.float32,)), v=(n, (torch.float32,)))
+            else:
+                blocks = (n + 255) // 256
+                want.update(m=(n, (torch.float8_e4m3fn,)), v=(n, (torch.uint8,)), m_scale=(blocks, (torch.float32,)),
+                            v_scale=(blocks, (torch.float32,)))
+            for name in ("master", "m_scale", "v_scale"):
+                if t.get(name) is None:
+                    if name in want and name != "master":
+                        raise AeroError(f"tensor {i}: 8-bit states need {name}")
+                    want.pop(name, None)
+            if "master" in want and t["param"].dtype != torch.bfloat16:
+                raise AeroError(f"tensor {i}: only a bf16 param has a master")
+            d = self.array[i]
+            for name, (size, dtypes) in want.items():
+                x = t[name]
+                if not x.is_cuda or not x.is_contiguous():
+                    raise AeroError(f"tensor {i}: {name} must be a contiguous CUDA tensor")
+                if x.dtype not in dtypes:
+                    raise AeroError(f"tensor {i}: {name} must have dtype {' or '.join(map(str, dtypes))}, got {x.dtype}")
+                if x.numel() != size:
+                    raise AeroError(f"tensor {i}: {name} must have {size} elements, got {x.numel()}")
+                self.device = self.device if self.device is not None else x.device
+                if x.device != self.device:
+                    raise AeroError(f"tensor {i}: {name} is on {x.device}, others on {self.device}")
+                if name != "grad" and size > 0:
+                    if x.data_ptr() in written:
+                        raise AeroError(f"tensor {i}: {name} occurs twice")
+                    written.add(x.data_ptr())
+                setattr(d, name, x.data_ptr())
+            d.n, d.state_bits = n, bits
+            d.param_dtype, d.grad_dtype = self._DTYPES[t["param"].dtype], self._DTYPES[t["grad"].dtype]
+            d.weight_decay, d.lr_scale = t.get("weight_decay", 0.0), t.get("lr_scale", 1.0)
+
+    def __len__(self):
+        return len(self.tensors)
 
 
 def _ptr(t, dtype=None, numel=None, name="tensor"):
@@ -607,6 +694,39 @@ class Context:
                                      self._arg(o, out_dtype, (T, V), "out"))
         _check(rc, "aero_lmhead_q8")
         return o
+
+    # ---- AdamW over many tensors ---------------------------------------------------------------
+    def _plan(self, plan):
+        if plan.device is not None and plan.device != self.device:
+            raise AeroError(f"the plan's tensors must be on {self.device}, got {plan.device}")
+
+    def adamw_step(self, ac, plan, step, lr=None, stats=None):
+        """aero_adamw_step: updates the plan's tensors and step [1] int64 (device) in place; lr [1] f32 (device) in place of
+        ac.lr.  Returns stats [4]: norm, clip, 1 if skipped, number of the step."""
+        self._plan(plan)
+        stats = stats if stats is not None else self._new((4,), torch.float32)
+        ws = self._scratch(self.lib.aero_adamw_workspace_bytes(len(plan)))
+        _check(self.lib.aero_adamw_step(self.h, C.byref(ac), len(plan), plan.array, self._arg(step, torch.int64, (1,), "step"),
+                                        self._arg(lr, torch.float32, (1,), "lr"), self._arg(stats, torch.float32, (4,), "stats"),
+                                        ws.data_ptr(), ws.numel()), "aero_adamw_step")
+        return stats
+
+    def adamw_states(self, plan, m=None, v=None, out_dtype=torch.bfloat16):
+        """aero_adamw_states: (m, v) of the plan's tensors as numbers, two lists of flat tensors (made unless given)."""
+        self._plan(plan)
+        if out_dtype not in AdamWPlan._DTYPES:
+            raise AeroError(f"out_dtype must be torch.bfloat16 or torch.float32, got {out_dtype}")
+        made, arrays = [], []
+        for name, given in (("m", m), ("v", v)):
+            if given is None:
+                given = [self._new((t["param"].numel(),), out_dtype) for t in plan.tensors]
+            if len(given) != len(plan):
+                raise AeroError(f"{name} must hold {len(plan)} tensors, got {len(given)}")
+            made.append(given)
+            arrays.append((C.c_void_p * max(1, len(plan)))(*[
+                self._arg(x, out_dtype, (t["param"].numel(),), f"{name}[{i}]") for i, (x, t) in enumerate(zip(given, plan.tensors))]))
+        _check(self.lib.aero_adamw_states(self.h, len(plan), plan.array, AdamWPlan._DTYPES[out_dtype], *arrays), "aero_adamw_states")
+        return made[0], made[1]
 
     # ---- distillation from a teacher's top logits --------------------------------------------
     def _distill_inputs(self, cfg, H, W, ids, logits, teacher_lse, cs, w, keep):

@@ -1,0 +1,497 @@
+// One AdamW step over many tensors.  Per element, with g' = grad_scale clip g and t the number of this step:
+//   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
+//   p = (1 - lr wd) p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+// m and v are fp32, or 8 bits an element with a scale per 256 elements: m as e4m3, the root of v as an unsigned float of
+// four exponent and four mantissa bits (v spans twice as many octaves as m; its root fits the same range, and the sign's bit
+// goes to the mantissa).  The step itself uses the fp32 values before they are rounded.  Bound by memory: 28 bytes an element
+// in fp32, 16 with 8-bit states, a bf16 gradient and a bf16 parameter with its fp32 master; each is read and written once, by one
+// launch for up to 128 tensors.  The tensors' addresses travel in the kernel's parameters, so that nothing is copied to the device.
+#include "entry.cuh"
+#include "vec.cuh"
+
+#include <cuda_fp8.h>
+
+namespace {
+
+constexpr int kSlots = 128;             // tensors per launch
+constexpr int kBlock = 256;             // elements per scale of the 8-bit states; a warp's share of a tensor at a time
+constexpr int kWarps = 8, kChunk = kWarps * kBlock, kEach = kBlock / 32;
+constexpr int kMaxBlocks = 2048;        // of a launch
+constexpr float kTopM = 448.f, kTopV = 496.f;          // largest values of the two 8-bit formats
+constexpr float kLeast = 0x1p-100f;     // scales are made of at least this: 448 / it stays finite
+
+enum : uint32_t { kParam16 = 1, kGrad16 = 2, kState8 = 4, kAligned = 8, kOut16 = 16 };
+
+struct Slot {
+  long long n;
+  void* param;
+  const void* grad;
+  float* master;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  float weight_decay, lr_scale;
+  uint32_t flags;
+};
+struct Table {
+  int count;
+  long long chunk0[kSlots + 1];         // first chunk of each tensor among those of the launch
+  Slot slot[kSlots];
+};
+
+// What the step's kernels share, in the workspace: made of the gradients' norm and the step's number.
+struct Scalars {
+  float g_factor;                       // grad_scale clip
+  float lr, c1, c2;                     // 1 / (1 - beta^t)
+  int skip;
+};
+
+struct Hyper {
+  float beta1, beta2, rest1, rest2, eps;      // rest = 1 - beta
+};
+
+__device__ __forceinline__ int slot_of(const Table& t, long long chunk) {
+  int lo = 0, hi = t.count;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (t.chunk0[mid] <= chunk) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// A warp's 256 elements from e0 on: eight neighbours a lane where every array of the tensor is made of whole 16-byte vectors,
+// else every 32nd element from the lane's own, as far as the tensor goes.
+struct Span {
+  long long e0;
+  int left;                             // elements from e0 to the tensor's end
+  bool vec;
+  int lane;
+  __device__ bool has(int i) const { return vec || i * 32 + lane < left; }
+  __device__ long long at(int i) const { return e0 + i * 32 + lane; }
+  __device__ long long first() const { return e0 + lane * kEach; }
+};
+
+__device__ __forceinline__ void load32(const float* p, const Span& s, float (&x)[kEach]) {
+  if (s.vec) {
+    const float4 a = reinterpret_cast<const float4*>(p + s.first())[0], b = reinterpret_cast<const float4*>(p + s.first())[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = s.has(i) ? p[s.at(i)] : 0.f;
+  }
+}
+__device__ __forceinline__ void load16(const __nv_bfloat16* p, const Span& s, float (&x)[kEach]) {
+  if (s.vec) {
+    rowvec::load<__nv_bfloat16, 8>(p + s.first(), x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) x[i] = s.has(i) ? __bfloat162float(p[s.at(i)]) : 0.f;
+  }
+}
+__device__ __forceinline__ void load(const void* p, bool half, const Span& s, float (&x)[kEach]) {
+  if (half) load16(static_cast<const __nv_bfloat16*>(p), s, x);
+  else load32(static_cast<const float*>(p), s, x);
+}
+__device__ __forceinline__ void store32(float* p, const Span& s, const float (&x)[kEach]) {
+  if (s.vec) {
+    reinterpret_cast<float4*>(p + s.first())[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p + s.first())[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (s.has(i)) p[s.at(i)] = x[i];
+  }
+}
+__device__ __forceinline__ void store16(__nv_bfloat16* p, const Span& s, const float (&x)[kEach]) {
+  if (s.vec) {
+    rowvec::store<__nv_bfloat16, 8>(p + s.first(), x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (s.has(i)) p[s.at(i)] = __float2bfloat16_rn(x[i]);
+  }
+}
+__device__ __forceinline__ void store(void* p, bool half, const Span& s, const float (&x)[kEach]) {
+  if (half) store16(static_cast<__nv_bfloat16*>(p), s, x);
+  else store32(static_cast<float*>(p), s, x);
+}
+__device__ __forceinline__ void load_codes(const uint8_t* p, const Span& s, uint8_t (&c)[kEach]) {
+  if (s.vec) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p + s.first());
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      c[i] = (uint8_t)(u.x >> (8 * i));
+      c[4 + i] = (uint8_t)(u.y >> (8 * i));
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) c[i] = s.has(i) ? p[s.at(i)] : 0;
+  }
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, const Span& s, const uint8_t (&c)[kEach]) {
+  if (s.vec) {
+    uint2 u = make_uint2(0, 0);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u.x |= (uint32_t)c[i] << (8 * i);
+      u.y |= (uint32_t)c[4 + i] << (8 * i);
+    }
+    *reinterpret_cast<uint2*>(p + s.first()) = u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (s.has(i)) p[s.at(i)] = c[i];
+  }
+}
+
+// Largest magnitude of the warp's elements; compared as bits, so that a NaN is larger than all and comes through.
+__device__ __forceinline__ float warp_top(const float (&x)[kEach]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+}
+// What a block's scale is made of: its largest magnitude, or NaN where that is no finite number.
+__device__ __forceinline__ float scale_top(float top) {
+  return top < INFINITY ? fmaxf(top, kLeast) : __uint_as_float(0x7fffffffu);
+}
+
+__device__ __forceinline__ void open_m(const Slot& t, const Span& s, float (&m)[kEach]) {
+  uint8_t c[kEach];
+  load_codes(static_cast<const uint8_t*>(t.m), s, c);
+  const float scale = t.m_scale[s.e0 / kBlock];
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) {
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[i] | c[i + 1] << 8), __NV_E4M3);
+    const float2 f = __half22float2(__half2(h));
+    m[i] = f.x * scale;
+    m[i + 1] = f.y * scale;
+  }
+}
+__device__ __forceinline__ void close_m(const Slot& t, const Span& s, const float (&m)[kEach]) {
+  const float top = scale_top(warp_top(m)), inv = kTopM / top;
+  uint8_t c[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) {
+    const __nv_fp8x2_storage_t u = __nv_cvt_float2_to_fp8x2(make_float2(m[i] * inv, m[i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+    c[i] = (uint8_t)u;
+    c[i + 1] = (uint8_t)(u >> 8);
+  }
+  store_codes(static_cast<uint8_t*>(t.m), s, c);
+  if (s.lane == 0) t.m_scale[s.e0 / kBlock] = top / kTopM;
+}
+// The root's codes are the upper bits of a float whose exponent is moved by 120, so that the smallest normal numbers of the
+// two formats fall together and the subnormal ones do too.
+__device__ __forceinline__ void open_v(const Slot& t, const Span& s, float (&v)[kEach]) {
+  uint8_t c[kEach];
+  load_codes(static_cast<const uint8_t*>(t.v), s, c);
+  const float scale = t.v_scale[s.e0 / kBlock];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const float r = __uint_as_float((uint32_t)c[i] << 19) * 0x1p120f * scale;
+    v[i] = r * r;
+  }
+}
+__device__ __forceinline__ void close_v(const Slot& t, const Span& s, const float (&v)[kEach]) {
+  float r[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) r[i] = sqrtf(v[i]);
+  const float top = scale_top(warp_top(r)), inv = kTopV / top;
+  uint8_t c[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const uint32_t b = __float_as_uint(r[i] * inv * 0x1p-120f);
+    uint32_t code = min((b + 0x3ffffu + ((b >> 19) & 1u)) >> 19, 255u);      // to even
+    if (r[i] > 0.f) code = max(code, 1u);           // a root that is not zero divides the step: it does not become zero
+    c[i] = (uint8_t)code;
+  }
+  store_codes(static_cast<uint8_t*>(t.v), s, c);
+  if (s.lane == 0) t.v_scale[s.e0 / kBlock] = top / kTopV;
+}
+
+// The warps' spans of a launch, chunk by chunk.
+template <typename F>
+__device__ __forceinline__ void for_spans(const Table& tab, F&& f) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  for (long long c = blockIdx.x; c < tab.chunk0[tab.count]; c += gridDim.x) {
+    const int k = slot_of(tab, c);
+    const Slot& t = tab.slot[k];
+    const long long e0 = (c - tab.chunk0[k]) * kChunk + warp * kBlock, left = t.n - e0;
+    if (left <= 0) continue;
+    f(t, Span{e0, (int)(left < kBlock ? left : kBlock), (t.flags & kAligned) && left >= kBlock, lane});
+  }
+}
+
+// Sum of the gradients' squares, one record per block: eight squares at a time in fp32, then in 64 bits.  Groups whose sum
+// leaves the range in which fp32 holds squares are taken in 64 bits from the start.
+__global__ void __launch_bounds__(kWarps * 32) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partials) {
+  __shared__ double sh[kWarps];
+  double sum = 0.0;
+  for_spans(tab, [&](const Slot& t, const Span& s) {
+    float g[kEach];
+    load(t.grad, t.flags & kGrad16, s, g);
+    float q = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) q = fmaf(g[i], g[i], q);
+    if (q > 0x1p-80f && q < 0x1p120f) {
+      sum += q;
+    } else {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) sum += (double)g[i] * g[i];
+    }
+  });
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kWarps; ++w) sum += sh[w];
+    partials[blockIdx.x] = sum;
+  }
+}
+
+struct PrepareArgs {
+  const double* partials;               // NULL: no norm
+  int n_partials;
+  double beta1, beta2;
+  float lr, max_norm, grad_scale;
+  int skip_nonfinite;
+  const float* lr_dev;
+  long long* step;
+  float* stats;
+  Scalars* out;
+};
+__global__ void __launch_bounds__(256) adamw_prepare_kernel(PrepareArgs a) {
+  __shared__ double sh[8];
+  double sum = 0.0;
+  if (a.partials)
+    for (int i = threadIdx.x; i < a.n_partials; i += 256) sum += a.partials[i];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 8; ++w) sum += sh[w];
+  const double norm = sqrt(sum) * fabs((double)a.grad_scale);
+  double clip = 1.0;
+  if (a.max_norm > 0.f) {
+    clip = a.max_norm / (norm + 1e-6);
+    if (clip > 1.0) clip = 1.0;
+  }
+  const bool skip = a.partials && a.skip_nonfinite && !(norm < INFINITY);
+  const long long t = *a.step + (skip ? 0 : 1);
+  if (!skip) *a.step = t;
+  Scalars s;
+  s.g_factor = (float)(clip * (double)a.grad_scale);
+  s.lr = a.lr_dev ? *a.lr_dev : a.lr;
+  s.c1 = (float)(1.0 / (1.0 - pow(a.beta1, (double)t)));
+  s.c2 = (float)(1.0 / (1.0 - pow(a.beta2, (double)t)));
+  s.skip = skip ? 1 : 0;
+  *a.out = s;
+  if (a.stats) {
+    a.stats[0] = (float)norm;
+    a.stats[1] = (float)clip;
+    a.stats[2] = skip ? 1.f : 0.f;
+    a.stats[3] = (float)t;
+  }
+}
+
+__global__ void __launch_bounds__(kWarps * 32) adamw_step_kernel(const __grid_constant__ Table tab, const Hyper h,
+                                                                 const Scalars* __restrict__ scalars) {
+  const Scalars sc = *scalars;
+  if (sc.skip) return;
+  for_spans(tab, [&](const Slot& t, const Span& s) {
+    const bool half = t.flags & kParam16, bits8 = t.flags & kState8;
+    float g[kEach], p[kEach], m[kEach], v[kEach];
+    load(t.grad, t.flags & kGrad16, s, g);
+    if (t.master) load32(t.master, s, p);
+    else load(t.param, half, s, p);
+    if (bits8) {
+      open_m(t, s, m);
+      open_v(t, s, v);
+    } else {
+      load32(static_cast<const float*>(t.m), s, m);
+      load32(static_cast<const float*>(t.v), s, v);
+    }
+    const float lr = sc.lr * t.lr_scale, keep = 1.f - lr * t.weight_decay, rate = lr * sc.c1;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const float x = g[i] * sc.g_factor;
+      m[i] = fmaf(h.beta1, m[i], h.rest1 * x);
+      v[i] = fmaf(h.beta2, v[i], h.rest2 * (x * x));
+      p[i] = fmaf(keep, p[i], -rate * m[i] / (sqrtf(v[i] * sc.c2) + h.eps));
+    }
+    if (t.master) store32(t.master, s, p);
+    store(t.param, half, s, p);
+    if (bits8) {
+      close_m(t, s, m);
+      close_v(t, s, v);
+    } else {
+      store32(static_cast<float*>(t.m), s, m);
+      store32(static_cast<float*>(t.v), s, v);
+    }
+  });
+}
+
+// The states as numbers: param and master stand for the outputs of m and v.
+__global__ void __launch_bounds__(kWarps * 32) adamw_states_kernel(const __grid_constant__ Table tab) {
+  for_spans(tab, [&](const Slot& t, const Span& s) {
+    float x[kEach];
+    if (t.param) {
+      if (t.flags & kState8) open_m(t, s, x);
+      else load32(static_cast<const float*>(t.m), s, x);
+      store(t.param, t.flags & kOut16, s, x);
+    }
+    if (t.master) {
+      if (t.flags & kState8) open_v(t, s, x);
+      else load32(static_cast<const float*>(t.v), s, x);
+      store(t.master, t.flags & kOut16, s, x);
+    }
+  });
+}
+
+bool aligned_to(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+// The states of one tensor as the calls take them.
+int check_states(const aero_adamw_tensor& t) {
+  if (t.n < 0) return AERO_ERR_INVALID;
+  if (t.state_bits != 8 && t.state_bits != 32) return AERO_ERR_UNSUPPORTED;
+  if (t.n == 0) return AERO_OK;
+  if (!t.m || !t.v) return AERO_ERR_INVALID;
+  if (t.state_bits == 8 ? !t.m_scale || !t.v_scale || !aligned_to(t.m_scale, 4) || !aligned_to(t.v_scale, 4)
+                        : !aligned_to(t.m, 4) || !aligned_to(t.v, 4))
+    return AERO_ERR_INVALID;
+  return AERO_OK;
+}
+int check_tensor(const aero_adamw_tensor& t) {
+  const int rc = check_states(t);
+  if (rc) return rc;
+  for (const int32_t dt : {t.param_dtype, t.grad_dtype})
+    if (dt != AERO_BF16 && dt != AERO_FP32) return AERO_ERR_UNSUPPORTED;
+  if (t.master && t.param_dtype != AERO_BF16) return AERO_ERR_INVALID;        // the parameter is its own master
+  if (!(t.weight_decay >= 0.f) || !(t.lr_scale >= 0.f)) return AERO_ERR_INVALID;
+  if (t.n == 0) return AERO_OK;
+  if (!t.param || !t.grad) return AERO_ERR_INVALID;
+  if (!aligned_to(t.param, t.param_dtype == AERO_FP32 ? 4 : 2) || !aligned_to(t.grad, t.grad_dtype == AERO_FP32 ? 4 : 2) ||
+      !aligned_to(t.master, 4))
+    return AERO_ERR_INVALID;
+  return AERO_OK;
+}
+
+// Fills the table with tensors from *next on, leaving empty ones out, and moves *next on.
+void fill(Table& tab, const aero_adamw_tensor* tensors, int32_t n, int32_t* next) {
+  tab.count = 0;
+  tab.chunk0[0] = 0;
+  for (; *next < n && tab.count < kSlots; ++*next) {
+    const aero_adamw_tensor& t = tensors[*next];
+    if (t.n == 0) continue;
+    Slot& s = tab.slot[tab.count];
+    s = {t.n, t.param, t.grad, t.master, t.m, t.v, t.m_scale, t.v_scale, t.weight_decay, t.lr_scale, 0};
+    bool aligned = true;
+    for (const void* p : {(const void*)t.param, t.grad, (const void*)t.master, (const void*)t.m, (const void*)t.v})
+      aligned &= aligned_to(p, 16);
+    s.flags = (t.param_dtype == AERO_BF16 ? kParam16 : 0) | (t.grad_dtype == AERO_BF16 ? kGrad16 : 0) |
+              (t.state_bits == 8 ? kState8 : 0) | (aligned ? kAligned : 0);
+    tab.chunk0[tab.count + 1] = tab.chunk0[tab.count] + (t.n + kChunk - 1) / kChunk;
+    ++tab.count;
+  }
+}
+
+int grid_of(const Table& tab) {
+  const long long chunks = tab.chunk0[tab.count];
+  return (int)(chunks < kMaxBlocks ? chunks : kMaxBlocks);
+}
+int launches_of(int32_t n) { return (n + kSlots - 1) / kSlots; }
+
+}  // namespace
+
+extern "C" {
+
+void aero_adamw_cfg_default(aero_adamw_cfg* ac) {
+  if (!ac) return;
+  ac->lr = 1e-3f; ac->beta1 = 0.9; ac->beta2 = 0.999; ac->eps = 1e-8f;
+  ac->max_norm = 0.f; ac->grad_scale = 1.f; ac->skip_nonfinite = 0;
+}
+
+size_t aero_adamw_workspace_bytes(int32_t n_tensors) {
+  if (n_tensors < 0) return 0;
+  return 256 + aero_align_up((size_t)launches_of(n_tensors) * kMaxBlocks * sizeof(double), 256);
+}
+
+int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, const aero_adamw_tensor* tensors,
+                    int64_t* step, const float* lr, float* stats, void* workspace, size_t workspace_bytes) {
+  AeroRange nv("aero_adamw_step");
+  if (!ctx || !ac || n_tensors < 0 || (n_tensors > 0 && !tensors) || !step || !workspace || !aero_aligned256(workspace))
+    return AERO_ERR_INVALID;
+  if (!(ac->beta1 >= 0.0 && ac->beta1 < 1.0) || !(ac->beta2 >= 0.0 && ac->beta2 < 1.0) || !(ac->eps >= 0.f) ||
+      !(ac->lr >= 0.f) || !(ac->max_norm < INFINITY) || !(fabsf(ac->grad_scale) < INFINITY))
+    return AERO_ERR_INVALID;
+  for (int32_t i = 0; i < n_tensors; ++i)
+    if (const int rc = check_tensor(tensors[i])) return rc;
+  if (workspace_bytes < aero_adamw_workspace_bytes(n_tensors)) return AERO_ERR_WORKSPACE;
+  int rc = aero_check_ctx(ctx);
+  if (rc) return rc;
+  Scalars* scalars = static_cast<Scalars*>(workspace);
+  double* partials = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
+  const bool norm = ac->max_norm > 0.f || ac->skip_nonfinite;
+  Table tab;
+  int n_partials = 0;
+  if (norm) {
+    for (int32_t next = 0; next < n_tensors;) {
+      fill(tab, tensors, n_tensors, &next);
+      if (tab.count == 0) break;
+      adamw_norm_kernel<<<grid_of(tab), kWarps * 32, 0, ctx->stream>>>(tab, partials + n_partials);
+      n_partials += grid_of(tab);
+      ctx->launches += 1;
+    }
+  }
+  const PrepareArgs pa = {norm ? partials : nullptr, n_partials, ac->beta1, ac->beta2, ac->lr, ac->max_norm, ac->grad_scale,
+                          ac->skip_nonfinite, lr, reinterpret_cast<long long*>(step), stats, scalars};
+  adamw_prepare_kernel<<<1, 256, 0, ctx->stream>>>(pa);
+  ctx->launches += 1;
+  const Hyper h = {(float)ac->beta1, (float)ac->beta2, (float)(1.0 - ac->beta1), (float)(1.0 - ac->beta2), ac->eps};
+  for (int32_t next = 0; next < n_tensors;) {
+    fill(tab, tensors, n_tensors, &next);
+    if (tab.count == 0) break;
+    adamw_step_kernel<<<grid_of(tab), kWarps * 32, 0, ctx->stream>>>(tab, h, scalars);
+    ctx->launches += 1;
+  }
+  AERO_CUDA_TRY(cudaGetLastError());
+  return AERO_OK;
+}
+
+int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor* tensors, int32_t out_dtype, void* const* m_out,
+                      void* const* v_out) {
+  AeroRange nv("aero_adamw_states");
+  if (!ctx || n_tensors < 0 || (n_tensors > 0 && (!tensors || (!m_out && !v_out)))) return AERO_ERR_INVALID;
+  if (out_dtype != AERO_BF16 && out_dtype != AERO_FP32) return AERO_ERR_UNSUPPORTED;
+  for (int32_t i = 0; i < n_tensors; ++i) {
+    if (const int rc = check_states(tensors[i])) return rc;
+    for (void* const* out : {m_out, v_out})
+      if (out && tensors[i].n > 0 && (!out[i] || !aligned_to(out[i], out_dtype == AERO_FP32 ? 4 : 2))) return AERO_ERR_INVALID;
+  }
+  int rc = aero_check_ctx(ctx);
+  if (rc) return rc;
+  Table tab;
+  for (int32_t next = 0; next < n_tensors;) {
+    int32_t at = next;
+    fill(tab, tensors, n_tensors, &next);
+    if (tab.count == 0) break;
+    for (int k = 0; k < tab.count; ++k, ++at) {
+      while (tensors[at].n == 0) ++at;
+      Slot& s = tab.slot[k];
+      s.param = m_out ? m_out[at] : nullptr;
+      s.master = v_out ? static_cast<float*>(v_out[at]) : nullptr;
+      bool aligned = true;
+      for (const void* p : {(const void*)s.param, (const void*)s.master, (const void*)s.m, (const void*)s.v}) aligned &= aligned_to(p, 16);
+      s.flags = (s.flags & kState8) | (aligned ? kAligned : 0) | (out_dtype == AERO_BF16 ? kOut16 : 0);
+    }
+    adamw_states_kernel<<<grid_of(tab), kWarps * 32, 0, ctx->stream>>>(tab);
+    ctx->launches += 1;
+  }
+  AERO_CUDA_TRY(cudaGetLastError());
+  return AERO_OK;
+}
+
+}  // extern "C"

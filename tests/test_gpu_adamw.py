@@ -1,0 +1,266 @@
+"""GPU tests of the AdamW step (aero_adamw_step, aero_adamw_states) against the fp64 statement, applied to the state that the
+device held before each step.
+
+Tolerances.  u = 2^-24.  m is two products and a sum of values that carry the clipped gradient's two roundings: at most 5 u of
+|beta1 m| + |(1 - beta1) g'|.  v has one more product of those: 8 u of its (positive) terms.  The step divides m c1 by
+sqrt(v c2) + eps: m's 5, the rate's 3, half of v's 8, the root, the sum and the quotient: below 16 u of the step, but where m's two
+terms cancel 16 u of what they would make; p adds three roundings of itself.  An output in bf16 is off by 2^-8 of itself besides.
+8-bit states: a code is the nearest value of its table to the state over the block's scale, where the quotient carries 4 u (and
+the root of v 5): compared through its distance to the nearest value, with 2^-20 of the value to spare."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import pref_step as M
+from paper_2602_14338_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+U, HALF16 = 2.0 ** -24, 2.0 ** -8
+DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = B.Context(0)
+    yield c
+    assert c.last_status() == 0
+    c.close()
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+def shifted(n, dtype, shift):
+    return torch.zeros(n + shift, dtype=dtype, device="cuda")[shift:]
+
+
+def make(sizes, param, grad, bits, master, seed, shift=0):
+    g = torch.Generator().manual_seed(seed)
+    out = []
+    for i, n in enumerate(sizes):
+        t = dict(param=shifted(n, DT[param], shift), grad=shifted(n, DT[grad], shift), weight_decay=0.1 * (i % 2), lr_scale=1.0 + i % 3)
+        p = torch.randn(n, generator=g) * 0.1
+        t["param"].copy_(p)
+        if master:
+            t["master"] = shifted(n, torch.float32, shift)
+            t["master"].copy_(p)
+        t["grad"].copy_(torch.randn(n, generator=g) * 10.0 ** torch.randint(-4, 2, (n,), generator=g))
+        if bits == 32:
+            t["m"], t["v"] = shifted(n, torch.float32, shift), shifted(n, torch.float32, shift)
+        else:
+            t["m"], t["v"] = shifted(n, torch.float8_e4m3fn, shift), shifted(n, torch.uint8, shift)
+            t["m_scale"], t["v_scale"] = (torch.zeros((n + 255) // 256, device="cuda") for _ in range(2))
+        out.append(t)
+    return out
+
+
+def states(t):
+    """m and v of one tensor in 64 bits, decoded here."""
+    if t["m"].dtype == torch.float32:
+        return f64(t["m"]), f64(t["v"])
+    n = t["m"].numel()
+    ms, vs = (np.repeat(f64(t[k]), 256)[:n] for k in ("m_scale", "v_scale"))
+    return f64(t["m"]) * ms, (M.E4M4[t["v"].cpu().numpy()] * vs) ** 2
+
+
+def check_codes(t, m, v):
+    """The stored states of tensor t against the fp64 ones m, v."""
+    n = len(m)
+    ms, vs = M.state_scales(m, v)
+    assert np.all(np.abs(f64(t["m_scale"]) - ms) <= 8 * U * ms) and np.all(np.abs(f64(t["v_scale"]) - vs) <= 8 * U * vs)
+    y = m / np.repeat(ms, 256)[:n]
+    off = np.abs(f64(t["m"]) - y)
+    assert np.all(off <= M.nearest(np.abs(y), M.E4M3) + 2.0 ** -20 * np.abs(y))
+    r = np.sqrt(v) / np.repeat(vs, 256)[:n]
+    code = t["v"].cpu().numpy()
+    off = np.abs(M.E4M4[code] - r)
+    small = r < M.E4M4[1]                                            # not zero: code 1
+    assert np.all((off <= M.nearest(r, M.E4M4) + 2.0 ** -20 * r) | (small & (code == 1)))
+    assert np.all(code[(r > 0)] > 0) and np.all(code[r == 0] == 0)
+
+
+def step_and_check(ctx, tensors, step, **kw):
+    ac = B.adamw_cfg_default(**kw)
+    before = [(f64(t["master"] if "master" in t else t["param"]), *states(t)) for t in tensors]
+    t_before = int(step.item())
+    stats = ctx.adamw_step(ac, B.AdamWPlan(tensors), step).cpu().numpy()
+    norm = M.grad_norm([f64(t["grad"]) for t in tensors], ac.grad_scale)
+    clip = M.clip_of(norm, ac.max_norm)
+    if ac.max_norm > 0 or ac.skip_nonfinite:
+        assert abs(stats[0] - norm) <= 2.0 ** -20 * norm
+    assert abs(stats[1] - clip) <= 2.0 ** -20 and stats[2] == 0 and stats[3] == t_before + 1 == step.item()
+    for t, (p, m, v) in zip(tensors, before):
+        lr = np.float64(np.float32(ac.lr)) * t["lr_scale"]
+        wd = np.float64(np.float32(t["weight_decay"]))
+        eps = np.float64(np.float32(ac.eps))
+        factor = clip * np.float64(np.float32(ac.grad_scale))
+        p1, m1, v1 = M.adamw(p, f64(t["grad"]), m, v, t_before + 1, lr, ac.beta1, ac.beta2, eps, wd, factor)
+        g = np.abs(f64(t["grad"]) * factor)
+        terms = ac.beta1 * np.abs(m) + (1 - ac.beta1) * g
+        root = np.sqrt(v1 / (1 - ac.beta2 ** (t_before + 1))) + eps
+        size = lr * terms / (1 - ac.beta1 ** (t_before + 1)) / np.where(root > 0, root, 1)
+        tol = 16 * U * size + 3 * U * (np.abs(p) + size)
+        got = f64(t["master"] if "master" in t else t["param"])
+        off = np.abs(got - p1)
+        if t["param"].dtype == torch.bfloat16 and "master" not in t:
+            tol = tol + HALF16 * np.abs(p1) + tol
+        assert np.all(off <= tol), (off / np.maximum(tol, 1e-300)).max()
+        if "master" in t:
+            assert torch.equal(t["param"], t["master"].bfloat16())
+        if t["m"].dtype == torch.float32:
+            assert np.all(np.abs(f64(t["m"]) - m1) <= 5 * U * terms + 2.0 ** -149)
+            assert np.all(np.abs(f64(t["v"]) - v1) <= 8 * U * v1 + 2.0 ** -149)
+        else:
+            check_codes(t, m1, v1)
+
+
+SIZES = [[1], [255, 256, 257], [5000, 3, 1536, 2048], [0, 7, 0, 70000, 0]]
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,master,grad", [("fp32", False, "fp32"), ("bf16", True, "bf16"), ("bf16", False, "fp32"),
+                                               ("fp32", False, "bf16")])
+@pytest.mark.parametrize("sizes", SIZES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("shift", [0, 1])
+def test_steps(ctx, bits, param, master, grad, sizes, shift):
+    tensors = make(sizes, param, grad, bits, master, 1, shift)
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    g = torch.Generator().manual_seed(9)
+    for k in range(3):
+        step_and_check(ctx, tensors, step, lr=1e-2, beta2=0.99, max_norm=(0.0, 1.0, 1e9)[k], grad_scale=(1.0, 0.25, -2.0)[k])
+        for t in tensors:
+            t["grad"].copy_(torch.randn(t["grad"].numel(), generator=g))
+
+
+def test_more_tensors_than_a_launch_takes(ctx):
+    tensors = make([1 + 37 * i % 900 for i in range(300)], "bf16", "bf16", 8, True, 2)
+    step = torch.full((1,), 1000, dtype=torch.int64, device="cuda")
+    step_and_check(ctx, tensors, step, lr=1e-3, max_norm=0.5)
+    step_and_check(ctx, tensors, step, lr=1e-3, max_norm=0.5)
+
+
+def test_no_tensor(ctx):
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    stats = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0), B.AdamWPlan([]), step)
+    assert stats.tolist() == [0.0, 1.0, 0.0, 1.0] and step.item() == 1
+
+
+@pytest.mark.parametrize("size", [1e-25, 1e-42, 1e25])
+def test_norm_of_tiny_and_huge_gradients(ctx, size):
+    tensors = make([3000, 5], "fp32", "fp32", 32, False, 3)
+    for t in tensors:
+        t["grad"].copy_(torch.randn(t["grad"].numel(), generator=torch.Generator().manual_seed(4)).double() * size)
+    norm = M.grad_norm([f64(t["grad"]) for t in tensors])
+    stats = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0), B.AdamWPlan(tensors), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    assert abs(stats[0].item() - norm) <= 2.0 ** -20 * norm + 2.0 ** -149
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_nonfinite_gradient(ctx, bits, bad):
+    tensors = make([600, 40], "bf16", "fp32", bits, True, 5)
+    step = torch.full((1,), 7, dtype=torch.int64, device="cuda")
+    step_and_check(ctx, tensors, step, lr=1e-3)
+    tensors[0]["grad"][300] = bad
+    plan = B.AdamWPlan(tensors)
+    held = [{k: x.clone() for k, x in t.items() if torch.is_tensor(x)} for t in tensors]
+    stats = ctx.adamw_step(B.adamw_cfg_default(skip_nonfinite=1), plan, step)
+    assert stats[2].item() == 1 and step.item() == 8
+    for t, h in zip(tensors, held):
+        for k, x in h.items():
+            assert torch.equal(t[k].view(torch.uint8), x.view(torch.uint8)), k
+    stats = ctx.adamw_step(B.adamw_cfg_default(), plan, step)
+    assert stats[2].item() == 0 and step.item() == 9
+    assert not torch.isfinite(tensors[0]["master"][300]) and torch.isfinite(tensors[1]["master"]).all()
+    m, v = ctx.adamw_states(plan, out_dtype=torch.float32)
+    nan = torch.zeros(600, dtype=torch.bool, device="cuda")
+    nan[300] = True
+    if bits == 8:
+        nan[256:512] = True                                        # the whole block
+        assert torch.equal(torch.isnan(m[0]), nan) and torch.equal(torch.isnan(v[0]), nan)
+    else:
+        assert torch.equal(~torch.isfinite(m[0]), nan) and torch.equal(~torch.isfinite(v[0]), nan)
+    assert torch.isfinite(m[1]).all() and torch.isfinite(v[1]).all()
+
+
+def test_norm_that_is_no_number_without_skip(ctx):
+    """max_norm with an infinite norm and no skip: the clip is 0 and an infinite gradient becomes NaN, nothing faults."""
+    tensors = make([10], "fp32", "fp32", 32, False, 6)
+    tensors[0]["grad"][3] = float("inf")
+    stats = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0), B.AdamWPlan(tensors), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    assert stats[0].item() == float("inf") and stats[1].item() == 0
+    assert torch.isnan(tensors[0]["param"]).sum().item() == 1
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("shift", [0, 3])
+def test_states_as_numbers(ctx, bits, out, shift):
+    tensors = make([700, 0, 256, 1], "fp32", "fp32", bits, False, 8, shift)
+    ctx.adamw_step(B.adamw_cfg_default(), B.AdamWPlan(tensors), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    plan = B.AdamWPlan(tensors)
+    ms, vs = ctx.adamw_states(plan, out_dtype=out)
+    half = HALF16 if out == torch.bfloat16 else U
+    for t, m, v in zip(tensors, ms, vs):
+        em, ev = states(t)
+        assert np.all(np.abs(f64(m) - em) <= (half + 2 * U) * np.abs(em))
+        assert np.all(np.abs(f64(v) - ev) <= (half + 4 * U) * ev + 2.0 ** -149)
+    only = (C.c_void_p * 4)(*[x.data_ptr() for x in vs])             # one of the two alone
+    want = [v.clone() for v in vs]
+    for v in vs:
+        v.zero_()
+    assert ctx.lib.aero_adamw_states(ctx.h, 4, plan.array, B.AERO_BF16 if out == torch.bfloat16 else B.AERO_FP32, None, only) == 0
+    assert all(torch.equal(a, b) for a, b in zip(vs, want))
+
+
+def test_captured_and_replayed(ctx):
+    """The step counts on and the learning rate is read anew when a captured call is replayed."""
+    run, ref = make([5000, 300], "bf16", "fp32", 8, True, 11), make([5000, 300], "bf16", "fp32", 8, True, 11)
+    steps = [torch.zeros(1, dtype=torch.int64, device="cuda") for _ in range(2)]
+    lr = torch.tensor([1e-2], device="cuda")
+    ac = B.adamw_cfg_default(max_norm=1.0)
+    plan = B.AdamWPlan(run)
+    stream = torch.cuda.Stream()
+    own = B.Context(0, stream)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        stats = own.adamw_step(ac, plan, steps[0], lr=lr)
+    for k in range(3):
+        lr.fill_(1e-2 / (k + 1))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0, lr=lr.item()), B.AdamWPlan(ref), steps[1])
+        assert torch.equal(stats, want) and steps[0].item() == steps[1].item() == k + 1
+        for a, b in zip(run, ref):
+            for name in ("param", "master", "m", "v", "m_scale", "v_scale"):
+                assert torch.equal(a[name].view(torch.uint8), b[name].view(torch.uint8)), name
+    del graph
+    own.close()
+
+
+def test_beyond_32_bit_offsets(ctx):
+    n = 2 ** 31 + 300
+    t = dict(param=torch.zeros(n, dtype=torch.bfloat16, device="cuda"), grad=torch.zeros(n, dtype=torch.bfloat16, device="cuda"),
+             m=torch.zeros(n, dtype=torch.float8_e4m3fn, device="cuda"), v=torch.zeros(n, dtype=torch.uint8, device="cuda"))
+    t["m_scale"], t["v_scale"] = (torch.zeros((n + 255) // 256, device="cuda") for _ in range(2))
+    tail = 5000
+    small = {k: x[-tail:].clone() for k, x in t.items() if "scale" not in k}
+    small["param"].normal_()
+    small["grad"].normal_()
+    t["param"][-tail:], t["grad"][-tail:] = small["param"], small["grad"]
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    stats = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0, lr=0.1), B.AdamWPlan([t]), step).cpu().numpy()
+    norm = M.grad_norm([f64(small["grad"])])
+    assert abs(stats[0] - norm) <= 2.0 ** -20 * norm
+    p1, m1, v1 = M.adamw(f64(small["param"]), f64(small["grad"]), 0 * f64(small["param"]), 0 * f64(small["param"]), 1,
+                         np.float64(np.float32(0.1)), 0.9, 0.999, np.float64(np.float32(1e-8)), 0.0, M.clip_of(norm, 1.0))
+    got = f64(t["param"][-tail:])
+    assert np.all(np.abs(got - p1) <= HALF16 * np.abs(p1) + 40 * U * (np.abs(p1) + 0.2))
+    assert torch.count_nonzero(t["param"][:2 ** 31 - 8000]).item() == 0
+    ms = np.repeat(f64(t["m_scale"]), 256)[n - tail:n]
+    assert np.all(np.abs(f64(t["m"][-tail:]) * ms - m1) <= 2.0 ** -4 * np.abs(m1) + 2.0 ** -9 * ms)

@@ -1,0 +1,71 @@
+"""Calls of the operators of a preference-training step that are refused, before any device call: the error code of each argument
+error.  CPU only.  The context handed to the C calls is a block of zeros, which is all that the argument checks look at; no
+call here gets past them."""
+import ctypes as C
+
+import pytest
+
+from paper_2602_14338_b200 import binding as B
+
+INVALID, UNSUPPORTED, WORKSPACE = -1, -2, -3
+P = 4096                                    # a "pointer" that is aligned; never followed
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2602_14338_b200 import build
+
+    build.build()
+    return B.load_library()
+
+
+@pytest.fixture(scope="module")
+def fake():
+    return C.create_string_buffer(1 << 16)
+
+
+def cfg(dtype=B.AERO_BF16):
+    return C.byref(B.cfg_default(dtype=dtype))
+
+
+def adamw_tensor(**over):
+    t = dict(n=1000, param=P, grad=P, master=None, m=P, v=P, m_scale=P, v_scale=P, param_dtype=B.AERO_BF16, grad_dtype=B.AERO_FP32,
+             state_bits=8, weight_decay=0.0, lr_scale=1.0)
+    t.update(over)
+    return B.AeroAdamWTensor(**t)
+
+
+def test_adamw_refusals(lib, fake):
+    need = lib.aero_adamw_workspace_bytes(1)
+    assert need > 0 and lib.aero_adamw_workspace_bytes(-1) == 0 and lib.aero_adamw_workspace_bytes(0) >= 256
+
+    def step(ctx=fake, ac=None, n=1, t=None, stp=P, ws=P, wsb=need, **over):
+        ac = ac if ac is not None else B.adamw_cfg_default()
+        t = (B.AeroAdamWTensor * 1)(adamw_tensor(**over)) if t is None else t
+        return lib.aero_adamw_step(ctx, C.byref(ac), n, t, stp, None, None, ws, wsb)
+
+    assert step(ctx=None) == INVALID and step(n=-1) == INVALID and step(stp=None) == INVALID and step(ws=None) == INVALID
+    assert step(t=C.POINTER(B.AeroAdamWTensor)()) == INVALID
+    assert step(ws=P + 16) == INVALID and step(wsb=need - 1) == WORKSPACE
+    for name in ("param", "grad", "m", "v", "m_scale", "v_scale"):
+        assert step(**{name: None}) == INVALID, name
+    for name, off in (("param", 1), ("grad", 2), ("m_scale", 2), ("v_scale", 1)):
+        assert step(**{name: P + off}) == INVALID, name
+    assert step(state_bits=32, m=P + 2) == INVALID and step(state_bits=32, v=P + 1) == INVALID
+    assert step(master=P + 2) == INVALID and step(master=P, param_dtype=B.AERO_FP32) == INVALID
+    assert step(n=1, t=(B.AeroAdamWTensor * 1)(adamw_tensor(n=-1))) == INVALID
+    assert step(param_dtype=2) == UNSUPPORTED and step(grad_dtype=-1) == UNSUPPORTED and step(state_bits=16) == UNSUPPORTED
+    nan = float("nan")
+    assert step(weight_decay=-0.1) == INVALID and step(weight_decay=nan) == INVALID and step(lr_scale=-1.0) == INVALID
+    for name, bad in (("lr", -1.0), ("lr", nan), ("beta1", 1.0), ("beta1", -0.1), ("beta2", 1.0), ("beta2", nan), ("eps", -1e-8),
+                      ("eps", nan), ("max_norm", float("inf")), ("max_norm", nan), ("grad_scale", nan), ("grad_scale", float("inf"))):
+        assert step(ac=B.adamw_cfg_default(**{name: bad})) == INVALID, name
+
+    def states(ctx=fake, n=1, out=B.AERO_BF16, m=P, v=P, **over):
+        t = (B.AeroAdamWTensor * 1)(adamw_tensor(**over))
+        array = lambda p: None if p is None else (C.c_void_p * 1)(p or None)  # noqa: E731
+        return lib.aero_adamw_states(ctx, n, t, out, array(m), array(v))
+
+    assert states(ctx=None) == INVALID and states(n=-1) == INVALID and states(out=5) == UNSUPPORTED
+    assert states(m=None, v=None) == INVALID and states(m=0) == INVALID and states(m=P + 1) == INVALID
+    assert states(v=P + 2, out=B.AERO_FP32) == INVALID and states(m_scale=None) == INVALID and states(state_bits=4) == UNSUPPORTED
