@@ -676,6 +676,40 @@ int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, 
 int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor* tensors, int32_t out_dtype, void* const* m_out,
                       void* const* v_out);
 
+/* Rows in 4-bit floating point, and the lm_head product of them: a frozen reference or teacher scored at a quarter of the bytes
+ * of bf16.  A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) times the scale of its block of neighbours in the row:
+ *   block 16: an e4m3 code times the row's scale, a power of two;
+ *   block 32: a power of two (e8m0: code - 127 is its exponent, 255 stands for NaN).
+ * The rows [T,d] are held in
+ *   codes: tiles of 128 rows x 256 columns, 128 bytes to a row of a tile, the tiles of the same 128 rows one after the other.  Column
+ *     2 i of a tile is the lower half of byte i; the 16-byte chunk c of row r stands at chunk c xor (r mod 8) of the row.
+ *   scales: groups of 512 bytes, 128 rows x 4 blocks: byte 16 (r mod 32) + 4 ((r mod 128) / 32) + k for block k of the group; the
+ *     ceil(d / 256) 64 / block groups of the same 128 rows one after the other.
+ *   row_scale [T] f32 (block 16 only; NULL for block 32).
+ * Rows and columns that fill up the last tiles have codes and scales of zero.
+ * aero_quantize_fp4: of rows x [T,d] (cfg->dtype).
+ *   block 16: row_scale = the smallest power of two >= max|x_row| / (6 448), at least 2^-126 (a row of zeros: 0); with
+ *     x' = x / row_scale, scale = e4m3(max|x'_block| / 6), code = e2m1(x' / scale), 0 where the scale is.
+ *   block 32: scale = 2^(floor(log2 max|x_block|) - 2), at least 2^-127; code = e2m1(x / scale).
+ *   Rounded to even; values beyond 6 become 6.  A row (block 16) or block (block 32) with a NaN or an infinity gets a NaN scale.
+ * aero_dequantize_fp4: the values, rounded once to out_dtype (AERO_BF16 | AERO_FP32), out [T,d].
+ * aero_lmhead_fp4: out[t,v] = sum_k h_tk w_vk of the values, T rows h and V rows w in the same format; sums of exact products in
+ *   fp32 on the tensor cores, multiplied by the two rows' scales and rounded once to out_dtype; out [T,V].
+ * d % 32 == 0, d <= 65536, T and V <= 2^30; x, out of aero_dequantize_fp4, codes and scales 16-byte aligned.
+ */
+size_t aero_fp4_code_bytes(int64_t T, int32_t d);
+size_t aero_fp4_scale_bytes(int64_t T, int32_t d, int32_t block);
+
+int aero_quantize_fp4(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t block, const void* x, uint8_t* codes,
+                      uint8_t* scales, float* row_scale);
+
+int aero_dequantize_fp4(aero_ctx* ctx, int64_t T, int32_t d, int32_t block, const uint8_t* codes, const uint8_t* scales,
+                        const float* row_scale, int32_t out_dtype, void* out);
+
+int aero_lmhead_fp4(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, int32_t block, const uint8_t* h_codes, const uint8_t* h_scales,
+                    const float* h_row, const uint8_t* w_codes, const uint8_t* w_scales, const float* w_row, int32_t out_dtype,
+                    void* out);
+
 /* Optional timing of the dominant kernel.  With timing on, aero_grpo_loss_fwd_bwd records a pair of
  * CUDA events on the context's stream around each launch of its lm_head kernel (up to 256 launches
  * between read-outs; the events are created on first use).  aero_kernel_timing_ms synchronises the

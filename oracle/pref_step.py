@@ -47,3 +47,58 @@ def nearest(x, table):
     """Distance of each x from the nearest value of a table."""
     at = np.clip(np.searchsorted(table, x), 1, len(table) - 1)
     return np.minimum(np.abs(x - table[at - 1]), np.abs(table[at] - x))
+
+
+# ---- rows in 4-bit floating point -----------------------------------------------------------------
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def round_to(x, table):
+    """The nearest value of a table of magnitudes (its last one for what is larger), the one at an even place of two as near."""
+    a = np.minimum(np.abs(x), table[-1])
+    hi = np.clip(np.searchsorted(table, a), 1, len(table) - 1)
+    below, above = a - table[hi - 1], table[hi] - a
+    up = (above < below) | ((above == below) & (hi % 2 == 0))
+    return np.sign(x) * np.where(up, table[hi], table[hi - 1])
+
+
+def quantize_fp4(x, block):
+    """(values, scales of the blocks, row scales or None) of rows x."""
+    x = np.asarray(x, np.float64)
+    T, d = x.shape
+    xb = x.reshape(T, d // block, block)
+    top = np.abs(xb).max(axis=2)
+    if block == 32:
+        m, e = np.frexp(top)                                   # top = m 2^e, m in [0.5, 1)
+        scale, row = np.ldexp(1.0, np.where(top > 0, np.maximum(e - 3, -127), -127)), None
+    else:
+        m, e = np.frexp(np.abs(x).max(axis=1) / (6 * 448))
+        row = np.where(m > 0, np.ldexp(1.0, np.maximum(e - (m == 0.5), -126)), 0.0)
+        unit = np.where(row > 0, row, 1.0)
+        scale = round_to(top / 6 / unit[:, None], E4M3) * row[:, None]
+    safe = np.where(scale > 0, scale, 1.0)
+    value = round_to(xb / safe[:, :, None], E2M1) * scale[:, :, None]
+    return value.reshape(T, d), scale, row
+
+
+def fp4_places(T, d, block):
+    """Byte and half of each code, and byte of each scale, in the library's layout."""
+    slabs = -(-d // 256)
+    r, c = np.arange(T)[:, None], np.arange(d)[None, :]
+    byte = c % 256 // 2
+    at = ((r // 128 * slabs + c // 256) * 128 + r % 128) * 128 + ((byte // 16) ^ (r % 8)) * 16 + byte % 16
+    k = np.arange(d // block)[None, :]
+    groups = slabs * 64 // block
+    return at, c % 2 + 0 * r, (r // 128 * groups + k // 4) * 512 + r % 32 * 16 + r % 128 // 32 * 4 + k % 4
+
+
+def fp4_values(codes, scales, row, T, d, block):
+    """The values that buffers in that layout hold."""
+    at, half, where = fp4_places(T, d, block)
+    code = (codes[at] >> (4 * half)) & 15
+    s = scales[where].astype(np.int64)
+    if block == 32:
+        scale = np.where(s == 255, np.nan, np.ldexp(1.0, s - 127))
+    else:
+        scale = np.concatenate([E4M3, [np.nan]])[s & 127] * np.asarray(row, np.float64)[:, None]
+    return np.where(code >= 8, -1.0, 1.0) * E2M1[code & 7] * np.repeat(scale, block, axis=1)

@@ -39,6 +39,7 @@ EXPORTS = [
     "aero_distill_fwd", "aero_distill_bwd", "aero_distill_fwd_bwd", "aero_distill_fwd_workspace_bytes",
     "aero_distill_bwd_workspace_bytes", "aero_distill_fwd_bwd_workspace_bytes",
     "aero_adamw_cfg_default", "aero_adamw_workspace_bytes", "aero_adamw_step", "aero_adamw_states",
+    "aero_fp4_code_bytes", "aero_fp4_scale_bytes", "aero_quantize_fp4", "aero_dequantize_fp4", "aero_lmhead_fp4",
 ]
 
 
@@ -159,6 +160,13 @@ def load_library():
     lib.aero_adamw_workspace_bytes.argtypes = [i32]
     lib.aero_adamw_step.argtypes = [vp, ap, i32, tp, vp, vp, vp, vp, sz]
     lib.aero_adamw_states.argtypes = [vp, i32, tp, i32, C.POINTER(vp), C.POINTER(vp)]
+    lib.aero_fp4_code_bytes.restype = sz
+    lib.aero_fp4_code_bytes.argtypes = [i64, i32]
+    lib.aero_fp4_scale_bytes.restype = sz
+    lib.aero_fp4_scale_bytes.argtypes = [i64, i32, i32]
+    lib.aero_quantize_fp4.argtypes = [vp, cp, i64, i32, i32] + [vp] * 4
+    lib.aero_dequantize_fp4.argtypes = [vp, i64, i32, i32, vp, vp, vp, i32, vp]
+    lib.aero_lmhead_fp4.argtypes = [vp, i64, i32, i32, i32] + [vp] * 6 + [i32, vp]
     lib.aero_launch_count.restype = C.c_int64
     lib.aero_launch_count.argtypes = [vp]
     _lib = lib
@@ -257,6 +265,33 @@ class AdamWPlan:
 
     def __len__(self):
         return len(self.tensors)
+
+
+class Fp4Rows:
+    """rows x cols values in 4-bit floating point, in the layout that include/aero.h describes: codes and scales (uint8) and, for
+    block 16, row_scale [rows] f32.  The buffers are made unless given (on `device`)."""
+
+    def __init__(self, rows, cols, block=16, codes=None, scales=None, row_scale=None, device=None):
+        lib = load_library()
+        if block not in (16, 32):
+            raise AeroError(f"block must be 16 or 32, got {block}")
+        if rows < 0 or cols <= 0 or cols % 32:
+            raise AeroError(f"rows must be at least 0 and cols a multiple of 32, got {rows} x {cols}")
+        if block == 32 and row_scale is not None:
+            raise AeroError("block 32 has no row_scale")
+        self.rows, self.cols, self.block = rows, cols, block
+        sizes = lib.aero_fp4_code_bytes(rows, cols), lib.aero_fp4_scale_bytes(rows, cols, block)
+        self.codes = codes if codes is not None else torch.empty(sizes[0], dtype=torch.uint8, device=device)
+        self.scales = scales if scales is not None else torch.empty(sizes[1], dtype=torch.uint8, device=device)
+        if block == 16 and row_scale is None:
+            row_scale = torch.empty(rows, dtype=torch.float32, device=device)
+        self.row_scale = row_scale
+        want = [("codes", self.codes, torch.uint8, sizes[0]), ("scales", self.scales, torch.uint8, sizes[1])]
+        if block == 16:
+            want.append(("row_scale", self.row_scale, torch.float32, rows))
+        for name, t, dtype, numel in want:
+            if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+                raise AeroError(f"{name} must be a contiguous tensor of {numel} {dtype}, got {t.numel()} {t.dtype}")
 
 
 def _ptr(t, dtype=None, numel=None, name="tensor"):
@@ -693,6 +728,49 @@ class Context:
                                      AERO_FP32 if out_dtype == torch.float32 else AERO_BF16,
                                      self._arg(o, out_dtype, (T, V), "out"))
         _check(rc, "aero_lmhead_q8")
+        return o
+
+    # ---- rows in 4-bit floating point ------------------------------------------------------------
+    def _fp4(self, r, name):
+        return tuple(self._arg(t, t.dtype, tuple(t.shape), f"{name}.{part}") if t is not None else None
+                     for part, t in (("codes", r.codes), ("scales", r.scales), ("row_scale", r.row_scale)))
+
+    def quantize_fp4(self, cfg, x, block=16, out=None):
+        """aero_quantize_fp4: the rows of x as Fp4Rows."""
+        T, d = x.shape
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        px = self._arg(x, dt, (T, d), "x")
+        if out is None:
+            if block not in (16, 32) or d % 32:
+                raise AeroError(f"block must be 16 or 32 and the columns a multiple of 32, got {block} and {d}")
+            out = Fp4Rows(T, d, block, self._new((self.lib.aero_fp4_code_bytes(T, d),), torch.uint8),
+                          self._new((self.lib.aero_fp4_scale_bytes(T, d, block),), torch.uint8),
+                          self._new((T,), torch.float32) if block == 16 else None)
+        elif (out.rows, out.cols, out.block) != (T, d, block):
+            raise AeroError(f"out must hold {T} x {d} values in blocks of {block}, got {out.rows} x {out.cols} in {out.block}")
+        _check(self.lib.aero_quantize_fp4(self.h, C.byref(cfg), T, d, block, px, *self._fp4(out, "out")), "aero_quantize_fp4")
+        return out
+
+    def dequantize_fp4(self, rows, out_dtype=torch.bfloat16, out=None):
+        """aero_dequantize_fp4: the values of Fp4Rows."""
+        if out_dtype not in (torch.bfloat16, torch.float32):
+            raise AeroError(f"out_dtype must be torch.bfloat16 or torch.float32, got {out_dtype}")
+        o = out if out is not None else self._new((rows.rows, rows.cols), out_dtype)
+        _check(self.lib.aero_dequantize_fp4(self.h, rows.rows, rows.cols, rows.block, *self._fp4(rows, "rows"),
+                                            AERO_FP32 if out_dtype == torch.float32 else AERO_BF16,
+                                            self._arg(o, out_dtype, (rows.rows, rows.cols), "out")), "aero_dequantize_fp4")
+        return o
+
+    def lmhead_fp4(self, h, w, out_dtype=torch.bfloat16, out=None):
+        """aero_lmhead_fp4: logits [T,V] of Fp4Rows h [T,d] and w [V,d]."""
+        if (h.cols, h.block) != (w.cols, w.block):
+            raise AeroError(f"h and w must have the same columns and blocks, got {h.cols}, {h.block} and {w.cols}, {w.block}")
+        if out_dtype not in (torch.bfloat16, torch.float32):
+            raise AeroError(f"out_dtype must be torch.bfloat16 or torch.float32, got {out_dtype}")
+        o = out if out is not None else self._new((h.rows, w.rows), out_dtype)
+        _check(self.lib.aero_lmhead_fp4(self.h, h.rows, h.cols, w.rows, h.block, *self._fp4(h, "h"), *self._fp4(w, "w"),
+                                        AERO_FP32 if out_dtype == torch.float32 else AERO_BF16,
+                                        self._arg(o, out_dtype, (h.rows, w.rows), "out")), "aero_lmhead_fp4")
         return o
 
     # ---- AdamW over many tensors ---------------------------------------------------------------

@@ -84,6 +84,12 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* m, int
       ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(m)), "r"(c0), "r"(c1), "r"(smem_u32(bar))
       : "memory");
 }
+// Contiguous bytes global -> shared: both addresses 16-byte aligned, a multiple of 16 bytes.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_u32(dst)), "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
 // 3-D tiled load (used with the blocked view below: element, row, 64-column block).
 __device__ __forceinline__ void tma_load_3d(void* dst, const CUtensorMap* m, int c0, int c1, int c2, uint64_t* bar) {
   asm volatile(
@@ -274,6 +280,34 @@ __device__ __forceinline__ void umma_s8_pair(uint32_t tmem_d, uint64_t desc_a, u
       : "memory");
 }
 
+// Products of e2m1 values (two to a byte, K = 64 per instruction) with a scale per 16 (e4m3) or 32 (e8m0) of them along K,
+// read from TMEM, fp32 accumulators.  PAIR: over a CTA pair.
+template <int BLOCK, bool PAIR>
+__device__ __forceinline__ void umma_fp4(uint32_t tmem_d, uint64_t desc_a, uint64_t desc_b, uint32_t idesc, uint32_t tmem_sfa,
+                                         uint32_t tmem_sfb, uint32_t accumulate) {
+#define AERO_UMMA_FP4(GROUP, KIND, VEC)                                                                                  \
+  asm volatile(                                                                                                          \
+      "{\n\t"                                                                                                            \
+      ".reg .pred p;\n\t"                                                                                                \
+      "setp.ne.b32 p, %6, 0;\n\t"                                                                                        \
+      "tcgen05.mma.cta_group::" GROUP ".kind::" KIND ".block_scale.scale_vec::" VEC " [%0], %1, %2, %3, [%4], [%5], p;\n\t" \
+      "}" ::"r"(tmem_d),                                                                                                 \
+      "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(tmem_sfa), "r"(tmem_sfb), "r"(accumulate)                                \
+      : "memory")
+  if constexpr (BLOCK == 16 && PAIR) AERO_UMMA_FP4("2", "mxf4nvf4", "4X");
+  else if constexpr (BLOCK == 16) AERO_UMMA_FP4("1", "mxf4nvf4", "4X");
+  else if constexpr (PAIR) AERO_UMMA_FP4("2", "mxf4", "2X");
+  else AERO_UMMA_FP4("1", "mxf4", "2X");
+#undef AERO_UMMA_FP4
+}
+// 512 bytes of scales (32 rows of 16 bytes) from shared memory to four columns of all four quadrants of TMEM lanes; in a pair, of
+// each CTA from its own shared memory.  Runs in order with the products that the same thread issues after it.
+template <bool PAIR>
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
+  if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // 32 lanes x 32 consecutive fp32 columns: thread l of the warp receives row (lane base + l).
@@ -300,6 +334,16 @@ __host__ __device__ constexpr uint32_t make_idesc_bf16(int M, int N, int a_mn, i
 // Instruction descriptor of tcgen05.mma kind::i8 with signed 8-bit A and B (both K-major), s32 D.
 __host__ __device__ constexpr uint32_t make_idesc_s8(int M, int N) {
   return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// Instruction descriptor of the 4-bit kinds: e2m1 A and B (K-major), scales e4m3 or (e8m0 = 1) powers of two; sf: the byte of a
+// 32-bit cell of scales at which this instruction's begin.
+__host__ __device__ constexpr uint32_t make_idesc_fp4(int M, int N, int e8m0, int sf) {
+  return ((uint32_t)sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)e8m0 << 23) |
+         ((uint32_t)(M >> 4) << 24) | ((uint32_t)sf << 29);
+}
+// Shared-memory descriptor of 512 bytes of scales for tmem_copy_scales: unswizzled, 8 rows of 16 bytes every 128 bytes.
+__device__ __forceinline__ uint64_t make_scale_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | 1ull << 16 | 8ull << 32 | 1ull << 46;
 }
 // Shared-memory matrix descriptor, 128-byte swizzle, sm_100 format.  Byte offsets are
 // given in bytes and stored in 16-byte units.

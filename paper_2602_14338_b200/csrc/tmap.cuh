@@ -33,6 +33,29 @@ inline int aero_make_tmap_2d(aero_ctx* ctx, CUtensorMap* out, CUtensorMapDataTyp
   return r == CUDA_SUCCESS ? AERO_OK : AERO_ERR_CUDA;
 }
 
+// rows of row_words 32-bit words (at most 256) that already lie in memory as shared memory wants them: box of box_rows whole rows,
+// no swizzle.
+inline int aero_make_tmap_flat(aero_ctx* ctx, CUtensorMap* out, const void* base, uint64_t rows, uint32_t row_words,
+                               uint32_t box_rows) {
+  if (!ctx->tmap_encode) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess || !fn)
+      return AERO_ERR_CUDA;
+    ctx->tmap_encode = fn;
+  }
+  auto encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ctx->tmap_encode);
+  cuuint64_t gdim[2] = {row_words, rows};
+  cuuint64_t gstride[1] = {(uint64_t)row_words * 4};
+  cuuint32_t box[2] = {row_words, box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  CUresult r = encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<void*>(base), gdim, gstride, box, estr,
+                      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? AERO_OK : AERO_ERR_CUDA;
+}
+
 // Blocked 3-D view of a row-major bf16 matrix whose column count is a multiple of 64:
 // dimension 0 = the 64 elements of a column block (128 bytes), dimension 1 = rows,
 // dimension 2 = column blocks.  A box of (64, box_rows, n_blocks) lands in shared memory as

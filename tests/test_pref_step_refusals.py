@@ -69,3 +69,36 @@ def test_adamw_refusals(lib, fake):
     assert states(ctx=None) == INVALID and states(n=-1) == INVALID and states(out=5) == UNSUPPORTED
     assert states(m=None, v=None) == INVALID and states(m=0) == INVALID and states(m=P + 1) == INVALID
     assert states(v=P + 2, out=B.AERO_FP32) == INVALID and states(m_scale=None) == INVALID and states(state_bits=4) == UNSUPPORTED
+
+
+def test_fp4_refusals(lib, fake):
+    assert lib.aero_fp4_code_bytes(129, 288) == 2 * 2 * 128 * 128 and lib.aero_fp4_scale_bytes(129, 288, 16) == 2 * 2 * 2048
+    assert lib.aero_fp4_scale_bytes(1, 32, 32) == 1024 and lib.aero_fp4_scale_bytes(1, 32, 8) == 0
+    assert lib.aero_fp4_code_bytes(-1, 32) == 0 and lib.aero_fp4_code_bytes(0, 32) == 0
+
+    def quant(ctx=fake, c=None, T=4, d=64, block=16, x=P, codes=P, scales=P, row=P):
+        return lib.aero_quantize_fp4(ctx, c or cfg(), T, d, block, x, codes, scales, row)
+
+    def values(ctx=fake, T=4, d=64, block=16, codes=P, scales=P, row=P, dtype=B.AERO_BF16, out=P):
+        return lib.aero_dequantize_fp4(ctx, T, d, block, codes, scales, row, dtype, out)
+
+    def product(ctx=fake, T=4, d=64, V=10, block=16, h=P, hs=P, hr=P, w=P, ws=P, wr=P, dtype=B.AERO_BF16, out=P):
+        return lib.aero_lmhead_fp4(ctx, T, d, V, block, h, hs, hr, w, ws, wr, dtype, out)
+
+    for call in (quant, values, product):
+        assert call(ctx=None) == INVALID and call(T=-1) == INVALID and call(d=0) == INVALID
+        assert call(d=48) == UNSUPPORTED and call(d=65568) == UNSUPPORTED and call(T=(1 << 30) + 1) == UNSUPPORTED
+        assert call(block=64) == UNSUPPORTED and call(block=0) == UNSUPPORTED
+        assert call(block=32) == INVALID                                    # no row scales there
+    for name in ("x", "codes", "scales", "row"):
+        assert quant(**{name: None}) == INVALID, name
+    for name in ("x", "codes", "scales"):
+        assert quant(**{name: P + 8}) == INVALID, name
+    assert quant(row=P + 2) == INVALID and quant(c=cfg(5)) == UNSUPPORTED
+    for name in ("codes", "scales", "row", "out"):
+        assert values(**{name: None}) == INVALID and values(**{name: P + 2}) == INVALID, name
+    assert values(dtype=3) == UNSUPPORTED and product(dtype=3) == UNSUPPORTED
+    for name in ("h", "hs", "hr", "w", "ws", "wr", "out"):
+        assert product(**{name: None}) == INVALID and product(**{name: P + 1}) == INVALID, name
+    assert product(V=0) == INVALID and product(V=(1 << 30) + 1) == UNSUPPORTED
+    assert product(dtype=B.AERO_FP32, out=P + 2) == INVALID
