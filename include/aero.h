@@ -71,6 +71,8 @@ extern "C" {
                                     /* logits; the rows beyond the 1024 the call redoes have a saturated   */
                                     /* gradient (use the separate forward and backward calls instead)      */
 
+#define AERO_ST_BAD_PAIR      64u   /* a pair names a rollout outside [0,R): the pair does not count       */
+
 /* ---- enumerations ------------------------------------------------------------- */
 #define AERO_UNIFORM_MASK   0   /* all-correct / all-incorrect groups are dropped (Sec. 3.2)      */
 #define AERO_UNIFORM_BAYES  1   /* they use the posterior mean instead (Sec. 4.2 Strategy 2)      */
@@ -619,6 +621,66 @@ int aero_embed_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int
  */
 int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t* h8, const float* h_scale,
                    const int8_t* w8, const float* w_scale, int32_t out_dtype, void* out);
+
+/* Preference loss on pairs of rollouts through the lm_head: of two rollouts of a prompt (a correct and an incorrect one of a
+ * group, say) the first is to become more likely than the second, against a reference policy.  H, W, y, cs as in
+ * aero_grpo_loss_fwd; y_t = AERO_NO_TOKEN: the token is not scored (any other id outside [0,V) raises AERO_ST_BAD_TARGET besides).
+ *   r_i  = sum over the scored tokens t of rollout i of (logp_t - ref_logp_t), divided by their number if pc->mean != 0
+ *          (ref_logp NULL: no reference; no scored token: 0)
+ *   m_p  = beta (r_chosen - r_rejected) - margin,   (chosen, rejected) = pairs[p]
+ *   loss = sum_p u_p l(m_p),   u_p = pair_weight[p], or 1 / (number of pairs that count) with pair_weight NULL
+ *     AERO_PREF_LOGISTIC  l = (1 - s) log(1 + exp(-m)) + s log(1 + exp(m)),   s = label_smoothing
+ *     AERO_PREF_SQUARE    l = (m - 1/2)^2
+ *     AERO_PREF_HINGE     l = max(0, 1 - m)     (slope 0 at m = 1)
+ *   coef_i = d loss / d logp_t of each scored token of rollout i
+ *   dz_tv  = grad_scale coef_i (1[v == y_t] - p_tv);   dH = dz W,   dW (+)= dz^T H
+ * A rollout may be in any number of pairs; the rows of one that is in none are not touched (their outputs are 0).  A pair (-1, -1)
+ * is an empty place; one that names any other rollout outside [0,R) raises AERO_ST_BAD_PAIR and does not count.  Empty places
+ * have margin 0.  A rollout whose offsets leave [0,T] raises AERO_ST_BAD_OFFSETS and counts as one without tokens.
+ * Inputs   y [T] i32, ref_logp [T] f32 or NULL, cs [R+1] i64, pairs [P,2] i32 (8-byte aligned), pair_weight [P] f32 or NULL.
+ * Outputs  logp, lse [T], ratio, coef [R], margin [P] f32; loss [1] f32; metrics [4] f32 or NULL: fraction of the pairs with
+ *          r_chosen > r_rejected, mean beta r_chosen, mean beta r_rejected, number of pairs that count; dH [T,d] (cfg->dtype), dW
+ *          [V,d] of type dw_dtype as in aero_distill_bwd.
+ * aero_pref_bwd takes coef and lse from the forward and recomputes the logits (8 d V FLOP per token over the two calls; rollouts
+ * whose coef is 0 are left out).  aero_pref_fwd_bwd does not recompute them (6 d V) if the workspace holds all rows in one chunk, since
+ * a row's gradient needs the log-probs of all rows of its pairs; else it takes the two calls' passes.  cfg->dtype and d as in
+ * aero_distill_fwd; precision as there, with sums over rollouts and pairs in 64 bits; all sums have a fixed order.
+ * workspace: at least the matching *_workspace_bytes, 256-byte aligned.
+ */
+#define AERO_PREF_LOGISTIC 0
+#define AERO_PREF_SQUARE   1
+#define AERO_PREF_HINGE    2
+
+typedef struct aero_pref_cfg {
+  int32_t kind;            /* AERO_PREF_*       default LOGISTIC */
+  int32_t mean;            /* 1: r is a mean    default 0 */
+  float beta;              /* default 0.1 */
+  float margin;            /* default 0 */
+  float label_smoothing;   /* default 0; in [0,1], read by LOGISTIC only */
+} aero_pref_cfg;
+
+void aero_pref_cfg_default(aero_pref_cfg* pc);
+
+size_t aero_pref_fwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t P);
+
+int aero_pref_fwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_t T, int32_t d, int32_t V, int32_t R, int32_t P,
+                  const void* H, const void* W, const int32_t* y, const float* ref_logp, const int64_t* cs, const int32_t* pairs,
+                  const float* pair_weight, float* logp, float* lse, float* ratio, float* margin, float* coef, float* loss,
+                  float* metrics, void* workspace, size_t workspace_bytes);
+
+size_t aero_pref_bwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int64_t chunk_tokens, int32_t dw_dtype);
+
+int aero_pref_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, const void* H, const void* W,
+                  const int32_t* y, const int64_t* cs, const float* coef, const float* lse, float grad_scale, void* dH, void* dW,
+                  int32_t dw_dtype, int accumulate_dW, void* workspace, size_t workspace_bytes);
+
+size_t aero_pref_fwd_bwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t P, int64_t chunk_tokens, int32_t dw_dtype);
+
+int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_t T, int32_t d, int32_t V, int32_t R,
+                      int32_t P, const void* H, const void* W, const int32_t* y, const float* ref_logp, const int64_t* cs,
+                      const int32_t* pairs, const float* pair_weight, float* logp, float* lse, float* ratio, float* margin,
+                      float* coef, float* loss, float* metrics, float grad_scale, void* dH, void* dW, int32_t dw_dtype,
+                      int accumulate_dW, void* workspace, size_t workspace_bytes);
 
 /* One AdamW step over many tensors (the weights, norms and biases that dW and dgamma above are the gradients of).
  * With g' = grad_scale clip g, clip = min(1, max_norm / (norm + 1e-6)), norm the 2-norm of grad_scale g over all tensors

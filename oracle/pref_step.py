@@ -8,6 +8,62 @@ import numpy as np
 NO_TOKEN = -1
 
 
+# ---- preference loss on pairs of rollouts ---------------------------------------------------------
+def pref_pair(kind, m, smoothing=0.0):
+    """(loss, slope) of a margin."""
+    if kind == "logistic":
+        sig = lambda x: np.exp(-np.logaddexp(0.0, -x))  # noqa: E731
+        return ((1 - smoothing) * np.logaddexp(0.0, -m) + smoothing * np.logaddexp(0.0, m),
+                smoothing * sig(m) - (1 - smoothing) * sig(-m))
+    if kind == "square":
+        return (m - 0.5) ** 2, 2 * (m - 0.5)
+    return max(0.0, 1.0 - m), -1.0 if m < 1 else 0.0
+
+
+def preference(H, W, y, cs, pairs, ref=None, weight=None, kind="logistic", mean=False, beta=0.1, margin=0.0, smoothing=0.0,
+               grads=True):
+    """Outputs of the loss on pairs by its definition; rows of rollouts in no pair are 0."""
+    H, W = np.asarray(H, np.float64), np.asarray(W, np.float64)
+    T, V, R = len(H), len(W), len(cs) - 1
+    counted = [p for p, (c, r) in enumerate(pairs) if 0 <= c < R and 0 <= r < R]
+    used = sorted({i for p in counted for i in pairs[p]})
+    logp, lse = np.zeros(T), np.zeros(T)
+    ratio, coef = np.zeros(R), np.zeros(R)
+    scored = {i: [t for t in range(cs[i], cs[i + 1]) if 0 <= y[t] < V] for i in used}
+    for i in used:
+        for t in range(cs[i], cs[i + 1]):
+            z = W @ H[t]
+            lse[t] = z.max() + np.log(np.exp(z - z.max()).sum())
+        for t in scored[i]:
+            logp[t] = W[y[t]] @ H[t] - lse[t]
+        ratio[i] = sum(logp[t] - (0.0 if ref is None else float(ref[t])) for t in scored[i])
+        if mean and scored[i]:
+            ratio[i] /= len(scored[i])
+    m = np.zeros(len(pairs))
+    loss = 0.0
+    for p in counted:
+        c, r = pairs[p]
+        u = 1.0 / len(counted) if weight is None else float(weight[p])
+        m[p] = beta * (ratio[c] - ratio[r]) - margin
+        each, slope = pref_pair(kind, m[p], smoothing)
+        loss += u * each
+        for i, sign in ((c, 1.0), (r, -1.0)):
+            coef[i] += sign * u * beta * slope / (len(scored[i]) if mean and scored[i] else 1)
+    n = max(1, len(counted))
+    out = dict(logp=logp, lse=lse, ratio=ratio, margin=m, coef=coef, loss=loss,
+               metrics=np.array([sum(ratio[pairs[p][0]] > ratio[pairs[p][1]] for p in counted) / n,
+                                 beta * sum(ratio[pairs[p][0]] for p in counted) / n,
+                                 beta * sum(ratio[pairs[p][1]] for p in counted) / n, len(counted)]))
+    if grads:
+        dz = np.zeros((T, V))
+        for i in used:
+            for t in scored[i]:
+                dz[t] = -coef[i] * np.exp(W @ H[t] - lse[t])
+                dz[t, y[t]] += coef[i]
+        out.update(dz=dz, dH=dz @ W, dW=dz.T @ H)
+    return out
+
+
 # ---- AdamW ------------------------------------------------------------------------------------
 E4M3 = np.array([(8 * (c > 7) + c % 8) * 2.0 ** (max(c // 8, 1) - 10) for c in range(127)])          # magnitudes of codes 0 .. 126
 E4M4 = np.array([(16 * (c > 15) + c % 16) * 2.0 ** (max(c // 16, 1) - 11) for c in range(256)])

@@ -23,6 +23,8 @@ AERO_BF16, AERO_FP32 = 0, 1
 AERO_NO_TOKEN = -1
 AERO_ST_BAD_TARGET, AERO_ST_BAD_OFFSETS, AERO_ST_BAD_REWARD, AERO_ST_EMPTY_ROLLOUT, AERO_ST_TIMEOUT = 1, 2, 4, 8, 16
 AERO_ST_RANGE = 32
+AERO_ST_BAD_PAIR = 64
+AERO_PREF_LOGISTIC, AERO_PREF_SQUARE, AERO_PREF_HINGE = 0, 1, 2
 
 EXPORTS = [
     "aero_version", "aero_error_string", "aero_cfg_default", "aero_create", "aero_destroy",
@@ -40,6 +42,8 @@ EXPORTS = [
     "aero_distill_bwd_workspace_bytes", "aero_distill_fwd_bwd_workspace_bytes",
     "aero_adamw_cfg_default", "aero_adamw_workspace_bytes", "aero_adamw_step", "aero_adamw_states",
     "aero_fp4_code_bytes", "aero_fp4_scale_bytes", "aero_quantize_fp4", "aero_dequantize_fp4", "aero_lmhead_fp4",
+    "aero_pref_cfg_default", "aero_pref_fwd_workspace_bytes", "aero_pref_fwd", "aero_pref_bwd_workspace_bytes", "aero_pref_bwd",
+    "aero_pref_fwd_bwd_workspace_bytes", "aero_pref_fwd_bwd",
 ]
 
 
@@ -57,6 +61,10 @@ class AeroCfg(C.Structure):
 
 class AeroAllocCfg(C.Structure):
     _fields_ = [("n_extra", C.c_int32), ("k_max", C.c_int32), ("n_max", C.c_int32), ("n_budget", C.c_int32)]
+
+
+class AeroPrefCfg(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("mean", C.c_int32), ("beta", C.c_float), ("margin", C.c_float), ("label_smoothing", C.c_float)]
 
 
 class AeroAdamWCfg(C.Structure):
@@ -160,6 +168,18 @@ def load_library():
     lib.aero_adamw_workspace_bytes.argtypes = [i32]
     lib.aero_adamw_step.argtypes = [vp, ap, i32, tp, vp, vp, vp, vp, sz]
     lib.aero_adamw_states.argtypes = [vp, i32, tp, i32, C.POINTER(vp), C.POINTER(vp)]
+    pp = C.POINTER(AeroPrefCfg)
+    lib.aero_pref_cfg_default.restype = None
+    lib.aero_pref_cfg_default.argtypes = [pp]
+    lib.aero_pref_fwd_workspace_bytes.restype = sz
+    lib.aero_pref_fwd_workspace_bytes.argtypes = [i64, i32, i32, i32, i32]
+    lib.aero_pref_bwd_workspace_bytes.restype = sz
+    lib.aero_pref_bwd_workspace_bytes.argtypes = [i64, i32, i32, i32, i64, i32]
+    lib.aero_pref_fwd_bwd_workspace_bytes.restype = sz
+    lib.aero_pref_fwd_bwd_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i64, i32]
+    lib.aero_pref_fwd.argtypes = [vp, cp, pp, i64, i32, i32, i32, i32] + [vp] * 15 + [sz]
+    lib.aero_pref_bwd.argtypes = [vp, cp, i64, i32, i32, i32] + [vp] * 6 + [f32, vp, vp, i32, C.c_int, vp, sz]
+    lib.aero_pref_fwd_bwd.argtypes = [vp, cp, pp, i64, i32, i32, i32, i32] + [vp] * 14 + [f32, vp, vp, i32, C.c_int, vp, sz]
     lib.aero_fp4_code_bytes.restype = sz
     lib.aero_fp4_code_bytes.argtypes = [i64, i32]
     lib.aero_fp4_scale_bytes.restype = sz
@@ -207,6 +227,16 @@ def adamw_cfg_default(**over) -> AeroAdamWCfg:
             raise AttributeError(k)
         setattr(ac, k, v)
     return ac
+
+
+def pref_cfg_default(**over) -> AeroPrefCfg:
+    pc = AeroPrefCfg()
+    load_library().aero_pref_cfg_default(C.byref(pc))
+    for k, v in over.items():
+        if not hasattr(pc, k):
+            raise AttributeError(k)
+        setattr(pc, k, v)
+    return pc
 
 
 class AdamWPlan:
@@ -729,6 +759,62 @@ class Context:
                                      self._arg(o, out_dtype, (T, V), "out"))
         _check(rc, "aero_lmhead_q8")
         return o
+
+    # ---- preference loss on pairs of rollouts -----------------------------------------------------
+    def _pref(self, cfg, H, W, y, cs):
+        (T, d), V, R = H.shape, W.shape[0], cs.numel() - 1
+        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
+        ptrs = (self._arg(H, dt, (T, d), "H"), self._arg(W, dt, (V, d), "W"), self._arg(y, torch.int32, (T,), "y"))
+        return (T, d, V, R), dt, ptrs, self._arg(cs, torch.int64, (R + 1,), "cs")
+
+    @staticmethod
+    def _pref_chunk(T, R, chunk_tokens):
+        # by default all of a batch that fits four waves of token tiles: rows in one chunk save a pass over the logits
+        return chunk_tokens if chunk_tokens is not None else min(T + 128 * (R + 2), 4 * 148 * 128)
+
+    def _pref_call(self, cfg, H, W, y, cs, pairs, ref_logp, pair_weight, out):
+        (T, d, V, R), dt, ptrs, pcs = self._pref(cfg, H, W, y, cs)
+        P = pairs.shape[0]
+        o = dict(out) if out is not None else {}
+        outs = []
+        for name, n in (("logp", T), ("lse", T), ("ratio", R), ("margin", P), ("coef", R), ("loss", 1), ("metrics", 4)):
+            if name not in o:
+                o[name] = self._new((n,), torch.float32)
+            outs.append(self._arg(o[name], torch.float32, (n,), name))
+        return (T, d, V, R, P), dt, (*ptrs, self._arg(ref_logp, torch.float32, (T,), "ref_logp"), pcs,
+                                     self._arg(pairs, torch.int32, (P, 2), "pairs"),
+                                     self._arg(pair_weight, torch.float32, (P,), "pair_weight")), o, outs
+
+    def pref_fwd(self, cfg, pc, H, W, y, cs, pairs, ref_logp=None, pair_weight=None, out=None):
+        """aero_pref_fwd: a dict of logp, lse [T], ratio, coef [R], margin [P], loss [1] and metrics [4]."""
+        shape, _, ptrs, o, outs = self._pref_call(cfg, H, W, y, cs, pairs, ref_logp, pair_weight, out)
+        ws = self._scratch(self.lib.aero_pref_fwd_workspace_bytes(*shape))
+        _check(self.lib.aero_pref_fwd(self.h, C.byref(cfg), C.byref(pc), *shape, *ptrs, *outs, ws.data_ptr(), ws.numel()),
+               "aero_pref_fwd")
+        return o
+
+    def pref_bwd(self, cfg, H, W, y, cs, coef, lse, grad_scale=1.0, dH=None, dW=None, dw_dtype=torch.float32, accumulate_dW=False,
+                 chunk_tokens=None):
+        """aero_pref_bwd: (dH, dW) from the forward's coef and lse."""
+        (T, d, V, R), dt, ptrs, pcs = self._pref(cfg, H, W, y, cs)
+        dH, dW, pH, pW = self._distill_grads((T, d, V, R, 1), dt, dH, dW, dw_dtype, accumulate_dW)
+        dwt = AERO_FP32 if dw_dtype == torch.float32 else AERO_BF16
+        ws = self._scratch(self.lib.aero_pref_bwd_workspace_bytes(T, d, V, R, self._pref_chunk(T, R, chunk_tokens), dwt))
+        _check(self.lib.aero_pref_bwd(self.h, C.byref(cfg), T, d, V, R, *ptrs, pcs, self._arg(coef, torch.float32, (R,), "coef"),
+                                      self._arg(lse, torch.float32, (T,), "lse"), grad_scale, pH, pW, dwt,
+                                      1 if accumulate_dW else 0, ws.data_ptr(), ws.numel()), "aero_pref_bwd")
+        return dH, dW
+
+    def pref_fwd_bwd(self, cfg, pc, H, W, y, cs, pairs, ref_logp=None, pair_weight=None, out=None, grad_scale=1.0, dH=None, dW=None,
+                     dw_dtype=torch.float32, accumulate_dW=False, chunk_tokens=None):
+        """aero_pref_fwd_bwd: (forward outputs dict, dH, dW) in one call."""
+        shape, dt, ptrs, o, outs = self._pref_call(cfg, H, W, y, cs, pairs, ref_logp, pair_weight, out)
+        dH, dW, pH, pW = self._distill_grads((*shape[:4], 1), dt, dH, dW, dw_dtype, accumulate_dW)
+        dwt = AERO_FP32 if dw_dtype == torch.float32 else AERO_BF16
+        ws = self._scratch(self.lib.aero_pref_fwd_bwd_workspace_bytes(*shape, self._pref_chunk(shape[0], shape[3], chunk_tokens), dwt))
+        _check(self.lib.aero_pref_fwd_bwd(self.h, C.byref(cfg), C.byref(pc), *shape, *ptrs, *outs, grad_scale, pH, pW, dwt,
+                                          1 if accumulate_dW else 0, ws.data_ptr(), ws.numel()), "aero_pref_fwd_bwd")
+        return o, dH, dW
 
     # ---- rows in 4-bit floating point ------------------------------------------------------------
     def _fp4(self, r, name):

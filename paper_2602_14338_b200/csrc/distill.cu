@@ -19,6 +19,7 @@
 // entries, which are most of dz, reach dW with the rounding of dz alone, as the one-call step's dW then
 // is 2.4e-3 of its norm off instead of 2.9e-3.  The price is a second rounding of the softmax part, p~ and dz: where
 // a list holds little weight dH is 2.6e-3 of its norm off, 1.6e-3 with one.)
+#include "distill.cuh"
 #include "entry.cuh"
 #include "gemm_bwd_kernel.cuh"
 #include "lmhead_kernel.cuh"
@@ -902,6 +903,7 @@ struct Call {
   const int64_t* cs;
   const float* w;
   const uint8_t* keep;
+  AeroListed ex;
 };
 
 int check_call(const aero_cfg* cfg, const Call& c, const void* ws) {
@@ -988,6 +990,7 @@ int fwd_fp32(const Call& c, const Ws& s, float* lse, float* kl, float* loss, flo
     if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T, c.V))) return rc;
     if ((rc = rows_fp32(a, ctx))) return rc;
   }
+  if (!loss) return AERO_OK;
   return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
 }
 
@@ -1035,6 +1038,10 @@ int lmhead_launch(const Call& c, const Ws& s, lmhead::Params p, const CUtensorMa
   p.w_hint = aero_w_hint(ctx, mode != kFwd); p.k_zigzag = aero_k_zigzag(ctx);
   auto kern = mode == kFwd ? lmhead::lmhead_kernel<lmhead::MODE_FWD>
                            : (mode == kBoth ? lmhead::lmhead_kernel<lmhead::MODE_FWD_P> : lmhead::lmhead_kernel<lmhead::MODE_DZ>);
+  if (c.ex.gain && mode != kBwd) {
+    kern = mode == kFwd ? lmhead::lmhead_kernel<lmhead::MODE_FWD_GAIN> : lmhead::lmhead_kernel<lmhead::MODE_FWD_P_GAIN>;
+    p.z_gain = lmhead::kCut * (float)(c.d / 16);
+  }
   AERO_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lmhead::SMEM_BYTES));
   const int pairs = ctx->sm_count / 2 > 0 ? ctx->sm_count / 2 : 1;
   kern<<<2 * pairs, lmhead::THREADS, lmhead::SMEM_BYTES, ctx->stream>>>(tmH, tmW, tmDZ, p);
@@ -1091,6 +1098,7 @@ int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float
     ctx->launches += 2;
     AERO_CUDA_TRY(cudaGetLastError());
   }
+  if (!loss) return AERO_OK;
   return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
 }
 
@@ -1153,6 +1161,16 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
       p.range_rows = s.range_rows; p.range_count = s.range_count; p.range_seen = s.range_seen; p.range_cap = kRangeCap;
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBoth))) return rc;
       a.xstate = s.xstate;
+      if (c.ex.between) {
+        // the rows' log-probs alone; then their weights, which depend on all of them; then the pass below as ever
+        RowsArgs first = a;
+        first.ls.entry = nullptr; first.ls.partials = nullptr; first.g = nullptr; first.Hl = nullptr;
+        distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(first);
+        ctx->launches += 1;
+        if ((rc = c.ex.between(c.ex.arg, s.wrow))) return rc;
+        a.ls.kl = nullptr; a.ls.partials = nullptr;
+        b.a = a;
+      }
       distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);
       distill_scale_kernel<<<dim3((unsigned)b.nvt, (unsigned)(end - begin < 64 ? end - begin : 64)), 256, 0, ctx->stream>>>(b);
       RangeArgs f = {};
@@ -1220,6 +1238,81 @@ int grads_call(const Call& c, const Ws& s, Mode mode, const Room& room, float* l
 
 }  // namespace
 
+int aero_distill_fwd_listed(const AeroListed& ex, aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V,
+                            int32_t R, int32_t K, const void* H, const void* W, const int32_t* ids, const float* logits,
+                            const float* teacher_lse, const int64_t* cs, const float* w, const uint8_t* keep, float* lse,
+                            float* kl, float* loss, float* metrics, void* workspace, size_t workspace_bytes) {
+  const Call c = {ctx, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep, ex};
+  int rc = check_call(cfg, c, workspace);
+  if (rc) return rc;
+  if (T > 0 && (!lse || !kl)) return AERO_ERR_INVALID;
+  if (workspace_bytes < aero_distill_fwd_workspace_bytes(T, d, V, R, K)) return AERO_ERR_WORKSPACE;
+  if ((rc = aero_check_ctx(ctx))) return rc;
+  const Ws s = carve(workspace, T, d, V, R, K, kFwd);
+  return cfg->dtype == AERO_FP32 ? fwd_fp32(c, s, lse, kl, loss, metrics) : fwd_tc(c, s, lse, kl, loss, metrics);
+}
+
+int aero_distill_bwd_listed(const AeroListed& ex, aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V,
+                            int32_t R, int32_t K, const void* H, const void* W, const int32_t* ids, const float* logits,
+                            const float* teacher_lse, const int64_t* cs, const float* w, const uint8_t* keep,
+                            const float* lse, float grad_scale, void* dH, void* dW, int32_t dw_dtype, int accumulate_dW,
+                            void* workspace, size_t workspace_bytes) {
+  const Call c = {ctx, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep, ex};
+  int rc = check_call(cfg, c, workspace);
+  if (rc) return rc;
+  if (!dW || (T > 0 && (!lse || !dH))) return AERO_ERR_INVALID;
+  if ((rc = check_dw(cfg, dH, dW, dw_dtype, accumulate_dW))) return rc;
+  const Ws s = carve(workspace, T, d, V, R, K, kBwd);
+  if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
+  const Room room(workspace_bytes - s.head_bytes, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count);
+  if (cfg->dtype == AERO_BF16 && room.tpc < 1) return AERO_ERR_WORKSPACE;
+  if ((rc = aero_check_ctx(ctx))) return rc;
+  if (cfg->dtype == AERO_FP32)
+    return bwd_fp32(c, s, lse, grad_scale, static_cast<float*>(dH), static_cast<float*>(dW), accumulate_dW);
+  return grads_call(c, s, kBwd, room, const_cast<float*>(lse), nullptr, grad_scale, dH, dW, dw_dtype, accumulate_dW);
+}
+
+int aero_distill_fwd_bwd_listed(const AeroListed& ex, aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V,
+                                int32_t R, int32_t K, const void* H, const void* W, const int32_t* ids, const float* logits,
+                                const float* teacher_lse, const int64_t* cs, const float* w, const uint8_t* keep, float* lse,
+                                float* kl, float* loss, float* metrics, float grad_scale, void* dH, void* dW,
+                                int32_t dw_dtype, int accumulate_dW, void* workspace, size_t workspace_bytes) {
+  const Call c = {ctx, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep, ex};
+  int rc = check_call(cfg, c, workspace);
+  if (rc) return rc;
+  if (!dW || (T > 0 && (!lse || !kl || !dH))) return AERO_ERR_INVALID;
+  if ((rc = check_dw(cfg, dH, dW, dw_dtype, accumulate_dW))) return rc;
+  const Ws s = carve(workspace, T, d, V, R, K, kBoth);
+  if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
+  const Room room(workspace_bytes - s.head_bytes, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count);
+  if (cfg->dtype == AERO_BF16 && room.tpc < 1) return AERO_ERR_WORKSPACE;
+  if ((rc = aero_check_ctx(ctx))) return rc;
+  if (cfg->dtype == AERO_FP32) {
+    if ((rc = fwd_fp32(c, s, lse, kl, loss, metrics))) return rc;
+    return bwd_fp32(c, s, lse, grad_scale, static_cast<float*>(dH), static_cast<float*>(dW), accumulate_dW);
+  }
+  if ((rc = grads_call(c, s, kBoth, room, lse, kl, grad_scale, dH, dW, dw_dtype, accumulate_dW)) || !loss) return rc;
+  return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
+}
+
+int aero_distill_check(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, const void* H,
+                       const void* W, const int32_t* ids, const float* logits, const int64_t* cs, const float* w, const uint8_t* keep,
+                       const void* workspace) {
+  return check_call(cfg, {ctx, T, d, V, R, K, H, W, ids, logits, nullptr, cs, w, keep, {}}, workspace);
+}
+
+int aero_distill_check_grads(const aero_cfg* cfg, int64_t T, const void* dH, const void* dW, int32_t dw_dtype, int accumulate_dW) {
+  if (!dW || (T > 0 && !dH)) return AERO_ERR_INVALID;
+  return check_dw(cfg, dH, dW, dw_dtype, accumulate_dW);
+}
+
+bool aero_distill_one_chunk(const aero_ctx* ctx, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int32_t dw_dtype,
+                            size_t workspace_bytes) {
+  const size_t head = carve(nullptr, T, d, V, R, K, kBoth).head_bytes;
+  return workspace_bytes >= head &&
+         Room(workspace_bytes - head, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count).tpc >= max_tiles_of(T, R);
+}
+
 extern "C" {
 
 size_t aero_distill_fwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t K) {
@@ -1242,14 +1335,9 @@ int aero_distill_fwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, i
                      const int64_t* cs, const float* w, const uint8_t* keep,
                      float* lse, float* kl, float* loss, float* metrics, void* workspace, size_t workspace_bytes) {
   AeroRange nv("aero_distill_fwd");
-  const Call c = {ctx, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep};
-  int rc = check_call(cfg, c, workspace);
-  if (rc) return rc;
-  if (!loss || (T > 0 && (!lse || !kl))) return AERO_ERR_INVALID;
-  if (workspace_bytes < aero_distill_fwd_workspace_bytes(T, d, V, R, K)) return AERO_ERR_WORKSPACE;
-  if ((rc = aero_check_ctx(ctx))) return rc;
-  const Ws s = carve(workspace, T, d, V, R, K, kFwd);
-  return cfg->dtype == AERO_FP32 ? fwd_fp32(c, s, lse, kl, loss, metrics) : fwd_tc(c, s, lse, kl, loss, metrics);
+  if (!loss) return AERO_ERR_INVALID;
+  return aero_distill_fwd_listed({}, ctx, cfg, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep, lse, kl, loss,
+                                 metrics, workspace, workspace_bytes);
 }
 
 int aero_distill_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K,
@@ -1257,19 +1345,8 @@ int aero_distill_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, i
                      const int64_t* cs, const float* w, const uint8_t* keep, const float* lse, float grad_scale,
                      void* dH, void* dW, int32_t dw_dtype, int accumulate_dW, void* workspace, size_t workspace_bytes) {
   AeroRange nv("aero_distill_bwd");
-  const Call c = {ctx, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep};
-  int rc = check_call(cfg, c, workspace);
-  if (rc) return rc;
-  if (!dW || (T > 0 && (!lse || !dH))) return AERO_ERR_INVALID;
-  if ((rc = check_dw(cfg, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  const Ws s = carve(workspace, T, d, V, R, K, kBwd);
-  if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
-  const Room room(workspace_bytes - s.head_bytes, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count);
-  if (cfg->dtype == AERO_BF16 && room.tpc < 1) return AERO_ERR_WORKSPACE;
-  if ((rc = aero_check_ctx(ctx))) return rc;
-  if (cfg->dtype == AERO_FP32)
-    return bwd_fp32(c, s, lse, grad_scale, static_cast<float*>(dH), static_cast<float*>(dW), accumulate_dW);
-  return grads_call(c, s, kBwd, room, const_cast<float*>(lse), nullptr, grad_scale, dH, dW, dw_dtype, accumulate_dW);
+  return aero_distill_bwd_listed({}, ctx, cfg, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep, lse, grad_scale,
+                                 dH, dW, dw_dtype, accumulate_dW, workspace, workspace_bytes);
 }
 
 int aero_distill_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K,
@@ -1279,22 +1356,9 @@ int aero_distill_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t 
                          void* dH, void* dW, int32_t dw_dtype, int accumulate_dW, void* workspace,
                          size_t workspace_bytes) {
   AeroRange nv("aero_distill_fwd_bwd");
-  const Call c = {ctx, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep};
-  int rc = check_call(cfg, c, workspace);
-  if (rc) return rc;
-  if (!loss || !dW || (T > 0 && (!lse || !kl || !dH))) return AERO_ERR_INVALID;
-  if ((rc = check_dw(cfg, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  const Ws s = carve(workspace, T, d, V, R, K, kBoth);
-  if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
-  const Room room(workspace_bytes - s.head_bytes, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count);
-  if (cfg->dtype == AERO_BF16 && room.tpc < 1) return AERO_ERR_WORKSPACE;
-  if ((rc = aero_check_ctx(ctx))) return rc;
-  if (cfg->dtype == AERO_FP32) {
-    if ((rc = fwd_fp32(c, s, lse, kl, loss, metrics))) return rc;
-    return bwd_fp32(c, s, lse, grad_scale, static_cast<float*>(dH), static_cast<float*>(dW), accumulate_dW);
-  }
-  if ((rc = grads_call(c, s, kBoth, room, lse, kl, grad_scale, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
+  if (!loss) return AERO_ERR_INVALID;
+  return aero_distill_fwd_bwd_listed({}, ctx, cfg, T, d, V, R, K, H, W, ids, logits, teacher_lse, cs, w, keep, lse, kl, loss,
+                                     metrics, grad_scale, dH, dW, dw_dtype, accumulate_dW, workspace, workspace_bytes);
 }
 
 }  // extern "C"

@@ -102,3 +102,47 @@ def test_fp4_refusals(lib, fake):
         assert product(**{name: None}) == INVALID and product(**{name: P + 1}) == INVALID, name
     assert product(V=0) == INVALID and product(V=(1 << 30) + 1) == UNSUPPORTED
     assert product(dtype=B.AERO_FP32, out=P + 2) == INVALID
+
+
+def test_pref_refusals(lib, fake):
+    fwd_need = lib.aero_pref_fwd_workspace_bytes(40, 64, 10, 3, 4)
+    both_need = lib.aero_pref_fwd_bwd_workspace_bytes(40, 64, 10, 3, 4, 128, B.AERO_FP32)
+    bwd_need = lib.aero_pref_bwd_workspace_bytes(40, 64, 10, 3, 128, B.AERO_FP32)
+    assert 0 < fwd_need <= both_need and 0 < bwd_need <= both_need
+    assert lib.aero_pref_fwd_workspace_bytes(-1, 64, 10, 3, 4) == 0 and lib.aero_pref_fwd_workspace_bytes(40, 64, 10, 3, -1) == 0
+
+    def fwd(ctx=fake, c=None, pc=None, T=40, d=64, V=10, R=3, n=4, H=P, W=P, y=P, ref=P, cs=P, pairs=P, pw=None, logp=P, lse=P, ratio=P,
+            margin=P, coef=P, loss=P, ws=P, wsb=fwd_need):
+        pc = C.byref(pc if pc is not None else B.pref_cfg_default())
+        return lib.aero_pref_fwd(ctx, c or cfg(), pc, T, d, V, R, n, H, W, y, ref, cs, pairs, pw, logp, lse, ratio, margin, coef, loss, None,
+                                 ws, wsb)
+
+    def both(ctx=fake, c=None, pc=None, T=40, d=64, V=10, R=3, n=4, H=P, W=P, y=P, ref=P, cs=P, pairs=P, pw=None, logp=P, lse=P, ratio=P,
+             margin=P, coef=P, loss=P, dH=P, dW=P, dt=B.AERO_FP32, acc=0, ws=P, wsb=both_need):
+        pc = C.byref(pc if pc is not None else B.pref_cfg_default())
+        return lib.aero_pref_fwd_bwd(ctx, c or cfg(), pc, T, d, V, R, n, H, W, y, ref, cs, pairs, pw, logp, lse, ratio, margin, coef, loss,
+                                     None, 1.0, dH, dW, dt, acc, ws, wsb)
+
+    def bwd(ctx=fake, c=None, T=40, d=64, V=10, R=3, H=P, W=P, y=P, cs=P, coef=P, lse=P, dH=P, dW=P, dt=B.AERO_FP32, acc=0, ws=P,
+            wsb=bwd_need):
+        return lib.aero_pref_bwd(ctx, c or cfg(), T, d, V, R, H, W, y, cs, coef, lse, 1.0, dH, dW, dt, acc, ws, wsb)
+
+    for call in (fwd, both, bwd):
+        for name in ("ctx", "H", "W", "y", "cs", "lse", "coef", "ws"):
+            assert call(**{name: None}) == INVALID, name
+        assert call(T=-1) == INVALID and call(T=1 << 31) == INVALID and call(d=0) == INVALID and call(V=0) == INVALID and call(R=-1) == INVALID
+        assert call(d=65) == UNSUPPORTED and call(c=cfg(9)) == UNSUPPORTED and call(d=1088, c=cfg(B.AERO_FP32)) == UNSUPPORTED
+        assert call(H=P + 8) == INVALID and call(W=P + 2) == INVALID and call(ws=P + 16) == INVALID
+        assert call(wsb=255) == WORKSPACE
+    assert fwd(wsb=fwd_need - 1) == WORKSPACE and both(wsb=both_need - 1) == WORKSPACE and bwd(wsb=bwd_need - 1) == WORKSPACE
+    for call in (fwd, both):
+        for name in ("pairs", "logp", "ratio", "margin", "loss"):
+            assert call(**{name: None}) == INVALID, name
+        assert call(n=-1) == INVALID and call(pairs=P + 4) == INVALID and call(pc=B.pref_cfg_default(kind=3)) == UNSUPPORTED
+        for name, bad in (("beta", float("nan")), ("beta", float("inf")), ("margin", float("nan")), ("label_smoothing", -0.1),
+                          ("label_smoothing", 1.1), ("label_smoothing", float("nan"))):
+            assert call(pc=B.pref_cfg_default(**{name: bad})) == INVALID, name
+    for call in (both, bwd):
+        assert call(dH=None) == INVALID and call(dW=None) == INVALID and call(dH=P + 8) == INVALID and call(dW=P + 4) == INVALID
+        assert call(dt=4) == UNSUPPORTED and call(dt=B.AERO_BF16, acc=1) == INVALID
+        assert call(dt=B.AERO_BF16, c=cfg(B.AERO_FP32)) == UNSUPPORTED
