@@ -165,21 +165,21 @@ __device__ __forceinline__ void open_m(const Slot& t, const Span& s, float (&m)[
   for (int i = 0; i < kEach; i += 2) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(c[i] | c[i + 1] << 8), __NV_E4M3);
     const float2 f = __half22float2(__half2(h));
-    m[i] = f.x * scale;
-    m[i + 1] = f.y * scale;
+    m[i] = __fmul_rn(f.x, scale);
+    m[i + 1] = __fmul_rn(f.y, scale);
   }
 }
 __device__ __forceinline__ void close_m(const Slot& t, const Span& s, const float (&m)[kEach]) {
-  const float top = scale_top(warp_top(m)), inv = kTopM / top;
+  const float top = scale_top(warp_top(m)), inv = __fmul_rn(__frcp_rn(top), kTopM);
   uint8_t c[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; i += 2) {
-    const __nv_fp8x2_storage_t u = __nv_cvt_float2_to_fp8x2(make_float2(m[i] * inv, m[i + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+    const __nv_fp8x2_storage_t u = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(m[i], inv), __fmul_rn(m[i + 1], inv)), __NV_SATFINITE, __NV_E4M3);
     c[i] = (uint8_t)u;
     c[i + 1] = (uint8_t)(u >> 8);
   }
   store_codes(static_cast<uint8_t*>(t.m), s, c);
-  if (s.lane == 0) t.m_scale[s.e0 / kBlock] = top / kTopM;
+  if (s.lane == 0) t.m_scale[s.e0 / kBlock] = top * (1.f / kTopM);
 }
 // The root's codes are the upper bits of a float whose exponent is moved by 120, so that the smallest normal numbers of the
 // two formats fall together and the subnormal ones do too.
@@ -189,25 +189,25 @@ __device__ __forceinline__ void open_v(const Slot& t, const Span& s, float (&v)[
   const float scale = t.v_scale[s.e0 / kBlock];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const float r = __uint_as_float((uint32_t)c[i] << 19) * 0x1p120f * scale;
-    v[i] = r * r;
+    const float r = __fmul_rn(__uint_as_float((uint32_t)c[i] << 19) * 0x1p120f, scale);
+    v[i] = __fmul_rn(r, r);
   }
 }
 __device__ __forceinline__ void close_v(const Slot& t, const Span& s, const float (&v)[kEach]) {
   float r[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) r[i] = sqrtf(v[i]);
-  const float top = scale_top(warp_top(r)), inv = kTopV / top;
+  const float top = scale_top(warp_top(r)), inv = __fmul_rn(__frcp_rn(top), kTopV);
   uint8_t c[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const uint32_t b = __float_as_uint(r[i] * inv * 0x1p-120f);
+    const uint32_t b = __float_as_uint(__fmul_rn(r[i], inv) * 0x1p-120f);
     uint32_t code = min((b + 0x3ffffu + ((b >> 19) & 1u)) >> 19, 255u);      // to even
     if (r[i] > 0.f) code = max(code, 1u);           // a root that is not zero divides the step: it does not become zero
     c[i] = (uint8_t)code;
   }
   store_codes(static_cast<uint8_t*>(t.v), s, c);
-  if (s.lane == 0) t.v_scale[s.e0 / kBlock] = top / kTopV;
+  if (s.lane == 0) t.v_scale[s.e0 / kBlock] = top * (1.f / kTopV);
 }
 
 // The warps' spans of a launch, chunk by chunk.
@@ -317,9 +317,11 @@ __global__ void __launch_bounds__(kWarps * 32) adamw_step_kernel(const __grid_co
     const float lr = sc.lr * t.lr_scale, keep = 1.f - lr * t.weight_decay, rate = lr * sc.c1;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const float x = g[i] * sc.g_factor;
-      m[i] = fmaf(h.beta1, m[i], h.rest1 * x);
-      v[i] = fmaf(h.beta2, v[i], h.rest2 * (x * x));
+      const float x = __fmul_rn(g[i], sc.g_factor);
+      // (each operation rounded by itself: a compiler's choice of which product to fuse would decide, near the border of two codes,
+      // which of them an 8-bit state gets)
+      m[i] = __fadd_rn(__fmul_rn(h.beta1, m[i]), __fmul_rn(h.rest1, x));
+      v[i] = __fadd_rn(__fmul_rn(h.beta2, v[i]), __fmul_rn(__fmul_rn(h.rest2, x), x));
       p[i] = fmaf(keep, p[i], -rate * m[i] / (sqrtf(v[i] * sc.c2) + h.eps));
     }
     if (t.master) store32(t.master, s, p);

@@ -1306,6 +1306,13 @@ int aero_distill_check_grads(const aero_cfg* cfg, int64_t T, const void* dH, con
   return check_dw(cfg, dH, dW, dw_dtype, accumulate_dW);
 }
 
+bool aero_distill_bwd_fits(const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int32_t dw_dtype,
+                           size_t workspace_bytes) {
+  const size_t head = carve(nullptr, T, d, V, R, K, kBwd).head_bytes;
+  return workspace_bytes >= head &&
+         (cfg->dtype == AERO_FP32 || Room(workspace_bytes - head, T, d, V, R, dw_dtype == AERO_BF16, 0).tpc >= 1);
+}
+
 bool aero_distill_one_chunk(const aero_ctx* ctx, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int32_t dw_dtype,
                             size_t workspace_bytes) {
   const size_t head = carve(nullptr, T, d, V, R, K, kBoth).head_bytes;

@@ -34,6 +34,10 @@ int aero_distill_check(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d,
                        const void* workspace);
 int aero_distill_check_grads(const aero_cfg* cfg, int64_t T, const void* dH, const void* dW, int32_t dw_dtype, int accumulate_dW);
 
+// Whether the backward can run in so much workspace.
+bool aero_distill_bwd_fits(const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int32_t dw_dtype,
+                           size_t workspace_bytes);
+
 // Whether a one-call step with so much workspace takes all rows in one chunk.
 bool aero_distill_one_chunk(const aero_ctx* ctx, int64_t T, int32_t d, int32_t V, int32_t R, int32_t K, int32_t dw_dtype,
                             size_t workspace_bytes);

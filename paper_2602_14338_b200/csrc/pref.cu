@@ -344,7 +344,8 @@ int aero_pref_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int3
   if (!cfg || !workspace || (R > 0 && !coef) || (T > 0 && !lse)) return AERO_ERR_INVALID;
   int rc = aero_distill_check(ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, cs, s.w, s.keep, workspace);
   if (rc || (rc = aero_distill_check_grads(cfg, T, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  if (workspace_bytes < aero_pref_bwd_workspace_bytes(T, d, V, R, 128, dw_dtype)) return AERO_ERR_WORKSPACE;
+  if (workspace_bytes < s.head_bytes || !aero_distill_bwd_fits(cfg, T, d, V, R, 1, dw_dtype, workspace_bytes - s.head_bytes))
+    return AERO_ERR_WORKSPACE;
   if ((rc = aero_check_ctx(ctx))) return rc;
   AERO_CUDA_TRY(cudaMemsetAsync(s.zeros, 0, (size_t)T * 4, ctx->stream));
   if (R > 0) {
@@ -365,14 +366,17 @@ int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* p
   const Ws s = carve(workspace, T > 0 ? T : 0, R > 0 ? R : 0, P > 0 ? P : 0);
   int rc = check_call(ctx, cfg, pc, T, d, V, R, P, H, W, y, cs, pairs, logp, lse, ratio, margin, coef, loss, s, workspace);
   if (rc || (rc = aero_distill_check_grads(cfg, T, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  if (workspace_bytes < aero_pref_fwd_bwd_workspace_bytes(T, d, V, R, P, 128, dw_dtype)) return AERO_ERR_WORKSPACE;
+  if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
+  const size_t room = workspace_bytes - s.head_bytes;
+  const bool one_chunk = cfg->dtype == AERO_BF16 && T > 0 && R > 0 && aero_distill_one_chunk(ctx, T, d, V, R, 1, dw_dtype, room);
+  if (!one_chunk && (room < aero_distill_fwd_workspace_bytes(T, d, V, R, 1) || !aero_distill_bwd_fits(cfg, T, d, V, R, 1, dw_dtype, room)))
+    return AERO_ERR_WORKSPACE;
   if ((rc = aero_check_ctx(ctx))) return rc;
   Between b = {ctx, args_of(ctx, pc, T, V, R, P, y, ref_logp, cs, pairs, pair_weight, s, logp, ratio, margin, coef), loss, metrics};
-  const size_t room = workspace_bytes - s.head_bytes;
   AeroListed ex;
   ex.gain = true;
   if ((rc = begin(ctx, s, b.a))) return rc;
-  if (cfg->dtype == AERO_BF16 && T > 0 && R > 0 && aero_distill_one_chunk(ctx, T, d, V, R, 1, dw_dtype, room)) {
+  if (one_chunk) {
     ex.between = Between::call;
     ex.arg = &b;
     return aero_distill_fwd_bwd_listed(ex, ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, nullptr, cs, s.w, s.keep, lse, logp, nullptr,

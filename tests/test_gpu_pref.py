@@ -158,6 +158,20 @@ def test_shapes(ctx, T, R, V, d, P):
         check_grads(b, dH, dW, want, 1.0, "bf16")
 
 
+@pytest.mark.parametrize("dw", [torch.bfloat16, torch.float32])
+def test_workspaces_of_exactly_the_size_asked_for(ctx, dw):
+    """One chunk, several chunks: the call takes what its size function says (a bf16 dW of several chunks needs V d floats more)."""
+    T, d, V, R = 300, 256, 20000, 4
+    b = batch(T, d, V, [0, 80, 150, 230, 300], [(0, 1), (2, 3)], "bf16", seed=3)
+    cfg, pc = cfg_of("bf16"), B.pref_cfg_default()
+    want = oracle(b, beta=float(np.float32(0.1)))
+    for chunk in (128, 256, 384, 1 << 20):
+        out, dH, dW = ctx.pref_fwd_bwd(cfg, pc, *args(b), ref_logp=b["ref"], dw_dtype=dw, chunk_tokens=chunk)
+        check_grads(b, dH, dW, want, 1.0, "bf16")
+        dH, dW = ctx.pref_bwd(cfg, *args(b)[:4], out["coef"], out["lse"], dw_dtype=dw, chunk_tokens=chunk)
+        check_grads(b, dH, dW, want, 1.0, "bf16")
+
+
 def test_nothing_to_do(ctx):
     """No tokens, no pairs, no rollouts: a loss of its own, gradients of zero."""
     empty = torch.zeros(0, 2, dtype=torch.int32, device="cuda")
