@@ -253,7 +253,11 @@ __global__ void __launch_bounds__(256) fp4_values_kernel(ValueArgs a) {
 }
 
 // ---- the product ---------------------------------------------------------------------------------------------------
-constexpr int EPI_WARPS = 8, kShare = EPI_WARPS / 4, THREADS = (EPI_WARPS + 2) * 32;
+// Warps 0-7 epilogue (one vocabulary row per thread, two warps per quadrant of TMEM), warp 8 copies, warp 9 MMA, warps 10-13 scales:
+// each reads the groups of scales that have arrived and stores them to its quadrant's lanes (the tensor cores want all four
+// alike).  The asynchronous copy that brings 512 bytes to all quadrants, issued between the products, held these up by 60 cycles
+// each, 12 times for 4 products of 150 cycles (2048 tokens, d = 3584, V = 152064: 1008 us with it).
+constexpr int EPI_WARPS = 8, kShare = EPI_WARPS / 4, SCALE_WARPS = 4, THREADS = (EPI_WARPS + 2 + SCALE_WARPS) * 32;
 constexpr int kRowsN = 128, kPairN = 192;         // most tokens per tile
 constexpr int kRowBlock = 32;                     // fp4_rows_kernel: ranges of vocabulary rows are multiples of it
 constexpr int kMaxStages = 8, kMaxSets = 8;
@@ -263,9 +267,22 @@ constexpr size_t kRing = 204 * 1024;
 template <int STAGES>
 struct Ctl {
   uint64_t full[STAGES], empty[STAGES], tfull[2], tempty[2];
+  uint64_t sfull[STAGES];       // pair kernel: a stage's scales have arrived in this CTA
+  uint64_t scales[STAGES];      // scales are in TMEM: of a stage (rows), of a set (pair)
   uint32_t tmem_base;
   int abort;
 };
+// GROUPS groups of 512 bytes of scales (this thread's 16 bytes of each) to 4 columns each of this warp's quadrant
+template <int GROUPS>
+__device__ __forceinline__ void scales_to_tmem(uint32_t taddr, const uint8_t* smem, int lane) {
+  uint32_t r[4 * GROUPS];
+#pragma unroll
+  for (int g = 0; g < GROUPS; ++g) {
+    const uint4 v = *reinterpret_cast<const uint4*>(smem + g * kGroupBytes + lane * 16);
+    r[4 * g] = v.x; r[4 * g + 1] = v.y; r[4 * g + 2] = v.z; r[4 * g + 3] = v.w;
+  }
+  tc::tmem_st_32x32<4 * GROUPS>(taddr, r);
+}
 constexpr size_t R_SMEM = 1024 + kRing + sizeof(Ctl<kMaxStages>);
 
 struct Operand {
@@ -330,7 +347,11 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
   auto* ctl = reinterpret_cast<Ctl<kMaxStages>*>(smem + (size_t)stages * per * slab_bytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < stages; ++s) { tc::mbar_init(&ctl->full[s], 1); tc::mbar_init(&ctl->empty[s], 1); }
+    for (int s = 0; s < stages; ++s) {
+      tc::mbar_init(&ctl->full[s], 1);
+      tc::mbar_init(&ctl->empty[s], 1);
+      tc::mbar_init(&ctl->scales[s], SCALE_WARPS);
+    }
     for (int b = 0; b < 2; ++b) { tc::mbar_init(&ctl->tfull[b], 1); tc::mbar_init(&ctl->tempty[b], EPI_WARPS); }
     ctl->abort = 0;
     tc::fence_barrier_init();
@@ -384,19 +405,15 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
         if (!tc::mbar_wait(&ctl->tempty[buf], ((at >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
         tc::tc_fence_after();
         for (int kb = 0; kb < nkb; kb += per) {
-          if (!tc::mbar_wait(&ctl->full[s], ph, abort_flag)) { ok = false; break; }
+          // (the scales' warps have waited for the whole stage)
+          if (!tc::mbar_wait(&ctl->scales[s], ph, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
           // (a tile of fewer than 128 rows leaves older codes in the other rows of A: their accumulator rows are not read)
           const int nk = min(per, nkb - kb);
           for (int k = 0; k < nk; ++k) {
-            const uint32_t a_addr = tc::smem_u32(smem + (size_t)(s * per + k) * slab_bytes), s_addr = a_addr + kTileBytes + b_slab;
+            const uint32_t a_addr = tc::smem_u32(smem + (size_t)(s * per + k) * slab_bytes);
             // each place of the ring has scale columns of its own
             const uint32_t sfa = tmem_base + kScaleCols + (uint32_t)(s * per + k) * kSetCols, sfb = sfa + 4 * kGroups;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-              tc::tmem_copy_scales<false>(sfa + 4 * g, tc::make_scale_desc(s_addr + g * kGroupBytes));
-              tc::tmem_copy_scales<false>(sfb + 4 * g, tc::make_scale_desc(s_addr + kScales + g * kGroupBytes));
-            }
             const uint64_t adesc = tc::make_smem_desc(a_addr, 16, 1024), bdesc = tc::make_smem_desc(a_addr + kTileBytes, 16, 1024);
 #pragma unroll
             for (int kk = 0; kk < kSlab / 64; ++kk) {
@@ -410,6 +427,28 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
           if (++s == stages) { s = 0; ph ^= 1u; }
         }
         if (ok) tc::umma_commit(&ctl->tfull[buf]);
+      }
+    }
+  } else if (warp >= EPI_WARPS + 2) {
+    const int quad = warp & 3;                   // (a warp reaches the lanes of its number mod 4)
+    int s = 0;
+    uint32_t ph = 0;
+    bool ok = true;
+    for (int b = b0; ok && b < b1; b += step(b)) {
+      for (int kb = 0; kb < nkb; kb += per) {
+        if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->full[s], ph, abort_flag))) { ok = false; break; }
+        const int nk = min(per, nkb - kb);
+        for (int k = 0; k < nk; ++k) {
+          const uint8_t* from = smem + (size_t)(s * per + k) * slab_bytes + kTileBytes + b_slab;
+          const uint32_t to = tmem_base + ((uint32_t)(quad * 32) << 16) + kScaleCols + (uint32_t)(s * per + k) * kSetCols;
+          scales_to_tmem<kGroups>(to, from, lane);
+          scales_to_tmem<kGroups>(to + 4 * kGroups, from + kScales, lane);
+        }
+        tc::tmem_st_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(&ctl->scales[s]);
+        if (++s == stages) { s = 0; ph ^= 1u; }
       }
     }
   } else {
@@ -460,12 +499,18 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   constexpr int kGroups = groups_per_slab(BLOCK);
   constexpr uint32_t kStage = pair_stage(BLOCK), kScales = kGroups * kGroupBytes, kSetCols = 12 * kGroups;
+  constexpr int kSets = 2;                            // of scale columns, behind the accumulators (5 in block 32: no faster)
   auto* ctl = reinterpret_cast<Ctl<PSTAGES>*>(smem + (size_t)PSTAGES * kStage);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_ctarank();        // 0 issues the MMAs of the pair
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
   if (threadIdx.x == 0) {
-    for (int s = 0; s < PSTAGES; ++s) { tc::mbar_init(&ctl->full[s], 1); tc::mbar_init(&ctl->empty[s], 1); }
+    for (int s = 0; s < PSTAGES; ++s) {
+      tc::mbar_init(&ctl->full[s], 1);
+      tc::mbar_init(&ctl->empty[s], 1);
+      tc::mbar_init(&ctl->sfull[s], 1);
+    }
+    for (int k = 0; k < kSets; ++k) tc::mbar_init(&ctl->scales[k], 2 * SCALE_WARPS);
     for (int b = 0; b < 2; ++b) { tc::mbar_init(&ctl->tfull[b], 1); tc::mbar_init(&ctl->tempty[b], 2 * EPI_WARPS); }
     ctl->abort = 0;
     tc::fence_barrier_init();
@@ -488,7 +533,7 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       uint32_t it = 0;
       bool ok = true;
       const int pieces = p.n / 2 / kPiece;
-      const uint32_t bytes = 2 * (kTileBytes + (uint32_t)p.n / 2 * kRowBytes + 3 * kScales);
+      const uint32_t bytes = 2 * (kTileBytes + (uint32_t)p.n / 2 * kRowBytes);
       for (long long u = pair; ok && u < units; u += npairs) {
         const int tile = (int)(u / p.n_tok) * 2 + (int)rank, t0 = (int)(u % p.n_tok) * p.n, th = t0 + (int)rank * (p.n / 2);
         for (int kb = 0; kb < nkb; ++kb, ++it) {
@@ -505,9 +550,10 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
             tc::tma_load_2d_pair(at + i * kPiece * kRowBytes, &tmH, 0, (t / kTile * nkb + kb) * kTile + t % kTile, full0);
           }
           at += kPairN / 2 * kRowBytes;
-          tc::tma_load_2d_pair(at, &tmWs, 0, (tile * nkb + kb) * kGroups, full0);
+          tc::mbar_arrive_expect_tx(&ctl->sfull[s], 3 * kScales);
+          tc::tma_load_2d(at, &tmWs, 0, (tile * nkb + kb) * kGroups, &ctl->sfull[s]);
           for (int i = 0; i < 2; ++i)
-            tc::tma_load_2d_pair(at + (1 + i) * kScales, &tmHs, 0, ((t0 / kTile + i) * nkb + kb) * kGroups, full0);
+            tc::tma_load_2d(at + (1 + i) * kScales, &tmHs, 0, ((t0 / kTile + i) * nkb + kb) * kGroups, &ctl->sfull[s]);
         }
       }
     }
@@ -523,28 +569,56 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         tc::tc_fence_after();
         for (int kb = 0; kb < nkb; ++kb, ++it) {
           const int s = it % PSTAGES;
-          if (!tc::mbar_wait(&ctl->full[s], (it / PSTAGES) & 1u, abort_flag)) { ok = false; break; }
+          if (!tc::mbar_wait(&ctl->full[s], (it / PSTAGES) & 1u, abort_flag) ||
+              !tc::mbar_wait(&ctl->scales[it % kSets], (it / kSets) & 1u, abort_flag)) { ok = false; break; }
           tc::tc_fence_after();
           const uint32_t a_addr = tc::smem_u32(smem + (size_t)s * kStage), b_addr = a_addr + kTileBytes;
-          const uint32_t s_addr = b_addr + kPairN / 2 * kRowBytes;
-          const uint32_t sfa = tmem_base + kPairAccCols + (it & 1u) * kSetCols, sfb = sfa + 4 * kGroups;
-#pragma unroll
-          for (int g = 0; g < kGroups; ++g) {
-            tc::tmem_copy_scales<true>(sfa + 4 * g, tc::make_scale_desc(s_addr + g * kGroupBytes));
-            tc::tmem_copy_scales<true>(sfb + 8 * g, tc::make_scale_desc(s_addr + kScales + g * kGroupBytes));
-            tc::tmem_copy_scales<true>(sfb + 8 * g + 4, tc::make_scale_desc(s_addr + 2 * kScales + g * kGroupBytes));
-          }
+          const uint32_t sfa = tmem_base + kPairAccCols + (it % kSets) * kSetCols, sfb = sfa + 4 * kGroups + shift;
           const uint64_t adesc = tc::make_smem_desc(a_addr, 16, 1024), bdesc = tc::make_smem_desc(b_addr, 16, 1024);
 #pragma unroll
           for (int kk = 0; kk < kSlab / 64; ++kk) {
             const int g = kk * kGroups / 4;
             const uint32_t idesc = tc::make_idesc_fp4(2 * kTile, p.n, BLOCK == 32, BLOCK == 32 ? 2 * (kk & 1) : 0);
             tc::umma_fp4<BLOCK, true>(tmem_base + buf * kPairN, adesc + 2u * kk, bdesc + 2u * kk, idesc, sfa + 4 * g,
-                                      sfb + 8 * g + shift, (kb | kk) != 0 ? 1u : 0u);
+                                      sfb + 8 * g, (kb | kk) != 0 ? 1u : 0u);
           }
           tc::umma_commit_pair(&ctl->empty[s], 3);     // frees the stage in both CTAs when these MMAs retire
         }
         if (ok) tc::umma_commit_pair(&ctl->tfull[buf], 3);
+      }
+    }
+  } else if (warp >= EPI_WARPS + 2) {
+    const int quad = warp & 3;                   // (a warp reaches the lanes of its number mod 4)
+    uint32_t it = 0;
+    bool ok = true;
+    for (long long u = pair; ok && u < units; u += npairs) {
+      for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const int s = it % PSTAGES;
+        // the set's columns are free when the products of kSets slabs ago have retired, which their stage's barrier tells
+        const uint32_t old = it - kSets;
+        bool here = tc::mbar_wait(&ctl->sfull[s], (it / PSTAGES) & 1u, abort_flag);
+        if (here && it >= (uint32_t)kSets) here = tc::mbar_wait(&ctl->empty[old % PSTAGES], (old / PSTAGES) & 1u, abort_flag);
+        if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
+        tc::tc_fence_after();
+        const uint8_t* from = smem + (size_t)s * kStage + kTileBytes + kPairN / 2 * kRowBytes;
+        const uint32_t to = tmem_base + ((uint32_t)(quad * 32) << 16) + kPairAccCols + (it % kSets) * kSetCols;
+        scales_to_tmem<kGroups>(to, from, lane);
+        // the tokens' two groups of rows side by side
+        uint32_t r[8 * kGroups];
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint4 v = *reinterpret_cast<const uint4*>(from + (1 + i) * kScales + g * kGroupBytes + lane * 16);
+            r[8 * g + 4 * i] = v.x; r[8 * g + 4 * i + 1] = v.y; r[8 * g + 4 * i + 2] = v.z; r[8 * g + 4 * i + 3] = v.w;
+          }
+        }
+        tc::tmem_st_32x32<8 * kGroups>(to + 4 * kGroups, r);
+        tc::tmem_st_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        // (the stores to this CTA's TMEM, which its own tensor core reads, are complete)
+        if (lane == 0) tc::mbar_arrive_cluster_bare(tc::mapa_shared(tc::smem_u32(&ctl->scales[it % kSets]), 0));
       }
     }
   } else {

@@ -192,6 +192,11 @@ __device__ __forceinline__ void cluster_sync_all() {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_addr) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
+// The same for an arrival that publishes nothing in memory (what precedes it has been waited for): the cluster-wide release of the
+// other costs its warp about 1500 cycles where other warps of the SM have stores under way.
+__device__ __forceinline__ void mbar_arrive_cluster_bare(uint32_t cluster_addr) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
+}
 // Tiled loads of a CTA pair: data lands in the executing CTA's shared memory, the byte count is
 // credited to the barrier at `bar_cluster_addr`, which may be the peer's.  No multicast.
 __device__ __forceinline__ void tma_load_2d_pair(void* dst, const CUtensorMap* m, int c0, int c1,
@@ -300,13 +305,25 @@ __device__ __forceinline__ void umma_fp4(uint32_t tmem_d, uint64_t desc_a, uint6
   else AERO_UMMA_FP4("1", "mxf4", "2X");
 #undef AERO_UMMA_FP4
 }
-// 512 bytes of scales (32 rows of 16 bytes) from shared memory to four columns of all four quadrants of TMEM lanes; in a pair, of
-// each CTA from its own shared memory.  Runs in order with the products that the same thread issues after it.
-template <bool PAIR>
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc) {
-  if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
-  else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+// Registers of a warp to 32 lanes of TMEM (lane base + l: thread l), N consecutive 32-bit columns.
+template <int N>
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const uint32_t* r) {
+  if constexpr (N == 8) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+  } else if constexpr (N == 16) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                 ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+                 "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+  } else {
+    static_assert(N == 32, "8, 16 or 32 columns");
+    tmem_st_32x32<16>(taddr, r);
+    tmem_st_32x32<16>(taddr + 16, r + 16);
+  }
 }
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
@@ -340,10 +357,6 @@ __host__ __device__ constexpr uint32_t make_idesc_s8(int M, int N) {
 __host__ __device__ constexpr uint32_t make_idesc_fp4(int M, int N, int e8m0, int sf) {
   return ((uint32_t)sf << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)e8m0 << 23) |
          ((uint32_t)(M >> 4) << 24) | ((uint32_t)sf << 29);
-}
-// Shared-memory descriptor of 512 bytes of scales for tmem_copy_scales: unswizzled, 8 rows of 16 bytes every 128 bytes.
-__device__ __forceinline__ uint64_t make_scale_desc(uint32_t saddr) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | 1ull << 16 | 8ull << 32 | 1ull << 46;
 }
 // Shared-memory matrix descriptor, 128-byte swizzle, sm_100 format.  Byte offsets are
 // given in bytes and stored in 16-byte units.
