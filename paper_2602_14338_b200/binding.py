@@ -246,52 +246,52 @@ class AdamWPlan:
     program whose gradients move makes another one."""
 
     _DTYPES = {torch.bfloat16: AERO_BF16, torch.float32: AERO_FP32}
+    _KEYS = {"param", "grad", "master", "m", "v", "m_scale", "v_scale", "weight_decay", "lr_scale"}
 
     def __init__(self, tensors):
         self.tensors = [dict(t) for t in tensors]
         self.device = None
         self.array = (AeroAdamWTensor * max(1, len(self.tensors)))()
-        written = set()
+        written, index = set(), None
+        floats, fp32 = tuple(self._DTYPES), (torch.float32,)
         for i, t in enumerate(self.tensors):
-            unknown = set(t) - {"param", "grad", "master", "m", "v", "m_scale", "v_scale", "weight_decay", "lr_scale"}
-            if unknown:
-                raise AeroError(f"tensor {i}: unknown {sorted(unknown)}")
-            n = t["param"].numel()
-            bits = 32 if t["m"].dtype == torch.float32 else 8
-            want = dict(param=(n, tuple(self._DTYPES)), grad=(n, tuple(self._DTYPES)), master=(n, (torch.float32,)))
+            if not self._KEYS.issuperset(t):
+                raise AeroError(f"tensor {i}: unknown {sorted(set(t) - self._KEYS)}")
+            param, m, master = t["param"], t["m"], t.get("master")
+            n, bits = param.numel(), 32 if m.dtype == torch.float32 else 8
+            checks = [("param", param, n, floats), ("grad", t["grad"], n, floats)]
             if bits == 32:
-                want.update(m=(n, (torch.float32,)), v=(n, (torch.float32,)))
+                checks += [("m", m, n, fp32), ("v", t["v"], n, fp32)]
             else:
                 blocks = (n + 255) // 256
-                want.update(m=(n, (torch.float8_e4m3fn,)), v=(n, (torch.uint8,)), m_scale=(blocks, (torch.float32,)),
-                            v_scale=(blocks, (torch.float32,)))
-            for name in ("master", "m_scale", "v_scale"):
-                if t.get(name) is None:
-                    if name in want and name != "master":
-                        raise AeroError(f"tensor {i}: 8-bit states need {name}")
-                    want.pop(name, None)
-            if "master" in want and t["param"].dtype != torch.bfloat16:
-                raise AeroError(f"tensor {i}: only a bf16 param has a master")
-            d = self.array[i]
-            for name, (size, dtypes) in want.items():
-                x = t[name]
+                if t.get("m_scale") is None or t.get("v_scale") is None:
+                    raise AeroError(f"tensor {i}: 8-bit states need m_scale and v_scale")
+                checks += [("m", m, n, (torch.float8_e4m3fn,)), ("v", t["v"], n, (torch.uint8,)),
+                           ("m_scale", t["m_scale"], blocks, fp32), ("v_scale", t["v_scale"], blocks, fp32)]
+            if master is not None:
+                if param.dtype != torch.bfloat16:
+                    raise AeroError(f"tensor {i}: only a bf16 param has a master")
+                checks.append(("master", master, n, fp32))
+            ptr = {}
+            for name, x, size, dtypes in checks:
                 if not x.is_cuda or not x.is_contiguous():
                     raise AeroError(f"tensor {i}: {name} must be a contiguous CUDA tensor")
                 if x.dtype not in dtypes:
                     raise AeroError(f"tensor {i}: {name} must have dtype {' or '.join(map(str, dtypes))}, got {x.dtype}")
                 if x.numel() != size:
                     raise AeroError(f"tensor {i}: {name} must have {size} elements, got {x.numel()}")
-                self.device = self.device if self.device is not None else x.device
-                if x.device != self.device:
+                if index is None:
+                    self.device, index = x.device, x.get_device()
+                if x.get_device() != index:
                     raise AeroError(f"tensor {i}: {name} is on {x.device}, others on {self.device}")
-                if name != "grad" and size > 0:
-                    if x.data_ptr() in written:
+                ptr[name] = p = x.data_ptr()
+                if size and name != "grad":
+                    if p in written:
                         raise AeroError(f"tensor {i}: {name} occurs twice")
-                    written.add(x.data_ptr())
-                setattr(d, name, x.data_ptr())
-            d.n, d.state_bits = n, bits
-            d.param_dtype, d.grad_dtype = self._DTYPES[t["param"].dtype], self._DTYPES[t["grad"].dtype]
-            d.weight_decay, d.lr_scale = t.get("weight_decay", 0.0), t.get("lr_scale", 1.0)
+                    written.add(p)
+            self.array[i] = AeroAdamWTensor(n, ptr["param"], ptr["grad"], ptr.get("master"), ptr["m"], ptr["v"], ptr.get("m_scale"),
+                                            ptr.get("v_scale"), self._DTYPES[param.dtype], self._DTYPES[t["grad"].dtype], bits,
+                                            t.get("weight_decay", 0.0), t.get("lr_scale", 1.0))
 
     def __len__(self):
         return len(self.tensors)

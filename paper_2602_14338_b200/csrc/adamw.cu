@@ -15,8 +15,13 @@ namespace {
 
 constexpr int kSlots = 128;             // tensors per launch
 constexpr int kBlock = 256;             // elements per scale of the 8-bit states; a warp's share of a tensor at a time
-constexpr int kWarps = 8, kChunk = kWarps * kBlock, kEach = kBlock / 32;
-constexpr int kMaxBlocks = 2048;        // of a launch
+constexpr int kWarps = 8, kEach = kBlock / 32;
+constexpr int kChunk = kWarps * kBlock;  // elements of one span per warp
+constexpr int kSpans = 4;                // spans of a warp per chunk of the norm and of the states as numbers
+constexpr int kNormBlocks = 148 * 8;     // of the norm's launch: a record each
+// Of the others.  (Step with 8-bit states and states as numbers, 233 M elements: 1031 us with 592 blocks, 1023 with 1184, 999 with
+// 2368, 966 with 9472, 993 with one per chunk; with fp32 states 1694, 1700, 1599, 1518, 1484.)
+constexpr int kMaxBlocks = 148 * 64;
 constexpr float kTopM = 448.f, kTopV = 496.f;          // largest values of the two 8-bit formats
 constexpr float kLeast = 0x1p-100f;     // scales are made of at least this: 448 / it stays finite
 
@@ -43,7 +48,7 @@ struct Table {
 // What the step's kernels share, in the workspace: made of the gradients' norm and the step's number.
 struct Scalars {
   float g_factor;                       // grad_scale clip
-  float lr, c1, c2;                     // 1 / (1 - beta^t)
+  float lr, c1, c2;                     // 1 / (1 - beta1^t), the root of 1 / (1 - beta2^t)
   int skip;
 };
 
@@ -116,40 +121,39 @@ __device__ __forceinline__ void store(void* p, bool half, const Span& s, const f
   if (half) store16(static_cast<__nv_bfloat16*>(p), s, x);
   else store32(static_cast<float*>(p), s, x);
 }
-__device__ __forceinline__ void load_codes(const uint8_t* p, const Span& s, uint8_t (&c)[kEach]) {
+// (a code per register; what is above its 8 bits is not stored)
+__device__ __forceinline__ void load_codes(const uint8_t* p, const Span& s, uint32_t (&c)[kEach]) {
   if (s.vec) {
     const uint2 u = *reinterpret_cast<const uint2*>(p + s.first());
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      c[i] = (uint8_t)(u.x >> (8 * i));
-      c[4 + i] = (uint8_t)(u.y >> (8 * i));
+      c[i] = __byte_perm(u.x, 0, 0x4440 + i);
+      c[4 + i] = __byte_perm(u.y, 0, 0x4440 + i);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) c[i] = s.has(i) ? p[s.at(i)] : 0;
   }
 }
-__device__ __forceinline__ void store_codes(uint8_t* p, const Span& s, const uint8_t (&c)[kEach]) {
+__device__ __forceinline__ void store_codes(uint8_t* p, const Span& s, const uint32_t (&c)[kEach]) {
   if (s.vec) {
-    uint2 u = make_uint2(0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      u.x |= (uint32_t)c[i] << (8 * i);
-      u.y |= (uint32_t)c[4 + i] << (8 * i);
-    }
-    *reinterpret_cast<uint2*>(p + s.first()) = u;
+    auto word = [&](int i) {
+      return __byte_perm(__byte_perm(c[i], c[i + 1], 0x0040), __byte_perm(c[i + 2], c[i + 3], 0x0040), 0x5410);
+    };
+    *reinterpret_cast<uint2*>(p + s.first()) = make_uint2(word(0), word(4));
   } else {
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (s.has(i)) p[s.at(i)] = c[i];
+      if (s.has(i)) p[s.at(i)] = (uint8_t)c[i];
   }
 }
 
 // Largest magnitude of the warp's elements; compared as bits, so that a NaN is larger than all and comes through.
+template <bool SIGNED>
 __device__ __forceinline__ float warp_top(const float (&x)[kEach]) {
   uint32_t top = 0;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+  for (int i = 0; i < kEach; ++i) top = max(top, SIGNED ? __float_as_uint(x[i]) & 0x7fffffffu : __float_as_uint(x[i]));
   return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
 }
 // What a block's scale is made of: its largest magnitude, or NaN where that is no finite number.
@@ -158,7 +162,7 @@ __device__ __forceinline__ float scale_top(float top) {
 }
 
 __device__ __forceinline__ void open_m(const Slot& t, const Span& s, float (&m)[kEach]) {
-  uint8_t c[kEach];
+  uint32_t c[kEach];
   load_codes(static_cast<const uint8_t*>(t.m), s, c);
   const float scale = t.m_scale[s.e0 / kBlock];
 #pragma unroll
@@ -170,13 +174,13 @@ __device__ __forceinline__ void open_m(const Slot& t, const Span& s, float (&m)[
   }
 }
 __device__ __forceinline__ void close_m(const Slot& t, const Span& s, const float (&m)[kEach]) {
-  const float top = scale_top(warp_top(m)), inv = __fmul_rn(__frcp_rn(top), kTopM);
-  uint8_t c[kEach];
+  const float top = scale_top(warp_top<true>(m)), inv = __fmul_rn(__frcp_rn(top), kTopM);
+  uint32_t c[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; i += 2) {
     const __nv_fp8x2_storage_t u = __nv_cvt_float2_to_fp8x2(make_float2(__fmul_rn(m[i], inv), __fmul_rn(m[i + 1], inv)), __NV_SATFINITE, __NV_E4M3);
-    c[i] = (uint8_t)u;
-    c[i + 1] = (uint8_t)(u >> 8);
+    c[i] = u;
+    c[i + 1] = u >> 8;
   }
   store_codes(static_cast<uint8_t*>(t.m), s, c);
   if (s.lane == 0) t.m_scale[s.e0 / kBlock] = top * (1.f / kTopM);
@@ -184,61 +188,78 @@ __device__ __forceinline__ void close_m(const Slot& t, const Span& s, const floa
 // The root's codes are the upper bits of a float whose exponent is moved by 120, so that the smallest normal numbers of the
 // two formats fall together and the subnormal ones do too.
 __device__ __forceinline__ void open_v(const Slot& t, const Span& s, float (&v)[kEach]) {
-  uint8_t c[kEach];
+  uint32_t c[kEach];
   load_codes(static_cast<const uint8_t*>(t.v), s, c);
   const float scale = t.v_scale[s.e0 / kBlock];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
-    const float r = __fmul_rn(__uint_as_float((uint32_t)c[i] << 19) * 0x1p120f, scale);
+    const float r = __fmul_rn(__uint_as_float(c[i] << 19) * 0x1p120f, scale);
     v[i] = __fmul_rn(r, r);
   }
 }
-__device__ __forceinline__ void close_v(const Slot& t, const Span& s, const float (&v)[kEach]) {
-  float r[kEach];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) r[i] = sqrtf(v[i]);
-  const float top = scale_top(warp_top(r)), inv = __fmul_rn(__frcp_rn(top), kTopV);
-  uint8_t c[kEach];
+// (r: the roots)
+__device__ __forceinline__ void close_v(const Slot& t, const Span& s, const float (&r)[kEach]) {
+  const float top = scale_top(warp_top<false>(r)), inv = __fmul_rn(__frcp_rn(top), kTopV);
+  uint32_t c[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const uint32_t b = __float_as_uint(__fmul_rn(r[i], inv) * 0x1p-120f);
-    uint32_t code = min((b + 0x3ffffu + ((b >> 19) & 1u)) >> 19, 255u);      // to even
-    if (r[i] > 0.f) code = max(code, 1u);           // a root that is not zero divides the step: it does not become zero
-    c[i] = (uint8_t)code;
+    // to even; a root that is not zero divides the step: it does not become zero
+    c[i] = max((b + 0x3ffffu + ((b >> 19) & 1u)) >> 19, min(__float_as_uint(r[i]), 1u));
   }
   store_codes(static_cast<uint8_t*>(t.v), s, c);
   if (s.lane == 0) t.v_scale[s.e0 / kBlock] = top * (1.f / kTopV);
 }
 
-// The warps' spans of a launch, chunk by chunk.
+// The chunks of a launch, SPANS spans per warp each; neighbouring warps take neighbouring spans, so that a tensor of a few spans
+// keeps as many warps busy.  f(tensor, the warp's first element).
 template <typename F>
-__device__ __forceinline__ void for_spans(const Table& tab, F&& f) {
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ void for_chunks(const Table& tab, int spans, F&& f) {
   for (long long c = blockIdx.x; c < tab.chunk0[tab.count]; c += gridDim.x) {
     const int k = slot_of(tab, c);
-    const Slot& t = tab.slot[k];
-    const long long e0 = (c - tab.chunk0[k]) * kChunk + warp * kBlock, left = t.n - e0;
-    if (left <= 0) continue;
-    f(t, Span{e0, (int)(left < kBlock ? left : kBlock), (t.flags & kAligned) && left >= kBlock, lane});
+    f(tab.slot[k], (c - tab.chunk0[k]) * (spans * kChunk) + (threadIdx.x >> 5) * kBlock);
   }
+}
+__device__ __forceinline__ Span span_at(const Slot& t, long long e0) {
+  const long long left = t.n - e0;
+  return {e0, (int)(left < kBlock ? left : kBlock), (t.flags & kAligned) && left >= kBlock, (int)(threadIdx.x & 31)};
 }
 
 // Sum of the gradients' squares, one record per block: eight squares at a time in fp32, then in 64 bits.  Groups whose sum
 // leaves the range in which fp32 holds squares are taken in 64 bits from the start.
+__device__ __forceinline__ double squares(const float (&g)[kEach]) {
+  float q = 0.f;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) q = fmaf(g[i], g[i], q);
+  if (q > 0x1p-80f && q < 0x1p120f) return q;
+  double sum = 0.0;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) sum += (double)g[i] * g[i];
+  return sum;
+}
 __global__ void __launch_bounds__(kWarps * 32) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partials) {
   __shared__ double sh[kWarps];
   double sum = 0.0;
-  for_spans(tab, [&](const Slot& t, const Span& s) {
-    float g[kEach];
-    load(t.grad, t.flags & kGrad16, s, g);
-    float q = 0.f;
+  for_chunks(tab, kSpans, [&](const Slot& t, long long e0) {
+    if ((t.flags & kAligned) && (t.flags & kGrad16) && t.n - e0 >= (kSpans - 1) * kChunk + kBlock) {
+      // all loads of the chunk under way at once (one at a time keeps half of the bytes that the memory needs under way)
+      uint4 u[kSpans];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) q = fmaf(g[i], g[i], q);
-    if (q > 0x1p-80f && q < 0x1p120f) {
-      sum += q;
+      for (int q = 0; q < kSpans; ++q)
+        u[q] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.grad) + e0 + q * kChunk + (threadIdx.x & 31) * kEach);
+#pragma unroll
+      for (int q = 0; q < kSpans; ++q) {
+        float g[kEach];
+        rowvec::unpack(u[q], g);
+        sum += squares(g);
+      }
     } else {
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) sum += (double)g[i] * g[i];
+#pragma unroll 1
+      for (int q = 0; q < kSpans && e0 < t.n; ++q, e0 += kChunk) {
+        float g[kEach];
+        load(t.grad, t.flags & kGrad16, span_at(t, e0), g);
+        sum += squares(g);
+      }
     }
   });
 #pragma unroll
@@ -262,8 +283,14 @@ struct PrepareArgs {
   float* stats;
   Scalars* out;
 };
+// One block.  Two warps raise the betas to the step's number while the others wait for the norm's records.
 __global__ void __launch_bounds__(256) adamw_prepare_kernel(PrepareArgs a) {
-  __shared__ double sh[8];
+  __shared__ double sh[8], correction[2];
+  const long long taken = *a.step;
+  if (threadIdx.x == 192 || threadIdx.x == 224) {
+    const int k = threadIdx.x == 224;
+    correction[k] = 1.0 / (1.0 - pow(k ? a.beta2 : a.beta1, (double)(taken + 1)));
+  }
   double sum = 0.0;
   if (a.partials)
     for (int i = threadIdx.x; i < a.n_partials; i += 256) sum += a.partials[i];
@@ -280,39 +307,128 @@ __global__ void __launch_bounds__(256) adamw_prepare_kernel(PrepareArgs a) {
     if (clip > 1.0) clip = 1.0;
   }
   const bool skip = a.partials && a.skip_nonfinite && !(norm < INFINITY);
-  const long long t = *a.step + (skip ? 0 : 1);
-  if (!skip) *a.step = t;
+  if (!skip) *a.step = taken + 1;
   Scalars s;
   s.g_factor = (float)(clip * (double)a.grad_scale);
   s.lr = a.lr_dev ? *a.lr_dev : a.lr;
-  s.c1 = (float)(1.0 / (1.0 - pow(a.beta1, (double)t)));
-  s.c2 = (float)(1.0 / (1.0 - pow(a.beta2, (double)t)));
+  s.c1 = (float)correction[0];
+  s.c2 = (float)sqrt(correction[1]);
   s.skip = skip ? 1 : 0;
   *a.out = s;
   if (a.stats) {
     a.stats[0] = (float)norm;
     a.stats[1] = (float)clip;
     a.stats[2] = skip ? 1.f : 0.f;
-    a.stats[3] = (float)t;
+    a.stats[3] = (float)(taken + (skip ? 0 : 1));
   }
 }
 
-__global__ void __launch_bounds__(kWarps * 32) adamw_step_kernel(const __grid_constant__ Table tab, const Hyper h,
+// The root of eight values.  Within 2^-100 .. 2^100: one step of the residual form of Newton's iteration from the hardware's
+// reciprocal root (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), which gives the
+// same bits as sqrtf there (tested over all values).  Else, zeros among them, sqrtf.
+__device__ __forceinline__ void roots(const float (&v)[kEach], float (&r)[kEach]) {
+  bool plain = true;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) plain &= v[i] > 0x1p-100f && v[i] < 0x1p100f;
+  if (plain) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      float y;
+      asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v[i]));
+      const float g = __fmul_rn(v[i], y);
+      r[i] = __fmaf_rn(__fmaf_rn(-g, g, v[i]), 0.5f * y, g);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) r[i] = sqrtf(v[i]);
+  }
+}
+
+__device__ __forceinline__ void open_m(uint2 u, float scale, float (&m)[kEach]) {
+#pragma unroll
+  for (int i = 0; i < kEach; i += 2) {
+    const uint32_t w = (i < 4 ? u.x : u.y) >> (8 * (i % 4));
+    const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3)));
+    m[i] = __fmul_rn(f.x, scale);
+    m[i + 1] = __fmul_rn(f.y, scale);
+  }
+}
+__device__ __forceinline__ void open_v(uint2 u, float scale, float (&v)[kEach]) {
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const uint32_t c = __byte_perm(i < 4 ? u.x : u.y, 0, 0x4440 + i % 4);
+    const float r = __fmul_rn(__uint_as_float(c << 19) * 0x1p120f, scale);
+    v[i] = __fmul_rn(r, r);
+  }
+}
+
+// What a lane loads of a whole span with 8-bit states.
+struct Raw {
+  uint4 g[2], p[2];
+  uint2 m, v;
+  float m_scale, v_scale;
+};
+__device__ __forceinline__ void load_raw(const Slot& t, const Span& s, Raw& r) {
+  const long long e = s.first();
+  if (t.flags & kGrad16) {
+    r.g[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.grad) + e);
+  } else {
+    r.g[0] = reinterpret_cast<const uint4*>(static_cast<const float*>(t.grad) + e)[0];
+    r.g[1] = reinterpret_cast<const uint4*>(static_cast<const float*>(t.grad) + e)[1];
+  }
+  if (t.master || !(t.flags & kParam16)) {
+    const uint4* p = reinterpret_cast<const uint4*>((t.master ? t.master : static_cast<const float*>(t.param)) + e);
+    r.p[0] = p[0];
+    r.p[1] = p[1];
+  } else {
+    r.p[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.param) + e);
+  }
+  r.m = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.m) + e);
+  r.v = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(t.v) + e);
+  r.m_scale = t.m_scale[s.e0 / kBlock];
+  r.v_scale = t.v_scale[s.e0 / kBlock];
+}
+__device__ __forceinline__ void open(const uint4 (&u)[2], bool half, float (&x)[kEach]) {
+  if (half) {
+    rowvec::unpack(u[0], x);
+  } else {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      x[4 * q] = __uint_as_float(u[q].x); x[4 * q + 1] = __uint_as_float(u[q].y);
+      x[4 * q + 2] = __uint_as_float(u[q].z); x[4 * q + 3] = __uint_as_float(u[q].w);
+    }
+  }
+}
+
+// The step of the tensors with states of BITS bits.
+template <int BITS>
+__global__ void __launch_bounds__(kWarps * 32, 4) adamw_step_kernel(const __grid_constant__ Table tab, const Hyper h,
                                                                  const Scalars* __restrict__ scalars) {
   const Scalars sc = *scalars;
   if (sc.skip) return;
-  for_spans(tab, [&](const Slot& t, const Span& s) {
-    const bool half = t.flags & kParam16, bits8 = t.flags & kState8;
-    float g[kEach], p[kEach], m[kEach], v[kEach];
-    load(t.grad, t.flags & kGrad16, s, g);
-    if (t.master) load32(t.master, s, p);
-    else load(t.param, half, s, p);
-    if (bits8) {
-      open_m(t, s, m);
-      open_v(t, s, v);
+  for_chunks(tab, 1, [&](const Slot& t, long long e0) {
+    if (e0 >= t.n) return;
+    const Span s = span_at(t, e0);
+    const bool half = t.flags & kParam16;
+    float g[kEach], p[kEach], m[kEach], v[kEach], r[kEach];
+    if (BITS == 8 && s.vec) {
+      Raw now;
+      load_raw(t, s, now);
+      open(now.g, t.flags & kGrad16, g);
+      open(now.p, half && !t.master, p);
+      open_m(now.m, now.m_scale, m);
+      open_v(now.v, now.v_scale, v);
     } else {
-      load32(static_cast<const float*>(t.m), s, m);
-      load32(static_cast<const float*>(t.v), s, v);
+      load(t.grad, t.flags & kGrad16, s, g);
+      if (t.master) load32(t.master, s, p);
+      else load(t.param, half, s, p);
+      if (BITS == 8) {
+        open_m(t, s, m);
+        open_v(t, s, v);
+      } else {
+        load32(static_cast<const float*>(t.m), s, m);
+        load32(static_cast<const float*>(t.v), s, v);
+      }
     }
     const float lr = sc.lr * t.lr_scale, keep = 1.f - lr * t.weight_decay, rate = lr * sc.c1;
 #pragma unroll
@@ -322,13 +438,19 @@ __global__ void __launch_bounds__(kWarps * 32) adamw_step_kernel(const __grid_co
       // which of them an 8-bit state gets)
       m[i] = __fadd_rn(__fmul_rn(h.beta1, m[i]), __fmul_rn(h.rest1, x));
       v[i] = __fadd_rn(__fmul_rn(h.beta2, v[i]), __fmul_rn(__fmul_rn(h.rest2, x), x));
-      p[i] = fmaf(keep, p[i], -rate * m[i] / (sqrtf(v[i] * sc.c2) + h.eps));
+    }
+    roots(v, r);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      float inv;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(r[i], sc.c2, h.eps)));
+      p[i] = fmaf(keep, p[i], -rate * m[i] * inv);
     }
     if (t.master) store32(t.master, s, p);
     store(t.param, half, s, p);
-    if (bits8) {
+    if (BITS == 8) {
       close_m(t, s, m);
-      close_v(t, s, v);
+      close_v(t, s, r);
     } else {
       store32(static_cast<float*>(t.m), s, m);
       store32(static_cast<float*>(t.v), s, v);
@@ -338,17 +460,48 @@ __global__ void __launch_bounds__(kWarps * 32) adamw_step_kernel(const __grid_co
 
 // The states as numbers: param and master stand for the outputs of m and v.
 __global__ void __launch_bounds__(kWarps * 32) adamw_states_kernel(const __grid_constant__ Table tab) {
-  for_spans(tab, [&](const Slot& t, const Span& s) {
-    float x[kEach];
-    if (t.param) {
-      if (t.flags & kState8) open_m(t, s, x);
-      else load32(static_cast<const float*>(t.m), s, x);
-      store(t.param, t.flags & kOut16, s, x);
-    }
-    if (t.master) {
-      if (t.flags & kState8) open_v(t, s, x);
-      else load32(static_cast<const float*>(t.v), s, x);
-      store(t.master, t.flags & kOut16, s, x);
+  for_chunks(tab, kSpans, [&](const Slot& t, long long e0) {
+    const bool half = t.flags & kOut16;
+    const auto write = [&](long long e, const float (&x)[kEach], void* out) { store(out, half, span_at(t, e), x); };
+    if ((t.flags & kAligned) && (t.flags & kState8) && t.n - e0 >= (kSpans - 1) * kChunk + kBlock) {
+      const auto codes = [&](const void* from, const float* scales, uint2 (&u)[kSpans], float (&scale)[kSpans]) {
+#pragma unroll
+        for (int q = 0; q < kSpans; ++q) {
+          u[q] = *reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(from) + e0 + q * kChunk + (threadIdx.x & 31) * kEach);
+          scale[q] = scales[(e0 + q * kChunk) / kBlock];
+        }
+      };
+      uint2 m[kSpans], v[kSpans];
+      float ms[kSpans], vs[kSpans], x[kEach];
+      if (t.param) codes(t.m, t.m_scale, m, ms);
+      if (t.master) codes(t.v, t.v_scale, v, vs);
+#pragma unroll
+      for (int q = 0; q < kSpans; ++q) {
+        if (t.param) {
+          open_m(m[q], ms[q], x);
+          write(e0 + q * kChunk, x, t.param);
+        }
+        if (t.master) {
+          open_v(v[q], vs[q], x);
+          write(e0 + q * kChunk, x, t.master);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int q = 0; q < kSpans && e0 < t.n; ++q, e0 += kChunk) {
+        const Span s = span_at(t, e0);
+        float x[kEach];
+        if (t.param) {
+          if (t.flags & kState8) open_m(t, s, x);
+          else load32(static_cast<const float*>(t.m), s, x);
+          write(e0, x, t.param);
+        }
+        if (t.master) {
+          if (t.flags & kState8) open_v(t, s, x);
+          else load32(static_cast<const float*>(t.v), s, x);
+          write(e0, x, t.master);
+        }
+      }
     }
   });
 }
@@ -381,13 +534,13 @@ int check_tensor(const aero_adamw_tensor& t) {
   return AERO_OK;
 }
 
-// Fills the table with tensors from *next on, leaving empty ones out, and moves *next on.
-void fill(Table& tab, const aero_adamw_tensor* tensors, int32_t n, int32_t* next) {
+// Fills the table with tensors from *next on that have states of so many bits (0: any), leaving empty ones out, and moves *next on.
+void fill(Table& tab, const aero_adamw_tensor* tensors, int32_t n, int32_t* next, int bits, int spans) {
   tab.count = 0;
   tab.chunk0[0] = 0;
   for (; *next < n && tab.count < kSlots; ++*next) {
     const aero_adamw_tensor& t = tensors[*next];
-    if (t.n == 0) continue;
+    if (t.n == 0 || (bits && t.state_bits != bits)) continue;
     Slot& s = tab.slot[tab.count];
     s = {t.n, t.param, t.grad, t.master, t.m, t.v, t.m_scale, t.v_scale, t.weight_decay, t.lr_scale, 0};
     bool aligned = true;
@@ -395,14 +548,14 @@ void fill(Table& tab, const aero_adamw_tensor* tensors, int32_t n, int32_t* next
       aligned &= aligned_to(p, 16);
     s.flags = (t.param_dtype == AERO_BF16 ? kParam16 : 0) | (t.grad_dtype == AERO_BF16 ? kGrad16 : 0) |
               (t.state_bits == 8 ? kState8 : 0) | (aligned ? kAligned : 0);
-    tab.chunk0[tab.count + 1] = tab.chunk0[tab.count] + (t.n + kChunk - 1) / kChunk;
+    tab.chunk0[tab.count + 1] = tab.chunk0[tab.count] + (t.n + spans * kChunk - 1) / (spans * kChunk);
     ++tab.count;
   }
 }
 
-int grid_of(const Table& tab) {
+int grid_of(const Table& tab, int most) {
   const long long chunks = tab.chunk0[tab.count];
-  return (int)(chunks < kMaxBlocks ? chunks : kMaxBlocks);
+  return (int)(chunks < most ? chunks : most);
 }
 int launches_of(int32_t n) { return (n + kSlots - 1) / kSlots; }
 
@@ -418,7 +571,7 @@ void aero_adamw_cfg_default(aero_adamw_cfg* ac) {
 
 size_t aero_adamw_workspace_bytes(int32_t n_tensors) {
   if (n_tensors < 0) return 0;
-  return 256 + aero_align_up((size_t)launches_of(n_tensors) * kMaxBlocks * sizeof(double), 256);
+  return 256 + aero_align_up((size_t)launches_of(n_tensors) * kNormBlocks * sizeof(double), 256);
 }
 
 int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, const aero_adamw_tensor* tensors,
@@ -441,10 +594,10 @@ int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, 
   int n_partials = 0;
   if (norm) {
     for (int32_t next = 0; next < n_tensors;) {
-      fill(tab, tensors, n_tensors, &next);
+      fill(tab, tensors, n_tensors, &next, 0, kSpans);
       if (tab.count == 0) break;
-      adamw_norm_kernel<<<grid_of(tab), kWarps * 32, 0, ctx->stream>>>(tab, partials + n_partials);
-      n_partials += grid_of(tab);
+      adamw_norm_kernel<<<grid_of(tab, kNormBlocks), kWarps * 32, 0, ctx->stream>>>(tab, partials + n_partials);
+      n_partials += grid_of(tab, kNormBlocks);
       ctx->launches += 1;
     }
   }
@@ -453,11 +606,14 @@ int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, 
   adamw_prepare_kernel<<<1, 256, 0, ctx->stream>>>(pa);
   ctx->launches += 1;
   const Hyper h = {(float)ac->beta1, (float)ac->beta2, (float)(1.0 - ac->beta1), (float)(1.0 - ac->beta2), ac->eps};
-  for (int32_t next = 0; next < n_tensors;) {
-    fill(tab, tensors, n_tensors, &next);
-    if (tab.count == 0) break;
-    adamw_step_kernel<<<grid_of(tab), kWarps * 32, 0, ctx->stream>>>(tab, h, scalars);
-    ctx->launches += 1;
+  for (const int bits : {8, 32}) {
+    for (int32_t next = 0; next < n_tensors;) {
+      fill(tab, tensors, n_tensors, &next, bits, 1);
+      if (tab.count == 0) break;
+      if (bits == 8) adamw_step_kernel<8><<<grid_of(tab, kMaxBlocks), kWarps * 32, 0, ctx->stream>>>(tab, h, scalars);
+      else adamw_step_kernel<32><<<grid_of(tab, kMaxBlocks), kWarps * 32, 0, ctx->stream>>>(tab, h, scalars);
+      ctx->launches += 1;
+    }
   }
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
@@ -478,7 +634,7 @@ int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor*
   Table tab;
   for (int32_t next = 0; next < n_tensors;) {
     int32_t at = next;
-    fill(tab, tensors, n_tensors, &next);
+    fill(tab, tensors, n_tensors, &next, 0, kSpans);
     if (tab.count == 0) break;
     for (int k = 0; k < tab.count; ++k, ++at) {
       while (tensors[at].n == 0) ++at;
@@ -489,7 +645,7 @@ int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor*
       for (const void* p : {(const void*)s.param, (const void*)s.master, (const void*)s.m, (const void*)s.v}) aligned &= aligned_to(p, 16);
       s.flags = (s.flags & kState8) | (aligned ? kAligned : 0) | (out_dtype == AERO_BF16 ? kOut16 : 0);
     }
-    adamw_states_kernel<<<grid_of(tab), kWarps * 32, 0, ctx->stream>>>(tab);
+    adamw_states_kernel<<<grid_of(tab, kMaxBlocks), kWarps * 32, 0, ctx->stream>>>(tab);
     ctx->launches += 1;
   }
   AERO_CUDA_TRY(cudaGetLastError());

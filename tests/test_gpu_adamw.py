@@ -264,3 +264,20 @@ def test_beyond_32_bit_offsets(ctx):
     assert torch.count_nonzero(t["param"][:2 ** 31 - 8000]).item() == 0
     ms = np.repeat(f64(t["m_scale"]), 256)[n - tail:n]
     assert np.all(np.abs(f64(t["m"][-tail:]) * ms - m1) <= 2.0 ** -4 * np.abs(m1) + 2.0 ** -9 * ms)
+
+
+def test_roots_over_all_values(ctx):
+    """A block's scale is the root of its largest v times 1 / 496, so its bits tell whether the root is the correctly rounded one.  With
+    beta2 = 1/2 and no gradient v is half the square of the decoded root, whose scale takes every fifth fp32 pattern of two binades
+    and some of every exponent (the values of a block are all within the range of the fast form, or none is)."""
+    g = torch.cat([torch.arange(0x3f800000, 0x40800000, 5, dtype=torch.int32).view(torch.float32),
+                   torch.arange(1, 0x7f000000, 99991, dtype=torch.int32).view(torch.float32).clamp(max=1e15)]).cuda()
+    n = g.numel()
+    t = dict(param=torch.zeros(n * 256, dtype=torch.bfloat16, device="cuda"), grad=torch.zeros(n * 256, dtype=torch.bfloat16, device="cuda"),
+             m=torch.zeros(n * 256, dtype=torch.float8_e4m3fn, device="cuda"), v=torch.zeros(n * 256, dtype=torch.uint8, device="cuda"),
+             m_scale=torch.zeros(n, device="cuda"), v_scale=g.clone())
+    t["v"].view(n, 256)[:, 0], t["v"].view(n, 256)[:, 1:] = 176, 160          # 16 2^(11 - 11) = 16, and 8
+    ctx.adamw_step(B.adamw_cfg_default(beta2=0.5, lr=0.0), B.AdamWPlan([t]), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    v = (16 * g) * (16 * g) * 0.5
+    want = torch.sqrt(v).clamp(min=2.0 ** -100) * torch.tensor(1.0 / 496.0, device="cuda")
+    assert torch.equal(t["v_scale"], want)
