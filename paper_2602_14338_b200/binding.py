@@ -302,7 +302,6 @@ class Fp4Rows:
     block 16, row_scale [rows] f32.  The buffers are made unless given (on `device`)."""
 
     def __init__(self, rows, cols, block=16, codes=None, scales=None, row_scale=None, device=None):
-        lib = load_library()
         if block not in (16, 32):
             raise AeroError(f"block must be 16 or 32, got {block}")
         if rows < 0 or cols <= 0 or cols % 32:
@@ -310,18 +309,16 @@ class Fp4Rows:
         if block == 32 and row_scale is not None:
             raise AeroError("block 32 has no row_scale")
         self.rows, self.cols, self.block = rows, cols, block
-        sizes = lib.aero_fp4_code_bytes(rows, cols), lib.aero_fp4_scale_bytes(rows, cols, block)
-        self.codes = codes if codes is not None else torch.empty(sizes[0], dtype=torch.uint8, device=device)
-        self.scales = scales if scales is not None else torch.empty(sizes[1], dtype=torch.uint8, device=device)
-        if block == 16 and row_scale is None:
-            row_scale = torch.empty(rows, dtype=torch.float32, device=device)
-        self.row_scale = row_scale
-        want = [("codes", self.codes, torch.uint8, sizes[0]), ("scales", self.scales, torch.uint8, sizes[1])]
-        if block == 16:
-            want.append(("row_scale", self.row_scale, torch.float32, rows))
-        for name, t, dtype, numel in want:
-            if t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
-                raise AeroError(f"{name} must be a contiguous tensor of {numel} {dtype}, got {t.numel()} {t.dtype}")
+        tiles = -(-rows // 128) * -(-cols // 256)              # aero_fp4_code_bytes, aero_fp4_scale_bytes
+        for name, given, dtype, numel in (("codes", codes, torch.uint8, tiles * 16384), ("scales", scales, torch.uint8, tiles * 32768 // block),
+                                          ("row_scale", row_scale, torch.float32, rows if block == 16 else None)):
+            if numel is None:
+                given = None
+            elif given is None:
+                given = torch.empty(numel, dtype=dtype, device=device)
+            elif given.dtype != dtype or given.numel() != numel or not given.is_cuda or not given.is_contiguous():
+                raise AeroError(f"{name} must be a contiguous CUDA tensor of {numel} {dtype}, got {given.numel()} {given.dtype}")
+            setattr(self, name, given)
 
 
 def _ptr(t, dtype=None, numel=None, name="tensor"):
@@ -818,20 +815,23 @@ class Context:
 
     # ---- rows in 4-bit floating point ------------------------------------------------------------
     def _fp4(self, r, name):
-        return tuple(self._arg(t, t.dtype, tuple(t.shape), f"{name}.{part}") if t is not None else None
-                     for part, t in (("codes", r.codes), ("scales", r.scales), ("row_scale", r.row_scale)))
+        """Data pointers of Fp4Rows, whose sizes and types its constructor has checked."""
+        index = self.device.index
+        for part, t in (("codes", r.codes), ("scales", r.scales), ("row_scale", r.row_scale)):
+            if t is not None and t.get_device() != index:
+                raise AeroError(f"{name}.{part} must be on {self.device}, got {t.device}")
+        return r.codes.data_ptr(), r.scales.data_ptr(), r.row_scale.data_ptr() if r.row_scale is not None else None
 
     def quantize_fp4(self, cfg, x, block=16, out=None):
         """aero_quantize_fp4: the rows of x as Fp4Rows."""
         T, d = x.shape
-        dt = torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32
-        px = self._arg(x, dt, (T, d), "x")
+        px = self._arg(x, torch.bfloat16 if cfg.dtype == AERO_BF16 else torch.float32, (T, d), "x")
         if out is None:
-            if block not in (16, 32) or d % 32:
-                raise AeroError(f"block must be 16 or 32 and the columns a multiple of 32, got {block} and {d}")
-            out = Fp4Rows(T, d, block, self._new((self.lib.aero_fp4_code_bytes(T, d),), torch.uint8),
-                          self._new((self.lib.aero_fp4_scale_bytes(T, d, block),), torch.uint8),
-                          self._new((T,), torch.float32) if block == 16 else None)
+            if torch._C._cuda_getCurrentRawStream(self.device.index) == self.stream.cuda_stream:
+                out = Fp4Rows(T, d, block, device=self.device)
+            else:
+                with torch.cuda.stream(self.stream):           # (memory for the stream on which the kernels run)
+                    out = Fp4Rows(T, d, block, device=self.device)
         elif (out.rows, out.cols, out.block) != (T, d, block):
             raise AeroError(f"out must hold {T} x {d} values in blocks of {block}, got {out.rows} x {out.cols} in {out.block}")
         _check(self.lib.aero_quantize_fp4(self.h, C.byref(cfg), T, d, block, px, *self._fp4(out, "out")), "aero_quantize_fp4")

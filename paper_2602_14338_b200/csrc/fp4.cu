@@ -32,7 +32,7 @@ __host__ __device__ constexpr int groups_per_slab(int block) { return kSlab / (4
 // A warp per row; a lane takes 16 neighbouring columns, so a step of the warp is 512 columns, two tiles.
 constexpr int kLane = 16, kStep = 32 * kLane;
 
-// Where lane's 8 bytes of codes, and the byte of its scale, stand for columns c .. c + 15 of row r.
+// Where the bytes of codes, and the byte of the scale, of neighbouring columns from c on of row r stand.
 __device__ __forceinline__ size_t code_at(long long r, int c, int slabs) {
   const int in = (c % kSlab) / 2, rr = (int)(r % kTile);
   return ((size_t)(r / kTile) * slabs + c / kSlab) * kTileBytes + rr * kRowBytes + (((in / 16) ^ (rr & 7)) * 16) + in % 16;
@@ -94,31 +94,55 @@ template <> struct Raw16<float> {
 
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }      // -126 .. 127
 
+// Eight values' e2m1 codes in a word, the first lowest.
+__device__ __forceinline__ uint32_t e2m1_word(const float (&y)[8]) {
+  uint32_t w;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(w)
+      : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return w;
+}
+
 // e2m1 codes of 16 values y_i = x_i f / s: f is a power of two, s the value of an e4m3 code (1 for block 32).
-// bf16 rows multiply by the rounded 1 / s.  Where x f / s is half way between two codes, which 8 and 4 significant bits often make
-// it, the rounded product may fall to either side; any other quotient is at least 2^-8 of itself from there.  Rounding the product
-// to a multiple of 2^-12 puts it back (2 instructions instead of a division each).
+// bf16 rows multiply by an approximate 1 / s.  Where x f / s is half way between two codes, which 8 and 4 significant bits often
+// make it, the product may fall to either side; any other quotient is at least 2^-8 of itself from there.  Rounding the product
+// to a multiple of 2^-12 (by adding 1.5 2^11, in the product's own fma, and taking it off) puts it back: 2 instructions a value
+// instead of a division.
 template <typename T>
 __device__ __forceinline__ uint2 to_e2m1(const float (&x)[16], float f, float s) {
-  uint32_t w[2] = {0, 0};
-  // (a row so small that f / s might overflow takes f first)
-  const bool first = f > 0x1p100f;
-  const float inv = __fdiv_rn(1.f, s) * (first ? 1.f : f), pre = first ? f : 1.f;
+  uint32_t w[2];
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  const bool small = f > 0x1p100f;                 // (a row so small that f / s might overflow takes f first)
+  if (!small) inv *= f;
 #pragma unroll
-  for (int i = 0; i < 16; i += 2) {
-    float2 y;
-    if constexpr (sizeof(T) == 2) {
-      constexpr float kSnap = 0x1.8p11f;
-      y = first ? make_float2(x[i] * pre, x[i + 1] * pre) : make_float2(x[i], x[i + 1]);
-      y.x = __fadd_rn(__fadd_rn(__fmul_rn(y.x, inv), kSnap), -kSnap);
-      y.y = __fadd_rn(__fadd_rn(__fmul_rn(y.y, inv), kSnap), -kSnap);
-    } else {
-      y.x = __fdiv_rn(__fmul_rn(x[i], f), s);
-      y.y = __fdiv_rn(__fmul_rn(x[i + 1], f), s);
+  for (int q = 0; q < 2; ++q) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float v = x[8 * q + i];
+      if constexpr (sizeof(T) == 2) {
+        constexpr float kSnap = 0x1.8p11f;
+        y[i] = __fadd_rn(__fmaf_rn(small ? v * f : v, inv, kSnap), -kSnap);
+      } else {
+        y[i] = __fdiv_rn(__fmul_rn(v, f), s);
+      }
     }
-    w[i / 8] |= (uint32_t)__nv_cvt_float2_to_fp4x2(y, __NV_E2M1, cudaRoundNearest) << (4 * (i % 8));
+    w[q] = e2m1_word(y);
   }
   return make_uint2(w[0], w[1]);
+}
+
+// The e4m3 code of top / 6, to nearest: for bf16 by the same argument, here with a rounding to 14 bits.
+template <typename T>
+__device__ __forceinline__ uint32_t e4m3_of_sixth(float top) {
+  float y;
+  if constexpr (sizeof(T) == 2) y = __uint_as_float((__float_as_uint(top * (1.f / 6.f)) + 0x200u) & ~0x3ffu);
+  else y = __fdiv_rn(top, 6.f);
+  return __nv_cvt_float_to_fp8(y, __NV_SATFINITE, __NV_E4M3);
 }
 
 struct QuantArgs {
@@ -141,38 +165,44 @@ __global__ void __launch_bounds__(256) fp4_quantize_kernel(QuantArgs a) {
   const int cols = a.slabs * kSlab;
   constexpr int kHeld = STEPS > 0 ? STEPS : 1;
   Raw16<T> held[kHeld];
+  uint32_t tops[kHeld];
   float f = 1.f;
-  if constexpr (BLOCK == 16 || STEPS > 0) {
+  if constexpr (STEPS > 0) {
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q) {
+      const int c = q * kStep + lane * kLane;
+      if (there && c < a.d) held[q].load(x + c);
+      else held[q].zero();
+    }
+  }
+  if constexpr (BLOCK == 16) {
     uint32_t top = 0;
     if constexpr (STEPS > 0) {
 #pragma unroll
-      for (int q = 0; q < STEPS; ++q) {
-        const int c = q * kStep + lane * kLane;
-        if (there && c < a.d) held[q].load(x + c);
-        else held[q].zero();
-      }
-#pragma unroll
-      for (int q = 0; q < STEPS; ++q) top = max(top, held[q].top());
+      for (int q = 0; q < STEPS; ++q) top = max(top, tops[q] = held[q].top());
     } else if (there) {
       for (int c = lane * kLane; c < a.d; c += kStep) {
         held[0].load(x + c);
         top = max(top, held[0].top());
       }
     }
-    if constexpr (BLOCK == 16) {
-      top = __reduce_max_sync(0xffffffffu, top);
-      // the smallest power of two that brings the largest of the row's scales, top / 6, to 448 at most
-      const float row = __uint_as_float(top);
-      float scale = 0.f;
-      if (!(row < INFINITY)) scale = __uint_as_float(0x7fffffffu);
-      else if (row > 0.f) {
-        const int e = max((int)((__float_as_uint(__fdiv_rn(row, 2688.f)) + 0x7fffffu) >> 23) - 127, -126);
-        scale = power_of_two(e);
-        f = power_of_two(-e);
-      }
-      if (there && lane == 0) a.row_scale[r] = scale;
+    top = __reduce_max_sync(0xffffffffu, top);
+    // the smallest power of two that brings the largest of the row's scales, top / 6, to 448 at most
+    const float row = __uint_as_float(top);
+    float scale = 0.f;
+    if (!(row < INFINITY)) scale = __uint_as_float(0x7fffffffu);
+    else if (row > 0.f) {
+      const int e = max((int)((__float_as_uint(__fdiv_rn(row, 2688.f)) + 0x7fffffu) >> 23) - 127, -126);
+      scale = power_of_two(e);
+      f = power_of_two(-e);
     }
+    if (there && lane == 0) a.row_scale[r] = scale;
   }
+  // where the first step's codes and scales go; the next one's are two tiles further
+  constexpr int kApart = BLOCK / kLane;                      // lanes from one block to the next
+  constexpr int kTilesPerStep = kStep / kSlab;
+  uint8_t* codes = a.codes + code_at(r, lane * kLane, a.slabs);
+  uint8_t* scales = a.scales + scale_at<BLOCK>(r, lane * kLane, a.slabs);
 #pragma unroll (STEPS > 0 ? STEPS : 1)
   for (int q = 0; q < (STEPS > 0 ? STEPS : 1 << 20); ++q) {
     const int c = q * kStep + lane * kLane;
@@ -182,11 +212,10 @@ __global__ void __launch_bounds__(256) fp4_quantize_kernel(QuantArgs a) {
       else held[0].zero();
     }
     const Raw16<T>& h = held[STEPS > 0 ? q : 0];
-    uint32_t top = h.top();
     float s = 1.f, factor = f;
-    uint32_t byte = 0;
+    uint32_t byte, top = BLOCK == 16 && STEPS > 0 ? tops[STEPS > 0 ? q : 0] : h.top();
     if constexpr (BLOCK == 16) {
-      byte = __nv_cvt_float_to_fp8(__fdiv_rn(__uint_as_float(top) * f, 6.f), __NV_SATFINITE, __NV_E4M3);
+      byte = e4m3_of_sixth<T>(__uint_as_float(top) * f);
       s = __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
     } else {
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -201,13 +230,14 @@ __global__ void __launch_bounds__(256) fp4_quantize_kernel(QuantArgs a) {
     if (!(s > 0.f)) code = make_uint2(0, 0);
     // four blocks' scales are neighbours: gathered into a word
     uint32_t word = byte;
-    constexpr int kApart = BLOCK / kLane;                    // lanes from one block to the next
 #pragma unroll
     for (int k = 1; k < 4; ++k) word |= __shfl_down_sync(0xffffffffu, byte, k * kApart) << (8 * k);
     if (c < cols) {
-      *reinterpret_cast<uint2*>(a.codes + code_at(r, c, a.slabs)) = code;
-      if (lane % (4 * kApart) == 0) *reinterpret_cast<uint32_t*>(a.scales + scale_at<BLOCK>(r, c, a.slabs)) = word;
+      *reinterpret_cast<uint2*>(codes) = code;
+      if (lane % (4 * kApart) == 0) *reinterpret_cast<uint32_t*>(scales) = word;
     }
+    codes += kTilesPerStep * kTileBytes;
+    scales += kTilesPerStep * groups_per_slab(BLOCK) * kGroupBytes;
   }
 }
 
@@ -220,34 +250,47 @@ struct ValueArgs {
   void* out;
 };
 
+// A lane takes 8 neighbouring columns of each tile, so that a warp's stores are whole lines; the loads of kAhead tiles go first.
 template <typename O, int BLOCK>
 __global__ void __launch_bounds__(256) fp4_values_kernel(ValueArgs a) {
+  constexpr int kAhead = 4, kCols = kSlab / 32;
   const int lane = threadIdx.x & 31;
   const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
   if (r >= a.T) return;
   const float row = BLOCK == 16 ? a.row_scale[r] : 1.f;
-  O* out = static_cast<O*>(a.out) + r * a.d;
-  for (int c = lane * kLane; c < a.d; c += kStep) {
-    const uint2 code = *reinterpret_cast<const uint2*>(a.codes + code_at(r, c, a.slabs));
-    const uint32_t byte = a.scales[scale_at<BLOCK>(r, c, a.slabs)];
-    float s;
-    if constexpr (BLOCK == 16) s = row * __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte, __NV_E4M3)));
-    else s = byte == 255 ? __uint_as_float(0x7fffffffu) : (byte == 0 ? 0x1p-127f : __uint_as_float(byte << 23));
-    float v[16];
+  O* out = static_cast<O*>(a.out) + r * a.d + lane * kCols;
+  const uint8_t* codes = a.codes + code_at(r, lane * kCols, a.slabs);
+  const uint8_t* scales = a.scales + scale_at<BLOCK>(r, lane * kCols, a.slabs);
+  for (int t0 = 0; t0 < a.slabs; t0 += kAhead) {
+    uint32_t w[kAhead], byte[kAhead];
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-      const uint32_t w = i < 8 ? code.x : code.y;
-      const float2 y = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w >> (4 * (i % 8))), __NV_E2M1)));
-      v[i] = y.x * s;
-      v[i + 1] = y.y * s;
+    for (int q = 0; q < kAhead; ++q) {
+      if (t0 + q < a.slabs) {
+        w[q] = *reinterpret_cast<const uint32_t*>(codes + (size_t)(t0 + q) * kTileBytes);
+        byte[q] = scales[(size_t)(t0 + q) * groups_per_slab(BLOCK) * kGroupBytes];
+      }
     }
-    constexpr int VEC = rowvec::Elem<O>::kVec;
 #pragma unroll
-    for (int i = 0; i < 16; i += VEC) {
-      float part[VEC];
+    for (int q = 0; q < kAhead; ++q) {
+      if ((t0 + q) * kSlab + lane * kCols >= a.d) break;
+      float s;
+      if constexpr (BLOCK == 16) s = row * __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)byte[q], __NV_E4M3)));
+      else s = byte[q] == 255 ? __uint_as_float(0x7fffffffu) : (byte[q] == 0 ? 0x1p-127f : __uint_as_float(byte[q] << 23));
+      float v[kCols];
 #pragma unroll
-      for (int k = 0; k < VEC; ++k) part[k] = v[i + k];
-      rowvec::store<O, VEC>(out + c + i, part);
+      for (int i = 0; i < kCols; i += 2) {
+        const float2 y = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w[q] >> (4 * i)), __NV_E2M1)));
+        v[i] = y.x * s;
+        v[i + 1] = y.y * s;
+      }
+      constexpr int VEC = rowvec::Elem<O>::kVec;
+#pragma unroll
+      for (int i = 0; i < kCols; i += VEC) {
+        float part[VEC];
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) part[k] = v[i + k];
+        rowvec::store<O, VEC>(out + (size_t)(t0 + q) * kSlab + i, part);
+      }
     }
   }
 }

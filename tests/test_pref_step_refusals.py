@@ -4,6 +4,7 @@ call here gets past them."""
 import ctypes as C
 
 import pytest
+import torch
 
 from paper_2602_14338_b200 import binding as B
 
@@ -146,3 +147,23 @@ def test_pref_refusals(lib, fake):
         assert call(dH=None) == INVALID and call(dW=None) == INVALID and call(dH=P + 8) == INVALID and call(dW=P + 4) == INVALID
         assert call(dt=4) == UNSUPPORTED and call(dt=B.AERO_BF16, acc=1) == INVALID
         assert call(dt=B.AERO_BF16, c=cfg(B.AERO_FP32)) == UNSUPPORTED
+
+
+@pytest.mark.parametrize("rows,cols", [(0, 32), (1, 32), (128, 256), (129, 288), (1000, 65536)])
+@pytest.mark.parametrize("block", [16, 32])
+def test_buffers_of_fp4_rows_have_the_sizes_of_the_library(lib, rows, cols, block):
+    r = B.Fp4Rows(rows, cols, block, device="meta")
+    assert r.codes.numel() == lib.aero_fp4_code_bytes(rows, cols) and r.scales.numel() == lib.aero_fp4_scale_bytes(rows, cols, block)
+    assert (r.row_scale is None) if block == 32 else r.row_scale.numel() == rows
+
+
+def test_binding_refusals():
+    for bad in (dict(rows=4, cols=48), dict(rows=4, cols=64, block=8), dict(rows=-1, cols=64)):
+        with pytest.raises(B.AeroError):
+            B.Fp4Rows(**bad, device="meta")
+    with pytest.raises(B.AeroError):
+        B.Fp4Rows(4, 64, 16, codes=torch.zeros(7, dtype=torch.uint8))
+    n = torch.zeros(8)
+    for bad in (dict(param=n, grad=n, m=n, v=n), dict(param=n, grad=n, m=n, v=n, lr=1.0)):          # host tensors, an unknown key
+        with pytest.raises(B.AeroError):
+            B.AdamWPlan([bad])
