@@ -634,9 +634,10 @@ int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t*
  *     AERO_PREF_HINGE     l = max(0, 1 - m)     (slope 0 at m = 1)
  *   coef_i = d loss / d logp_t of each scored token of rollout i
  *   dz_tv  = grad_scale coef_i (1[v == y_t] - p_tv);   dH = dz W,   dW (+)= dz^T H
- * A rollout may be in any number of pairs; the rows of one that is in none are not touched (their outputs are 0).  A pair (-1, -1)
+ * A rollout may be in any number of pairs; the rows of one that is in none are not read.  A pair (-1, -1)
  * is an empty place; one that names any other rollout outside [0,R) raises AERO_ST_BAD_PAIR and does not count.  Empty places
- * have margin 0.  A rollout whose offsets leave [0,T] raises AERO_ST_BAD_OFFSETS and counts as one without tokens.
+ * have margin 0.  A rollout whose offsets leave [0,T] raises AERO_ST_BAD_OFFSETS and counts as one without tokens; so do all of them
+ * where offsets overlap so that they have more than T scored tokens.  Rows that are not scored have logp = lse = 0 and dH = 0.
  * Inputs   y [T] i32, ref_logp [T] f32 or NULL, cs [R+1] i64, pairs [P,2] i32 (8-byte aligned), pair_weight [P] f32 or NULL.
  * Outputs  logp, lse [T], ratio, coef [R], margin [P] f32; loss [1] f32; metrics [4] f32 or NULL: fraction of the pairs with
  *          r_chosen > r_rejected, mean beta r_chosen, mean beta r_rejected, number of pairs that count; dH [T,d] (cfg->dtype), dW

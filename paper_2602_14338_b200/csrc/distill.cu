@@ -457,7 +457,8 @@ __global__ void __launch_bounds__(256) distill_scatter_kernel(BlockArgs b) {
 
 // dH of the chunk's rows from the fp32 sums of the ranges, added in order; a warp takes 256 columns of a row.
 __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const int* __restrict__ ksplit,
-                                                              const float* __restrict__ part, __nv_bfloat16* __restrict__ dH) {
+                                                              const float* __restrict__ part, const float* __restrict__ factor,
+                                                              __nv_bfloat16* __restrict__ dH) {
   const int ks = *ksplit;
   if (ks <= 1) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -476,7 +477,30 @@ __global__ void __launch_bounds__(256) distill_join_dh_kernel(RowsArgs a, const 
       s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
       s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
     }
+    if (factor) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) s[e] *= factor[t];
+    }
     rowvec::store<__nv_bfloat16, 8>(dH + t * a.d + c, s);
+  }
+}
+
+// The chunk's rows of H times the factors of their rows (AeroListed::row_factor).
+__global__ void __launch_bounds__(256) distill_scale_rows_kernel(RowsArgs a, const float* __restrict__ factor) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long n = units_of(a);
+  for (long long u = blockIdx.x; u < n; u += gridDim.x) {
+    const long long t = row_of(a, u, warp);
+    if (t < 0) continue;
+    const float f = factor[t];
+    uint4* p = reinterpret_cast<uint4*>(a.Hl + ((size_t)u * 8 + warp) * a.d);
+    for (int k = lane; k < a.d / 8; k += 32) {
+      float x[8];
+      rowvec::unpack(p[k], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] *= f;
+      p[k] = rowvec::pack(x);
+    }
   }
 }
 
@@ -491,6 +515,7 @@ struct FirstArgs {
   const float* logits;
   const int64_t* cs;
   const float* w;
+  const float* w_row;      // [T] weights of rows in place of w, or NULL
   const uint8_t* keep;
   int32_t* y;
   float* wrow;
@@ -536,7 +561,7 @@ __global__ void __launch_bounds__(256) distill_first_kernel(FirstArgs a) {
     if (__any_sync(0xffffffffu, bad) && lane == 0) aero_raise(a.status, AERO_ST_BAD_TARGET);
     if (lane == 0) {
       a.y[t] = first < a.K ? a.ids[t * a.K + first] : 0;
-      a.wrow[t] = a.w[owner];
+      a.wrow[t] = a.w_row ? a.w_row[t] : a.w[owner];
     }
   }
 }
@@ -945,7 +970,7 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
   AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, zero_bytes((size_t)chunk_tiles), ctx->stream));
   if (partials) AERO_CUDA_TRY(cudaMemsetAsync(s.partials, 0, s.n_partials * kPartialStride * sizeof(double), ctx->stream));
   if (c.T == 0) return AERO_OK;
-  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.logits, c.cs, c.w, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
+  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.logits, c.cs, c.w, c.ex.row_weights, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
                        ctx->d_status};
   distill_first_kernel<<<row_grid(c.T), 256, 0, ctx->stream>>>(f);
   ctx->launches += 1;
@@ -1161,16 +1186,6 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
       p.range_rows = s.range_rows; p.range_count = s.range_count; p.range_seen = s.range_seen; p.range_cap = kRangeCap;
       if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmDZ_st, kBoth))) return rc;
       a.xstate = s.xstate;
-      if (c.ex.between) {
-        // the rows' log-probs alone; then their weights, which depend on all of them; then the pass below as ever
-        RowsArgs first = a;
-        first.ls.entry = nullptr; first.ls.partials = nullptr; first.g = nullptr; first.Hl = nullptr;
-        distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(first);
-        ctx->launches += 1;
-        if ((rc = c.ex.between(c.ex.arg, s.wrow))) return rc;
-        a.ls.kl = nullptr; a.ls.partials = nullptr;
-        b.a = a;
-      }
       distill_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a);
       distill_scale_kernel<<<dim3((unsigned)b.nvt, (unsigned)(end - begin < 64 ? end - begin : 64)), 256, 0, ctx->stream>>>(b);
       RangeArgs f = {};
@@ -1191,6 +1206,11 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
       ctx->launches += 1;
     }
     distill_scatter_kernel<<<row_blocks, 256, 0, ctx->stream>>>(b);
+    if (c.ex.between && (rc = c.ex.between(c.ex.arg))) return rc;
+    if (c.ex.row_factor) {
+      distill_scale_rows_kernel<<<row_blocks, 256, 0, ctx->stream>>>(a, c.ex.row_factor);
+      ctx->launches += 1;
+    }
     gemmbwd::Params gp = {};
     gp.T = c.T; gp.d = d; gp.V = V; gp.ldz = ldz;
     gp.tile_row = s.tiles.tile_row; gp.tile_valid = s.tiles.tile_valid; gp.n_tiles = s.tiles.n_tiles;
@@ -1198,12 +1218,13 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     gp.dH = gr.dH; gp.dW = gr.dW; gp.status = ctx->d_status;
     gp.out = gr.dW16 ? gemmbwd::kOutBf16 : (begin == 0 && !gr.accumulate ? gemmbwd::kOutFp32 : 0);
     gp.h_local = 1;
+    gp.row_scale = c.ex.row_factor;
     gp.ksplit = s.k_hi > 1 ? s.plan + 1 : nullptr; gp.part = s.part;
     gp.nsync = many ? aero_gemm_sync(ctx) : 0;
     gp.sync_ctr = reinterpret_cast<unsigned int*>(s.zero) + 4;
     k_dh<<<gemm_grid, gemmbwd::THREADS, dh_smem, ctx->stream>>>(tmDZ_k, tmW_mn, tmDZ_k, gp);
     if (s.k_hi > 1) {
-      distill_join_dh_kernel<<<dim3(row_blocks, (unsigned)((d + 255) / 256)), 256, 0, ctx->stream>>>(a, s.plan + 1, s.part, gr.dH);
+      distill_join_dh_kernel<<<dim3(row_blocks, (unsigned)((d + 255) / 256)), 256, 0, ctx->stream>>>(a, s.plan + 1, s.part, c.ex.row_factor, gr.dH);
       ctx->launches += 1;
     }
     gp.sync_ctr = reinterpret_cast<unsigned int*>(s.zero) + 8;

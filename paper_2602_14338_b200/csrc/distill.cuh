@@ -6,9 +6,14 @@
 
 struct AeroListed {
   bool gain = false;                    // log-probs with lmhead::Params::z_gain
-  // One-call step whose rows fit one chunk: called when the rows' log-probs are there and before their weights are used, to write
-  // these (wrow [T], rows of kept rollouts only) on the context's stream.  NULL: the weights are w's.
-  int (*between)(void* arg, float* wrow) = nullptr;
+  const float* row_weights = nullptr;   // [T] in place of w (fp32 rows)
+  // bf16 rows: factors of the rows' gradients that are left out of dz [T], on top of the weights.  They go on the finished rows of dH and,
+  // rounded once, on the rows of H that enter dW: with one listed token per row the largest entry of dz is close to its weight,
+  // and one weight for all tokens of a rollout would be rounded with the same error in all of them.
+  const float* row_factor = nullptr;
+  // One-call step whose rows fit one chunk: called when the rows' log-probs are there and before the factors are used, to write
+  // these on the context's stream.
+  int (*between)(void* arg) = nullptr;
   void* arg = nullptr;
 };
 

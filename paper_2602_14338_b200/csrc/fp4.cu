@@ -343,13 +343,15 @@ struct Params {
 };
 
 // Writes the accumulator columns of tokens t0 .. t0 + n of vocabulary row v: a thread has one row, so the 32 lanes of a warp store
-// 32 neighbouring logits of a token at a time; the two warps of a quadrant of TMEM take chunks of 32 tokens in turn.  The tokens'
-// scales come from a lane each, loaded before the accumulator is waited for.
+// 32 neighbouring logits of a token at a time; the two warps of a quadrant of TMEM take chunks of 32 tokens in turn.  The rows'
+// scales are loaded before the accumulator is waited for, a token's by a lane each.
 template <typename O, int N>
 struct Epilogue {
   static constexpr int kChunks = (N / 32 + kShare - 1) / kShare;
   float sh[kChunks];
-  __device__ void load_scales(const Params& p, int t0, int half, int lane) {
+  float sw;
+  __device__ void load_scales(const Params& p, int t0, int half, int lane, int v) {
+    sw = v < p.V && p.w.row ? p.w.row[v] : 1.f;
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
       const int t = (kShare * i + half) * 32 + lane;
@@ -357,7 +359,6 @@ struct Epilogue {
     }
   }
   __device__ void store(const Params& p, uint32_t taddr, int t0, int half, int v, bool row_ok) const {
-    const float sw = row_ok && p.w.row ? p.w.row[v] : 1.f;
     const int n = min(p.n, p.T - t0);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
@@ -498,12 +499,12 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
     uint32_t at = 0;
     const int quad = warp & 3, half = warp >> 2;
     Epilogue<O, kRowsN> epi;
-    epi.load_scales(p, 0, half, lane);
     for (int b = b0; b < b1; b += step(b), ++at) {
       const uint32_t buf = at & 1u;
+      const int first = b % kPerTile, v = b / kPerTile * kTile + quad * 32 + lane;
+      epi.load_scales(p, 0, half, lane, v);
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], (at >> 1) & 1u, abort_flag))) break;
       tc::tc_fence_after();
-      const int first = b % kPerTile, v = b / kPerTile * kTile + quad * 32 + lane;
       if (quad >= first && quad < first + step(b))         // this warp's block of 32 rows is among this CTA's
         epi.store(p, tmem_base + ((uint32_t)(quad * 32) << 16) + buf * kRowsN, 0, half, v, v < p.V);
       tc::tc_fence_before();
@@ -671,14 +672,14 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     for (long long u = pair; u < units; u += npairs, ++at) {
       const int t0 = (int)(u % p.n_tok) * p.n;
       const uint32_t buf = at & 1u;
-      epi.load_scales(p, t0, half, lane);
+      const int v = (int)(u / p.n_tok) * 2 * kTile + (int)rank * kTile + quad * 32 + lane;
+      epi.load_scales(p, t0, half, lane, v);
       if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], (at >> 1) & 1u, abort_flag))) break;
       tc::tc_fence_after();
-      const int v = (int)(u / p.n_tok) * 2 * kTile + (int)rank * kTile + quad * 32 + lane;
       epi.store(p, tmem_base + ((uint32_t)(quad * 32) << 16) + buf * kPairN, t0, half, v, v < p.V);
       tc::tc_fence_before();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive_cluster(tc::mapa_shared(tc::smem_u32(&ctl->tempty[buf]), 0));
+      if (lane == 0) tc::mbar_arrive_cluster_bare(tc::mapa_shared(tc::smem_u32(&ctl->tempty[buf]), 0));     // (TMEM has been read)
     }
   }
   __syncwarp();

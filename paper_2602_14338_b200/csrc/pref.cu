@@ -3,55 +3,102 @@
 //   loss = sum_p u_p l(m_p),   coef_i = (sum_{p: c = i} - sum_{p: r = i}) u_p beta l'(m_p) [/ scored tokens of i]
 //   dz_tv = grad_scale coef_i (1[v = y_t] - p_tv),   dH = dz W,   dW (+)= dz^T H
 // Everything between H, W and the log-probs, and between coef and dH, dW, is distillation's with one listed token per row
-// (distill.cuh); what is here are the sums over rollouts and pairs.  The gradient of a row needs all rows of all of its rollout's
-// pairs, so the one-call step computes the log-probs of a chunk, then coef, then the chunk's gradients; rows that do not fit
-// one chunk of the workspace take the separate passes, which compute the logits twice (8 d V FLOP per token instead of 6).
-// The kernels here read 12 bytes per token and 8 bytes per pair and rollout: microseconds beside the products.  All sums are in
-// 64 bits and have a fixed order.
+// (distill.cuh); what is here are the sums over rollouts and pairs.  The products are what a call takes its time for, and
+// their row tiles are of 128, so the scored rows of the rollouts in pairs are first gathered into one run (prompts, padding and
+// rollouts in no pair cost nothing but that copy): at T = 333 with 253 scored rows two tiles instead of three.
+// The gradient of a row needs all rows of all of its rollout's pairs, so the one-call step computes the log-probs of a chunk, then
+// coef, then the chunk's gradients; rows that do not fit one chunk of the workspace take the separate passes, which compute the
+// logits twice (8 d V FLOP per token instead of 6).  The kernels here read 16 bytes per token, 8 bytes per pair and rollout and
+// copy the rows: microseconds beside the products.  All sums are in 64 bits and have a fixed order.
 #include "distill.cuh"
 #include "entry.cuh"
 #include "loss_common.cuh"
 
 namespace {
 
-constexpr int kPairBlocks = 148, kThreads = 128;
+constexpr int kPairBlocks = 148, kThreads = 128, kPlanThreads = 1024;
 
 struct PrefArgs {
   long long T;
-  int V, R, P;
+  int d, V, R, P;
+  int elem;                       // bytes of an element of H
+  int backward;                   // the backward alone: rollouts whose coef is not 0, lse given
   int kind, mean;
   double beta, margin, smoothing;
+  const void* H;
   const int32_t* y;
   const float* ref;               // NULL: no reference
   const int64_t* cs;
   const int32_t* pairs;           // [P][2]
   const float* weight;            // NULL: 1 / counted pairs
+  const float* coef_in;
+  const float* lse_in;
+  // gathered rows: src[p] is the token row of gathered row p, rollout i owns off[i] .. off[i + 1]
   uint8_t* keep;                  // rollouts in some counted pair
   int* counted;                   // pairs counted
+  int64_t* off;                   // [R + 1]
+  int64_t* run;                   // [2]: 0 and the number of gathered rows
+  uint8_t* one;                   // [1]: 1, the run is kept
+  int32_t* src;                   // [T]
+  uint8_t* Hg;                    // [T][d]
+  int32_t* yg;                    // [T]
+  float* lseg;                    // [T]
+  float* klg;                     // [T] minus the log-probs
+  uint8_t* dHg;                   // [T][d], with gradients
+  float* row_weights;             // [T] -grad_scale coef of the row's rollout
+  float* w;                       // [1]: 1
+  float grad_scale;
   double* r;                      // [R] log ratios
-  int* scored;                    // [R]
   double* slope;                  // [P] d loss / d r_chosen
   double* partials;               // [kPairBlocks][kPartialStride]
-  float* logp;                    // in: minus the log-probs
+  float* logp;
+  float* lse;
   float* ratio;
   float* margins;
   float* coef;
-  float* w;                       // [R] -coef
-  float* wrow;                    // [T], or NULL
   uint32_t* status;
 };
 
 // A pair that counts: both rollouts exist.  (-1, -1) is an empty place.
 __device__ __forceinline__ bool pair_of(const PrefArgs& a, int p, int* c, int* r) {
-  *c = a.pairs[2 * (long long)p];
-  *r = a.pairs[2 * (long long)p + 1];
+  const int2 q = reinterpret_cast<const int2*>(a.pairs)[p];
+  *c = q.x;
+  *r = q.y;
   return *c >= 0 && *c < a.R && *r >= 0 && *r < a.R;
 }
 
-__global__ void __launch_bounds__(256) pref_mark_kernel(PrefArgs a) {
+// Rows t0 .. t1 of a rollout that is used, none where its offsets leave [0, T].
+__device__ __forceinline__ bool rows_of(const PrefArgs& a, int i, long long* t0, long long* t1) {
+  *t0 = a.cs[i];
+  *t1 = a.cs[i + 1];
+  return a.keep[i] != 0 && *t0 >= 0 && *t1 >= *t0 && *t1 <= a.T;
+}
+__device__ __forceinline__ bool scored(const PrefArgs& a, long long t) { return a.y[t] >= 0 && a.y[t] < a.V; }
+
+// f(t, whether the row is scored, scored rows of its group of 32 as a word) by the 32 lanes of a warp, four groups' loads at a time.
+template <typename F>
+__device__ __forceinline__ void for_rows(const PrefArgs& a, long long t0, long long t1, int lane, F&& f) {
+  for (long long t = t0; t < t1; t += 128) {
+    bool s[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s[q] = t + 32 * q + lane < t1 && scored(a, t + 32 * q + lane);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) f(t + 32 * q + lane, s[q], __ballot_sync(0xffffffffu, s[q]));
+  }
+}
+
+// One block: which rollouts are used, where their scored rows go, and the list of these rows.  (A warp reads a rollout's targets at a few
+// GB/s, 4 bytes a token: 1 % of the time of the products at the smallest vocabularies.)
+__global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
+  __shared__ long long sums[32];
+  __shared__ int total;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) total = 0;
+  for (int i = threadIdx.x; i < a.R; i += kPlanThreads) a.keep[i] = a.backward && a.coef_in[i] != 0.f ? 1 : 0;
+  __syncthreads();
   int n = 0;
   bool bad = false;
-  for (int p = blockIdx.x * 256 + threadIdx.x; p < a.P; p += gridDim.x * 256) {
+  for (int p = threadIdx.x; p < a.P; p += kPlanThreads) {
     int c, r;
     if (pair_of(a, p, &c, &r)) {
       a.keep[c] = 1;
@@ -62,8 +109,104 @@ __global__ void __launch_bounds__(256) pref_mark_kernel(PrefArgs a) {
     }
   }
   n = __reduce_add_sync(0xffffffffu, n);
-  if ((threadIdx.x & 31) == 0 && n) atomicAdd(a.counted, n);
+  if (lane == 0 && n) atomicAdd(&total, n);
   if (bad) aero_raise(a.status, AERO_ST_BAD_PAIR);
+  __syncthreads();
+  // scored rows of each rollout (at most T in all where offsets do not overlap), then their running sums
+  for (int i = warp; i < a.R; i += 32) {
+    long long t0, t1, rows = 0;
+    if (rows_of(a, i, &t0, &t1)) {
+      bool wrong = false;
+      for_rows(a, t0, t1, lane, [&](long long t, bool s, unsigned word) {
+        rows += __popc(word);
+        wrong |= t < t1 && !s && a.y[t] != AERO_NO_TOKEN;
+      });
+      if (wrong) aero_raise(a.status, AERO_ST_BAD_TARGET);
+    } else if (lane == 0 && !(t0 >= 0 && t1 >= t0 && t1 <= a.T)) {
+      aero_raise(a.status, AERO_ST_BAD_OFFSETS);
+    }
+    if (lane == 0) a.off[i + 1] = rows;
+  }
+  __syncthreads();
+  long long carry = 0;
+  for (int base = 0; base < a.R; base += kPlanThreads) {
+    const int i = base + threadIdx.x;
+    long long v = i < a.R ? a.off[i + 1] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
+    }
+    if (lane == 31) sums[warp] = v;
+    __syncthreads();
+    if (warp == 0) {
+      long long s = sums[lane];
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += u;
+      }
+      sums[lane] = s;
+    }
+    __syncthreads();
+    v += carry + (warp > 0 ? sums[warp - 1] : 0);
+    if (i < a.R) a.off[i + 1] = v;
+    carry += sums[31];
+    __syncthreads();
+  }
+  if (carry > a.T) {                                // offsets that overlap: no rollout has tokens
+    if (threadIdx.x == 0) aero_raise(a.status, AERO_ST_BAD_OFFSETS);
+    for (int i = threadIdx.x; i < a.R; i += kPlanThreads) a.keep[i] = a.off[i + 1] = 0;
+    carry = 0;
+  }
+  if (threadIdx.x == 0) {
+    a.off[0] = 0;
+    a.run[0] = 0;
+    a.run[1] = carry;
+    *a.one = 1;
+    *a.w = 1.f;
+    *a.counted = total;
+  }
+  __syncthreads();
+  for (int i = warp; i < a.R; i += 32) {
+    long long t0, t1, at = a.off[i];
+    if (rows_of(a, i, &t0, &t1))
+      for_rows(a, t0, t1, lane, [&](long long t, bool s, unsigned word) {
+        if (s) a.src[at + __popc(word & ((1u << lane) - 1u))] = (int32_t)t;
+        at += __popc(word);
+      });
+  }
+}
+
+// A warp per row: n16 16-byte vectors where both rows are made of such, else bytes.
+__device__ __forceinline__ void copy_row(uint8_t* dst, const uint8_t* src, int bytes, bool vec, int lane) {
+  if (vec) {
+    for (int k = lane; k < bytes / 16; k += 32) reinterpret_cast<uint4*>(dst)[k] = reinterpret_cast<const uint4*>(src)[k];
+  } else {
+    for (int k = lane; k < bytes / 4; k += 32) reinterpret_cast<uint32_t*>(dst)[k] = reinterpret_cast<const uint32_t*>(src)[k];
+  }
+}
+// The rows of H, their targets and, for the backward alone, lse and weights, into the run; GATHER false: the run's rows of dH to theirs.
+template <bool GATHER>
+__global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, uint8_t* dH) {
+  const int lane = threadIdx.x & 31, bytes = a.d * a.elem;
+  const bool vec = bytes % 16 == 0;
+  const long long n = a.run[1];
+  for (long long p = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); p < n; p += (long long)gridDim.x * 8) {
+    const long long t = a.src[p];
+    if (GATHER) {
+      copy_row(a.Hg + p * bytes, static_cast<const uint8_t*>(a.H) + t * bytes, bytes, vec, lane);
+      if (lane == 0) {
+        a.yg[p] = a.y[t];
+        if (a.backward) {
+          a.lseg[p] = a.lse_in[t];
+          a.row_weights[p] = -a.grad_scale * a.coef_in[aero_owner(a.off, a.R, p)];
+        }
+      }
+    } else {
+      copy_row(dH + t * bytes, a.dHg + p * bytes, bytes, vec, lane);
+    }
+  }
 }
 
 // Sum over the block's threads; every thread gets it.
@@ -78,39 +221,23 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return v;
 }
 
-// Rows a .. b of a rollout, none where its offsets leave [0, T].
-__device__ __forceinline__ bool rows_of(const PrefArgs& a, int i, long long* t0, long long* t1) {
-  *t0 = a.cs[i];
-  *t1 = a.cs[i + 1];
-  return *t0 >= 0 && *t1 >= *t0 && *t1 <= a.T;
-}
-
-// A block per rollout: its log ratio, and its tokens' log-probs (which arrive negated).
+// A block per rollout: its log ratio, and its tokens' outputs (the log-probs arrive negated).
 __global__ void __launch_bounds__(kThreads) pref_ratio_kernel(PrefArgs a) {
   __shared__ double sh[kThreads / 32];
   for (int i = blockIdx.x; i < a.R; i += gridDim.x) {
-    long long t0, t1;
+    const long long p0 = a.off[i], p1 = a.off[i + 1];
     double sum = 0.0;
-    int n = 0;
-    if (!rows_of(a, i, &t0, &t1)) {
-      if (threadIdx.x == 0) aero_raise(a.status, AERO_ST_BAD_OFFSETS);
-    } else if (a.keep[i]) {
-      for (long long t = t0 + threadIdx.x; t < t1; t += kThreads) {
-        const float lp = 0.f - a.logp[t];
-        const int v = a.y[t];
-        a.logp[t] = lp;
-        if (v >= 0 && v < a.V) {
-          sum += (double)lp - (a.ref ? (double)a.ref[t] : 0.0);
-          ++n;
-        }
-      }
+    for (long long p = p0 + threadIdx.x; p < p1; p += kThreads) {
+      const long long t = a.src[p];
+      const float lp = 0.f - a.klg[p];
+      a.logp[t] = lp;
+      a.lse[t] = a.lseg[p];
+      sum += (double)lp - (a.ref ? (double)a.ref[t] : 0.0);
     }
     sum = block_sum(sum, sh);
-    n = (int)block_sum((double)n, sh);
     if (threadIdx.x == 0) {
-      if (a.mean && n > 0) sum /= n;
+      if (a.mean && p1 > p0) sum /= (double)(p1 - p0);
       a.r[i] = sum;
-      a.scored[i] = n;
       a.ratio[i] = (float)sum;
     }
   }
@@ -172,59 +299,51 @@ __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PrefArgs a) {
       }
     }
     sum = block_sum(sum, sh);
-    if (a.mean && a.scored[i] > 0) sum /= a.scored[i];
+    const long long p0 = a.off[i], p1 = a.off[i + 1];
+    if (a.mean && p1 > p0) sum /= (double)(p1 - p0);
     const float coef = (float)sum;
-    if (threadIdx.x == 0) {
-      a.coef[i] = coef;
-      a.w[i] = -coef;
-    }
-    long long t0, t1;
-    if (a.wrow && a.keep[i] && rows_of(a, i, &t0, &t1))
-      for (long long t = t0 + threadIdx.x; t < t1; t += kThreads) a.wrow[t] = -coef;
-  }
-}
-
-// The backward alone: rollouts with a gradient, and their weights.
-__global__ void __launch_bounds__(256) pref_weights_kernel(int R, const float* __restrict__ coef, uint8_t* __restrict__ keep,
-                                                           float* __restrict__ w) {
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < R; i += gridDim.x * 256) {
-    keep[i] = coef[i] != 0.f ? 1 : 0;
-    w[i] = -coef[i];
+    if (threadIdx.x == 0) a.coef[i] = coef;
+    for (long long p = p0 + threadIdx.x; p < p1; p += kThreads) a.row_weights[p] = -a.grad_scale * coef;
   }
 }
 
 struct Ws {
-  uint8_t* keep;                  // starts at zero, with counted
-  int* counted;
+  PrefArgs a;                     // its buffers
   float* zeros;                   // [T]: the listed tokens' teacher logits
-  float* w;                       // [R]
-  double* r;
-  int* scored;
-  double* slope;
-  double* partials;
-  size_t zero_bytes;
   char* rest;
   size_t head_bytes;
 };
 
-Ws carve(void* base, int64_t T, int32_t R, int32_t P) {
+// (elem: bytes of an element of H; 0: whichever needs more)
+Ws carve(void* base, int64_t T, int32_t d, int32_t R, int32_t P, int elem, bool grads) {
   Ws s = {};
   char* p = static_cast<char*>(base);
   size_t off = 0;
   auto take = [&](size_t bytes) { char* q = p + off; off += aero_align_up(bytes, 256); return q; };
-  s.counted = reinterpret_cast<int*>(take(4));
-  s.keep = reinterpret_cast<uint8_t*>(take((size_t)R + 1));
-  s.zeros = reinterpret_cast<float*>(take((size_t)(T + 1) * 4));
-  s.w = reinterpret_cast<float*>(take((size_t)(R + 1) * 4));
-  s.zero_bytes = off;
-  s.r = reinterpret_cast<double*>(take((size_t)(R + 1) * 8));
-  s.scored = reinterpret_cast<int*>(take((size_t)(R + 1) * 4));
-  s.slope = reinterpret_cast<double*>(take((size_t)(P + 1) * 8));
-  s.partials = reinterpret_cast<double*>(take((size_t)kPairBlocks * kPartialStride * 8));
+  const size_t Tn = (size_t)T + 1, rows = Tn * (size_t)d * (elem ? elem : 4);
+  s.a.counted = reinterpret_cast<int*>(take(4));
+  s.a.one = reinterpret_cast<uint8_t*>(take(1));
+  s.a.run = reinterpret_cast<int64_t*>(take(16));
+  s.a.keep = reinterpret_cast<uint8_t*>(take((size_t)R + 1));
+  s.a.off = reinterpret_cast<int64_t*>(take((size_t)(R + 1) * 8));
+  s.a.src = reinterpret_cast<int32_t*>(take(Tn * 4));
+  s.a.yg = reinterpret_cast<int32_t*>(take(Tn * 4));
+  s.a.lseg = reinterpret_cast<float*>(take(Tn * 4));
+  s.a.klg = reinterpret_cast<float*>(take(Tn * 4));
+  s.a.row_weights = reinterpret_cast<float*>(take(Tn * 4));
+  s.zeros = reinterpret_cast<float*>(take(Tn * 4));
+  s.a.w = reinterpret_cast<float*>(take(4));
+  s.a.r = reinterpret_cast<double*>(take((size_t)(R + 1) * 8));
+  s.a.slope = reinterpret_cast<double*>(take((size_t)(P + 1) * 8));
+  s.a.partials = reinterpret_cast<double*>(take((size_t)kPairBlocks * kPartialStride * 8));
+  s.a.Hg = reinterpret_cast<uint8_t*>(take(rows));
+  if (grads) s.a.dHg = reinterpret_cast<uint8_t*>(take(rows));
   s.rest = p + off;
   s.head_bytes = off;
   return s;
 }
+
+int elem_of(const aero_cfg* cfg) { return cfg && cfg->dtype == AERO_BF16 ? 2 : 4; }
 
 int grid_for(long long n, int per, int most) {
   const long long blocks = (n + per - 1) / per;
@@ -240,52 +359,90 @@ int check_pref(const aero_pref_cfg* pc, int32_t P, const int32_t* pairs) {
   return AERO_OK;
 }
 
-int check_call(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_t T, int32_t d, int32_t V, int32_t R, int32_t P,
-               const void* H, const void* W, const int32_t* y, const int64_t* cs, const int32_t* pairs, const float* logp,
-               const float* lse, const float* ratio, const float* margin, const float* coef, const float* loss, const Ws& s,
-               const void* workspace) {
-  int rc = check_pref(pc, P, pairs);
-  if (rc) return rc;
-  if (!cfg || !workspace || !loss || (R > 0 && (!ratio || !coef)) || (P > 0 && !margin) || (T > 0 && (!logp || !lse)))
-    return AERO_ERR_INVALID;
-  return aero_distill_check(ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, cs, s.w, s.keep, workspace);
-}
-
-// What stands between the log-probs and the gradients.
-struct Between {
+// One call: the user's arrays, the workspace, and the pieces that the three entry points put together.
+struct Call {
   aero_ctx* ctx;
-  PrefArgs a;
+  const aero_cfg* cfg;
+  Ws s;
+  const void* W;
   float *loss, *metrics;
 
-  int run(float* wrow) {
-    a.wrow = wrow;
-    const int rollouts = grid_for(a.R, 1, 65535);
-    if (a.R > 0) pref_ratio_kernel<<<rollouts, kThreads, 0, ctx->stream>>>(a);
-    const int blocks = grid_for(a.P, kThreads, kPairBlocks);
-    pref_pairs_kernel<<<blocks, kThreads, 0, ctx->stream>>>(a);
-    if (a.R > 0) pref_coef_kernel<<<rollouts, kThreads, 0, ctx->stream>>>(a);
-    ctx->launches += a.R > 0 ? 3 : 1;
-    AERO_CUDA_TRY(cudaGetLastError());
-    return aero_loss_finalize(ctx, a.partials, blocks, kPartialStride, loss, metrics, 0);
+  int check(const void* workspace) {
+    if (!cfg || !workspace || s.a.R < 0) return AERO_ERR_INVALID;
+    // (as the calls below check them; H and y are the caller's, the rest stands for what the workspace holds)
+    return aero_distill_check(ctx, cfg, s.a.T, s.a.d, s.a.V, s.a.R, 1, s.a.H, W, s.a.y, reinterpret_cast<const float*>(workspace), s.a.cs,
+                              reinterpret_cast<const float*>(workspace), static_cast<const uint8_t*>(workspace), workspace);
   }
-  static int call(void* self, float* wrow) { return static_cast<Between*>(self)->run(wrow); }
+  int check_forward(const aero_pref_cfg* pc, const void* workspace) {
+    const PrefArgs& p = s.a;
+    int rc = check_pref(pc, p.P, p.pairs);
+    if (rc) return rc;
+    if (!loss || (p.R > 0 && (!p.ratio || !p.coef)) || (p.P > 0 && !p.margins) || (p.T > 0 && (!p.logp || !p.lse))) return AERO_ERR_INVALID;
+    return check(workspace);
+  }
+
+  int gather() {
+    const cudaStream_t stream = ctx->stream;
+    if (!s.a.backward && s.a.T > 0) {
+      AERO_CUDA_TRY(cudaMemsetAsync(s.a.logp, 0, (size_t)s.a.T * 4, stream));
+      AERO_CUDA_TRY(cudaMemsetAsync(s.a.lse, 0, (size_t)s.a.T * 4, stream));
+    }
+    AERO_CUDA_TRY(cudaMemsetAsync(s.zeros, 0, (size_t)s.a.T * 4 + 4, stream));
+    pref_plan_kernel<<<1, kPlanThreads, 0, stream>>>(s.a);
+    if (s.a.T > 0) pref_rows_kernel<true><<<grid_for(s.a.T, 8, 16 * ctx->sm_count), 256, 0, stream>>>(s.a, nullptr);
+    ctx->launches += s.a.T > 0 ? 2 : 1;
+    AERO_CUDA_TRY(cudaGetLastError());
+    return AERO_OK;
+  }
+
+  int forward(const AeroListed& ex, size_t room) {
+    return aero_distill_fwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.zeros, nullptr,
+                                   s.a.run, s.a.w, s.a.one, s.a.lseg, s.a.klg, nullptr, nullptr, s.rest,
+                                   room);
+  }
+
+  // What stands between the log-probs and the gradients.
+  int pairs() {
+    const int rollouts = grid_for(s.a.R, 1, 65535);
+    if (s.a.R > 0) pref_ratio_kernel<<<rollouts, kThreads, 0, ctx->stream>>>(s.a);
+    const int blocks = grid_for(s.a.P, kThreads, kPairBlocks);
+    pref_pairs_kernel<<<blocks, kThreads, 0, ctx->stream>>>(s.a);
+    if (s.a.R > 0) pref_coef_kernel<<<rollouts, kThreads, 0, ctx->stream>>>(s.a);
+    ctx->launches += s.a.R > 0 ? 3 : 1;
+    AERO_CUDA_TRY(cudaGetLastError());
+    return aero_loss_finalize(ctx, s.a.partials, blocks, kPartialStride, loss, metrics, 0);
+  }
+  static int between(void* self) { return static_cast<Call*>(self)->pairs(); }
+
+  int backward(void* dW, int32_t dw_dtype, int accumulate_dW, size_t room) {
+    AeroListed ex;
+    (cfg->dtype == AERO_BF16 ? ex.row_factor : ex.row_weights) = s.a.row_weights;
+    return aero_distill_bwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.zeros, nullptr,
+                                   s.a.run, s.a.w, s.a.one, s.a.lseg, 1.f, s.a.dHg, dW, dw_dtype,
+                                   accumulate_dW, s.rest, room);
+  }
+
+  int scatter(void* dH) {
+    if (s.a.T == 0) return AERO_OK;
+    AERO_CUDA_TRY(cudaMemsetAsync(dH, 0, (size_t)s.a.T * s.a.d * s.a.elem, ctx->stream));
+    pref_rows_kernel<false><<<grid_for(s.a.T, 8, 16 * ctx->sm_count), 256, 0, ctx->stream>>>(s.a, static_cast<uint8_t*>(dH));
+    ctx->launches += 1;
+    AERO_CUDA_TRY(cudaGetLastError());
+    return AERO_OK;
+  }
 };
 
-int begin(aero_ctx* ctx, const Ws& s, const PrefArgs& a) {
-  AERO_CUDA_TRY(cudaMemsetAsync(s.counted, 0, s.zero_bytes, ctx->stream));
-  if (a.P > 0) {
-    pref_mark_kernel<<<grid_for(a.P, 256, 592), 256, 0, ctx->stream>>>(a);
-    ctx->launches += 1;
+Call call_of(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_t T, int32_t d, int32_t V, int32_t R, int32_t P,
+             const void* H, const void* W, const int32_t* y, const int64_t* cs, void* workspace, bool grads) {
+  Call c = {ctx, cfg, carve(workspace, T > 0 ? T : 0, d > 0 ? d : 0, R > 0 ? R : 0, P > 0 ? P : 0, elem_of(cfg), grads), W, nullptr,
+            nullptr};
+  PrefArgs& a = c.s.a;
+  a.T = T; a.d = d; a.V = V; a.R = R; a.P = P; a.elem = elem_of(cfg); a.H = H; a.y = y; a.cs = cs;
+  if (ctx) a.status = ctx->d_status;
+  if (pc) {
+    a.kind = pc->kind; a.mean = pc->mean; a.beta = pc->beta; a.margin = pc->margin; a.smoothing = pc->label_smoothing;
   }
-  AERO_CUDA_TRY(cudaGetLastError());
-  return AERO_OK;
-}
-
-PrefArgs args_of(aero_ctx* ctx, const aero_pref_cfg* pc, int64_t T, int32_t V, int32_t R, int32_t P, const int32_t* y,
-                 const float* ref, const int64_t* cs, const int32_t* pairs, const float* weight, const Ws& s, float* logp, float* ratio,
-                 float* margin, float* coef) {
-  return {T, V, R, P, pc->kind, pc->mean, pc->beta, pc->margin, pc->label_smoothing, y, ref, cs, pairs, weight, s.keep, s.counted,
-          s.r, s.scored, s.slope, s.partials, logp, ratio, margin, coef, s.w, nullptr, ctx->d_status};
+  return c;
 }
 
 }  // namespace
@@ -298,22 +455,22 @@ void aero_pref_cfg_default(aero_pref_cfg* pc) {
 }
 
 size_t aero_pref_fwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t P) {
-  const size_t inner = aero_distill_fwd_workspace_bytes(T, d, V, R, 1);
-  return inner == 0 || P < 0 ? 0 : carve(nullptr, T, R, P).head_bytes + inner;
+  const size_t inner = aero_distill_fwd_workspace_bytes(T, d, V, 1, 1);
+  return inner == 0 || R < 0 || P < 0 ? 0 : carve(nullptr, T, d, R, P, 0, false).head_bytes + inner;
 }
 
 size_t aero_pref_bwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int64_t chunk_tokens, int32_t dw_dtype) {
-  const size_t inner = aero_distill_bwd_workspace_bytes(T, d, V, R, 1, chunk_tokens, dw_dtype);
-  return inner == 0 ? 0 : carve(nullptr, T, R, 0).head_bytes + inner;
+  const size_t inner = aero_distill_bwd_workspace_bytes(T, d, V, 1, 1, chunk_tokens, dw_dtype);
+  return inner == 0 || R < 0 ? 0 : carve(nullptr, T, d, R, 0, 0, true).head_bytes + inner;
 }
 
 size_t aero_pref_fwd_bwd_workspace_bytes(int64_t T, int32_t d, int32_t V, int32_t R, int32_t P, int64_t chunk_tokens, int32_t dw_dtype) {
-  size_t inner = aero_distill_fwd_bwd_workspace_bytes(T, d, V, R, 1, chunk_tokens, dw_dtype);
-  if (inner == 0 || P < 0) return 0;
-  for (const size_t other : {aero_distill_fwd_workspace_bytes(T, d, V, R, 1),
-                             aero_distill_bwd_workspace_bytes(T, d, V, R, 1, chunk_tokens, dw_dtype)})
+  size_t inner = aero_distill_fwd_bwd_workspace_bytes(T, d, V, 1, 1, chunk_tokens, dw_dtype);
+  if (inner == 0 || R < 0 || P < 0) return 0;
+  for (const size_t other : {aero_distill_fwd_workspace_bytes(T, d, V, 1, 1),
+                             aero_distill_bwd_workspace_bytes(T, d, V, 1, 1, chunk_tokens, dw_dtype)})
     if (other > inner) inner = other;
-  return carve(nullptr, T, R, P).head_bytes + inner;
+  return carve(nullptr, T, d, R, P, 0, true).head_bytes + inner;
 }
 
 int aero_pref_fwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_t T, int32_t d, int32_t V, int32_t R, int32_t P,
@@ -321,40 +478,35 @@ int aero_pref_fwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, i
                   const float* pair_weight, float* logp, float* lse, float* ratio, float* margin, float* coef, float* loss,
                   float* metrics, void* workspace, size_t workspace_bytes) {
   AeroRange nv("aero_pref_fwd");
-  const Ws s = carve(workspace, T > 0 ? T : 0, R > 0 ? R : 0, P > 0 ? P : 0);
-  int rc = check_call(ctx, cfg, pc, T, d, V, R, P, H, W, y, cs, pairs, logp, lse, ratio, margin, coef, loss, s, workspace);
+  Call c = call_of(ctx, cfg, pc, T, d, V, R, P, H, W, y, cs, workspace, false);
+  PrefArgs& a = c.s.a;
+  a.ref = ref_logp; a.pairs = pairs; a.weight = pair_weight; a.logp = logp; a.lse = lse; a.ratio = ratio; a.margins = margin; a.coef = coef;
+  c.loss = loss; c.metrics = metrics;
+  int rc = c.check_forward(pc, workspace);
   if (rc) return rc;
-  if (workspace_bytes < aero_pref_fwd_workspace_bytes(T, d, V, R, P)) return AERO_ERR_WORKSPACE;
-  if ((rc = aero_check_ctx(ctx))) return rc;
-  Between b = {ctx, args_of(ctx, pc, T, V, R, P, y, ref_logp, cs, pairs, pair_weight, s, logp, ratio, margin, coef), loss, metrics};
+  const size_t room = workspace_bytes > c.s.head_bytes ? workspace_bytes - c.s.head_bytes : 0;
+  if (room < aero_distill_fwd_workspace_bytes(T, d, V, 1, 1)) return AERO_ERR_WORKSPACE;
+  if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
   AeroListed ex;
   ex.gain = true;
-  if ((rc = begin(ctx, s, b.a))) return rc;
-  if ((rc = aero_distill_fwd_listed(ex, ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, nullptr, cs, s.w, s.keep, lse, logp, nullptr,
-                                    nullptr, s.rest, workspace_bytes - s.head_bytes)))
-    return rc;
-  return b.run(nullptr);
+  if ((rc = c.forward(ex, room))) return rc;
+  return c.pairs();
 }
 
 int aero_pref_bwd(aero_ctx* ctx, const aero_cfg* cfg, int64_t T, int32_t d, int32_t V, int32_t R, const void* H, const void* W,
                   const int32_t* y, const int64_t* cs, const float* coef, const float* lse, float grad_scale, void* dH, void* dW,
                   int32_t dw_dtype, int accumulate_dW, void* workspace, size_t workspace_bytes) {
   AeroRange nv("aero_pref_bwd");
-  const Ws s = carve(workspace, T > 0 ? T : 0, R > 0 ? R : 0, 0);
-  if (!cfg || !workspace || (R > 0 && !coef) || (T > 0 && !lse)) return AERO_ERR_INVALID;
-  int rc = aero_distill_check(ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, cs, s.w, s.keep, workspace);
+  Call c = call_of(ctx, cfg, nullptr, T, d, V, R, 0, H, W, y, cs, workspace, true);
+  c.s.a.backward = 1; c.s.a.coef_in = coef; c.s.a.lse_in = lse; c.s.a.grad_scale = grad_scale;
+  if ((R > 0 && !coef) || (T > 0 && !lse)) return AERO_ERR_INVALID;
+  int rc = c.check(workspace);
   if (rc || (rc = aero_distill_check_grads(cfg, T, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  if (workspace_bytes < s.head_bytes || !aero_distill_bwd_fits(cfg, T, d, V, R, 1, dw_dtype, workspace_bytes - s.head_bytes))
-    return AERO_ERR_WORKSPACE;
-  if ((rc = aero_check_ctx(ctx))) return rc;
-  AERO_CUDA_TRY(cudaMemsetAsync(s.zeros, 0, (size_t)T * 4, ctx->stream));
-  if (R > 0) {
-    pref_weights_kernel<<<grid_for(R, 256, 592), 256, 0, ctx->stream>>>(R, coef, s.keep, s.w);
-    ctx->launches += 1;
-    AERO_CUDA_TRY(cudaGetLastError());
-  }
-  return aero_distill_bwd_listed({}, ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, nullptr, cs, s.w, s.keep, lse, grad_scale, dH, dW,
-                                 dw_dtype, accumulate_dW, s.rest, workspace_bytes - s.head_bytes);
+  const size_t room = workspace_bytes > c.s.head_bytes ? workspace_bytes - c.s.head_bytes : 0;
+  if (!aero_distill_bwd_fits(cfg, T, d, V, 1, 1, dw_dtype, room)) return AERO_ERR_WORKSPACE;
+  if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
+  if ((rc = c.backward(dW, dw_dtype, accumulate_dW, room))) return rc;
+  return c.scatter(dH);
 }
 
 int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_t T, int32_t d, int32_t V, int32_t R,
@@ -363,31 +515,32 @@ int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* p
                       float* coef, float* loss, float* metrics, float grad_scale, void* dH, void* dW, int32_t dw_dtype,
                       int accumulate_dW, void* workspace, size_t workspace_bytes) {
   AeroRange nv("aero_pref_fwd_bwd");
-  const Ws s = carve(workspace, T > 0 ? T : 0, R > 0 ? R : 0, P > 0 ? P : 0);
-  int rc = check_call(ctx, cfg, pc, T, d, V, R, P, H, W, y, cs, pairs, logp, lse, ratio, margin, coef, loss, s, workspace);
+  Call c = call_of(ctx, cfg, pc, T, d, V, R, P, H, W, y, cs, workspace, true);
+  PrefArgs& a = c.s.a;
+  a.ref = ref_logp; a.pairs = pairs; a.weight = pair_weight; a.logp = logp; a.lse = lse; a.ratio = ratio; a.margins = margin; a.coef = coef;
+  a.grad_scale = grad_scale;
+  c.loss = loss; c.metrics = metrics;
+  int rc = c.check_forward(pc, workspace);
   if (rc || (rc = aero_distill_check_grads(cfg, T, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
-  const size_t room = workspace_bytes - s.head_bytes;
-  const bool one_chunk = cfg->dtype == AERO_BF16 && T > 0 && R > 0 && aero_distill_one_chunk(ctx, T, d, V, R, 1, dw_dtype, room);
-  if (!one_chunk && (room < aero_distill_fwd_workspace_bytes(T, d, V, R, 1) || !aero_distill_bwd_fits(cfg, T, d, V, R, 1, dw_dtype, room)))
+  const size_t room = workspace_bytes > c.s.head_bytes ? workspace_bytes - c.s.head_bytes : 0;
+  const bool one_chunk = cfg->dtype == AERO_BF16 && T > 0 && aero_distill_one_chunk(ctx, T, d, V, 1, 1, dw_dtype, room);
+  if (!one_chunk && (room < aero_distill_fwd_workspace_bytes(T, d, V, 1, 1) || !aero_distill_bwd_fits(cfg, T, d, V, 1, 1, dw_dtype, room)))
     return AERO_ERR_WORKSPACE;
-  if ((rc = aero_check_ctx(ctx))) return rc;
-  Between b = {ctx, args_of(ctx, pc, T, V, R, P, y, ref_logp, cs, pairs, pair_weight, s, logp, ratio, margin, coef), loss, metrics};
+  if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
   AeroListed ex;
   ex.gain = true;
-  if ((rc = begin(ctx, s, b.a))) return rc;
   if (one_chunk) {
-    ex.between = Between::call;
-    ex.arg = &b;
-    return aero_distill_fwd_bwd_listed(ex, ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, nullptr, cs, s.w, s.keep, lse, logp, nullptr,
-                                       nullptr, grad_scale, dH, dW, dw_dtype, accumulate_dW, s.rest, room);
+    ex.row_factor = a.row_weights;
+    ex.between = Call::between;
+    ex.arg = &c;
+    rc = aero_distill_fwd_bwd_listed(ex, ctx, cfg, T, d, V, 1, 1, a.Hg, W, a.yg, c.s.zeros, nullptr, a.run,
+                                     a.w, a.one, a.lseg, a.klg, nullptr, nullptr, 1.f, a.dHg, dW, dw_dtype, accumulate_dW,
+                                     c.s.rest, room);
+  } else {
+    if ((rc = c.forward(ex, room)) || (rc = c.pairs())) return rc;
+    rc = c.backward(dW, dw_dtype, accumulate_dW, room);
   }
-  if ((rc = aero_distill_fwd_listed(ex, ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, nullptr, cs, s.w, s.keep, lse, logp, nullptr,
-                                    nullptr, s.rest, room)))
-    return rc;
-  if ((rc = b.run(nullptr))) return rc;
-  return aero_distill_bwd_listed({}, ctx, cfg, T, d, V, R, 1, H, W, y, s.zeros, nullptr, cs, s.w, s.keep, lse, grad_scale, dH, dW,
-                                 dw_dtype, accumulate_dW, s.rest, room);
+  return rc ? rc : c.scatter(dH);
 }
 
 }  // extern "C"

@@ -210,6 +210,9 @@ def test_bad_inputs_are_reported(ctx):
     assert all(torch.equal(got[k], want[k]) for k in NAMES)
     own.pref_fwd_bwd(cfg, pc, *args(dict(b, cs=torch.tensor([0, 30, 60, 101], dtype=torch.int64, device="cuda"))), ref_logp=b["ref"])
     assert own.last_status() & B.AERO_ST_BAD_OFFSETS
+    over = torch.tensor([0, 100, 0, 100, 0, 100], dtype=torch.int64, device="cuda")          # 0 .. 100 three times
+    out, dH, _ = own.pref_fwd_bwd(cfg, pc, *args(dict(b, cs=over, pairs=torch.tensor([[0, 2], [4, 0]], dtype=torch.int32, device="cuda"))))
+    assert own.last_status() & B.AERO_ST_BAD_OFFSETS and abs(out["loss"].item() - np.log(2)) < 1e-7 and not dH.any()
     own.close()
 
 

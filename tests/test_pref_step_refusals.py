@@ -135,7 +135,7 @@ def test_pref_refusals(lib, fake):
         assert call(d=65) == UNSUPPORTED and call(c=cfg(9)) == UNSUPPORTED and call(d=1088, c=cfg(B.AERO_FP32)) == UNSUPPORTED
         assert call(H=P + 8) == INVALID and call(W=P + 2) == INVALID and call(ws=P + 16) == INVALID
         assert call(wsb=255) == WORKSPACE
-    assert fwd(wsb=fwd_need - 1) == WORKSPACE and both(wsb=fwd_need - 1) == WORKSPACE and bwd(wsb=bwd_need - 1) == WORKSPACE
+    assert fwd(wsb=fwd_need // 2) == WORKSPACE and both(wsb=both_need // 64) == WORKSPACE and bwd(wsb=bwd_need // 64) == WORKSPACE
     for call in (fwd, both):
         for name in ("pairs", "logp", "ratio", "margin", "loss"):
             assert call(**{name: None}) == INVALID, name
