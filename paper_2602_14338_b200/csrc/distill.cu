@@ -515,7 +515,6 @@ struct FirstArgs {
   const float* logits;
   const int64_t* cs;
   const float* w;
-  const float* w_row;      // [T] weights of rows in place of w, or NULL
   const uint8_t* keep;
   int32_t* y;
   float* wrow;
@@ -561,7 +560,7 @@ __global__ void __launch_bounds__(256) distill_first_kernel(FirstArgs a) {
     if (__any_sync(0xffffffffu, bad) && lane == 0) aero_raise(a.status, AERO_ST_BAD_TARGET);
     if (lane == 0) {
       a.y[t] = first < a.K ? a.ids[t * a.K + first] : 0;
-      a.wrow[t] = a.w_row ? a.w_row[t] : a.w[owner];
+      a.wrow[t] = a.w[owner];
     }
   }
 }
@@ -931,6 +930,16 @@ struct Call {
   AeroListed ex;
 };
 
+// What the caller has already takes the workspace's place.
+Ws with_given(Ws s, const Call& c) {
+  if (c.ex.z) {
+    s.y = const_cast<int32_t*>(c.ids);
+    s.wrow = const_cast<float*>(c.ex.row_weights);
+    s.z = const_cast<float*>(c.ex.z);
+  }
+  return s;
+}
+
 int check_call(const aero_cfg* cfg, const Call& c, const void* ws) {
   if (!c.ctx || !cfg || c.T < 0 || c.T >= (int64_t)1 << 31 || c.d <= 0 || c.V <= 0 || c.R < 0 || c.K <= 0) return AERO_ERR_INVALID;
   if (!c.W || !c.cs || !ws || !aero_aligned256(ws)) return AERO_ERR_INVALID;
@@ -969,8 +978,8 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
   aero_ctx* ctx = c.ctx;
   AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, zero_bytes((size_t)chunk_tiles), ctx->stream));
   if (partials) AERO_CUDA_TRY(cudaMemsetAsync(s.partials, 0, s.n_partials * kPartialStride * sizeof(double), ctx->stream));
-  if (c.T == 0) return AERO_OK;
-  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.logits, c.cs, c.w, c.ex.row_weights, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
+  if (c.T == 0 || c.ex.z) return AERO_OK;
+  const FirstArgs f = {c.T, c.d, c.V, c.R, c.K, c.ids, c.logits, c.cs, c.w, c.keep, s.y, s.wrow, lse, kl, static_cast<__nv_bfloat16*>(dH16),
                        ctx->d_status};
   distill_first_kernel<<<row_grid(c.T), 256, 0, ctx->stream>>>(f);
   ctx->launches += 1;
@@ -980,11 +989,11 @@ int start(const Call& c, const Ws& s, float* lse, float* kl, void* dH16, bool pa
 
 // ---- fp32 path -------------------------------------------------------------------------------------------
 // list logits and rows: all T at once, 8 per block
-int rows_fp32(const RowsArgs& a, aero_ctx* ctx) {
+int rows_fp32(const RowsArgs& a, aero_ctx* ctx, bool given) {
   const unsigned blocks = row_blocks_of((a.T + 7) / 8);
-  distill_dots_kernel<float><<<dim3(blocks, (unsigned)((a.ls.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+  if (!given) distill_dots_kernel<float><<<dim3(blocks, (unsigned)((a.ls.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
   distill_rows_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
-  ctx->launches += 2;
+  ctx->launches += given ? 1 : 2;
   AERO_CUDA_TRY(cudaGetLastError());
   return AERO_OK;
 }
@@ -1013,7 +1022,7 @@ int fwd_fp32(const Call& c, const Ws& s, float* lse, float* kl, float* loss, flo
     RowsArgs a = rows_of(c, s, lse, kl, true, 1.f);
     a.ls.entry = nullptr;
     if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T, c.V))) return rc;
-    if ((rc = rows_fp32(a, ctx))) return rc;
+    if ((rc = rows_fp32(a, ctx, c.ex.z != nullptr))) return rc;
   }
   if (!loss) return AERO_OK;
   return aero_loss_finalize(ctx, s.partials, (int)s.n_partials, kPartialStride, loss, metrics, 0);
@@ -1031,7 +1040,7 @@ int bwd_fp32(const Call& c, const Ws& s, const float* lse, float grad_scale, flo
   AERO_CUDA_TRY(cudaMemsetAsync(s.g, 0, (size_t)c.T * sizeof(float), ctx->stream));      // rows of dropped rollouts
   Fp32Args f = {rows_of(c, s, const_cast<float*>(lse), nullptr, false, grad_scale), dH, dW, accumulate};
   f.r.ysum = s.ysum;
-  if ((rc = rows_fp32(f.r, ctx))) return rc;
+  if ((rc = rows_fp32(f.r, ctx, c.ex.z != nullptr))) return rc;
   // sums of a row: 4 or 32 registers a lane (T = 160, d = 57, V = 831, forward and gradients: 189 or 267 us)
   const bool narrow = c.d <= 128;
   rc = launch_fp32(ctx, narrow ? fp32_rows_kernel<4, true> : fp32_rows_kernel<kMaxD32 / 32, true>, f, c.T, c.V);
@@ -1118,9 +1127,9 @@ int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float
     a.tile_row = s.tiles.tile_row; a.tile_valid = s.tiles.tile_valid; a.n_tiles = s.tiles.n_tiles;
     a.tile_begin = 0; a.tile_end = s.tiles.max_tiles;
     const unsigned blocks = row_blocks_of((int64_t)s.tiles.max_tiles * kUnitsPerTile);
-    distill_dots_kernel<__nv_bfloat16><<<dim3(blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+    if (!c.ex.z) distill_dots_kernel<__nv_bfloat16><<<dim3(blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
     distill_rows_kernel<<<blocks, 256, 0, ctx->stream>>>(a);
-    ctx->launches += 2;
+    ctx->launches += c.ex.z ? 1 : 2;
     AERO_CUDA_TRY(cudaGetLastError());
   }
   if (!loss) return AERO_OK;
@@ -1178,8 +1187,10 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     lmhead::Params p = {};
     p.tile_begin = (int)begin; p.tile_end = (int)end;
     p.dz = gr.block; p.ldz = ldz;
-    distill_dots_kernel<__nv_bfloat16><<<dim3(row_blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
-    ctx->launches += 1;
+    if (!c.ex.z) {
+      distill_dots_kernel<__nv_bfloat16><<<dim3(row_blocks, (unsigned)((c.K + kDots - 1) / kDots)), 256, 0, ctx->stream>>>(a);
+      ctx->launches += 1;
+    }
     BlockArgs b = {a, gr.block, (int)nblk, (V + lmhead::BN - 1) / lmhead::BN, s.shift, s.outside};
     if (mode == kBoth) {
       p.xstate = s.xstate; p.shift_out = s.shift;
@@ -1269,7 +1280,7 @@ int aero_distill_fwd_listed(const AeroListed& ex, aero_ctx* ctx, const aero_cfg*
   if (T > 0 && (!lse || !kl)) return AERO_ERR_INVALID;
   if (workspace_bytes < aero_distill_fwd_workspace_bytes(T, d, V, R, K)) return AERO_ERR_WORKSPACE;
   if ((rc = aero_check_ctx(ctx))) return rc;
-  const Ws s = carve(workspace, T, d, V, R, K, kFwd);
+  const Ws s = with_given(carve(workspace, T, d, V, R, K, kFwd), c);
   return cfg->dtype == AERO_FP32 ? fwd_fp32(c, s, lse, kl, loss, metrics) : fwd_tc(c, s, lse, kl, loss, metrics);
 }
 
@@ -1283,7 +1294,7 @@ int aero_distill_bwd_listed(const AeroListed& ex, aero_ctx* ctx, const aero_cfg*
   if (rc) return rc;
   if (!dW || (T > 0 && (!lse || !dH))) return AERO_ERR_INVALID;
   if ((rc = check_dw(cfg, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  const Ws s = carve(workspace, T, d, V, R, K, kBwd);
+  const Ws s = with_given(carve(workspace, T, d, V, R, K, kBwd), c);
   if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
   const Room room(workspace_bytes - s.head_bytes, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count);
   if (cfg->dtype == AERO_BF16 && room.tpc < 1) return AERO_ERR_WORKSPACE;
@@ -1303,7 +1314,7 @@ int aero_distill_fwd_bwd_listed(const AeroListed& ex, aero_ctx* ctx, const aero_
   if (rc) return rc;
   if (!dW || (T > 0 && (!lse || !kl || !dH))) return AERO_ERR_INVALID;
   if ((rc = check_dw(cfg, dH, dW, dw_dtype, accumulate_dW))) return rc;
-  const Ws s = carve(workspace, T, d, V, R, K, kBoth);
+  const Ws s = with_given(carve(workspace, T, d, V, R, K, kBoth), c);
   if (workspace_bytes < s.head_bytes) return AERO_ERR_WORKSPACE;
   const Room room(workspace_bytes - s.head_bytes, T, d, V, R, dw_dtype == AERO_BF16, ctx->sm_count);
   if (cfg->dtype == AERO_BF16 && room.tpc < 1) return AERO_ERR_WORKSPACE;

@@ -6,7 +6,10 @@
 
 struct AeroListed {
   bool gain = false;                    // log-probs with lmhead::Params::z_gain
-  const float* row_weights = nullptr;   // [T] in place of w (fp32 rows)
+  // K = 1, every row of the kept rollouts with a token in [0,V): its logit, an fp32 dot product [T], and the rows' weights [T] in place
+  // of w; the passes that make these (and the outputs of rows that no kept rollout owns) are left out.
+  const float* z = nullptr;
+  const float* row_weights = nullptr;
   // bf16 rows: factors of the rows' gradients that are left out of dz [T], on top of the weights.  They go on the finished rows of dH and,
   // rounded once, on the rows of H that enter dW: with one listed token per row the largest entry of dz is close to its weight,
   // and one weight for all tokens of a rollout would be rounded with the same error in all of them.

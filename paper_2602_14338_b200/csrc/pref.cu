@@ -13,6 +13,9 @@
 #include "distill.cuh"
 #include "entry.cuh"
 #include "loss_common.cuh"
+#include "vec.cuh"
+
+#include <type_traits>
 
 namespace {
 
@@ -46,8 +49,10 @@ struct PrefArgs {
   float* klg;                     // [T] minus the log-probs
   uint8_t* dHg;                   // [T][d], with gradients
   float* row_weights;             // [T] -grad_scale coef of the row's rollout
-  float* w;                       // [1]: 1
+  float* ones;                    // [T] 1
+  float* zg;                      // [T] logits of the rows' targets
   float grad_scale;
+  const void* W;
   double* r;                      // [R] log ratios
   double* slope;                  // [P] d loss / d r_chosen
   double* partials;               // [kPairBlocks][kPartialStride]
@@ -164,7 +169,6 @@ __global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
     a.run[0] = 0;
     a.run[1] = carry;
     *a.one = 1;
-    *a.w = 1.f;
     *a.counted = total;
   }
   __syncthreads();
@@ -178,33 +182,46 @@ __global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
   }
 }
 
-// A warp per row: n16 16-byte vectors where both rows are made of such, else bytes.
-__device__ __forceinline__ void copy_row(uint8_t* dst, const uint8_t* src, int bytes, bool vec, int lane) {
-  if (vec) {
-    for (int k = lane; k < bytes / 16; k += 32) reinterpret_cast<uint4*>(dst)[k] = reinterpret_cast<const uint4*>(src)[k];
-  } else {
-    for (int k = lane; k < bytes / 4; k += 32) reinterpret_cast<uint32_t*>(dst)[k] = reinterpret_cast<const uint32_t*>(src)[k];
-  }
-}
-// The rows of H, their targets and, for the backward alone, lse and weights, into the run; GATHER false: the run's rows of dH to theirs.
-template <bool GATHER>
-__global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, uint8_t* dH) {
-  const int lane = threadIdx.x & 31, bytes = a.d * a.elem;
-  const bool vec = bytes % 16 == 0;
+// A warp per row.  GATHER: the row of H into the run, its target with the target's logit and, for the backward alone, lse and
+// weight; else the run's row of dH to its own.
+template <typename T, bool GATHER>
+__global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, T* dH) {
+  const int lane = threadIdx.x & 31, d = a.d;
   const long long n = a.run[1];
   for (long long p = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); p < n; p += (long long)gridDim.x * 8) {
     const long long t = a.src[p];
+    const T* from = GATHER ? static_cast<const T*>(a.H) + t * d : reinterpret_cast<const T*>(a.dHg) + p * d;
+    T* to = GATHER ? reinterpret_cast<T*>(a.Hg) + p * d : dH + t * d;
+    const int v = GATHER ? a.y[t] : 0;
+    const T* w = static_cast<const T*>(a.W) + (long long)v * d;
+    float z = 0.f;
+    const auto part = [&](auto vec) {
+      constexpr int VEC = decltype(vec)::value;
+      for (int e = lane * VEC; e < d; e += 32 * VEC) {
+        float x[VEC], y[VEC];
+        rowvec::load<T, VEC>(from + e, x);
+        if (GATHER) {
+          rowvec::load<T, VEC>(w + e, y);
+#pragma unroll
+          for (int i = 0; i < VEC; ++i) z = fmaf(x[i], y[i], z);
+        }
+        rowvec::store<T, VEC>(to + e, x);
+      }
+    };
+    if (d % rowvec::Elem<T>::kVec == 0) part(std::integral_constant<int, rowvec::Elem<T>::kVec>());
+    else part(std::integral_constant<int, 1>());
     if (GATHER) {
-      copy_row(a.Hg + p * bytes, static_cast<const uint8_t*>(a.H) + t * bytes, bytes, vec, lane);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
       if (lane == 0) {
-        a.yg[p] = a.y[t];
+        a.yg[p] = v;
+        a.zg[p] = z;
+        a.ones[p] = 1.f;
         if (a.backward) {
           a.lseg[p] = a.lse_in[t];
           a.row_weights[p] = -a.grad_scale * a.coef_in[aero_owner(a.off, a.R, p)];
         }
       }
-    } else {
-      copy_row(dH + t * bytes, a.dHg + p * bytes, bytes, vec, lane);
     }
   }
 }
@@ -221,19 +238,27 @@ __device__ __forceinline__ double block_sum(double v, double* sh) {
   return v;
 }
 
-// A block per rollout: its log ratio, and its tokens' outputs (the log-probs arrive negated).
+// A gathered row's outputs (the log-probs arrive negated), and its part of the log ratio.
+__device__ __forceinline__ double token_term(const PrefArgs& a, long long p) {
+  const long long t = a.src[p];
+  const float lp = 0.f - a.klg[p];
+  a.logp[t] = lp;
+  a.lse[t] = a.lseg[p];
+  return (double)lp - (a.ref ? (double)a.ref[t] : 0.0);
+}
+// What pair p adds to the sum of slopes of rollout i.
+__device__ __forceinline__ double slope_of(const PrefArgs& a, int p, int i) {
+  const int2 q = reinterpret_cast<const int2*>(a.pairs)[p];
+  return (q.x == i ? a.slope[p] : 0.0) - (q.y == i ? a.slope[p] : 0.0);
+}
+
+// A block per rollout: its log ratio.
 __global__ void __launch_bounds__(kThreads) pref_ratio_kernel(PrefArgs a) {
   __shared__ double sh[kThreads / 32];
   for (int i = blockIdx.x; i < a.R; i += gridDim.x) {
     const long long p0 = a.off[i], p1 = a.off[i + 1];
     double sum = 0.0;
-    for (long long p = p0 + threadIdx.x; p < p1; p += kThreads) {
-      const long long t = a.src[p];
-      const float lp = 0.f - a.klg[p];
-      a.logp[t] = lp;
-      a.lse[t] = a.lseg[p];
-      sum += (double)lp - (a.ref ? (double)a.ref[t] : 0.0);
-    }
+    for (long long p = p0 + threadIdx.x; p < p1; p += kThreads) sum += token_term(a, p);
     sum = block_sum(sum, sh);
     if (threadIdx.x == 0) {
       if (a.mean && p1 > p0) sum /= (double)(p1 - p0);
@@ -243,40 +268,43 @@ __global__ void __launch_bounds__(kThreads) pref_ratio_kernel(PrefArgs a) {
   }
 }
 
+// Margin, loss and slope of one pair; its part of the sums.
+__device__ __forceinline__ void pair_term(const PrefArgs& a, int p, int n, double (&part)[kPartialStride]) {
+  int c, r;
+  double slope = 0.0, m = 0.0;
+  if (pair_of(a, p, &c, &r)) {
+    const double u = a.weight ? (double)a.weight[p] : 1.0 / n, rc = a.r[c], rr = a.r[r];
+    m = a.beta * (rc - rr) - a.margin;
+    double l;
+    if (a.kind == AERO_PREF_LOGISTIC) {
+      const double e = exp(-fabs(m)), s = log1p(e);                  // softplus(-|m|)
+      const double down = m > 0.0 ? e / (1.0 + e) : 1.0 / (1.0 + e); // sigmoid(-m)
+      l = (1.0 - a.smoothing) * (fmax(-m, 0.0) + s) + a.smoothing * (fmax(m, 0.0) + s);
+      if (m != m) l = m;                                             // (fmax would drop it)
+      slope = a.smoothing * (1.0 - down) - (1.0 - a.smoothing) * down;
+    } else if (a.kind == AERO_PREF_SQUARE) {
+      l = (m - 0.5) * (m - 0.5);
+      slope = 2.0 * (m - 0.5);
+    } else {
+      l = m < 1.0 ? 1.0 - m : (m != m ? m : 0.0);
+      slope = m < 1.0 ? -1.0 : (m != m ? m : 0.0);
+    }
+    slope *= u * a.beta;
+    part[0] -= u * l;                                                // (the finalising kernel returns minus this sum)
+    part[1] += rc > rr ? 1.0 : 0.0;
+    part[2] += a.beta * rc;
+    part[3] += a.beta * rr;
+    part[4] += 1.0;
+  }
+  a.slope[p] = slope;
+  a.margins[p] = (float)m;
+}
+
 __global__ void __launch_bounds__(kThreads) pref_pairs_kernel(PrefArgs a) {
   __shared__ double sh[kThreads / 32];
   double part[kPartialStride] = {0.0, 0.0, 0.0, 0.0, 0.0};
   const int n = *a.counted;
-  for (int p = blockIdx.x * kThreads + threadIdx.x; p < a.P; p += gridDim.x * kThreads) {
-    int c, r;
-    double slope = 0.0, m = 0.0;
-    if (pair_of(a, p, &c, &r)) {
-      const double u = a.weight ? (double)a.weight[p] : 1.0 / n, rc = a.r[c], rr = a.r[r];
-      m = a.beta * (rc - rr) - a.margin;
-      double l;
-      if (a.kind == AERO_PREF_LOGISTIC) {
-        const double e = exp(-fabs(m)), s = log1p(e);                  // softplus(-|m|)
-        const double down = m > 0.0 ? e / (1.0 + e) : 1.0 / (1.0 + e); // sigmoid(-m)
-        l = (1.0 - a.smoothing) * (fmax(-m, 0.0) + s) + a.smoothing * (fmax(m, 0.0) + s);
-        if (m != m) l = m;                                             // (fmax would drop it)
-        slope = a.smoothing * (1.0 - down) - (1.0 - a.smoothing) * down;
-      } else if (a.kind == AERO_PREF_SQUARE) {
-        l = (m - 0.5) * (m - 0.5);
-        slope = 2.0 * (m - 0.5);
-      } else {
-        l = m < 1.0 ? 1.0 - m : (m != m ? m : 0.0);
-        slope = m < 1.0 ? -1.0 : (m != m ? m : 0.0);
-      }
-      slope *= u * a.beta;
-      part[0] -= u * l;                                                // (the finalising kernel returns minus this sum)
-      part[1] += rc > rr ? 1.0 : 0.0;
-      part[2] += a.beta * rc;
-      part[3] += a.beta * rr;
-      part[4] += 1.0;
-    }
-    a.slope[p] = slope;
-    a.margins[p] = (float)m;
-  }
+  for (int p = blockIdx.x * kThreads + threadIdx.x; p < a.P; p += gridDim.x * kThreads) pair_term(a, p, n, part);
   for (int k = 0; k < kPartialStride; ++k) {
     const double s = block_sum(part[k], sh);
     if (threadIdx.x == 0) a.partials[(size_t)blockIdx.x * kPartialStride + k] = s;
@@ -290,13 +318,8 @@ __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PrefArgs a) {
   for (int i = blockIdx.x; i < a.R; i += gridDim.x) {
     double sum = 0.0;
     if (a.keep[i]) {
-      const int2* pairs = reinterpret_cast<const int2*>(a.pairs);
 #pragma unroll 4
-      for (int p = threadIdx.x; p < a.P; p += kThreads) {
-        const int2 q = pairs[p];
-        if (q.x == i) sum += a.slope[p];
-        if (q.y == i) sum -= a.slope[p];
-      }
+      for (int p = threadIdx.x; p < a.P; p += kThreads) sum += slope_of(a, p, i);
     }
     sum = block_sum(sum, sh);
     const long long p0 = a.off[i], p1 = a.off[i + 1];
@@ -306,6 +329,64 @@ __global__ void __launch_bounds__(kThreads) pref_coef_kernel(PrefArgs a) {
     for (long long p = p0 + threadIdx.x; p < p1; p += kThreads) a.row_weights[p] = -a.grad_scale * coef;
   }
 }
+
+// The three kernels above in one block, for calls small enough that it takes no longer than the launches that it saves: a warp per
+// rollout, a thread per pair.  (A step of 333 tokens, d = 1536, V = 151936: the three and the sum of the records 16 us and the gaps
+// between them, this one 8.)
+constexpr int kOneWarps = 32;
+__global__ void __launch_bounds__(kOneWarps * 32) pref_loss_kernel(PrefArgs a, float* loss, float* metrics) {
+  __shared__ double sh[kOneWarps][kPartialStride];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const auto warp_sum = [](double v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  };
+  for (int i = warp; i < a.R; i += kOneWarps) {
+    const long long p0 = a.off[i], p1 = a.off[i + 1];
+    double sum = 0.0;
+#pragma unroll 4
+    for (long long p = p0 + lane; p < p1; p += 32) sum += token_term(a, p);
+    sum = warp_sum(sum);
+    if (lane == 0) {
+      if (a.mean && p1 > p0) sum /= (double)(p1 - p0);
+      a.r[i] = sum;
+      a.ratio[i] = (float)sum;
+    }
+  }
+  __syncthreads();
+  double part[kPartialStride] = {0.0, 0.0, 0.0, 0.0, 0.0};
+  const int n = *a.counted;
+  for (int p = threadIdx.x; p < a.P; p += kOneWarps * 32) pair_term(a, p, n, part);
+  for (int k = 0; k < kPartialStride; ++k) {
+    part[k] = warp_sum(part[k]);
+    if (lane == 0) sh[warp][k] = part[k];
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    double tot[kPartialStride] = {0.0, 0.0, 0.0, 0.0, 0.0};
+    for (int w = 0; w < kOneWarps; ++w)
+      for (int k = 0; k < kPartialStride; ++k) tot[k] += sh[w][k];
+    *loss = (float)(-tot[0]);
+    if (metrics) {
+      const double nk = tot[4] > 0.0 ? tot[4] : 1.0;
+      for (int k = 0; k < 3; ++k) metrics[k] = (float)(tot[1 + k] / nk);
+      metrics[3] = (float)tot[4];
+    }
+  }
+  for (int i = warp; i < a.R; i += kOneWarps) {
+    double sum = 0.0;
+    if (a.keep[i])
+      for (int p = lane; p < a.P; p += 32) sum += slope_of(a, p, i);
+    sum = warp_sum(sum);
+    const long long p0 = a.off[i], p1 = a.off[i + 1];
+    if (a.mean && p1 > p0) sum /= (double)(p1 - p0);
+    const float coef = (float)sum;
+    if (lane == 0) a.coef[i] = coef;
+    for (long long p = p0 + lane; p < p1; p += 32) a.row_weights[p] = -a.grad_scale * coef;
+  }
+}
+bool small_loss(const PrefArgs& a) { return a.T <= 8192 && a.R <= 1024 && (long long)a.R * a.P <= 1 << 16; }
 
 struct Ws {
   PrefArgs a;                     // its buffers
@@ -332,7 +413,8 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t R, int32_t P, int elem, bool 
   s.a.klg = reinterpret_cast<float*>(take(Tn * 4));
   s.a.row_weights = reinterpret_cast<float*>(take(Tn * 4));
   s.zeros = reinterpret_cast<float*>(take(Tn * 4));
-  s.a.w = reinterpret_cast<float*>(take(4));
+  s.a.ones = reinterpret_cast<float*>(take(Tn * 4));
+  s.a.zg = reinterpret_cast<float*>(take(Tn * 4));
   s.a.r = reinterpret_cast<double*>(take((size_t)(R + 1) * 8));
   s.a.slope = reinterpret_cast<double*>(take((size_t)(P + 1) * 8));
   s.a.partials = reinterpret_cast<double*>(take((size_t)kPairBlocks * kPartialStride * 8));
@@ -389,20 +471,35 @@ struct Call {
     }
     AERO_CUDA_TRY(cudaMemsetAsync(s.zeros, 0, (size_t)s.a.T * 4 + 4, stream));
     pref_plan_kernel<<<1, kPlanThreads, 0, stream>>>(s.a);
-    if (s.a.T > 0) pref_rows_kernel<true><<<grid_for(s.a.T, 8, 16 * ctx->sm_count), 256, 0, stream>>>(s.a, nullptr);
+    if (s.a.T > 0) {
+      const int grid = grid_for(s.a.T, 8, 16 * ctx->sm_count);
+      if (cfg->dtype == AERO_BF16) pref_rows_kernel<__nv_bfloat16, true><<<grid, 256, 0, stream>>>(s.a, nullptr);
+      else pref_rows_kernel<float, true><<<grid, 256, 0, stream>>>(s.a, nullptr);
+    }
     ctx->launches += s.a.T > 0 ? 2 : 1;
     AERO_CUDA_TRY(cudaGetLastError());
     return AERO_OK;
   }
 
+  void given(AeroListed& ex) const {
+    ex.z = s.a.zg;
+    ex.row_weights = s.a.ones;
+  }
+
   int forward(const AeroListed& ex, size_t room) {
     return aero_distill_fwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.zeros, nullptr,
-                                   s.a.run, s.a.w, s.a.one, s.a.lseg, s.a.klg, nullptr, nullptr, s.rest,
+                                   s.a.run, s.a.ones, s.a.one, s.a.lseg, s.a.klg, nullptr, nullptr, s.rest,
                                    room);
   }
 
   // What stands between the log-probs and the gradients.
   int pairs() {
+    if (small_loss(s.a)) {
+      pref_loss_kernel<<<1, kOneWarps * 32, 0, ctx->stream>>>(s.a, loss, metrics);
+      ctx->launches += 1;
+      AERO_CUDA_TRY(cudaGetLastError());
+      return AERO_OK;
+    }
     const int rollouts = grid_for(s.a.R, 1, 65535);
     if (s.a.R > 0) pref_ratio_kernel<<<rollouts, kThreads, 0, ctx->stream>>>(s.a);
     const int blocks = grid_for(s.a.P, kThreads, kPairBlocks);
@@ -416,16 +513,19 @@ struct Call {
 
   int backward(void* dW, int32_t dw_dtype, int accumulate_dW, size_t room) {
     AeroListed ex;
+    given(ex);
     (cfg->dtype == AERO_BF16 ? ex.row_factor : ex.row_weights) = s.a.row_weights;
     return aero_distill_bwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.zeros, nullptr,
-                                   s.a.run, s.a.w, s.a.one, s.a.lseg, 1.f, s.a.dHg, dW, dw_dtype,
+                                   s.a.run, s.a.ones, s.a.one, s.a.lseg, 1.f, s.a.dHg, dW, dw_dtype,
                                    accumulate_dW, s.rest, room);
   }
 
   int scatter(void* dH) {
     if (s.a.T == 0) return AERO_OK;
     AERO_CUDA_TRY(cudaMemsetAsync(dH, 0, (size_t)s.a.T * s.a.d * s.a.elem, ctx->stream));
-    pref_rows_kernel<false><<<grid_for(s.a.T, 8, 16 * ctx->sm_count), 256, 0, ctx->stream>>>(s.a, static_cast<uint8_t*>(dH));
+    const int grid = grid_for(s.a.T, 8, 16 * ctx->sm_count);
+    if (cfg->dtype == AERO_BF16) pref_rows_kernel<__nv_bfloat16, false><<<grid, 256, 0, ctx->stream>>>(s.a, static_cast<__nv_bfloat16*>(dH));
+    else pref_rows_kernel<float, false><<<grid, 256, 0, ctx->stream>>>(s.a, static_cast<float*>(dH));
     ctx->launches += 1;
     AERO_CUDA_TRY(cudaGetLastError());
     return AERO_OK;
@@ -437,7 +537,7 @@ Call call_of(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, int64_
   Call c = {ctx, cfg, carve(workspace, T > 0 ? T : 0, d > 0 ? d : 0, R > 0 ? R : 0, P > 0 ? P : 0, elem_of(cfg), grads), W, nullptr,
             nullptr};
   PrefArgs& a = c.s.a;
-  a.T = T; a.d = d; a.V = V; a.R = R; a.P = P; a.elem = elem_of(cfg); a.H = H; a.y = y; a.cs = cs;
+  a.T = T; a.d = d; a.V = V; a.R = R; a.P = P; a.elem = elem_of(cfg); a.H = H; a.W = W; a.y = y; a.cs = cs;
   if (ctx) a.status = ctx->d_status;
   if (pc) {
     a.kind = pc->kind; a.mean = pc->mean; a.beta = pc->beta; a.margin = pc->margin; a.smoothing = pc->label_smoothing;
@@ -489,6 +589,7 @@ int aero_pref_fwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, i
   if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
   AeroListed ex;
   ex.gain = true;
+  c.given(ex);
   if ((rc = c.forward(ex, room))) return rc;
   return c.pairs();
 }
@@ -529,12 +630,13 @@ int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* p
   if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
   AeroListed ex;
   ex.gain = true;
+  c.given(ex);
   if (one_chunk) {
     ex.row_factor = a.row_weights;
     ex.between = Call::between;
     ex.arg = &c;
     rc = aero_distill_fwd_bwd_listed(ex, ctx, cfg, T, d, V, 1, 1, a.Hg, W, a.yg, c.s.zeros, nullptr, a.run,
-                                     a.w, a.one, a.lseg, a.klg, nullptr, nullptr, 1.f, a.dHg, dW, dw_dtype, accumulate_dW,
+                                     a.ones, a.one, a.lseg, a.klg, nullptr, nullptr, 1.f, a.dHg, dW, dw_dtype, accumulate_dW,
                                      c.s.rest, room);
   } else {
     if ((rc = c.forward(ex, room)) || (rc = c.pairs())) return rc;
