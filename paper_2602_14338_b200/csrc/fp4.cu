@@ -9,7 +9,7 @@
 //   z_tv = h_row_t w_row_v sum_k (scaled h codes)(scaled w codes),   fp32 accumulators of tcgen05 kinds mxf4nvf4 / mxf4, which take the
 // block scales from TMEM.  W is operand A (128 or 256 vocabulary rows), the tokens are operand B, as in the 8-bit product.
 //   fp4_rows_kernel   up to 128 tokens: bound by reading W once; each CTA streams a contiguous range of vocabulary rows
-//   fp4_pair_kernel   more tokens: CTA pairs, 256 vocabulary rows x up to 192 tokens per unit
+//   fp4_pair_kernel   more tokens: CTA pairs, 256 vocabulary rows x up to 384 tokens per unit, in two accumulators of 192
 #include "entry.cuh"
 #include "tc_ptx.cuh"
 #include "tmap.cuh"
@@ -301,7 +301,7 @@ __global__ void __launch_bounds__(256) fp4_values_kernel(ValueArgs a) {
 // alike).  The asynchronous copy that brings 512 bytes to all quadrants, issued between the products, held these up by 60 cycles
 // each, 12 times for 4 products of 150 cycles (2048 tokens, d = 3584, V = 152064: 1008 us with it).
 constexpr int EPI_WARPS = 8, kShare = EPI_WARPS / 4, SCALE_WARPS = 4, THREADS = (EPI_WARPS + 2 + SCALE_WARPS) * 32;
-constexpr int kRowsN = 128, kPairN = 192;         // most tokens per tile
+constexpr int kRowsN = 128, kPairN = 192, kPairT = 2 * kPairN;         // most tokens per tile
 constexpr int kRowBlock = 32;                     // fp4_rows_kernel: ranges of vocabulary rows are multiples of it
 constexpr int kMaxStages = 8, kMaxSets = 8;
 constexpr uint32_t kScaleCols = 256;              // fp4_rows_kernel: first TMEM column of the scales
@@ -335,7 +335,8 @@ struct Operand {
 };
 struct Params {
   int T, V, slabs;
-  int n, n_tok;               // tokens per tile (N of the products), token tiles
+  int n;                      // fp4_rows_kernel: tokens in steps of 16 (N of the products)
+  int n_tok;                  // fp4_pair_kernel: token tiles
   Operand h, w;
   void* out;
   uint32_t* status;
@@ -346,7 +347,7 @@ struct Params {
 // 32 neighbouring logits of a token at a time; the two warps of a quadrant of TMEM take chunks of 32 tokens in turn.  The rows'
 // scales are loaded before the accumulator is waited for, a token's by a lane each.
 template <typename O, int N>
-struct Epilogue {
+struct Epilogue {                // of fp4_rows_kernel
   static constexpr int kChunks = (N / 32 + kShare - 1) / kShare;
   float sh[kChunks];
   float sw;
@@ -526,14 +527,44 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
   }
 }
 
-// A stage of the pair kernel, per CTA: codes of 128 rows of W and of half of the tokens, scales of these rows of W, and of the two
-// groups of 128 token rows that hold all of the tile's tokens (both CTAs' tensor cores multiply all N columns).
-constexpr int PSTAGES = 6, kPiece = 32;
-constexpr uint32_t kPairAccCols = 2 * kPairN;
+// 32 values of an output type in registers.
+template <typename O> struct Held;
+template <> struct Held<float> {
+  float v[32];
+  __device__ void take(const uint32_t (&r)[32]) {
+#pragma unroll
+    for (int q = 0; q < 32; ++q) v[q] = __uint_as_float(r[q]);
+  }
+  __device__ float at(int q) const { return v[q]; }
+};
+template <> struct Held<__nv_bfloat16> {
+  __nv_bfloat162 v[16];
+  __device__ void take(const uint32_t (&r)[32]) {
+#pragma unroll
+    for (int q = 0; q < 16; ++q) v[q] = __floats2bfloat162_rn(__uint_as_float(r[2 * q]), __uint_as_float(r[2 * q + 1]));
+  }
+  __device__ __nv_bfloat16 at(int q) const { return q & 1 ? v[q / 2].y : v[q / 2].x; }
+};
+
+// The pair kernel is bound by what the SMs read from L2: 10 TB/s.  The tokens of a unit are therefore as many as the accumulators
+// hold, 2 x 192 (with 512 columns of TMEM and 128 of them for scales), and both accumulators use the rows of W that were
+// loaded once.  (With units of 192 tokens and one accumulator filling while the other was read, 2048 tokens of d = 3584, V = 152064
+// took 701 us instead of 668.)  An accumulator is emptied into registers as soon as its products are done, rounded there, and stored
+// while the next unit's products run.
+// A stage, per CTA: codes of 128 rows of W and of its half of each accumulator's tokens, scales of these rows of W, and of the three
+// groups of 128 token rows (both CTAs' tensor cores multiply all columns).
+constexpr int PSTAGES = 4, kPiece = 32, kTokenGroups = kPairT / kTile;
+constexpr uint32_t kHalfBytes = kPairN / 2 * kRowBytes;
 __host__ __device__ constexpr uint32_t pair_stage(int block) {
-  return kTileBytes + kPairN / 2 * kRowBytes + 3 * groups_per_slab(block) * kGroupBytes;
+  return kTileBytes + 2 * kHalfBytes + (1 + kTokenGroups) * groups_per_slab(block) * kGroupBytes;
 }
 constexpr size_t p_smem(int block) { return 1024 + (size_t)PSTAGES * pair_stage(block) + sizeof(Ctl<PSTAGES>); }
+
+// Tokens of each accumulator in the unit that begins with token t0: half of what is left, in steps of 64.
+__host__ __device__ inline int pair_n(int T, int t0) {
+  const int n = ((T - t0 + 1) / 2 + 63) / 64 * 64;
+  return n < kPairN ? n : kPairN;
+}
 
 template <typename O, int BLOCK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
@@ -542,8 +573,12 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   constexpr int kGroups = groups_per_slab(BLOCK);
-  constexpr uint32_t kStage = pair_stage(BLOCK), kScales = kGroups * kGroupBytes, kSetCols = 12 * kGroups;
-  constexpr int kSets = 2;                            // of scale columns, behind the accumulators (5 in block 32: no faster)
+  constexpr uint32_t kStage = pair_stage(BLOCK), kScales = kGroups * kGroupBytes;
+  // columns of TMEM: two accumulators, then kSets sets of a slab's scales, W's and for each k step the tokens'.  (Four sets of half a
+  // slab: 969 us, a set's way through the scales' warps takes longer than the products of half a slab.)
+  constexpr int kSets = 2;
+  constexpr uint32_t kSetCols = 4 * kGroups * (1 + kTokenGroups), kScaleBase = 2 * kPairN;
+  static_assert(kScaleBase + kSets * kSetCols <= 512, "TMEM");
   auto* ctl = reinterpret_cast<Ctl<PSTAGES>*>(smem + (size_t)PSTAGES * kStage);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_ctarank();        // 0 issues the MMAs of the pair
@@ -576,10 +611,9 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     if (lane == 0) {
       uint32_t it = 0;
       bool ok = true;
-      const int pieces = p.n / 2 / kPiece;
-      const uint32_t bytes = 2 * (kTileBytes + (uint32_t)p.n / 2 * kRowBytes);
       for (long long u = pair; ok && u < units; u += npairs) {
-        const int tile = (int)(u / p.n_tok) * 2 + (int)rank, t0 = (int)(u % p.n_tok) * p.n, th = t0 + (int)rank * (p.n / 2);
+        const int tile = (int)(u / p.n_tok) * 2 + (int)rank, t0 = (int)(u % p.n_tok) * kPairT, n = pair_n(p.T, t0);
+        const uint32_t bytes = 2 * (kTileBytes + (uint32_t)n * kRowBytes);
         for (int kb = 0; kb < nkb; ++kb, ++it) {
           const int s = it % PSTAGES;
           if (!tc::mbar_wait(&ctl->empty[s], ((it / PSTAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
@@ -588,15 +622,17 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
           if (rank == 0) tc::mbar_arrive_expect_tx(&ctl->full[s], bytes);
           // (rows past the last tile of W or of the tokens are filled with zeros by the copies)
           tc::tma_load_2d_pair(at, &tmW, 0, (tile * nkb + kb) * kTile, full0);
-          at += kTileBytes;
-          for (int i = 0; i < pieces; ++i) {
-            const int t = th + i * kPiece;
-            tc::tma_load_2d_pair(at + i * kPiece * kRowBytes, &tmH, 0, (t / kTile * nkb + kb) * kTile + t % kTile, full0);
+          for (int acc = 0; acc < 2; ++acc) {
+            for (int i = 0; i < n / 2 / kPiece; ++i) {
+              const int t = t0 + acc * n + (int)rank * (n / 2) + i * kPiece;
+              tc::tma_load_2d_pair(at + kTileBytes + acc * kHalfBytes + i * kPiece * kRowBytes, &tmH, 0,
+                                   (t / kTile * nkb + kb) * kTile + t % kTile, full0);
+            }
           }
-          at += kPairN / 2 * kRowBytes;
-          tc::mbar_arrive_expect_tx(&ctl->sfull[s], 3 * kScales);
+          at += kTileBytes + 2 * kHalfBytes;
+          tc::mbar_arrive_expect_tx(&ctl->sfull[s], (1 + kTokenGroups) * kScales);
           tc::tma_load_2d(at, &tmWs, 0, (tile * nkb + kb) * kGroups, &ctl->sfull[s]);
-          for (int i = 0; i < 2; ++i)
+          for (int i = 0; i < kTokenGroups; ++i)
             tc::tma_load_2d(at + (1 + i) * kScales, &tmHs, 0, ((t0 / kTile + i) * nkb + kb) * kGroups, &ctl->sfull[s]);
         }
       }
@@ -606,29 +642,32 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       uint32_t it = 0, at = 0;
       bool ok = true;
       for (long long u = pair; ok && u < units; u += npairs, ++at) {
-        const uint32_t buf = at & 1u;
-        // the tile's tokens begin in the first group's row 0, 32, 64 or 96: scales of 32 rows are a column
-        const uint32_t shift = (uint32_t)((int)(u % p.n_tok) * p.n % kTile) / 32;
-        if (!tc::mbar_wait(&ctl->tempty[buf], ((at >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-        tc::tc_fence_after();
-        for (int kb = 0; kb < nkb; ++kb, ++it) {
+        const int n = pair_n(p.T, (int)(u % p.n_tok) * kPairT);
+        for (int kb = 0; ok && kb < nkb; ++kb, ++it) {
           const int s = it % PSTAGES;
           if (!tc::mbar_wait(&ctl->full[s], (it / PSTAGES) & 1u, abort_flag) ||
               !tc::mbar_wait(&ctl->scales[it % kSets], (it / kSets) & 1u, abort_flag)) { ok = false; break; }
-          tc::tc_fence_after();
-          const uint32_t a_addr = tc::smem_u32(smem + (size_t)s * kStage), b_addr = a_addr + kTileBytes;
-          const uint32_t sfa = tmem_base + kPairAccCols + (it % kSets) * kSetCols, sfb = sfa + 4 * kGroups + shift;
-          const uint64_t adesc = tc::make_smem_desc(a_addr, 16, 1024), bdesc = tc::make_smem_desc(b_addr, 16, 1024);
+          const uint32_t a_addr = tc::smem_u32(smem + (size_t)s * kStage);
+          const uint32_t sfa = tmem_base + kScaleBase + (it % kSets) * kSetCols;
+          for (int acc = 0; acc < 2; ++acc) {
+            // the accumulator of the unit before has been read
+            if (kb == 0 && !tc::mbar_wait(&ctl->tempty[acc], (at & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+            tc::tc_fence_after();
+            // (a column holds the scales of 32 rows)
+            const uint32_t sfb = sfa + 4 * kGroups + (uint32_t)(acc * n) / 32;
+            const uint64_t adesc = tc::make_smem_desc(a_addr, 16, 1024);
+            const uint64_t bdesc = tc::make_smem_desc(a_addr + kTileBytes + acc * kHalfBytes, 16, 1024);
 #pragma unroll
-          for (int kk = 0; kk < kSlab / 64; ++kk) {
-            const int g = kk * kGroups / 4;
-            const uint32_t idesc = tc::make_idesc_fp4(2 * kTile, p.n, BLOCK == 32, BLOCK == 32 ? 2 * (kk & 1) : 0);
-            tc::umma_fp4<BLOCK, true>(tmem_base + buf * kPairN, adesc + 2u * kk, bdesc + 2u * kk, idesc, sfa + 4 * g,
-                                      sfb + 8 * g, (kb | kk) != 0 ? 1u : 0u);
+            for (int kk = 0; kk < kSlab / 64; ++kk) {
+              const int g = kk * kGroups / 4;                     // block 32: a group holds two instructions' scales
+              const uint32_t idesc = tc::make_idesc_fp4(2 * kTile, n, BLOCK == 32, BLOCK == 32 ? 2 * (kk & 1) : 0);
+              tc::umma_fp4<BLOCK, true>(tmem_base + acc * kPairN, adesc + 2u * kk, bdesc + 2u * kk, idesc, sfa + 4 * g,
+                                        sfb + 4 * kTokenGroups * g, (kb | kk) != 0 ? 1u : 0u);
+            }
+            if (kb == nkb - 1) tc::umma_commit_pair(&ctl->tfull[acc], 3);
           }
-          tc::umma_commit_pair(&ctl->empty[s], 3);     // frees the stage in both CTAs when these MMAs retire
+          if (ok) tc::umma_commit_pair(&ctl->empty[s], 3);     // frees the stage in both CTAs when these MMAs retire
         }
-        if (ok) tc::umma_commit_pair(&ctl->tfull[buf], 3);
       }
     }
   } else if (warp >= EPI_WARPS + 2) {
@@ -638,26 +677,25 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     for (long long u = pair; ok && u < units; u += npairs) {
       for (int kb = 0; kb < nkb; ++kb, ++it) {
         const int s = it % PSTAGES;
+        if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->sfull[s], (it / PSTAGES) & 1u, abort_flag))) { ok = false; break; }
+        const uint8_t* from = smem + (size_t)s * kStage + kTileBytes + 2 * kHalfBytes + lane * 16;
+        // W's, then for each k step the tokens' three groups of rows side by side
+        uint32_t r[4 * kGroups * (1 + kTokenGroups)];
+#pragma unroll
+        for (int k = 0; k < kGroups * (1 + kTokenGroups); ++k) {
+          const int g = k < kGroups ? k : (k - kGroups) / kTokenGroups, i = k < kGroups ? 0 : 1 + (k - kGroups) % kTokenGroups;
+          const uint4 v = *reinterpret_cast<const uint4*>(from + i * kScales + g * kGroupBytes);
+          r[4 * k] = v.x; r[4 * k + 1] = v.y; r[4 * k + 2] = v.z; r[4 * k + 3] = v.w;
+        }
         // the set's columns are free when the products of kSets slabs ago have retired, which their stage's barrier tells
         const uint32_t old = it - kSets;
-        bool here = tc::mbar_wait(&ctl->sfull[s], (it / PSTAGES) & 1u, abort_flag);
-        if (here && it >= (uint32_t)kSets) here = tc::mbar_wait(&ctl->empty[old % PSTAGES], (old / PSTAGES) & 1u, abort_flag);
-        if (!__all_sync(0xffffffffu, here)) { ok = false; break; }
+        const bool free = it < (uint32_t)kSets || tc::mbar_wait(&ctl->empty[old % PSTAGES], (old / PSTAGES) & 1u, abort_flag);
+        if (!__all_sync(0xffffffffu, free)) { ok = false; break; }
         tc::tc_fence_after();
-        const uint8_t* from = smem + (size_t)s * kStage + kTileBytes + kPairN / 2 * kRowBytes;
-        const uint32_t to = tmem_base + ((uint32_t)(quad * 32) << 16) + kPairAccCols + (it % kSets) * kSetCols;
-        scales_to_tmem<kGroups>(to, from, lane);
-        // the tokens' two groups of rows side by side
-        uint32_t r[8 * kGroups];
+        const uint32_t to = tmem_base + ((uint32_t)(quad * 32) << 16) + kScaleBase + (it % kSets) * kSetCols;
+        constexpr int kPart = 8 * kGroups;                       // (32 columns a store at most)
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4 v = *reinterpret_cast<const uint4*>(from + (1 + i) * kScales + g * kGroupBytes + lane * 16);
-            r[8 * g + 4 * i] = v.x; r[8 * g + 4 * i + 1] = v.y; r[8 * g + 4 * i + 2] = v.z; r[8 * g + 4 * i + 3] = v.w;
-          }
-        }
-        tc::tmem_st_32x32<8 * kGroups>(to + 4 * kGroups, r);
+        for (int k = 0; k < 4 * kGroups * (1 + kTokenGroups); k += kPart) tc::tmem_st_32x32<kPart>(to + k, r + k);
         tc::tmem_st_wait();
         tc::tc_fence_before();
         __syncwarp();
@@ -666,20 +704,62 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
       }
     }
   } else {
+    // a thread has a vocabulary row, so the 32 lanes of a warp store 32 neighbouring logits of a token at a time; the two warps of a
+    // quadrant of TMEM take chunks of 32 tokens in turn
+    constexpr int kChunks = kPairN / 32 / kShare;
     uint32_t at = 0;
     const int quad = warp & 3, half = warp >> 2;
-    Epilogue<O, kPairN> epi;
     for (long long u = pair; u < units; u += npairs, ++at) {
-      const int t0 = (int)(u % p.n_tok) * p.n;
-      const uint32_t buf = at & 1u;
+      const int t0 = (int)(u % p.n_tok) * kPairT, n = pair_n(p.T, t0);
       const int v = (int)(u / p.n_tok) * 2 * kTile + (int)rank * kTile + quad * 32 + lane;
-      epi.load_scales(p, t0, half, lane, v);
-      if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[buf], (at >> 1) & 1u, abort_flag))) break;
-      tc::tc_fence_after();
-      epi.store(p, tmem_base + ((uint32_t)(quad * 32) << 16) + buf * kPairN, t0, half, v, v < p.V);
-      tc::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive_cluster_bare(tc::mapa_shared(tc::smem_u32(&ctl->tempty[buf]), 0));     // (TMEM has been read)
+      const bool row_ok = v < p.V;
+      const float sw = row_ok && p.w.row ? p.w.row[v] : 1.f;
+      const auto take = [&](int acc, Held<O> (&held)[kChunks]) {
+        float sh[kChunks];
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          const int t = t0 + acc * n + (kShare * i + half) * 32 + lane;
+          sh[i] = t < p.T && p.h.row ? p.h.row[t] : 1.f;
+        }
+        if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[acc], at & 1u, abort_flag))) return false;
+        tc::tc_fence_after();
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          const int c = (kShare * i + half) * 32;
+          if (c < n) {
+            uint32_t r[32];
+            __syncwarp();                                  // the TMEM load is warp-collective
+            tc::tmem_ld_32x32(tmem_base + ((uint32_t)(quad * 32) << 16) + acc * kPairN + c, r);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int q = 0; q < 32; ++q) r[q] = __float_as_uint(__uint_as_float(r[q]) * __shfl_sync(0xffffffffu, sh[i], q) * sw);
+            held[i].take(r);
+          }
+        }
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive_cluster_bare(tc::mapa_shared(tc::smem_u32(&ctl->tempty[acc]), 0));     // (TMEM has been read)
+        return true;
+      };
+      const auto put = [&](int acc, const Held<O> (&held)[kChunks]) {
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+          const int c = t0 + acc * n + (kShare * i + half) * 32, left = min(n - (kShare * i + half) * 32, p.T - c);
+          O* o = static_cast<O*>(p.out) + (long long)c * p.V + v;
+#pragma unroll
+          for (int q = 0; q < 32; ++q) {
+            if (row_ok && q < left) *o = held[i].at(q);
+            o += p.V;
+          }
+        }
+      };
+      // both accumulators are emptied before anything is stored where the registers hold them
+      Held<O> first[kChunks], second[kChunks];
+      if (!take(0, first)) break;
+      if (sizeof(O) == 4) put(0, first);
+      if (!take(1, second)) break;
+      if (sizeof(O) == 2) put(0, first);
+      put(1, second);
     }
   }
   __syncwarp();
@@ -720,10 +800,7 @@ template <typename O, int BLOCK>
 int product(aero_ctx* ctx, Params p) {
   constexpr uint32_t kScales = groups_per_slab(BLOCK) * kGroupBytes;
   if (p.T > kRowsN) {
-    // equal token tiles of 128 or 192
-    p.n_tok = (p.T + kPairN - 1) / kPairN;
-    p.n = ((p.T + p.n_tok - 1) / p.n_tok + 63) / 64 * 64;
-    p.n_tok = (p.T + p.n - 1) / p.n;
+    p.n_tok = (p.T + kPairT - 1) / kPairT;
     CUtensorMap tmW, tmWs, tmH, tmHs;
     const uint64_t w_rows = (uint64_t)tiles_of(p.V) * p.slabs, h_rows = (uint64_t)tiles_of(p.T) * p.slabs;
     constexpr uint32_t kGroups = groups_per_slab(BLOCK);
