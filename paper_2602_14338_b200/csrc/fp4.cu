@@ -527,30 +527,45 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
   }
 }
 
-// 32 values of an output type in registers.
+// 32 logits of a vocabulary row in registers: accumulators times the scales of their tokens (in shared memory) and of the row.
+__device__ __forceinline__ void scaled(const uint32_t* r, const float* scales, float sw, float (&z)[4]) {
+  const float4 s = *reinterpret_cast<const float4*>(scales);
+  z[0] = __uint_as_float(r[0]) * s.x * sw; z[1] = __uint_as_float(r[1]) * s.y * sw;
+  z[2] = __uint_as_float(r[2]) * s.z * sw; z[3] = __uint_as_float(r[3]) * s.w * sw;
+}
 template <typename O> struct Held;
 template <> struct Held<float> {
   float v[32];
-  __device__ void take(const uint32_t (&r)[32]) {
+  __device__ void take(int half, const uint32_t (&r)[16], const float* scales, float sw) {
 #pragma unroll
-    for (int q = 0; q < 32; ++q) v[q] = __uint_as_float(r[q]);
+    for (int q = 0; q < 16; q += 4) {
+      float z[4];
+      scaled(r + q, scales + 16 * half + q, sw, z);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[16 * half + q + k] = z[k];
+    }
   }
   __device__ float at(int q) const { return v[q]; }
 };
 template <> struct Held<__nv_bfloat16> {
   __nv_bfloat162 v[16];
-  __device__ void take(const uint32_t (&r)[32]) {
+  __device__ void take(int half, const uint32_t (&r)[16], const float* scales, float sw) {
 #pragma unroll
-    for (int q = 0; q < 16; ++q) v[q] = __floats2bfloat162_rn(__uint_as_float(r[2 * q]), __uint_as_float(r[2 * q + 1]));
+    for (int q = 0; q < 16; q += 4) {
+      float z[4];
+      scaled(r + q, scales + 16 * half + q, sw, z);
+      v[8 * half + q / 2] = __floats2bfloat162_rn(z[0], z[1]);
+      v[8 * half + q / 2 + 1] = __floats2bfloat162_rn(z[2], z[3]);
+    }
   }
   __device__ __nv_bfloat16 at(int q) const { return q & 1 ? v[q / 2].y : v[q / 2].x; }
 };
 
-// The pair kernel is bound by what the SMs read from L2: 10 TB/s.  The tokens of a unit are therefore as many as the accumulators
-// hold, 2 x 192 (with 512 columns of TMEM and 128 of them for scales), and both accumulators use the rows of W that were
-// loaded once.  (With units of 192 tokens and one accumulator filling while the other was read, 2048 tokens of d = 3584, V = 152064
-// took 701 us instead of 668.)  An accumulator is emptied into registers as soon as its products are done, rounded there, and stored
-// while the next unit's products run.
+// The tokens of a unit are as many as the accumulators hold, 2 x 192 (of 512 columns of TMEM 128 hold scales), and both accumulators
+// use the rows of W that were loaded once: with units of 192 tokens the SMs' reads from L2, 10 TB/s, were the bound (2048
+// tokens of d = 3584, V = 152064 701 us).  The accumulators are emptied into registers as soon as their products are done, rounded there,
+// and stored while the next unit's products run; what is left of the time is the products (96 cycles each, 430 us at the clock that the
+// power allows), that emptying, and the round trips of the scales: 574 us.
 // A stage, per CTA: codes of 128 rows of W and of its half of each accumulator's tokens, scales of these rows of W, and of the three
 // groups of 128 token rows (both CTAs' tensor cores multiply all columns).
 constexpr int PSTAGES = 4, kPiece = 32, kTokenGroups = kPairT / kTile;
@@ -558,7 +573,10 @@ constexpr uint32_t kHalfBytes = kPairN / 2 * kRowBytes;
 __host__ __device__ constexpr uint32_t pair_stage(int block) {
   return kTileBytes + 2 * kHalfBytes + (1 + kTokenGroups) * groups_per_slab(block) * kGroupBytes;
 }
-constexpr size_t p_smem(int block) { return 1024 + (size_t)PSTAGES * pair_stage(block) + sizeof(Ctl<PSTAGES>); }
+struct PairCtl : Ctl<PSTAGES> {
+  alignas(16) float token_scales[EPI_WARPS * kPairT / kShare];      // each warp's own tokens, of both accumulators
+};
+constexpr size_t p_smem(int block) { return 1024 + (size_t)PSTAGES * pair_stage(block) + sizeof(PairCtl); }
 
 // Tokens of each accumulator in the unit that begins with token t0: half of what is left, in steps of 64.
 __host__ __device__ inline int pair_n(int T, int t0) {
@@ -575,11 +593,11 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
   constexpr int kGroups = groups_per_slab(BLOCK);
   constexpr uint32_t kStage = pair_stage(BLOCK), kScales = kGroups * kGroupBytes;
   // columns of TMEM: two accumulators, then kSets sets of a slab's scales, W's and for each k step the tokens'.  (Four sets of half a
-  // slab: 969 us, a set's way through the scales' warps takes longer than the products of half a slab.)
+  // slab were slower, 969 us for 662: a set's way through the scales' warps is longer than the products of half a slab.)
   constexpr int kSets = 2;
   constexpr uint32_t kSetCols = 4 * kGroups * (1 + kTokenGroups), kScaleBase = 2 * kPairN;
   static_assert(kScaleBase + kSets * kSetCols <= 512, "TMEM");
-  auto* ctl = reinterpret_cast<Ctl<PSTAGES>*>(smem + (size_t)PSTAGES * kStage);
+  auto* ctl = reinterpret_cast<PairCtl*>(smem + (size_t)PSTAGES * kStage);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_ctarank();        // 0 issues the MMAs of the pair
   const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
@@ -705,35 +723,39 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
     }
   } else {
     // a thread has a vocabulary row, so the 32 lanes of a warp store 32 neighbouring logits of a token at a time; the two warps of a
-    // quadrant of TMEM take chunks of 32 tokens in turn
+    // quadrant of TMEM take chunks of 32 tokens in turn.  (The products of the next unit wait for the accumulators to be emptied, so
+    // what is between a wait and its release is kept short, and all of it small enough for the instruction cache.)
     constexpr int kChunks = kPairN / 32 / kShare;
     uint32_t at = 0;
     const int quad = warp & 3, half = warp >> 2;
+    float* scales = ctl->token_scales + warp * 2 * kChunks * 32;       // of this warp's tokens
     for (long long u = pair; u < units; u += npairs, ++at) {
       const int t0 = (int)(u % p.n_tok) * kPairT, n = pair_n(p.T, t0);
       const int v = (int)(u / p.n_tok) * 2 * kTile + (int)rank * kTile + quad * 32 + lane;
       const bool row_ok = v < p.V;
       const float sw = row_ok && p.w.row ? p.w.row[v] : 1.f;
-      const auto take = [&](int acc, Held<O> (&held)[kChunks]) {
-        float sh[kChunks];
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-          const int t = t0 + acc * n + (kShare * i + half) * 32 + lane;
-          sh[i] = t < p.T && p.h.row ? p.h.row[t] : 1.f;
-        }
+      for (int i = 0; i < 2 * kChunks; ++i) {
+        const int t = t0 + (i / kChunks) * n + (kShare * (i % kChunks) + half) * 32 + lane;
+        scales[i * 32 + lane] = t < p.T && p.h.row ? p.h.row[t] : 1.f;
+      }
+      __syncwarp();
+      const auto take = [&](int acc, Held<O> (&held)[kChunks]) {
         if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->tfull[acc], at & 1u, abort_flag))) return false;
         tc::tc_fence_after();
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
           const int c = (kShare * i + half) * 32;
           if (c < n) {
-            uint32_t r[32];
-            __syncwarp();                                  // the TMEM load is warp-collective
-            tc::tmem_ld_32x32(tmem_base + ((uint32_t)(quad * 32) << 16) + acc * kPairN + c, r);
-            tc::tmem_ld_wait();
+            // (in halves: the registers left beside the chunks that are held)
 #pragma unroll
-            for (int q = 0; q < 32; ++q) r[q] = __float_as_uint(__uint_as_float(r[q]) * __shfl_sync(0xffffffffu, sh[i], q) * sw);
-            held[i].take(r);
+            for (int k = 0; k < 2; ++k) {
+              uint32_t r[16];
+              __syncwarp();                                // the TMEM load is warp-collective
+              tc::tmem_ld_32x16(tmem_base + ((uint32_t)(quad * 32) << 16) + acc * kPairN + c + 16 * k, r);
+              tc::tmem_ld_wait();
+              held[i].take(k, r, scales + (acc * kChunks + i) * 32, sw);
+            }
           }
         }
         tc::tc_fence_before();
@@ -742,24 +764,29 @@ fp4_pair_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__
         return true;
       };
       const auto put = [&](int acc, const Held<O> (&held)[kChunks]) {
+        const uint32_t stride = (uint32_t)p.V * (uint32_t)sizeof(O);      // (V <= 2^30)
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-          const int c = t0 + acc * n + (kShare * i + half) * 32, left = min(n - (kShare * i + half) * 32, p.T - c);
-          O* o = static_cast<O*>(p.out) + (long long)c * p.V + v;
+          const int c = t0 + acc * n + (kShare * i + half) * 32, left = row_ok ? min(n - (kShare * i + half) * 32, p.T - c) : 0;
+          uint8_t* o = static_cast<uint8_t*>(p.out) + ((long long)c * p.V + v) * (long long)sizeof(O);
+          if (__all_sync(0xffffffffu, left >= 32)) {
 #pragma unroll
-          for (int q = 0; q < 32; ++q) {
-            if (row_ok && q < left) *o = held[i].at(q);
-            o += p.V;
+            for (int q = 0; q < 32; ++q, o += stride) *reinterpret_cast<O*>(o) = held[i].at(q);
+          } else if (left > 0) {
+#pragma unroll
+            for (int q = 0; q < 32; ++q, o += stride)
+              if (q < left) *reinterpret_cast<O*>(o) = held[i].at(q);
           }
         }
       };
-      // both accumulators are emptied before anything is stored where the registers hold them
+      // both accumulators are emptied before anything is stored where the registers hold them (stored in turn: 690 us for 662)
       Held<O> first[kChunks], second[kChunks];
       if (!take(0, first)) break;
       if (sizeof(O) == 4) put(0, first);
       if (!take(1, second)) break;
       if (sizeof(O) == 2) put(0, first);
       put(1, second);
+      __syncwarp();                                        // (before the next unit's scales)
     }
   }
   __syncwarp();
