@@ -758,7 +758,7 @@ int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor*
  * aero_dequantize_fp4: the values, rounded once to out_dtype (AERO_BF16 | AERO_FP32), out [T,d].
  * aero_lmhead_fp4: out[t,v] = sum_k h_tk w_vk of the values, T rows h and V rows w in the same format; sums of exact products in
  *   fp32 on the tensor cores, multiplied by the two rows' scales and rounded once to out_dtype; out [T,V].
- * d % 32 == 0, d <= 65536, T and V <= 2^30; x, out of aero_dequantize_fp4, codes and scales 16-byte aligned.
+ * d % 32 == 0, d <= 65536, T and V <= 2^30 (aero_lmhead_fp4: codes of at most 2^38 bytes); x, out of aero_dequantize_fp4, codes and scales 16-byte aligned.
  */
 size_t aero_fp4_code_bytes(int64_t T, int32_t d);
 size_t aero_fp4_scale_bytes(int64_t T, int32_t d, int32_t block);

@@ -7,7 +7,7 @@
 
 extern "C" {
 
-int aero_version(void) { return 104; }
+int aero_version(void) { return 105; }
 
 const char* aero_error_string(int code) {
   switch (code) {

@@ -937,6 +937,8 @@ int aero_lmhead_fp4(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, int32_t bloc
       reinterpret_cast<uintptr_t>(h_row) % 4 || reinterpret_cast<uintptr_t>(w_row) % 4 ||
       reinterpret_cast<uintptr_t>(out) % (out_dtype == AERO_FP32 ? 4 : 2))
     return AERO_ERR_INVALID;
+  // rows of tiles are counted in 32 bits
+  if (tiles_of(T > V ? T : V) * slabs_of(d) * kTile > 0x7fffffffll - kPairT) return AERO_ERR_UNSUPPORTED;
   if ((rc = aero_check_ctx(ctx))) return rc;
   if (T == 0) return AERO_OK;
   const Params p = {(int)T, V, slabs_of(d), 0, 1, {h_codes, h_scales, h_row}, {w_codes, w_scales, w_row}, out, ctx->d_status, 0, 0};

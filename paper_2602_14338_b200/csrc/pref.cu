@@ -80,20 +80,59 @@ __device__ __forceinline__ bool rows_of(const PrefArgs& a, int i, long long* t0,
 }
 __device__ __forceinline__ bool scored(const PrefArgs& a, long long t) { return a.y[t] >= 0 && a.y[t] < a.V; }
 
-// f(t, whether the row is scored, scored rows of its group of 32 as a word) by the 32 lanes of a warp, four groups' loads at a time.
-template <typename F>
+// f(t, whether the row is scored, scored rows of its group of 32 as a word) by the 32 lanes of a warp, four groups' loads at a time;
+// LANES 1: by one thread, row by row.
+template <int LANES, typename F>
 __device__ __forceinline__ void for_rows(const PrefArgs& a, long long t0, long long t1, int lane, F&& f) {
-  for (long long t = t0; t < t1; t += 128) {
-    bool s[4];
+  if constexpr (LANES == 1) {
+    for (long long t = t0; t < t1; ++t) {
+      const bool s = scored(a, t);
+      f(t, s, s ? 1u : 0u);
+    }
+  } else {
+    for (long long t = t0; t < t1; t += 128) {
+      bool s[4];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) s[q] = t + 32 * q + lane < t1 && scored(a, t + 32 * q + lane);
+      for (int q = 0; q < 4; ++q) s[q] = t + 32 * q + lane < t1 && scored(a, t + 32 * q + lane);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) f(t + 32 * q + lane, s[q], __ballot_sync(0xffffffffu, s[q]));
+      for (int q = 0; q < 4; ++q) f(t + 32 * q + lane, s[q], __ballot_sync(0xffffffffu, s[q]));
+    }
+  }
+}
+// Scored rows of the rollouts i, i + step, ..., to off; with LANES 32 a warp, with 1 a thread for each.
+template <int LANES>
+__device__ __forceinline__ void count_rows(const PrefArgs& a) {
+  const int lane = threadIdx.x % LANES;
+  for (int i = threadIdx.x / LANES; i < a.R; i += kPlanThreads / LANES) {
+    long long t0, t1, rows = 0;
+    if (rows_of(a, i, &t0, &t1)) {
+      bool wrong = false;
+      for_rows<LANES>(a, t0, t1, lane, [&](long long t, bool s, unsigned word) {
+        rows += __popc(word);
+        wrong |= t < t1 && !s && a.y[t] != AERO_NO_TOKEN;
+      });
+      if (wrong) aero_raise(a.status, AERO_ST_BAD_TARGET);
+    } else if (lane == 0 && !(t0 >= 0 && t1 >= t0 && t1 <= a.T)) {
+      aero_raise(a.status, AERO_ST_BAD_OFFSETS);
+    }
+    if (lane == 0) a.off[i + 1] = rows;
+  }
+}
+template <int LANES>
+__device__ __forceinline__ void list_rows(const PrefArgs& a) {
+  const int lane = threadIdx.x % LANES;
+  for (int i = threadIdx.x / LANES; i < a.R; i += kPlanThreads / LANES) {
+    long long t0, t1, at = a.off[i];
+    if (rows_of(a, i, &t0, &t1))
+      for_rows<LANES>(a, t0, t1, lane, [&](long long t, bool s, unsigned word) {
+        if (s) a.src[at + (LANES == 1 ? 0 : __popc(word & ((1u << lane) - 1u)))] = (int32_t)t;
+        at += __popc(word);
+      });
   }
 }
 
-// One block: which rollouts are used, where their scored rows go, and the list of these rows.  (A warp reads a rollout's targets at a few
-// GB/s, 4 bytes a token: 1 % of the time of the products at the smallest vocabularies.)
+// One block: which rollouts are used, where their scored rows go, and the list of these rows.  (6 us for a few rollouts of hundreds of
+// tokens; a rollout takes far less time here than the products of one token.)
 __global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
   __shared__ long long sums[32];
   __shared__ int total;
@@ -118,20 +157,10 @@ __global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
   if (bad) aero_raise(a.status, AERO_ST_BAD_PAIR);
   __syncthreads();
   // scored rows of each rollout (at most T in all where offsets do not overlap), then their running sums
-  for (int i = warp; i < a.R; i += 32) {
-    long long t0, t1, rows = 0;
-    if (rows_of(a, i, &t0, &t1)) {
-      bool wrong = false;
-      for_rows(a, t0, t1, lane, [&](long long t, bool s, unsigned word) {
-        rows += __popc(word);
-        wrong |= t < t1 && !s && a.y[t] != AERO_NO_TOKEN;
-      });
-      if (wrong) aero_raise(a.status, AERO_ST_BAD_TARGET);
-    } else if (lane == 0 && !(t0 >= 0 && t1 >= t0 && t1 <= a.T)) {
-      aero_raise(a.status, AERO_ST_BAD_OFFSETS);
-    }
-    if (lane == 0) a.off[i + 1] = rows;
-  }
+  // (a thread for a rollout where a warp would mostly idle)
+  const bool brief = a.T < 32ll * a.R;
+  if (brief) count_rows<1>(a);
+  else count_rows<32>(a);
   __syncthreads();
   long long carry = 0;
   for (int base = 0; base < a.R; base += kPlanThreads) {
@@ -172,14 +201,8 @@ __global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
     *a.counted = total;
   }
   __syncthreads();
-  for (int i = warp; i < a.R; i += 32) {
-    long long t0, t1, at = a.off[i];
-    if (rows_of(a, i, &t0, &t1))
-      for_rows(a, t0, t1, lane, [&](long long t, bool s, unsigned word) {
-        if (s) a.src[at + __popc(word & ((1u << lane) - 1u))] = (int32_t)t;
-        at += __popc(word);
-      });
-  }
+  if (brief) list_rows<1>(a);
+  else list_rows<32>(a);
 }
 
 // A warp per row.  GATHER: the row of H into the run, its target with the target's logit and, for the backward alone, lse and

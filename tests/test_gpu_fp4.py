@@ -159,3 +159,33 @@ PRODUCTS = [(1, 32, 1), (1, 256, 128), (1, 1536, 1000), (2, 64, 31), (17, 288, 1
 def test_product(ctx, T, d, V, block, out):
     got, want, size = product_of(ctx, T, d, V, block, out)
     check_product(got, want, size, d, out)
+
+
+@pytest.mark.parametrize("T", [5, 300])
+def test_captured_on_another_stream_beside_another_call(ctx, T):
+    """A chain captured on a stream of its own and replayed while the first context runs the same on another stream, on other inputs."""
+    d, V = 512, 3000
+    cfg = cfg_of("bf16")
+    x, w = values(T, d, torch.bfloat16, 1), values(V, d, torch.bfloat16, 2)
+    want = ctx.lmhead_fp4(ctx.quantize_fp4(cfg, x), ctx.quantize_fp4(cfg, w), out_dtype=torch.float32)
+    x2 = x.flip(0).contiguous()
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    own = B.Context(0, stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        rows = own.quantize_fp4(cfg, x)
+        z = own.lmhead_fp4(rows, own.quantize_fp4(cfg, w), out_dtype=torch.float32)
+        back = own.dequantize_fp4(rows)
+    for _ in range(3):
+        z.fill_(float("nan"))
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            graph.replay()
+        other = ctx.lmhead_fp4(ctx.quantize_fp4(cfg, x2), ctx.quantize_fp4(cfg, w), out_dtype=torch.float32)
+        torch.cuda.synchronize()
+        assert torch.equal(z, want) and torch.equal(other, want.flip(0))
+    assert torch.equal(back, ctx.dequantize_fp4(ctx.quantize_fp4(cfg, x)))
+    assert own.last_status() == 0
+    del graph
+    own.close()

@@ -101,7 +101,7 @@ def test_fp4_refusals(lib, fake):
     assert values(dtype=3) == UNSUPPORTED and product(dtype=3) == UNSUPPORTED
     for name in ("h", "hs", "hr", "w", "ws", "wr", "out"):
         assert product(**{name: None}) == INVALID and product(**{name: P + 1}) == INVALID, name
-    assert product(V=0) == INVALID and product(V=(1 << 30) + 1) == UNSUPPORTED
+    assert product(V=0) == INVALID and product(V=(1 << 30) + 1) == UNSUPPORTED and product(V=1 << 30, d=1024) == UNSUPPORTED
     assert product(dtype=B.AERO_FP32, out=P + 2) == INVALID
 
 
