@@ -1016,10 +1016,10 @@ int launch_fp32(aero_ctx* ctx, K kernel, const Fp32Args& f, long long rows, long
 
 int fwd_fp32(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float* metrics) {
   aero_ctx* ctx = c.ctx;
-  int rc = start(c, s, lse, kl, nullptr, true);
+  int rc = start(c, s, lse, kl, nullptr, loss != nullptr);
   if (rc) return rc;
   if (c.T > 0 && c.R > 0) {
-    RowsArgs a = rows_of(c, s, lse, kl, true, 1.f);
+    RowsArgs a = rows_of(c, s, lse, kl, loss != nullptr, 1.f);
     a.ls.entry = nullptr;
     if ((rc = launch_fp32(ctx, fp32_rows_kernel<1, false>, {a, nullptr, nullptr, 0}, c.T, c.V))) return rc;
     if ((rc = rows_fp32(a, ctx, c.ex.z != nullptr))) return rc;
@@ -1109,7 +1109,7 @@ int plan_launch(const Call& c, const Ws& s, long long begin, long long tpc, bool
 
 int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float* metrics) {
   aero_ctx* ctx = c.ctx;
-  int rc = start(c, s, lse, kl, nullptr, true);
+  int rc = start(c, s, lse, kl, nullptr, loss != nullptr);
   if (rc) return rc;
   if (c.T > 0 && c.R > 0) {
     if ((rc = aero_build_tiles(ctx, c.T, c.R, c.cs, c.keep, lmhead::BM, s.tiles))) return rc;
@@ -1122,7 +1122,7 @@ int fwd_tc(const Call& c, const Ws& s, float* lse, float* kl, float* loss, float
     p.tile_begin = 0; p.tile_end = s.tiles.max_tiles;
     p.xstate = s.xstate;
     if ((rc = lmhead_launch(c, s, p, tmH, tmW, tmH, kFwd))) return rc;
-    RowsArgs a = rows_of(c, s, lse, kl, true, 1.f);
+    RowsArgs a = rows_of(c, s, lse, kl, loss != nullptr, 1.f);
     a.xstate = s.xstate;
     a.tile_row = s.tiles.tile_row; a.tile_valid = s.tiles.tile_valid; a.n_tiles = s.tiles.n_tiles;
     a.tile_begin = 0; a.tile_end = s.tiles.max_tiles;
@@ -1141,7 +1141,8 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
   aero_ctx* ctx = c.ctx;
   const int d = c.d, V = c.V;
   const long long tpc = gr.tpc, listed_tiles = mode == kBoth ? tpc : 0;
-  int rc = start(c, s, mode == kBoth ? lse : nullptr, kl, gr.dH, mode == kBoth, listed_tiles);
+  const bool sums = mode == kBoth && !c.ex.between;      // (the loss of another caller is its own)
+  int rc = start(c, s, mode == kBoth ? lse : nullptr, kl, gr.dH, sums, listed_tiles);
   if (rc) return rc;
   if (c.T == 0 || c.R == 0) {
     if (gr.dW16) AERO_CUDA_TRY(cudaMemsetAsync(gr.dW16, 0, (size_t)V * d * 2, ctx->stream));
@@ -1181,7 +1182,7 @@ int grads_tc(const Call& c, const Ws& s, Mode mode, float* lse, float* kl, const
     void* clear = begin > 0 || gr.accumulate ? nullptr : (gr.dW16 ? static_cast<void*>(gr.dW16) : static_cast<void*>(gr.dW));
     if (begin > 0) AERO_CUDA_TRY(cudaMemsetAsync(s.zero, 0, zero_bytes((size_t)listed_tiles), ctx->stream));
     if ((rc = plan_launch(c, s, begin, tpc, pairs, clear, (size_t)V * d * (gr.dW16 ? 2 : 4)))) return rc;
-    RowsArgs a = rows_of(c, s, lse, kl, mode == kBoth, gr.grad_scale);
+    RowsArgs a = rows_of(c, s, lse, kl, sums, gr.grad_scale);
     a.tile_row = s.tiles.tile_row; a.tile_valid = s.tiles.tile_valid; a.n_tiles = s.tiles.n_tiles;
     a.tile_begin = (int)begin; a.tile_end = (int)end; a.Hl = Hl;
     lmhead::Params p = {};

@@ -50,6 +50,7 @@ struct PrefArgs {
   uint8_t* dHg;                   // [T][d], with gradients
   float* row_weights;             // [T] -grad_scale coef of the row's rollout
   float* ones;                    // [T] 1
+  float* zeros;                   // [T] 0: the listed tokens' teacher logits
   float* zg;                      // [T] logits of the rows' targets
   float grad_scale;
   const void* W;
@@ -211,6 +212,9 @@ template <typename T, bool GATHER>
 __global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, T* dH) {
   const int lane = threadIdx.x & 31, d = a.d;
   const long long n = a.run[1];
+  if (GATHER && !a.backward) {                      // rows that are not scored keep these
+    for (long long t = (long long)blockIdx.x * 256 + threadIdx.x; t < a.T; t += (long long)gridDim.x * 256) a.logp[t] = a.lse[t] = 0.f;
+  }
   for (long long p = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); p < n; p += (long long)gridDim.x * 8) {
     const long long t = a.src[p];
     const T* from = GATHER ? static_cast<const T*>(a.H) + t * d : reinterpret_cast<const T*>(a.dHg) + p * d;
@@ -220,6 +224,7 @@ __global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, T* dH) {
     float z = 0.f;
     const auto part = [&](auto vec) {
       constexpr int VEC = decltype(vec)::value;
+#pragma unroll 4
       for (int e = lane * VEC; e < d; e += 32 * VEC) {
         float x[VEC], y[VEC];
         rowvec::load<T, VEC>(from + e, x);
@@ -240,6 +245,7 @@ __global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, T* dH) {
         a.yg[p] = v;
         a.zg[p] = z;
         a.ones[p] = 1.f;
+        a.zeros[p] = 0.f;
         if (a.backward) {
           a.lseg[p] = a.lse_in[t];
           a.row_weights[p] = -a.grad_scale * a.coef_in[aero_owner(a.off, a.R, p)];
@@ -413,7 +419,6 @@ bool small_loss(const PrefArgs& a) { return a.T <= 8192 && a.R <= 1024 && (long 
 
 struct Ws {
   PrefArgs a;                     // its buffers
-  float* zeros;                   // [T]: the listed tokens' teacher logits
   char* rest;
   size_t head_bytes;
 };
@@ -435,7 +440,7 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t R, int32_t P, int elem, bool 
   s.a.lseg = reinterpret_cast<float*>(take(Tn * 4));
   s.a.klg = reinterpret_cast<float*>(take(Tn * 4));
   s.a.row_weights = reinterpret_cast<float*>(take(Tn * 4));
-  s.zeros = reinterpret_cast<float*>(take(Tn * 4));
+  s.a.zeros = reinterpret_cast<float*>(take(Tn * 4));
   s.a.ones = reinterpret_cast<float*>(take(Tn * 4));
   s.a.zg = reinterpret_cast<float*>(take(Tn * 4));
   s.a.r = reinterpret_cast<double*>(take((size_t)(R + 1) * 8));
@@ -488,11 +493,6 @@ struct Call {
 
   int gather() {
     const cudaStream_t stream = ctx->stream;
-    if (!s.a.backward && s.a.T > 0) {
-      AERO_CUDA_TRY(cudaMemsetAsync(s.a.logp, 0, (size_t)s.a.T * 4, stream));
-      AERO_CUDA_TRY(cudaMemsetAsync(s.a.lse, 0, (size_t)s.a.T * 4, stream));
-    }
-    AERO_CUDA_TRY(cudaMemsetAsync(s.zeros, 0, (size_t)s.a.T * 4 + 4, stream));
     pref_plan_kernel<<<1, kPlanThreads, 0, stream>>>(s.a);
     if (s.a.T > 0) {
       const int grid = grid_for(s.a.T, 8, 16 * ctx->sm_count);
@@ -510,7 +510,7 @@ struct Call {
   }
 
   int forward(const AeroListed& ex, size_t room) {
-    return aero_distill_fwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.zeros, nullptr,
+    return aero_distill_fwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.a.zeros, nullptr,
                                    s.a.run, s.a.ones, s.a.one, s.a.lseg, s.a.klg, nullptr, nullptr, s.rest,
                                    room);
   }
@@ -538,7 +538,7 @@ struct Call {
     AeroListed ex;
     given(ex);
     (cfg->dtype == AERO_BF16 ? ex.row_factor : ex.row_weights) = s.a.row_weights;
-    return aero_distill_bwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.zeros, nullptr,
+    return aero_distill_bwd_listed(ex, ctx, cfg, s.a.T, s.a.d, s.a.V, 1, 1, s.a.Hg, W, s.a.yg, s.a.zeros, nullptr,
                                    s.a.run, s.a.ones, s.a.one, s.a.lseg, 1.f, s.a.dHg, dW, dw_dtype,
                                    accumulate_dW, s.rest, room);
   }
@@ -658,7 +658,7 @@ int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* p
     ex.row_factor = a.row_weights;
     ex.between = Call::between;
     ex.arg = &c;
-    rc = aero_distill_fwd_bwd_listed(ex, ctx, cfg, T, d, V, 1, 1, a.Hg, W, a.yg, c.s.zeros, nullptr, a.run,
+    rc = aero_distill_fwd_bwd_listed(ex, ctx, cfg, T, d, V, 1, 1, a.Hg, W, a.yg, a.zeros, nullptr, a.run,
                                      a.ones, a.one, a.lseg, a.klg, nullptr, nullptr, 1.f, a.dHg, dW, dw_dtype, accumulate_dW,
                                      c.s.rest, room);
   } else {
