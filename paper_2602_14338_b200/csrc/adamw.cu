@@ -22,6 +22,10 @@ constexpr int kNormBlocks = 148 * 8;     // of the norm's launch: a record each
 // Of the others.  (Step with 8-bit states and states as numbers, 233 M elements: 1031 us with 592 blocks, 1023 with 1184, 999 with
 // 2368, 966 with 9472, 993 with one per chunk; with fp32 states 1694, 1700, 1599, 1518, 1484.)
 constexpr int kMaxBlocks = 148 * 64;
+// Chunks at most of a call whose step's blocks add the norm's records up themselves: a record each.  (Without / with, bf16 params with
+// fp32 masters, from the host, +-1 us: 60 x 1536 17.4 / 14.3 us, 8 x 98304 21.4 / 18.4, 16 x 98304 25.6 / 22.5, 24 x 98304 = 1152 chunks
+// 29.6 / 26.6, 40 x 98304 33.8 / 33.8; 8 x 2^20, with 592 blocks for the step, 53 / 59.)
+constexpr int kJoinChunks = kNormBlocks;
 constexpr float kTopM = 448.f, kTopV = 496.f;          // largest values of the two 8-bit formats
 constexpr float kLeast = 0x1p-100f;     // scales are made of at least this: 448 / it stays finite
 
@@ -50,10 +54,24 @@ struct Scalars {
   float g_factor;                       // grad_scale clip
   float lr, c1, c2;                     // 1 / (1 - beta1^t), the root of 1 / (1 - beta2^t)
   int skip;
+  long long t;
 };
 
 struct Hyper {
   float beta1, beta2, rest1, rest2, eps;      // rest = 1 - beta
+};
+
+// Numbers that the step is made of besides the tensors.
+struct PrepareArgs {
+  const double* partials;               // NULL: no norm
+  int n_partials;
+  double beta1, beta2;
+  float lr, max_norm, grad_scale;
+  int skip_nonfinite;
+  const float* lr_dev;
+  long long* step;
+  float* stats;
+  Scalars* out;
 };
 
 __device__ __forceinline__ int slot_of(const Table& t, long long chunk) {
@@ -237,11 +255,21 @@ __device__ __forceinline__ double squares(const float (&g)[kEach]) {
   for (int i = 0; i < kEach; ++i) sum += (double)g[i] * g[i];
   return sum;
 }
-__global__ void __launch_bounds__(kWarps * 32) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partials) {
-  __shared__ double sh[kWarps];
+__device__ __forceinline__ double correction(double beta, long long t) { return 1.0 / (1.0 - pow(beta, (double)t)); }
+
+// JOIN: one span per chunk, and block 0 also counts the step and leaves all scalars but the gradients' factor, which the step's blocks then make.
+template <bool JOIN>
+__global__ void __launch_bounds__(kWarps * 32) adamw_norm_kernel(const __grid_constant__ Table tab, double* __restrict__ partials,
+                                                                 const PrepareArgs a) {
+  constexpr int kEachSpans = JOIN ? 1 : kSpans;
+  __shared__ double sh[kWarps], corr[2];
+  const bool count = JOIN && blockIdx.x == 0;
+  const long long taken = count ? *a.step : 0;
+  if (count && (threadIdx.x == 192 || threadIdx.x == 224))
+    corr[threadIdx.x == 224] = correction(threadIdx.x == 224 ? a.beta2 : a.beta1, taken + 1);
   double sum = 0.0;
-  for_chunks(tab, kSpans, [&](const Slot& t, long long e0) {
-    if ((t.flags & kAligned) && (t.flags & kGrad16) && t.n - e0 >= (kSpans - 1) * kChunk + kBlock) {
+  for_chunks(tab, kEachSpans, [&](const Slot& t, long long e0) {
+    if (!JOIN && (t.flags & kAligned) && (t.flags & kGrad16) && t.n - e0 >= (kSpans - 1) * kChunk + kBlock) {
       // all loads of the chunk under way at once (one at a time keeps half of the bytes that the memory needs under way)
       uint4 u[kSpans];
 #pragma unroll
@@ -255,7 +283,7 @@ __global__ void __launch_bounds__(kWarps * 32) adamw_norm_kernel(const __grid_co
       }
     } else {
 #pragma unroll 1
-      for (int q = 0; q < kSpans && e0 < t.n; ++q, e0 += kChunk) {
+      for (int q = 0; q < kEachSpans && e0 < t.n; ++q, e0 += kChunk) {
         float g[kEach];
         load(t.grad, t.flags & kGrad16, span_at(t, e0), g);
         sum += squares(g);
@@ -269,58 +297,48 @@ __global__ void __launch_bounds__(kWarps * 32) adamw_norm_kernel(const __grid_co
   if (threadIdx.x == 0) {
     for (int w = 1; w < kWarps; ++w) sum += sh[w];
     partials[blockIdx.x] = sum;
+    if (count) {
+      *a.step = taken + 1;
+      *a.out = {0.f, a.lr_dev ? *a.lr_dev : a.lr, (float)corr[0], (float)sqrt(corr[1]), 0, taken + 1};
+    }
   }
 }
 
-struct PrepareArgs {
-  const double* partials;               // NULL: no norm
-  int n_partials;
-  double beta1, beta2;
-  float lr, max_norm, grad_scale;
-  int skip_nonfinite;
-  const float* lr_dev;
-  long long* step;
-  float* stats;
-  Scalars* out;
-};
-// One block.  Two warps raise the betas to the step's number while the others wait for the norm's records.
-__global__ void __launch_bounds__(256) adamw_prepare_kernel(PrepareArgs a) {
-  __shared__ double sh[8], correction[2];
-  const long long taken = *a.step;
-  if (threadIdx.x == 192 || threadIdx.x == 224) {
-    const int k = threadIdx.x == 224;
-    correction[k] = 1.0 / (1.0 - pow(k ? a.beta2 : a.beta1, (double)(taken + 1)));
-  }
+// Thread 0 of a block gets the norm, from the records in a fixed order, and the factor that clips to max_norm.
+__device__ __forceinline__ void norm_and_clip(const PrepareArgs& a, double* sh, double* norm, double* clip) {
   double sum = 0.0;
   if (a.partials)
-    for (int i = threadIdx.x; i < a.n_partials; i += 256) sum += a.partials[i];
+    for (int i = threadIdx.x; i < a.n_partials; i += kWarps * 32) sum += a.partials[i];
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = sum;
   __syncthreads();
   if (threadIdx.x != 0) return;
-  for (int w = 1; w < 8; ++w) sum += sh[w];
-  const double norm = sqrt(sum) * fabs((double)a.grad_scale);
-  double clip = 1.0;
-  if (a.max_norm > 0.f) {
-    clip = a.max_norm / (norm + 1e-6);
-    if (clip > 1.0) clip = 1.0;
-  }
+  for (int w = 1; w < kWarps; ++w) sum += sh[w];
+  *norm = sqrt(sum) * fabs((double)a.grad_scale);
+  *clip = a.max_norm > 0.f ? fmin(1.0, a.max_norm / (*norm + 1e-6)) : 1.0;
+  if (*norm != *norm && a.max_norm > 0.f) *clip = *norm;
+}
+__device__ __forceinline__ void write_stats(const PrepareArgs& a, double norm, double clip, bool skip, long long t) {
+  if (!a.stats) return;
+  a.stats[0] = (float)norm;
+  a.stats[1] = (float)clip;
+  a.stats[2] = skip ? 1.f : 0.f;
+  a.stats[3] = (float)t;
+}
+
+// One block.  Two warps raise the betas to the step's number while the others wait for the norm's records.
+__global__ void __launch_bounds__(kWarps * 32) adamw_prepare_kernel(PrepareArgs a) {
+  __shared__ double sh[kWarps], corr[2];
+  const long long taken = *a.step;
+  if (threadIdx.x == 192 || threadIdx.x == 224) corr[threadIdx.x == 224] = correction(threadIdx.x == 224 ? a.beta2 : a.beta1, taken + 1);
+  double norm, clip;
+  norm_and_clip(a, sh, &norm, &clip);
+  if (threadIdx.x != 0) return;
   const bool skip = a.partials && a.skip_nonfinite && !(norm < INFINITY);
   if (!skip) *a.step = taken + 1;
-  Scalars s;
-  s.g_factor = (float)(clip * (double)a.grad_scale);
-  s.lr = a.lr_dev ? *a.lr_dev : a.lr;
-  s.c1 = (float)correction[0];
-  s.c2 = (float)sqrt(correction[1]);
-  s.skip = skip ? 1 : 0;
-  *a.out = s;
-  if (a.stats) {
-    a.stats[0] = (float)norm;
-    a.stats[1] = (float)clip;
-    a.stats[2] = skip ? 1.f : 0.f;
-    a.stats[3] = (float)(taken + (skip ? 0 : 1));
-  }
+  *a.out = {(float)(clip * (double)a.grad_scale), a.lr_dev ? *a.lr_dev : a.lr, (float)corr[0], (float)sqrt(corr[1]), skip ? 1 : 0, taken + 1};
+  write_stats(a, norm, clip, skip, taken + (skip ? 0 : 1));
 }
 
 // The root of eight values.  Within 2^-100 .. 2^100: one step of the residual form of Newton's iteration from the hardware's
@@ -401,11 +419,25 @@ __device__ __forceinline__ void open(const uint4 (&u)[2], bool half, float (&x)[
 }
 
 // The step of the tensors with states of BITS bits.
-template <int BITS>
+// JOIN: each block makes the gradients' factor from the norm's records; else the launch before has left it.
+template <int BITS, bool JOIN>
 __global__ void __launch_bounds__(kWarps * 32, 4) adamw_step_kernel(const __grid_constant__ Table tab, const Hyper h,
-                                                                 const Scalars* __restrict__ scalars) {
-  const Scalars sc = *scalars;
-  if (sc.skip) return;
+                                                                 const Scalars* __restrict__ scalars, const PrepareArgs a) {
+  Scalars sc = *scalars;
+  if constexpr (JOIN) {
+    __shared__ double sh[kWarps];
+    __shared__ float g_factor;
+    double norm, clip;
+    norm_and_clip(a, sh, &norm, &clip);
+    if (threadIdx.x == 0) {
+      g_factor = (float)(clip * (double)a.grad_scale);
+      if (blockIdx.x == 0) write_stats(a, norm, clip, false, sc.t);
+    }
+    __syncthreads();
+    sc.g_factor = g_factor;
+  } else if (sc.skip) {
+    return;
+  }
   for_chunks(tab, 1, [&](const Slot& t, long long e0) {
     if (e0 >= t.n) return;
     const Span s = span_at(t, e0);
@@ -591,28 +623,50 @@ int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, 
   double* partials = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
   const bool norm = ac->max_norm > 0.f || ac->skip_nonfinite;
   Table tab;
-  int n_partials = 0;
+  PrepareArgs pa = {norm ? partials : nullptr, 0, ac->beta1, ac->beta2, ac->lr, ac->max_norm, ac->grad_scale, ac->skip_nonfinite, lr,
+                    reinterpret_cast<long long*>(step), stats, scalars};
+  // Small calls have no launch of their own between norm and step: each block of the step adds the norm's records up itself.
+  long long chunks = 0, live = 0;
+  bool mixed = false;
+  for (int32_t i = 0, bits = 0; i < n_tensors; ++i) {
+    if (tensors[i].n == 0) continue;
+    chunks += (tensors[i].n + kChunk - 1) / kChunk;
+    mixed |= bits && bits != tensors[i].state_bits;
+    bits = tensors[i].state_bits;
+    ++live;
+  }
+  const bool join = norm && !ac->skip_nonfinite && !mixed && live > 0 && live <= kSlots && chunks <= kJoinChunks;
   if (norm) {
     for (int32_t next = 0; next < n_tensors;) {
-      fill(tab, tensors, n_tensors, &next, 0, kSpans);
+      fill(tab, tensors, n_tensors, &next, 0, join ? 1 : kSpans);
       if (tab.count == 0) break;
-      adamw_norm_kernel<<<grid_of(tab, kNormBlocks), kWarps * 32, 0, ctx->stream>>>(tab, partials + n_partials);
-      n_partials += grid_of(tab, kNormBlocks);
+      const int grid = grid_of(tab, kNormBlocks);
+      if (join) adamw_norm_kernel<true><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, partials, pa);
+      else adamw_norm_kernel<false><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, partials + pa.n_partials, pa);
+      pa.n_partials += grid;
       ctx->launches += 1;
     }
   }
-  const PrepareArgs pa = {norm ? partials : nullptr, n_partials, ac->beta1, ac->beta2, ac->lr, ac->max_norm, ac->grad_scale,
-                          ac->skip_nonfinite, lr, reinterpret_cast<long long*>(step), stats, scalars};
-  adamw_prepare_kernel<<<1, 256, 0, ctx->stream>>>(pa);
-  ctx->launches += 1;
+  if (!join) {
+    adamw_prepare_kernel<<<1, kWarps * 32, 0, ctx->stream>>>(pa);
+    ctx->launches += 1;
+  }
   const Hyper h = {(float)ac->beta1, (float)ac->beta2, (float)(1.0 - ac->beta1), (float)(1.0 - ac->beta2), ac->eps};
-  for (const int bits : {8, 32}) {
-    for (int32_t next = 0; next < n_tensors;) {
-      fill(tab, tensors, n_tensors, &next, bits, 1);
-      if (tab.count == 0) break;
-      if (bits == 8) adamw_step_kernel<8><<<grid_of(tab, kMaxBlocks), kWarps * 32, 0, ctx->stream>>>(tab, h, scalars);
-      else adamw_step_kernel<32><<<grid_of(tab, kMaxBlocks), kWarps * 32, 0, ctx->stream>>>(tab, h, scalars);
-      ctx->launches += 1;
+  if (join) {                         // the table is the norm's
+    const int grid = grid_of(tab, kJoinChunks);
+    if (tab.slot[0].flags & kState8) adamw_step_kernel<8, true><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, h, scalars, pa);
+    else adamw_step_kernel<32, true><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, h, scalars, pa);
+    ctx->launches += 1;
+  } else {
+    for (const int bits : {8, 32}) {
+      for (int32_t next = 0; next < n_tensors;) {
+        fill(tab, tensors, n_tensors, &next, bits, 1);
+        if (tab.count == 0) break;
+        const int grid = grid_of(tab, kMaxBlocks);
+        if (bits == 8) adamw_step_kernel<8, false><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, h, scalars, pa);
+        else adamw_step_kernel<32, false><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, h, scalars, pa);
+        ctx->launches += 1;
+      }
     }
   }
   AERO_CUDA_TRY(cudaGetLastError());

@@ -281,3 +281,49 @@ def test_roots_over_all_values(ctx):
     v = (16 * g) * (16 * g) * 0.5
     want = torch.sqrt(v).clamp(min=2.0 ** -100) * torch.tensor(1.0 / 496.0, device="cuda")
     assert torch.equal(t["v_scale"], want)
+
+
+# Chunks are 2048 elements of one tensor; up to 1184 of them in 128 tensors of one kind of states are summed by the step's blocks.
+JOINED = {"one": ([1], 2), "limit": ([1184 * 2048], 2), "beyond": ([1184 * 2048 + 1], 3),
+          "limit, many": ([9 * 2048] * 127 + [41 * 2048 - 5], 2), "empty ones": ([0, 700, 0, 2049] + [0] * 140, 2),
+          "tensors": ([40] * 129, 5)}
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("name", JOINED)
+def test_norm_summed_by_the_step(ctx, name, bits):
+    """Two or three launches leave the same bits: with skip_nonfinite the step has a launch between norm and step.  The gradients
+    are whole numbers below 2^11, so that the sum of their squares is the same in every order."""
+    sizes, launches = JOINED[name]
+    one, two = make(sizes, "bf16", "fp32", bits, True, 21), make(sizes, "bf16", "fp32", bits, True, 21)
+    for a, b in zip(one, two):
+        a["grad"].copy_(torch.randint(-1000, 1001, (a["grad"].numel(),), generator=torch.Generator().manual_seed(22)).float())
+        b["grad"].copy_(a["grad"])
+    steps = [torch.full((1,), 3, dtype=torch.int64, device="cuda") for _ in range(2)]
+    for k in range(2):
+        n = ctx.launch_count()
+        got = ctx.adamw_step(B.adamw_cfg_default(max_norm=0.7, grad_scale=0.25), B.AdamWPlan(one), steps[0])
+        assert ctx.launch_count() - n == launches
+        want = ctx.adamw_step(B.adamw_cfg_default(max_norm=0.7, grad_scale=0.25, skip_nonfinite=1), B.AdamWPlan(two), steps[1])
+        assert torch.equal(got, want) and steps[0].item() == steps[1].item() == 4 + k
+    for a, b in zip(one, two):
+        for key in a:
+            if torch.is_tensor(a[key]):
+                assert torch.equal(a[key].view(torch.uint8), b[key].view(torch.uint8)), key
+
+
+def test_both_kinds_of_states_in_a_small_call(ctx):
+    tensors = make([700, 30], "fp32", "fp32", 32, False, 23) + make([900], "bf16", "bf16", 8, True, 24)
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    step_and_check(ctx, tensors, step, lr=1e-3, max_norm=0.5)
+    step_and_check(ctx, tensors, step, lr=1e-3, max_norm=0.5)
+
+
+@pytest.mark.parametrize("n", [10, 1184 * 2048 + 1])
+def test_nan_gradient_without_skip(ctx, n):
+    """A norm that is NaN makes the clip and so every element NaN, in calls of either number of launches."""
+    tensors = make([n], "fp32", "fp32", 32, False, 25)
+    tensors[0]["grad"][3] = float("nan")
+    stats = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0), B.AdamWPlan(tensors), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    assert torch.isnan(stats[:2]).all() and stats[2:].tolist() == [0.0, 1.0]
+    assert torch.isnan(tensors[0]["param"]).all()
