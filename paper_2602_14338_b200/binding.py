@@ -247,6 +247,7 @@ class AdamWPlan:
 
     _DTYPES = {torch.bfloat16: AERO_BF16, torch.float32: AERO_FP32}
     _KEYS = {"param", "grad", "master", "m", "v", "m_scale", "v_scale", "weight_decay", "lr_scale"}
+    _NEEDED = {"param", "grad", "m", "v"}
 
     def __init__(self, tensors):
         self.tensors = [dict(t) for t in tensors]
@@ -257,6 +258,8 @@ class AdamWPlan:
         for i, t in enumerate(self.tensors):
             if not self._KEYS.issuperset(t):
                 raise AeroError(f"tensor {i}: unknown {sorted(set(t) - self._KEYS)}")
+            if not self._NEEDED.issubset(t):
+                raise AeroError(f"tensor {i}: needs {sorted(self._NEEDED - set(t))}")
             param, m, master = t["param"], t["m"], t.get("master")
             n, bits = param.numel(), 32 if m.dtype == torch.float32 else 8
             checks = [("param", param, n, floats), ("grad", t["grad"], n, floats)]

@@ -167,3 +167,10 @@ def test_binding_refusals():
     for bad in (dict(param=n, grad=n, m=n, v=n), dict(param=n, grad=n, m=n, v=n, lr=1.0)):          # host tensors, an unknown key
         with pytest.raises(B.AeroError):
             B.AdamWPlan([bad])
+
+
+@pytest.mark.parametrize("missing", ["param", "grad", "m", "v"])
+def test_adamw_plan_with_a_tensor_missing(missing):
+    t = {k: torch.zeros(4) for k in ("param", "grad", "m", "v") if k != missing}
+    with pytest.raises(B.AeroError, match=missing):
+        B.AdamWPlan([t])
