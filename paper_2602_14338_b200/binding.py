@@ -251,7 +251,7 @@ class AdamWPlan:
 
     def __init__(self, tensors):
         self.tensors = [dict(t) for t in tensors]
-        self.device = None
+        self.device, self.shapes = None, []
         self.array = (AeroAdamWTensor * max(1, len(self.tensors)))()
         written, index = set(), None
         floats, fp32 = tuple(self._DTYPES), (torch.float32,)
@@ -275,6 +275,7 @@ class AdamWPlan:
                 if param.dtype != torch.bfloat16:
                     raise AeroError(f"tensor {i}: only a bf16 param has a master")
                 checks.append(("master", master, n, fp32))
+            self.shapes.append((n,))
             ptr = {}
             for name, x, size, dtypes in checks:
                 if not x.is_cuda or not x.is_contiguous():
@@ -886,12 +887,17 @@ class Context:
         made, arrays = [], []
         for name, given in (("m", m), ("v", v)):
             if given is None:
-                given = [self._new((t["param"].numel(),), out_dtype) for t in plan.tensors]
+                given = [self._new(shape, out_dtype) for shape in plan.shapes]
             if len(given) != len(plan):
                 raise AeroError(f"{name} must hold {len(plan)} tensors, got {len(given)}")
             made.append(given)
-            arrays.append((C.c_void_p * max(1, len(plan)))(*[
-                self._arg(x, out_dtype, (t["param"].numel(),), f"{name}[{i}]") for i, (x, t) in enumerate(zip(given, plan.tensors))]))
+            index, ptrs = self.device.index, []
+            for i, (x, shape) in enumerate(zip(given, plan.shapes)):        # (a message is made only where something is wrong)
+                if x is None or x.shape != shape or x.dtype != out_dtype or x.get_device() != index or not x.is_contiguous():
+                    self._arg(x, out_dtype, shape, f"{name}[{i}]")
+                    raise AeroError(f"{name}[{i}] must be a CUDA tensor")
+                ptrs.append(x.data_ptr())
+            arrays.append((C.c_void_p * max(1, len(plan)))(*ptrs))
         _check(self.lib.aero_adamw_states(self.h, len(plan), plan.array, AdamWPlan._DTYPES[out_dtype], *arrays), "aero_adamw_states")
         return made[0], made[1]
 
