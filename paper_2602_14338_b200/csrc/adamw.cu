@@ -645,6 +645,7 @@ int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, 
       else adamw_norm_kernel<false><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, partials + pa.n_partials, pa);
       pa.n_partials += grid;
       ctx->launches += 1;
+      if (join) break;                // (all tensors that are not empty: the step runs over the same table)
     }
   }
   if (!join) {
@@ -652,7 +653,7 @@ int aero_adamw_step(aero_ctx* ctx, const aero_adamw_cfg* ac, int32_t n_tensors, 
     ctx->launches += 1;
   }
   const Hyper h = {(float)ac->beta1, (float)ac->beta2, (float)(1.0 - ac->beta1), (float)(1.0 - ac->beta2), ac->eps};
-  if (join) {                         // the table is the norm's
+  if (join) {
     const int grid = grid_of(tab, kJoinChunks);
     if (tab.slot[0].flags & kState8) adamw_step_kernel<8, true><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, h, scalars, pa);
     else adamw_step_kernel<32, true><<<grid, kWarps * 32, 0, ctx->stream>>>(tab, h, scalars, pa);

@@ -327,3 +327,24 @@ def test_nan_gradient_without_skip(ctx, n):
     stats = ctx.adamw_step(B.adamw_cfg_default(max_norm=1.0), B.AdamWPlan(tensors), torch.zeros(1, dtype=torch.int64, device="cuda"))
     assert torch.isnan(stats[:2]).all() and stats[2:].tolist() == [0.0, 1.0]
     assert torch.isnan(tensors[0]["param"]).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("behind", [1, 5, 200])
+def test_empty_tensors_behind_a_full_launch(ctx, bits, behind):
+    """As many tensors as a launch takes, and empty ones behind them: both launches of the call run over the same tensors."""
+    sizes = [40] * 128 + [0] * behind
+    one, two = make(sizes, "bf16", "fp32", bits, True, 31), make(sizes, "bf16", "fp32", bits, True, 31)
+    for a, b in zip(one, two):
+        a["grad"].copy_(torch.randint(-1000, 1001, (a["grad"].numel(),), generator=torch.Generator().manual_seed(32)).float())
+        b["grad"].copy_(a["grad"])
+    steps = [torch.full((1,), 3, dtype=torch.int64, device="cuda") for _ in range(2)]
+    n = ctx.launch_count()
+    got = ctx.adamw_step(B.adamw_cfg_default(max_norm=0.7), B.AdamWPlan(one), steps[0])
+    assert ctx.launch_count() - n == 2
+    want = ctx.adamw_step(B.adamw_cfg_default(max_norm=0.7, skip_nonfinite=1), B.AdamWPlan(two), steps[1])
+    assert torch.equal(got, want) and steps[0].item() == steps[1].item() == 4
+    for a, b in zip(one, two):
+        for key in a:
+            if torch.is_tensor(a[key]):
+                assert torch.equal(a[key].view(torch.uint8), b[key].view(torch.uint8)), key
