@@ -1,6 +1,8 @@
 // One AdamW step over many tensors.  Per element, with g' = grad_scale clip g and t the number of this step:
 //   m = beta1 m + (1 - beta1) g',   v = beta2 v + (1 - beta2) g'^2
-//   p = (1 - lr wd) p - lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+//   p = p - (lr wd p + lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps))
+// (1 - lr wd as a factor of p would be rounded to a multiple of 2^-24 first: at lr = 1e-6 a decay of 0.1 would become one of 0.119 and
+// one of 0.01 none at all, in every element and step.)
 // m and v are fp32, or 8 bits an element with a scale per 256 elements: m as e4m3, the root of v as an unsigned float of
 // four exponent and four mantissa bits (v spans twice as many octaves as m; its root fits the same range, and the sign's bit
 // goes to the mantissa).  The step itself uses the fp32 values before they are rounded.  Bound by memory: 28 bytes an element
@@ -462,7 +464,7 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_step_kernel(const __grid
         load32(static_cast<const float*>(t.v), s, v);
       }
     }
-    const float lr = sc.lr * t.lr_scale, keep = 1.f - lr * t.weight_decay, rate = lr * sc.c1;
+    const float lr = sc.lr * t.lr_scale, decay = lr * t.weight_decay, rate = lr * sc.c1;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const float x = __fmul_rn(g[i], sc.g_factor);
@@ -472,12 +474,20 @@ __global__ void __launch_bounds__(kWarps * 32, 4) adamw_step_kernel(const __grid
       v[i] = __fadd_rn(__fmul_rn(h.beta2, v[i]), __fmul_rn(__fmul_rn(h.rest2, x), x));
     }
     roots(v, r);
+    float top = 0.f, step[kEach];
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       float inv;
       asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(fmaf(r[i], sc.c2, h.eps)));
-      p[i] = fmaf(keep, p[i], -rate * m[i] * inv);
+      step[i] = fmaf(decay, p[i], rate * m[i] * inv);
+      top = fmaxf(top, fabsf(p[i]));
     }
+    if (top == INFINITY) {                // infinity less a part of itself would be NaN: only an m that is no number changes it
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) step[i] = fabsf(p[i]) == INFINITY ? 0.f * m[i] : step[i];
+    }
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) p[i] -= step[i];
     if (t.master) store32(t.master, s, p);
     store(t.param, half, s, p);
     if (BITS == 8) {

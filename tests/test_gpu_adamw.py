@@ -348,3 +348,61 @@ def test_empty_tensors_behind_a_full_launch(ctx, bits, behind):
         for key in a:
             if torch.is_tensor(a[key]):
                 assert torch.equal(a[key].view(torch.uint8), b[key].view(torch.uint8)), key
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("decay", [0.01, 0.1])
+def test_weight_decay_at_small_learning_rates(ctx, bits, decay):
+    """lr weight_decay of 1e-8 and 1e-7, below what 1 - lr weight_decay can hold in fp32: the mean of many masters still falls by
+    it.  A step's rounding of p in [0.5, 1) is 2^-25 at most, to either side as the step's other part (lr times a number that differs
+    from element to element) decides: over 100 steps of 2^18 elements its mean has a deviation below 2^-25 10 / 512, 6e-10; the step
+    itself is off by 16 u of lr, 1e-10 in all.  What is looked for is 7e-7 and more; 2 % of it is allowed."""
+    n, steps, lr = 2 ** 18, 100, float(np.float32(1e-6))
+    wd = float(np.float32(decay))
+    g = torch.Generator(device="cuda").manual_seed(41)
+    t = dict(param=torch.zeros(n, dtype=torch.bfloat16, device="cuda"), grad=torch.zeros(n, device="cuda"), weight_decay=decay,
+             master=0.5 + 0.5 * torch.rand(n, generator=g, device="cuda"))
+    if bits == 32:
+        t["m"], t["v"] = torch.randn(n, generator=g, device="cuda") * 0.1, 0.5 + torch.rand(n, generator=g, device="cuda")
+    else:
+        t["m"] = (torch.randn(n, generator=g, device="cuda") * 40).to(torch.float8_e4m3fn)
+        t["v"] = torch.randint(160, 192, (n,), generator=g, device="cuda").to(torch.uint8)
+        t["m_scale"], t["v_scale"] = torch.full((n // 256,), 1 / 400, device="cuda"), torch.full((n // 256,), 1 / 20, device="cuda")
+    step = torch.full((1,), 1000, dtype=torch.int64, device="cuda")
+    plan, ac = B.AdamWPlan([t]), B.adamw_cfg_default(lr=lr, beta2=0.99)
+    eps = float(np.float32(1e-8))
+    want = t["master"].double()
+    for k in range(1001, 1001 + steps):
+        t["grad"].copy_(torch.randn(n, generator=g, device="cuda"))
+        if bits == 32:
+            m, v = t["m"].double(), t["v"].double()
+        else:
+            each = lambda s: s.double().repeat_interleave(256)  # noqa: E731
+            m = t["m"].double() * each(t["m_scale"])
+            v = (torch.from_numpy(M.E4M4).cuda()[t["v"].long()] * each(t["v_scale"])) ** 2
+        m = 0.9 * m + (1 - 0.9) * t["grad"].double()
+        v = 0.99 * v + (1 - 0.99) * t["grad"].double() ** 2
+        want = (1 - lr * wd) * want - lr * (m / (1 - 0.9 ** k)) / ((v / (1 - 0.99 ** k)).sqrt() + eps)
+        ctx.adamw_step(ac, plan, step)
+    off = (t["master"].double() - want).mean().item()
+    assert abs(off) <= 0.02 * steps * lr * wd * 0.75, off / (steps * lr * wd * 0.75)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("decay", [0.0, 0.1])
+def test_infinite_parameters_stay(ctx, bits, decay):
+    """A parameter of -inf (a logit's bias that masks a token) stays what it is, with decay and without; so does a NaN."""
+    tensors = make([600, 1], "fp32", "fp32", bits, False, 42)
+    for t in tensors:
+        t["weight_decay"] = decay
+    tensors[0]["param"][[3, 300]] = torch.tensor([float("-inf"), float("inf")], device="cuda")
+    tensors[0]["param"][400] = float("nan")
+    tensors[1]["param"][0] = float("-inf")
+    ctx.adamw_step(B.adamw_cfg_default(lr=1e-2), B.AdamWPlan(tensors), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    p = tensors[0]["param"]
+    assert p[3].item() == float("-inf") and p[300].item() == float("inf") and tensors[1]["param"].item() == float("-inf")
+    bad = ~torch.isfinite(p)
+    assert torch.isnan(p[400]) and bad.sum().item() == 3
+    tensors[1]["grad"][0] = float("nan")
+    ctx.adamw_step(B.adamw_cfg_default(lr=1e-2), B.AdamWPlan(tensors), torch.ones(1, dtype=torch.int64, device="cuda"))
+    assert torch.isnan(tensors[1]["param"][0]) and p[3].item() == float("-inf")
