@@ -482,6 +482,7 @@ __global__ void __launch_bounds__(THREADS, 1) fp4_rows_kernel(const Params p) {
     for (int b = b0; ok && b < b1; b += step(b)) {
       for (int kb = 0; kb < nkb; kb += per) {
         if (!__all_sync(0xffffffffu, tc::mbar_wait(&ctl->full[s], ph, abort_flag))) { ok = false; break; }
+        tc::tc_fence_after();                    // the products of the ring's turn before have read these columns
         const int nk = min(per, nkb - kb);
         for (int k = 0; k < nk; ++k) {
           const uint8_t* from = smem + (size_t)(s * per + k) * slab_bytes + kTileBytes + b_slab;

@@ -189,3 +189,24 @@ def test_captured_on_another_stream_beside_another_call(ctx, T):
     assert own.last_status() == 0
     del graph
     own.close()
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("T", [1, 33, 128])
+def test_scales_that_change_from_slab_to_slab(ctx, T, block):
+    """A row of many slabs whose scales differ by powers of two from one slab of 256 columns to the next, up to 2^7 and back: a slab
+    multiplied with scales of another one would be off by its whole size.  Several turns of the ring, many rows of W for each CTA."""
+    d, V = 256 * 40, 148 * 160
+    cfg = cfg_of("bf16")
+    g = torch.Generator(device="cuda").manual_seed(9)
+    size = torch.exp2(((torch.arange(d, device="cuda") // 256 * 5) % 8).float())
+    h = (torch.randn(T, d, generator=g, device="cuda") * size).bfloat16()
+    w = (torch.randn(V, d, generator=g, device="cuda") * size.flip(0)).bfloat16()
+    hr, wr = ctx.quantize_fp4(cfg, h, block=block), ctx.quantize_fp4(cfg, w, block=block)
+    a, b = ctx.dequantize_fp4(hr, torch.float32), ctx.dequantize_fp4(wr, torch.float32)
+    got = ctx.lmhead_fp4(hr, wr, out_dtype=torch.float32)
+    again = ctx.lmhead_fp4(hr, wr, out_dtype=torch.float32)
+    assert torch.equal(got, again)
+    for v in range(0, V, 4736):
+        part = b[v:v + 4736].double()
+        check_product(got[:, v:v + 4736].double(), a.double() @ part.T, a.double().abs() @ part.abs().T, d, torch.float32)
