@@ -303,7 +303,7 @@ class AdamWPlan:
 
 class Fp4Rows:
     """rows x cols values in 4-bit floating point, in the layout that include/aero.h describes: codes and scales (uint8) and, for
-    block 16, row_scale [rows] f32.  The buffers are made unless given (on `device`)."""
+    block 16, row_scale [rows] f32.  The buffers are given, all of them, or made (on `device`)."""
 
     def __init__(self, rows, cols, block=16, codes=None, scales=None, row_scale=None, device=None):
         if block not in (16, 32):
@@ -312,6 +312,10 @@ class Fp4Rows:
             raise AeroError(f"rows must be at least 0 and cols a multiple of 32, got {rows} x {cols}")
         if block == 32 and row_scale is not None:
             raise AeroError("block 32 has no row_scale")
+        parts = {"codes": codes, "scales": scales, **({"row_scale": row_scale} if block == 16 else {})}
+        missing = [name for name, given in parts.items() if given is None]
+        if 0 < len(missing) < len(parts):
+            raise AeroError(f"some of the buffers are given without {' and '.join(missing)}")
         self.rows, self.cols, self.block = rows, cols, block
         tiles = -(-rows // 128) * -(-cols // 256)              # aero_fp4_code_bytes, aero_fp4_scale_bytes
         for name, given, dtype, numel in (("codes", codes, torch.uint8, tiles * 16384), ("scales", scales, torch.uint8, tiles * 32768 // block),

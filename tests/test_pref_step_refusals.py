@@ -174,3 +174,16 @@ def test_adamw_plan_with_a_tensor_missing(missing):
     t = {k: torch.zeros(4) for k in ("param", "grad", "m", "v") if k != missing}
     with pytest.raises(B.AeroError, match=missing):
         B.AdamWPlan([t])
+
+
+@pytest.mark.parametrize("block", [16, 32])
+def test_fp4_rows_of_a_part_of_the_buffers(block):
+    """Buffers are given all together or not at all: one that is missing would be filled with whatever the memory holds."""
+    r = B.Fp4Rows(4, 64, block, device="meta")
+    parts = dict(codes=r.codes, scales=r.scales)
+    if block == 16:
+        parts["row_scale"] = r.row_scale
+    for name in parts:
+        some = {k: x for k, x in parts.items() if k != name}
+        with pytest.raises(B.AeroError, match=f"without {name}"):
+            B.Fp4Rows(4, 64, block, device="meta", **some)
