@@ -690,7 +690,8 @@ int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* p
  *   p = (1 - lr_i weight_decay_i) p - lr_i (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),   lr_i = lr lr_scale_i
  * (lr_i weight_decay_i p and the rest are added up before p is rounded, so that decays below what 1 - lr_i weight_decay_i can hold
  * in fp32 still count; an infinite p stays infinite).
- * Tensors are described by an array in HOST memory, which is read before the call returns; no tensor may occur twice.
+ * Tensors are described by an array in HOST memory, which is read before the call returns; what is written (all but grad) shares no
+ * memory with any other array of the call, gradients among them.
  *   param [n] bf16 or fp32, updated in place; with master [n] f32 (bf16 parameters only) the master is updated and param
  *   is its rounding, without it a bf16 param is rounded after each step.  grad [n] bf16 or fp32, read only.
  *   state_bits 32: m, v [n] f32.

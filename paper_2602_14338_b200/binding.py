@@ -242,8 +242,8 @@ def pref_cfg_default(**over) -> AeroPrefCfg:
 class AdamWPlan:
     """The tensors of Context.adamw_step, checked and described once: a list of dicts with param, grad, m and v and, where they
     apply, master (fp32 master of a bf16 param), m_scale and v_scale (8-bit states), weight_decay (0) and lr_scale (1).  States
-    are fp32, or m in torch.float8_e4m3fn and v in torch.uint8 with a scale per 256 elements.  The plan keeps the tensors; a
-    program whose gradients move makes another one."""
+    are fp32, or m in torch.float8_e4m3fn and v in torch.uint8 with a scale per 256 elements.  What the step writes shares no memory with
+    anything else in the plan; gradients may share theirs.  The plan keeps the tensors; a program whose gradients move makes another one."""
 
     _DTYPES = {torch.bfloat16: AERO_BF16, torch.float32: AERO_FP32}
     _KEYS = {"param", "grad", "master", "m", "v", "m_scale", "v_scale", "weight_decay", "lr_scale"}
@@ -253,7 +253,7 @@ class AdamWPlan:
         self.tensors = [dict(t) for t in tensors]
         self.device, self.shapes = None, []
         self.array = (AeroAdamWTensor * max(1, len(self.tensors)))()
-        written, index = set(), None
+        ranges, index = [], None
         floats, fp32 = tuple(self._DTYPES), (torch.float32,)
         for i, t in enumerate(self.tensors):
             if not self._KEYS.issuperset(t):
@@ -278,24 +278,37 @@ class AdamWPlan:
             self.shapes.append((n,))
             ptr = {}
             for name, x, size, dtypes in checks:
-                if not x.is_cuda or not x.is_contiguous():
-                    raise AeroError(f"tensor {i}: {name} must be a contiguous CUDA tensor")
-                if x.dtype not in dtypes:
-                    raise AeroError(f"tensor {i}: {name} must have dtype {' or '.join(map(str, dtypes))}, got {x.dtype}")
-                if x.numel() != size:
-                    raise AeroError(f"tensor {i}: {name} must have {size} elements, got {x.numel()}")
-                if index is None:
-                    self.device, index = x.device, x.get_device()
-                if x.get_device() != index:
-                    raise AeroError(f"tensor {i}: {name} is on {x.device}, others on {self.device}")
+                if x.get_device() != index or x.dtype not in dtypes or x.numel() != size or not x.is_contiguous():
+                    if not x.is_cuda or not x.is_contiguous():
+                        raise AeroError(f"tensor {i}: {name} must be a contiguous CUDA tensor")
+                    if x.dtype not in dtypes:
+                        raise AeroError(f"tensor {i}: {name} must have dtype {' or '.join(map(str, dtypes))}, got {x.dtype}")
+                    if x.numel() != size:
+                        raise AeroError(f"tensor {i}: {name} must have {size} elements, got {x.numel()}")
+                    if index is None:
+                        self.device, index = x.device, x.get_device()
+                    else:
+                        raise AeroError(f"tensor {i}: {name} is on {x.device}, others on {self.device}")
                 ptr[name] = p = x.data_ptr()
-                if size and name != "grad":
-                    if p in written:
-                        raise AeroError(f"tensor {i}: {name} occurs twice")
-                    written.add(p)
+                ranges.append((p, p + size * x.itemsize, i, name))
             self.array[i] = AeroAdamWTensor(n, ptr["param"], ptr["grad"], ptr.get("master"), ptr["m"], ptr["v"], ptr.get("m_scale"),
                                             ptr.get("v_scale"), self._DTYPES[param.dtype], self._DTYPES[t["grad"].dtype], bits,
                                             t.get("weight_decay", 0.0), t.get("lr_scale", 1.0))
+        self._check_apart(ranges)
+
+    @staticmethod
+    def _check_apart(ranges):
+        """Refuses ranges (first address, end, tensor, name) that share an address, unless both are gradients', which are not written."""
+        last = last_written = (0, 0)                   # of the ranges so far, and of those that are written, the one that ends last
+        for r in sorted(ranges):
+            writes = r[3] != "grad"
+            other = last if writes else last_written
+            if r[0] < other[1] and r[0] < r[1]:
+                raise AeroError(f"tensor {r[2]}: {r[3]} and {other[3]} of tensor {other[2]} overlap")
+            if r[1] > last[1]:
+                last = r
+            if writes and r[1] > last_written[1]:
+                last_written = r
 
     def __len__(self):
         return len(self.tensors)

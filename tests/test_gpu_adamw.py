@@ -406,3 +406,18 @@ def test_infinite_parameters_stay(ctx, bits, decay):
     tensors[1]["grad"][0] = float("nan")
     ctx.adamw_step(B.adamw_cfg_default(lr=1e-2), B.AdamWPlan(tensors), torch.ones(1, dtype=torch.int64, device="cuda"))
     assert torch.isnan(tensors[1]["param"][0]) and p[3].item() == float("-inf")
+
+
+def test_plan_of_overlapping_tensors():
+    """Slices that share elements, a gradient that is written or shares elements with what is: refused; neighbours and shared gradients are not."""
+    f = lambda n: torch.zeros(n, device="cuda")  # noqa: E731
+    base, grads = f(100), f(100)
+    t = lambda p, g, m=None, **over: dict(param=p, grad=g, m=m if m is not None else f(p.numel()), v=f(p.numel()), **over)  # noqa: E731
+    B.AdamWPlan([t(base[:50], grads[:50]), t(base[50:], grads[:50])])
+    for bad in ([t(base[:51], grads[:51]), t(base[50:], grads[50:])],                 # slices with an element in common
+                [t(base[:50], base[50:])] + [t(base[99:], grads[:1])],                # a gradient with an element that is a parameter's
+                [t(base[:50], base[:50])],                                            # a gradient that is its parameter
+                [t(base[:50], grads[:50], m=base[25:75])],                            # a state over the parameter
+                [t(base[:50], grads[:50], m=grads[50:]), t(base[50:], grads[50:])]):  # a state that is another tensor's gradient
+        with pytest.raises(B.AeroError, match="overlap|twice"):
+            B.AdamWPlan(bad)

@@ -187,3 +187,19 @@ def test_fp4_rows_of_a_part_of_the_buffers(block):
         some = {k: x for k, x in parts.items() if k != name}
         with pytest.raises(B.AeroError, match=f"without {name}"):
             B.Fp4Rows(4, 64, block, device="meta", **some)
+
+
+def test_adamw_plan_arrays_that_share_memory():
+    """Ranges [first, end) of addresses: those that are written touch no other, those that are read may share."""
+    def check(written, read):
+        B.AdamWPlan._check_apart(written + read)
+
+    a, b, c = (100, 200, 0, "param"), (200, 240, 0, "m"), (240, 300, 1, "v")
+    check([a, b, c], [(300, 400, 0, "grad"), (300, 400, 1, "grad"), (350, 360, 2, "grad"), (0, 100, 3, "grad")])
+    check([], [])
+    check([a], [(100, 100, 1, "grad"), (150, 150, 1, "grad")])                        # nothing in them
+    for written, read in (([a, (199, 201, 1, "param")], []), ([a, a], []), ([a, (100, 300, 1, "v"), c], []), ([a], [(150, 160, 0, "grad")]),
+                          ([a, b], [(0, 101, 0, "grad")]), ([a, b], [(239, 900, 0, "grad")]), ([(0, 1000, 0, "param"), (10, 20, 1, "m")], []),
+                          ([a, c], [(0, 1000, 0, "grad"), (500, 600, 1, "grad")]), ([c], [(0, 1000, 0, "grad"), (20, 30, 1, "grad")])):
+        with pytest.raises(B.AeroError, match="overlap"):
+            check(written, read)
