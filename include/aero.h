@@ -629,7 +629,8 @@ int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t*
  *          (ref_logp NULL: no reference; no scored token: 0)
  *   m_p  = beta (r_chosen - r_rejected) - margin,   (chosen, rejected) = pairs[p]
  *   loss = sum_p u_p l(m_p),   u_p = pair_weight[p], or 1 / (number of pairs that count) with pair_weight NULL
- *     AERO_PREF_LOGISTIC  l = (1 - s) log(1 + exp(-m)) + s log(1 + exp(m)),   s = label_smoothing
+ *     AERO_PREF_LOGISTIC  l = (1 - s) log(1 + exp(-m)) + s log(1 + exp(m)),   s = label_smoothing (a part whose factor is 0 counts
+ *                         nothing, also where m is infinite)
  *     AERO_PREF_SQUARE    l = (m - 1/2)^2
  *     AERO_PREF_HINGE     l = max(0, 1 - m)     (slope 0 at m = 1)
  *   coef_i = d loss / d logp_t of each scored token of rollout i

@@ -308,7 +308,8 @@ __device__ __forceinline__ void pair_term(const PrefArgs& a, int p, int n, doubl
     if (a.kind == AERO_PREF_LOGISTIC) {
       const double e = exp(-fabs(m)), s = log1p(e);                  // softplus(-|m|)
       const double down = m > 0.0 ? e / (1.0 + e) : 1.0 / (1.0 + e); // sigmoid(-m)
-      l = (1.0 - a.smoothing) * (fmax(-m, 0.0) + s) + a.smoothing * (fmax(m, 0.0) + s);
+      // (a part without weight counts nothing, also where the margin is infinite)
+      l = (a.smoothing < 1.0 ? (1.0 - a.smoothing) * (fmax(-m, 0.0) + s) : 0.0) + (a.smoothing > 0.0 ? a.smoothing * (fmax(m, 0.0) + s) : 0.0);
       if (m != m) l = m;                                             // (fmax would drop it)
       slope = a.smoothing * (1.0 - down) - (1.0 - a.smoothing) * down;
     } else if (a.kind == AERO_PREF_SQUARE) {

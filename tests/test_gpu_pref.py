@@ -311,3 +311,32 @@ def test_a_preference_step_together(ctx):
         assert torch.equal(state["param"], state["master"].bfloat16())
         losses.append(out["loss"].item())
     assert np.isfinite(losses).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("smoothing", [0.0, 0.25, 1.0])
+def test_infinite_margins(ctx, dtype, sign, smoothing):
+    """A reference that gives a token no probability at all makes its rollout's log ratio infinite.  A part of the loss whose factor is 0
+    (the second one without smoothing, the first with smoothing 1) adds nothing then either; coef is the slope's limit."""
+    b = batch(60, 64, 300, [0, 20, 40, 60], [(0, 1), (1, 2)], dtype, seed=8)
+    b["y"][3] = 7
+    b["ref"][3] = -float("inf")
+    if sign < 0:
+        b["pairs"] = b["pairs"].flip(1).contiguous()
+    pc = B.pref_cfg_default(label_smoothing=smoothing)
+    out, dH, dW = ctx.pref_fwd_bwd(cfg_of(dtype), pc, *args(b), ref_logp=b["ref"])
+    two = ctx.pref_fwd(cfg_of(dtype), pc, *args(b), ref_logp=b["ref"])
+    other = out["margin"][1].double().cpu().numpy()
+    each, slope = M.pref_pair("logistic", other, smoothing)
+    weight = smoothing if sign > 0 else 1 - smoothing                                 # of the part that is infinite
+    loss = 0.5 * each if weight == 0 else float("inf")
+    beta = float(np.float32(0.1))
+    for got in (out, two):
+        assert got["margin"][0].item() == sign * float("inf")
+        assert got["loss"].item() == loss or abs(got["loss"].item() - loss) <= 2.0 ** -22 * abs(loss)
+        first = 0.5 * beta * (smoothing if sign > 0 else smoothing - 1)               # d loss / d r_chosen of the pair
+        want = np.array([first, 0.5 * beta * slope - first, -0.5 * beta * slope]) if sign > 0 else \
+            np.array([-first, first - 0.5 * beta * slope, 0.5 * beta * slope])
+        assert np.abs(f64(got["coef"]) - want).max() <= 2.0 ** -22
+    assert torch.isfinite(dH.float()).all() and torch.isfinite(dW).all()
