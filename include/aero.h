@@ -647,6 +647,9 @@ int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t*
  * whose coef is 0 are left out).  aero_pref_fwd_bwd does not recompute them (6 d V) if the workspace holds all rows in one chunk, since
  * a row's gradient needs the log-probs of all rows of its pairs; else it takes the two calls' passes.  cfg->dtype and d as in
  * aero_distill_fwd; precision as there, with sums over rollouts and pairs in 64 bits; all sums have a fixed order.
+ * logp has no mean error that would add up over a rollout's tokens, as that of the other calls has (5e-6 a token at d = 3584, from the
+ * tensor cores' accumulation); a reference of this library is therefore best scored by aero_pref_fwd too (P = 0 pairs would leave all
+ * rows out: name each rollout in a pair, with itself if need be).
  * workspace: at least the matching *_workspace_bytes, 256-byte aligned.
  */
 #define AERO_PREF_LOGISTIC 0

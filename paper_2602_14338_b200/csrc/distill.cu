@@ -1072,9 +1072,9 @@ int lmhead_launch(const Call& c, const Ws& s, lmhead::Params p, const CUtensorMa
   p.w_hint = aero_w_hint(ctx, mode != kFwd); p.k_zigzag = aero_k_zigzag(ctx);
   auto kern = mode == kFwd ? lmhead::lmhead_kernel<lmhead::MODE_FWD>
                            : (mode == kBoth ? lmhead::lmhead_kernel<lmhead::MODE_FWD_P> : lmhead::lmhead_kernel<lmhead::MODE_DZ>);
-  if (c.ex.gain && mode != kBwd) {
+  if (c.ex.z_gain && mode != kBwd) {
     kern = mode == kFwd ? lmhead::lmhead_kernel<lmhead::MODE_FWD_GAIN> : lmhead::lmhead_kernel<lmhead::MODE_FWD_P_GAIN>;
-    p.z_gain = lmhead::kCut * (float)(c.d / 16);
+    p.z_gain = c.ex.z_gain;
   }
   AERO_CUDA_TRY(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)lmhead::SMEM_BYTES));
   const int pairs = ctx->sm_count / 2 > 0 ? ctx->sm_count / 2 : 1;

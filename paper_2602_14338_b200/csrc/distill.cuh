@@ -5,7 +5,7 @@
 #include "common.cuh"
 
 struct AeroListed {
-  bool gain = false;                    // log-probs with lmhead::Params::z_gain
+  const float* z_gain = nullptr;        // bf16 rows: log-probs with lmhead::Params::z_gain [T]
   // K = 1, every row of the kept rollouts with a token in [0,V): its logit, an fp32 dot product [T], and the rows' weights [T] in place
   // of w; the passes that make these (and the outputs of rows that no kept rollout owns) are left out.
   const float* z = nullptr;

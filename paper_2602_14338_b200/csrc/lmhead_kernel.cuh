@@ -54,7 +54,7 @@ constexpr int BM = 128, BN = 256, BNH = BN / 2, BK = 64, STAGES = AERO_LMHEAD_ST
 constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = BNH * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int THREADS = 192;
 // bit 0: dz mode, bit 1: entropy term, bit 2: the forward also stores exp(z - c_t) of the chunk (see MODE_FWD_P)
-// bit 3: the forward takes the logits times 1 + z_gain
+// bit 3: the forward takes a row's logits times 1 + z_gain
 constexpr int MODE_FWD = 0, MODE_DZ = 1, MODE_FWD_ENT = 2, MODE_DZ_ENT = 3, MODE_FWD_P = 4, MODE_FWD_P_ENT = 6;
 constexpr int MODE_FWD_GAIN = 8, MODE_FWD_P_GAIN = 12;
 constexpr float kShiftMargin = 40.f;   // c_t = (largest logit of the row's first 32 columns) + this margin
@@ -63,7 +63,6 @@ constexpr float kShiftMargin = 40.f;   // c_t = (largest logit of the row's firs
 constexpr float kMasked = -0x1p100f;
 constexpr float kMaskedMax2 = -0x1p99f;   // a running maximum below this (log2 domain) has seen masked columns only
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr float kCut = 1.55e-8f;          // see Params::z_gain
 
 struct Ctl {
   uint64_t full[STAGES], empty[STAGES], tfull[2], tempty[2];
@@ -130,11 +129,8 @@ struct Params {
   int* range_count;
   unsigned int* range_seen;     // bit per chunk-local row: already listed (cleared with the count)
   int range_cap;
-  // _GAIN modes.  Each product of 16 terms is added to the accumulator with what does not fit its 24 bits cut off, towards
-  // zero: a sum of d / 16 of them comes out short by about d / 16 times kCut of itself, whatever its sign, and log-sum-exp
-  // with it (kCut from the mean error of log-probs of normal H and W: 1.60e-8 at d = 1536, 1.53e-8 at d = 3584).  A token's log-prob
-  // has an error of 1e-6 to 5e-6 from it, which matters only where the log-probs of a whole rollout are added up.
-  float z_gain;
+  // _GAIN modes: per row, what its logits are multiplied by, less one, for what the tensor cores' accumulation has cut off.
+  const float* z_gain;
   double* partials;             // [tile][4 epilogue warps][kPartialStride]
   // dz modes
   const float* lse_in;
@@ -251,7 +247,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1)
 lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ CUtensorMap tmW,
               const __grid_constant__ CUtensorMap tmDZ, const Params p) {
   constexpr bool IS_DZ = (MODE & 1) != 0, ENT = (MODE & 2) != 0, STORE_P = (MODE & 4) != 0, GAIN = (MODE & 8) != 0;
-  const float z_log2e = GAIN ? kLog2e * (1.f + p.z_gain) : kLog2e;      // log2 domain of the running sums
   constexpr bool STORES = IS_DZ || STORE_P;       // the epilogue writes a tile of the chunk's block
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -397,6 +392,7 @@ lmhead_kernel(const __grid_constant__ CUtensorMap tmH, const __grid_constant__ C
       const bool bad_y = valid_row && (yt < 0 || yt >= p.V);
       if (bad_y) { aero_raise(p.status, AERO_ST_BAD_TARGET); yt = -1; }
       const bool live = valid_row && !bad_y;
+      const float z_log2e = GAIN && live ? kLog2e * (1.f + p.z_gain[row]) : kLog2e;      // log2 domain of the running sums
 
       float m2 = -INFINITY, l = 0.f, zy = 0.f, sz = 0.f;   // forward running state (log2 domain); sz = sum e^(z-m) z
       float c2 = 0.f;                                      // MODE_FWD_P: shift of the stored exponentials, log2 domain

@@ -52,6 +52,7 @@ struct PrefArgs {
   float* ones;                    // [T] 1
   float* zeros;                   // [T] 0: the listed tokens' teacher logits
   float* zg;                      // [T] logits of the rows' targets
+  float* gain;                    // [T] forward of bf16 rows: factors of the rows' logits, less one
   float grad_scale;
   const void* W;
   double* r;                      // [R] log ratios
@@ -206,6 +207,50 @@ __global__ void __launch_bounds__(kPlanThreads) pref_plan_kernel(PrefArgs a) {
   else list_rows<32>(a);
 }
 
+// Each product of 16 terms is added to the accumulator with what does not fit its 24 bits cut off, towards zero.  A dense sum of
+// d / 16 of them comes out short by about d / 16 times kCut of itself, on average, and log-sum-exp with it: a token's log-prob has an
+// error of 1e-6 to 5e-6 from it, which matters only where the log-probs of a whole rollout are added up.  kCut is a fit to the mean
+// error of log-probs of normal H and W (1.60e-8 at d = 1536, 1.53e-8 at d = 3584), not a bound: dense inputs of other
+// distributions need 1.48e-8 to 1.72e-8.  Walking d both ways (k_zigzag) makes it hold wherever along d the large columns are; sums of
+// fewer or shorter terms lose less (CutOff).
+constexpr float kCut = 1.55e-8f;
+// How much a sum of these products of 16 loses to the tensor cores' accumulation, against a dense sum: the products of a row of H and
+// its target's row of W are added up in steps of 16 as the tensor cores do, with what falls below the 24 bits of each partial sum counted.
+// In dense rows that is 2.4e-8 to 4.4e-8 of the partial sums (normal, shifted, heavy-tailed, d = 1536 and 3584); in rows of which one
+// column in 16, or 16 in 128, is not zero 2.5e-9 to 3.2e-9, where log-sum-exp loses as much less; of whole numbers 0.  A step that is
+// below the accumulator's last two bits is dropped whole, before it is added.  (Mean error of a log-prob in such rows, d = 1536 and 3584:
+// as if they were dense 1.7e-6 and 4.4e-6, with no correction -2e-7 to -6e-7, with this one at most 1.2e-7.)
+constexpr float kDenseLoss = 1.7e-8f;
+struct CutOff {
+  float carry = 0.f, lost = 0.f, size = 0.f;
+  // s: the sum of 8 neighbouring products, if there are any; a pair of lanes has a step's 16
+  __device__ void add(float s, bool any, int lane) {
+    s += __shfl_xor_sync(0xffffffffu, s, 1);
+    float v = s;
+#pragma unroll
+    for (int o = 2; o < 32; o <<= 1) {
+      const float u = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v += u;
+    }
+    const float up = __shfl_up_sync(0xffffffffu, v, 2);
+    const float before = carry + (lane >= 2 ? up : 0.f), sum = __fadd_rz(before, s);
+    const bool falls = fabsf(before) >= fabsf(s);
+    const float rest = falls ? s - (sum - before) : before - (sum - s);
+    if (fabsf(s) > 0x1p-25f * fabsf(before)) lost += fabsf(rest);
+    if (any) size += fabsf(sum);
+    carry += __shfl_sync(0xffffffffu, v, 31);
+  }
+  // (a row without products to look at: as dense)
+  __device__ float gain(int d) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      lost += __shfl_xor_sync(0xffffffffu, lost, o);
+      size += __shfl_xor_sync(0xffffffffu, size, o);
+    }
+    return kCut * (float)(d / 16) * fminf(lost / (size * kDenseLoss), 1.f);
+  }
+};
+
 // A warp per row.  GATHER: the row of H into the run, its target with the target's logit and, for the backward alone, lse and
 // weight; else the run's row of dH to its own.
 template <typename T, bool GATHER>
@@ -222,18 +267,28 @@ __global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, T* dH) {
     const int v = GATHER ? a.y[t] : 0;
     const T* w = static_cast<const T*>(a.W) + (long long)v * d;
     float z = 0.f;
+    CutOff cut;
+    const bool watch = GATHER && sizeof(T) == 2 && !a.backward;
     const auto part = [&](auto vec) {
       constexpr int VEC = decltype(vec)::value;
 #pragma unroll 4
-      for (int e = lane * VEC; e < d; e += 32 * VEC) {
-        float x[VEC], y[VEC];
-        rowvec::load<T, VEC>(from + e, x);
-        if (GATHER) {
-          rowvec::load<T, VEC>(w + e, y);
+      for (int e0 = 0; e0 < d; e0 += 32 * VEC) {
+        const int e = e0 + lane * VEC;
+        float s = 0.f;
+        if (e < d) {
+          float x[VEC], y[VEC];
+          rowvec::load<T, VEC>(from + e, x);
+          if (GATHER) {
+            rowvec::load<T, VEC>(w + e, y);
 #pragma unroll
-          for (int i = 0; i < VEC; ++i) z = fmaf(x[i], y[i], z);
+            for (int i = 0; i < VEC; ++i) {
+              z = fmaf(x[i], y[i], z);
+              s = fmaf(x[i], y[i], s);
+            }
+          }
+          rowvec::store<T, VEC>(to + e, x);
         }
-        rowvec::store<T, VEC>(to + e, x);
+        if (watch) cut.add(s, e < d, lane);
       }
     };
     if (d % rowvec::Elem<T>::kVec == 0) part(std::integral_constant<int, rowvec::Elem<T>::kVec>());
@@ -241,7 +296,9 @@ __global__ void __launch_bounds__(256) pref_rows_kernel(PrefArgs a, T* dH) {
     if (GATHER) {
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+      const float gain = watch ? cut.gain(d) : 0.f;
       if (lane == 0) {
+        if (watch) a.gain[p] = gain;
         a.yg[p] = v;
         a.zg[p] = z;
         a.ones[p] = 1.f;
@@ -444,6 +501,7 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t R, int32_t P, int elem, bool 
   s.a.zeros = reinterpret_cast<float*>(take(Tn * 4));
   s.a.ones = reinterpret_cast<float*>(take(Tn * 4));
   s.a.zg = reinterpret_cast<float*>(take(Tn * 4));
+  s.a.gain = reinterpret_cast<float*>(take(Tn * 4));
   s.a.r = reinterpret_cast<double*>(take((size_t)(R + 1) * 8));
   s.a.slope = reinterpret_cast<double*>(take((size_t)(P + 1) * 8));
   s.a.partials = reinterpret_cast<double*>(take((size_t)kPairBlocks * kPartialStride * 8));
@@ -612,7 +670,7 @@ int aero_pref_fwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* pc, i
   if (room < aero_distill_fwd_workspace_bytes(T, d, V, 1, 1)) return AERO_ERR_WORKSPACE;
   if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
   AeroListed ex;
-  ex.gain = true;
+  ex.z_gain = c.s.a.gain;
   c.given(ex);
   if ((rc = c.forward(ex, room))) return rc;
   return c.pairs();
@@ -653,7 +711,7 @@ int aero_pref_fwd_bwd(aero_ctx* ctx, const aero_cfg* cfg, const aero_pref_cfg* p
     return AERO_ERR_WORKSPACE;
   if ((rc = aero_check_ctx(ctx)) || (rc = c.gather())) return rc;
   AeroListed ex;
-  ex.gain = true;
+  ex.z_gain = c.s.a.gain;
   c.given(ex);
   if (one_chunk) {
     ex.row_factor = a.row_weights;

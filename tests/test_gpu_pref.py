@@ -340,3 +340,59 @@ def test_infinite_margins(ctx, dtype, sign, smoothing):
             np.array([-first, first - 0.5 * beta * slope, 0.5 * beta * slope])
         assert np.abs(f64(got["coef"]) - want).max() <= 2.0 ** -22
     assert torch.isfinite(dH.float()).all() and torch.isfinite(dW).all()
+
+
+CUTS = ["early", "late", "blocks", "sparse", "whole", "tiny"]
+
+
+@pytest.mark.parametrize("d", [1536, 3584])
+@pytest.mark.parametrize("kind", CUTS)
+def test_sums_of_other_inputs(ctx, kind, d):
+    """The mean error of log-probs where the products are not alike along d: large ones at its start or end, most columns of H zero
+    (one in 16, or 16 in 128) or of 1e-9 of the others, whole numbers, of which nothing is cut off.  A correction may leave a
+    quarter of what the additions lose of dense inputs (test_sums_over_long_rollouts) where they lose as much, and nowhere more than
+    without it; 2e-7 for the mean of 500 roundings of 4e-6 at most."""
+    T, V = 500, 20000
+    g = torch.Generator(device="cuda").manual_seed(d)
+    W = torch.randn(V, d, generator=g, device="cuda") * (1.43 / d) ** 0.5
+    H = torch.randn(T, d, generator=g, device="cuda")
+    k = torch.arange(d, device="cuda")
+    if kind == "whole":
+        W, H = (torch.randint(-3, 4, (n, d), generator=g, device="cuda").float() / s for n, s in ((V, 128), (T, 1)))
+    else:
+        H *= dict(early=(k < 64) * 30.0 + 1, late=(k >= d - 64) * 30.0 + 1, blocks=(k % 128 < 16).float(), sparse=(k % 16 == 0).float(),
+                  tiny=torch.where(k % 128 < 16, 1.0, 1e-9))[kind]
+        H *= d ** 0.5 / H.norm(dim=1, keepdim=True)
+    W, H = W.bfloat16(), H.bfloat16()
+    y = torch.randint(0, V, (T,), generator=g, device="cuda").int()
+    z = H.double() @ W.double().T
+    want = torch.logsumexp(z, 1)
+    mean_z = (torch.softmax(z, 1) * z).sum(1).mean().item()
+    one = torch.ones(1, device="cuda")
+    plain = ctx.distill_fwd(cfg_of("bf16"), H, W, y[:, None].contiguous(), torch.zeros(T, 1, device="cuda"), torch.tensor([0, T], device="cuda"),
+                            one, one.to(torch.uint8))["lse"]
+    out = ctx.pref_fwd(cfg_of("bf16"), B.pref_cfg_default(), H, W, y, torch.tensor([0, T, T], device="cuda"),
+                       torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"))
+    off, without = ((x.double() - want).mean().item() for x in (out["lse"], plain))
+    dense = 0.25 * d / 16 * 1.55e-8 * mean_z if kind in ("early", "late") else abs(without)
+    assert abs(off) <= dense + 2e-7, (off, without)
+
+
+def test_a_policy_against_itself(ctx):
+    """Log-probs of the same weights as reference: margins of zero where they come from this loss's own forward; from aero_logprob_fwd,
+    whose logits keep what the tensor cores' additions cut off, margins of no more than both calls' errors in the log-probs."""
+    T, d, V = 700, 1536, 5000
+    cs = [0, 300, 310, 500, 700]
+    b = batch(T, d, V, cs, [(0, 1), (2, 3), (3, 1)], "bf16", seed=12)
+    cfg, pc = cfg_of("bf16"), B.pref_cfg_default()
+    first = ctx.pref_fwd(cfg, pc, *args(b))
+    again = ctx.pref_fwd(cfg, pc, *args(b), ref_logp=first["logp"])
+    assert not again["margin"].any() and not again["ratio"].any() and abs(again["loss"].item() - np.log(2)) < 1e-7
+    S = float((b["H"].float().abs() @ b["W"].float().abs().T).max())
+    tol = (d / 16 + 2) * 2.0 ** -23 * S + (V / 32 + 64) * 2.0 ** -24 + 2.0 ** -23 * first["logp"].abs().max().item()
+    n = np.array([(b["y"][x:z] >= 0).sum().item() for x, z in zip(cs, cs[1:])])
+    one, dH, dW = ctx.pref_fwd_bwd(cfg, pc, *args(b), ref_logp=first["logp"])
+    assert (np.abs(f64(one["ratio"])) <= 2 * n * tol).all()
+    other = ctx.logprob_fwd(cfg, b["H"], b["W"], b["y"].clamp(min=0))["logp"]
+    got = ctx.pref_fwd(cfg, pc, *args(b), ref_logp=other)
+    assert (np.abs(f64(got["ratio"])) <= 2 * n * tol).all()
