@@ -345,7 +345,9 @@ __global__ void __launch_bounds__(kWarps * 32) adamw_prepare_kernel(PrepareArgs 
 
 // The root of eight values.  Within 2^-100 .. 2^100: one step of the residual form of Newton's iteration from the hardware's
 // reciprocal root (P. Markstein, "Computation of elementary functions on the IBM RISC System/6000 processor", 1990), which gives the
-// same bits as sqrtf there (tested over all values).  Else, zeros among them, sqrtf.
+// same bits as sqrtf there: for every v of two binades, and with them of all, any reciprocal root within the instruction's documented
+// 2^-22.9 leads to the correctly rounded root, but for two v, for which the device's own does (tests/test_adamw_roots.py carries it
+// out; the device is tested on the two at every power of four).  Else, zeros among them, sqrtf.
 __device__ __forceinline__ void roots(const float (&v)[kEach], float (&r)[kEach]) {
   bool plain = true;
 #pragma unroll

@@ -421,3 +421,26 @@ def test_plan_of_overlapping_tensors():
                 [t(base[:50], grads[:50], m=grads[50:]), t(base[50:], grads[50:])]):  # a state that is another tensor's gradient
         with pytest.raises(B.AeroError, match="overlap|twice"):
             B.AdamWPlan(bad)
+
+
+ROOTS = [(1.9692776203155518, 0.1, 1.4792181253433228), (3.7277493476867676, 0.5, 2.730475902557373)]
+
+
+
+@pytest.mark.parametrize("v,beta2,grad", ROOTS)
+def test_roots_of_the_special_values(ctx, v, beta2, grad):
+    """The two mantissas whose root depends on which of the reciprocal roots within the documented bound the instruction gives
+    (tests/test_adamw_roots.py: no other does), at every power of four of the fast form's range: v is (1 - beta2) grad^2 of a first step."""
+    powers = torch.arange(-49, 50, device="cuda").double()
+    g = (grad * torch.exp2(powers)).float()
+    n = g.numel()
+    t = dict(param=torch.zeros(n * 256, device="cuda"), grad=g.repeat_interleave(256), m=torch.zeros(n * 256, dtype=torch.float8_e4m3fn, device="cuda"),
+             v=torch.zeros(n * 256, dtype=torch.uint8, device="cuda"), m_scale=torch.zeros(n, device="cuda"), v_scale=torch.zeros(n, device="cuda"))
+    rest = float(np.float32(1 - beta2))
+    values = ((rest * g.double()).float().double() * g.double()).float()
+    assert torch.equal(values, (v * torch.exp2(2 * powers)).float())
+    ctx.adamw_step(B.adamw_cfg_default(beta2=beta2, lr=0.0), B.AdamWPlan([t]), torch.zeros(1, dtype=torch.int64, device="cuda"))
+    root = torch.sqrt(values.double()).float()                        # (53 bits are enough to round the root of 24 once)
+    want = root.clamp(min=2.0 ** -100) * torch.tensor(1.0 / 496.0, device="cuda")
+    other = torch.nextafter(root, torch.full_like(root, float("inf"))) * torch.tensor(1.0 / 496.0, device="cuda")
+    assert torch.all(want != other) and torch.equal(t["v_scale"], want)
