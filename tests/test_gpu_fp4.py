@@ -210,3 +210,23 @@ def test_scales_that_change_from_slab_to_slab(ctx, T, block):
     for v in range(0, V, 4736):
         part = b[v:v + 4736].double()
         check_product(got[:, v:v + 4736].double(), a.double() @ part.T, a.double().abs() @ part.abs().T, d, torch.float32)
+
+
+@pytest.mark.parametrize("block", [16, 32])
+@pytest.mark.parametrize("out", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T", [1, 7, 61, 130, 700])
+def test_product_of_rows_that_are_no_numbers(ctx, T, block, out):
+    """A NaN or an infinity in a row of tokens or of W: that row's logits are NaN, all others stay what they are."""
+    d, V = 288, 700
+    h, w = values(T, d, torch.bfloat16, 5), values(V, d, torch.bfloat16, 6)
+    cfg = cfg_of("bf16")
+    want = ctx.lmhead_fp4(ctx.quantize_fp4(cfg, h, block=block), ctx.quantize_fp4(cfg, w, block=block), out_dtype=out)
+    rows, cols = sorted({0, T // 2, T - 1}), [0, 130, 255, 699]
+    for i, r in enumerate(rows):
+        h[r, (37 * i) % d] = (float("nan"), float("inf"), -float("inf"))[i]
+    for i, c in enumerate(cols):
+        w[c, (101 * i + 5) % d] = (float("inf"), float("nan"), -float("inf"), float("nan"))[i]
+    got = ctx.lmhead_fp4(ctx.quantize_fp4(cfg, h, block=block), ctx.quantize_fp4(cfg, w, block=block), out_dtype=out)
+    nan = torch.zeros(T, V, dtype=torch.bool, device="cuda")
+    nan[rows], nan[:, cols] = True, True
+    assert torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], want[~nan])
