@@ -638,7 +638,8 @@ int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t*
  * A rollout may be in any number of pairs; the rows of one that is in none are not read.  A pair (-1, -1)
  * is an empty place; one that names any other rollout outside [0,R) raises AERO_ST_BAD_PAIR and does not count.  Empty places
  * have margin 0.  A rollout whose offsets leave [0,T] raises AERO_ST_BAD_OFFSETS and counts as one without tokens; so do all of them
- * where offsets overlap so that they have more than T scored tokens.  Rows that are not scored have logp = lse = 0 and dH = 0.
+ * where offsets overlap so that they have more than T scored tokens (where they overlap and have fewer, dH of a row that two rollouts
+ * hold is that of one of them).  Rows that are not scored have logp = lse = 0 and dH = 0.
  * Inputs   y [T] i32, ref_logp [T] f32 or NULL, cs [R+1] i64, pairs [P,2] i32 (8-byte aligned), pair_weight [P] f32 or NULL.
  * Outputs  logp, lse [T], ratio, coef [R], margin [P] f32; loss [1] f32; metrics [4] f32 or NULL: fraction of the pairs with
  *          r_chosen > r_rejected, mean beta r_chosen, mean beta r_rejected, number of pairs that count; dH [T,d] (cfg->dtype), dW
@@ -646,7 +647,7 @@ int aero_lmhead_q8(aero_ctx* ctx, int64_t T, int32_t d, int32_t V, const int8_t*
  * aero_pref_bwd takes coef and lse from the forward and recomputes the logits (8 d V FLOP per token over the two calls; rollouts
  * whose coef is 0 are left out).  aero_pref_fwd_bwd does not recompute them (6 d V) if the workspace holds all rows in one chunk, since
  * a row's gradient needs the log-probs of all rows of its pairs; else it takes the two calls' passes.  cfg->dtype and d as in
- * aero_distill_fwd; precision as there, with sums over rollouts and pairs in 64 bits; all sums have a fixed order.
+ * aero_distill_fwd, R and P <= 2^30; precision as there, with sums over rollouts and pairs in 64 bits; all sums have a fixed order.
  * logp has no mean error that would add up over a rollout's tokens, as that of the other calls has (5e-6 a token at d = 3584, from the
  * tensor cores' accumulation); a reference of this library is therefore best scored by aero_pref_fwd too (P = 0 pairs would leave all
  * rows out: name each rollout in a pair, with itself if need be).

@@ -492,7 +492,7 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t R, int32_t P, int elem, bool 
   s.a.one = reinterpret_cast<uint8_t*>(take(1));
   s.a.run = reinterpret_cast<int64_t*>(take(16));
   s.a.keep = reinterpret_cast<uint8_t*>(take((size_t)R + 1));
-  s.a.off = reinterpret_cast<int64_t*>(take((size_t)(R + 1) * 8));
+  s.a.off = reinterpret_cast<int64_t*>(take(((size_t)R + 1) * 8));
   s.a.src = reinterpret_cast<int32_t*>(take(Tn * 4));
   s.a.yg = reinterpret_cast<int32_t*>(take(Tn * 4));
   s.a.lseg = reinterpret_cast<float*>(take(Tn * 4));
@@ -502,8 +502,8 @@ Ws carve(void* base, int64_t T, int32_t d, int32_t R, int32_t P, int elem, bool 
   s.a.ones = reinterpret_cast<float*>(take(Tn * 4));
   s.a.zg = reinterpret_cast<float*>(take(Tn * 4));
   s.a.gain = reinterpret_cast<float*>(take(Tn * 4));
-  s.a.r = reinterpret_cast<double*>(take((size_t)(R + 1) * 8));
-  s.a.slope = reinterpret_cast<double*>(take((size_t)(P + 1) * 8));
+  s.a.r = reinterpret_cast<double*>(take(((size_t)R + 1) * 8));
+  s.a.slope = reinterpret_cast<double*>(take(((size_t)P + 1) * 8));
   s.a.partials = reinterpret_cast<double*>(take((size_t)kPairBlocks * kPartialStride * 8));
   s.a.Hg = reinterpret_cast<uint8_t*>(take(rows));
   if (grads) s.a.dHg = reinterpret_cast<uint8_t*>(take(rows));
@@ -519,8 +519,11 @@ int grid_for(long long n, int per, int most) {
   return (int)(blocks < 1 ? 1 : (blocks < most ? blocks : most));
 }
 
+constexpr int32_t kMost = 1 << 30;        // pairs, rollouts: the kernels' indexes step past the last one in 32 bits
+
 int check_pref(const aero_pref_cfg* pc, int32_t P, const int32_t* pairs) {
   if (!pc || P < 0 || (P > 0 && !pairs)) return AERO_ERR_INVALID;
+  if (P > kMost) return AERO_ERR_UNSUPPORTED;
   if (pc->kind != AERO_PREF_LOGISTIC && pc->kind != AERO_PREF_SQUARE && pc->kind != AERO_PREF_HINGE) return AERO_ERR_UNSUPPORTED;
   if (!(fabsf(pc->beta) < INFINITY) || !(fabsf(pc->margin) < INFINITY) || !(pc->label_smoothing >= 0.f && pc->label_smoothing <= 1.f))
     return AERO_ERR_INVALID;
@@ -538,6 +541,7 @@ struct Call {
 
   int check(const void* workspace) {
     if (!cfg || !workspace || s.a.R < 0) return AERO_ERR_INVALID;
+    if (s.a.R > kMost) return AERO_ERR_UNSUPPORTED;
     // (as the calls below check them; H and y are the caller's, the rest stands for what the workspace holds)
     return aero_distill_check(ctx, cfg, s.a.T, s.a.d, s.a.V, s.a.R, 1, s.a.H, W, s.a.y, reinterpret_cast<const float*>(workspace), s.a.cs,
                               reinterpret_cast<const float*>(workspace), static_cast<const uint8_t*>(workspace), workspace);

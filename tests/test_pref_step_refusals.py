@@ -203,3 +203,13 @@ def test_adamw_plan_arrays_that_share_memory():
                           ([a, c], [(0, 1000, 0, "grad"), (500, 600, 1, "grad")]), ([c], [(0, 1000, 0, "grad"), (20, 30, 1, "grad")])):
         with pytest.raises(B.AeroError, match="overlap"):
             check(written, read)
+
+
+def test_more_pairs_or_rollouts_than_the_indexes_hold(lib, fake):
+    """Steps past the last of 2^31 - 1 would wrap; 2^30 is the limit of both.  (The call ends before the sizes are followed anywhere.)"""
+    pc, big = C.byref(B.pref_cfg_default()), (1 << 30) + 1
+    for R, pairs in ((big, 4), (3, big), (2 ** 31 - 1, 2 ** 31 - 1)):
+        assert lib.aero_pref_fwd(fake, cfg(), pc, 40, 64, 10, R, pairs, P, P, P, P, P, P, None, P, P, P, P, P, P, None, P, 1 << 62) == UNSUPPORTED
+        assert lib.aero_pref_fwd_bwd(fake, cfg(), pc, 40, 64, 10, R, pairs, P, P, P, P, P, P, None, P, P, P, P, P, P, None, 1.0, P, P,
+                                     B.AERO_FP32, 0, P, 1 << 62) == UNSUPPORTED
+    assert lib.aero_pref_bwd(fake, cfg(), 40, 64, 10, big, P, P, P, P, P, P, 1.0, P, P, B.AERO_FP32, 0, P, 1 << 62) == UNSUPPORTED
