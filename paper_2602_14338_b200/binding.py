@@ -787,7 +787,8 @@ class Context:
 
     @staticmethod
     def _pref_chunk(T, R, chunk_tokens):
-        # by default all of a batch that fits four waves of token tiles: rows in one chunk save a pass over the logits
+        # by default all of a batch that fits four waves of token tiles: rows in one chunk save a pass over the logits (60000 tokens in one
+        # chunk and in chunks of two waves: d = 1536, V = 151936 64.7 and 79.9 ms with 19 and 13 GB, d = 3584, V = 152064 140 and 184 ms with 20 and 16)
         return chunk_tokens if chunk_tokens is not None else min(T + 128 * (R + 2), 4 * 148 * 128)
 
     def _pref_call(self, cfg, H, W, y, cs, pairs, ref_logp, pair_weight, out):

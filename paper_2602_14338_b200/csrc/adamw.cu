@@ -26,7 +26,8 @@ constexpr int kNormBlocks = 148 * 8;     // of the norm's launch: a record each
 constexpr int kMaxBlocks = 148 * 64;
 // Chunks at most of a call whose step's blocks add the norm's records up themselves: a record each.  (Without / with, bf16 params with
 // fp32 masters, from the host, +-1 us: 60 x 1536 17.4 / 14.3 us, 8 x 98304 21.4 / 18.4, 16 x 98304 25.6 / 22.5, 24 x 98304 = 1152 chunks
-// 29.6 / 26.6, 40 x 98304 33.8 / 33.8; 8 x 2^20, with 592 blocks for the step, 53 / 59.)
+// 29.6 / 26.6, 40 x 98304 33.8 / 33.8; 8 x 2^20, with 592 blocks for the step, 53 / 59; calls in a row, fp32, 1 x 1000 17.3 / 14.8,
+// 60 x 1536 18.3 / 15.6, 24 x 98304 23.7 / 21.1.)
 constexpr int kJoinChunks = kNormBlocks;
 constexpr float kTopM = 448.f, kTopV = 496.f;          // largest values of the two 8-bit formats
 constexpr float kLeast = 0x1p-100f;     // scales are made of at least this: 448 / it stays finite

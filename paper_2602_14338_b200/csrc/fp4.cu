@@ -566,7 +566,9 @@ template <> struct Held<__nv_bfloat16> {
 // use the rows of W that were loaded once: with units of 192 tokens the SMs' reads from L2, 10 TB/s, were the bound (2048
 // tokens of d = 3584, V = 152064 701 us).  The accumulators are emptied into registers as soon as their products are done, rounded there,
 // and stored while the next unit's products run; what is left of the time is the products (96 cycles each, 430 us at the clock that the
-// power allows), that emptying, and the round trips of the scales: 574 us.
+// power allows), that emptying, and the round trips of the scales: 690 us in a row at 1.61 GHz under the power cap, 634 alone, 574 in a row
+// in one run whose clock was not sampled.  Half the scales (block 32: 657 in a row at 1.66 GHz) save 1.6 % of the cycles, so reading them is
+// not what bounds it.
 // A stage, per CTA: codes of 128 rows of W and of its half of each accumulator's tokens, scales of these rows of W, and of the three
 // groups of 128 token rows (both CTAs' tensor cores multiply all columns).
 constexpr int PSTAGES = 4, kPiece = 32, kTokenGroups = kPairT / kTile;
