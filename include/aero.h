@@ -762,7 +762,8 @@ int aero_adamw_states(aero_ctx* ctx, int32_t n_tensors, const aero_adamw_tensor*
  *   block 16: row_scale = the smallest power of two >= max|x_row| / (6 448), at least 2^-126 (a row of zeros: 0); with
  *     x' = x / row_scale, scale = e4m3(max|x'_block| / 6), code = e2m1(x' / scale), 0 where the scale is.
  *   block 32: scale = 2^(floor(log2 max|x_block|) - 2), at least 2^-127; code = e2m1(x / scale).
- *   Rounded to even; values beyond 6 become 6.  A row (block 16) or block (block 32) with a NaN or an infinity gets a NaN scale.
+ *   Rounded to even; values beyond 6 become 6; a value that becomes zero has a zero of either sign.  A row (block 16) or block
+ *   (block 32) with a NaN or an infinity gets a NaN scale.
  * aero_dequantize_fp4: the values, rounded once to out_dtype (AERO_BF16 | AERO_FP32), out [T,d].
  * aero_lmhead_fp4: out[t,v] = sum_k h_tk w_vk of the values, T rows h and V rows w in the same format; sums of exact products in
  *   fp32 on the tensor cores, multiplied by the two rows' scales and rounded once to out_dtype; out [T,V].
